@@ -41,7 +41,8 @@ enum {
     NO_ERR_TIMEOUT = -7        /* a kernel's bounded wait on another workgroup expired; the outputs of that call are invalid */
 };
 
-typedef enum { NO_F32 = 0, NO_BF16 = 1 } no_dtype;
+/* NO_E4M3 (8 bits: sign, 4 exponent, 3 mantissa bits, largest value 448) is a type of rows with a scale each, and only where a function says so. */
+typedef enum { NO_F32 = 0, NO_BF16 = 1, NO_E4M3 = 2 } no_dtype;
 /* Layer form: GraphSAGE-mean (separate self path, two matrices) or GCN-style (Eq. 1 as printed: the aggregate runs
  * over N_in(v) U {v}; Eq. 2 with one matrix). The GCN-style aggregate a_v = r_v (s_v x_v + sum over the sampled row of
  * s_u x_u) comes in the forms Eq. 1 and Table 1 name:
@@ -270,6 +271,102 @@ int32_t no_gcn_layer_fwd(const no_block_view* blk, no_arch form, const void* d_x
 int32_t no_gcn_layer_bwd(const no_block_view* blk, no_arch form, int32_t d_in, const float* d_agg, const float* d_h,
                          const float* d_grad_h, const float* d_w, int32_t d_out, int32_t relu, float* d_gw,
                          float* d_gbias, float* d_grad_x_src, void* d_ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Operators for learned inputs and large answers: table rows by id with their gradient, RMS norm, a loss against a teacher's
+ * top logits, log probabilities of given classes
+ *
+ * What they have in common. Rows are dense in themselves; row strides are in bytes, multiples of the element size and at least a row; any
+ * alignment of a whole element will do. The number of rows is n = *d_n_rows (clamped to [0, n_rows_cap]) where a device scalar is given, else
+ * n_rows_cap; rows from n on are neither read nor written, and with n_rows_cap == 0 the row arrays may be NULL. Sums, norms and softmax statistics are
+ * fp32 or wider, results are rounded once, to nearest even. Reductions run in a fixed order. Offsets are 64 bits wide. A call that
+ * takes a workspace may write all of it and leaves nothing there that has to survive; calls that overlap in time need one each. Workspaces are
+ * 16-byte aligned. The ..._ws_bytes functions give 0 for sizes that the call refuses. Errors: NO_ERR_INVALID_ARG (NULL, sizes, strides,
+ * alignment, types), NO_ERR_CAPACITY (workspace too small), NO_ERR_UNSUPPORTED (a width beyond the limits below), NO_ERR_HIP.
+ * ---------------------------------------------------------------------------------------- */
+
+enum {
+    NO_MAX_NORM_DIM = 65536,       /* widest row of no_rmsnorm_* */
+    NO_MAX_CLASSES = 1 << 22,      /* widest row of no_distill_* and no_logprobs_* */
+    NO_MAX_TEACHER = 256,          /* teacher entries a row */
+    NO_MAX_ALTERNATIVES = 64       /* alternatives a row */
+};
+
+/* Table rows by id: d_out[i, :] = scale * d_row_scale[id] * d_table[id, :] with id = d_ids[i], i < n; zeros where id lies outside [0, n_rows)
+ * (padding, -1 for instance). dt: NO_F32, NO_BF16, NO_E4M3; dt_out: NO_F32, NO_BF16. d_row_scale fp32 [n_rows] or NULL (1).
+ * The product of the two scales is rounded to fp32, and so is its product with an element, before that is rounded to dt_out. */
+int32_t no_embed_fwd(const void* d_table, no_dtype dt, int64_t n_rows, int32_t dim, int64_t table_stride_bytes, const float* d_row_scale,
+                     const int32_t* d_ids, const int32_t* d_n_ids, int32_t n_ids_cap, float scale, void* d_out, no_dtype dt_out,
+                     int64_t out_stride_bytes, void* stream);
+
+/* Its gradient: d_grad_table[v, :] = scale * sum of d_grad_out[i, :] over the i < n with d_ids[i] == v, fp32; rows that no id names become zeros,
+ * or, with accumulate != 0, the sum is added to what is there and other rows are left alone. (With accumulate, scale = -learning rate
+ * times the forward scale and d_grad_table an fp32 table itself, the call is the update of plain SGD.) Ids outside [0, n_rows) add nothing.
+ * dt: type of d_grad_out, NO_F32 or NO_BF16. The order of a row's sum is that of the positions i, in runs whose
+ * length depends on the sizes alone: the same ids give the same bits. */
+size_t no_embed_ws_bytes(int32_t n_ids_cap, int32_t dim);
+int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t grad_stride_bytes, const int32_t* d_ids, const int32_t* d_n_ids,
+                     int32_t n_ids_cap, float scale, int32_t accumulate, float* d_grad_table, int64_t n_rows, int32_t dim,
+                     int64_t table_stride_bytes, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Root-mean-square norm of rows: s = d_x + d_residual rounded to dt (s = d_x where d_residual is NULL), rstd = 1 / sqrt(mean of s^2 + eps),
+ * y = s * rstd * d_weight (1 where d_weight is NULL). dt: type of d_x, d_residual and d_sum: NO_F32 or NO_BF16.
+ * Outputs: d_sum (NULL: not stored) takes s; d_rstd fp32 [n] (may be NULL); d_y of dt_y: NO_F32, NO_BF16, or NO_E4M3, then
+ * d_row_scale fp32 [n] takes max(max |y|, 2^-100) / 448 of each row and d_y holds y divided by it (NULL otherwise). d_sum may be d_x or d_residual
+ * itself, and so may d_y where dt_y == dt (same address and stride; two outputs never share an array); no other overlap. A row whose
+ * squares leave fp32 (|s| beyond 1.8e19, infinities, NaN) has rstd 0 or NaN and y = s * rstd * weight by that; in NO_E4M3 all of it is NaN, its scale too. */
+int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_residual, int64_t residual_stride_bytes,
+                       const float* d_weight, float eps, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t dim, void* d_sum,
+                       int64_t sum_stride_bytes, void* d_y, no_dtype dt_y, int64_t y_stride_bytes, float* d_row_scale, float* d_rstd,
+                       void* stream);
+
+/* Its gradients: with u = d_s * d_rstd and wg = d_weight * d_grad_y: d_grad_x = d_rstd (wg - u * mean(wg * u)) + d_grad_sum, the gradient of x and
+ * of the residual alike (d_grad_sum: the gradient that reaches s itself, NULL: none); d_grad_weight fp32 [dim] = sum over the rows of d_grad_y * u
+ * (overwritten; NULL: not computed). d_s is what the forward pass stored in d_sum (or its d_x). dt: type of d_s, d_grad_y, d_grad_sum and
+ * d_grad_x. d_grad_x may be d_grad_y, d_grad_sum or d_s itself (same address and stride). */
+size_t no_rmsnorm_ws_bytes(int32_t n_rows_cap, int32_t dim);
+int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride_bytes, const float* d_weight, const float* d_rstd,
+                       const void* d_grad_y, int64_t grad_y_stride_bytes, const void* d_grad_sum, int64_t grad_sum_stride_bytes,
+                       const int32_t* d_n_rows, int32_t n_rows_cap, int32_t dim, void* d_grad_x, int64_t grad_x_stride_bytes,
+                       float* d_grad_weight, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Distillation from a teacher's top logits. A row has k entries (d_teacher_ids int32 [n, k], d_teacher_logits fp32 [n, k], dense); an entry whose id
+ * lies outside [0, n_classes) is left out. p = softmax(teacher logits / T) over the row's entries (an id may stand twice: its shares add up),
+ * log q = z / T - lse, lse = log sum exp(z / T) over all classes of the student's row d_z (dt: NO_F32 or NO_BF16), and with the row's weight w
+ * (d_row_weight fp32 [n], NULL: 1):
+ *   d_loss[i] = w T^2 sum p (log p - log q)        d_grad_z[i, c] = w T (q_c - p_c), of type dt
+ * The factor T^2 keeps the gradient's size as T grows. A row of weight 0 has loss 0 and gradient 0 whatever it holds, and so has a row without
+ * entries above -inf. A logit of -inf takes part in nothing (q = 0): the loss is +inf where the teacher gives it a share. +inf or NaN in a row
+ * make the row's results NaN.
+ * no_distill_fwd stores d_loss and d_lse (fp32 [n]); no_distill_bwd takes that d_lse (an upstream gradient of the losses goes into the
+ * weights); no_distill_fwd_bwd makes all of it at once (d_lse may be NULL). d_grad_z may be d_z itself (same stride). */
+size_t no_distill_ws_bytes(int32_t n_rows_cap, int32_t n_classes);
+int32_t no_distill_fwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
+                       const int32_t* d_teacher_ids, const float* d_teacher_logits, int32_t k, float temperature, const float* d_row_weight,
+                       float* d_loss, float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
+int32_t no_distill_bwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
+                       const int32_t* d_teacher_ids, const float* d_teacher_logits, int32_t k, float temperature, const float* d_row_weight,
+                       const float* d_lse, void* d_grad_z, int64_t grad_stride_bytes, void* stream);
+int32_t no_distill_fwd_bwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap,
+                           int32_t n_classes, const int32_t* d_teacher_ids, const float* d_teacher_logits, int32_t k, float temperature,
+                           const float* d_row_weight, float* d_loss, float* d_lse, void* d_grad_z, int64_t grad_stride_bytes, void* d_ws,
+                           size_t ws_bytes, void* stream);
+
+/* Log probabilities of given classes, with log p = z / T - lse, lse = log sum exp(z / T) over the row:
+ *   d_logprob[i] = log p of class d_tokens[i] (0 where that lies outside [0, n_classes): a position without an answer),
+ *   d_entropy[i] = -sum p log p, d_lse[i]; all fp32 [n];
+ *   d_top_ids int32 [n, k] / d_top_logprobs fp32 [n, k] (dense; both NULL with k == 0): the k largest logits in descending order, equal ones by
+ *   ascending class. Logits of -inf are no alternatives: places left over hold -1 and -inf.
+ * A row of -inf alone has lse = -inf, log p = -inf and entropy 0; +inf or NaN in a row make its numbers NaN and its alternatives -1.
+ * Backward: d_grad_z[i, c] = (g_lp ([c == token] - p_c) - g_H p_c (log p_c + H)) / T with the forward pass's d_lse and d_entropy and the gradients
+ * d_grad_logprob, d_grad_entropy (either may be NULL: 0); a position without an answer takes no g_lp. d_grad_z (of dt) may be d_z itself. */
+size_t no_logprobs_ws_bytes(int32_t n_rows_cap, int32_t n_classes, int32_t k);
+int32_t no_logprobs_fwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
+                        const int32_t* d_tokens, float temperature, float* d_logprob, float* d_entropy, float* d_lse, int32_t k,
+                        int32_t* d_top_ids, float* d_top_logprobs, void* d_ws, size_t ws_bytes, void* stream);
+int32_t no_logprobs_bwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
+                        const int32_t* d_tokens, float temperature, const float* d_lse, const float* d_entropy,
+                        const float* d_grad_logprob, const float* d_grad_entropy, void* d_grad_z, int64_t grad_stride_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
  * Whole step (loop body of Algorithm 1 with plain SGD, plus hot-embedding reuse)

@@ -17,7 +17,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libneutronorch.so")
 
-NO_F32, NO_BF16 = 0, 1
+NO_F32, NO_BF16, NO_E4M3 = 0, 1, 2
 NO_ARCH_SAGE_MEAN, NO_ARCH_GCN, NO_ARCH_GCN_SUM, NO_ARCH_GCN_SYM = 0, 1, 2, 3
 ARCH_OF_NAME = {"sage": NO_ARCH_SAGE_MEAN, "gcn": NO_ARCH_GCN, "gcn_sum": NO_ARCH_GCN_SUM, "gcn_sym": NO_ARCH_GCN_SYM}
 NO_CSR_INPUT_ON_DEVICE, NO_CSR_IDS_64, NO_CSR_SYMMETRISE, NO_CSR_DEDUP = 1, 2, 4, 8
@@ -76,6 +76,19 @@ _SIGNATURES = {
     "no_sage_layer_bwd": (_I32, [_P, _P, _I32, _I32, _P, _P, _P, _P, _P, _I32, _I32, _P, _P, _P, _P, _P,
                                  C.c_size_t, _P]),
     "no_sage_layer_bwd_static": (_I32, [_P, _P, _I32, _I32, _P, _P, _P, _P, _P, _I32, _I32, _P, _P, _P, _P, _P]),
+    "no_embed_fwd": (_I32, [_P, _I32, _I64, _I32, _I64, _P, _P, _P, _I32, C.c_float, _P, _I32, _I64, _P]),
+    "no_embed_ws_bytes": (C.c_size_t, [_I32, _I32]),
+    "no_embed_bwd": (_I32, [_P, _I32, _I64, _P, _P, _I32, C.c_float, _I32, _P, _I64, _I32, _I64, _P, C.c_size_t, _P]),
+    "no_rmsnorm_fwd": (_I32, [_P, _I32, _I64, _P, _I64, _P, C.c_float, _P, _I32, _I32, _P, _I64, _P, _I32, _I64, _P, _P, _P]),
+    "no_rmsnorm_ws_bytes": (C.c_size_t, [_I32, _I32]),
+    "no_rmsnorm_bwd": (_I32, [_P, _I32, _I64, _P, _P, _P, _I64, _P, _I64, _P, _I32, _I32, _P, _I64, _P, _P, C.c_size_t, _P]),
+    "no_distill_ws_bytes": (C.c_size_t, [_I32, _I32]),
+    "no_distill_fwd": (_I32, [_P, _I32, _I64, _P, _I32, _I32, _P, _P, _I32, C.c_float, _P, _P, _P, _P, C.c_size_t, _P]),
+    "no_distill_bwd": (_I32, [_P, _I32, _I64, _P, _I32, _I32, _P, _P, _I32, C.c_float, _P, _P, _P, _I64, _P]),
+    "no_distill_fwd_bwd": (_I32, [_P, _I32, _I64, _P, _I32, _I32, _P, _P, _I32, C.c_float, _P, _P, _P, _P, _I64, _P, C.c_size_t, _P]),
+    "no_logprobs_ws_bytes": (C.c_size_t, [_I32, _I32, _I32]),
+    "no_logprobs_fwd": (_I32, [_P, _I32, _I64, _P, _I32, _I32, _P, C.c_float, _P, _P, _P, _I32, _P, _P, _P, C.c_size_t, _P]),
+    "no_logprobs_bwd": (_I32, [_P, _I32, _I64, _P, _I32, _I32, _P, C.c_float, _P, _P, _P, _P, _P, _I64, _P]),
     "no_model_create": (_I32, [_P, _I32, _P, _I32, _P, _I32, _P]),
     "no_model_params": (_I32, [_P, _I32, _P, _P, _P]),
     "no_model_grads": (_I32, [_P, _I32, _P, _P, _P]),
@@ -436,6 +449,158 @@ def no_gcn_layer_bwd(blk: no_block_view, agg: torch.Tensor, h: torch.Tensor, gra
     _check(lib().no_gcn_layer_bwd(C.byref(blk), form, d_in, agg.data_ptr(), h.data_ptr(), grad_h.data_ptr(), w.data_ptr(), d_out,
                                   1 if relu else 0, gw.data_ptr(), gbias.data_ptr(), _ptr(grad_x_src), ws.data_ptr(),
                                   ws.numel() * ws.element_size(), _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------ learned inputs, large answers
+
+NO_MAX_NORM_DIM, NO_MAX_CLASSES, NO_MAX_TEACHER, NO_MAX_ALTERNATIVES = 65536, 1 << 22, 256, 64
+_OP_DTYPES = {torch.float32: NO_F32, torch.bfloat16: NO_BF16, torch.float8_e4m3fn: NO_E4M3}
+
+
+def _rows(t: Optional[torch.Tensor], n: int, dim: int, dtype: Optional[torch.dtype] = None):
+    """(address, stride in bytes) of a row matrix [n, dim] whose rows are dense; (None, 0) of None."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.dim() == 2 and t.shape[0] == n and t.shape[1] == dim, "a CUDA tensor [%d, %d] is needed, got %s" % (n, dim, tuple(t.shape))
+    assert t.stride(1) == 1 or dim == 1, "rows must be dense"
+    assert dtype is None or t.dtype == dtype, "%s is needed, got %s" % (dtype, t.dtype)
+    es = t.element_size()
+    return t.data_ptr(), t.stride(0) * es if n > 1 else max(t.stride(0), dim) * es     # (a single row's stride says nothing)
+
+
+def _vec(t: Optional[torch.Tensor], n: int, dtype: torch.dtype = torch.float32) -> Optional[int]:
+    """Address of a dense array of n values; None of None."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == dtype and t.numel() == n and t.is_contiguous(), "a dense CUDA tensor of %d %s values is needed" % (n, dtype)
+    return t.data_ptr()
+
+
+def _count(n: Optional[torch.Tensor]) -> Optional[int]:
+    return _vec(n, 1, torch.int32)
+
+
+def _ws(ws: torch.Tensor):
+    assert ws.is_cuda and ws.is_contiguous()
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def no_embed_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+                 row_scale: Optional[torch.Tensor] = None, n_ids: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[i,:] = scale * row_scale[ids[i]] * table[ids[i],:], zeros for ids outside the table. table: float32, bfloat16 or
+    float8_e4m3fn; out: float32 or bfloat16; n_ids (1-element int32 CUDA tensor) limits the rows written."""
+    v, dim = table.shape
+    n = ids.numel()
+    (pt, st), (po, so) = _rows(table, v, dim), _rows(out, n, dim)
+    _check(lib().no_embed_fwd(pt, _OP_DTYPES.get(table.dtype, -1), v, dim, st, _vec(row_scale, v), _vec(ids, n, torch.int32),
+                              _count(n_ids), n, scale, po, _OP_DTYPES.get(out.dtype, -1), so, _stream(stream)))
+    return out
+
+
+def no_embed_ws_bytes(n_ids_cap: int, dim: int) -> int:
+    return int(lib().no_embed_ws_bytes(n_ids_cap, dim))
+
+
+def no_embed_bwd(grad_out: torch.Tensor, ids: torch.Tensor, grad_table: torch.Tensor, ws: torch.Tensor, scale: float = 1.0,
+                 accumulate: bool = False, n_ids: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """grad_table[v,:] (+)= scale * the sum of grad_out[i,:] over ids[i] == v; without accumulate every row is written."""
+    v, dim = grad_table.shape
+    n = ids.numel()
+    (pg, sg), (pt, st), (pw, bw) = _rows(grad_out, n, dim), _rows(grad_table, v, dim, torch.float32), _ws(ws)
+    _check(lib().no_embed_bwd(pg, _OP_DTYPES.get(grad_out.dtype, -1), sg, _vec(ids, n, torch.int32), _count(n_ids), n, scale,
+                              1 if accumulate else 0, pt, v, dim, st, pw, bw, _stream(stream)))
+    return grad_table
+
+
+def no_rmsnorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, y: torch.Tensor,
+                   residual: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
+                   row_scale: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                   n_rows: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """s = x + residual (rounded to x's type, stored in sum_out), y = s * rstd * weight in y's type: float32, bfloat16, or
+    float8_e4m3fn with the rows' scales in row_scale."""
+    n, dim = x.shape
+    (px, sx), (pr, sr), (ps, ss), (py, sy) = _rows(x, n, dim), _rows(residual, n, dim, x.dtype), _rows(sum_out, n, dim, x.dtype), _rows(y, n, dim)
+    _check(lib().no_rmsnorm_fwd(px, _OP_DTYPES.get(x.dtype, -1), sx, pr, sr, _vec(weight, dim), eps, _count(n_rows), n, dim, ps, ss,
+                                py, _OP_DTYPES.get(y.dtype, -1), sy, _vec(row_scale, n), _vec(rstd, n), _stream(stream)))
+    return y
+
+
+def no_rmsnorm_ws_bytes(n_rows_cap: int, dim: int) -> int:
+    return int(lib().no_rmsnorm_ws_bytes(n_rows_cap, dim))
+
+
+def no_rmsnorm_bwd(s: torch.Tensor, weight: Optional[torch.Tensor], rstd: torch.Tensor, grad_y: torch.Tensor, grad_x: torch.Tensor,
+                   grad_weight: Optional[torch.Tensor], ws: torch.Tensor, grad_sum: Optional[torch.Tensor] = None,
+                   n_rows: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of no_rmsnorm_fwd: grad_x (of x and of the residual alike, grad_sum added) and grad_weight."""
+    n, dim = s.shape
+    (ps, ss), (pg, sg), (pa, sa) = _rows(s, n, dim), _rows(grad_y, n, dim, s.dtype), _rows(grad_sum, n, dim, s.dtype)
+    (px, sx), (pw, bw) = _rows(grad_x, n, dim, s.dtype), _ws(ws)
+    _check(lib().no_rmsnorm_bwd(ps, _OP_DTYPES.get(s.dtype, -1), ss, _vec(weight, dim), _vec(rstd, n), pg, sg, pa, sa, _count(n_rows), n,
+                                dim, px, sx, _vec(grad_weight, dim), pw, bw, _stream(stream)))
+
+
+def _teacher(z: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor, row_weight: Optional[torch.Tensor], n_rows):
+    n, c = z.shape
+    k = ids.shape[1]
+    assert ids.shape == logits.shape and ids.shape[0] == n
+    pz, sz = _rows(z, n, c)
+    return (pz, _OP_DTYPES.get(z.dtype, -1), sz, _count(n_rows), n, c, _vec(ids, n * k, torch.int32), _vec(logits, n * k), k), _vec(row_weight, n)
+
+
+def no_distill_ws_bytes(n_rows_cap: int, n_classes: int) -> int:
+    return int(lib().no_distill_ws_bytes(n_rows_cap, n_classes))
+
+
+def no_distill_fwd(z: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, temperature: float,
+                   row_weight: Optional[torch.Tensor], loss: torch.Tensor, lse: torch.Tensor, ws: torch.Tensor, n_rows=None, stream=None):
+    """Per-row loss of the logits z against the teacher's k entries (ids outside the classes are left out), and the rows' lse."""
+    args, w = _teacher(z, teacher_ids, teacher_logits, row_weight, n_rows)
+    _check(lib().no_distill_fwd(*args, temperature, w, _vec(loss, z.shape[0]), _vec(lse, z.shape[0]), *_ws(ws), _stream(stream)))
+
+
+def no_distill_bwd(z: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, temperature: float,
+                   row_weight: Optional[torch.Tensor], lse: torch.Tensor, grad_z: torch.Tensor, n_rows=None, stream=None):
+    """grad_z = row_weight * T * (softmax(z / T) - teacher's shares), from the forward pass's lse."""
+    args, w = _teacher(z, teacher_ids, teacher_logits, row_weight, n_rows)
+    pg, sg = _rows(grad_z, *z.shape, z.dtype)
+    _check(lib().no_distill_bwd(*args, temperature, w, _vec(lse, z.shape[0]), pg, sg, _stream(stream)))
+
+
+def no_distill_fwd_bwd(z: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, temperature: float,
+                       row_weight: Optional[torch.Tensor], loss: torch.Tensor, lse: Optional[torch.Tensor], grad_z: torch.Tensor,
+                       ws: torch.Tensor, n_rows=None, stream=None):
+    """Loss and gradient in one call (the row weights are known before it)."""
+    args, w = _teacher(z, teacher_ids, teacher_logits, row_weight, n_rows)
+    pg, sg = _rows(grad_z, *z.shape, z.dtype)
+    _check(lib().no_distill_fwd_bwd(*args, temperature, w, _vec(loss, z.shape[0]), _vec(lse, z.shape[0]), pg, sg, *_ws(ws), _stream(stream)))
+
+
+def no_logprobs_ws_bytes(n_rows_cap: int, n_classes: int, k: int) -> int:
+    return int(lib().no_logprobs_ws_bytes(n_rows_cap, n_classes, k))
+
+
+def no_logprobs_fwd(z: torch.Tensor, tokens: torch.Tensor, temperature: float, logprob: torch.Tensor, entropy: torch.Tensor,
+                    lse: torch.Tensor, ws: torch.Tensor, top_ids: Optional[torch.Tensor] = None,
+                    top_logprobs: Optional[torch.Tensor] = None, n_rows=None, stream=None):
+    """Log probability of tokens[i] in row i of the logits, the row's entropy and lse, and its largest alternatives."""
+    n, c = z.shape
+    k = 0 if top_ids is None else top_ids.shape[1]
+    assert (top_ids is None) == (top_logprobs is None) and (top_ids is None or tuple(top_ids.shape) == tuple(top_logprobs.shape) == (n, k))
+    pz, sz = _rows(z, n, c)
+    _check(lib().no_logprobs_fwd(pz, _OP_DTYPES.get(z.dtype, -1), sz, _count(n_rows), n, c, _vec(tokens, n, torch.int32), temperature,
+                                 _vec(logprob, n), _vec(entropy, n), _vec(lse, n), k, _vec(top_ids, n * k, torch.int32),
+                                 _vec(top_logprobs, n * k), *_ws(ws), _stream(stream)))
+
+
+def no_logprobs_bwd(z: torch.Tensor, tokens: torch.Tensor, temperature: float, lse: torch.Tensor, entropy: torch.Tensor,
+                    grad_logprob: Optional[torch.Tensor], grad_entropy: Optional[torch.Tensor], grad_z: torch.Tensor, n_rows=None,
+                    stream=None):
+    """Gradient of the log probabilities and entropies with respect to the logits."""
+    n, c = z.shape
+    (pz, sz), (pg, sg) = _rows(z, n, c), _rows(grad_z, n, c, z.dtype)
+    _check(lib().no_logprobs_bwd(pz, _OP_DTYPES.get(z.dtype, -1), sz, _count(n_rows), n, c, _vec(tokens, n, torch.int32), temperature,
+                                 _vec(lse, n), _vec(entropy, n), _vec(grad_logprob, n), _vec(grad_entropy, n), pg, sg, _stream(stream)))
 
 
 # ------------------------------------------------------------------------------------------ model / step

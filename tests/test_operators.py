@@ -1,0 +1,784 @@
+"""The operators for learned inputs and large answers (rows of a table by id and their gradient, RMS norm, distillation loss, log
+probabilities) against their formulas in 64 bits, element by element.
+
+u = 2^-24 is the unit roundoff of fp32 and `half(t)` half a step of an output type, relative. Bounds count roundings: a sum whose longest
+chain of additions has k terms is off by at most (k + the depth of the tree above) u of the sum of magnitudes; exp(x) of an x that is off by a is off by a,
+relatively. Tensors stand in wider arrays filled with a mark, so that a write beside a row shows."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TINY = 1e-37            # results below the normal range may be flushed
+MARK = 77.0
+F32, BF16, E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+NAN, INF = float("nan"), float("inf")
+
+
+def nb():
+    from paper_2311_13225_amd import binding
+    return binding
+
+
+def half(dtype):
+    return 0.0 if dtype == F32 else torch.finfo(dtype).eps / 2
+
+
+def rng(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def randn(shape, gen, dtype=F32, spread=1.0):
+    return (torch.randn(shape, generator=gen, device="cuda") * spread).to(dtype)
+
+
+class Rows:
+    """A row matrix inside a marked array: `pad` elements between rows, `off` in front."""
+
+    def __init__(self, n, dim, dtype, pad=0, off=0, like=None):
+        self.n, self.dim, self.pad, self.off = n, dim, pad, off
+        self.base = torch.full((off + (n + 1) * (dim + pad),), MARK, device="cuda").to(dtype)
+        self.t = self.base[off:off + n * (dim + pad)].view(n, dim + pad)[:, :dim]
+        if like is not None:
+            self.t.copy_(like)
+
+    def untouched(self, rows=None):
+        """Whether everything beside rows [0, rows) still holds the mark."""
+        rows = self.n if rows is None else rows
+        mark = torch.tensor(MARK).to(self.base.dtype).item()       # (as its type holds it)
+        b = self.base.clone().float()
+        b[self.off:self.off + self.n * (self.dim + self.pad)].view(self.n, self.dim + self.pad)[:rows, :self.dim] = mark
+        return bool((b == mark).all())
+
+
+def close(got, ref, tol, what=""):
+    got, ref = got.double(), ref.double()
+    assert got.shape == ref.shape, (what, got.shape, ref.shape)
+    if ref.numel() == 0:
+        return
+    same = (got == ref) | (got.isnan() & ref.isnan())
+    err = (got - ref).abs()
+    tol = torch.as_tensor(tol, device=ref.device, dtype=torch.float64).expand_as(ref)
+    bad = ~(same | (err <= tol))
+    assert not bad.any(), "%s: %d of %d outside, first at %s: got %r, want %r, tolerance %.3g" % (
+        what, int(bad.sum()), ref.numel(), bad.nonzero()[0].tolist(), got[bad][0].item(), ref[bad][0].item(), tol[bad][0].item())
+
+
+def count(n):
+    return torch.tensor([n], dtype=torch.int32, device="cuda")
+
+
+def ws_of(size):
+    assert size > 0
+    return torch.full((size,), 0xA5, dtype=torch.uint8, device="cuda")
+
+
+# ------------------------------------------------------------------------------------------------------- embed
+
+def embed_ref(table, ids, scale, row_scale, out_dtype):
+    """The fp32 operations that the definition names: equal to the last bit."""
+    v = table.shape[0]
+    inside = (ids >= 0) & (ids < v)
+    at = torch.where(inside, ids, 0).long()
+    by = torch.full((ids.numel(),), scale, device="cuda", dtype=F32)
+    if row_scale is not None:
+        by = by * row_scale[at]
+    rows = table.view(torch.uint8)[at].view(E4M3).float() if table.dtype == E4M3 else table[at].float()
+    return torch.where(inside[:, None], rows * by[:, None], 0.0).to(out_dtype)
+
+
+@pytest.mark.parametrize("n,v,dim,pad,off", [(1, 1, 1, 0, 0), (1, 10, 64, 0, 0), (3, 7, 5, 3, 1), (63, 100, 100, 0, 0), (64, 50, 129, 1, 3),
+                                             (777, 1000, 602, 0, 0), (1000, 333, 256, 8, 8), (5, 9, 4099, 0, 1), (20_000, 5000, 16, 0, 0),
+                                             (70_001, 40, 8, 0, 0), (257, 3000, 2048, 16, 0)])
+@pytest.mark.parametrize("dt", [F32, BF16, E4M3], ids=["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("dt_out", [F32, BF16], ids=["to_f32", "to_bf16"])
+def test_embed_fwd(n, v, dim, pad, off, dt, dt_out):
+    g = rng(n + dim)
+    table = Rows(v, dim, dt, pad, off, randn((v, dim), g, F32, 3.0).to(dt))
+    row_scale = torch.rand((v,), generator=g, device="cuda") + 0.5 if dt == E4M3 or n % 2 else None
+    ids = torch.randint(-2, v + 2, (n,), generator=g, device="cuda", dtype=torch.int32)
+    out = Rows(n, dim, dt_out, pad, off)
+    nb().no_embed_fwd(table.t, ids, out.t, scale=1.7, row_scale=row_scale)
+    assert torch.equal(out.t, embed_ref(table.t.contiguous(), ids, 1.7, row_scale, dt_out))
+    assert out.untouched()
+
+
+def test_embed_fwd_special_values_and_count():
+    b = nb()
+    table = torch.tensor([[INF, -INF, NAN, 0.0, -0.0, 1e-40, 3e38, 1.0]], device="cuda")
+    out = Rows(4, 8, F32)
+    b.no_embed_fwd(table, torch.tensor([0, -1, 0, 0], dtype=torch.int32, device="cuda"), out.t, scale=2.0, n_ids=count(3))
+    want = table.cpu() * 2.0
+    got = out.t.cpu()
+    assert torch.equal(got[0].nan_to_num(7.5), want[0].nan_to_num(7.5)) and got[0, 2].isnan() and math.copysign(1.0, got[0, 4]) == -1.0
+    assert (got[1] == 0).all() and torch.equal(got[2].nan_to_num(7.5), got[0].nan_to_num(7.5))
+    assert out.untouched(rows=3)
+    b.no_embed_fwd(table, torch.zeros(4, dtype=torch.int32, device="cuda"), out.t, n_ids=count(0))
+    assert out.untouched(rows=3)
+    b.no_embed_fwd(table, torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty((0, 8), device="cuda"))
+
+
+def test_embed_fwd_far_rows():
+    """Rows whose byte offset passes 2^32, 8-bit values and their scales."""
+    v, dim = 4_400_000, 1024
+    table = torch.empty((v, dim), dtype=torch.uint8, device="cuda")
+    table.random_(0, 126, generator=rng(1))
+    ids = torch.tensor([0, v - 1, 4_194_304, 4_194_303, 2_097_152, v], dtype=torch.int32, device="cuda")
+    scale = torch.rand((v,), device="cuda", generator=rng(2))
+    out = torch.empty((6, dim), dtype=F32, device="cuda")
+    nb().no_embed_fwd(table.view(E4M3), ids, out, scale=0.5, row_scale=scale)
+    assert torch.equal(out, embed_ref(table.view(E4M3), ids, 0.5, scale, F32))
+
+
+def embed_grad_ref(grad, ids, v, scale):
+    inside = ((ids >= 0) & (ids < v)).nonzero()[:, 0]
+    at, g = ids[inside].long(), grad[inside].double()
+    z = lambda: torch.zeros((v, grad.shape[1]), dtype=torch.float64, device="cuda")  # noqa: E731
+    n = torch.zeros((v,), dtype=torch.float64, device="cuda").index_add_(0, at, torch.ones_like(at, dtype=torch.float64))
+    return scale * z().index_add_(0, at, g), abs(scale) * z().index_add_(0, at, g.abs()), n
+
+
+@pytest.mark.parametrize("n,v,dim,pad,off,popular", [
+    (1, 1, 1, 0, 0, 0.0), (1, 5, 64, 0, 0, 0.0), (2, 3, 100, 1, 1, 1.0), (33, 10, 7, 0, 0, 0.5), (64, 1000, 256, 0, 0, 0.0), (777, 1000, 100, 4, 0, 0.3),
+    (1000, 4, 33, 0, 3, 0.2), (4096, 1, 16, 0, 0, 0.0), (4097, 70_000, 130, 2, 1, 0.7), (8193, 300, 64, 0, 0, 0.9), (16_385, 900, 512, 0, 0, 0.5),
+    (40_000, 131_072, 48, 0, 0, 0.4), (100_003, 20_000, 24, 0, 0, 0.95), (300_000, 2, 5, 0, 0, 0.0), (70_000, 100_000, 4, 0, 0, 0.0), (65, 9, 8200, 0, 0, 0.8)])
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_embed_bwd(n, v, dim, pad, off, popular, dt, accumulate):
+    """`popular`: share of the ids that name one row."""
+    b, g = nb(), rng(n + dim)
+    grad = Rows(n, dim, dt, pad, off, randn((n, dim), g, dt))
+    ids = torch.randint(-2, v + 2, (n,), generator=g, device="cuda", dtype=torch.int32)
+    ids[torch.rand((n,), generator=g, device="cuda") < popular] = v // 2
+    start = randn((v, dim), g)
+    table = Rows(v, dim, F32, pad, off, start)
+    ws = ws_of(b.no_embed_ws_bytes(n, dim))
+    b.no_embed_bwd(grad.t, ids, table.t, ws, scale=-0.37, accumulate=accumulate)
+    total, size, n_of = embed_grad_ref(grad.t, ids, v, -0.37)
+    # scale is rounded to fp32; a row's sum of c terms: c - 1 additions in any order, the product, the last addition
+    tol = (n_of[:, None] + 3) * U * size
+    if accumulate:
+        ref = start.double() + total
+        close(table.t, ref, tol + U * (ref.abs() + tol), "table")
+        assert torch.equal(table.t[n_of == 0], start[n_of == 0])
+    else:
+        close(table.t, total, tol + TINY, "grad_table")
+        assert (table.t[n_of == 0] == 0).all()
+    assert table.untouched()
+    first = table.t.clone()
+    table.t.copy_(start)
+    ws.fill_(0x3C)
+    b.no_embed_bwd(grad.t, ids, table.t, ws, scale=-0.37, accumulate=accumulate)
+    assert torch.equal(first, table.t)                  # the same bits, whatever the workspace held
+
+
+def test_embed_bwd_counts_and_empty():
+    b = nb()
+    for n, here in ((50, 0), (50, 1), (50, 49), (5000, 37), (20_000, 19_999), (70_000, 1000)):
+        g = rng(n)
+        grad = randn((n, 20), g)
+        grad[here:] = NAN                                # rows that are not there are not read into anything
+        ids = torch.randint(0, 30, (n,), generator=g, device="cuda", dtype=torch.int32)
+        table = torch.full((30, 20), MARK, device="cuda")
+        b.no_embed_bwd(grad, ids, table, ws_of(b.no_embed_ws_bytes(n, 20)), n_ids=count(here))
+        total, size, n_of = embed_grad_ref(grad[:here], ids[:here], 30, 1.0)
+        close(table, total, (n_of[:, None] + 3) * U * size)
+    table = torch.full((30, 20), MARK, device="cuda")
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    b.no_embed_bwd(torch.empty((0, 20), device="cuda"), none, table, ws_of(b.no_embed_ws_bytes(0, 20)), accumulate=True)
+    assert (table == MARK).all()
+    b.no_embed_bwd(torch.empty((0, 20), device="cuda"), none, table, ws_of(b.no_embed_ws_bytes(0, 20)))
+    assert (table == 0).all()
+
+
+def test_embed_bwd_keeps_infinities_in_their_rows():
+    b = nb()
+    grad = torch.ones((100, 16), device="cuda")
+    grad[40], grad[41, 3], grad[70] = INF, NAN, NAN
+    ids = (torch.arange(100, device="cuda") // 10).to(torch.int32)
+    ids[70] = -1                                         # a masked position
+    table = torch.empty((12, 16), device="cuda")
+    b.no_embed_bwd(grad, ids, table, ws_of(b.no_embed_ws_bytes(100, 16)))
+    want = torch.full((12, 16), 10.0)
+    want[4], want[4, 3], want[7], want[10:] = INF, NAN, 9.0, 0.0
+    assert torch.equal(table.cpu().nan_to_num(-1.0), want.nan_to_num(-1.0))
+
+
+# ------------------------------------------------------------------------------------------------------- rmsnorm
+
+NORM_SIZES = [(1, 1, 0, 0), (1, 64, 0, 0), (3, 5, 2, 1), (7, 63, 0, 0), (64, 100, 4, 4), (100, 602, 0, 0), (65, 256, 0, 0), (1000, 128, 0, 0), (33, 1025, 3, 1),
+              (19, 2048, 0, 0), (5, 4096, 8, 8), (3, 4099, 0, 0), (2, 8192, 0, 0), (2, 16_385, 1, 0), (1, 40_000, 0, 0), (2, 65_536, 0, 0), (9000, 32, 0, 0)]
+
+
+def chain(dim):
+    return min(dim, 256) + 16      # a lane adds at most 256 terms of a row, a tree joins the lanes
+
+
+def norm_ref(x, residual, weight, eps):
+    s = x if residual is None else (x.float() + residual.float()).to(x.dtype)
+    v = s.double()
+    rstd = 1.0 / torch.sqrt(v.square().mean(1) + eps)
+    return s, rstd, v * rstd[:, None] * (1.0 if weight is None else weight.double())
+
+
+@pytest.mark.parametrize("n,dim,pad,off", NORM_SIZES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("dt_y", [F32, BF16, E4M3], ids=["to_f32", "to_bf16", "to_e4m3"])
+@pytest.mark.parametrize("residual", [False, True])
+def test_rmsnorm_fwd(n, dim, pad, off, dt, dt_y, residual):
+    b, g = nb(), rng(n + dim)
+    x = Rows(n, dim, dt, pad, off, randn((n, dim), g, dt, 2.0))
+    r = Rows(n, dim, dt, 0, off, randn((n, dim), g, dt)) if residual else None
+    weight = 1 + 0.3 * randn((dim,), g) if n != 65 else None
+    if n > 4:
+        x.t[2] = 0
+        if residual:
+            r.t[2] = 0
+    s, y = (Rows(n, dim, dt, pad, off) if residual or n % 2 else None), Rows(n, dim, dt_y, pad, off)
+    rstd = torch.full((n,), MARK, device="cuda")
+    row_scale = torch.full((n,), MARK, device="cuda") if dt_y == E4M3 else None
+    b.no_rmsnorm_fwd(x.t, weight, 1e-5, y.t, residual=r.t if r else None, sum_out=s.t if s else None, row_scale=row_scale, rstd=rstd)
+    ref_s, ref_rstd, ref_y = norm_ref(x.t, r.t if r else None, weight, 1e-5)
+    if s:
+        assert torch.equal(s.t, ref_s) and s.untouched()
+    rel = chain(dim) * U + 8 * U            # rstd: half of the sum's error, mean, addition, root, quotient; y: two products more
+    close(rstd, ref_rstd, rel * ref_rstd, "rstd")
+    if dt_y == E4M3:
+        most = ref_y.abs().amax(1).clamp(min=2.0 ** -100) / 448
+        close(row_scale, most, rel * most, "scale")
+        back = y.t.contiguous().view(torch.uint8).view(E4M3).double() * row_scale.double()[:, None]
+        close(back, ref_y, (2.0 ** -4 + 2 * rel) * ref_y.abs() + 2.0 ** -10 * most[:, None], "y")      # half a step; of the smallest ones below 2^-6
+        assert bool((back.abs().amax(1) >= (1 - 2 * rel) * 448 * row_scale.double() * (ref_y.abs().amax(1) > 0)).all())
+    else:
+        close(y.t, ref_y, (rel + half(dt_y) * (1 + rel)) * ref_y.abs() + TINY, "y")
+    assert y.untouched()
+
+
+def test_rmsnorm_fwd_in_place_counts_and_extremes():
+    b, g = nb(), rng(4)
+    for dt, n, dim in ((BF16, 9, 1000), (F32, 9, 1000), (BF16, 3, 20_000), (F32, 5, 7)):
+        x, r, w = randn((n, dim), g, dt), randn((n, dim), g, dt), randn((dim,), g)
+        s, y = torch.empty_like(x), torch.empty_like(x)
+        b.no_rmsnorm_fwd(x, w, 1e-6, y, residual=r, sum_out=s)
+        x1, r1 = x.clone(), r.clone()
+        b.no_rmsnorm_fwd(x1, w, 1e-6, x1, residual=r1, sum_out=r1)          # the sum over the residual, the result over x
+        assert torch.equal(x1, y) and torch.equal(r1, s)
+        out = Rows(n, dim, dt)
+        b.no_rmsnorm_fwd(x, w, 1e-6, out.t, residual=r, n_rows=count(2))
+        assert torch.equal(out.t[:2], y[:2]) and out.untouched(rows=2)
+        b.no_rmsnorm_fwd(x, w, 1e-6, out.t, n_rows=count(0))
+        assert out.untouched(rows=2)
+    b.no_rmsnorm_fwd(torch.empty((0, 8), device="cuda"), None, 1e-6, torch.empty((0, 8), device="cuda"))
+    x = torch.ones((4, 64), device="cuda")
+    x[0, 5], x[1, 6], x[2] = NAN, INF, 1e-30
+    y, sc, rstd = torch.empty((4, 64), device="cuda"), torch.empty((4,), device="cuda"), torch.empty((4,), device="cuda")
+    b.no_rmsnorm_fwd(x, None, 0.0, y, rstd=rstd)
+    assert y[0].isnan().all() and rstd[0].isnan() and y[1, 6].isnan() and rstd[1] == 0
+    q = torch.empty((4, 64), device="cuda", dtype=E4M3)
+    b.no_rmsnorm_fwd(x, None, 1e-6, q, row_scale=sc)
+    assert sc[:2].isnan().all() and q.float()[:2].isnan().all() and (q.float()[2:].abs() == 448).all()
+    x[:] = 0
+    b.no_rmsnorm_fwd(x, None, 1e-6, q, row_scale=sc)
+    assert (q.float() == 0).all() and (sc == 2.0 ** -100 / 448).all()
+
+
+@pytest.mark.parametrize("n,dim,pad,off", NORM_SIZES + [(3000, 7, 0, 0), (70_000, 16, 0, 0), (600, 2049, 1, 1)])
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("joined", [False, True])
+def test_rmsnorm_bwd(n, dim, pad, off, dt, joined):
+    b, g = nb(), rng(n + dim)
+    s = Rows(n, dim, dt, pad, off, randn((n, dim), g, dt, 2.0))
+    gy = Rows(n, dim, dt, 0, off, randn((n, dim), g, dt))
+    gs = Rows(n, dim, dt, pad, 0, randn((n, dim), g, dt)) if joined else None
+    weight = 1 + 0.3 * randn((dim,), g) if n != 65 else None
+    rstd = (1.0 / torch.sqrt(s.t.double().square().mean(1) + 1e-5)).float()
+    gx, gw = Rows(n, dim, dt, pad, off), torch.full((dim,), MARK, device="cuda")
+    ws = ws_of(b.no_rmsnorm_ws_bytes(n, dim))
+    b.no_rmsnorm_bwd(s.t, weight, rstd, gy.t, gx.t, gw, ws, grad_sum=gs.t if gs else None)
+    r = rstd.double()[:, None]
+    u_, wg = s.t.double() * r, gy.t.double() * (1.0 if weight is None else weight.double())
+    dot, size = (wg * u_).mean(1, keepdim=True), (wg * u_).abs().mean(1, keepdim=True)
+    ref = r * (wg - u_ * dot)
+    # the mean: three products, its chain, the division; then three products and a difference
+    tol = r * (4 * U * wg.abs() + u_.abs() * ((chain(dim) + 8) * U * size + 4 * U * dot.abs()))
+    if joined:
+        ref = ref + gs.t.double()
+        tol = tol + U * ref.abs()
+    close(gx.t, ref, tol + half(dt) * (ref.abs() + tol) + TINY, "grad_x")
+    close(gw, (gy.t.double() * u_).sum(0), (n + 4) * U * (gy.t.double() * u_).abs().sum(0), "grad_weight")
+    assert gx.untouched()
+    again, gw2 = torch.empty((n, dim), device="cuda", dtype=dt), torch.empty_like(gw)
+    ws.fill_(0x3C)
+    b.no_rmsnorm_bwd(s.t, weight, rstd, gy.t, again, gw2, ws, grad_sum=gs.t if gs else None)
+    assert torch.equal(again, gx.t) and torch.equal(gw, gw2)
+    b.no_rmsnorm_bwd(s.t, weight, rstd, gy.t, gy.t, gw2, ws, grad_sum=gs.t if gs else None)        # over the incoming gradient
+    assert torch.equal(gy.t, again) and torch.equal(gw, gw2)
+
+
+def test_rmsnorm_bwd_counts_and_parts():
+    b, g = nb(), rng(6)
+    n, dim = 500, 96
+    s, gy = randn((n, dim), g), randn((n, dim), g)
+    rstd = 1.0 / s.square().mean(1).sqrt()
+    ws = ws_of(b.no_rmsnorm_ws_bytes(n, dim))
+    for here in (0, 1, 130, 499):
+        s[here:], rstd[here:] = NAN, NAN
+        s[:here], rstd[:here] = randn((here, dim), g), 1.5
+        gx, gw = Rows(n, dim, F32), torch.full((dim,), MARK, device="cuda")
+        b.no_rmsnorm_bwd(s, None, rstd, gy, gx.t, gw, ws, n_rows=count(here))
+        terms = gy[:here].double() * s[:here].double() * 1.5
+        close(gw, terms.sum(0), (here + 4) * U * terms.abs().sum(0))
+        assert gx.untouched(rows=here) and not gx.t[:here].isnan().any()
+        alone = torch.empty((n, dim), device="cuda")
+        b.no_rmsnorm_bwd(s, None, rstd, gy, alone, None, ws, n_rows=count(here))
+        assert torch.equal(alone[:here], gx.t[:here])
+    b.no_rmsnorm_bwd(s[:0], None, rstd[:0], gy[:0], gx.t[:0], gw, ws)
+    assert (gw == 0).all()
+
+
+def test_rmsnorm_gradient_against_differences():
+    b, g = nb(), rng(8)
+    n, dim, h = 3, 40, 1e-3
+    x, w, gy = randn((n, dim), g), 1 + 0.2 * randn((dim,), g), randn((n, dim), g)
+    rstd, y = torch.empty((n,), device="cuda"), torch.empty((n, dim), device="cuda")
+    b.no_rmsnorm_fwd(x, w, 1e-5, y, rstd=rstd)
+    gx, gw = torch.empty_like(x), torch.empty_like(w)
+    b.no_rmsnorm_bwd(x, w, rstd, gy, gx, gw, ws_of(b.no_rmsnorm_ws_bytes(n, dim)))
+    f = lambda xx, ww: (norm_ref(xx, None, ww, 1e-5)[2] * gy.double()).sum().item()  # noqa: E731
+    for i, c in ((0, 0), (1, 17), (2, 39)):
+        d = torch.zeros((n, dim), device="cuda", dtype=torch.float64)
+        d[i, c] = h
+        # central differences of a smooth function: off by about h^2 of its third derivative
+        assert abs((f(x.double() + d, w) - f(x.double() - d, w)) / (2 * h) - gx[i, c].item()) < 1e-4
+        assert abs((f(x, w.double() + d[i]) - f(x, w.double() - d[i])) / (2 * h) - gw[c].item()) < 1e-4
+
+
+# ------------------------------------------------------------------------------------------------------- logits
+
+CLASSES = [(1, 1, 0, 0), (5, 2, 0, 0), (9, 7, 1, 1), (300, 47, 0, 0), (33, 64, 0, 0), (1025, 172, 4, 0), (17, 513, 0, 3), (12, 2048, 0, 0), (6, 4099, 0, 0),
+           (600, 5000, 8, 8), (3, 16_385, 1, 0), (2, 32_768, 0, 0), (5, 50_001, 0, 0), (1, 131_072, 0, 0), (2, 131_073, 0, 1), (1, 300_001, 0, 0),
+           (270, 40_003, 0, 0), (20_000, 10, 0, 0)]
+
+
+def logits(n, c, pad, off, dt, g, masked=True):
+    z = Rows(n, c, dt, pad, off, randn((n, c), g, dt, 3.0))
+    if masked and c > 4:
+        z.t[:, c // 3] = -INF
+        z.t[n // 2, : c // 2] = -INF
+    return z
+
+
+def row_stats(z, t):
+    """(z / T, lse, bound of lse, log p) in 64 bits. The bound: products with 1 / T (of the largest logit and of the differences), a chain of
+    C / 256 additions and the tree, the logarithm, the last addition."""
+    x = z.double() / t
+    lse = torch.logsumexp(x, 1)
+    m = x.amax(1).nan_to_num(0.0, 0.0, 0.0).abs()
+    return x, lse, 4 * U * (m + lse.abs()) + (z.shape[1] / 256 + 64) * U, x - lse[:, None]
+
+
+def teacher(n, c, k, g, repeats=False):
+    ids = torch.stack([torch.randperm(c, generator=g, device="cuda")[:k] for _ in range(min(n, 40))]) if c >= k and not repeats else \
+        torch.randint(0, c, (min(n, 40), k), generator=g, device="cuda")
+    ids = ids[torch.arange(n, device="cuda") % ids.shape[0]].to(torch.int32)
+    return ids.contiguous(), randn((n, k), g, F32, 2.0)
+
+
+def distill_ref(z, ids, tl, t, w, lse=None):
+    """loss, its bound; gradient, its bound (before rounding to z's type); lse, its bound. In 64 bits."""
+    n, c = z.shape
+    k = ids.shape[1]
+    x, own_lse, lse_tol, log_q = row_stats(z, t)
+    rel = lse_tol[:, None]
+    if lse is not None:
+        log_q = x - lse.double()[:, None]
+        rel = torch.zeros_like(rel)
+    there = (ids >= 0) & (ids < c)
+    tt = torch.where(there, tl.double() / t, -INF)
+    any_ = (tt > -INF).any(1)
+    log_p = torch.where(any_[:, None], tt - torch.logsumexp(tt, 1, keepdim=True), -INF)
+    p = log_p.exp()
+    at = torch.where(there, ids, 0).long()
+    ql = log_q.gather(1, at)
+    term = torch.where(p > 0, p * (log_p - ql), 0.0)
+    size = torch.where(p > 0, p * (log_p.abs() + ql.abs()), 0.0).sum(1)
+    w = torch.ones((n,), device="cuda", dtype=torch.float64) if w is None else w.double()
+    live = (w != 0) & any_
+    loss = torch.where(live, w * t * t * term.sum(1), 0.0)
+    # a share: exponent, sum of k, quotient; its logarithm; the difference; the sum of k
+    loss_tol = (w * t * t).abs() * ((2 * k + 32) * U * size + lse_tol + 8 * U)
+    q = torch.where(x > -INF, log_q.exp(), 0.0)
+    dense = torch.zeros_like(x).scatter_add_(1, at, p)
+    p_size = torch.zeros_like(x).scatter_add_(1, at, torch.where(p > 0, p * (2 * k + 16 + 8 * log_p.abs()), 0.0))
+    by = (w * t)[:, None]
+    grad = torch.where(live[:, None], by * (q - dense), 0.0)
+    finite = torch.where(log_q.isfinite(), log_q, 0.0).abs()
+    xs = torch.where(x.isfinite(), x, 0.0).abs()
+    own = (lse if lse is not None else own_lse).double().nan_to_num(0.0, 0.0, 0.0).abs()[:, None]
+    grad_tol = by.abs() * (q * (rel + 4 * U * (xs + own) + 8 * U * (1 + finite)) + U * p_size) + 2 * U * grad.abs() + TINY
+    return loss, loss_tol, grad, grad_tol, own_lse, lse_tol
+
+
+@pytest.mark.parametrize("n,c,pad,off", CLASSES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("k,t", [(1, 1.0), (8, 2.0), (100, 0.7), (256, 1.0)])
+def test_distill(n, c, pad, off, dt, k, t):
+    b, g = nb(), rng(n + c + k)
+    z = logits(n, c, pad, off, dt, g)
+    ids, tl = teacher(n, c, k, g, repeats=k > c)
+    # the teacher's entries stand at logits above -inf here, but for some left out
+    bad = z.t.gather(1, ids.long()) == -INF
+    ids[bad] = -1
+    if n > 3 and k > 1:
+        ids[3, 0], ids[1, 1] = c, -7
+        tl[2, 0] = -INF
+    w = torch.rand((n,), generator=g, device="cuda") if k > 1 else None
+    if w is not None and n > 6:
+        w[::5] = 0
+    loss, lse = torch.full((n,), MARK, device="cuda"), torch.full((n,), MARK, device="cuda")
+    ws = ws_of(b.no_distill_ws_bytes(n, c))
+    b.no_distill_fwd(z.t, ids, tl, t, w, loss, lse, ws)
+    ref = distill_ref(z.t, ids, tl, t, w)
+    close(loss, ref[0], ref[1], "loss")
+    close(lse, ref[4], ref[5], "lse")
+    grad = Rows(n, c, dt, pad, off)
+    b.no_distill_bwd(z.t, ids, tl, t, w, lse, grad.t)
+    g2 = distill_ref(z.t, ids, tl, t, w, lse)
+    close(grad.t, g2[2], g2[3] + half(dt) * (g2[2].abs() + g2[3]), "grad")
+    assert grad.untouched()
+    loss2, lse2, grad2 = torch.empty_like(loss), torch.empty_like(lse), Rows(n, c, dt, pad, off)
+    ws.fill_(0x3C)
+    b.no_distill_fwd_bwd(z.t, ids, tl, t, w, loss2, lse2, grad2.t, ws)
+    close(loss2, ref[0], ref[1], "loss of both")
+    close(lse2, ref[4], ref[5], "lse of both")
+    close(grad2.t, ref[2], ref[3] + half(dt) * (ref[2].abs() + ref[3]), "grad of both")
+    assert grad2.untouched()
+    keep, first = z.t.clone(), grad2.t.clone()
+    b.no_distill_fwd_bwd(z.t, ids, tl, t, w, loss, None, z.t, ws)            # the gradient over the logits
+    assert torch.equal(z.t, first) and torch.equal(loss, loss2) and z.untouched()
+    z.t.copy_(keep)
+    b.no_distill_bwd(z.t, ids, tl, t, w, lse, z.t)
+    assert torch.equal(z.t, grad.t)
+
+
+@pytest.mark.parametrize("c", [40, 700, 9000, 70_000, 140_000])
+@pytest.mark.parametrize("n", [8, 400])
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_distill_masks_and_special_rows(c, n, dt):
+    b, g = nb(), rng(c)
+    z, k, t = randn((n, c), g, dt), 4, 2.0
+    ids, tl = teacher(n, c, k, g)
+    w = torch.ones((n,), device="cuda")
+    z[0] = NAN
+    w[0] = 0                                    # masked, whatever it holds
+    z[1, c - 1] = NAN
+    z[2, 3] = INF
+    z[3] = -INF                                 # nothing left
+    z[4, ids[4, 1].item()] = -INF               # the teacher gives a share to a masked class
+    ids[5] = -1                                 # no entries
+    tl[6] = -INF
+    ids[7, 1] = ids[7, 0]                       # an id twice
+    loss, lse, grad = torch.empty((n,), device="cuda"), torch.empty((n,), device="cuda"), torch.empty_like(z)
+    ws = ws_of(b.no_distill_ws_bytes(n, c))
+    ref = distill_ref(z, ids, tl, t, w)
+    for both in (True, False):
+        if both:
+            b.no_distill_fwd_bwd(z, ids, tl, t, w, loss, lse, grad, ws)
+        else:
+            b.no_distill_fwd(z, ids, tl, t, w, loss, lse, ws)
+            b.no_distill_bwd(z, ids, tl, t, w, lse, grad)
+        assert loss[0] == 0 and (grad[0] == 0).all()
+        assert loss[1].isnan() and lse[1].isnan() and grad[1].isnan().all()
+        assert loss[2].isnan() and grad[2].isnan().all()
+        assert loss[3] == INF and lse[3] == -INF
+        want = torch.zeros((c,), device="cuda", dtype=torch.float64).scatter_add_(0, ids[3].long(), -t * torch.softmax(tl[3].double() / t, 0))
+        close(grad[3], want, (half(dt) + 32 * U) * want.abs(), "grad of an empty row")
+        assert loss[4] == INF and not grad[4].isnan().any()
+        assert (loss[5:7] == 0).all() and (grad[5:7] == 0).all() and lse[5:7].isfinite().all()
+        for rows in (slice(4, 5), slice(7, n)):
+            bound = ref[3][rows] * (1 if both else 2) + half(dt) * ref[2][rows].abs() * 1.01 + (0 if both else 4 * U * ref[2][rows].abs() + ref[5][rows][:, None] * 2)
+            close(grad[rows], ref[2][rows], bound, "grad")
+        close(loss[7:], ref[0][7:], ref[1][7:], "loss")
+
+
+def test_distill_counts():
+    b, g = nb(), rng(11)
+    for n, c, dt in ((50, 100, F32), (300, 20_000, BF16), (20, 90_000, F32), (3, 200_001, BF16)):
+        z, (ids, tl) = randn((n, c), g, dt), teacher(n, c, 5, g)
+        ws = ws_of(b.no_distill_ws_bytes(n, c))
+        whole, lse, grad = torch.empty((n,), device="cuda"), torch.empty((n,), device="cuda"), torch.empty_like(z)
+        b.no_distill_fwd_bwd(z, ids, tl, 1.0, None, whole, lse, grad, ws)
+        for here in (0, 2):
+            loss, l2, out = torch.full((n,), MARK, device="cuda"), torch.full((n,), MARK, device="cuda"), Rows(n, c, dt)
+            b.no_distill_fwd_bwd(z, ids, tl, 1.0, None, loss, l2, out.t, ws, n_rows=count(here))
+            assert torch.equal(loss[:here], whole[:here]) and (loss[here:] == MARK).all() and (l2[here:] == MARK).all()
+            assert torch.equal(out.t[:here], grad[:here]) and out.untouched(rows=here)
+            b.no_distill_fwd(z, ids, tl, 1.0, None, loss, l2, ws, n_rows=count(here))
+            assert (loss[here:] == MARK).all() and (l2[here:] == MARK).all() and torch.equal(l2[:here], lse[:here])
+            out = Rows(n, c, dt)
+            b.no_distill_bwd(z, ids, tl, 1.0, None, lse, out.t, n_rows=count(here))
+            assert out.untouched(rows=here)
+    none = torch.empty((0, 9), device="cuda")
+    e = torch.empty((0,), device="cuda")
+    b.no_distill_fwd_bwd(none, torch.empty((0, 2), dtype=torch.int32, device="cuda"), torch.empty((0, 2), device="cuda"), 1.0, None, e, e, none,
+                         ws_of(b.no_distill_ws_bytes(0, 9)))
+
+
+def test_distill_gradient_against_differences():
+    b, g = nb(), rng(12)
+    n, c, k, t, h = 3, 30, 5, 2.0, 1e-3
+    z, (ids, tl) = randn((n, c), g), teacher(n, c, k, g)
+    w = torch.tensor([0.5, 2.0, 1.0], device="cuda")
+    loss, grad = torch.empty((n,), device="cuda"), torch.empty_like(z)
+    b.no_distill_fwd_bwd(z, ids, tl, t, w, loss, None, grad, ws_of(b.no_distill_ws_bytes(n, c)))
+    for i, at in ((0, int(ids[0, 0])), (1, 3), (2, int(ids[2, 4]))):
+        d = torch.zeros((n, c), device="cuda", dtype=torch.float64)
+        d[i, at] = h
+        f = lambda zz: distill_ref(zz, ids, tl, t, w)[0].sum().item()  # noqa: E731
+        assert abs((f(z.double() + d) - f(z.double() - d)) / (2 * h) - grad[i, at].item()) < 1e-5
+
+
+def logprobs_ref(z, tok, t, k):
+    n, c = z.shape
+    x, lse, lse_tol, log_p = row_stats(z, t)
+    there = (tok >= 0) & (tok < c)
+    lp = torch.where(there, log_p.gather(1, torch.where(there, tok, 0).long()[:, None])[:, 0], 0.0)
+    p = log_p.exp()
+    plogp = torch.where(p > 0, p * log_p, 0.0)
+    # by value, then by class; -inf is no alternative
+    value, at = torch.sort(z.float(), dim=1, descending=True, stable=True)
+    kk = min(k, c)
+    ids = torch.full((n, k), -1, device="cuda", dtype=torch.int32)
+    ids[:, :kk] = torch.where(value[:, :kk] > -INF, at[:, :kk], -1).to(torch.int32)
+    top = torch.full((n, k), -INF, device="cuda", dtype=torch.float64)
+    top[:, :kk] = log_p.gather(1, at[:, :kk])
+    return lp, -plogp.sum(1), lse, lse_tol, ids, top, plogp.abs().sum(1)
+
+
+@pytest.mark.parametrize("n,c,pad,off", CLASSES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("k,t", [(0, 1.0), (1, 0.7), (8, 2.0), (20, 1.0), (64, 1.0)])
+def test_logprobs_fwd(n, c, pad, off, dt, k, t):
+    b, g = nb(), rng(n + c + k)
+    z = logits(n, c, pad, off, dt, g)
+    tok = torch.randint(-1, c + 1, (n,), generator=g, device="cuda", dtype=torch.int32)
+    lp, ent, lse = (torch.full((n,), MARK, device="cuda") for _ in range(3))
+    ids, top = torch.full((n, k), 77, dtype=torch.int32, device="cuda"), torch.full((n, k), MARK, device="cuda")
+    ws = ws_of(b.no_logprobs_ws_bytes(n, c, k))
+    b.no_logprobs_fwd(z.t, tok, t, lp, ent, lse, ws, top_ids=ids if k else None, top_logprobs=top if k else None)
+    ref = logprobs_ref(z.t, tok, t, k)
+    one = ref[3] + 8 * U * (1 + torch.where(ref[0].isfinite(), ref[0].abs(), 0.0))
+    close(lp, ref[0], one, "logprob")
+    close(lse, ref[2], ref[3], "lse")
+    close(ent, ref[1], 4 * ref[3] + 16 * U * ref[6] + (c / 256 + 64) * U * (1 + ref[6]), "entropy")
+    assert torch.equal(ids, ref[4])
+    close(top, ref[5], ref[3][:, None] + 8 * U * (1 + torch.where(ref[5].isfinite(), ref[5].abs(), 0.0)), "top")
+    again = [torch.empty_like(v) for v in (lp, ent, lse, ids, top)]
+    ws.fill_(0x3C)
+    b.no_logprobs_fwd(z.t, tok, t, *again[:3], ws, top_ids=again[3] if k else None, top_logprobs=again[4] if k else None)
+    for x, y in zip(again, (lp, ent, lse, ids, top)):
+        assert torch.equal(x, y)
+
+
+def crowded(kind, n, c, dt, g):
+    """Rows whose largest values stand where a search by parts finds them hardest."""
+    z = randn((n, c), g, dt)
+    if kind == "equal":
+        z[:] = 1.5
+    elif kind == "two values":
+        z = (torch.rand((n, c), generator=g, device="cuda") < 0.5).to(dt)
+    elif kind == "ascending":
+        z[:] = torch.linspace(-9, 9, c, device="cuda").to(dt)
+    elif kind == "descending":
+        z[:] = torch.linspace(9, -9, c, device="cuda").to(dt)
+    elif kind == "one run":                      # all large values side by side
+        z[:, c // 2:c // 2 + 3000] += 40
+    elif kind == "one lane":                     # ... or at distances of a lane's units
+        for s in (64, 256, 512, 1024, 2048, 8192):
+            z[:, 5::s] += 20 + (torch.rand(z[:, 5::s].shape, generator=g, device="cuda") * 4).to(dt)
+    elif kind == "few":                          # fewer than k above -inf
+        z[:] = -INF
+        z[:, c // 7::max(1, c // 6)] = 2.0
+    elif kind == "zeros":
+        z[:] = 0.0
+        z[:, ::2] = -0.0
+    elif kind == "large":
+        z *= 1e37
+    return z
+
+
+@pytest.mark.parametrize("kind", ["equal", "two values", "ascending", "descending", "one run", "one lane", "few", "zeros", "large"])
+@pytest.mark.parametrize("n,c", [(3, 100), (2, 5000), (2, 40_000), (1, 131_072), (300, 33_000)])
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("k", [1, 64])
+def test_logprobs_alternatives_of_crowded_rows(kind, n, c, dt, k):
+    b, g = nb(), rng(c)
+    z = crowded(kind, n, c, dt, g)
+    tok = torch.zeros((n,), dtype=torch.int32, device="cuda")
+    lp, ent, lse, top = (torch.empty(s, device="cuda") for s in ((n,), (n,), (n,), (n, k)))
+    ids = torch.empty((n, k), dtype=torch.int32, device="cuda")
+    b.no_logprobs_fwd(z, tok, 1.0, lp, ent, lse, ws_of(b.no_logprobs_ws_bytes(n, c, k)), top_ids=ids, top_logprobs=top)
+    ref = logprobs_ref(z, tok, 1.0, k)
+    assert torch.equal(ids, ref[4])
+    bound = ref[3][:, None] + 8 * U * (1 + torch.where(ref[5].isfinite(), ref[5].abs(), 0.0))
+    close(top, ref[5], bound, "top")
+    close(lse, ref[2], ref[3], "lse")
+
+
+@pytest.mark.parametrize("c", [30, 700, 9000, 70_000, 140_000])
+@pytest.mark.parametrize("n", [5, 400])
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_logprobs_special_rows(c, n, dt):
+    b, g = nb(), rng(c)
+    z = randn((n, c), g, dt)
+    z[0, 7], z[1, 8], z[2] = NAN, INF, -INF
+    z[3], z[3, c - 1] = -INF, 2.0
+    tok = torch.full((n,), c - 1, dtype=torch.int32, device="cuda")
+    k = 3
+    lp, ent, lse, top = (torch.empty(s, device="cuda") for s in ((n,), (n,), (n,), (n, k)))
+    ids = torch.empty((n, k), dtype=torch.int32, device="cuda")
+    b.no_logprobs_fwd(z, tok, 1.0, lp, ent, lse, ws_of(b.no_logprobs_ws_bytes(n, c, k)), top_ids=ids, top_logprobs=top)
+    for v in (lp[:2], ent[:2], lse[:2], top[:2]):
+        assert v.isnan().all()
+    assert (ids[:3] == -1).all()
+    assert lp[2] == -INF and ent[2] == 0 and lse[2] == -INF and (top[2] == -INF).all()
+    assert abs(lp[3]) <= 4 * U and abs(ent[3]) <= 4 * U and abs(lse[3] - 2) <= 8 * U and ids[3].tolist() == [c - 1, -1, -1]
+    assert top[3].tolist()[1:] == [-INF, -INF]
+    grad = torch.empty_like(z)
+    one = torch.ones((n,), device="cuda")
+    b.no_logprobs_bwd(z, tok, 1.0, lse, ent, one, one, grad)
+    assert grad[0].isnan().all() and grad[1].isnan().all()
+    want = torch.zeros((c,), device="cuda")
+    want[c - 1] = 1.0
+    assert torch.equal(grad[2].float(), want) and (grad[3, :c - 1] == 0).all() and abs(grad[3, c - 1].item()) <= 16 * U
+
+
+@pytest.mark.parametrize("n,c,pad,off", CLASSES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("parts", ["both", "logprob", "entropy"])
+def test_logprobs_bwd(n, c, pad, off, dt, parts):
+    b, g, t = nb(), rng(n + c), 0.8
+    z = logits(n, c, pad, off, dt, g)
+    tok = torch.randint(-1, c + 1, (n,), generator=g, device="cuda", dtype=torch.int32)
+    x, lse, _, _ = row_stats(z.t, t)
+    lse = lse.float()
+    log_p = x - lse.double()[:, None]
+    p = torch.where(x > -INF, log_p.exp(), 0.0)
+    ent = (-torch.where(p > 0, p * log_p, 0.0).sum(1)).float()
+    gl = randn((n,), g) if parts != "entropy" else None
+    gh = randn((n,), g) if parts != "logprob" else None
+    grad = Rows(n, c, dt, pad, off)
+    b.no_logprobs_bwd(z.t, tok, t, lse, ent, gl, gh, grad.t)
+    there = (tok >= 0) & (tok < c)
+    hit = torch.zeros_like(x).scatter_add_(1, torch.where(there, tok, 0).long()[:, None], there.double()[:, None])
+    l = torch.zeros_like(x) if gl is None else torch.where(there, gl.double(), 0.0)[:, None].expand_as(x)
+    e = torch.zeros_like(x) if gh is None else gh.double()[:, None].expand_as(x)
+    lp = torch.where(p > 0, log_p, 0.0)
+    ref = (l * (hit - p) - e * p * (lp + ent.double()[:, None])) / t
+    rel = 4 * U * (torch.where(x.isfinite(), x, 0.0).abs() + lse.double().abs()[:, None]) + 8 * U * (1 + lp.abs())
+    size = (l.abs() * (hit + p) + e.abs() * p * (lp.abs() + ent.double()[:, None])) / t
+    tol = (rel + 8 * U) * size + rel * p * (e.abs()) / t + TINY
+    close(grad.t, ref, tol + half(dt) * (ref.abs() + tol), "grad")
+    assert grad.untouched()
+    keep = grad.t.clone()
+    b.no_logprobs_bwd(z.t, tok, t, lse, ent, gl, gh, z.t)
+    assert torch.equal(z.t, keep) and z.untouched()
+
+
+def test_logprobs_counts():
+    b, g = nb(), rng(13)
+    for n, c in ((50, 100), (300, 20_000), (3, 200_001)):
+        z, tok, k = randn((n, c), g), torch.zeros((n,), dtype=torch.int32, device="cuda"), 6
+        ws = ws_of(b.no_logprobs_ws_bytes(n, c, k))
+        for here in (0, 2):
+            lp, ent, lse, top = (torch.full(s, MARK, device="cuda") for s in ((n,), (n,), (n,), (n, k)))
+            ids = torch.full((n, k), 77, dtype=torch.int32, device="cuda")
+            b.no_logprobs_fwd(z, tok, 1.0, lp, ent, lse, ws, top_ids=ids, top_logprobs=top, n_rows=count(here))
+            for v in (lp, ent, lse, top, ids):
+                assert (v[here:] == 77).all() and (v[:here] != 77).all()
+            grad = Rows(n, c, F32)
+            b.no_logprobs_bwd(z, tok, 1.0, lse, ent, lp, None, grad.t, n_rows=count(here))
+            assert grad.untouched(rows=here)
+
+
+def test_logprobs_gradient_against_differences():
+    b, g, t, h = nb(), rng(14), 1.3, 1e-3
+    n, c = 3, 25
+    z, tok = randn((n, c), g), torch.tensor([4, 24, -1], dtype=torch.int32, device="cuda")
+    gl, gh = randn((n,), g), randn((n,), g)
+    lp, ent, lse, grad = torch.empty((n,), device="cuda"), torch.empty((n,), device="cuda"), torch.empty((n,), device="cuda"), torch.empty_like(z)
+    b.no_logprobs_fwd(z, tok, t, lp, ent, lse, ws_of(b.no_logprobs_ws_bytes(n, c, 0)))
+    b.no_logprobs_bwd(z, tok, t, lse, ent, gl, gh, grad)
+
+    def f(zz):
+        r = logprobs_ref(zz, tok, t, 0)
+        return (r[0] * gl.double() + r[1] * gh.double()).sum().item()
+    for i, at in ((0, 4), (0, 9), (1, 24), (2, 0)):
+        d = torch.zeros((n, c), device="cuda", dtype=torch.float64)
+        d[i, at] = h
+        assert abs((f(z.double() + d) - f(z.double() - d)) / (2 * h) - grad[i, at].item()) < 1e-5
+
+
+# ------------------------------------------------------------------------------------------------------- streams, graphs
+
+def test_operators_on_another_stream_and_in_a_graph():
+    """Every call on a stream of the caller's, then captured and replayed among eager work, each replay against the eager result."""
+    b, g = nb(), rng(15)
+    v, d, n, c, k = 500, 96, 700, 3001, 5
+    table, w = randn((v, d), g), 1 + 0.1 * randn((d,), g)
+    ids = torch.randint(0, v, (n,), generator=g, device="cuda", dtype=torch.int32)
+    z, (tid, tl) = randn((n, c), g), teacher(n, c, k, g)
+    one = torch.ones((n,), device="cuda")
+    ws = [ws_of(s) for s in (b.no_embed_ws_bytes(n, d), b.no_rmsnorm_ws_bytes(n, d), b.no_distill_ws_bytes(n, c), b.no_logprobs_ws_bytes(n, c, k))]
+    e = lambda *s: torch.empty(s, device="cuda")  # noqa: E731
+    o = dict(x=e(n, d), y=e(n, d), rstd=e(n), gx=e(n, d), gw=e(d), gt=e(v, d), loss=e(n), lse=e(n), gz=e(n, c), lp=e(n), ent=e(n), lse2=e(n),
+             ids=torch.empty((n, k), dtype=torch.int32, device="cuda"), top=e(n, k), gz2=e(n, c), gz3=e(n, c))
+
+    def calls():
+        b.no_embed_fwd(table, ids, o["x"], scale=2.0)
+        b.no_rmsnorm_fwd(o["x"], w, 1e-5, o["y"], rstd=o["rstd"])
+        b.no_rmsnorm_bwd(o["x"], w, o["rstd"], o["y"], o["gx"], o["gw"], ws[1])
+        b.no_embed_bwd(o["gx"], ids, o["gt"], ws[0])
+        b.no_distill_fwd_bwd(z, tid, tl, 1.0, None, o["loss"], o["lse"], o["gz"], ws[2])
+        b.no_distill_fwd(z, tid, tl, 1.0, None, o["loss"], o["lse"], ws[2])
+        b.no_distill_bwd(z, tid, tl, 1.0, None, o["lse"], o["gz3"])
+        b.no_logprobs_fwd(z, ids, 1.0, o["lp"], o["ent"], o["lse2"], ws[3], top_ids=o["ids"], top_logprobs=o["top"])
+        b.no_logprobs_bwd(z, ids, 1.0, o["lse2"], o["ent"], one, one, o["gz2"])
+
+    def state():
+        return {name: t.clone() for name, t in o.items()}
+
+    calls()
+    torch.cuda.synchronize()
+    eager = state()
+    side = torch.cuda.Stream()
+    for t in o.values():
+        t.fill_(3)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        calls()
+    side.synchronize()
+    for name, t in state().items():
+        assert torch.equal(t, eager[name]), name
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for turn in range(4):
+        for t in o.values():
+            t.fill_(5)
+        if turn == 2:                        # new inputs under the same graph
+            z.add_(randn((n, c), g))
+            table.mul_(0.5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = state()
+        calls()
+        torch.cuda.synchronize()
+        for name, t in state().items():
+            assert torch.equal(t, replayed[name]), (turn, name)
