@@ -61,7 +61,7 @@ inline int32_t launch_status(const char* what) {
         else hipLaunchKernelGGL(kernel, grid, block, 0, st, __VA_ARGS__);                            \
     } while (0)
 
-static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+static inline constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline int ilog2_ceil(uint64_t x) { int b = 0; while ((1ull << b) < x) ++b; return b; }
 
 // Device memory through the library's pool (pool.hip). A free waits for the block's device first; inside a ReleaseScope

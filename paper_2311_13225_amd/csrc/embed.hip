@@ -1,5 +1,6 @@
 // no_embed_fwd / no_embed_bwd: rows of a table by id, scaled, and the gradient of the table.
 #include "rows.hpp"
+#include "radix.hpp"
 
 namespace no {
 
@@ -15,21 +16,232 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_
     }
 }
 
-// A block a table row: walks all ids.
-template <typename T>
-__global__ void __launch_bounds__(256) embed_bwd_kernel(RowsOf grad, const int32_t* ids, const int32_t* d_n, int32_t cap, float scale, bool accumulate,
-                                                        RowsOf table, int64_t n_rows, int32_t dim) {
-    const int32_t n = rows_here(d_n, cap);
-    for (int64_t v = blockIdx.x; v < n_rows; v += gridDim.x)
-        for (int32_t c = threadIdx.x; c < dim; c += 256) {
-            float sum = 0.0f;
-            bool any = false;
-            for (int32_t i = 0; i < n; ++i)
-                if (ids[i] == v) { sum += to_f32(grad.row<T>(i)[c]); any = true; }
-            float* to = table.row<float>(v) + c;
-            if (accumulate) { if (any) *to += scale * sum; }
-            else *to = scale * sum;
+// ------------------------------------------------------------------------------------------------------- gradient
+//
+// G[v] = scale * sum over the positions i with ids[i] == v of g[i]. The positions are ordered by id (stable, so by position within an id); then the
+// ordered list is cut into chunks of EMBED_CHUNK positions whatever the ids are, and a lane group walks a chunk with the sum of the id at hand
+// in registers: an id that is named a thousand times costs what a thousand rare ones do. Sums of ids that lie inside a chunk go
+// straight to the table; those that reach over a chunk's border go to the workspace and are added up, in chunk order, by a second launch. Rows that no
+// id names are found by a search in the ordered ids and cleared beside the sums. No atomics: the same ids give the same bits.
+
+constexpr int EMBED_CHUNK = 32;
+constexpr int32_t EMBED_RANK_MOST = 16384;
+
+struct EmbedPlan {      // the workspace, cut up
+    int64_t n, chunks;
+    bool by_rank;
+    size_t keys, pos, keys_tmp, pos_tmp, sort_ws, parts, total;
+    EmbedPlan(int32_t n_, int32_t dim) : n(n_), chunks(ceil_div(n_, EMBED_CHUNK)), by_rank(n_ <= EMBED_RANK_MOST) {
+        const size_t list = (size_t)ceil_div(chunks * EMBED_CHUNK * 4, 16) * 16;
+        keys = 0;
+        pos = keys + list;
+        keys_tmp = pos + list;
+        pos_tmp = keys_tmp + (by_rank ? 0 : list);
+        sort_ws = pos_tmp + (by_rank ? 0 : list);
+        parts = sort_ws + (by_rank ? 0 : (size_t)ceil_div((int64_t)radix_ws_bytes(n), 16) * 16);
+        total = parts + (size_t)chunks * 2 * (size_t)dim * 4 + 16;
+    }
+};
+
+// The place of position i in the order by id, then by position, is the number of positions before it in that order. n^2 comparisons, but in one
+// launch and from registers: a lane per position, and the sixteen wavefronts of a block share the positions that it is compared with.
+__global__ void __launch_bounds__(1024) embed_rank_kernel(const int32_t* __restrict__ ids, const int32_t* d_n, int32_t cap, uint32_t* keys, uint32_t* pos) {
+    __shared__ uint32_t part[16][64];
+    const int32_t n = rows_here(d_n, cap), first = (int32_t)blockIdx.x * 64;
+    if (first >= n) return;
+    const int32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6)), i = first + lane;
+    const uint32_t* key = reinterpret_cast<const uint32_t*>(ids);       // ids outside the table are larger than all inside, as unsigned
+    const uint32_t mine = i < n ? key[i] : 0u;
+    const int32_t each = (int32_t)ceil_div(n, 16 * 16) * 16, lo = min(n, wave * each), hi = min(n, lo + each);
+    uint32_t before = 0;
+    // equal ids count where they stand earlier: all of those left of this block's positions, none right of it, and among the block's own by lane
+    const int32_t a = min(max(lo, first), hi), b = min(max(lo, first + 64), hi);
+#pragma unroll 16
+    for (int32_t j = lo; j < a; ++j) before += key[j] <= mine;
+    for (int32_t j = a; j < b; ++j) before += key[j] < mine || (key[j] == mine && j < i);
+#pragma unroll 16
+    for (int32_t j = b; j < hi; ++j) before += key[j] < mine;
+    part[wave][lane] = before;
+    __syncthreads();
+    if (wave == 0 && i < n) {
+        uint32_t at = 0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) at += part[w][lane];
+        keys[at] = mine;
+        pos[at] = (uint32_t)i;
+    }
+}
+
+// What the first pass of the radix sort reads: ids outside the table, and positions that are not there, come last.
+struct IdSource {
+    const int32_t* ids;
+    const int32_t* d_n;
+    int32_t cap;
+    uint32_t none;
+    __device__ __forceinline__ uint32_t key(int64_t i) const { return i < rows_here(d_n, cap) ? min((uint32_t)ids[i], none) : none; }
+    __device__ __forceinline__ void keys_checked(int64_t i, int here, uint32_t (&k)[RS_ITEMS]) const {
+#pragma unroll
+        for (int it = 0; it < RS_ITEMS; ++it) k[it] = it < here ? key(i + it) : 0u;
+    }
+    __device__ __forceinline__ uint32_t val(int64_t i) const { return (uint32_t)i; }
+};
+
+struct EmbedSums {
+    const uint32_t* keys;
+    const uint32_t* pos;
+    const int32_t* d_n;
+    int32_t cap;
+    float scale;
+    bool accumulate;
+    RowsOf grad, table;
+    int64_t n_rows;
+    int32_t dim;
+    float* parts;       // [chunks][2][dim]: the sum of an id that began in an earlier chunk, and of one that goes on in the next
+};
+
+template <typename T, int W>
+__global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t chunks, int32_t g_log2, int32_t col_tiles, uint32_t sum_blocks) {
+    const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id();
+    if (blockIdx.x >= sum_blocks) {     // rows without an id: 16 to a wavefront
+        const int64_t v0 = ((int64_t)(blockIdx.x - sum_blocks) * 4 + (threadIdx.x >> 6)) * 16;
+        if (v0 >= a.n_rows) return;
+        const int64_t v = v0 + (lane & 15);
+        int32_t lo = 0, hi = n;
+        while (lo < hi) {
+            const int32_t mid = (lo + hi) >> 1;
+            if ((int64_t)a.keys[mid] < v) lo = mid + 1; else hi = mid;
         }
+        uint32_t empty = (uint32_t)__ballot(v < a.n_rows && !(lo < n && (int64_t)a.keys[lo] == v)) & 0xffffu;
+        Run<float, 4> zero;
+        const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        zero.set(z);
+        while (empty) {
+            const int32_t at = __builtin_ctz(empty);
+            empty &= empty - 1;
+            float* row = a.table.row<float>(v0 + at);
+            for (int32_t c = lane * 4; c < a.dim; c += 256) zero.store(row + c, a.dim - c);
+        }
+        return;
+    }
+    const int32_t groups = 64 >> g_log2, u = lane & ((1 << g_log2) - 1);
+    const int64_t item = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * groups + (lane >> g_log2);
+    const int64_t chunk = item / col_tiles;
+    const int32_t col = ((int32_t)(item % col_tiles) * 64 + u) * W, width = a.dim - col;
+    const int64_t e0 = chunk * EMBED_CHUNK;
+    if (chunk >= chunks || e0 >= n || width <= 0) return;
+    const int32_t len = (int32_t)min((int64_t)EMBED_CHUNK, n - e0);
+    const uint32_t before = chunk ? a.keys[e0 - 1] : ~0u, after = e0 + len < n ? a.keys[e0 + len] : ~0u;
+    float* const parts = a.parts + chunk * 2 * a.dim + col;
+    float acc[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) acc[w] = 0.0f;
+    auto flush = [&](uint32_t key, int32_t start, int32_t end) {
+        if (key >= (uint64_t)a.n_rows) return;
+        Run<float, W> out;
+        if (start == 0 && key == before) { out.set(acc); return out.store(parts, width); }
+        if (end == len && key == after) { out.set(acc); return out.store(parts + a.dim, width); }
+        float* to = a.table.row<float>(key) + col;
+        float f[W];
+        if (a.accumulate) {
+            out.load(to, width, 0.0f);
+            out.get(f);
+#pragma unroll
+            for (int w = 0; w < W; ++w) f[w] += a.scale * acc[w];
+        } else {
+#pragma unroll
+            for (int w = 0; w < W; ++w) f[w] = a.scale * acc[w];
+        }
+        out.set(f);
+        out.store(to, width);
+    };
+    uint32_t cur = a.keys[e0];
+    int32_t start = 0;
+    constexpr int UNR = 8;              // rows requested before the first is added
+    for (int32_t e = 0; e < len; e += UNR) {
+        uint32_t key[UNR], p[UNR];
+        Run<T, W> r[UNR];
+#pragma unroll
+        for (int k = 0; k < UNR; ++k) {
+            key[k] = e + k < len ? a.keys[e0 + e + k] : ~0u;
+            p[k] = e + k < len ? a.pos[e0 + e + k] : 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < UNR; ++k)
+            if (key[k] < (uint64_t)a.n_rows) r[k].load(a.grad.row<T>(p[k]) + col, width, from_f32<T>(0.0f));
+#pragma unroll
+        for (int k = 0; k < UNR; ++k) {
+            if (e + k >= len) break;
+            if (key[k] != cur) {
+                flush(cur, start, e + k);
+                cur = key[k];
+                start = e + k;
+#pragma unroll
+                for (int w = 0; w < W; ++w) acc[w] = 0.0f;
+            }
+            if (cur < (uint64_t)a.n_rows) {
+                float f[W];
+                r[k].get(f);
+#pragma unroll
+                for (int w = 0; w < W; ++w) acc[w] += f[w];
+            }
+        }
+    }
+    flush(cur, start, len);
+}
+
+// Adds up the sums that reach over borders: the chunk where such an id begins owns it. Four wavefronts share the later chunks' parts.
+__global__ void __launch_bounds__(256) embed_join_kernel(EmbedSums a, int64_t chunks) {
+    __shared__ float share[4][64][4];
+    const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id(), wave = (int32_t)(threadIdx.x >> 6), col = ((int32_t)blockIdx.y * 64 + lane) * 4, width = a.dim - col;
+    const int64_t here = min(chunks, ceil_div(n, EMBED_CHUNK));
+    for (int64_t c = blockIdx.x; c + 1 < here; c += gridDim.x) {
+        const uint32_t key = a.keys[(c + 1) * EMBED_CHUNK - 1];
+        if (key >= (uint64_t)a.n_rows || a.keys[(c + 1) * EMBED_CHUNK] != key) continue;
+        if (c > 0 && a.keys[c * EMBED_CHUNK] == key && a.keys[c * EMBED_CHUNK - 1] == key) continue;
+        int64_t lo = c + 2, hi = here;          // the first chunk that does not begin with this id
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (a.keys[mid * EMBED_CHUNK] == key) lo = mid + 1; else hi = mid;
+        }
+        const int64_t parts = lo - c, each = ceil_div(parts, 4), p0 = min(parts, wave * each), p1 = min(parts, p0 + each);
+        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (width > 0) {
+#pragma unroll 4
+            for (int64_t p = p0; p < p1; ++p) {
+                Run<float, 4> r;
+                r.load(a.parts + ((c + p) * 2 + (p == 0)) * a.dim + col, width, 0.0f);
+                float f[4];
+                r.get(f);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) acc[w] += f[w];
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) share[wave][lane][w] = acc[w];
+        __syncthreads();
+        if (wave == 0 && width > 0) {
+            float* to = a.table.row<float>(key) + col;
+            Run<float, 4> out;
+            float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (a.accumulate) { out.load(to, width, 0.0f); out.get(f); }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) f[w] += a.scale * ((share[0][lane][w] + share[1][lane][w]) + (share[2][lane][w] + share[3][lane][w]));
+            out.set(f);
+            out.store(to, width);
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T>
+static void launch_sums(const EmbedSums& a, int64_t chunks, hipStream_t st) {
+    constexpr int W = 16 / (int)sizeof(T);
+    const int32_t units = (int32_t)ceil_div(a.dim, W), col_tiles = (int32_t)ceil_div(units, 64);
+    int g_log2 = 0;
+    while ((1 << g_log2) < units && g_log2 < 6) ++g_log2;
+    const int64_t sum_blocks = ceil_div(ceil_div(chunks * col_tiles, 64 >> g_log2), 4), zero_blocks = a.accumulate ? 0 : ceil_div(a.n_rows, 64);
+    if (sum_blocks + zero_blocks)
+        hipLaunchKernelGGL((embed_sums_kernel<T, W>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks);
 }
 
 }  // namespace no
@@ -58,24 +270,45 @@ extern "C" int32_t no_embed_fwd(const void* d_table, no_dtype dt, int64_t n_rows
 
 extern "C" size_t no_embed_ws_bytes(int32_t n_ids_cap, int32_t dim) {
     if (n_ids_cap < 0 || dim < 1) return 0;
-    return 16;
+    return EmbedPlan(n_ids_cap, dim).total;
 }
 
 extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t grad_stride_bytes, const int32_t* d_ids, const int32_t* d_n_ids,
                                 int32_t n_ids_cap, float scale, int32_t accumulate, float* d_grad_table, int64_t n_rows, int32_t dim,
                                 int64_t table_stride_bytes, void* d_ws, size_t ws_bytes, void* stream) {
     clear_error();
-    NO_REQUIRE(dt == NO_F32 || dt == NO_BF16, NO_ERR_INVALID_ARG, "no_embed_bwd: gradients are NO_F32 or NO_BF16");
-    NO_REQUIRE(n_rows >= 1 && n_rows <= INT32_MAX && dim >= 1 && n_ids_cap >= 0, NO_ERR_INVALID_ARG, "no_embed_bwd: bad sizes");
-    NO_CHECK(check_rows("no_embed_bwd", "grad_out", d_grad_out, dt, n_ids_cap, dim, grad_stride_bytes));
-    NO_CHECK(check_rows("no_embed_bwd", "grad_table", d_grad_table, NO_F32, n_rows, dim, table_stride_bytes));
-    NO_REQUIRE(d_ids || n_ids_cap == 0, NO_ERR_INVALID_ARG, "no_embed_bwd: ids are NULL");
-    NO_REQUIRE(d_ws && (uintptr_t)d_ws % 16 == 0, NO_ERR_INVALID_ARG, "no_embed_bwd: the workspace is NULL or misaligned");
-    NO_REQUIRE(ws_bytes >= no_embed_ws_bytes(n_ids_cap, dim), NO_ERR_CAPACITY, "no_embed_bwd: workspace too small");
-    const dim3 grid((unsigned)(n_rows < 65536 ? n_rows : 65536));
-    const RowsOf grad = rows_of(d_grad_out, grad_stride_bytes), table = rows_of(d_grad_table, table_stride_bytes);
-#define NO_EMBED(T) hipLaunchKernelGGL(embed_bwd_kernel<T>, grid, dim3(256), 0, (hipStream_t)stream, grad, d_ids, d_n_ids, n_ids_cap, scale, accumulate != 0, table, n_rows, dim)
-    if (dt == NO_F32) NO_EMBED(float); else NO_EMBED(bf16_t);
-#undef NO_EMBED
-    return launch_status("no_embed_bwd");
+    const char* who = "no_embed_bwd";
+    NO_REQUIRE(dt == NO_F32 || dt == NO_BF16, NO_ERR_INVALID_ARG, "%s: gradients are NO_F32 or NO_BF16", who);
+    NO_REQUIRE(n_rows >= 1 && n_rows <= INT32_MAX && dim >= 1 && n_ids_cap >= 0, NO_ERR_INVALID_ARG, "%s: bad sizes", who);
+    NO_CHECK(check_rows(who, "grad_out", d_grad_out, dt, n_ids_cap, dim, grad_stride_bytes));
+    NO_CHECK(check_rows(who, "grad_table", d_grad_table, NO_F32, n_rows, dim, table_stride_bytes));
+    NO_REQUIRE(d_ids || n_ids_cap == 0, NO_ERR_INVALID_ARG, "%s: ids are NULL", who);
+    NO_REQUIRE(d_ws && (uintptr_t)d_ws % 16 == 0, NO_ERR_INVALID_ARG, "%s: the workspace is NULL or misaligned", who);
+    const EmbedPlan plan(n_ids_cap, dim);
+    NO_REQUIRE(ws_bytes >= plan.total, NO_ERR_CAPACITY, "%s: workspace too small", who);
+    hipStream_t st = (hipStream_t)stream;
+    char* ws = (char*)d_ws;
+    uint32_t *keys = (uint32_t*)(ws + plan.keys), *pos = (uint32_t*)(ws + plan.pos);
+    if (n_ids_cap > 0) {
+        if (plan.by_rank) {
+            hipLaunchKernelGGL(embed_rank_kernel, dim3((unsigned)ceil_div(n_ids_cap, 64)), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, keys, pos);
+        } else {
+            const int bits = ilog2_ceil((uint64_t)n_rows + 1), passes = radix_passes(bits), digit = radix_digit_bits(bits);
+            const RadixPlan radix(n_ids_cap);
+            uint32_t *k[2] = {keys, (uint32_t*)(ws + plan.keys_tmp)}, *v[2] = {pos, (uint32_t*)(ws + plan.pos_tmp)};
+            int to = (passes & 1) ? 0 : 1;          // the last pass ends in the first pair of arrays
+            for (int p = 0; p < passes; ++p, to ^= 1) {
+                const int shift = p * digit, width = bits - shift < digit ? bits - shift : digit;
+                if (p == 0) NO_CHECK(radix_pass(IdSource{d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows}, radix, shift, width, k[to], v[to], ws + plan.sort_ws, st));
+                else NO_CHECK(radix_pass(PairArrays{k[to ^ 1], v[to ^ 1]}, radix, shift, width, k[to], v[to], ws + plan.sort_ws, st));
+            }
+        }
+    }
+    const EmbedSums a{keys, pos, d_n_ids, n_ids_cap, scale, accumulate != 0, rows_of(d_grad_out, grad_stride_bytes), rows_of(d_grad_table, table_stride_bytes), n_rows, dim,
+                      (float*)(ws + plan.parts)};
+    if (dt == NO_F32) launch_sums<float>(a, plan.chunks, st);
+    else launch_sums<bf16_t>(a, plan.chunks, st);
+    if (plan.chunks > 1)
+        hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(plan.chunks - 1 < 1024 ? plan.chunks - 1 : 1024), (unsigned)ceil_div(dim, 256)), dim3(256), 0, st, a, plan.chunks);
+    return launch_status(who);
 }

@@ -36,6 +36,75 @@ struct RowsOf {
 };
 static inline RowsOf rows_of(const void* p, int64_t stride) { return RowsOf{(char*)p, stride}; }
 
+// W consecutive values of a row, `here` of which are there (the others read as `fill` and are not written). A whole run goes in 16-byte (or
+// narrower, for short runs) requests at any alignment of an element: global memory takes unaligned requests on this chip, so that odd row
+// widths, whose rows begin anywhere, take the same path.
+template <int BYTES> struct Chunk;
+template <> struct Chunk<4> { typedef uint32_t raw __attribute__((aligned(1), may_alias)); typedef uint32_t val; };
+template <> struct Chunk<8> { typedef uint32_t val __attribute__((ext_vector_type(2))); typedef val raw __attribute__((aligned(1), may_alias)); };
+template <> struct Chunk<16> { typedef uint32_t val __attribute__((ext_vector_type(4))); typedef val raw __attribute__((aligned(1), may_alias)); };
+
+template <typename T, int W>
+struct Run {
+    static constexpr int BYTES = W * (int)sizeof(T), REQ = BYTES < 16 ? BYTES : 16, N = BYTES / REQ, PER = W / N;
+    typedef typename Chunk<REQ>::val val;
+    typedef typename Chunk<REQ>::raw raw;
+    val v[N];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = reinterpret_cast<const raw*>(p)[i];
+    }
+    __device__ __forceinline__ void load(const T* p, int here, T fill) {
+        if (here >= W) return load(p);
+        T e[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) e[i] = i < here ? p[i] : fill;
+        __builtin_memcpy(v, e, BYTES);
+    }
+    __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) reinterpret_cast<raw*>(p)[i] = v[i];
+    }
+    __device__ __forceinline__ void store(T* p, int here) const {
+        if (here >= W) return store(p);
+        T e[W];
+        __builtin_memcpy(e, v, BYTES);
+#pragma unroll
+        for (int i = 0; i < W; ++i) if (i < here) p[i] = e[i];
+    }
+    __device__ __forceinline__ void get(float (&f)[W]) const {
+        if constexpr (sizeof(T) == 1) {
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            uint32_t w[BYTES / 4];
+            __builtin_memcpy(w, v, BYTES);
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) {
+                const f2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
+                f[4 * i] = a.x; f[4 * i + 1] = a.y; f[4 * i + 2] = b.x; f[4 * i + 3] = b.y;
+            }
+        } else {
+            T e[W];
+            __builtin_memcpy(e, v, BYTES);
+#pragma unroll
+            for (int i = 0; i < W; ++i) f[i] = to_f32(e[i]);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&f)[W]) {
+        if constexpr (sizeof(T) == 1) {
+            uint32_t w[BYTES / 4];
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i)
+                w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2], f[4 * i + 3], __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i], f[4 * i + 1], 0, false), true);
+            __builtin_memcpy(v, w, BYTES);
+        } else {
+            T e[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) e[i] = from_f32<T>(f[i]);
+            __builtin_memcpy(v, e, BYTES);
+        }
+    }
+};
+
 // What every call checks of a row matrix. The stride counts from the second row on.
 static inline int32_t check_rows(const char* who, const char* what, const void* p, no_dtype dt, int64_t n, int64_t dim, int64_t stride) {
     const int32_t es = size_of(dt);

@@ -209,6 +209,24 @@ def test_embed_bwd_keeps_infinities_in_their_rows():
     assert torch.equal(table.cpu().nan_to_num(-1.0), want.nan_to_num(-1.0))
 
 
+def test_embed_bwd_far_rows():
+    """A gradient row and table rows whose offsets pass 2^32 bytes."""
+    b = nb()
+    n, v, dim = 530_000, 530_000, 2050
+    grad = torch.zeros((n, dim), device="cuda")
+    ids = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    at = torch.tensor([0, 5, 523_777, 523_776, 262_143, n - 1], device="cuda")
+    grad[at] = randn((6, dim), rng(3))
+    ids[at] = torch.tensor([v - 1, 7, v - 1, 524_000, 3, 523_777], dtype=torch.int32, device="cuda")
+    table = torch.full((v, dim), MARK, device="cuda")
+    b.no_embed_bwd(grad, ids, table, ws_of(b.no_embed_ws_bytes(n, dim)))
+    rows = torch.tensor([v - 1, 7, 524_000, 3, 523_777], device="cuda")
+    want = torch.stack([grad[0] + grad[523_777], grad[5], grad[523_776], grad[262_143], grad[n - 1]])
+    assert torch.equal(table[rows], want)
+    table[rows] = 0
+    assert not table.any()
+
+
 # ------------------------------------------------------------------------------------------------------- rmsnorm
 
 NORM_SIZES = [(1, 1, 0, 0), (1, 64, 0, 0), (3, 5, 2, 1), (7, 63, 0, 0), (64, 100, 4, 4), (100, 602, 0, 0), (65, 256, 0, 0), (1000, 128, 0, 0), (33, 1025, 3, 1),
