@@ -4,16 +4,55 @@
 
 namespace no {
 
-template <typename T, typename O>
-__global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_rows, int32_t dim, const float* row_scale, const int32_t* ids,
-                                                        const int32_t* d_n, int32_t cap, float scale, RowsOf out) {
-    const int32_t n = rows_here(d_n, cap);
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const int32_t id = ids[i];
+// A group of lanes (a power of two, at most 64) copies a row in runs of W values, W such that the wider side moves 16 or 32 bytes a lane. The next
+// row's id is requested before this row's values, so that a row costs one round trip, its scale beside it.
+template <typename T, typename O, int W, int UNR>
+__global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_rows, int32_t dim, const float* __restrict__ row_scale, const int32_t* __restrict__ ids,
+                                                        const int32_t* d_n, int32_t cap, float scale, RowsOf out, int32_t units, int32_t g_log2) {
+    const int32_t n = rows_here(d_n, cap), lane = lane_id(), g = 1 << g_log2, sub = lane >> g_log2, u0 = lane & (g - 1), rows = 64 >> g_log2;
+    const int64_t wave = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 6, stride = (int64_t)gridDim.x * 4 * rows;
+    int64_t r = wave * rows + sub;
+    int32_t id = r < n ? ids[r] : -1;
+    for (; r - sub < n; r += stride) {
+        const int32_t next = r + stride < n ? ids[r + stride] : -1;
         const bool there = id >= 0 && id < n_rows;
         const float by = there ? (row_scale ? scale * row_scale[id] : scale) : 0.0f;
-        for (int32_t c = threadIdx.x; c < dim; c += 256) out.row<O>(i)[c] = there ? from_f32<O>(to_f32(table.row<T>(id)[c]) * by) : from_f32<O>(0.0f);
+        const T* src = table.row<T>(there ? id : 0);
+        for (int32_t ub = u0; ub < units && r < n; ub += g * UNR) {
+            Run<T, W> v[UNR];
+#pragma unroll
+            for (int j = 0; j < UNR; ++j) {
+                const int32_t c = (ub + j * g) * W;
+                if (there && c < dim) v[j].load(src + c, dim - c, from_f32<T>(0.0f));
+            }
+#pragma unroll
+            for (int j = 0; j < UNR; ++j) {
+                const int32_t c = (ub + j * g) * W;
+                if (c >= dim) break;
+                float f[W];
+                v[j].get(f);
+#pragma unroll
+                for (int w = 0; w < W; ++w) f[w] = there ? f[w] * by : 0.0f;
+                Run<O, W> o;
+                o.set(f);
+                o.store(out.row<O>(r) + c, dim - c);
+            }
+        }
+        id = next;
     }
+}
+
+template <typename T, typename O>
+static void launch_embed(const RowsOf& table, int64_t n_rows, int32_t dim, const float* row_scale, const int32_t* ids, const int32_t* d_n, int32_t cap, float scale,
+                         const RowsOf& out, hipStream_t st) {
+    constexpr int W = sizeof(T) == 4 && sizeof(O) == 4 ? 4 : 8;
+    const int32_t units = (int32_t)ceil_div(dim, W);
+    int g_log2 = 0;
+    while ((1 << g_log2) < units && g_log2 < 6) ++g_log2;
+    int64_t blocks = ceil_div(ceil_div(cap, 64 >> g_log2), 4);
+    if (blocks > 2048) blocks = 2048;
+    if (units > 64) hipLaunchKernelGGL((embed_fwd_kernel<T, O, W, 4>), dim3((unsigned)blocks), dim3(256), 0, st, table, n_rows, dim, row_scale, ids, d_n, cap, scale, out, units, g_log2);
+    else hipLaunchKernelGGL((embed_fwd_kernel<T, O, W, 1>), dim3((unsigned)blocks), dim3(256), 0, st, table, n_rows, dim, row_scale, ids, d_n, cap, scale, out, units, g_log2);
 }
 
 // ------------------------------------------------------------------------------------------------------- gradient
@@ -260,8 +299,7 @@ extern "C" int32_t no_embed_fwd(const void* d_table, no_dtype dt, int64_t n_rows
     if (n_ids_cap == 0) return NO_OK;
     NO_REQUIRE(d_ids, NO_ERR_INVALID_ARG, "no_embed_fwd: ids are NULL");
     const RowsOf table = rows_of(d_table, table_stride_bytes), out = rows_of(d_out, out_stride_bytes);
-    const dim3 grid((unsigned)(n_ids_cap < 65536 ? n_ids_cap : 65536));
-#define NO_EMBED(T, O) hipLaunchKernelGGL((embed_fwd_kernel<T, O>), grid, dim3(256), 0, (hipStream_t)stream, table, n_rows, dim, d_row_scale, d_ids, d_n_ids, n_ids_cap, scale, out)
+#define NO_EMBED(T, O) launch_embed<T, O>(table, n_rows, dim, d_row_scale, d_ids, d_n_ids, n_ids_cap, scale, out, (hipStream_t)stream)
     if (dt_out == NO_F32) { if (dt == NO_F32) NO_EMBED(float, float); else if (dt == NO_BF16) NO_EMBED(bf16_t, float); else NO_EMBED(e4m3_t, float); }
     else { if (dt == NO_F32) NO_EMBED(float, bf16_t); else if (dt == NO_BF16) NO_EMBED(bf16_t, bf16_t); else NO_EMBED(e4m3_t, bf16_t); }
 #undef NO_EMBED

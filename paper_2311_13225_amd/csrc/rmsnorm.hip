@@ -5,70 +5,257 @@ namespace no {
 
 constexpr float E4M3_MOST = 448.0f, SMALLEST_MOST = 0x1p-100f;
 
-template <typename T, typename Y>
-__global__ void __launch_bounds__(256) rmsnorm_fwd_kernel(RowsOf x, RowsOf residual, const float* weight, float eps, const int32_t* d_n, int32_t cap,
-                                                          int32_t dim, RowsOf sum, RowsOf y, float* row_scale, float* rstd_out) {
-    __shared__ float smem[4];
-    const int32_t n = rows_here(d_n, cap);
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-        auto s_at = [&](int32_t c) {
-            const float v = to_f32(x.row<T>(i)[c]);
-            return residual.p ? to_f32(from_f32<T>(v + to_f32(residual.row<T>(i)[c]))) : v;
-        };
-        float ss = 0.0f;
-        for (int32_t c = threadIdx.x; c < dim; c += 256) { const float v = s_at(c); ss += v * v; }
-        ss = block_sum<float, 256>(ss, smem);
-        const float rstd = 1.0f / sqrtf(ss / (float)dim + eps);
-        float most = 0.0f;
-        for (int32_t c = threadIdx.x; c < dim; c += 256) most = fmaxf(most, fabsf(s_at(c) * rstd * (weight ? weight[c] : 1.0f)));
-        for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-        if (lane_id() == 0) smem[threadIdx.x >> 6] = most;
-        __syncthreads();
-        most = fmaxf(fmaxf(smem[0], smem[1]), fmaxf(smem[2], smem[3]));
-        __syncthreads();
-        float scale = 1.0f;
-        if constexpr (TypeOf<Y>::code == NO_E4M3) scale = ss < INFINITY ? fmaxf(most, SMALLEST_MOST) / E4M3_MOST : NAN;
-        for (int32_t c = threadIdx.x; c < dim; c += 256) {
-            const float v = s_at(c);
-            if (sum.p) sum.row<T>(i)[c] = from_f32<T>(v);
-            float o = v * rstd * (weight ? weight[c] : 1.0f);
-            if constexpr (TypeOf<Y>::code == NO_E4M3) o = o / scale;
-            y.row<Y>(i)[c] = from_f32<Y>(o);
+// A team of lanes holds a row in registers, U runs of 16 bytes a lane, and walks rows with a stride of all teams, the weights in registers too where they fit. The
+// row is read once and written once.
+template <typename T, typename Y, int TEAM, int THREADS, int U>
+__global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf residual, const float* __restrict__ weight, float eps, const int32_t* d_n, int32_t cap,
+                                                              int32_t dim, RowsOf sum, RowsOf y, float* row_scale, float* rstd_out) {
+    constexpr int W = 16 / (int)sizeof(T), PER_BLOCK = THREADS / TEAM;
+    constexpr bool KEEP = U * W <= 32;          // weights in registers
+    __shared__ float smem[2 * THREADS / 64];
+    Team<TEAM, THREADS> team(smem);
+    const int32_t n = rows_here(d_n, cap), t = team.lane();
+    float wk[KEEP ? U : 1][W];
+    auto weights = [&](int u, float (&f)[W]) {
+        const int32_t c = (t + u * TEAM) * W;
+        if (weight) {
+            Run<float, W> r;
+            r.load(weight + min(c, dim), dim - c, 0.0f);
+            r.get(f);
+        } else {
+#pragma unroll
+            for (int w = 0; w < W; ++w) f[w] = 1.0f;
         }
-        if (threadIdx.x == 0) {
+    };
+    if constexpr (KEEP)
+#pragma unroll
+        for (int u = 0; u < U; ++u) weights(u, wk[u]);
+    for (int64_t i = (int64_t)blockIdx.x * PER_BLOCK + team.index(); i < n; i += (int64_t)gridDim.x * PER_BLOCK) {
+        Run<T, W> s[U], r[U];
+        const T zero = from_f32<T>(0.0f);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t c = (t + u * TEAM) * W;
+            s[u].load(x.row<T>(i) + min(c, dim), dim - c, zero);
+            if (residual.p) r[u].load(residual.row<T>(i) + min(c, dim), dim - c, zero);
+        }
+        float ss = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[W];
+            s[u].get(f);
+            if (residual.p) {
+                float g[W];
+                r[u].get(g);
+#pragma unroll
+                for (int w = 0; w < W; ++w) f[w] += g[w];
+                s[u].set(f);
+                s[u].get(f);
+            }
+#pragma unroll
+            for (int w = 0; w < W; ++w) ss += f[w] * f[w];
+        }
+        if (sum.p)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t c = (t + u * TEAM) * W;
+                if (c < dim) s[u].store(sum.row<T>(i) + c, dim - c);
+            }
+        ss = team.sum(ss);
+        const float rstd = 1.0f / sqrtf(ss / (float)dim + eps);
+        auto values = [&](int u, float (&f)[W]) {
+            float k[W];
+            s[u].get(f);
+            if constexpr (!KEEP) weights(u, k);
+#pragma unroll
+            for (int w = 0; w < W; ++w) f[w] = f[w] * rstd * (KEEP ? wk[KEEP ? u : 0][w] : k[w]);
+        };
+        float scale = 1.0f, inv = 1.0f;
+        if constexpr (TypeOf<Y>::code == NO_E4M3) {
+            float most = 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float f[W];
+                values(u, f);
+#pragma unroll
+                for (int w = 0; w < W; ++w) most = fmaxf(most, fabsf(f[w]));
+            }
+            most = team.max(most);
+            scale = ss < INFINITY ? fmaxf(most, SMALLEST_MOST) / E4M3_MOST : NAN;
+            inv = 1.0f / scale;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t c = (t + u * TEAM) * W;
+            if (c < dim) {
+                float f[W];
+                values(u, f);
+                if constexpr (TypeOf<Y>::code == NO_E4M3)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) f[w] *= inv;
+                Run<Y, W> o;
+                o.set(f);
+                o.store(y.row<Y>(i) + c, dim - c);
+            }
+        }
+        if (t == 0) {
             if (rstd_out) rstd_out[i] = rstd;
             if (TypeOf<Y>::code == NO_E4M3) row_scale[i] = scale;
         }
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) rmsnorm_grad_weight_kernel(RowsOf s, const float* rstd, RowsOf grad_y, const int32_t* d_n, int32_t cap,
-                                                                  int32_t dim, float* grad_weight) {
-    const int32_t n = rows_here(d_n, cap), c = (int32_t)(blockIdx.x * 256 + threadIdx.x);
-    if (c >= dim) return;
-    double sum = 0.0;
-    for (int64_t i = 0; i < n; ++i) sum += to_f32(grad_y.row<T>(i)[c]) * (to_f32(s.row<T>(i)[c]) * rstd[i]);
-    grad_weight[c] = (float)sum;
+// ------------------------------------------------------------------------------------------------------- gradients
+//
+// The weight's gradient is a sum over rows for every column: a team adds its rows' terms in registers while it makes their input gradients, a block joins its
+// teams' sums in LDS and stores one row of parts, and a second launch adds the blocks' parts in order.
+
+constexpr int32_t NORM_PARTS = 512;     // rows of parts, at most
+
+template <typename T, int TEAM, int THREADS, int U>
+__global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(RowsOf s, const float* __restrict__ weight, const float* __restrict__ rstd, RowsOf grad_y, RowsOf grad_sum,
+                                                              const int32_t* d_n, int32_t cap, int32_t dim, RowsOf grad_x, float* parts, float* grad_weight) {
+    constexpr int W = 16 / (int)sizeof(T), PER_BLOCK = THREADS / TEAM;
+    __shared__ float smem[2 * THREADS / 64];
+    __shared__ float joined[PER_BLOCK > 1 ? U * TEAM * W : 1];
+    Team<TEAM, THREADS> team(smem);
+    const int32_t n = rows_here(d_n, cap), t = team.lane();
+    const T zero = from_f32<T>(0.0f);
+    float wk[U][W], dw[U][W];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t c = (t + u * TEAM) * W;
+        Run<float, W> r;
+        if (weight) { r.load(weight + min(c, dim), dim - c, 0.0f); r.get(wk[u]); }
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (!weight) wk[u][w] = 1.0f;
+            dw[u][w] = 0.0f;
+        }
+    }
+    for (int64_t i = (int64_t)blockIdx.x * PER_BLOCK + team.index(); i < n; i += (int64_t)gridDim.x * PER_BLOCK) {
+        Run<T, W> rs[U], rg[U], ra[U];
+        const float r = rstd[i];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t c = (t + u * TEAM) * W, at = min(c, dim);
+            rs[u].load(s.row<T>(i) + at, dim - c, zero);
+            rg[u].load(grad_y.row<T>(i) + at, dim - c, zero);
+            if (grad_sum.p) ra[u].load(grad_sum.row<T>(i) + at, dim - c, zero);
+        }
+        float dot = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[W], g[W];
+            rs[u].get(v);
+            rg[u].get(g);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float gu = g[w] * (v[w] * r);
+                dw[u][w] += gu;
+                dot += gu * wk[u][w];
+            }
+        }
+        const float mean = team.sum(dot) / (float)dim;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t c = (t + u * TEAM) * W;
+            if (c < dim) {
+                float v[W], g[W], a[W];
+                rs[u].get(v);
+                rg[u].get(g);
+                if (grad_sum.p) ra[u].get(a);
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const float dx = r * (g[w] * wk[u][w] - v[w] * r * mean);
+                    g[w] = grad_sum.p ? dx + a[w] : dx;
+                }
+                Run<T, W> o;
+                o.set(g);
+                o.store(grad_x.row<T>(i) + c, dim - c);
+            }
+        }
+    }
+    if (!grad_weight) return;
+    if constexpr (PER_BLOCK > 1) {      // the block's teams in turn
+        for (int k = 0; k < PER_BLOCK; ++k) {
+            if (team.index() == k)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        float& to = joined[((t + u * TEAM) * W) + w];
+                        to = k ? to + dw[u][w] : dw[u][w];
+                        if (k == PER_BLOCK - 1) dw[u][w] = to;
+                    }
+            __syncthreads();
+        }
+        if (team.index() != PER_BLOCK - 1) return;
+    }
+    float* to = gridDim.x == 1 ? grad_weight : parts + (int64_t)blockIdx.x * dim;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t c = (t + u * TEAM) * W;
+        if (c < dim) {
+            Run<float, W> o;
+            o.set(dw[u]);
+            o.store(to + c, dim - c);
+        }
+    }
 }
 
+// Rows too wide for registers: read twice.
 template <typename T>
-__global__ void __launch_bounds__(256) rmsnorm_grad_x_kernel(RowsOf s, const float* weight, const float* rstd, RowsOf grad_y, RowsOf grad_sum,
-                                                             const int32_t* d_n, int32_t cap, int32_t dim, RowsOf grad_x) {
-    __shared__ float smem[4];
+__global__ void __launch_bounds__(1024) rmsnorm_bwd_wide_kernel(RowsOf s, const float* __restrict__ weight, const float* __restrict__ rstd, RowsOf grad_y, RowsOf grad_sum,
+                                                                const int32_t* d_n, int32_t cap, int32_t dim, RowsOf grad_x) {
+    __shared__ float smem[32];
+    Team<1024, 1024> team(smem);
     const int32_t n = rows_here(d_n, cap);
     for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
         const float r = rstd[i];
         float dot = 0.0f;
-        for (int32_t c = threadIdx.x; c < dim; c += 256)
-            dot += to_f32(grad_y.row<T>(i)[c]) * (weight ? weight[c] : 1.0f) * (to_f32(s.row<T>(i)[c]) * r);
-        const float mean = block_sum<float, 256>(dot, smem) / (float)dim;
-        for (int32_t c = threadIdx.x; c < dim; c += 256) {
-            const float wg = to_f32(grad_y.row<T>(i)[c]) * (weight ? weight[c] : 1.0f);
-            const float dx = r * (wg - to_f32(s.row<T>(i)[c]) * r * mean);
+        for (int32_t c = threadIdx.x; c < dim; c += 1024)
+            dot += to_f32(grad_y.row<T>(i)[c]) * (to_f32(s.row<T>(i)[c]) * r) * (weight ? weight[c] : 1.0f);
+        const float mean = team.sum(dot) / (float)dim;
+        for (int32_t c = threadIdx.x; c < dim; c += 1024) {
+            const float dx = r * (to_f32(grad_y.row<T>(i)[c]) * (weight ? weight[c] : 1.0f) - to_f32(s.row<T>(i)[c]) * r * mean);
             grad_x.row<T>(i)[c] = from_f32<T>(grad_sum.p ? dx + to_f32(grad_sum.row<T>(i)[c]) : dx);
         }
     }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) rmsnorm_wide_parts_kernel(RowsOf s, const float* __restrict__ rstd, RowsOf grad_y, const int32_t* d_n, int32_t cap, int32_t dim,
+                                                                 float* parts) {
+    const int32_t n = rows_here(d_n, cap), c = (int32_t)(blockIdx.x * 256 + threadIdx.x);
+    if (c >= dim) return;
+    float sum = 0.0f;
+    for (int64_t i = blockIdx.y; i < n; i += gridDim.y) sum += to_f32(grad_y.row<T>(i)[c]) * (to_f32(s.row<T>(i)[c]) * rstd[i]);
+    parts[(int64_t)blockIdx.y * dim + c] = sum;
+}
+
+// A column a lane, the parts shared by a block's sixteen wavefronts.
+__global__ void __launch_bounds__(1024) rmsnorm_join_kernel(const float* __restrict__ parts, int32_t n_parts, int32_t dim, float* grad_weight) {
+    __shared__ float share[16][64];
+    const int32_t lane = lane_id(), wave = (int32_t)(threadIdx.x >> 6), c = (int32_t)blockIdx.x * 64 + lane;
+    float sum = 0.0f;
+    if (c < dim) {
+#pragma unroll 8
+        for (int32_t p = wave; p < n_parts; p += 16) sum += parts[(int64_t)p * dim + c];
+    }
+    share[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < dim) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) sum += share[w][lane];
+        grad_weight[c] = sum;
+    }
+}
+
+// Blocks for n rows: at most what fills the chip, so that a team walks several rows with the weights it holds.
+static inline int64_t norm_blocks(int64_t n, int per_block, int64_t most) {
+    const int64_t b = ceil_div(n, per_block);
+    return b < most ? b : most;
 }
 
 }  // namespace no
@@ -92,17 +279,34 @@ extern "C" int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride
     if (n_rows_cap == 0) return NO_OK;
     NO_REQUIRE((dt_y == NO_E4M3) == (d_row_scale != nullptr), NO_ERR_INVALID_ARG, "%s: row scales go with NO_E4M3, and with it alone", who);
     const RowsOf x = rows_of(d_x, x_stride_bytes), r = rows_of(d_residual, residual_stride_bytes), s = rows_of(d_sum, sum_stride_bytes), y = rows_of(d_y, y_stride_bytes);
-    const dim3 grid((unsigned)(n_rows_cap < 65536 ? n_rows_cap : 65536));
-#define NO_NORM(T, Y) hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, Y>), grid, dim3(256), 0, (hipStream_t)stream, x, r, d_weight, eps, d_n_rows, n_rows_cap, dim, s, y, d_row_scale, d_rstd)
+    hipStream_t st = (hipStream_t)stream;
+#define NO_NORM_AS(T, Y, TEAM, THREADS, U)                                                                                                          \
+    hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, Y, TEAM, THREADS, U>), dim3((unsigned)norm_blocks(n_rows_cap, THREADS / TEAM, THREADS == 256 ? 2048 : 512)), \
+                       dim3(THREADS), 0, st, x, r, d_weight, eps, d_n_rows, n_rows_cap, dim, s, y, d_row_scale, d_rstd)
+#define NO_NORM(T, Y)                                              \
+    do {                                                           \
+        const int64_t units = ceil_div(dim, 16 / (int)sizeof(T));  \
+        if (units <= 8) NO_NORM_AS(T, Y, 8, 256, 1);               \
+        else if (units <= 32) NO_NORM_AS(T, Y, 32, 256, 1);        \
+        else if (units <= 64) NO_NORM_AS(T, Y, 64, 256, 1);        \
+        else if (units <= 128) NO_NORM_AS(T, Y, 64, 256, 2);       \
+        else if (units <= 256) NO_NORM_AS(T, Y, 64, 256, 4);       \
+        else if (units <= 512) NO_NORM_AS(T, Y, 256, 256, 2);      \
+        else if (units <= 1024) NO_NORM_AS(T, Y, 256, 256, 4);     \
+        else if (units <= 2048) NO_NORM_AS(T, Y, 256, 256, 8);     \
+        else if (units <= 8192) NO_NORM_AS(T, Y, 1024, 1024, 8);   \
+        else NO_NORM_AS(T, Y, 1024, 1024, sizeof(T) == 4 ? 16 : 8); \
+    } while (0)
     if (dt == NO_F32) { if (dt_y == NO_F32) NO_NORM(float, float); else if (dt_y == NO_BF16) NO_NORM(float, bf16_t); else NO_NORM(float, e4m3_t); }
     else { if (dt_y == NO_F32) NO_NORM(bf16_t, float); else if (dt_y == NO_BF16) NO_NORM(bf16_t, bf16_t); else NO_NORM(bf16_t, e4m3_t); }
 #undef NO_NORM
+#undef NO_NORM_AS
     return launch_status(who);
 }
 
 extern "C" size_t no_rmsnorm_ws_bytes(int32_t n_rows_cap, int32_t dim) {
     if (n_rows_cap < 0 || dim < 1 || dim > NO_MAX_NORM_DIM) return 0;
-    return 16;
+    return 16 + (size_t)(n_rows_cap < NORM_PARTS ? n_rows_cap : NORM_PARTS) * (size_t)dim * 4;
 }
 
 extern "C" int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride_bytes, const float* d_weight, const float* d_rstd,
@@ -122,15 +326,41 @@ extern "C" int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride
     NO_REQUIRE(d_ws && (uintptr_t)d_ws % 16 == 0, NO_ERR_INVALID_ARG, "%s: the workspace is NULL or misaligned", who);
     NO_REQUIRE(ws_bytes >= no_rmsnorm_ws_bytes(n_rows_cap, dim), NO_ERR_CAPACITY, "%s: workspace too small", who);
     const RowsOf s = rows_of(d_s, s_stride_bytes), gy = rows_of(d_grad_y, grad_y_stride_bytes), gs = rows_of(d_grad_sum, grad_sum_stride_bytes), gx = rows_of(d_grad_x, grad_x_stride_bytes);
-    const dim3 grid((unsigned)(n_rows_cap < 65536 ? n_rows_cap : 65536)), cols((unsigned)ceil_div(dim, 256));
     hipStream_t st = (hipStream_t)stream;
-    // the weight's gradient first: grad_x may overwrite what it reads
+    float* parts = (float*)d_ws;
+    int64_t n_parts = 0;
+#define NO_NORM_AS(T, TEAM, THREADS, U)                                                                                                              \
+    do {                                                                                                                                             \
+        n_parts = norm_blocks(n_rows_cap, THREADS / TEAM, NORM_PARTS);                                                                               \
+        hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, TEAM, THREADS, U>), dim3((unsigned)n_parts), dim3(THREADS), 0, st, s, d_weight, d_rstd, gy, gs, d_n_rows, n_rows_cap, dim, \
+                           gx, parts, d_grad_weight);                                                                                                \
+    } while (0)
 #define NO_NORM(T)                                                                                                                                   \
     do {                                                                                                                                             \
-        if (d_grad_weight) hipLaunchKernelGGL(rmsnorm_grad_weight_kernel<T>, cols, dim3(256), 0, st, s, d_rstd, gy, d_n_rows, n_rows_cap, dim, d_grad_weight); \
-        if (n_rows_cap) hipLaunchKernelGGL(rmsnorm_grad_x_kernel<T>, grid, dim3(256), 0, st, s, d_weight, d_rstd, gy, gs, d_n_rows, n_rows_cap, dim, gx);      \
+        const int64_t units = ceil_div(dim, 16 / (int)sizeof(T));                                                                                    \
+        if (units <= 8) NO_NORM_AS(T, 8, 256, 1);                                                                                                    \
+        else if (units <= 32) NO_NORM_AS(T, 32, 256, 1);                                                                                             \
+        else if (units <= 64) NO_NORM_AS(T, 64, 256, 1);                                                                                             \
+        else if (units <= 128) NO_NORM_AS(T, 64, 256, 2);                                                                                            \
+        else if (units <= 256) NO_NORM_AS(T, 64, 256, 4);                                                                                            \
+        else if (units <= 512) NO_NORM_AS(T, 256, 256, 2);                                                                                           \
+        else if (units <= 1024) NO_NORM_AS(T, 256, 256, 4);                                                                                          \
+        else if (units <= 4096) NO_NORM_AS(T, 1024, 1024, 4);                                                                                        \
+        else {                                                                                                                                       \
+            n_parts = n_rows_cap < NORM_PARTS ? n_rows_cap : NORM_PARTS;                                                                             \
+            if (n_parts > 64) n_parts = 64;                                                                                                          \
+            /* before the input gradient, which may overwrite what this reads; always joined, so never one part straight into the result */          \
+            if (d_grad_weight)                                                                                                                       \
+                hipLaunchKernelGGL(rmsnorm_wide_parts_kernel<T>, dim3((unsigned)ceil_div(dim, 256), (unsigned)n_parts), dim3(256), 0, st, s, d_rstd, gy, d_n_rows, n_rows_cap, dim, parts); \
+            hipLaunchKernelGGL(rmsnorm_bwd_wide_kernel<T>, dim3((unsigned)norm_blocks(n_rows_cap, 1, 512)), dim3(1024), 0, st, s, d_weight, d_rstd, gy, gs, d_n_rows, n_rows_cap, dim, gx); \
+            direct = false;                                                                                                                          \
+        }                                                                                                                                            \
     } while (0)
-    if (dt == NO_F32) NO_NORM(float); else NO_NORM(bf16_t);
+    bool direct = true;         // a single block has stored the weight's gradient itself
+    if (n_rows_cap > 0) { if (dt == NO_F32) NO_NORM(float); else NO_NORM(bf16_t); }
 #undef NO_NORM
+#undef NO_NORM_AS
+    if (d_grad_weight && !(direct && n_parts == 1))
+        hipLaunchKernelGGL(rmsnorm_join_kernel, dim3((unsigned)ceil_div(dim, 64)), dim3(1024), 0, st, parts, (int32_t)n_parts, dim, d_grad_weight);
     return launch_status(who);
 }

@@ -105,6 +105,36 @@ struct Run {
     }
 };
 
+// TEAM lanes that share a row: a part of a wavefront, a wavefront, or a block. Sums and maxima reach every lane. Across wavefronts they cost one
+// barrier each: two slots take turns, and a wavefront that writes a slot again has passed the barrier behind its last reads.
+template <int TEAM, int THREADS>
+struct Team {
+    static_assert(TEAM <= 64 || TEAM == THREADS, "a team is a part of a wavefront or the block");
+    static constexpr int WAVES = TEAM <= 64 ? 1 : TEAM / 64, PER_BLOCK = THREADS / TEAM;
+    float* smem;        // [2][WAVES] where a team spans wavefronts
+    int turn = 0;
+    __device__ __forceinline__ explicit Team(float* s) : smem(s) {}
+    __device__ __forceinline__ static int lane() { return (int)threadIdx.x & (TEAM - 1); }
+    __device__ __forceinline__ static int index() { return (int)threadIdx.x / TEAM; }
+    template <typename Op>
+    __device__ __forceinline__ float reduce(float v, Op op) {
+#pragma unroll
+        for (int o = (TEAM < 64 ? TEAM : 64) / 2; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
+        if constexpr (TEAM > 64) {
+            float* s = smem + turn * WAVES;
+            turn ^= 1;
+            if (lane_id() == 0) s[threadIdx.x >> 6] = v;
+            __syncthreads();
+            v = s[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v = op(v, s[w]);
+        }
+        return v;
+    }
+    __device__ __forceinline__ float sum(float v) { return reduce(v, [](float a, float b) { return a + b; }); }
+    __device__ __forceinline__ float max(float v) { return reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
+};
+
 // What every call checks of a row matrix. The stride counts from the second row on.
 static inline int32_t check_rows(const char* who, const char* what, const void* p, no_dtype dt, int64_t n, int64_t dim, int64_t stride) {
     const int32_t es = size_of(dt);

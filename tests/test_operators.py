@@ -136,11 +136,13 @@ def test_embed_fwd_far_rows():
 
 
 def embed_grad_ref(grad, ids, v, scale):
+    """Sum, sum of magnitudes and count of every row (on the host: thousands of additions to one row queue up on the device)."""
+    grad, ids = grad.cpu().double(), ids.cpu()
     inside = ((ids >= 0) & (ids < v)).nonzero()[:, 0]
-    at, g = ids[inside].long(), grad[inside].double()
-    z = lambda: torch.zeros((v, grad.shape[1]), dtype=torch.float64, device="cuda")  # noqa: E731
-    n = torch.zeros((v,), dtype=torch.float64, device="cuda").index_add_(0, at, torch.ones_like(at, dtype=torch.float64))
-    return scale * z().index_add_(0, at, g), abs(scale) * z().index_add_(0, at, g.abs()), n
+    at, g = ids[inside].long(), grad[inside]
+    z = lambda: torch.zeros((v, grad.shape[1]), dtype=torch.float64)  # noqa: E731
+    n = torch.zeros((v,), dtype=torch.float64).index_add_(0, at, torch.ones_like(at, dtype=torch.float64))
+    return (scale * z().index_add_(0, at, g)).cuda(), (abs(scale) * z().index_add_(0, at, g.abs())).cuda(), n.cuda()
 
 
 @pytest.mark.parametrize("n,v,dim,pad,off,popular", [
