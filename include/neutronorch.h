@@ -286,6 +286,7 @@ int32_t no_gcn_layer_bwd(const no_block_view* blk, no_arch form, int32_t d_in, c
  * ---------------------------------------------------------------------------------------- */
 
 enum {
+    NO_MAX_EMBED_DIM = 1 << 20,    /* widest row of no_embed_* */
     NO_MAX_NORM_DIM = 65536,       /* widest row of no_rmsnorm_* */
     NO_MAX_CLASSES = 1 << 22,      /* widest row of no_distill_* and no_logprobs_* */
     NO_MAX_TEACHER = 256,          /* teacher entries a row */

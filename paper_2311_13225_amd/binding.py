@@ -453,7 +453,7 @@ def no_gcn_layer_bwd(blk: no_block_view, agg: torch.Tensor, h: torch.Tensor, gra
 
 # ------------------------------------------------------------------------------------------ learned inputs, large answers
 
-NO_MAX_NORM_DIM, NO_MAX_CLASSES, NO_MAX_TEACHER, NO_MAX_ALTERNATIVES = 65536, 1 << 22, 256, 64
+NO_MAX_EMBED_DIM, NO_MAX_NORM_DIM, NO_MAX_CLASSES, NO_MAX_TEACHER, NO_MAX_ALTERNATIVES = 1 << 20, 65536, 1 << 22, 256, 64
 _OP_DTYPES = {torch.float32: NO_F32, torch.bfloat16: NO_BF16, torch.float8_e4m3fn: NO_E4M3}
 
 

@@ -141,8 +141,8 @@ struct EmbedSums {
 template <typename T, int W>
 __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t chunks, int32_t g_log2, int32_t col_tiles, uint32_t sum_blocks) {
     const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id();
-    if (blockIdx.x >= sum_blocks) {     // rows without an id: 16 to a wavefront
-        const int64_t v0 = ((int64_t)(blockIdx.x - sum_blocks) * 4 + (threadIdx.x >> 6)) * 16;
+    for (int64_t v0 = ((int64_t)blockIdx.x - sum_blocks) * 64 + (threadIdx.x >> 6) * 16; blockIdx.x >= sum_blocks;
+         v0 += ((int64_t)gridDim.x - sum_blocks) * 64) {     // rows without an id: 16 to a wavefront at a time
         if (v0 >= a.n_rows) return;
         const int64_t v = v0 + (lane & 15);
         int32_t lo = 0, hi = n;
@@ -160,7 +160,6 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
             float* row = a.table.row<float>(v0 + at);
             for (int32_t c = lane * 4; c < a.dim; c += 256) zero.store(row + c, a.dim - c);
         }
-        return;
     }
     const int32_t groups = 64 >> g_log2, u = lane & ((1 << g_log2) - 1);
     const int64_t item = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * groups + (lane >> g_log2);
@@ -278,7 +277,8 @@ static void launch_sums(const EmbedSums& a, int64_t chunks, hipStream_t st) {
     const int32_t units = (int32_t)ceil_div(a.dim, W), col_tiles = (int32_t)ceil_div(units, 64);
     int g_log2 = 0;
     while ((1 << g_log2) < units && g_log2 < 6) ++g_log2;
-    const int64_t sum_blocks = ceil_div(ceil_div(chunks * col_tiles, 64 >> g_log2), 4), zero_blocks = a.accumulate ? 0 : ceil_div(a.n_rows, 64);
+    const int64_t sum_blocks = ceil_div(ceil_div(chunks * col_tiles, 64 >> g_log2), 4), zero_rows = ceil_div(a.n_rows, 64),
+                  zero_blocks = a.accumulate ? 0 : zero_rows < (1 << 20) ? zero_rows : 1 << 20;
     if (sum_blocks + zero_blocks)
         hipLaunchKernelGGL((embed_sums_kernel<T, W>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks);
 }
@@ -294,6 +294,7 @@ extern "C" int32_t no_embed_fwd(const void* d_table, no_dtype dt, int64_t n_rows
     NO_REQUIRE(dt == NO_F32 || dt == NO_BF16 || dt == NO_E4M3, NO_ERR_INVALID_ARG, "no_embed_fwd: unknown table type");
     NO_REQUIRE(dt_out == NO_F32 || dt_out == NO_BF16, NO_ERR_INVALID_ARG, "no_embed_fwd: outputs are NO_F32 or NO_BF16");
     NO_REQUIRE(n_rows >= 1 && dim >= 1 && n_ids_cap >= 0, NO_ERR_INVALID_ARG, "no_embed_fwd: bad sizes");
+    NO_REQUIRE(dim <= NO_MAX_EMBED_DIM, NO_ERR_UNSUPPORTED, "no_embed_fwd: rows of more than %d values", NO_MAX_EMBED_DIM);
     NO_CHECK(check_rows("no_embed_fwd", "table", d_table, dt, n_rows, dim, table_stride_bytes));
     NO_CHECK(check_rows("no_embed_fwd", "out", d_out, dt_out, n_ids_cap, dim, out_stride_bytes));
     if (n_ids_cap == 0) return NO_OK;
@@ -307,7 +308,7 @@ extern "C" int32_t no_embed_fwd(const void* d_table, no_dtype dt, int64_t n_rows
 }
 
 extern "C" size_t no_embed_ws_bytes(int32_t n_ids_cap, int32_t dim) {
-    if (n_ids_cap < 0 || dim < 1) return 0;
+    if (n_ids_cap < 0 || dim < 1 || dim > NO_MAX_EMBED_DIM) return 0;
     return EmbedPlan(n_ids_cap, dim).total;
 }
 
@@ -318,6 +319,7 @@ extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t gra
     const char* who = "no_embed_bwd";
     NO_REQUIRE(dt == NO_F32 || dt == NO_BF16, NO_ERR_INVALID_ARG, "%s: gradients are NO_F32 or NO_BF16", who);
     NO_REQUIRE(n_rows >= 1 && n_rows <= INT32_MAX && dim >= 1 && n_ids_cap >= 0, NO_ERR_INVALID_ARG, "%s: bad sizes", who);
+    NO_REQUIRE(dim <= NO_MAX_EMBED_DIM, NO_ERR_UNSUPPORTED, "%s: rows of more than %d values", who, NO_MAX_EMBED_DIM);
     NO_CHECK(check_rows(who, "grad_out", d_grad_out, dt, n_ids_cap, dim, grad_stride_bytes));
     NO_CHECK(check_rows(who, "grad_table", d_grad_table, NO_F32, n_rows, dim, table_stride_bytes));
     NO_REQUIRE(d_ids || n_ids_cap == 0, NO_ERR_INVALID_ARG, "%s: ids are NULL", who);

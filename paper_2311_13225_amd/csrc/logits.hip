@@ -1,162 +1,545 @@
-// no_distill_* and no_logprobs_*: one pass or two over rows of logits.
+// no_distill_* and no_logprobs_*: rows of logits, read once.
+//
+// A team of lanes (a wavefront or a block) holds a row, or a piece of one, in registers, U runs of 16 bytes a lane, and takes the maximum, the sum of
+// exponentials and whatever follows from there. Rows that are longer than a team's registers, and rows that are too few to fill the chip, are cut into pieces whose sums a
+// second launch joins. Exponentials are 2^((z - m) c), c = log2(e) / T, with the difference taken first: it is exact next to the maximum m, where the
+// exponentials are large, so that its rounding costs nothing there.
 #include "rows.hpp"
 
 namespace no {
 
-__device__ __forceinline__ float block_max(float v, float* smem) {
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    if (lane_id() == 0) smem[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = fmaxf(fmaxf(smem[0], smem[1]), fmaxf(smem[2], smem[3]));
-    __syncthreads();
-    return v;
-}
+constexpr float LOG2E = 1.44269504088896340736f;
 
-// Largest logit (0 where there is none above -inf), sum of exponentials, sum of e * (z - m).
-struct RowSums { float m, s, h; bool none; };
+// Sums of a row or a piece: largest logit (-inf: there is none above), sum of 2^((z - m) c), sum of that times (z - m).
+struct Sums { float m, s, h; };
 
-template <typename T>
-__device__ RowSums row_sums(const T* z, int32_t classes, float inv_t, float* smem) {
-    RowSums r;
+__device__ __forceinline__ float above(float m) { return m == -INFINITY ? 0.0f : m; }      // what differences are taken from
+
+template <typename T, int U, int TEAM>
+struct Piece {      // a lane's runs of z[0, len): run u covers values [(lane + u TEAM) W, + W)
+    static constexpr int W = 16 / (int)sizeof(T);
+    Run<T, W> v[U];
+    __device__ __forceinline__ static int32_t at(int t, int u) { return (t + u * TEAM) * W; }
+    __device__ __forceinline__ void load(const T* z, int32_t len, int t) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t c = at(t, u);
+            v[u].load(z + min(c, len), len - c, from_f32<T>(-INFINITY));
+        }
+    }
+    __device__ __forceinline__ float lane_max() const {
+        float m = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[W];
+            v[u].get(f);
+#pragma unroll
+            for (int w = 0; w < W; ++w) m = fmaxf(m, f[w]);
+        }
+        return m;
+    }
+    // adds the lane's terms of s, and of h if ENTROPY; 0 (-inf) counts as 0
+    template <bool ENTROPY>
+    __device__ __forceinline__ void add(float from, float c, float& s, float& h) const {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[W];
+            v[u].get(f);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float d = f[w] - from, e = __builtin_amdgcn_exp2f(d * c);
+                s += e;
+                if constexpr (ENTROPY) h += e * fmaxf(d, -3.0e38f);
+            }
+        }
+    }
+};
+
+// Joins the sums of a row's pieces, each with its own maximum: a lane takes pieces t, t + TEAM, ...
+template <int TEAM, int THREADS>
+__device__ __forceinline__ Sums join_sums(const Sums* parts, int32_t pieces, float c, Team<TEAM, THREADS>& team) {
     float m = -INFINITY;
-    for (int32_t c = threadIdx.x; c < classes; c += 256) m = fmaxf(m, to_f32(z[c]));
-    m = block_max(m, smem);
+    const int t = team.lane();
+    for (int32_t p = t; p < pieces; p += TEAM) m = fmaxf(m, parts[p].m);
+    m = team.max(m);
     float s = 0.0f, h = 0.0f;
-    const float from = m == -INFINITY ? 0.0f : m;
-    for (int32_t c = threadIdx.x; c < classes; c += 256) {
-        const float d = (to_f32(z[c]) - from) * inv_t, e = expf(d);
-        s += e;
-        if (e != 0.0f) h += e * d;
+    for (int32_t p = t; p < pieces; p += TEAM) {
+        const Sums q = parts[p];
+        const float d = above(q.m) - above(m), e = q.s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(d * c);
+        s += e * q.s;
+        h += e * (q.h + d * q.s);
     }
-    r.s = block_sum<float, 256>(s, smem);
-    r.h = block_sum<float, 256>(h, smem);
-    r.none = r.s == 0.0f;
-    r.m = from;
-    return r;
+    return Sums{m, team.sum(s), team.sum(h)};
 }
 
-// The teacher's shares of a row into p[k] (0 for entries that are left out); ids_out[k] = -1 for those. Returns whether there are any.
-__device__ bool teacher_shares(const int32_t* ids, const float* logits, int32_t k, int32_t classes, float inv_t, float* p, float* log_p, int32_t* ids_out,
-                               float* smem) {
-    const int j = threadIdx.x;
-    const int32_t id = j < k ? ids[j] : -1;
-    const bool there = id >= 0 && id < classes;
-    const float t = there ? logits[j] * inv_t : -INFINITY;
-    const float m = block_max(t, smem), from = m == -INFINITY ? 0.0f : m;
-    const float e = there ? expf(t - from) : 0.0f, s = block_sum<float, 256>(e, smem);
-    if (j < k) {
-        p[j] = s == 0.0f ? 0.0f : e / s;
-        log_p[j] = t - from - logf(s);
-        ids_out[j] = there ? id : -1;
+// ------------------------------------------------------------------------------------------------------- teacher
+
+// The teacher's entries of a row in LDS: class (-1: left out), share, its logarithm, and the student's logit there.
+struct Teacher {
+    int32_t id[NO_MAX_TEACHER];
+    float p[NO_MAX_TEACHER], log_p[NO_MAX_TEACHER], z[NO_MAX_TEACHER];
+};
+
+// Fills `to` with softmax(logits / T) over the entries inside the classes, and with the student's logits at those in [lo, hi); returns whether any
+// entry is above -inf.
+template <typename T, int TEAM, int THREADS>
+__device__ __forceinline__ bool teacher_shares(const int32_t* __restrict__ ids, const float* __restrict__ logits, int32_t k, int32_t classes, float inv_t, const T* z, int32_t lo, int32_t hi,
+                                               Teacher& to, Team<TEAM, THREADS>& team) {
+    constexpr int Q = TEAM < NO_MAX_TEACHER ? NO_MAX_TEACHER / TEAM : 1;
+    const int t = team.lane();
+    int32_t id[Q];
+    float x[Q], zz[Q], m = -INFINITY, s = 0.0f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int j = t + q * TEAM;
+        id[q] = j < k ? ids[j] : -1;
+        const bool there = id[q] >= 0 && id[q] < classes;
+        x[q] = there ? logits[j] : -INFINITY;
+        zz[q] = id[q] >= lo && id[q] < hi ? to_f32(z[id[q]]) : 0.0f;
+        if (!there) id[q] = -1;
+        m = fmaxf(m, x[q]);
     }
-    __syncthreads();
+    const float from = above(team.max(m));
+    float e[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        e[q] = id[q] < 0 ? 0.0f : expf((x[q] - from) * inv_t);
+        s += e[q];
+    }
+    s = team.sum(s);
+    const float log_s = logf(s);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int j = t + q * TEAM;
+        if (j < k) {
+            to.id[j] = id[q];
+            to.p[j] = s == 0.0f ? 0.0f : e[q] / s;
+            to.log_p[j] = (x[q] - from) * inv_t - log_s;
+            to.z[j] = zz[q];
+        }
+    }
+    team.sync();
     return s != 0.0f;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) distill_kernel(RowsOf z, const int32_t* d_n, int32_t cap, int32_t classes, const int32_t* t_ids, const float* t_logits,
-                                                      int32_t k, float temperature, const float* weight, float* loss, const float* lse_in, float* lse_out, RowsOf grad) {
-    __shared__ float smem[4], p[256], log_p[256], at[256];
-    __shared__ int32_t ids[256];
-    const int32_t n = rows_here(d_n, cap);
-    const float inv_t = 1.0f / temperature;
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const T* row = z.row<T>(i);
-        const float w = weight ? weight[i] : 1.0f;
-        const bool any = teacher_shares(t_ids + i * k, t_logits + i * k, k, classes, inv_t, p, log_p, ids, smem);
-        if ((int)threadIdx.x < k) at[threadIdx.x] = ids[threadIdx.x] >= 0 ? to_f32(row[ids[threadIdx.x]]) : 0.0f;
-        RowSums r{0, 0, 0, false};
-        float log_s = 0.0f;
-        if (!lse_in) {
-            r = row_sums(row, classes, inv_t, smem);
-            log_s = logf(r.s);
-            if (threadIdx.x == 0 && lse_out) lse_out[i] = r.m * inv_t + log_s;
+struct Distill {
+    RowsOf z;
+    const int32_t* d_n;
+    int64_t row0;                   // the launch's first row
+    int32_t cap, classes;
+    const int32_t* ids;
+    const float* logits;
+    int32_t k;
+    float temperature, inv_t, c;    // 1 / T, log2(e) / T
+    const float* weight;
+    float* loss;
+    const float* lse_in;
+    float* lse_out;
+    RowsOf grad;
+    Sums* parts;                    // [cap][pieces] where rows are cut
+    int32_t pieces, piece;          // pieces a row, values a piece (a multiple of a run)
+};
+
+// Loss and lse of a row whose sums are known; all lanes of the team call it.
+template <int TEAM, int THREADS>
+__device__ __forceinline__ void distill_loss(const Distill& a, int64_t i, const Sums& r, float w, bool any, const Teacher& te, Team<TEAM, THREADS>& team) {
+    const float log_s = logf(r.s), from = above(r.m);
+    if (a.loss) {
+        float term = 0.0f;
+        for (int j = team.lane(); j < a.k; j += TEAM)
+            if (te.p[j] != 0.0f) term += te.p[j] * (te.log_p[j] - (r.s == 0.0f ? -INFINITY : (te.z[j] - from) * a.inv_t - log_s));
+        term = team.sum(term);
+        if (team.lane() == 0) a.loss[i] = w == 0.0f || !any ? 0.0f : w * a.temperature * a.temperature * term;
+    }
+    if (a.lse_out && team.lane() == 0) a.lse_out[i] = from * a.inv_t + log_s;
+}
+
+// A share of a class in the student's row: from the row's sums, or from its lse.
+struct Share {
+    float from, c, inv_s, inv_t, lse;
+    bool by_lse;
+    __device__ __forceinline__ float operator()(float z) const {
+        if (by_lse) return z == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((z * inv_t - lse) * LOG2E);
+        return z == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((z - from) * c) * inv_s;
+    }
+};
+
+// The gradient of values [first, first + len) of a row, held in `v`: w T q everywhere, then the classes that the teacher names once more with
+// their shares taken off (the barrier orders the two stores; an entry that stands twice stores the same value twice).
+template <typename T, int U, int TEAM, int THREADS>
+__device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_t first, int32_t len, const Piece<T, U, TEAM>& v, const Share& q, float w, bool any, const Teacher& te,
+                                             Team<TEAM, THREADS>& team) {
+    constexpr int W = Piece<T, U, TEAM>::W;
+    const int t = team.lane();
+    T* const out = a.grad.row<T>(i) + first;
+    const float by = w * a.temperature;
+    const bool live = w != 0.0f && any;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t c = v.at(t, u);
+        if (c < len) {
+            float f[W];
+            v.v[u].get(f);
+#pragma unroll
+            for (int x = 0; x < W; ++x) f[x] = live ? by * q(f[x]) : 0.0f;
+            Run<T, W> o;
+            o.set(f);
+            o.store(out + c, len - c);
         }
-        __syncthreads();
-        if (loss) {
-            const int j = threadIdx.x;
-            float term = 0.0f;
-            if (j < k && p[j] != 0.0f) term = p[j] * (log_p[j] - (r.none ? -INFINITY : (at[j] - r.m) * inv_t - log_s));
-            const float sum = block_sum<float, 256>(term, smem);
-            if (j == 0) loss[i] = w == 0.0f || !any ? 0.0f : w * temperature * temperature * sum;
-        }
-        if (grad.p) {
-            T* out = grad.row<T>(i);
-            const float by = w * temperature, lse = lse_in ? lse_in[i] : 0.0f, inv_s = 1.0f / r.s;
-            auto q_of = [&](float v) { return v == -INFINITY ? 0.0f : lse_in ? expf(v * inv_t - lse) : expf((v - r.m) * inv_t) * inv_s; };
-            for (int32_t c = threadIdx.x; c < classes; c += 256) out[c] = from_f32<T>(w == 0.0f || !any ? 0.0f : by * q_of(to_f32(row[c])));
-            __syncthreads();
-            const int j = threadIdx.x;
-            if (j < k && ids[j] >= 0 && w != 0.0f && any) {
+    }
+    team.sync();
+    if (live)
+        for (int j = t; j < a.k; j += TEAM) {
+            const int32_t at = te.id[j] - first;
+            if (te.id[j] >= 0 && at >= 0 && at < len) {
                 float share = 0.0f;
-                for (int32_t o = 0; o < k; ++o) if (ids[o] == ids[j]) share += p[o];
-                out[ids[j]] = from_f32<T>(by * (q_of(at[j]) - share));
+                for (int o = 0; o < a.k; ++o) share += te.id[o] == te.id[j] ? te.p[o] : 0.0f;
+                out[at] = from_f32<T>(by * (q(te.z[j]) - share));
             }
         }
-        __syncthreads();
+}
+
+// A whole row in a team's registers: everything in one read.
+template <typename T, int TEAM, int THREADS, int U>
+__global__ void __launch_bounds__(THREADS) distill_row_kernel(Distill a) {
+    __shared__ float smem[2 * THREADS / 64];
+    __shared__ Teacher teachers[THREADS / TEAM];
+    Team<TEAM, THREADS> team(smem);
+    Teacher& te = teachers[team.index()];
+    const int32_t n = rows_here(a.d_n, a.cap);
+    const int64_t i = a.row0 + (int64_t)blockIdx.x * (THREADS / TEAM) + team.index();
+    if (i >= n) return;
+    const T* z = a.z.row<T>(i);
+    Piece<T, U, TEAM> v;
+    v.load(z, a.classes, team.lane());
+    const float w = a.weight ? a.weight[i] : 1.0f;
+    const bool any = teacher_shares(a.ids + i * a.k, a.logits + i * a.k, a.k, a.classes, a.inv_t, z, 0, a.classes, te, team);
+    Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
+    v.template add<false>(above(r.m), a.c, r.s, r.h);
+    r.s = team.sum(r.s);
+    distill_loss(a, i, r, w, any, te, team);
+    if (a.grad.p) distill_grad(a, i, 0, a.classes, v, Share{above(r.m), a.c, 1.0f / r.s, a.inv_t, 0.0f, false}, w, any, te, team);
+}
+
+// Sums of one piece of a row.
+template <typename T, int THREADS, int U>
+__global__ void __launch_bounds__(THREADS) distill_sums_kernel(Distill a) {
+    __shared__ float smem[2 * THREADS / 64];
+    Team<THREADS, THREADS> team(smem);
+    const int64_t i = a.row0 + blockIdx.x / (uint32_t)a.pieces;
+    const int32_t p = (int32_t)(blockIdx.x % (uint32_t)a.pieces);
+    if (i >= rows_here(a.d_n, a.cap)) return;
+    Piece<T, U, THREADS> v;
+    v.load(a.z.row<T>(i) + (int64_t)p * a.piece, min(a.piece, a.classes - p * a.piece), team.lane());
+    Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
+    v.template add<false>(above(r.m), a.c, r.s, r.h);
+    r.s = team.sum(r.s);
+    if (threadIdx.x == 0) a.parts[i * a.pieces + p] = r;
+}
+
+// One piece of a row's gradient, from the sums of the row's pieces or from a given lse. The gradient may go over the logits, so the loss, which
+// reads them all over the row, is made by a launch before this one (distill_loss_kernel).
+template <typename T, int THREADS, int U>
+__global__ void __launch_bounds__(THREADS) distill_grad_kernel(Distill a) {
+    __shared__ float smem[2 * THREADS / 64];
+    __shared__ Teacher te;
+    Team<THREADS, THREADS> team(smem);
+    const int64_t i = a.row0 + blockIdx.x / (uint32_t)a.pieces;
+    const int32_t p = (int32_t)(blockIdx.x % (uint32_t)a.pieces), first = p * a.piece, len = min(a.piece, a.classes - first);
+    if (i >= rows_here(a.d_n, a.cap)) return;
+    const T* z = a.z.row<T>(i);
+    Piece<T, U, THREADS> v;
+    v.load(z + first, len, team.lane());
+    const float w = a.weight ? a.weight[i] : 1.0f;
+    const bool any = teacher_shares(a.ids + i * a.k, a.logits + i * a.k, a.k, a.classes, a.inv_t, z, first, first + len, te, team);
+    if (a.lse_in) {
+        distill_grad(a, i, first, len, v, Share{0.0f, a.c, 0.0f, a.inv_t, a.lse_in[i], true}, w, any, te, team);
+    } else {
+        const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);
+        distill_grad(a, i, first, len, v, Share{above(r.m), a.c, 1.0f / r.s, a.inv_t, 0.0f, false}, w, any, te, team);
     }
 }
 
-// Order of alternatives: larger value first, then the lower class.
-__device__ __forceinline__ uint64_t order_key(float v, int32_t c) {
-    const uint32_t b = __float_as_uint(v + 0.0f);                    // (-0 counts as 0)
-    return (uint64_t)((b & 0x80000000u) ? ~b : b | 0x80000000u) << 32 | (uint32_t)~c;
+// Loss and lse from the sums of a row's pieces.
+template <typename T>
+__global__ void __launch_bounds__(256) distill_loss_kernel(Distill a) {
+    __shared__ Teacher teachers[4];
+    Team<64, 256> team(nullptr);
+    Teacher& te = teachers[team.index()];
+    const int64_t i = a.row0 + (int64_t)blockIdx.x * 4 + team.index();
+    if (i >= rows_here(a.d_n, a.cap)) return;
+    const float w = a.weight ? a.weight[i] : 1.0f;
+    const bool any = teacher_shares(a.ids + i * a.k, a.logits + i * a.k, a.k, a.classes, a.inv_t, a.z.row<T>(i), 0, a.classes, te, team);
+    const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);
+    distill_loss(a, i, r, w, any, te, team);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) logprobs_fwd_kernel(RowsOf z, const int32_t* d_n, int32_t cap, int32_t classes, const int32_t* tokens, float temperature,
-                                                           float* logprob, float* entropy, float* lse, int32_t k, int32_t* top_ids, float* top_logprobs) {
-    __shared__ float smem[4];
-    __shared__ uint64_t keys[4];
-    const int32_t n = rows_here(d_n, cap);
-    const float inv_t = 1.0f / temperature;
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const T* row = z.row<T>(i);
-        const RowSums r = row_sums(row, classes, inv_t, smem);
-        const float log_s = logf(r.s);
-        auto log_of = [&](float v) { return v == -INFINITY && !(r.s != r.s) ? -INFINITY : (v - r.m) * inv_t - log_s; };
-        if (threadIdx.x == 0) {
-            const int32_t t = tokens[i];
-            logprob[i] = t >= 0 && t < classes ? log_of(to_f32(row[t])) : 0.0f;
-            entropy[i] = r.none ? 0.0f : log_s - r.h / r.s;
-            lse[i] = r.m * inv_t + log_s;
+// ------------------------------------------------------------------------------------------------------- log probabilities
+
+// Order of alternatives: larger value first, then the lower class; -0 counts as 0.
+__device__ __forceinline__ uint32_t order_of(float v) {
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ uint64_t order_key(float v, int32_t c) { return (uint64_t)order_of(v) << 32 | (uint32_t)~c; }
+
+template <int TEAM>
+struct TopSpace {
+    static constexpr int CAP = 512;         // candidates that are ranked against each other
+    uint64_t key[CAP];
+    int32_t count;
+    float lane_max[TEAM > 64 ? TEAM : 1];
+    float from;
+};
+
+// The k largest values of a piece, as order keys in `to.key[0 .. min(count, CAP))`, in no order, with others that are smaller among them perhaps. The k-th largest of the lanes'
+// own maxima is a bound that k values at least reach, and few others do as a rule: those that do are collected. Where more do than there is room for (equal
+// values, or large ones that sit in few lanes), the bound is raised bit by bit, first by value, then among equal ones by class.
+template <typename T, int U, int TEAM, int THREADS>
+__device__ void top_candidates(const Piece<T, U, TEAM>& v, float lane_max, int32_t first, int32_t k, TopSpace<TEAM>& to, Team<TEAM, THREADS>& team) {
+    constexpr int W = Piece<T, U, TEAM>::W, Q = TEAM > 64 ? TEAM / 64 : 1;
+    const int t = team.lane();
+    // the k-th largest lane maximum, its upper 16 bits (so a little less than it): one wavefront looks for them bit by bit
+    float bound = 0.0f;
+    if constexpr (TEAM > 64) {
+        to.lane_max[t] = lane_max;
+        if (t == 0) to.count = 0;
+        team.sync();
+    } else if (t == 0) to.count = 0;
+    if (TEAM <= 64 || threadIdx.x < 64) {
+        uint32_t o[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            if constexpr (TEAM > 64) o[q] = order_of(to.lane_max[lane_id() + q * 64]);
+            else o[q] = order_of(lane_max);
         }
-        uint64_t before = ~0ull;
-        for (int32_t j = 0; j < k; ++j) {
-            uint64_t best = 0;
-            for (int32_t c = threadIdx.x; c < classes; c += 256) {
-                const float v = to_f32(row[c]);
-                const uint64_t key = v > -INFINITY ? order_key(v, c) : 0;
-                if (key < before && key > best) best = key;
-            }
-            for (int o = 32; o > 0; o >>= 1) best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, o, 64));
-            if (lane_id() == 0) keys[threadIdx.x >> 6] = best;
-            __syncthreads();
-            best = max(max(keys[0], keys[1]), max(keys[2], keys[3]));
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                const int32_t c = best ? (int32_t)~(uint32_t)best : -1;
-                top_ids[i * k + j] = r.s != r.s ? -1 : c;
-                top_logprobs[i * k + j] = r.s != r.s ? NAN : c < 0 ? -INFINITY : log_of(to_f32(row[c]));
-            }
-            before = best ? best : 0;
+        uint32_t best = 0;
+        for (int b = 31; b >= 16; --b) {
+            const uint32_t cand = best | 1u << b;
+            int here = 0;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) here += __popcll(__ballot(o[q] >= cand));
+            if (here >= k) best = cand;
+        }
+        bound = value_of(best);
+        if (best <= order_of(-3.4028234663852886e38f)) bound = -3.4028234663852886e38f;     // (-inf is no candidate)
+        if constexpr (TEAM > 64) if (threadIdx.x == 0) to.from = bound;
+    }
+    team.sync();
+    if constexpr (TEAM > 64) bound = to.from;
+    if (lane_max >= bound) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[W];
+            v.v[u].get(f);
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                if (f[w] >= bound) {
+                    const int32_t at = atomicAdd(&to.count, 1);
+                    if (at < TopSpace<TEAM>::CAP) to.key[at] = order_key(f[w], first + v.at(t, u) + w);
+                }
         }
     }
+    team.sync();
+    if (to.count <= TopSpace<TEAM>::CAP) return;
+    // how many values are at least x, or are larger than x or equal to it with a class below c
+    auto count = [&](float x, bool ties, int32_t c) {
+        int here = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[W];
+            v.v[u].get(f);
+#pragma unroll
+            for (int w = 0; w < W; ++w) here += ties ? f[w] > x || (f[w] == x && first + v.at(t, u) + w < c) : f[w] >= x;
+        }
+        return (int)team.sum((float)here);          // (exact: a piece has fewer than 2^24 values)
+    };
+    uint32_t best = 0;
+    bool fits = false;
+    for (int b = 31; b >= 0 && !fits; --b) {        // the largest value that k values reach (finite: -inf is no candidate, and a row with +inf has none)
+        const uint32_t cand = best | 1u << b;
+        const float x = value_of(cand);
+        if (!(x <= 3.4028234663852886e38f)) continue;
+        const int here = count(x, false, 0);
+        if (here >= k) { best = cand; fits = here <= TopSpace<TEAM>::CAP; }
+    }
+    const float x = value_of(best);
+    int32_t below = 0x7fffffff;
+    if (!fits) {                                    // more than fit reach it: the lowest classes of those equal to it
+        int32_t c = 0;
+        for (int b = 22; b >= 0; --b)
+            if (count(x, true, c | 1 << b) < k) c |= 1 << b;
+        below = c + 1;                              // (k values with a class below c + 1)
+    }
+    team.sync();
+    if (t == 0) to.count = 0;
+    team.sync();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[W];
+        v.v[u].get(f);
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const int32_t c = first + v.at(t, u) + w;
+            if (f[w] > x || (f[w] == x && c < below)) {
+                const int32_t at = atomicAdd(&to.count, 1);
+                if (at < TopSpace<TEAM>::CAP) to.key[at] = order_key(f[w], c);
+            }
+        }
+    }
+    team.sync();
+}
+
+struct Logprobs {
+    RowsOf z;
+    const int32_t* d_n;
+    int64_t row0;
+    int32_t cap, classes;
+    const int32_t* tokens;
+    float inv_t, c;
+    float *logprob, *entropy, *lse;
+    int32_t k;
+    int32_t* top_ids;
+    float* top_logprobs;
+    Sums* parts;                    // [cap][pieces]
+    uint64_t* keys;                 // [cap][pieces][k], each piece's in order, 0: none
+    int32_t pieces, piece;
+};
+
+// log p of a logit, from the row's sums
+__device__ __forceinline__ float log_share(const Logprobs& a, const Sums& r, float log_s, float z) {
+    if (r.s != r.s) return NAN;
+    return z == -INFINITY ? -INFINITY : (z - above(r.m)) * a.inv_t - log_s;
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) logprobs_bwd_kernel(RowsOf z, const int32_t* d_n, int32_t cap, int32_t classes, const int32_t* tokens, float temperature,
-                                                           const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy, RowsOf grad) {
-    const int32_t n = rows_here(d_n, cap);
-    const float inv_t = 1.0f / temperature;
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const int32_t t = tokens[i];
-        const float l = lse[i], h = entropy[i], gl = g_logprob && t >= 0 && t < classes ? g_logprob[i] : 0.0f, gh = g_entropy ? g_entropy[i] : 0.0f;
-        for (int32_t c = threadIdx.x; c < classes; c += 256) {
-            const float v = to_f32(z.row<T>(i)[c]);
-            const float log_p = v * inv_t - l, p = v == -INFINITY ? 0.0f : expf(log_p);
-            const float d = (c == t ? gl : 0.0f) - (p == 0.0f ? 0.0f : p * (gl + gh * (log_p + h)));
-            grad.row<T>(i)[c] = from_f32<T>(d * inv_t);
+__device__ __forceinline__ void store_row(const Logprobs& a, int64_t i, const Sums& r, float log_s) {
+    const int32_t tok = a.tokens[i];
+    a.logprob[i] = tok >= 0 && tok < a.classes ? log_share(a, r, log_s, to_f32(a.z.row<T>(i)[tok])) : 0.0f;
+    a.entropy[i] = r.s == 0.0f ? 0.0f : log_s - r.h * a.inv_t / r.s;
+    a.lse[i] = above(r.m) * a.inv_t + log_s;
+}
+
+__device__ __forceinline__ void store_top(const Logprobs& a, int64_t i, int32_t at, uint64_t key, const Sums& r, float log_s) {
+    const bool none = key == 0 || r.s != r.s;
+    a.top_ids[i * a.k + at] = none ? -1 : (int32_t)~(uint32_t)key;
+    a.top_logprobs[i * a.k + at] = r.s != r.s ? NAN : none ? -INFINITY : log_share(a, r, log_s, value_of((uint32_t)(key >> 32)));
+}
+
+template <typename T, int TEAM, int THREADS, int U, bool SPLIT>
+__global__ void __launch_bounds__(THREADS) logprobs_kernel(Logprobs a) {
+    __shared__ float smem[2 * THREADS / 64];
+    __shared__ TopSpace<TEAM> tops[THREADS / TEAM];
+    Team<TEAM, THREADS> team(smem);
+    const int t = team.lane();
+    int64_t i = a.row0 + (int64_t)blockIdx.x * (THREADS / TEAM) + team.index();
+    int32_t p = 0;
+    if constexpr (SPLIT) {
+        p = (int32_t)(blockIdx.x % (uint32_t)a.pieces);
+        i = a.row0 + blockIdx.x / (uint32_t)a.pieces;
+    }
+    if (i >= rows_here(a.d_n, a.cap)) return;
+    const int32_t first = SPLIT ? p * a.piece : 0, len = SPLIT ? min(a.piece, a.classes - first) : a.classes;
+    Piece<T, U, TEAM> v;
+    v.load(a.z.row<T>(i) + first, len, t);
+    const float mine = v.lane_max();
+    Sums r{team.max(mine), 0.0f, 0.0f};
+    v.template add<true>(above(r.m), a.c, r.s, r.h);
+    r.s = team.sum(r.s);
+    r.h = team.sum(r.h);
+    const float log_s = logf(r.s);
+    if (t == 0) {
+        if constexpr (SPLIT) a.parts[i * a.pieces + p] = r;
+        else store_row<T>(a, i, r, log_s);
+    }
+    if (a.k == 0) return;
+    TopSpace<TEAM>& top = tops[team.index()];
+    top_candidates(v, mine, first, a.k, top, team);
+    const int32_t count = min(top.count, TopSpace<TEAM>::CAP);
+    auto put = [&](int32_t at, uint64_t key) {
+        if constexpr (SPLIT) a.keys[(i * a.pieces + p) * a.k + at] = key;
+        else store_top(a, i, at, key, r, log_s);
+    };
+    for (int32_t j = t; j < count; j += TEAM) {
+        const uint64_t key = top.key[j];
+        int32_t rank = 0;
+        for (int32_t o = 0; o < count; ++o) rank += top.key[o] > key;
+        if (rank < a.k) put(rank, key);
+    }
+    for (int32_t j = count + t; j < a.k; j += TEAM) put(j, 0);
+}
+
+// A row from its pieces. A key's rank is the number of larger keys in every piece's ordered list.
+template <typename T>
+__global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
+    constexpr int HELD = 2048;
+    __shared__ float smem[8];
+    __shared__ uint64_t held[HELD];
+    Team<256, 256> team(smem);
+    const int64_t i = a.row0 + blockIdx.x;
+    if (i >= rows_here(a.d_n, a.cap)) return;
+    const int32_t all = a.pieces * a.k;
+    const uint64_t* keys = a.keys + i * all;
+    if (all <= HELD)
+        for (int32_t j = threadIdx.x; j < all; j += 256) held[j] = keys[j];
+    const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);
+    const float log_s = logf(r.s);
+    if (threadIdx.x == 0) store_row<T>(a, i, r, log_s);
+    __syncthreads();
+    auto ranks = [&](const uint64_t* list) {
+        for (int32_t j = threadIdx.x; j < all; j += 256) {
+            const uint64_t key = list[j];
+            const int32_t own = j / a.k;
+            int32_t rank = j - own * a.k;               // larger ones in its own list
+            if (key == 0) {                             // places left over: in order behind all keys
+                for (int32_t o = 0; o < own; ++o) rank += a.k;
+            }
+            for (int32_t o = 0; o < a.pieces; ++o) {
+                if (o == own || rank >= a.k) continue;
+                if (key == 0 && o < own) continue;
+                const uint64_t* l = list + o * a.k;
+                int32_t lo = 0, hi = a.k;
+                while (lo < hi) {
+                    const int32_t mid = (lo + hi) >> 1;
+                    if (l[mid] > key) lo = mid + 1; else hi = mid;
+                }
+                rank += lo;
+            }
+            if (rank < a.k) store_top(a, i, rank, key, r, log_s);
+        }
+    };
+    if (all <= HELD) ranks(held); else ranks(keys);
+}
+
+template <typename T, int U>
+__global__ void __launch_bounds__(256) logprobs_grad_kernel(RowsOf z, const int32_t* d_n, int64_t row0, int32_t cap, int32_t classes, int32_t pieces, const int32_t* __restrict__ tokens, float inv_t,
+                                                            const float* __restrict__ lse, const float* __restrict__ entropy, const float* __restrict__ g_logprob,
+                                                            const float* __restrict__ g_entropy, RowsOf grad) {
+    constexpr int W = Piece<T, U, 256>::W, PIECE = W * U * 256;
+    const int64_t i = row0 + blockIdx.x / (uint32_t)pieces;
+    const int32_t first = (int32_t)(blockIdx.x % (uint32_t)pieces) * PIECE, len = min(PIECE, classes - first);
+    if (i >= rows_here(d_n, cap)) return;
+    Piece<T, U, 256> v;
+    v.load(z.row<T>(i) + first, len, threadIdx.x);
+    const int32_t tok = tokens[i];
+    const float l = lse[i], h = entropy[i], gl = g_logprob && tok >= 0 && tok < classes ? g_logprob[i] : 0.0f, gh = g_entropy ? g_entropy[i] : 0.0f;
+    T* const out = grad.row<T>(i) + first;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t c = v.at(threadIdx.x, u);
+        if (c < len) {
+            float f[W];
+            v.v[u].get(f);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float log_p = f[w] * inv_t - l, p = f[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(log_p * LOG2E);
+                const float d = p == 0.0f ? 0.0f : -(p * (gl + gh * (log_p + h)));
+                f[w] = (first + c + w == tok ? gl + d : d) * inv_t;
+            }
+            Run<T, W> o;
+            o.set(f);
+            o.store(out + c, len - c);
         }
     }
 }
@@ -182,14 +565,131 @@ static int32_t check_teacher(const char* who, int32_t n, const int32_t* ids, con
     return NO_OK;
 }
 
+// Rows in pieces: as many as fill the chip while rows are few, of a multiple of a block's runs.
+struct Cut {
+    int32_t u, piece, pieces;
+    Cut(int32_t n, int32_t classes, int32_t w) {
+        u = 8;
+        while (u > 1 && (int64_t)n * ceil_div(classes, 256 * w * u) < 1024) u >>= 1;
+        piece = 256 * w * u;
+        pieces = (int32_t)ceil_div(classes, piece);
+    }
+};
+static int32_t most_pieces(int32_t n, int32_t classes) { return Cut(n, classes, 4).pieces; }      // (of either type)
+
+constexpr int64_t FEW_ROWS = 128;       // rows that leave half of the chip idle when each is one block's
+
+// A launch holds fewer than 2^32 threads, 2^21 blocks of 1024 among them: more rows go in several.
+template <typename F>
+static void in_slabs(int64_t rows, int64_t rows_per_launch, F launch) {
+    for (int64_t r = 0; r < rows; r += rows_per_launch) launch(r, rows - r < rows_per_launch ? rows - r : rows_per_launch);
+}
+constexpr int64_t MOST_BLOCKS = 1 << 21;
+
+template <typename T>
+static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
+    constexpr int W = 16 / (int)sizeof(T);
+    const int64_t units = ceil_div(a.classes, W);
+#define NO_ROW(TEAM, THREADS, U)                                                                                                                  \
+    in_slabs(a.cap, MOST_BLOCKS * (THREADS / TEAM), [&](int64_t row0, int64_t rows) {                                                             \
+        a.row0 = row0;                                                                                                                            \
+        hipLaunchKernelGGL((distill_row_kernel<T, TEAM, THREADS, U>), dim3((unsigned)ceil_div(rows, THREADS / TEAM)), dim3(THREADS), 0, st, a);   \
+    })
+    const bool row = !a.lse_in && units <= 16384 && (units <= 2048 || (a.grad.p && a.cap >= FEW_ROWS));
+    if (row) {
+        if (units <= 64) NO_ROW(64, 256, 1);
+        else if (units <= 128) NO_ROW(64, 256, 2);
+        else if (units <= 256) NO_ROW(64, 256, 4);
+        else if (units <= 512) NO_ROW(256, 256, 2);
+        else if (units <= 1024) NO_ROW(256, 256, 4);
+        else if (units <= 2048) NO_ROW(256, 256, 8);
+        else if (units <= 4096) NO_ROW(1024, 1024, 4);
+        else if (units <= 8192) NO_ROW(1024, 1024, 8);
+        else NO_ROW(1024, 1024, 16);
+        return launch_status(who);
+    }
+#undef NO_ROW
+    const Cut cut(a.cap, a.classes, W);
+    a.piece = cut.piece;
+    a.pieces = cut.pieces;
+    a.parts = (Sums*)ws;
+#define NO_PIECES(KERNEL)                                                                                              \
+    in_slabs(a.cap, MOST_BLOCKS / a.pieces, [&](int64_t row0, int64_t rows) {                                          \
+        const dim3 grid((unsigned)(rows * a.pieces));                                                                  \
+        a.row0 = row0;                                                                                                 \
+        if (cut.u == 8) hipLaunchKernelGGL((KERNEL<T, 256, 8>), grid, dim3(256), 0, st, a);                            \
+        else if (cut.u == 4) hipLaunchKernelGGL((KERNEL<T, 256, 4>), grid, dim3(256), 0, st, a);                       \
+        else if (cut.u == 2) hipLaunchKernelGGL((KERNEL<T, 256, 2>), grid, dim3(256), 0, st, a);                       \
+        else hipLaunchKernelGGL((KERNEL<T, 256, 1>), grid, dim3(256), 0, st, a);                                       \
+    })
+    if (!a.lse_in) {
+        NO_PIECES(distill_sums_kernel);
+        in_slabs(a.cap, MOST_BLOCKS * 4, [&](int64_t row0, int64_t rows) {
+            a.row0 = row0;
+            hipLaunchKernelGGL(distill_loss_kernel<T>, dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, a);
+        });
+    }
+    if (a.grad.p) NO_PIECES(distill_grad_kernel);
+#undef NO_PIECES
+    return launch_status(who);
+}
+
 static int32_t distill(const char* who, const void* z, no_dtype dt, int64_t stride, const int32_t* d_n, int32_t cap, int32_t classes, const int32_t* ids,
                        const float* logits, int32_t k, float temperature, const float* weight, float* loss, const float* lse_in, float* lse_out, void* grad,
-                       int64_t grad_stride, hipStream_t st) {
-    if (cap == 0) return NO_OK;
-    const dim3 grid((unsigned)(cap < 65536 ? cap : 65536));
-    const RowsOf rows = rows_of(z, stride), out = rows_of(grad, grad_stride);
-    if (dt == NO_F32) hipLaunchKernelGGL(distill_kernel<float>, grid, dim3(256), 0, st, rows, d_n, cap, classes, ids, logits, k, temperature, weight, loss, lse_in, lse_out, out);
-    else hipLaunchKernelGGL(distill_kernel<bf16_t>, grid, dim3(256), 0, st, rows, d_n, cap, classes, ids, logits, k, temperature, weight, loss, lse_in, lse_out, out);
+                       int64_t grad_stride, void* ws, hipStream_t st) {
+    const float inv_t = 1.0f / temperature;
+    const Distill a{rows_of(z, stride), d_n, 0, cap, classes, ids, logits, k, temperature, inv_t, inv_t * LOG2E, weight, loss, lse_in, lse_out, rows_of(grad, grad_stride),
+                    nullptr, 1, classes};
+    return dt == NO_F32 ? distill<float>(who, a, ws, st) : distill<bf16_t>(who, a, ws, st);
+}
+
+static size_t parts_bytes(int32_t n, int32_t classes) { return ((size_t)n * (size_t)most_pieces(n, classes) * sizeof(Sums) + 15) / 16 * 16; }
+
+template <typename T>
+static int32_t logprobs(const char* who, Logprobs a, void* ws, hipStream_t st) {
+    constexpr int W = 16 / (int)sizeof(T);
+    const int64_t units = ceil_div(a.classes, W);
+#define NO_ROW(TEAM, U)                                                                                                                        \
+    in_slabs(a.cap, MOST_BLOCKS * (256 / TEAM), [&](int64_t row0, int64_t rows) {                                                              \
+        a.row0 = row0;                                                                                                                         \
+        hipLaunchKernelGGL((logprobs_kernel<T, TEAM, 256, U, false>), dim3((unsigned)ceil_div(rows, 256 / TEAM)), dim3(256), 0, st, a);        \
+    })
+    if (units <= 64) NO_ROW(64, 1);
+    else if (units <= 128) NO_ROW(64, 2);
+    else if (units <= 256) NO_ROW(64, 4);
+    else if (units <= 512) NO_ROW(256, 2);
+    else if (units <= 1024) NO_ROW(256, 4);
+    else if (units <= 2048) NO_ROW(256, 8);
+#undef NO_ROW
+    else {
+        const Cut cut(a.cap, a.classes, W);
+        a.piece = cut.piece;
+        a.pieces = cut.pieces;
+        a.parts = (Sums*)ws;
+        a.keys = (uint64_t*)((char*)ws + parts_bytes(a.cap, a.classes));
+        in_slabs(a.cap, MOST_BLOCKS / a.pieces, [&](int64_t row0, int64_t rows) {
+            const dim3 grid((unsigned)(rows * a.pieces));
+            a.row0 = row0;
+            if (cut.u == 8) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 8, true>), grid, dim3(256), 0, st, a);
+            else if (cut.u == 4) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 4, true>), grid, dim3(256), 0, st, a);
+            else if (cut.u == 2) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 2, true>), grid, dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 1, true>), grid, dim3(256), 0, st, a);
+            hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)rows), dim3(256), 0, st, a);
+        });
+    }
+    return launch_status(who);
+}
+
+template <typename T>
+static int32_t logprobs_grad(const char* who, const RowsOf& z, const int32_t* d_n, int32_t cap, int32_t classes, const int32_t* tokens, float inv_t, const float* lse,
+                             const float* entropy, const float* g_logprob, const float* g_entropy, const RowsOf& grad, hipStream_t st) {
+    const Cut cut(cap, classes, 16 / (int)sizeof(T));
+#define NO_GRAD(U) hipLaunchKernelGGL((logprobs_grad_kernel<T, U>), grid, dim3(256), 0, st, z, d_n, row0, cap, classes, cut.pieces, tokens, inv_t, lse, entropy, g_logprob, g_entropy, grad)
+    in_slabs(cap, MOST_BLOCKS / cut.pieces, [&](int64_t row0, int64_t rows) {
+        const dim3 grid((unsigned)(rows * cut.pieces));
+        if (cut.u == 8) NO_GRAD(8); else if (cut.u == 4) NO_GRAD(4); else if (cut.u == 2) NO_GRAD(2); else NO_GRAD(1);
+    });
+#undef NO_GRAD
     return launch_status(who);
 }
 
@@ -199,7 +699,7 @@ using namespace no;
 
 extern "C" size_t no_distill_ws_bytes(int32_t n_rows_cap, int32_t n_classes) {
     if (n_rows_cap < 0 || n_classes < 1 || n_classes > NO_MAX_CLASSES) return 0;
-    return 16;
+    return 16 + parts_bytes(n_rows_cap, n_classes);
 }
 
 extern "C" int32_t no_distill_fwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
@@ -212,7 +712,7 @@ extern "C" int32_t no_distill_fwd(const void* d_z, no_dtype dt, int64_t z_stride
     NO_REQUIRE((d_loss && d_lse) || n_rows_cap == 0, NO_ERR_INVALID_ARG, "%s: NULL output", who);
     NO_CHECK(check_ws(who, d_ws, ws_bytes, no_distill_ws_bytes(n_rows_cap, n_classes)));
     return distill(who, d_z, dt, z_stride_bytes, d_n_rows, n_rows_cap, n_classes, d_teacher_ids, d_teacher_logits, k, temperature, d_row_weight, d_loss, nullptr,
-                   d_lse, nullptr, 0, (hipStream_t)stream);
+                   d_lse, nullptr, 0, d_ws, (hipStream_t)stream);
 }
 
 extern "C" int32_t no_distill_bwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
@@ -225,7 +725,7 @@ extern "C" int32_t no_distill_bwd(const void* d_z, no_dtype dt, int64_t z_stride
     NO_CHECK(check_rows(who, "grad_z", d_grad_z, dt, n_rows_cap, n_classes, grad_stride_bytes));
     NO_REQUIRE(d_lse || n_rows_cap == 0, NO_ERR_INVALID_ARG, "%s: lse is NULL", who);
     return distill(who, d_z, dt, z_stride_bytes, d_n_rows, n_rows_cap, n_classes, d_teacher_ids, d_teacher_logits, k, temperature, d_row_weight, nullptr, d_lse,
-                   nullptr, d_grad_z, grad_stride_bytes, (hipStream_t)stream);
+                   nullptr, d_grad_z, grad_stride_bytes, nullptr, (hipStream_t)stream);
 }
 
 extern "C" int32_t no_distill_fwd_bwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap,
@@ -240,12 +740,12 @@ extern "C" int32_t no_distill_fwd_bwd(const void* d_z, no_dtype dt, int64_t z_st
     NO_REQUIRE(d_loss || n_rows_cap == 0, NO_ERR_INVALID_ARG, "%s: loss is NULL", who);
     NO_CHECK(check_ws(who, d_ws, ws_bytes, no_distill_ws_bytes(n_rows_cap, n_classes)));
     return distill(who, d_z, dt, z_stride_bytes, d_n_rows, n_rows_cap, n_classes, d_teacher_ids, d_teacher_logits, k, temperature, d_row_weight, d_loss, nullptr,
-                   d_lse, d_grad_z, grad_stride_bytes, (hipStream_t)stream);
+                   d_lse, d_grad_z, grad_stride_bytes, d_ws, (hipStream_t)stream);
 }
 
 extern "C" size_t no_logprobs_ws_bytes(int32_t n_rows_cap, int32_t n_classes, int32_t k) {
     if (n_rows_cap < 0 || n_classes < 1 || n_classes > NO_MAX_CLASSES || k < 0 || k > NO_MAX_ALTERNATIVES) return 0;
-    return 16;
+    return 16 + parts_bytes(n_rows_cap, n_classes) + (size_t)n_rows_cap * (size_t)most_pieces(n_rows_cap, n_classes) * (size_t)k * 8;
 }
 
 extern "C" int32_t no_logprobs_fwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
@@ -260,11 +760,10 @@ extern "C" int32_t no_logprobs_fwd(const void* d_z, no_dtype dt, int64_t z_strid
     NO_REQUIRE((d_top_ids && d_top_logprobs) || n_rows_cap == 0 || k == 0, NO_ERR_INVALID_ARG, "%s: the alternatives' arrays are NULL", who);
     NO_CHECK(check_ws(who, d_ws, ws_bytes, no_logprobs_ws_bytes(n_rows_cap, n_classes, k)));
     if (n_rows_cap == 0) return NO_OK;
-    const dim3 grid((unsigned)(n_rows_cap < 65536 ? n_rows_cap : 65536));
-    const RowsOf z = rows_of(d_z, z_stride_bytes);
-    if (dt == NO_F32) hipLaunchKernelGGL(logprobs_fwd_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, z, d_n_rows, n_rows_cap, n_classes, d_tokens, temperature, d_logprob, d_entropy, d_lse, k, d_top_ids, d_top_logprobs);
-    else hipLaunchKernelGGL(logprobs_fwd_kernel<bf16_t>, grid, dim3(256), 0, (hipStream_t)stream, z, d_n_rows, n_rows_cap, n_classes, d_tokens, temperature, d_logprob, d_entropy, d_lse, k, d_top_ids, d_top_logprobs);
-    return launch_status(who);
+    const float inv_t = 1.0f / temperature;
+    const Logprobs a{rows_of(d_z, z_stride_bytes), d_n_rows, 0, n_rows_cap, n_classes, d_tokens, inv_t, inv_t * LOG2E, d_logprob, d_entropy, d_lse, k, d_top_ids, d_top_logprobs,
+                     nullptr, nullptr, 1, n_classes};
+    return dt == NO_F32 ? logprobs<float>(who, a, d_ws, (hipStream_t)stream) : logprobs<bf16_t>(who, a, d_ws, (hipStream_t)stream);
 }
 
 extern "C" int32_t no_logprobs_bwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
@@ -276,9 +775,9 @@ extern "C" int32_t no_logprobs_bwd(const void* d_z, no_dtype dt, int64_t z_strid
     NO_CHECK(check_rows(who, "grad_z", d_grad_z, dt, n_rows_cap, n_classes, grad_stride_bytes));
     NO_REQUIRE((d_tokens && d_lse && d_entropy) || n_rows_cap == 0, NO_ERR_INVALID_ARG, "%s: NULL argument", who);
     if (n_rows_cap == 0) return NO_OK;
-    const dim3 grid((unsigned)(n_rows_cap < 65536 ? n_rows_cap : 65536));
     const RowsOf z = rows_of(d_z, z_stride_bytes), g = rows_of(d_grad_z, grad_stride_bytes);
-    if (dt == NO_F32) hipLaunchKernelGGL(logprobs_bwd_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, z, d_n_rows, n_rows_cap, n_classes, d_tokens, temperature, d_lse, d_entropy, d_grad_logprob, d_grad_entropy, g);
-    else hipLaunchKernelGGL(logprobs_bwd_kernel<bf16_t>, grid, dim3(256), 0, (hipStream_t)stream, z, d_n_rows, n_rows_cap, n_classes, d_tokens, temperature, d_lse, d_entropy, d_grad_logprob, d_grad_entropy, g);
-    return launch_status(who);
+    const float inv_t = 1.0f / temperature;
+    hipStream_t st = (hipStream_t)stream;
+    return dt == NO_F32 ? logprobs_grad<float>(who, z, d_n_rows, n_rows_cap, n_classes, d_tokens, inv_t, d_lse, d_entropy, d_grad_logprob, d_grad_entropy, g, st)
+                        : logprobs_grad<bf16_t>(who, z, d_n_rows, n_rows_cap, n_classes, d_tokens, inv_t, d_lse, d_entropy, d_grad_logprob, d_grad_entropy, g, st);
 }

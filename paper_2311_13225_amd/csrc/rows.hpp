@@ -131,6 +131,15 @@ struct Team {
         }
         return v;
     }
+    // what the team's lanes wrote before, its lanes see after
+    __device__ __forceinline__ static void sync() {
+        if constexpr (TEAM > 64) __syncthreads();
+        else {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+    }
     __device__ __forceinline__ float sum(float v) { return reduce(v, [](float a, float b) { return a + b; }); }
     __device__ __forceinline__ float max(float v) { return reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
 };

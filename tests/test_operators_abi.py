@@ -32,12 +32,13 @@ def test_embed_refusals(lib):
     good = [P, 0, 10, 8, 32, None, P, None, 4, 1.0, P, 0, 32, None]
     swept(lib.no_embed_fwd, good, [({0: None}, INVALID), ({6: None}, INVALID), ({10: None}, INVALID), ({1: 3}, INVALID), ({1: -1}, INVALID), ({11: 2}, INVALID),
                                    ({2: 0}, INVALID), ({3: 0}, INVALID), ({8: -1}, INVALID), ({4: 28}, INVALID), ({4: 33}, INVALID), ({12: 16}, INVALID),
-                                   ({0: ODD}, INVALID), ({1: 1, 0: ODD}, INVALID), ({12: -32}, INVALID)])
+                                   ({0: ODD}, INVALID), ({1: 1, 0: ODD}, INVALID), ({12: -32}, INVALID), ({3: (1 << 20) + 1, 4: 1 << 23, 12: 1 << 23}, UNSUPPORTED)])
     #       grad dt stride ids n cap scale acc table rows dim stride ws bytes stream
     good = [P, 0, 32, P, None, 4, 1.0, 0, P, 10, 8, 32, P, 1 << 30, None]
     swept(lib.no_embed_bwd, good, [({0: None}, INVALID), ({3: None}, INVALID), ({8: None}, INVALID), ({12: None}, INVALID), ({12: ODD}, INVALID), ({1: 2}, INVALID),
-                                   ({5: -1}, INVALID), ({9: 0}, INVALID), ({9: 1 << 31}, INVALID), ({10: 0}, INVALID), ({2: 28}, INVALID), ({11: 28}, INVALID), ({8: ODD}, INVALID), ({13: 1}, CAPACITY)])
-    assert lib.no_embed_ws_bytes(-1, 4) == 0 and lib.no_embed_ws_bytes(4, 0) == 0 and lib.no_embed_ws_bytes(0, 1) > 0
+                                   ({5: -1}, INVALID), ({9: 0}, INVALID), ({9: 1 << 31}, INVALID), ({10: 0}, INVALID), ({2: 28}, INVALID), ({11: 28}, INVALID), ({8: ODD}, INVALID), ({13: 1}, CAPACITY),
+                                   ({10: (1 << 20) + 1, 2: 1 << 23, 11: 1 << 23}, UNSUPPORTED)])
+    assert lib.no_embed_ws_bytes(-1, 4) == 0 and lib.no_embed_ws_bytes(4, 0) == 0 and lib.no_embed_ws_bytes(4, (1 << 20) + 1) == 0 and lib.no_embed_ws_bytes(0, 1) > 0
     assert lib.no_embed_ws_bytes(2_000_000_000, 100_000) >= lib.no_embed_ws_bytes(1_000_000, 100_000)
 
 
