@@ -27,6 +27,12 @@ struct Piece {      // a lane's runs of z[0, len): run u covers values [(lane + 
             v[u].load(z + min(c, len), len - c, from_f32<T>(-INFINITY));
         }
     }
+    // Between two passes over the values: without it the compiler keeps what the first one converted to fp32 (twice the registers, spilled in
+    // the largest kernels) instead of converting again, one instruction a value.
+    __device__ __forceinline__ void renew() {
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm volatile("" : "+v"(v[u].v[0]));
+    }
     __device__ __forceinline__ float lane_max() const {
         float m = -INFINITY;
 #pragma unroll
@@ -215,7 +221,9 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(Distill a) {
     const float w = a.weight ? a.weight[i] : 1.0f;
     const bool any = teacher_shares(a.ids + i * a.k, a.logits + i * a.k, a.k, a.classes, a.inv_t, z, 0, a.classes, te, team);
     Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
+    v.renew();
     v.template add<false>(above(r.m), a.c, r.s, r.h);
+    v.renew();
     r.s = team.sum(r.s);
     distill_loss(a, i, r, w, any, te, team);
     if (a.grad.p) distill_grad(a, i, 0, a.classes, v, Share{above(r.m), a.c, 1.0f / r.s, a.inv_t, 0.0f, false}, w, any, te, team);
@@ -232,6 +240,7 @@ __global__ void __launch_bounds__(THREADS) distill_sums_kernel(Distill a) {
     Piece<T, U, THREADS> v;
     v.load(a.z.row<T>(i) + (int64_t)p * a.piece, min(a.piece, a.classes - p * a.piece), team.lane());
     Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
+    v.renew();
     v.template add<false>(above(r.m), a.c, r.s, r.h);
     r.s = team.sum(r.s);
     if (threadIdx.x == 0) a.parts[i * a.pieces + p] = r;
@@ -297,7 +306,7 @@ struct TopSpace {
 // own maxima is a bound that k values at least reach, and few others do as a rule: those that do are collected. Where more do than there is room for (equal
 // values, or large ones that sit in few lanes), the bound is raised bit by bit, first by value, then among equal ones by class.
 template <typename T, int U, int TEAM, int THREADS>
-__device__ void top_candidates(const Piece<T, U, TEAM>& v, float lane_max, int32_t first, int32_t k, TopSpace<TEAM>& to, Team<TEAM, THREADS>& team) {
+__device__ __forceinline__ void top_candidates(Piece<T, U, TEAM>& v, float lane_max, int32_t first, int32_t k, TopSpace<TEAM>& to, Team<TEAM, THREADS>& team) {
     constexpr int W = Piece<T, U, TEAM>::W, Q = TEAM > 64 ? TEAM / 64 : 1;
     const int t = team.lane();
     // the k-th largest lane maximum, its upper 16 bits (so a little less than it): one wavefront looks for them bit by bit
@@ -346,6 +355,7 @@ __device__ void top_candidates(const Piece<T, U, TEAM>& v, float lane_max, int32
     // how many values are at least x, or are larger than x or equal to it with a class below c
     auto count = [&](float x, bool ties, int32_t c) {
         int here = 0;
+        v.renew();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float f[W];
@@ -375,6 +385,7 @@ __device__ void top_candidates(const Piece<T, U, TEAM>& v, float lane_max, int32
     team.sync();
     if (t == 0) to.count = 0;
     team.sync();
+    v.renew();
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         float f[W];
@@ -445,7 +456,9 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(Logprobs a) {
     v.load(a.z.row<T>(i) + first, len, t);
     const float mine = v.lane_max();
     Sums r{team.max(mine), 0.0f, 0.0f};
+    v.renew();
     v.template add<true>(above(r.m), a.c, r.s, r.h);
+    v.renew();
     r.s = team.sum(r.s);
     r.h = team.sum(r.h);
     const float log_s = logf(r.s);
@@ -470,35 +483,61 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(Logprobs a) {
     for (int32_t j = count + t; j < a.k; j += TEAM) put(j, 0);
 }
 
-// A row from its pieces. A key's rank is the number of larger keys in every piece's ordered list.
+// A row from its pieces. Of every piece's list the j-th key is looked at, j the least with j pieces >= k: r = ceil(k / j) lists whose j-th key reaches a bound hold k keys
+// that do, so the r-th largest of those keys is a bound; the keys that reach it are ranked against each other. (With more lists than lanes a lane
+// takes the largest of several lists' first keys.) Where large values stand in few pieces more keys than there is room for may reach the bound: then
+// every key is ranked by a search in every other list.
 template <typename T>
 __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
-    constexpr int HELD = 2048;
+    constexpr int CAP = 1024;
     __shared__ float smem[8];
-    __shared__ uint64_t held[HELD];
+    __shared__ uint64_t lane_key[256], cand[CAP], bound;
+    __shared__ int32_t count;
     Team<256, 256> team(smem);
     const int64_t i = a.row0 + blockIdx.x;
     if (i >= rows_here(a.d_n, a.cap)) return;
-    const int32_t all = a.pieces * a.k;
-    const uint64_t* keys = a.keys + i * all;
-    if (all <= HELD)
-        for (int32_t j = threadIdx.x; j < all; j += 256) held[j] = keys[j];
+    const int32_t t = threadIdx.x, all = a.pieces * a.k;
+    const uint64_t* const keys = a.keys + i * all;
+    if (a.k > 0) {
+        const int32_t j = (a.k + a.pieces - 1) / a.pieces, need = (a.k + j - 1) / j, lanes = min(a.pieces, 256);
+        uint64_t mine = 0;
+        for (int32_t p = t; p < a.pieces; p += 256) mine = max(mine, keys[p * a.k + j - 1]);
+        lane_key[t] = mine;
+        if (t == 0) { bound = 1; count = 0; }
+        __syncthreads();
+        int32_t rank = 0;
+        for (int32_t o = 0; o < lanes; ++o) rank += lane_key[o] > mine;
+        if (rank == need - 1 && mine != 0) bound = mine;        // (keys are all different; fewer than `need` above 0: all of them)
+    }
     const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);
     const float log_s = logf(r.s);
-    if (threadIdx.x == 0) store_row<T>(a, i, r, log_s);
+    if (t == 0) store_row<T>(a, i, r, log_s);
+    if (a.k == 0) return;
     __syncthreads();
-    auto ranks = [&](const uint64_t* list) {
-        for (int32_t j = threadIdx.x; j < all; j += 256) {
-            const uint64_t key = list[j];
-            const int32_t own = j / a.k;
-            int32_t rank = j - own * a.k;               // larger ones in its own list
-            if (key == 0) {                             // places left over: in order behind all keys
-                for (int32_t o = 0; o < own; ++o) rank += a.k;
-            }
-            for (int32_t o = 0; o < a.pieces; ++o) {
-                if (o == own || rank >= a.k) continue;
-                if (key == 0 && o < own) continue;
-                const uint64_t* l = list + o * a.k;
+    for (int32_t e = t; e < all; e += 256) {
+        const uint64_t key = keys[e];
+        if (key >= bound) {
+            const int32_t at = atomicAdd(&count, 1);
+            if (at < CAP) cand[at] = key;
+        }
+    }
+    __syncthreads();
+    if (count <= CAP) {
+        for (int32_t e = t; e < count; e += 256) {
+            const uint64_t key = cand[e];
+            int32_t rank = 0;
+            for (int32_t o = 0; o < count; ++o) rank += cand[o] > key;
+            if (rank < a.k) store_top(a, i, rank, key, r, log_s);
+        }
+    } else {
+        for (int32_t e = t; e < all; e += 256) {
+            const uint64_t key = keys[e];
+            if (key < bound) continue;
+            const int32_t own = e / a.k;
+            int32_t rank = e - own * a.k;                       // larger ones in its own list
+            for (int32_t o = 0; o < a.pieces && rank < a.k; ++o) {
+                if (o == own) continue;
+                const uint64_t* l = keys + o * a.k;
                 int32_t lo = 0, hi = a.k;
                 while (lo < hi) {
                     const int32_t mid = (lo + hi) >> 1;
@@ -508,8 +547,8 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
             }
             if (rank < a.k) store_top(a, i, rank, key, r, log_s);
         }
-    };
-    if (all <= HELD) ranks(held); else ranks(keys);
+    }
+    for (int32_t e = count + t; e < a.k; e += 256) store_top(a, i, e, 0, r, log_s);
 }
 
 template <typename T, int U>
