@@ -457,6 +457,13 @@ NO_MAX_EMBED_DIM, NO_MAX_NORM_DIM, NO_MAX_CLASSES, NO_MAX_TEACHER, NO_MAX_ALTERN
 _OP_DTYPES = {torch.float32: NO_F32, torch.bfloat16: NO_BF16, torch.float8_e4m3fn: NO_E4M3}
 
 
+def _stream_of(stream) -> int:
+    """_stream for calls of a few microseconds: the current stream's address without the object around it."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return _stream(stream)
+
+
 def _rows(t: Optional[torch.Tensor], n: int, dim: int, dtype: Optional[torch.dtype] = None):
     """(address, stride in bytes) of a row matrix [n, dim] whose rows are dense; (None, 0) of None."""
     if t is None:
@@ -493,7 +500,7 @@ def no_embed_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scal
     n = ids.numel()
     (pt, st), (po, so) = _rows(table, v, dim), _rows(out, n, dim)
     _check(lib().no_embed_fwd(pt, _OP_DTYPES.get(table.dtype, -1), v, dim, st, _vec(row_scale, v), _vec(ids, n, torch.int32),
-                              _count(n_ids), n, scale, po, _OP_DTYPES.get(out.dtype, -1), so, _stream(stream)))
+                              _count(n_ids), n, scale, po, _OP_DTYPES.get(out.dtype, -1), so, _stream_of(stream)))
     return out
 
 
@@ -508,7 +515,7 @@ def no_embed_bwd(grad_out: torch.Tensor, ids: torch.Tensor, grad_table: torch.Te
     n = ids.numel()
     (pg, sg), (pt, st), (pw, bw) = _rows(grad_out, n, dim), _rows(grad_table, v, dim, torch.float32), _ws(ws)
     _check(lib().no_embed_bwd(pg, _OP_DTYPES.get(grad_out.dtype, -1), sg, _vec(ids, n, torch.int32), _count(n_ids), n, scale,
-                              1 if accumulate else 0, pt, v, dim, st, pw, bw, _stream(stream)))
+                              1 if accumulate else 0, pt, v, dim, st, pw, bw, _stream_of(stream)))
     return grad_table
 
 
@@ -521,7 +528,7 @@ def no_rmsnorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, 
     n, dim = x.shape
     (px, sx), (pr, sr), (ps, ss), (py, sy) = _rows(x, n, dim), _rows(residual, n, dim, x.dtype), _rows(sum_out, n, dim, x.dtype), _rows(y, n, dim)
     _check(lib().no_rmsnorm_fwd(px, _OP_DTYPES.get(x.dtype, -1), sx, pr, sr, _vec(weight, dim), eps, _count(n_rows), n, dim, ps, ss,
-                                py, _OP_DTYPES.get(y.dtype, -1), sy, _vec(row_scale, n), _vec(rstd, n), _stream(stream)))
+                                py, _OP_DTYPES.get(y.dtype, -1), sy, _vec(row_scale, n), _vec(rstd, n), _stream_of(stream)))
     return y
 
 
@@ -537,7 +544,7 @@ def no_rmsnorm_bwd(s: torch.Tensor, weight: Optional[torch.Tensor], rstd: torch.
     (ps, ss), (pg, sg), (pa, sa) = _rows(s, n, dim), _rows(grad_y, n, dim, s.dtype), _rows(grad_sum, n, dim, s.dtype)
     (px, sx), (pw, bw) = _rows(grad_x, n, dim, s.dtype), _ws(ws)
     _check(lib().no_rmsnorm_bwd(ps, _OP_DTYPES.get(s.dtype, -1), ss, _vec(weight, dim), _vec(rstd, n), pg, sg, pa, sa, _count(n_rows), n,
-                                dim, px, sx, _vec(grad_weight, dim), pw, bw, _stream(stream)))
+                                dim, px, sx, _vec(grad_weight, dim), pw, bw, _stream_of(stream)))
 
 
 def _teacher(z: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor, row_weight: Optional[torch.Tensor], n_rows):
@@ -556,7 +563,7 @@ def no_distill_fwd(z: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: t
                    row_weight: Optional[torch.Tensor], loss: torch.Tensor, lse: torch.Tensor, ws: torch.Tensor, n_rows=None, stream=None):
     """Per-row loss of the logits z against the teacher's k entries (ids outside the classes are left out), and the rows' lse."""
     args, w = _teacher(z, teacher_ids, teacher_logits, row_weight, n_rows)
-    _check(lib().no_distill_fwd(*args, temperature, w, _vec(loss, z.shape[0]), _vec(lse, z.shape[0]), *_ws(ws), _stream(stream)))
+    _check(lib().no_distill_fwd(*args, temperature, w, _vec(loss, z.shape[0]), _vec(lse, z.shape[0]), *_ws(ws), _stream_of(stream)))
 
 
 def no_distill_bwd(z: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, temperature: float,
@@ -564,7 +571,7 @@ def no_distill_bwd(z: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: t
     """grad_z = row_weight * T * (softmax(z / T) - teacher's shares), from the forward pass's lse."""
     args, w = _teacher(z, teacher_ids, teacher_logits, row_weight, n_rows)
     pg, sg = _rows(grad_z, *z.shape, z.dtype)
-    _check(lib().no_distill_bwd(*args, temperature, w, _vec(lse, z.shape[0]), pg, sg, _stream(stream)))
+    _check(lib().no_distill_bwd(*args, temperature, w, _vec(lse, z.shape[0]), pg, sg, _stream_of(stream)))
 
 
 def no_distill_fwd_bwd(z: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, temperature: float,
@@ -573,7 +580,7 @@ def no_distill_fwd_bwd(z: torch.Tensor, teacher_ids: torch.Tensor, teacher_logit
     """Loss and gradient in one call (the row weights are known before it)."""
     args, w = _teacher(z, teacher_ids, teacher_logits, row_weight, n_rows)
     pg, sg = _rows(grad_z, *z.shape, z.dtype)
-    _check(lib().no_distill_fwd_bwd(*args, temperature, w, _vec(loss, z.shape[0]), _vec(lse, z.shape[0]), pg, sg, *_ws(ws), _stream(stream)))
+    _check(lib().no_distill_fwd_bwd(*args, temperature, w, _vec(loss, z.shape[0]), _vec(lse, z.shape[0]), pg, sg, *_ws(ws), _stream_of(stream)))
 
 
 def no_logprobs_ws_bytes(n_rows_cap: int, n_classes: int, k: int) -> int:
@@ -590,7 +597,7 @@ def no_logprobs_fwd(z: torch.Tensor, tokens: torch.Tensor, temperature: float, l
     pz, sz = _rows(z, n, c)
     _check(lib().no_logprobs_fwd(pz, _OP_DTYPES.get(z.dtype, -1), sz, _count(n_rows), n, c, _vec(tokens, n, torch.int32), temperature,
                                  _vec(logprob, n), _vec(entropy, n), _vec(lse, n), k, _vec(top_ids, n * k, torch.int32),
-                                 _vec(top_logprobs, n * k), *_ws(ws), _stream(stream)))
+                                 _vec(top_logprobs, n * k), *_ws(ws), _stream_of(stream)))
 
 
 def no_logprobs_bwd(z: torch.Tensor, tokens: torch.Tensor, temperature: float, lse: torch.Tensor, entropy: torch.Tensor,
@@ -600,7 +607,7 @@ def no_logprobs_bwd(z: torch.Tensor, tokens: torch.Tensor, temperature: float, l
     n, c = z.shape
     (pz, sz), (pg, sg) = _rows(z, n, c), _rows(grad_z, n, c, z.dtype)
     _check(lib().no_logprobs_bwd(pz, _OP_DTYPES.get(z.dtype, -1), sz, _count(n_rows), n, c, _vec(tokens, n, torch.int32), temperature,
-                                 _vec(lse, n), _vec(entropy, n), _vec(grad_logprob, n), _vec(grad_entropy, n), pg, sg, _stream(stream)))
+                                 _vec(lse, n), _vec(entropy, n), _vec(grad_logprob, n), _vec(grad_entropy, n), pg, sg, _stream_of(stream)))
 
 
 # ------------------------------------------------------------------------------------------ model / step

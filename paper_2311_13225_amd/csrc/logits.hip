@@ -24,7 +24,7 @@ struct Piece {      // a lane's runs of z[0, len): run u covers values [(lane + 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t c = at(t, u);
-            v[u].load(z + min(c, len), len - c, from_f32<T>(-INFINITY));
+            v[u].load(z + u * TEAM * W + t * W, len - c, from_f32<T>(-INFINITY));      // (not followed where nothing is there)
         }
     }
     // Between two passes over the values: without it the compiler keeps what the first one converted to fp32 (twice the registers, spilled in
@@ -80,53 +80,15 @@ __device__ __forceinline__ Sums join_sums(const Sums* parts, int32_t pieces, flo
 
 // ------------------------------------------------------------------------------------------------------- teacher
 
-// The teacher's entries of a row in LDS: class (-1: left out), share, its logarithm, and the student's logit there.
+// The teacher's entries of a row in LDS: class (-1: left out), share, its logarithm, and the student's logit there. One wavefront makes them, four entries a
+// lane, without a barrier; in blocks of several the others take the row's maximum meanwhile.
 struct Teacher {
     int32_t id[NO_MAX_TEACHER];
     float p[NO_MAX_TEACHER], log_p[NO_MAX_TEACHER], z[NO_MAX_TEACHER];
+    int32_t any;        // whether an entry is above -inf
 };
-
-// Fills `to` with softmax(logits / T) over the entries inside the classes, and with the student's logits at those in [lo, hi); returns whether any
-// entry is above -inf.
-template <typename T, int TEAM, int THREADS>
-__device__ __forceinline__ bool teacher_shares(const int32_t* __restrict__ ids, const float* __restrict__ logits, int32_t k, int32_t classes, float inv_t, const T* z, int32_t lo, int32_t hi,
-                                               Teacher& to, Team<TEAM, THREADS>& team) {
-    constexpr int Q = TEAM < NO_MAX_TEACHER ? NO_MAX_TEACHER / TEAM : 1;
-    const int t = team.lane();
-    int32_t id[Q];
-    float x[Q], zz[Q], m = -INFINITY, s = 0.0f;
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        const int j = t + q * TEAM;
-        id[q] = j < k ? ids[j] : -1;
-        const bool there = id[q] >= 0 && id[q] < classes;
-        x[q] = there ? logits[j] : -INFINITY;
-        zz[q] = id[q] >= lo && id[q] < hi ? to_f32(z[id[q]]) : 0.0f;
-        if (!there) id[q] = -1;
-        m = fmaxf(m, x[q]);
-    }
-    const float from = above(team.max(m));
-    float e[Q];
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        e[q] = id[q] < 0 ? 0.0f : expf((x[q] - from) * inv_t);
-        s += e[q];
-    }
-    s = team.sum(s);
-    const float log_s = logf(s);
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        const int j = t + q * TEAM;
-        if (j < k) {
-            to.id[j] = id[q];
-            to.p[j] = s == 0.0f ? 0.0f : e[q] / s;
-            to.log_p[j] = (x[q] - from) * inv_t - log_s;
-            to.z[j] = zz[q];
-        }
-    }
-    team.sync();
-    return s != 0.0f;
-}
+constexpr int TEACHER_Q = NO_MAX_TEACHER / 64;
+static_assert(TEACHER_Q * 64 == NO_MAX_TEACHER, "entries go evenly over a wavefront");
 
 struct Distill {
     RowsOf z;
@@ -146,40 +108,94 @@ struct Distill {
     int32_t pieces, piece;          // pieces a row, values a piece (a multiple of a run)
 };
 
-// Loss and lse of a row whose sums are known; all lanes of the team call it.
-template <int TEAM, int THREADS>
-__device__ __forceinline__ void distill_loss(const Distill& a, int64_t i, const Sums& r, float w, bool any, const Teacher& te, Team<TEAM, THREADS>& team) {
-    const float log_s = logf(r.s), from = above(r.m);
-    if (a.loss) {
-        float term = 0.0f;
-        for (int j = team.lane(); j < a.k; j += TEAM)
-            if (te.p[j] != 0.0f) term += te.p[j] * (te.log_p[j] - (r.s == 0.0f ? -INFINITY : (te.z[j] - from) * a.inv_t - log_s));
-        term = team.sum(term);
-        if (team.lane() == 0) a.loss[i] = w == 0.0f || !any ? 0.0f : w * a.temperature * a.temperature * term;
-    }
-    if (a.lse_out && team.lane() == 0) a.lse_out[i] = from * a.inv_t + log_s;
-}
+typedef Team<64, 64> Wave;
 
-// A share of a class in the student's row: from the row's sums, or from its lse.
-struct Share {
-    float from, c, inv_s, inv_t, lse;
-    bool by_lse;
-    __device__ __forceinline__ float operator()(float z) const {
-        if (by_lse) return z == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((z * inv_t - lse) * LOG2E);
-        return z == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((z - from) * c) * inv_s;
+struct Entries {        // a lane's entries as they come from memory
+    int32_t id[TEACHER_Q];
+    float x[TEACHER_Q], z[TEACHER_Q], w;
+    __device__ __forceinline__ void load(const Distill& a, int64_t i) {
+        w = a.weight ? a.weight[i] : 1.0f;
+#pragma unroll
+        for (int q = 0; q < TEACHER_Q; ++q) {
+            const int j = lane_id() + q * 64;
+            id[q] = j < a.k ? a.ids[i * a.k + j] : -1;
+            x[q] = j < a.k ? a.logits[i * a.k + j] : -INFINITY;
+        }
+    }
+    // the student's logits at those in [lo, hi)
+    template <typename T>
+    __device__ __forceinline__ void load_logits(const T* row, int32_t classes, int32_t lo, int32_t hi) {
+#pragma unroll
+        for (int q = 0; q < TEACHER_Q; ++q) {
+            if (id[q] < 0 || id[q] >= classes) id[q] = -1;
+            z[q] = id[q] >= lo && id[q] < hi ? to_f32(row[id[q]]) : 0.0f;
+        }
+    }
+    // softmax(logits / T) over the entries inside the classes
+    __device__ __forceinline__ void shares(const Distill& a, Teacher& to) const {
+        Wave wave(nullptr);
+        float m = -INFINITY, s = 0.0f, e[TEACHER_Q];
+#pragma unroll
+        for (int q = 0; q < TEACHER_Q; ++q) if (id[q] >= 0) m = fmaxf(m, x[q]);
+        const float from = above(wave.max(m));
+#pragma unroll
+        for (int q = 0; q < TEACHER_Q; ++q) {
+            e[q] = id[q] < 0 ? 0.0f : expf((x[q] - from) * a.inv_t);
+            s += e[q];
+        }
+        s = wave.sum(s);
+        const float log_s = logf(s);
+#pragma unroll
+        for (int q = 0; q < TEACHER_Q; ++q) {
+            const int j = lane_id() + q * 64;
+            if (j < a.k) {
+                to.id[j] = id[q];
+                to.p[j] = s == 0.0f ? 0.0f : e[q] / s;
+                to.log_p[j] = (x[q] - from) * a.inv_t - log_s;
+                to.z[j] = z[q];
+            }
+        }
+        if (lane_id() == 0) to.any = s != 0.0f;
     }
 };
 
+// Loss and lse of a row whose sums are known, by one wavefront.
+__device__ __forceinline__ void distill_loss(const Distill& a, int64_t i, const Sums& r, float w, const Teacher& te) {
+    const float log_s = logf(r.s), from = above(r.m);
+    if (a.loss) {
+        float term = 0.0f;
+        for (int j = lane_id(); j < a.k; j += 64)
+            if (te.p[j] != 0.0f) term += te.p[j] * (te.log_p[j] - (r.s == 0.0f ? -INFINITY : (te.z[j] - from) * a.inv_t - log_s));
+        term = Wave(nullptr).sum(term);
+        if (lane_id() == 0) a.loss[i] = w == 0.0f || !te.any ? 0.0f : w * a.temperature * a.temperature * term;
+    }
+    if (a.lse_out && lane_id() == 0) a.lse_out[i] = from * a.inv_t + log_s;
+}
+
+// A class's share in the student's row, times `by`: from the row's sums, or from its lse. (A row of -inf alone has no share anywhere: the factor is 0
+// then, or the lse counts as +inf.)
+struct ShareBySums {
+    float from, c, by;
+    __device__ __forceinline__ ShareBySums(const Sums& r, float c_, float by_) : from(above(r.m)), c(c_), by(r.s == 0.0f ? 0.0f : by_ / r.s) {}
+    __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z - from) * c) * by; }
+};
+struct ShareByLse {
+    float inv_t, lse, by;
+    __device__ __forceinline__ ShareByLse(float inv_t_, float lse_, float by_) : inv_t(inv_t_), lse(lse_ == -INFINITY ? INFINITY : lse_), by(by_) {}
+    __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z * inv_t - lse) * LOG2E) * by; }
+};
+
 // The gradient of values [first, first + len) of a row, held in `v`: w T q everywhere, then the classes that the teacher names once more with
-// their shares taken off (the barrier orders the two stores; an entry that stands twice stores the same value twice).
-template <typename T, int U, int TEAM, int THREADS>
-__device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_t first, int32_t len, const Piece<T, U, TEAM>& v, const Share& q, float w, bool any, const Teacher& te,
-                                             Team<TEAM, THREADS>& team) {
+// their shares taken off (the barrier orders the two stores; an entry that stands twice stores the same value twice). `after(u)` follows the last use of
+// run u.
+template <typename T, int U, int TEAM, int THREADS, typename Q, typename After>
+__device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_t first, int32_t len, Piece<T, U, TEAM>& v, const Q& q, float w, const Teacher& te,
+                                             Team<TEAM, THREADS>& team, After after) {
     constexpr int W = Piece<T, U, TEAM>::W;
     const int t = team.lane();
     T* const out = a.grad.row<T>(i) + first;
-    const float by = w * a.temperature;
-    const bool live = w != 0.0f && any;
+    constexpr int TW = TEAM * W;
+    const bool live = w != 0.0f && te.any;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int32_t c = v.at(t, u);
@@ -187,11 +203,12 @@ __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_
             float f[W];
             v.v[u].get(f);
 #pragma unroll
-            for (int x = 0; x < W; ++x) f[x] = live ? by * q(f[x]) : 0.0f;
+            for (int x = 0; x < W; ++x) f[x] = live ? q(f[x]) : 0.0f;
             Run<T, W> o;
             o.set(f);
-            o.store(out + c, len - c);
+            o.store(out + u * TW + t * W, len - c);
         }
+        after(u);
     }
     team.sync();
     if (live)
@@ -200,33 +217,83 @@ __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_
             if (te.id[j] >= 0 && at >= 0 && at < len) {
                 float share = 0.0f;
                 for (int o = 0; o < a.k; ++o) share += te.id[o] == te.id[j] ? te.p[o] : 0.0f;
-                out[at] = from_f32<T>(by * (q(te.z[j]) - share));
+                out[at] = from_f32<T>(q(te.z[j]) - w * a.temperature * share);
             }
         }
 }
 
-// A whole row in a team's registers: everything in one read.
+// Whole rows in a team's registers: everything in one read.
 template <typename T, int TEAM, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) distill_row_kernel(Distill a) {
     __shared__ float smem[2 * THREADS / 64];
     __shared__ Teacher teachers[THREADS / TEAM];
     Team<TEAM, THREADS> team(smem);
     Teacher& te = teachers[team.index()];
-    const int32_t n = rows_here(a.d_n, a.cap);
     const int64_t i = a.row0 + (int64_t)blockIdx.x * (THREADS / TEAM) + team.index();
-    if (i >= n) return;
+    if (i >= rows_here(a.d_n, a.cap)) return;
     const T* z = a.z.row<T>(i);
+    const bool first_wave = TEAM == 64 || threadIdx.x < 64;
+    Entries e;
+    if (first_wave) e.load(a, i);
     Piece<T, U, TEAM> v;
     v.load(z, a.classes, team.lane());
     const float w = a.weight ? a.weight[i] : 1.0f;
-    const bool any = teacher_shares(a.ids + i * a.k, a.logits + i * a.k, a.k, a.classes, a.inv_t, z, 0, a.classes, te, team);
+    if (first_wave) {
+        e.load_logits(z, a.classes, 0, a.classes);
+        e.shares(a, te);
+    }
     Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
     v.renew();
     v.template add<false>(above(r.m), a.c, r.s, r.h);
     v.renew();
     r.s = team.sum(r.s);
-    distill_loss(a, i, r, w, any, te, team);
-    if (a.grad.p) distill_grad(a, i, 0, a.classes, v, Share{above(r.m), a.c, 1.0f / r.s, a.inv_t, 0.0f, false}, w, any, te, team);
+    if constexpr (TEAM == 64) team.sync();      // (the entries; in larger teams a sum's barrier stood between)
+    if (first_wave) distill_loss(a, i, r, w, te);
+    if (a.grad.p) distill_grad(a, i, 0, a.classes, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [](int) {});
+}
+
+// The same for rows that fill the register file of a compute unit, one block to each: the block walks rows, and each run of the next row is requested when this
+// row's gradient has no more use for its registers, so that reading goes on beside the arithmetic and the stores.
+template <typename T, int U>
+__global__ void __launch_bounds__(1024) distill_rows_kernel(Distill a) {
+    __shared__ float smem[2 * 1024 / 64];
+    __shared__ Teacher teachers[2];
+    Team<1024, 1024> team(smem);
+    const int64_t n = min((int64_t)rows_here(a.d_n, a.cap), a.row0 + a.pieces);     // (pieces: the launch's rows)
+    const bool first_wave = threadIdx.x < 64;
+    int64_t i = a.row0 + blockIdx.x;
+    if (i >= n) return;
+    constexpr int W = Piece<T, U, 1024>::W;
+    Entries e;
+    Piece<T, U, 1024> v;
+    v.load(a.z.row<T>(i), a.classes, team.lane());
+    if (first_wave) {
+        e.load(a, i);
+        e.load_logits(a.z.row<T>(i), a.classes, 0, a.classes);
+    }
+    for (int turn = 0; i < n; turn ^= 1) {
+        Teacher& te = teachers[turn];
+        const int64_t next = i + gridDim.x;
+        const T* const next_row = a.z.row<T>(next < n ? next : i);
+        const int32_t next_len = next < n ? a.classes : 0;
+        const float w = a.weight ? a.weight[i] : 1.0f;
+        if (first_wave) e.shares(a, te);
+        v.renew();
+        Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
+        v.renew();
+        v.template add<false>(above(r.m), a.c, r.s, r.h);
+        v.renew();
+        r.s = team.sum(r.s);
+        if (first_wave) distill_loss(a, i, r, w, te);
+        distill_grad(a, i, 0, a.classes, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [&](int u) {
+            v.v[u].load(next_row + u * 1024 * W + (int)threadIdx.x * W, next_len - v.at(threadIdx.x, u), from_f32<T>(-INFINITY));
+        });
+        if (first_wave && next < n) {
+            e.load(a, next);
+            e.load_logits(next_row, a.classes, 0, a.classes);
+        }
+        i = next;
+    }
 }
 
 // Sums of one piece of a row.
@@ -257,15 +324,21 @@ __global__ void __launch_bounds__(THREADS) distill_grad_kernel(Distill a) {
     const int32_t p = (int32_t)(blockIdx.x % (uint32_t)a.pieces), first = p * a.piece, len = min(a.piece, a.classes - first);
     if (i >= rows_here(a.d_n, a.cap)) return;
     const T* z = a.z.row<T>(i);
+    Entries e;
+    if (threadIdx.x < 64) e.load(a, i);
     Piece<T, U, THREADS> v;
     v.load(z + first, len, team.lane());
     const float w = a.weight ? a.weight[i] : 1.0f;
-    const bool any = teacher_shares(a.ids + i * a.k, a.logits + i * a.k, a.k, a.classes, a.inv_t, z, first, first + len, te, team);
+    if (threadIdx.x < 64) {
+        e.load_logits(z, a.classes, first, first + len);
+        e.shares(a, te);
+    }
     if (a.lse_in) {
-        distill_grad(a, i, first, len, v, Share{0.0f, a.c, 0.0f, a.inv_t, a.lse_in[i], true}, w, any, te, team);
+        team.sync();
+        distill_grad(a, i, first, len, v, ShareByLse(a.inv_t, a.lse_in[i], w * a.temperature), w, te, team, [](int) {});
     } else {
-        const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);
-        distill_grad(a, i, first, len, v, Share{above(r.m), a.c, 1.0f / r.s, a.inv_t, 0.0f, false}, w, any, te, team);
+        const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);      // (its barriers stand behind the entries)
+        distill_grad(a, i, first, len, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [](int) {});
     }
 }
 
@@ -277,10 +350,14 @@ __global__ void __launch_bounds__(256) distill_loss_kernel(Distill a) {
     Teacher& te = teachers[team.index()];
     const int64_t i = a.row0 + (int64_t)blockIdx.x * 4 + team.index();
     if (i >= rows_here(a.d_n, a.cap)) return;
-    const float w = a.weight ? a.weight[i] : 1.0f;
-    const bool any = teacher_shares(a.ids + i * a.k, a.logits + i * a.k, a.k, a.classes, a.inv_t, a.z.row<T>(i), 0, a.classes, te, team);
+    const T* z = a.z.row<T>(i);
+    Entries e;
+    e.load(a, i);
+    e.load_logits(z, a.classes, 0, a.classes);
+    e.shares(a, te);
     const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);
-    distill_loss(a, i, r, w, any, te, team);
+    team.sync();
+    distill_loss(a, i, r, a.weight ? a.weight[i] : 1.0f, te);
 }
 
 // ------------------------------------------------------------------------------------------------------- log probabilities
@@ -634,6 +711,12 @@ static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
         a.row0 = row0;                                                                                                                            \
         hipLaunchKernelGGL((distill_row_kernel<T, TEAM, THREADS, U>), dim3((unsigned)ceil_div(rows, THREADS / TEAM)), dim3(THREADS), 0, st, a);   \
     })
+#define NO_ROWS(U)                                                                                                            \
+    in_slabs(a.cap, MOST_BLOCKS, [&](int64_t row0, int64_t rows) {                                                            \
+        a.row0 = row0;                                                                                                        \
+        a.pieces = (int32_t)rows;                                                                                             \
+        hipLaunchKernelGGL((distill_rows_kernel<T, U>), dim3((unsigned)(rows < 256 ? rows : 256)), dim3(1024), 0, st, a);     \
+    })
     const bool row = !a.lse_in && units <= 16384 && (units <= 2048 || (a.grad.p && a.cap >= FEW_ROWS));
     if (row) {
         if (units <= 64) NO_ROW(64, 256, 1);
@@ -643,11 +726,12 @@ static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
         else if (units <= 1024) NO_ROW(256, 256, 4);
         else if (units <= 2048) NO_ROW(256, 256, 8);
         else if (units <= 4096) NO_ROW(1024, 1024, 4);
-        else if (units <= 8192) NO_ROW(1024, 1024, 8);
-        else NO_ROW(1024, 1024, 16);
+        else if (units <= 8192) NO_ROWS(8);
+        else NO_ROWS(16);
         return launch_status(who);
     }
 #undef NO_ROW
+#undef NO_ROWS
     const Cut cut(a.cap, a.classes, W);
     a.piece = cut.piece;
     a.pieces = cut.pieces;
