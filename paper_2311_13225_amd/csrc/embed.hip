@@ -58,57 +58,134 @@ static void launch_embed(const RowsOf& table, int64_t n_rows, int32_t dim, const
 // ------------------------------------------------------------------------------------------------------- gradient
 //
 // G[v] = scale * sum over the positions i with ids[i] == v of g[i]. The positions are ordered by id (stable, so by position within an id); then the
-// ordered list is cut into chunks of EMBED_CHUNK positions whatever the ids are, and a lane group walks a chunk with the sum of the id at hand
+// ordered list is cut into chunks of 8 or 32 positions whatever the ids are, and a lane group walks a chunk with the sum of the id at hand
 // in registers: an id that is named a thousand times costs what a thousand rare ones do. Sums of ids that lie inside a chunk go
 // straight to the table; those that reach over a chunk's border go to the workspace and are added up, in chunk order, by a second launch. Rows that no
 // id names are found by a search in the ordered ids and cleared beside the sums. No atomics: the same ids give the same bits.
 
-constexpr int EMBED_CHUNK = 32;
-constexpr int32_t EMBED_RANK_MOST = 16384;
+constexpr int EMBED_TILE = 4096;                    // positions that a block orders in LDS
+constexpr int32_t EMBED_MERGE_MOST = 131072;        // positions that are ordered by tiles and ranks; more go through the radix sort
 
 struct EmbedPlan {      // the workspace, cut up
-    int64_t n, chunks;
-    bool by_rank;
-    size_t keys, pos, keys_tmp, pos_tmp, sort_ws, parts, total;
-    EmbedPlan(int32_t n_, int32_t dim) : n(n_), chunks(ceil_div(n_, EMBED_CHUNK)), by_rank(n_ <= EMBED_RANK_MOST) {
-        const size_t list = (size_t)ceil_div(chunks * EMBED_CHUNK * 4, 16) * 16;
+    int64_t n, tiles, chunks;
+    int32_t chunk;
+    bool merged, radix;
+    size_t keys, pos, keys_tmp, pos_tmp, rank, sort_ws, parts, total;
+    EmbedPlan(int32_t n_, int32_t dim) : n(n_), tiles(ceil_div(n_, EMBED_TILE)), chunk(n_ <= 16384 ? 8 : 32) {
+        chunks = ceil_div(n, chunk);
+        radix = n > EMBED_MERGE_MOST;
+        merged = !radix && tiles > 1;
+        const size_t list = (size_t)(tiles ? tiles : 1) * EMBED_TILE * 4;
         keys = 0;
         pos = keys + list;
         keys_tmp = pos + list;
-        pos_tmp = keys_tmp + (by_rank ? 0 : list);
-        sort_ws = pos_tmp + (by_rank ? 0 : list);
-        parts = sort_ws + (by_rank ? 0 : (size_t)ceil_div((int64_t)radix_ws_bytes(n), 16) * 16);
+        pos_tmp = keys_tmp + (merged || radix ? list : 0);
+        rank = pos_tmp + (merged || radix ? list : 0);
+        sort_ws = rank + (merged ? list : 0);
+        parts = sort_ws + (radix ? (size_t)ceil_div((int64_t)radix_ws_bytes(n), 16) * 16 : 0);
         total = parts + (size_t)chunks * 2 * (size_t)dim * 4 + 16;
     }
 };
 
-// The place of position i in the order by id, then by position, is the number of positions before it in that order. n^2 comparisons, but in one
-// launch and from registers: a lane per position, and the sixteen wavefronts of a block share the positions that it is compared with.
-__global__ void __launch_bounds__(1024) embed_rank_kernel(const int32_t* __restrict__ ids, const int32_t* d_n, int32_t cap, uint32_t* keys, uint32_t* pos) {
-    __shared__ uint32_t part[16][64];
-    const int32_t n = rows_here(d_n, cap), first = (int32_t)blockIdx.x * 64;
-    if (first >= n) return;
-    const int32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6)), i = first + lane;
-    const uint32_t* key = reinterpret_cast<const uint32_t*>(ids);       // ids outside the table are larger than all inside, as unsigned
-    const uint32_t mine = i < n ? key[i] : 0u;
-    const int32_t each = (int32_t)ceil_div(n, 16 * 16) * 16, lo = min(n, wave * each), hi = min(n, lo + each);
+// A tile's positions in order, in LDS: a bitonic network over (id, position in the tile), four elements a thread, so that distances of 1 and 2 stay in a
+// thread, 4 to 128 in a wavefront, and only the ten steps of 256 and more go through LDS. K: 32 bits where the ids leave 12 of them, else 64. Ids
+// outside the table, and positions that are not there, come last.
+template <typename K>
+__global__ void __launch_bounds__(1024) embed_tile_kernel(const int32_t* __restrict__ ids, const int32_t* d_n, int32_t cap, uint32_t n_rows, uint32_t* keys, uint32_t* pos,
+                                                          uint32_t* rank) {
+    __shared__ K held[EMBED_TILE];
+    const int32_t n = rows_here(d_n, cap), base = (int32_t)blockIdx.x * EMBED_TILE, t = threadIdx.x, here = min(EMBED_TILE, n - base);
+    if (here <= 0) return;
+    K x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int32_t i = 4 * t + e;
+        const uint32_t key = i < here ? min((uint32_t)ids[base + i], n_rows) : 0u;
+        x[e] = i < here ? ((K)key << 12 | (K)i) : ~(K)0;
+    }
+    const int32_t m = here <= 4 ? 4 : 1 << (32 - __builtin_clz((uint32_t)here - 1));       // elements behind it are all padding
+    auto order = [](K& lo, K& hi, bool up) {
+        const K a = lo < hi ? lo : hi, b = lo < hi ? hi : lo;
+        lo = up ? a : b;
+        hi = up ? b : a;
+    };
+    for (int k = 2; k <= m; k <<= 1) {
+        for (int j = k >> 1; j >= 256; j >>= 1) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 4; ++e) held[4 * t + e] = x[e];
+            __syncthreads();
+            const bool keep_small = ((4 * t & k) == 0) == ((4 * t & j) == 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const K o = held[(4 * t ^ j) + e];
+                x[e] = (o < x[e]) == keep_small ? o : x[e];
+            }
+        }
+        for (int j = min(k >> 1, 128); j >= 4; j >>= 1) {
+            const bool keep_small = ((4 * t & k) == 0) == ((4 * t & j) == 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                K o;
+                if constexpr (sizeof(K) == 4) o = (K)__shfl_xor((int)x[e], j >> 2, 64);
+                else o = (K)__shfl_xor((unsigned long long)x[e], j >> 2, 64);
+                x[e] = (o < x[e]) == keep_small ? o : x[e];
+            }
+        }
+        const bool up = (4 * t & k) == 0;
+        if (k >= 4) {
+            order(x[0], x[2], up);
+            order(x[1], x[3], up);
+            order(x[0], x[1], up);
+            order(x[2], x[3], up);
+        } else {                                    // pairs, in turn up and down
+            order(x[0], x[1], true);
+            order(x[2], x[3], false);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int32_t i = 4 * t + e;
+        const bool there = i < here;
+        keys[base + i] = there ? (uint32_t)(x[e] >> 12) : ~0u;
+        pos[base + i] = there ? (uint32_t)(x[e] & 4095) + (uint32_t)base : 0u;
+        if (rank) rank[base + i] = 0;
+    }
+}
+
+// An element's place among all tiles is the number of smaller ones in each, where equal ids count in the tiles left of its own. A block takes 1024 elements of a
+// tile and a share of the tiles to search; the shares add up in whole numbers, in any order.
+__global__ void __launch_bounds__(1024) embed_rank_kernel(const uint32_t* __restrict__ keys, const int32_t* d_n, int32_t cap, int32_t shares, uint32_t* rank) {
+    __shared__ __attribute__((aligned(16))) uint32_t held[EMBED_TILE];
+    const int32_t n = rows_here(d_n, cap), i = (int32_t)blockIdx.x * 1024 + (int32_t)threadIdx.x, own = (int32_t)blockIdx.x / (EMBED_TILE / 1024);
+    if (own * EMBED_TILE >= n) return;
+    const int32_t tiles = (n + EMBED_TILE - 1) / EMBED_TILE;
+    const uint32_t key = keys[i];
     uint32_t before = 0;
-    // equal ids count where they stand earlier: all of those left of this block's positions, none right of it, and among the block's own by lane
-    const int32_t a = min(max(lo, first), hi), b = min(max(lo, first + 64), hi);
-#pragma unroll 16
-    for (int32_t j = lo; j < a; ++j) before += key[j] <= mine;
-    for (int32_t j = a; j < b; ++j) before += key[j] < mine || (key[j] == mine && j < i);
-#pragma unroll 16
-    for (int32_t j = b; j < hi; ++j) before += key[j] < mine;
-    part[wave][lane] = before;
-    __syncthreads();
-    if (wave == 0 && i < n) {
+    for (int32_t o = blockIdx.y; o < tiles; o += shares) {
+        if (o == own) {
+            before += (uint32_t)(i - own * EMBED_TILE);
+            continue;
+        }
+        __syncthreads();
+        reinterpret_cast<uint4*>(held)[threadIdx.x] = reinterpret_cast<const uint4*>(keys + o * EMBED_TILE)[threadIdx.x];
+        __syncthreads();
+        // elements below `to`, or up to it in earlier tiles (key + 1 does not wrap: an id is at most n_rows; what is not there is not stored)
+        const uint32_t to = o < own ? key + 1 : key;
         uint32_t at = 0;
 #pragma unroll
-        for (int w = 0; w < 16; ++w) at += part[w][lane];
-        keys[at] = mine;
-        pos[at] = (uint32_t)i;
+        for (int step = EMBED_TILE / 2; step > 0; step >>= 1) at += held[at + step - 1] < to ? step : 0;
+        before += at + (held[at] < to);
     }
+    if (key != ~0u) atomicAdd(&rank[i], before);
+}
+
+__global__ void __launch_bounds__(256) embed_place_kernel(const uint32_t* __restrict__ keys_in, const uint32_t* __restrict__ pos_in, const uint32_t* __restrict__ rank,
+                                                          const int32_t* d_n, int32_t cap, uint32_t* keys, uint32_t* pos) {
+    const int32_t n = rows_here(d_n, cap), i = (int32_t)(blockIdx.x * 256 + threadIdx.x);
+    if (i / EMBED_TILE * EMBED_TILE >= n || keys_in[i] == ~0u) return;
+    keys[rank[i]] = keys_in[i];
+    pos[rank[i]] = pos_in[i];
 }
 
 // What the first pass of the radix sort reads: ids outside the table, and positions that are not there, come last.
@@ -134,11 +211,11 @@ struct EmbedSums {
     bool accumulate;
     RowsOf grad, table;
     int64_t n_rows;
-    int32_t dim;
+    int32_t dim, chunk; // positions a chunk
     float* parts;       // [chunks][2][dim]: the sum of an id that began in an earlier chunk, and of one that goes on in the next
 };
 
-template <typename T, int W>
+template <typename T, int W, bool ADD>
 __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t chunks, int32_t g_log2, int32_t col_tiles, uint32_t sum_blocks) {
     const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id();
     for (int64_t v0 = ((int64_t)blockIdx.x - sum_blocks) * 64 + (threadIdx.x >> 6) * 16; blockIdx.x >= sum_blocks;
@@ -147,7 +224,7 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
         const int64_t v = v0 + (lane & 15);
         int32_t lo = 0, hi = n;
         while (lo < hi) {
-            const int32_t mid = (lo + hi) >> 1;
+            const int32_t mid = lo + ((hi - lo) >> 1);
             if ((int64_t)a.keys[mid] < v) lo = mid + 1; else hi = mid;
         }
         uint32_t empty = (uint32_t)__ballot(v < a.n_rows && !(lo < n && (int64_t)a.keys[lo] == v)) & 0xffffu;
@@ -165,86 +242,80 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
     const int64_t item = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * groups + (lane >> g_log2);
     const int64_t chunk = item / col_tiles;
     const int32_t col = ((int32_t)(item % col_tiles) * 64 + u) * W, width = a.dim - col;
-    const int64_t e0 = chunk * EMBED_CHUNK;
+    const int64_t e0 = chunk * a.chunk;
     if (chunk >= chunks || e0 >= n || width <= 0) return;
-    const int32_t len = (int32_t)min((int64_t)EMBED_CHUNK, n - e0);
+    const int32_t len = (int32_t)min((int64_t)a.chunk, n - e0);
     const uint32_t before = chunk ? a.keys[e0 - 1] : ~0u, after = e0 + len < n ? a.keys[e0 + len] : ~0u;
     float* const parts = a.parts + chunk * 2 * a.dim + col;
+    const uint32_t n_rows = (uint32_t)a.n_rows;     // (fewer than 2^31)
     float acc[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) acc[w] = 0.0f;
-    auto flush = [&](uint32_t key, int32_t start, int32_t end) {
-        if (key >= (uint64_t)a.n_rows) return;
-        Run<float, W> out;
-        if (start == 0 && key == before) { out.set(acc); return out.store(parts, width); }
-        if (end == len && key == after) { out.set(acc); return out.store(parts + a.dim, width); }
-        float* to = a.table.row<float>(key) + col;
-        float f[W];
-        if (a.accumulate) {
-            out.load(to, width, 0.0f);
-            out.get(f);
-#pragma unroll
-            for (int w = 0; w < W; ++w) f[w] += a.scale * acc[w];
-        } else {
-#pragma unroll
-            for (int w = 0; w < W; ++w) f[w] = a.scale * acc[w];
-        }
-        out.set(f);
-        out.store(to, width);
-    };
-    uint32_t cur = a.keys[e0];
     int32_t start = 0;
-    constexpr int UNR = 8;              // rows requested before the first is added
+    constexpr int UNR = ADD ? 4 : 8;                // rows requested before the first is added
     for (int32_t e = 0; e < len; e += UNR) {
-        uint32_t key[UNR], p[UNR];
+        uint32_t key[UNR + 1], p[UNR];
         Run<T, W> r[UNR];
+        Run<float, W> old[ADD ? UNR : 1];
 #pragma unroll
         for (int k = 0; k < UNR; ++k) {
             key[k] = e + k < len ? a.keys[e0 + e + k] : ~0u;
             p[k] = e + k < len ? a.pos[e0 + e + k] : 0u;
         }
-#pragma unroll
-        for (int k = 0; k < UNR; ++k)
-            if (key[k] < (uint64_t)a.n_rows) r[k].load(a.grad.row<T>(p[k]) + col, width, from_f32<T>(0.0f));
+        key[UNR] = e + UNR < len ? a.keys[e0 + e + UNR] : ~0u;
 #pragma unroll
         for (int k = 0; k < UNR; ++k) {
-            if (e + k >= len) break;
-            if (key[k] != cur) {
-                flush(cur, start, e + k);
-                cur = key[k];
-                start = e + k;
+            if (key[k] >= n_rows) continue;
+            r[k].load(a.grad.row<T>(p[k]) + col, width, from_f32<T>(0.0f));
+            // the row that a run's sum is added to, requested with the run's last gradient
+            if (ADD && key[k + 1] != key[k]) old[ADD ? k : 0].load(a.table.row<float>(key[k]) + col, width, 0.0f);
+        }
 #pragma unroll
-                for (int w = 0; w < W; ++w) acc[w] = 0.0f;
-            }
-            if (cur < (uint64_t)a.n_rows) {
-                float f[W];
-                r[k].get(f);
+        for (int k = 0; k < UNR; ++k) {
+            if (key[k] >= n_rows) continue;
+            float f[W];
+            r[k].get(f);
 #pragma unroll
-                for (int w = 0; w < W; ++w) acc[w] += f[w];
+            for (int w = 0; w < W; ++w) acc[w] += f[w];
+            if (key[k + 1] == key[k]) continue;     // (an id at the chunk's end goes on in the next, or does not: its sum is stored either way)
+            Run<float, W> out;
+            const bool last = e + k + 1 == len;
+            if (start == 0 && key[k] == before) { out.set(acc); out.store(parts, width); }
+            else if (last && key[k] == after) { out.set(acc); out.store(parts + a.dim, width); }
+            else {
+                if constexpr (ADD) old[ADD ? k : 0].get(f);
+#pragma unroll
+                for (int w = 0; w < W; ++w) f[w] = ADD ? f[w] + a.scale * acc[w] : a.scale * acc[w];
+                out.set(f);
+                out.store(a.table.row<float>(key[k]) + col, width);
             }
+            start = e + k + 1;
+#pragma unroll
+            for (int w = 0; w < W; ++w) acc[w] = 0.0f;
         }
     }
-    flush(cur, start, len);
 }
 
-// Adds up the sums that reach over borders: the chunk where such an id begins owns it. Four wavefronts share the later chunks' parts.
-__global__ void __launch_bounds__(256) embed_join_kernel(EmbedSums a, int64_t chunks) {
-    __shared__ float share[4][64][4];
-    const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id(), wave = (int32_t)(threadIdx.x >> 6), col = ((int32_t)blockIdx.y * 64 + lane) * 4, width = a.dim - col;
-    const int64_t here = min(chunks, ceil_div(n, EMBED_CHUNK));
+// Adds up the sums that reach over borders: the chunk where such an id begins owns it. A block's eight wavefronts share the later chunks' parts, and look for their
+// number 64 chunks at a time.
+__global__ void __launch_bounds__(512) embed_join_kernel(EmbedSums a, int64_t chunks) {
+    __shared__ float share[8][64][4];
+    const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id(), wave = (int32_t)(threadIdx.x >> 6), ch = a.chunk;
+    const int32_t col = ((int32_t)blockIdx.y * 64 + lane) * 4, width = a.dim - col;
+    const int64_t here = min(chunks, ceil_div(n, ch));
     for (int64_t c = blockIdx.x; c + 1 < here; c += gridDim.x) {
-        const uint32_t key = a.keys[(c + 1) * EMBED_CHUNK - 1];
-        if (key >= (uint64_t)a.n_rows || a.keys[(c + 1) * EMBED_CHUNK] != key) continue;
-        if (c > 0 && a.keys[c * EMBED_CHUNK] == key && a.keys[c * EMBED_CHUNK - 1] == key) continue;
-        int64_t lo = c + 2, hi = here;          // the first chunk that does not begin with this id
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (a.keys[mid * EMBED_CHUNK] == key) lo = mid + 1; else hi = mid;
+        const uint32_t first = a.keys[c * ch], key = a.keys[(c + 1) * ch - 1], next = a.keys[(c + 1) * ch], prior = c > 0 ? a.keys[c * ch - 1] : ~0u;
+        if ((int64_t)key >= a.n_rows || next != key || (first == key && prior == key)) continue;
+        int64_t end = c + 2;                    // the first chunk that does not begin with this id
+        for (;;) {
+            const uint64_t same = __ballot(end + lane < here && a.keys[min(end + lane, here - 1) * ch] == key);
+            end += same == ~0ull ? 64 : __builtin_ctzll(~same);
+            if (same != ~0ull) break;
         }
-        const int64_t parts = lo - c, each = ceil_div(parts, 4), p0 = min(parts, wave * each), p1 = min(parts, p0 + each);
+        const int64_t parts = end - c, each = ceil_div(parts, 8), p0 = min(parts, wave * each), p1 = min(parts, p0 + each);
         float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (width > 0) {
-#pragma unroll 4
+#pragma unroll 8
             for (int64_t p = p0; p < p1; ++p) {
                 Run<float, 4> r;
                 r.load(a.parts + ((c + p) * 2 + (p == 0)) * a.dim + col, width, 0.0f);
@@ -254,6 +325,7 @@ __global__ void __launch_bounds__(256) embed_join_kernel(EmbedSums a, int64_t ch
                 for (int w = 0; w < 4; ++w) acc[w] += f[w];
             }
         }
+        __syncthreads();
 #pragma unroll
         for (int w = 0; w < 4; ++w) share[wave][lane][w] = acc[w];
         __syncthreads();
@@ -263,11 +335,15 @@ __global__ void __launch_bounds__(256) embed_join_kernel(EmbedSums a, int64_t ch
             float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             if (a.accumulate) { out.load(to, width, 0.0f); out.get(f); }
 #pragma unroll
-            for (int w = 0; w < 4; ++w) f[w] += a.scale * ((share[0][lane][w] + share[1][lane][w]) + (share[2][lane][w] + share[3][lane][w]));
+            for (int w = 0; w < 4; ++w) {
+                float sum = share[0][lane][w];
+#pragma unroll
+                for (int o = 1; o < 8; ++o) sum += share[o][lane][w];
+                f[w] += a.scale * sum;
+            }
             out.set(f);
             out.store(to, width);
         }
-        __syncthreads();
     }
 }
 
@@ -279,8 +355,9 @@ static void launch_sums(const EmbedSums& a, int64_t chunks, hipStream_t st) {
     while ((1 << g_log2) < units && g_log2 < 6) ++g_log2;
     const int64_t sum_blocks = ceil_div(ceil_div(chunks * col_tiles, 64 >> g_log2), 4), zero_rows = ceil_div(a.n_rows, 64),
                   zero_blocks = a.accumulate ? 0 : zero_rows < (1 << 20) ? zero_rows : 1 << 20;
-    if (sum_blocks + zero_blocks)
-        hipLaunchKernelGGL((embed_sums_kernel<T, W>), dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks);
+    const dim3 grid((unsigned)(sum_blocks + zero_blocks));
+    if (a.accumulate) { if (sum_blocks) hipLaunchKernelGGL((embed_sums_kernel<T, W, true>), grid, dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks); }
+    else hipLaunchKernelGGL((embed_sums_kernel<T, W, false>), grid, dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks);
 }
 
 }  // namespace no
@@ -330,8 +407,17 @@ extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t gra
     char* ws = (char*)d_ws;
     uint32_t *keys = (uint32_t*)(ws + plan.keys), *pos = (uint32_t*)(ws + plan.pos);
     if (n_ids_cap > 0) {
-        if (plan.by_rank) {
-            hipLaunchKernelGGL(embed_rank_kernel, dim3((unsigned)ceil_div(n_ids_cap, 64)), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, keys, pos);
+        if (!plan.radix) {
+            uint32_t *k = plan.merged ? (uint32_t*)(ws + plan.keys_tmp) : keys, *v = plan.merged ? (uint32_t*)(ws + plan.pos_tmp) : pos,
+                     *rank = plan.merged ? (uint32_t*)(ws + plan.rank) : nullptr;
+            const unsigned tiles = (unsigned)plan.tiles;
+            if (n_rows < (1 << 20)) hipLaunchKernelGGL(embed_tile_kernel<uint32_t>, dim3(tiles), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows, k, v, rank);
+            else hipLaunchKernelGGL(embed_tile_kernel<uint64_t>, dim3(tiles), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows, k, v, rank);
+            if (plan.merged) {
+                const unsigned shares = tiles >= 64 ? 2 : tiles >= 32 ? 4 : tiles < 8 ? tiles : 8;
+                hipLaunchKernelGGL(embed_rank_kernel, dim3(tiles * (EMBED_TILE / 1024), shares), dim3(1024), 0, st, k, d_n_ids, n_ids_cap, (int32_t)shares, rank);
+                hipLaunchKernelGGL(embed_place_kernel, dim3(tiles * (EMBED_TILE / 256)), dim3(256), 0, st, k, v, rank, d_n_ids, n_ids_cap, keys, pos);
+            }
         } else {
             const int bits = ilog2_ceil((uint64_t)n_rows + 1), passes = radix_passes(bits), digit = radix_digit_bits(bits);
             const RadixPlan radix(n_ids_cap);
@@ -345,10 +431,10 @@ extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t gra
         }
     }
     const EmbedSums a{keys, pos, d_n_ids, n_ids_cap, scale, accumulate != 0, rows_of(d_grad_out, grad_stride_bytes), rows_of(d_grad_table, table_stride_bytes), n_rows, dim,
-                      (float*)(ws + plan.parts)};
+                      plan.chunk, (float*)(ws + plan.parts)};
     if (dt == NO_F32) launch_sums<float>(a, plan.chunks, st);
     else launch_sums<bf16_t>(a, plan.chunks, st);
     if (plan.chunks > 1)
-        hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(plan.chunks - 1 < 1024 ? plan.chunks - 1 : 1024), (unsigned)ceil_div(dim, 256)), dim3(256), 0, st, a, plan.chunks);
+        hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(plan.chunks - 1 < 1024 ? plan.chunks - 1 : 1024), (unsigned)ceil_div(dim, 256)), dim3(512), 0, st, a, plan.chunks);
     return launch_status(who);
 }

@@ -2,37 +2,32 @@
 //
 // A team of lanes (a wavefront or a block) holds a row, or a piece of one, in registers, U runs of 16 bytes a lane, and takes the maximum, the sum of
 // exponentials and whatever follows from there. Rows that are longer than a team's registers, and rows that are too few to fill the chip, are cut into pieces whose sums a
-// second launch joins. Exponentials are 2^((z - m) c), c = log2(e) / T, with the difference taken first: it is exact next to the maximum m, where the
-// exponentials are large, so that its rounding costs nothing there.
+// second launch joins. Exponentials are 2^x with x = (z - m) c, c = log2(e) / T, m the row's maximum, the difference taken first: it is exact next to the maximum,
+// where the exponentials are large, so that its rounding costs nothing there, and it stays in range for every logit. (fma(z, c, -mc) saves one instruction of
+// twelve, but is off by the rounding of mc = m c, which is no smaller than the result where |m c| passes 2^24: logits of 1e8, or a small T.)
 #include "rows.hpp"
 
 namespace no {
 
-constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
-// Sums of a row or a piece: largest logit (-inf: there is none above), sum of 2^((z - m) c), sum of that times (z - m).
+// Sums of a row or a piece: largest logit (-inf: there is none above), sum of 2^x, sum of x 2^x.
 struct Sums { float m, s, h; };
 
 __device__ __forceinline__ float above(float m) { return m == -INFINITY ? 0.0f : m; }      // what differences are taken from
 
+// x of a logit; the maximum is a row's, a piece's, or one that replaces it.
+struct Exponent {
+    float from, c;
+    __device__ __forceinline__ Exponent(float m, float c_) : from(above(m)), c(c_) {}
+    __device__ __forceinline__ float operator()(float z) const { return (z - from) * c; }
+};
+
 template <typename T, int U, int TEAM>
-struct Piece {      // a lane's runs of z[0, len): run u covers values [(lane + u TEAM) W, + W)
+struct Piece : RowRegs<T, 16 / (int)sizeof(T), U, TEAM> {      // logits of a row or a piece of one, in a lane's registers; -inf behind its end
     static constexpr int W = 16 / (int)sizeof(T);
-    Run<T, W> v[U];
-    __device__ __forceinline__ static int32_t at(int t, int u) { return (t + u * TEAM) * W; }
-    __device__ __forceinline__ void load(const T* z, int32_t len, int t) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t c = at(t, u);
-            v[u].load(z + u * TEAM * W + t * W, len - c, from_f32<T>(-INFINITY));      // (not followed where nothing is there)
-        }
-    }
-    // Between two passes over the values: without it the compiler keeps what the first one converted to fp32 (twice the registers, spilled in
-    // the largest kernels) instead of converting again, one instruction a value.
-    __device__ __forceinline__ void renew() {
-#pragma unroll
-        for (int u = 0; u < U; ++u) asm volatile("" : "+v"(v[u].v[0]));
-    }
+    using RowRegs<T, W, U, TEAM>::v;
+    __device__ __forceinline__ void load(const T* z, int32_t len, int t) { RowRegs<T, W, U, TEAM>::load(z, len, t, from_f32<T>(-INFINITY)); }
     __device__ __forceinline__ float lane_max() const {
         float m = -INFINITY;
 #pragma unroll
@@ -46,17 +41,18 @@ struct Piece {      // a lane's runs of z[0, len): run u covers values [(lane + 
     }
     // adds the lane's terms of s, and of h if ENTROPY; 0 (-inf) counts as 0
     template <bool ENTROPY>
-    __device__ __forceinline__ void add(float from, float c, float& s, float& h) const {
+    __device__ __forceinline__ void add(const Exponent& x, float& s, float& h) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float f[W];
             v[u].get(f);
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                const float d = f[w] - from, e = __builtin_amdgcn_exp2f(d * c);
+                const float d = x(f[w]), e = __builtin_amdgcn_exp2f(d);
                 s += e;
                 if constexpr (ENTROPY) h += e * fmaxf(d, -3.0e38f);
             }
+            if constexpr (ENTROPY) asm volatile("" : "+v"(h));      // (put off until h is asked for, its sum would keep every exponential in a register)
         }
     }
 };
@@ -68,12 +64,13 @@ __device__ __forceinline__ Sums join_sums(const Sums* parts, int32_t pieces, flo
     const int t = team.lane();
     for (int32_t p = t; p < pieces; p += TEAM) m = fmaxf(m, parts[p].m);
     m = team.max(m);
+    const Exponent x(m, c);
     float s = 0.0f, h = 0.0f;
     for (int32_t p = t; p < pieces; p += TEAM) {
         const Sums q = parts[p];
-        const float d = above(q.m) - above(m), e = q.s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(d * c);
+        const float d = x(above(q.m)), e = q.s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(d);
         s += e * q.s;
-        h += e * (q.h + d * q.s);
+        h += e * (q.h + fmaxf(d, -3.0e38f) * q.s);
     }
     return Sums{m, team.sum(s), team.sum(h)};
 }
@@ -161,23 +158,25 @@ struct Entries {        // a lane's entries as they come from memory
 
 // Loss and lse of a row whose sums are known, by one wavefront.
 __device__ __forceinline__ void distill_loss(const Distill& a, int64_t i, const Sums& r, float w, const Teacher& te) {
-    const float log_s = logf(r.s), from = above(r.m);
+    const Exponent x(r.m, a.c);
+    const float log_s = log2f(r.s);
     if (a.loss) {
         float term = 0.0f;
         for (int j = lane_id(); j < a.k; j += 64)
-            if (te.p[j] != 0.0f) term += te.p[j] * (te.log_p[j] - (r.s == 0.0f ? -INFINITY : (te.z[j] - from) * a.inv_t - log_s));
+            if (te.p[j] != 0.0f) term += te.p[j] * (te.log_p[j] - (r.s == 0.0f ? -INFINITY : (x(te.z[j]) - log_s) * LN2));
         term = Wave(nullptr).sum(term);
         if (lane_id() == 0) a.loss[i] = w == 0.0f || !te.any ? 0.0f : w * a.temperature * a.temperature * term;
     }
-    if (a.lse_out && lane_id() == 0) a.lse_out[i] = from * a.inv_t + log_s;
+    if (a.lse_out && lane_id() == 0) a.lse_out[i] = x.from * a.inv_t + log_s * LN2;
 }
 
 // A class's share in the student's row, times `by`: from the row's sums, or from its lse. (A row of -inf alone has no share anywhere: the factor is 0
 // then, or the lse counts as +inf.)
 struct ShareBySums {
-    float from, c, by;
-    __device__ __forceinline__ ShareBySums(const Sums& r, float c_, float by_) : from(above(r.m)), c(c_), by(r.s == 0.0f ? 0.0f : by_ / r.s) {}
-    __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z - from) * c) * by; }
+    Exponent x;
+    float by;
+    __device__ __forceinline__ ShareBySums(const Sums& r, float c, float by_) : x(r.m, c), by(r.s == 0.0f ? 0.0f : by_ / r.s) {}
+    __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f(x(z)) * by; }
 };
 struct ShareByLse {
     float inv_t, lse, by;
@@ -194,22 +193,22 @@ __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_
     constexpr int W = Piece<T, U, TEAM>::W;
     const int t = team.lane();
     T* const out = a.grad.row<T>(i) + first;
-    constexpr int TW = TEAM * W;
+    RowStore<T, W> store(out, len);
     const bool live = w != 0.0f && te.any;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int32_t c = v.at(t, u);
-        if (c < len) {
+        Run<T, W> o;
+        if (live) {
             float f[W];
             v.v[u].get(f);
 #pragma unroll
-            for (int x = 0; x < W; ++x) f[x] = live ? q(f[x]) : 0.0f;
-            Run<T, W> o;
+            for (int x = 0; x < W; ++x) f[x] = q(f[x]);
             o.set(f);
-            o.store(out + u * TW + t * W, len - c);
-        }
+        } else o.v[0] = 0;
+        store.put(v.at(t, u), o);
         after(u);
     }
+    store.finish();
     team.sync();
     if (live)
         for (int j = t; j < a.k; j += TEAM) {
@@ -244,7 +243,7 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(Distill a) {
     }
     Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
     v.renew();
-    v.template add<false>(above(r.m), a.c, r.s, r.h);
+    v.template add<false>(Exponent(r.m, a.c), r.s, r.h);
     v.renew();
     r.s = team.sum(r.s);
     if constexpr (TEAM == 64) team.sync();      // (the entries; in larger teams a sum's barrier stood between)
@@ -263,7 +262,6 @@ __global__ void __launch_bounds__(1024) distill_rows_kernel(Distill a) {
     const bool first_wave = threadIdx.x < 64;
     int64_t i = a.row0 + blockIdx.x;
     if (i >= n) return;
-    constexpr int W = Piece<T, U, 1024>::W;
     Entries e;
     Piece<T, U, 1024> v;
     v.load(a.z.row<T>(i), a.classes, team.lane());
@@ -281,13 +279,14 @@ __global__ void __launch_bounds__(1024) distill_rows_kernel(Distill a) {
         v.renew();
         Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
         v.renew();
-        v.template add<false>(above(r.m), a.c, r.s, r.h);
+        v.template add<false>(Exponent(r.m, a.c), r.s, r.h);
         v.renew();
         r.s = team.sum(r.s);
         if (first_wave) distill_loss(a, i, r, w, te);
         distill_grad(a, i, 0, a.classes, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [&](int u) {
-            v.v[u].load(next_row + u * 1024 * W + (int)threadIdx.x * W, next_len - v.at(threadIdx.x, u), from_f32<T>(-INFINITY));
+            v.load_run(next_row, next_len, threadIdx.x, u, from_f32<T>(-INFINITY));
         });
+        v.load_end(next_row, next_len, threadIdx.x, from_f32<T>(-INFINITY));
         if (first_wave && next < n) {
             e.load(a, next);
             e.load_logits(next_row, a.classes, 0, a.classes);
@@ -308,7 +307,7 @@ __global__ void __launch_bounds__(THREADS) distill_sums_kernel(Distill a) {
     v.load(a.z.row<T>(i) + (int64_t)p * a.piece, min(a.piece, a.classes - p * a.piece), team.lane());
     Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
     v.renew();
-    v.template add<false>(above(r.m), a.c, r.s, r.h);
+    v.template add<false>(Exponent(r.m, a.c), r.s, r.h);
     r.s = team.sum(r.s);
     if (threadIdx.x == 0) a.parts[i * a.pieces + p] = r;
 }
@@ -386,6 +385,54 @@ template <typename T, int U, int TEAM, int THREADS>
 __device__ __forceinline__ void top_candidates(Piece<T, U, TEAM>& v, float lane_max, int32_t first, int32_t k, TopSpace<TEAM>& to, Team<TEAM, THREADS>& team) {
     constexpr int W = Piece<T, U, TEAM>::W, Q = TEAM > 64 ? TEAM / 64 : 1;
     const int t = team.lane();
+    const int32_t base = first + t * W;     // class of a lane's first value; those of run u follow at u TEAM W (classes written out would be kept in registers)
+    // The values that `in` takes go to the list. Which runs hold any is found first; then a loop takes those runs, one or two in the lanes that
+    // have any (written out over all of a lane's runs it takes three times the registers).
+    auto collect = [&](auto in) {
+        uint32_t runs = 0;
+        v.renew();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[W];
+            v.v[u].get(f);
+            bool any = false;
+#pragma unroll
+            for (int w = 0; w < W; ++w) any |= in(f[w], u * TEAM * W + w);
+            runs |= any ? 1u << u : 0u;
+        }
+#pragma unroll 1
+        while (runs) {
+            const int at_u = __builtin_ctz(runs);
+            runs &= runs - 1;
+            uint32_t word[4];
+            __builtin_memcpy(word, &v.v[0], 16);
+#pragma unroll
+            for (int u = 1; u < U; ++u) {       // (selected word by word: taken as a whole, the runs would go through memory)
+                uint32_t other[4];
+                __builtin_memcpy(other, &v.v[u], 16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    asm volatile("" : "+v"(other[j]));
+                    word[j] = u == at_u ? other[j] : word[j];
+                }
+            }
+            Run<T, W> r;
+            __builtin_memcpy(&r, word, 16);
+            float f[W];
+            r.get(f);
+            const int32_t k0 = at_u * TEAM * W;
+            int32_t mine = 0;
+#pragma unroll
+            for (int w = 0; w < W; ++w) mine += in(f[w], k0 + w);
+            int32_t at = atomicAdd(&to.count, mine);
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                if (in(f[w], k0 + w)) {
+                    if (at < TopSpace<TEAM>::CAP) to.key[at] = order_key(f[w], base + k0 + w);
+                    ++at;
+                }
+        }
+    };
     // the k-th largest lane maximum, its upper 16 bits (so a little less than it): one wavefront looks for them bit by bit
     float bound = 0.0f;
     if constexpr (TEAM > 64) {
@@ -414,19 +461,7 @@ __device__ __forceinline__ void top_candidates(Piece<T, U, TEAM>& v, float lane_
     }
     team.sync();
     if constexpr (TEAM > 64) bound = to.from;
-    if (lane_max >= bound) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[W];
-            v.v[u].get(f);
-#pragma unroll
-            for (int w = 0; w < W; ++w)
-                if (f[w] >= bound) {
-                    const int32_t at = atomicAdd(&to.count, 1);
-                    if (at < TopSpace<TEAM>::CAP) to.key[at] = order_key(f[w], first + v.at(t, u) + w);
-                }
-        }
-    }
+    if (lane_max >= bound) collect([&](float f, int32_t) { return f >= bound; });
     team.sync();
     if (to.count <= TopSpace<TEAM>::CAP) return;
     // how many values are at least x, or are larger than x or equal to it with a class below c
@@ -438,7 +473,7 @@ __device__ __forceinline__ void top_candidates(Piece<T, U, TEAM>& v, float lane_
             float f[W];
             v.v[u].get(f);
 #pragma unroll
-            for (int w = 0; w < W; ++w) here += ties ? f[w] > x || (f[w] == x && first + v.at(t, u) + w < c) : f[w] >= x;
+            for (int w = 0; w < W; ++w) here += ties ? f[w] > x || (f[w] == x && u * TEAM * W + w < c - base) : f[w] >= x;
         }
         return (int)team.sum((float)here);          // (exact: a piece has fewer than 2^24 values)
     };
@@ -462,20 +497,7 @@ __device__ __forceinline__ void top_candidates(Piece<T, U, TEAM>& v, float lane_
     team.sync();
     if (t == 0) to.count = 0;
     team.sync();
-    v.renew();
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        float f[W];
-        v.v[u].get(f);
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const int32_t c = first + v.at(t, u) + w;
-            if (f[w] > x || (f[w] == x && c < below)) {
-                const int32_t at = atomicAdd(&to.count, 1);
-                if (at < TopSpace<TEAM>::CAP) to.key[at] = order_key(f[w], c);
-            }
-        }
-    }
+    collect([&](float f, int32_t k) { return f > x || (f == x && k < below - base); });
     team.sync();
 }
 
@@ -495,18 +517,18 @@ struct Logprobs {
     int32_t pieces, piece;
 };
 
-// log p of a logit, from the row's sums
+// log p of a logit, from the row's sums and the logarithm (to base 2) of their s
 __device__ __forceinline__ float log_share(const Logprobs& a, const Sums& r, float log_s, float z) {
     if (r.s != r.s) return NAN;
-    return z == -INFINITY ? -INFINITY : (z - above(r.m)) * a.inv_t - log_s;
+    return z == -INFINITY ? -INFINITY : (Exponent(r.m, a.c)(z) - log_s) * LN2;
 }
 
 template <typename T>
 __device__ __forceinline__ void store_row(const Logprobs& a, int64_t i, const Sums& r, float log_s) {
     const int32_t tok = a.tokens[i];
     a.logprob[i] = tok >= 0 && tok < a.classes ? log_share(a, r, log_s, to_f32(a.z.row<T>(i)[tok])) : 0.0f;
-    a.entropy[i] = r.s == 0.0f ? 0.0f : log_s - r.h * a.inv_t / r.s;
-    a.lse[i] = above(r.m) * a.inv_t + log_s;
+    a.entropy[i] = r.s == 0.0f ? 0.0f : (log_s - r.h / r.s) * LN2;
+    a.lse[i] = above(r.m) * a.inv_t + log_s * LN2;
 }
 
 __device__ __forceinline__ void store_top(const Logprobs& a, int64_t i, int32_t at, uint64_t key, const Sums& r, float log_s) {
@@ -516,7 +538,7 @@ __device__ __forceinline__ void store_top(const Logprobs& a, int64_t i, int32_t 
 }
 
 template <typename T, int TEAM, int THREADS, int U, bool SPLIT>
-__global__ void __launch_bounds__(THREADS) logprobs_kernel(Logprobs a) {
+__global__ void __launch_bounds__(THREADS, U == 8 ? 5 : U == 4 ? 7 : 8) logprobs_kernel(Logprobs a) {
     __shared__ float smem[2 * THREADS / 64];
     __shared__ TopSpace<TEAM> tops[THREADS / TEAM];
     Team<TEAM, THREADS> team(smem);
@@ -534,11 +556,11 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(Logprobs a) {
     const float mine = v.lane_max();
     Sums r{team.max(mine), 0.0f, 0.0f};
     v.renew();
-    v.template add<true>(above(r.m), a.c, r.s, r.h);
+    v.template add<true>(Exponent(r.m, a.c), r.s, r.h);
     v.renew();
     r.s = team.sum(r.s);
     r.h = team.sum(r.h);
-    const float log_s = logf(r.s);
+    const float log_s = log2f(r.s);
     if (t == 0) {
         if constexpr (SPLIT) a.parts[i * a.pieces + p] = r;
         else store_row<T>(a, i, r, log_s);
@@ -587,7 +609,7 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
         if (rank == need - 1 && mine != 0) bound = mine;        // (keys are all different; fewer than `need` above 0: all of them)
     }
     const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);
-    const float log_s = logf(r.s);
+    const float log_s = log2f(r.s);
     if (t == 0) store_row<T>(a, i, r, log_s);
     if (a.k == 0) return;
     __syncthreads();
@@ -640,24 +662,23 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(RowsOf z, const int3
     v.load(z.row<T>(i) + first, len, threadIdx.x);
     const int32_t tok = tokens[i];
     const float l = lse[i], h = entropy[i], gl = g_logprob && tok >= 0 && tok < classes ? g_logprob[i] : 0.0f, gh = g_entropy ? g_entropy[i] : 0.0f;
-    T* const out = grad.row<T>(i) + first;
+    RowStore<T, W> store(grad.row<T>(i) + first, len);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int32_t c = v.at(threadIdx.x, u);
-        if (c < len) {
-            float f[W];
-            v.v[u].get(f);
+        float f[W];
+        v.v[u].get(f);
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const float log_p = f[w] * inv_t - l, p = f[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(log_p * LOG2E);
-                const float d = p == 0.0f ? 0.0f : -(p * (gl + gh * (log_p + h)));
-                f[w] = (first + c + w == tok ? gl + d : d) * inv_t;
-            }
-            Run<T, W> o;
-            o.set(f);
-            o.store(out + c, len - c);
+        for (int w = 0; w < W; ++w) {
+            const float log_p = f[w] * inv_t - l, p = f[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(log_p * LOG2E);
+            const float d = p == 0.0f ? 0.0f : -(p * (gl + gh * (log_p + h)));
+            f[w] = (first + c + w == tok ? gl + d : d) * inv_t;
         }
+        Run<T, W> o;
+        o.set(f);
+        store.put(c, o);
     }
+    store.finish();
 }
 
 static int32_t check_logits(const char* who, const void* z, no_dtype dt, int64_t stride, int32_t n, int32_t classes, float temperature) {

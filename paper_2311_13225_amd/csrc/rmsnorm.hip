@@ -15,64 +15,60 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf r
     __shared__ float smem[2 * THREADS / 64];
     Team<TEAM, THREADS> team(smem);
     const int32_t n = rows_here(d_n, cap), t = team.lane();
-    float wk[KEEP ? U : 1][W];
-    auto weights = [&](int u, float (&f)[W]) {
-        const int32_t c = (t + u * TEAM) * W;
-        if (weight) {
-            Run<float, W> r;
-            r.load(weight + min(c, dim), dim - c, 0.0f);
-            r.get(f);
-        } else {
-#pragma unroll
-            for (int w = 0; w < W; ++w) f[w] = 1.0f;
-        }
-    };
-    if constexpr (KEEP)
-#pragma unroll
-        for (int u = 0; u < U; ++u) weights(u, wk[u]);
+    const T zero = from_f32<T>(0.0f);
+    RowRegs<float, W, KEEP ? U : 1, TEAM> wk;
+    if constexpr (KEEP) if (weight) wk.load(weight, dim, t, 0.0f);
     for (int64_t i = (int64_t)blockIdx.x * PER_BLOCK + team.index(); i < n; i += (int64_t)gridDim.x * PER_BLOCK) {
-        Run<T, W> s[U], r[U];
-        const T zero = from_f32<T>(0.0f);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t c = (t + u * TEAM) * W;
-            s[u].load(x.row<T>(i) + min(c, dim), dim - c, zero);
-            if (residual.p) r[u].load(residual.row<T>(i) + min(c, dim), dim - c, zero);
-        }
+        RowRegs<T, W, U, TEAM> s, r;
+        s.load(x.row<T>(i), dim, t, zero);
         float ss = 0.0f;
+        if (residual.p) {
+            r.load(residual.row<T>(i), dim, t, zero);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float f[W], g[W];
+                s.v[u].get(f);
+                r.v[u].get(g);
+#pragma unroll
+                for (int w = 0; w < W; ++w) f[w] += g[w];
+                s.v[u].set(f);
+            }
+        }
+        s.renew();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float f[W];
-            s[u].get(f);
-            if (residual.p) {
-                float g[W];
-                r[u].get(g);
-#pragma unroll
-                for (int w = 0; w < W; ++w) f[w] += g[w];
-                s[u].set(f);
-                s[u].get(f);
-            }
+            s.v[u].get(f);
 #pragma unroll
             for (int w = 0; w < W; ++w) ss += f[w] * f[w];
         }
-        if (sum.p)
+        if (sum.p) {
+            RowStore<T, W> store(sum.row<T>(i), dim);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int32_t c = (t + u * TEAM) * W;
-                if (c < dim) s[u].store(sum.row<T>(i) + c, dim - c);
-            }
+            for (int u = 0; u < U; ++u) store.put(s.at(t, u), s.v[u]);
+            store.finish();
+        }
         ss = team.sum(ss);
         const float rstd = 1.0f / sqrtf(ss / (float)dim + eps);
         auto values = [&](int u, float (&f)[W]) {
             float k[W];
-            s[u].get(f);
-            if constexpr (!KEEP) weights(u, k);
+            if (weight) {
+                if constexpr (KEEP) wk.v[KEEP ? u : 0].get(k);
+                else {
+                    Run<float, W> one;
+                    const int32_t c = s.at(t, u);
+                    one.load(weight + min(c, dim), dim - c, 0.0f);
+                    one.get(k);
+                }
+            }
+            s.v[u].get(f);
 #pragma unroll
-            for (int w = 0; w < W; ++w) f[w] = f[w] * rstd * (KEEP ? wk[KEEP ? u : 0][w] : k[w]);
+            for (int w = 0; w < W; ++w) f[w] = weight ? f[w] * rstd * k[w] : f[w] * rstd;
         };
         float scale = 1.0f, inv = 1.0f;
         if constexpr (TypeOf<Y>::code == NO_E4M3) {
             float most = 0.0f;
+            s.renew();
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float f[W];
@@ -84,20 +80,20 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf r
             scale = ss < INFINITY ? fmaxf(most, SMALLEST_MOST) / E4M3_MOST : NAN;
             inv = 1.0f / scale;
         }
+        s.renew();
+        RowStore<Y, W> store(y.row<Y>(i), dim);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int32_t c = (t + u * TEAM) * W;
-            if (c < dim) {
-                float f[W];
-                values(u, f);
-                if constexpr (TypeOf<Y>::code == NO_E4M3)
+            float f[W];
+            values(u, f);
+            if constexpr (TypeOf<Y>::code == NO_E4M3)
 #pragma unroll
-                    for (int w = 0; w < W; ++w) f[w] *= inv;
-                Run<Y, W> o;
-                o.set(f);
-                o.store(y.row<Y>(i) + c, dim - c);
-            }
+                for (int w = 0; w < W; ++w) f[w] *= inv;
+            Run<Y, W> o;
+            o.set(f);
+            store.put(s.at(t, u), o);
         }
+        store.finish();
         if (t == 0) {
             if (rstd_out) rstd_out[i] = rstd;
             if (TypeOf<Y>::code == NO_E4M3) row_scale[i] = scale;
@@ -121,60 +117,60 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(RowsOf s, const fl
     Team<TEAM, THREADS> team(smem);
     const int32_t n = rows_here(d_n, cap), t = team.lane();
     const T zero = from_f32<T>(0.0f);
-    float wk[U][W], dw[U][W];
+    RowRegs<float, W, U, TEAM> wk;
+    float dw[U][W];
+    if (weight) wk.load(weight, dim, t, 0.0f);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int32_t c = (t + u * TEAM) * W;
-        Run<float, W> r;
-        if (weight) { r.load(weight + min(c, dim), dim - c, 0.0f); r.get(wk[u]); }
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            if (!weight) wk[u][w] = 1.0f;
-            dw[u][w] = 0.0f;
+        for (int w = 0; w < W; ++w) dw[u][w] = 0.0f;
+        if (!weight) {
+            const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+#pragma unroll
+            for (int k = 0; k < Run<float, W>::N; ++k) __builtin_memcpy(&wk.v[u].v[k], one, 16);
         }
     }
     for (int64_t i = (int64_t)blockIdx.x * PER_BLOCK + team.index(); i < n; i += (int64_t)gridDim.x * PER_BLOCK) {
-        Run<T, W> rs[U], rg[U], ra[U];
+        RowRegs<T, W, U, TEAM> rs, rg, ra;
         const float r = rstd[i];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t c = (t + u * TEAM) * W, at = min(c, dim);
-            rs[u].load(s.row<T>(i) + at, dim - c, zero);
-            rg[u].load(grad_y.row<T>(i) + at, dim - c, zero);
-            if (grad_sum.p) ra[u].load(grad_sum.row<T>(i) + at, dim - c, zero);
-        }
+        rs.load(s.row<T>(i), dim, t, zero);
+        rg.load(grad_y.row<T>(i), dim, t, zero);
+        if (grad_sum.p) ra.load(grad_sum.row<T>(i), dim, t, zero);
         float dot = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float v[W], g[W];
-            rs[u].get(v);
-            rg[u].get(g);
+            float v[W], g[W], k[W];
+            rs.v[u].get(v);
+            rg.v[u].get(g);
+            wk.v[u].get(k);
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const float gu = g[w] * (v[w] * r);
                 dw[u][w] += gu;
-                dot += gu * wk[u][w];
+                dot += gu * k[w];
             }
         }
         const float mean = team.sum(dot) / (float)dim;
+        rs.renew();
+        rg.renew();
+        RowStore<T, W> store(grad_x.row<T>(i), dim);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int32_t c = (t + u * TEAM) * W;
-            if (c < dim) {
-                float v[W], g[W], a[W];
-                rs[u].get(v);
-                rg[u].get(g);
-                if (grad_sum.p) ra[u].get(a);
+            float v[W], g[W], k[W], a[W];
+            rs.v[u].get(v);
+            rg.v[u].get(g);
+            wk.v[u].get(k);
+            if (grad_sum.p) ra.v[u].get(a);
 #pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    const float dx = r * (g[w] * wk[u][w] - v[w] * r * mean);
-                    g[w] = grad_sum.p ? dx + a[w] : dx;
-                }
-                Run<T, W> o;
-                o.set(g);
-                o.store(grad_x.row<T>(i) + c, dim - c);
+            for (int w = 0; w < W; ++w) {
+                const float dx = r * (g[w] * k[w] - v[w] * r * mean);
+                g[w] = grad_sum.p ? dx + a[w] : dx;
             }
+            Run<T, W> o;
+            o.set(g);
+            store.put(rs.at(t, u), o);
         }
+        store.finish();
     }
     if (!grad_weight) return;
     if constexpr (PER_BLOCK > 1) {      // the block's teams in turn
@@ -294,6 +290,7 @@ extern "C" int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride
         else if (units <= 512) NO_NORM_AS(T, Y, 256, 256, 2);      \
         else if (units <= 1024) NO_NORM_AS(T, Y, 256, 256, 4);     \
         else if (units <= 2048) NO_NORM_AS(T, Y, 256, 256, 8);     \
+        else if (units <= 4096) NO_NORM_AS(T, Y, 1024, 1024, 4);   \
         else if (units <= 8192) NO_NORM_AS(T, Y, 1024, 1024, 8);   \
         else NO_NORM_AS(T, Y, 1024, 1024, sizeof(T) == 4 ? 16 : 8); \
     } while (0)
@@ -345,6 +342,7 @@ extern "C" int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride
         else if (units <= 256) NO_NORM_AS(T, 64, 256, 4);                                                                                            \
         else if (units <= 512) NO_NORM_AS(T, 256, 256, 2);                                                                                           \
         else if (units <= 1024) NO_NORM_AS(T, 256, 256, 4);                                                                                          \
+        else if (units <= 2048) NO_NORM_AS(T, 1024, 1024, 2);                                                                                        \
         else if (units <= 4096) NO_NORM_AS(T, 1024, 1024, 4);                                                                                        \
         else {                                                                                                                                       \
             n_parts = n_rows_cap < NORM_PARTS ? n_rows_cap : NORM_PARTS;                                                                             \

@@ -46,7 +46,7 @@ template <> struct Chunk<16> { typedef uint32_t val __attribute__((ext_vector_ty
 
 template <typename T, int W>
 struct Run {
-    static constexpr int BYTES = W * (int)sizeof(T), REQ = BYTES < 16 ? BYTES : 16, N = BYTES / REQ, PER = W / N;
+    static constexpr int BYTES = W * (int)sizeof(T), REQ = BYTES < 16 ? BYTES : 16, N = BYTES / REQ, WORDS = BYTES / 4, BITS = 8 * (int)sizeof(T);
     typedef typename Chunk<REQ>::val val;
     typedef typename Chunk<REQ>::raw raw;
     val v[N];
@@ -54,12 +54,22 @@ struct Run {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = reinterpret_cast<const raw*>(p)[i];
     }
+    // The end of a row: a value at a time, in a loop that shifts the run (written out, a branch a value, it costs the kernels more registers than
+    // the rest of them needs).
     __device__ __forceinline__ void load(const T* p, int here, T fill) {
         if (here >= W) return load(p);
-        T e[W];
+        uint32_t w[WORDS], f = bits(fill);
+        if constexpr (BITS == 8) f |= f << 8;
+        if constexpr (BITS <= 16) f |= f << 16;
 #pragma unroll
-        for (int i = 0; i < W; ++i) e[i] = i < here ? p[i] : fill;
-        __builtin_memcpy(v, e, BYTES);
+        for (int j = 0; j < WORDS; ++j) w[j] = f;
+#pragma unroll 1
+        for (int i = here - 1; i >= 0; --i) {
+#pragma unroll
+            for (int j = WORDS - 1; j > 0; --j) w[j] = BITS == 32 ? w[j - 1] : w[j] << (BITS & 31) | w[j - 1] >> (32 - BITS & 31);
+            w[0] = BITS == 32 ? bits(p[i]) : w[0] << (BITS & 31) | bits(p[i]);
+        }
+        __builtin_memcpy(v, w, BYTES);
     }
     __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
@@ -67,42 +77,112 @@ struct Run {
     }
     __device__ __forceinline__ void store(T* p, int here) const {
         if (here >= W) return store(p);
-        T e[W];
-        __builtin_memcpy(e, v, BYTES);
+        uint32_t w[WORDS];
+        __builtin_memcpy(w, v, BYTES);
+#pragma unroll 1
+        for (int i = 0; i < here; ++i) {
+            T e;
+            __builtin_memcpy(&e, w, sizeof(T));
+            p[i] = e;
 #pragma unroll
-        for (int i = 0; i < W; ++i) if (i < here) p[i] = e[i];
+            for (int j = 0; j < WORDS; ++j) {
+                const uint32_t up = j + 1 < WORDS ? w[j + 1 < WORDS ? j + 1 : 0] : 0u;
+                w[j] = BITS == 32 ? up : w[j] >> (BITS & 31) | up << (32 - BITS & 31);
+            }
+        }
+    }
+    __device__ __forceinline__ static uint32_t bits(T e) {
+        if constexpr (BITS == 32) return __builtin_bit_cast(uint32_t, e);
+        else if constexpr (BITS == 16) return __builtin_bit_cast(uint16_t, e);
+        else return __builtin_bit_cast(uint8_t, e);
     }
     __device__ __forceinline__ void get(float (&f)[W]) const {
-        if constexpr (sizeof(T) == 1) {
+        uint32_t w[WORDS];
+        __builtin_memcpy(w, v, BYTES);
+        if constexpr (BITS == 8) {
             typedef float f2 __attribute__((ext_vector_type(2)));
-            uint32_t w[BYTES / 4];
-            __builtin_memcpy(w, v, BYTES);
 #pragma unroll
             for (int i = 0; i < W / 4; ++i) {
                 const f2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w[i], true);
                 f[4 * i] = a.x; f[4 * i + 1] = a.y; f[4 * i + 2] = b.x; f[4 * i + 3] = b.y;
             }
-        } else {
-            T e[W];
-            __builtin_memcpy(e, v, BYTES);
+        } else if constexpr (BITS == 16) {
 #pragma unroll
-            for (int i = 0; i < W; ++i) f[i] = to_f32(e[i]);
+            for (int i = 0; i < W / 2; ++i) {
+                f[2 * i] = __uint_as_float(w[i] << 16);
+                f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) f[i] = __uint_as_float(w[i]);
         }
     }
     __device__ __forceinline__ void set(const float (&f)[W]) {
-        if constexpr (sizeof(T) == 1) {
-            uint32_t w[BYTES / 4];
+        uint32_t w[WORDS];
+        if constexpr (BITS == 8) {
 #pragma unroll
             for (int i = 0; i < W / 4; ++i)
                 w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2], f[4 * i + 3], __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i], f[4 * i + 1], 0, false), true);
-            __builtin_memcpy(v, w, BYTES);
-        } else {
-            T e[W];
+        } else if constexpr (BITS == 16) {
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-            for (int i = 0; i < W; ++i) e[i] = from_f32<T>(f[i]);
-            __builtin_memcpy(v, e, BYTES);
+            for (int i = 0; i < W / 2; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{f[2 * i], f[2 * i + 1]}), b2));
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[i] = __float_as_uint(f[i]);
         }
+        __builtin_memcpy(v, w, BYTES);
     }
+};
+
+// A row (or a piece of one) of `len` values in the registers of TEAM lanes: run u of lane t covers values [(t + u TEAM) W, + W).
+template <typename T, int W, int U, int TEAM>
+struct RowRegs {
+    Run<T, W> v[U];
+    __device__ __forceinline__ static int32_t at(int t, int u) { return (t + u * TEAM) * W; }
+    // run u, if all of it is there (else `fill`)
+    __device__ __forceinline__ void load_run(const T* p, int32_t len, int t, int u, T fill) {
+        if (at(t, u) + W <= len) v[u].load(p + u * TEAM * W + t * W);
+        else v[u].load(p, 0, fill);
+    }
+    // the run that the row ends in, by the lane that has it
+    __device__ __forceinline__ void load_end(const T* p, int32_t len, int t, T fill) {
+        if (len % W == 0) return;
+        const int32_t c = len / W * W;
+        if (len / W % TEAM != t) return;
+        Run<T, W> r;
+        r.load(p + c, len - c, fill);
+#pragma unroll
+        for (int u = 0; u < U; ++u) if (c == at(t, u)) v[u] = r;
+    }
+    __device__ __forceinline__ void load(const T* p, int32_t len, int t, T fill) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_run(p, len, t, u, fill);
+        load_end(p, len, t, fill);
+    }
+    // Between two passes over the values: without it the compiler keeps what the first one converted to fp32 (twice the registers of bf16 rows, spilled in
+    // the largest kernels) instead of converting again, one instruction a value.
+    __device__ __forceinline__ void renew() {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < Run<T, W>::N; ++i) asm volatile("" : "+v"(v[u].v[i]));
+    }
+};
+
+// Stores a row run by run; the run that the row ends in is kept until the others are stored.
+template <typename T, int W>
+struct RowStore {
+    T* p;
+    int32_t len, end = -1;
+    Run<T, W> last;
+    __device__ __forceinline__ RowStore(T* p_, int32_t len_) : p(p_), len(len_) {}
+    __device__ __forceinline__ void put(int32_t c, const Run<T, W>& r) {
+        if (c + W <= len) r.store(p + c);
+        else if (c < len) { last = r; end = c; }
+    }
+    __device__ __forceinline__ void finish() { if (end >= 0) last.store(p + end, len - end); }
 };
 
 // TEAM lanes that share a row: a part of a wavefront, a wavefront, or a block. Sums and maxima reach every lane. Across wavefronts they cost one
