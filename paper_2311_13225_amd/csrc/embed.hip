@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_
 template <typename T, typename O>
 static void launch_embed(const RowsOf& table, int64_t n_rows, int32_t dim, const float* row_scale, const int32_t* ids, const int32_t* d_n, int32_t cap, float scale,
                          const RowsOf& out, hipStream_t st) {
-    constexpr int W = sizeof(T) == 4 && sizeof(O) == 4 ? 4 : 8;
+    constexpr int W = sizeof(T) == 4 && sizeof(O) == 4 ? 4 : sizeof(T) == 1 ? 16 : 8;
     const int32_t units = (int32_t)ceil_div(dim, W);
     int g_log2 = 0;
     while ((1 << g_log2) < units && g_log2 < 6) ++g_log2;
@@ -63,7 +63,8 @@ static void launch_embed(const RowsOf& table, int64_t n_rows, int32_t dim, const
 // straight to the table; those that reach over a chunk's border go to the workspace and are added up, in chunk order, by a second launch. Rows that no
 // id names are found by a search in the ordered ids and cleared beside the sums. No atomics: the same ids give the same bits.
 
-constexpr int EMBED_TILE = 4096;                    // positions that a block orders in LDS
+constexpr int EMBED_TILE = 1024;                    // positions that a block orders in LDS
+constexpr int32_t EMBED_RANK_MOST = 8192;           // positions whose places are counted in one launch
 constexpr int32_t EMBED_MERGE_MOST = 131072;        // positions that are ordered by tiles and ranks; more go through the radix sort
 
 struct EmbedPlan {      // the workspace, cut up
@@ -74,7 +75,7 @@ struct EmbedPlan {      // the workspace, cut up
     EmbedPlan(int32_t n_, int32_t dim) : n(n_), tiles(ceil_div(n_, EMBED_TILE)), chunk(n_ <= 16384 ? 8 : 32) {
         chunks = ceil_div(n, chunk);
         radix = n > EMBED_MERGE_MOST;
-        merged = !radix && tiles > 1;
+        merged = !radix && n > EMBED_RANK_MOST;
         const size_t list = (size_t)(tiles ? tiles : 1) * EMBED_TILE * 4;
         keys = 0;
         pos = keys + list;
@@ -87,97 +88,90 @@ struct EmbedPlan {      // the workspace, cut up
     }
 };
 
-// A tile's positions in order, in LDS: a bitonic network over (id, position in the tile), four elements a thread, so that distances of 1 and 2 stay in a
-// thread, 4 to 128 in a wavefront, and only the ten steps of 256 and more go through LDS. K: 32 bits where the ids leave 12 of them, else 64. Ids
-// outside the table, and positions that are not there, come last.
-template <typename K>
-__global__ void __launch_bounds__(1024) embed_tile_kernel(const int32_t* __restrict__ ids, const int32_t* d_n, int32_t cap, uint32_t n_rows, uint32_t* keys, uint32_t* pos,
-                                                          uint32_t* rank) {
-    __shared__ K held[EMBED_TILE];
-    const int32_t n = rows_here(d_n, cap), base = (int32_t)blockIdx.x * EMBED_TILE, t = threadIdx.x, here = min(EMBED_TILE, n - base);
-    if (here <= 0) return;
-    K x[4];
+// The place of a position in the order by id, then by position, is the number of positions before it in that order. n^2 comparisons, but in one
+// launch and from registers: a lane per position, and the sixteen wavefronts of a block share the positions that it is compared with.
+__global__ void __launch_bounds__(1024) embed_count_kernel(const int32_t* __restrict__ ids, const int32_t* d_n, int32_t cap, uint32_t* keys, uint32_t* pos) {
+    __shared__ uint32_t part[16][64];
+    const int32_t n = rows_here(d_n, cap), first = (int32_t)blockIdx.x * 64;
+    if (first >= n) return;
+    const int32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6)), i = first + lane;
+    const uint32_t* key = reinterpret_cast<const uint32_t*>(ids);       // ids outside the table are larger than all inside, as unsigned
+    const uint32_t mine = i < n ? key[i] : 0u;
+    const int32_t each = (n + 255) / 256 * 16, lo = min(n, wave * each), hi = min(n, lo + each);
+    uint32_t before = 0;
+    // equal ids count where they stand earlier: all of those left of this block's positions, none right of it, and among the block's own by lane
+    const int32_t a = min(max(lo, first), hi), b = min(max(lo, first + 64), hi);
+#pragma unroll 16
+    for (int32_t j = lo; j < a; ++j) before += key[j] <= mine;
+    for (int32_t j = a; j < b; ++j) before += key[j] < mine || (key[j] == mine && j < i);
+#pragma unroll 16
+    for (int32_t j = b; j < hi; ++j) before += key[j] < mine;
+    part[wave][lane] = before;
+    __syncthreads();
+    if (wave == 0 && i < n) {
+        uint32_t at = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int32_t i = 4 * t + e;
-        const uint32_t key = i < here ? min((uint32_t)ids[base + i], n_rows) : 0u;
-        x[e] = i < here ? ((K)key << 12 | (K)i) : ~(K)0;
-    }
-    const int32_t m = here <= 4 ? 4 : 1 << (32 - __builtin_clz((uint32_t)here - 1));       // elements behind it are all padding
-    auto order = [](K& lo, K& hi, bool up) {
-        const K a = lo < hi ? lo : hi, b = lo < hi ? hi : lo;
-        lo = up ? a : b;
-        hi = up ? b : a;
-    };
-    for (int k = 2; k <= m; k <<= 1) {
-        for (int j = k >> 1; j >= 256; j >>= 1) {
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 4; ++e) held[4 * t + e] = x[e];
-            __syncthreads();
-            const bool keep_small = ((4 * t & k) == 0) == ((4 * t & j) == 0);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const K o = held[(4 * t ^ j) + e];
-                x[e] = (o < x[e]) == keep_small ? o : x[e];
-            }
-        }
-        for (int j = min(k >> 1, 128); j >= 4; j >>= 1) {
-            const bool keep_small = ((4 * t & k) == 0) == ((4 * t & j) == 0);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                K o;
-                if constexpr (sizeof(K) == 4) o = (K)__shfl_xor((int)x[e], j >> 2, 64);
-                else o = (K)__shfl_xor((unsigned long long)x[e], j >> 2, 64);
-                x[e] = (o < x[e]) == keep_small ? o : x[e];
-            }
-        }
-        const bool up = (4 * t & k) == 0;
-        if (k >= 4) {
-            order(x[0], x[2], up);
-            order(x[1], x[3], up);
-            order(x[0], x[1], up);
-            order(x[2], x[3], up);
-        } else {                                    // pairs, in turn up and down
-            order(x[0], x[1], true);
-            order(x[2], x[3], false);
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int32_t i = 4 * t + e;
-        const bool there = i < here;
-        keys[base + i] = there ? (uint32_t)(x[e] >> 12) : ~0u;
-        pos[base + i] = there ? (uint32_t)(x[e] & 4095) + (uint32_t)base : 0u;
-        if (rank) rank[base + i] = 0;
+        for (int w = 0; w < 16; ++w) at += part[w][lane];
+        keys[at] = mine;
+        pos[at] = (uint32_t)i;
     }
 }
 
-// An element's place among all tiles is the number of smaller ones in each, where equal ids count in the tiles left of its own. A block takes 1024 elements of a
-// tile and a share of the tiles to search; the shares add up in whole numbers, in any order.
+// A tile's positions in order: a bitonic network over (id, position in the tile), an element a thread; distances under 64 stay in a wavefront, the ten steps of more go
+// through LDS. K: 32 bits where the ids leave 10 of them, else 64. Ids outside the table come last, and behind them what is not there (~0).
+template <typename K>
+__global__ void __launch_bounds__(1024) embed_tile_kernel(const int32_t* __restrict__ ids, const int32_t* d_n, int32_t cap, uint32_t n_rows, uint32_t* keys, uint32_t* pos,
+                                                          uint32_t* rank) {
+    __shared__ K held[2][EMBED_TILE];
+    const int32_t n = rows_here(d_n, cap), base = (int32_t)blockIdx.x * EMBED_TILE, t = threadIdx.x, here = min(EMBED_TILE, n - base);
+    if (here <= 0) return;
+    K x = t < here ? (K)min((uint32_t)ids[base + t], n_rows) << 10 | (K)t : ~(K)0;
+    int turn = 0;
+    for (int k = 2; k <= EMBED_TILE; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            K o;
+            if (j >= 64) {              // (the other half of `held` was read before the barrier of the step between)
+                held[turn][t] = x;
+                __syncthreads();
+                o = held[turn][t ^ j];
+                turn ^= 1;
+            } else if constexpr (sizeof(K) == 4) o = (K)__shfl_xor((int)x, j, 64);
+            else o = (K)__shfl_xor((unsigned long long)x, j, 64);
+            x = (o < x) == (((t & k) == 0) == ((t & j) == 0)) ? o : x;
+        }
+    const bool there = t < here;
+    keys[base + t] = there ? (uint32_t)(x >> 10) : ~0u;
+    pos[base + t] = there ? (uint32_t)(x & 1023) + (uint32_t)base : 0u;
+    rank[base + t] = 0;
+}
+
+// An element's place among all tiles is the number of smaller ones in each, where equal ids count in the tiles left of its own. A block takes a tile's elements and a
+// share of the tiles to search, four at a time, so that four searches go on beside each other; the shares add up in whole numbers, in any order.
 __global__ void __launch_bounds__(1024) embed_rank_kernel(const uint32_t* __restrict__ keys, const int32_t* d_n, int32_t cap, int32_t shares, uint32_t* rank) {
-    __shared__ __attribute__((aligned(16))) uint32_t held[EMBED_TILE];
-    const int32_t n = rows_here(d_n, cap), i = (int32_t)blockIdx.x * 1024 + (int32_t)threadIdx.x, own = (int32_t)blockIdx.x / (EMBED_TILE / 1024);
+    __shared__ __attribute__((aligned(16))) uint32_t held[4][EMBED_TILE];
+    const int32_t n = rows_here(d_n, cap), own = (int32_t)blockIdx.x, t = threadIdx.x;
     if (own * EMBED_TILE >= n) return;
     const int32_t tiles = (n + EMBED_TILE - 1) / EMBED_TILE;
-    const uint32_t key = keys[i];
+    const uint32_t key = keys[own * EMBED_TILE + t];
     uint32_t before = 0;
-    for (int32_t o = blockIdx.y; o < tiles; o += shares) {
-        if (o == own) {
-            before += (uint32_t)(i - own * EMBED_TILE);
-            continue;
-        }
+    for (int32_t o = blockIdx.y * 4; o < tiles; o += shares * 4) {
         __syncthreads();
-        reinterpret_cast<uint4*>(held)[threadIdx.x] = reinterpret_cast<const uint4*>(keys + o * EMBED_TILE)[threadIdx.x];
+        const int32_t part = t >> 8, quad = t & 255;
+        reinterpret_cast<uint4*>(held[part])[quad] = o + part < tiles ? reinterpret_cast<const uint4*>(keys + (o + part) * EMBED_TILE)[quad] : uint4{~0u, ~0u, ~0u, ~0u};
         __syncthreads();
-        // elements below `to`, or up to it in earlier tiles (key + 1 does not wrap: an id is at most n_rows; what is not there is not stored)
-        const uint32_t to = o < own ? key + 1 : key;
-        uint32_t at = 0;
+        // elements below key, or up to it in earlier tiles (key + 1 does not wrap: an id is at most n_rows; what is not there is not stored)
+        uint32_t at[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int step = EMBED_TILE / 2; step > 0; step >>= 1) at += held[at + step - 1] < to ? step : 0;
-        before += at + (held[at] < to);
+        for (int step = EMBED_TILE / 2; step > 0; step >>= 1)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) at[q] += held[q][at[q] + step - 1] < (o + q < own ? key + 1 : key) ? step : 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (o + q >= tiles) continue;
+            before += o + q == own ? (uint32_t)t : at[q] + (held[q][at[q]] < (o + q < own ? key + 1 : key));
+        }
     }
-    if (key != ~0u) atomicAdd(&rank[i], before);
+    if (key != ~0u) atomicAdd(&rank[own * EMBED_TILE + t], before);
 }
 
 __global__ void __launch_bounds__(256) embed_place_kernel(const uint32_t* __restrict__ keys_in, const uint32_t* __restrict__ pos_in, const uint32_t* __restrict__ rank,
@@ -296,54 +290,82 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
     }
 }
 
-// Adds up the sums that reach over borders: the chunk where such an id begins owns it. A block's eight wavefronts share the later chunks' parts, and look for their
-// number 64 chunks at a time.
+// Adds up the sums that reach over borders: the chunk where such an id begins owns it. A wavefront looks at a chunk, counts the id's later chunks 64 at a time, and adds their
+// parts by itself where they are few; the parts of an id with many are shared by the block's eight wavefronts.
 __global__ void __launch_bounds__(512) embed_join_kernel(EmbedSums a, int64_t chunks) {
+    constexpr int64_t FEW = 16;
     __shared__ float share[8][64][4];
+    __shared__ int64_t many[8];             // parts of a wavefront's id, where they are many
     const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id(), wave = (int32_t)(threadIdx.x >> 6), ch = a.chunk;
     const int32_t col = ((int32_t)blockIdx.y * 64 + lane) * 4, width = a.dim - col;
     const int64_t here = min(chunks, ceil_div(n, ch));
-    for (int64_t c = blockIdx.x; c + 1 < here; c += gridDim.x) {
-        const uint32_t first = a.keys[c * ch], key = a.keys[(c + 1) * ch - 1], next = a.keys[(c + 1) * ch], prior = c > 0 ? a.keys[c * ch - 1] : ~0u;
-        if ((int64_t)key >= a.n_rows || next != key || (first == key && prior == key)) continue;
-        int64_t end = c + 2;                    // the first chunk that does not begin with this id
-        for (;;) {
-            const uint64_t same = __ballot(end + lane < here && a.keys[min(end + lane, here - 1) * ch] == key);
-            end += same == ~0ull ? 64 : __builtin_ctzll(~same);
-            if (same != ~0ull) break;
-        }
-        const int64_t parts = end - c, each = ceil_div(parts, 8), p0 = min(parts, wave * each), p1 = min(parts, p0 + each);
-        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (width > 0) {
+    auto add = [&](int64_t c, int64_t p0, int64_t p1, float (&acc)[4]) {
+        if (width <= 0) return;
 #pragma unroll 8
-            for (int64_t p = p0; p < p1; ++p) {
-                Run<float, 4> r;
-                r.load(a.parts + ((c + p) * 2 + (p == 0)) * a.dim + col, width, 0.0f);
-                float f[4];
-                r.get(f);
+        for (int64_t p = p0; p < p1; ++p) {
+            Run<float, 4> r;
+            r.load(a.parts + ((c + p) * 2 + (p == 0)) * a.dim + col, width, 0.0f);
+            float f[4];
+            r.get(f);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) acc[w] += f[w];
+            for (int w = 0; w < 4; ++w) acc[w] += f[w];
+        }
+    };
+    auto put = [&](uint32_t key, const float (&sum)[4]) {
+        if (width <= 0) return;
+        float* to = a.table.row<float>(key) + col;
+        Run<float, 4> out;
+        float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (a.accumulate) { out.load(to, width, 0.0f); out.get(f); }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) f[w] += a.scale * sum[w];
+        out.set(f);
+        out.store(to, width);
+    };
+    for (int64_t c0 = (int64_t)blockIdx.x * 8; c0 + 1 < here; c0 += (int64_t)gridDim.x * 8) {
+        const int64_t c = c0 + wave;
+        int64_t parts = 0;
+        uint32_t key = 0;
+        if (c + 1 < here) {
+            const uint32_t first = a.keys[c * ch], next = a.keys[(c + 1) * ch], prior = c > 0 ? a.keys[c * ch - 1] : ~0u;
+            key = a.keys[(c + 1) * ch - 1];
+            if ((int64_t)key < a.n_rows && next == key && !(first == key && prior == key)) {
+                int64_t end = c + 2;            // the first chunk that does not begin with this id
+                for (;;) {
+                    const uint64_t same = __ballot(end + lane < here && a.keys[min(end + lane, here - 1) * ch] == key);
+                    end += same == ~0ull ? 64 : __builtin_ctzll(~same);
+                    if (same != ~0ull) break;
+                }
+                parts = end - c;
             }
         }
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < 4; ++w) share[wave][lane][w] = acc[w];
-        __syncthreads();
-        if (wave == 0 && width > 0) {
-            float* to = a.table.row<float>(key) + col;
-            Run<float, 4> out;
-            float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (a.accumulate) { out.load(to, width, 0.0f); out.get(f); }
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                float sum = share[0][lane][w];
-#pragma unroll
-                for (int o = 1; o < 8; ++o) sum += share[o][lane][w];
-                f[w] += a.scale * sum;
-            }
-            out.set(f);
-            out.store(to, width);
+        if (parts > 0 && parts <= FEW) {
+            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            add(c, 0, parts, acc);
+            put(key, acc);
         }
+        if (lane == 0) many[wave] = parts > FEW ? parts : 0;
+        __syncthreads();
+        for (int w = 0; w < 8; ++w) {
+            const int64_t all = many[w], each = (all + 7) / 8, p0 = min(all, wave * each), p1 = min(all, p0 + each);
+            if (all == 0) continue;
+            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            add(c0 + w, p0, p1, acc);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) share[wave][lane][q] = acc[q];
+            __syncthreads();
+            if (wave == w) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    acc[q] = share[0][lane][q];
+#pragma unroll
+                    for (int o = 1; o < 8; ++o) acc[q] += share[o][lane][q];
+                }
+                put(key, acc);
+            }
+            __syncthreads();
+        }
+        __syncthreads();
     }
 }
 
@@ -407,17 +429,17 @@ extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t gra
     char* ws = (char*)d_ws;
     uint32_t *keys = (uint32_t*)(ws + plan.keys), *pos = (uint32_t*)(ws + plan.pos);
     if (n_ids_cap > 0) {
-        if (!plan.radix) {
-            uint32_t *k = plan.merged ? (uint32_t*)(ws + plan.keys_tmp) : keys, *v = plan.merged ? (uint32_t*)(ws + plan.pos_tmp) : pos,
-                     *rank = plan.merged ? (uint32_t*)(ws + plan.rank) : nullptr;
-            const unsigned tiles = (unsigned)plan.tiles;
-            if (n_rows < (1 << 20)) hipLaunchKernelGGL(embed_tile_kernel<uint32_t>, dim3(tiles), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows, k, v, rank);
+        const unsigned tiles = (unsigned)plan.tiles;
+        if (plan.merged) {
+            uint32_t *k = (uint32_t*)(ws + plan.keys_tmp), *v = (uint32_t*)(ws + plan.pos_tmp), *rank = (uint32_t*)(ws + plan.rank);
+            if (n_rows < (1 << 22)) hipLaunchKernelGGL(embed_tile_kernel<uint32_t>, dim3(tiles), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows, k, v, rank);
             else hipLaunchKernelGGL(embed_tile_kernel<uint64_t>, dim3(tiles), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows, k, v, rank);
-            if (plan.merged) {
-                const unsigned shares = tiles >= 64 ? 2 : tiles >= 32 ? 4 : tiles < 8 ? tiles : 8;
-                hipLaunchKernelGGL(embed_rank_kernel, dim3(tiles * (EMBED_TILE / 1024), shares), dim3(1024), 0, st, k, d_n_ids, n_ids_cap, (int32_t)shares, rank);
-                hipLaunchKernelGGL(embed_place_kernel, dim3(tiles * (EMBED_TILE / 256)), dim3(256), 0, st, k, v, rank, d_n_ids, n_ids_cap, keys, pos);
-            }
+            // about 512 blocks, two to a compute unit
+            const unsigned groups = (tiles + 3) / 4, wanted = (512 + tiles - 1) / tiles, shares = wanted < groups ? wanted : groups;
+            hipLaunchKernelGGL(embed_rank_kernel, dim3(tiles, shares), dim3(1024), 0, st, k, d_n_ids, n_ids_cap, (int32_t)shares, rank);
+            hipLaunchKernelGGL(embed_place_kernel, dim3(tiles * (EMBED_TILE / 256)), dim3(256), 0, st, k, v, rank, d_n_ids, n_ids_cap, keys, pos);
+        } else if (!plan.radix) {
+            hipLaunchKernelGGL(embed_count_kernel, dim3((unsigned)ceil_div(n_ids_cap, 64)), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, keys, pos);
         } else {
             const int bits = ilog2_ceil((uint64_t)n_rows + 1), passes = radix_passes(bits), digit = radix_digit_bits(bits);
             const RadixPlan radix(n_ids_cap);
@@ -434,7 +456,9 @@ extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t gra
                       plan.chunk, (float*)(ws + plan.parts)};
     if (dt == NO_F32) launch_sums<float>(a, plan.chunks, st);
     else launch_sums<bf16_t>(a, plan.chunks, st);
-    if (plan.chunks > 1)
-        hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(plan.chunks - 1 < 1024 ? plan.chunks - 1 : 1024), (unsigned)ceil_div(dim, 256)), dim3(512), 0, st, a, plan.chunks);
+    if (plan.chunks > 1) {
+        const int64_t eights = ceil_div(plan.chunks - 1, 8);
+        hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(eights < 4096 ? eights : 4096), (unsigned)ceil_div(dim, 256)), dim3(512), 0, st, a, plan.chunks);
+    }
     return launch_status(who);
 }

@@ -11,16 +11,25 @@ namespace no {
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
-// Sums of a row or a piece: largest logit (-inf: there is none above), sum of 2^x, sum of x 2^x.
-struct Sums { float m, s, h; };
-
 __device__ __forceinline__ float above(float m) { return m == -INFINITY ? 0.0f : m; }      // what differences are taken from
 
-// x of a logit; the maximum is a row's, a piece's, or one that replaces it.
+// x of a logit under a maximum.
 struct Exponent {
     float from, c;
     __device__ __forceinline__ Exponent(float m, float c_) : from(above(m)), c(c_) {}
     __device__ __forceinline__ float operator()(float z) const { return (z - from) * c; }
+};
+
+// Sums of a row, a piece or a lane's values: largest logit (-inf: there is none above), sum of 2^x, sum of x 2^x.
+struct Sums {
+    float m, s, h;
+    // s and h as they are under another maximum, no smaller than m
+    template <bool ENTROPY>
+    __device__ __forceinline__ void move(const Exponent& to) {
+        const float d = to(above(m)), e = s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(d);
+        if constexpr (ENTROPY) h = e * (h + fmaxf(d, -3.0e38f) * s);
+        s *= e;
+    }
 };
 
 template <typename T, int U, int TEAM>
@@ -28,51 +37,54 @@ struct Piece : RowRegs<T, 16 / (int)sizeof(T), U, TEAM> {      // logits of a ro
     static constexpr int W = 16 / (int)sizeof(T);
     using RowRegs<T, W, U, TEAM>::v;
     __device__ __forceinline__ void load(const T* z, int32_t len, int t) { RowRegs<T, W, U, TEAM>::load(z, len, t, from_f32<T>(-INFINITY)); }
-    __device__ __forceinline__ float lane_max() const {
-        float m = -INFINITY;
+    // Sums of the lane's values, run by run with the maximum so far, so that the first runs are added while later ones are still on their way; what was added under a smaller
+    // maximum is scaled down, one exponential a run.
+    template <bool ENTROPY>
+    __device__ __forceinline__ Sums lane_sums(float c) {
+        Sums r{-INFINITY, 0.0f, 0.0f};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float f[W];
+            float f[W], m = r.m;
             v[u].get(f);
 #pragma unroll
             for (int w = 0; w < W; ++w) m = fmaxf(m, f[w]);
-        }
-        return m;
-    }
-    // adds the lane's terms of s, and of h if ENTROPY; 0 (-inf) counts as 0
-    template <bool ENTROPY>
-    __device__ __forceinline__ void add(const Exponent& x, float& s, float& h) const {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[W];
-            v[u].get(f);
+            const Exponent x(m, c);
+            if (u > 0) r.move<ENTROPY>(x);
+            r.m = m;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const float d = x(f[w]), e = __builtin_amdgcn_exp2f(d);
-                s += e;
-                if constexpr (ENTROPY) h += e * fmaxf(d, -3.0e38f);
+                r.s += e;
+                if constexpr (ENTROPY) r.h += e * fmaxf(d, -3.0e38f);     // (-inf counts as 0)
             }
-            if constexpr (ENTROPY) asm volatile("" : "+v"(h));      // (put off until h is asked for, its sum would keep every exponential in a register)
+            // The next run waits for this one's sums: taken ahead for their maximum, or put off until h is asked for, all runs' values or exponentials
+            // would stand in registers at once.
+            asm volatile("" : "+v"(v[u + 1 < U ? u + 1 : u].v[0]), "+v"(r.s), "+v"(r.h));
         }
+        return r;
     }
 };
+
+// Sums of a team's lanes, or of a lane's share of a row's pieces, each with its own maximum, as the team's.
+template <bool ENTROPY, int TEAM, int THREADS>
+__device__ __forceinline__ Sums team_sums(Sums r, float c, Team<TEAM, THREADS>& team) {
+    const float m = team.max(r.m);
+    r.move<ENTROPY>(Exponent(m, c));
+    return Sums{m, team.sum(r.s), ENTROPY ? team.sum(r.h) : 0.0f};
+}
 
 // Joins the sums of a row's pieces, each with its own maximum: a lane takes pieces t, t + TEAM, ...
 template <int TEAM, int THREADS>
 __device__ __forceinline__ Sums join_sums(const Sums* parts, int32_t pieces, float c, Team<TEAM, THREADS>& team) {
-    float m = -INFINITY;
-    const int t = team.lane();
-    for (int32_t p = t; p < pieces; p += TEAM) m = fmaxf(m, parts[p].m);
-    m = team.max(m);
-    const Exponent x(m, c);
-    float s = 0.0f, h = 0.0f;
-    for (int32_t p = t; p < pieces; p += TEAM) {
-        const Sums q = parts[p];
-        const float d = x(above(q.m)), e = q.s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(d);
-        s += e * q.s;
-        h += e * (q.h + fmaxf(d, -3.0e38f) * q.s);
+    Sums r{-INFINITY, 0.0f, 0.0f};
+    for (int32_t p = team.lane(); p < pieces; p += TEAM) {
+        Sums q = parts[p];
+        const Exponent x(fmaxf(r.m, q.m), c);
+        r.move<true>(x);
+        q.move<true>(x);
+        r = Sums{fmaxf(r.m, q.m), r.s + q.s, r.h + q.h};
     }
-    return Sums{m, team.sum(s), team.sum(h)};
+    return team_sums<true>(r, c, team);
 }
 
 // ------------------------------------------------------------------------------------------------------- teacher
@@ -191,7 +203,8 @@ template <typename T, int U, int TEAM, int THREADS, typename Q, typename After>
 __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_t first, int32_t len, Piece<T, U, TEAM>& v, const Q& q, float w, const Teacher& te,
                                              Team<TEAM, THREADS>& team, After after) {
     constexpr int W = Piece<T, U, TEAM>::W;
-    const int t = team.lane();
+    int t = team.lane();
+    asm volatile("" : "+v"(t));
     T* const out = a.grad.row<T>(i) + first;
     RowStore<T, W> store(out, len);
     const bool live = w != 0.0f && te.any;
@@ -241,11 +254,13 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(Distill a) {
         e.load_logits(z, a.classes, 0, a.classes);
         e.shares(a, te);
     }
-    Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
+    if (a.lse_in) {
+        team.sync();
+        distill_grad(a, i, 0, a.classes, v, ShareByLse(a.inv_t, a.lse_in[i], w * a.temperature), w, te, team, [](int) {});
+        return;
+    }
+    const Sums r = team_sums<false>(v.template lane_sums<false>(a.c), a.c, team);
     v.renew();
-    v.template add<false>(Exponent(r.m, a.c), r.s, r.h);
-    v.renew();
-    r.s = team.sum(r.s);
     if constexpr (TEAM == 64) team.sync();      // (the entries; in larger teams a sum's barrier stood between)
     if (first_wave) distill_loss(a, i, r, w, te);
     if (a.grad.p) distill_grad(a, i, 0, a.classes, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [](int) {});
@@ -262,31 +277,30 @@ __global__ void __launch_bounds__(1024) distill_rows_kernel(Distill a) {
     const bool first_wave = threadIdx.x < 64;
     int64_t i = a.row0 + blockIdx.x;
     if (i >= n) return;
+    int t = threadIdx.x;
     Entries e;
     Piece<T, U, 1024> v;
-    v.load(a.z.row<T>(i), a.classes, team.lane());
+    v.load(a.z.row<T>(i), a.classes, t);
     if (first_wave) {
         e.load(a, i);
         e.load_logits(a.z.row<T>(i), a.classes, 0, a.classes);
     }
     for (int turn = 0; i < n; turn ^= 1) {
         Teacher& te = teachers[turn];
+        asm volatile("" : "+v"(t));                 // (what follows from it is made anew in each row, not kept in registers over all of them)
         const int64_t next = i + gridDim.x;
         const T* const next_row = a.z.row<T>(next < n ? next : i);
         const int32_t next_len = next < n ? a.classes : 0;
         const float w = a.weight ? a.weight[i] : 1.0f;
         if (first_wave) e.shares(a, te);
         v.renew();
-        Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
+        const Sums r = team_sums<false>(v.template lane_sums<false>(a.c), a.c, team);
         v.renew();
-        v.template add<false>(Exponent(r.m, a.c), r.s, r.h);
-        v.renew();
-        r.s = team.sum(r.s);
         if (first_wave) distill_loss(a, i, r, w, te);
         distill_grad(a, i, 0, a.classes, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [&](int u) {
-            v.load_run(next_row, next_len, threadIdx.x, u, from_f32<T>(-INFINITY));
+            v.load_run(next_row, next_len, t, u, from_f32<T>(-INFINITY));
         });
-        v.load_end(next_row, next_len, threadIdx.x, from_f32<T>(-INFINITY));
+        v.load_end(next_row, next_len, t, from_f32<T>(-INFINITY));
         if (first_wave && next < n) {
             e.load(a, next);
             e.load_logits(next_row, a.classes, 0, a.classes);
@@ -305,10 +319,7 @@ __global__ void __launch_bounds__(THREADS) distill_sums_kernel(Distill a) {
     if (i >= rows_here(a.d_n, a.cap)) return;
     Piece<T, U, THREADS> v;
     v.load(a.z.row<T>(i) + (int64_t)p * a.piece, min(a.piece, a.classes - p * a.piece), team.lane());
-    Sums r{team.max(v.lane_max()), 0.0f, 0.0f};
-    v.renew();
-    v.template add<false>(Exponent(r.m, a.c), r.s, r.h);
-    r.s = team.sum(r.s);
+    const Sums r = team_sums<false>(v.template lane_sums<false>(a.c), a.c, team);
     if (threadIdx.x == 0) a.parts[i * a.pieces + p] = r;
 }
 
@@ -374,16 +385,17 @@ struct TopSpace {
     static constexpr int CAP = 512;         // candidates that are ranked against each other
     uint64_t key[CAP];
     int32_t count;
-    float lane_max[TEAM > 64 ? TEAM : 1];
-    float from;
+    uint32_t alone[TEAM / 64], shared[TEAM / 64];
 };
 
-// The k largest values of a piece, as order keys in `to.key[0 .. min(count, CAP))`, in no order, with others that are smaller among them perhaps. The k-th largest of the lanes'
-// own maxima is a bound that k values at least reach, and few others do as a rule: those that do are collected. Where more do than there is room for (equal
+// The k largest values of a piece, as order keys in `to.key[0 .. min(count, CAP))`, in no order, with others that are smaller among them perhaps: all that reach a bound which
+// k values at least reach, and few others as a rule. Where n wavefronts share the piece, the ceil(k / n)-th largest of a wavefront's 64 lane maxima is reached by that many
+// of its values, and the least of the n such values by k of the piece; the k-th largest lane maximum of any one wavefront will do as well, and does better where
+// another holds masked classes alone. The larger of the two is the bound. Where more do than there is room for (equal
 // values, or large ones that sit in few lanes), the bound is raised bit by bit, first by value, then among equal ones by class.
 template <typename T, int U, int TEAM, int THREADS>
 __device__ __forceinline__ void top_candidates(Piece<T, U, TEAM>& v, float lane_max, int32_t first, int32_t k, TopSpace<TEAM>& to, Team<TEAM, THREADS>& team) {
-    constexpr int W = Piece<T, U, TEAM>::W, Q = TEAM > 64 ? TEAM / 64 : 1;
+    constexpr int W = Piece<T, U, TEAM>::W;
     const int t = team.lane();
     const int32_t base = first + t * W;     // class of a lane's first value; those of run u follow at u TEAM W (classes written out would be kept in registers)
     // The values that `in` takes go to the list. Which runs hold any is found first; then a loop takes those runs, one or two in the lanes that
@@ -433,34 +445,32 @@ __device__ __forceinline__ void top_candidates(Piece<T, U, TEAM>& v, float lane_
                 }
         }
     };
-    // the k-th largest lane maximum, its upper 16 bits (so a little less than it): one wavefront looks for them bit by bit
-    float bound = 0.0f;
-    if constexpr (TEAM > 64) {
-        to.lane_max[t] = lane_max;
-        if (t == 0) to.count = 0;
-        team.sync();
-    } else if (t == 0) to.count = 0;
-    if (TEAM <= 64 || threadIdx.x < 64) {
-        uint32_t o[Q];
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            if constexpr (TEAM > 64) o[q] = order_of(to.lane_max[lane_id() + q * 64]);
-            else o[q] = order_of(lane_max);
-        }
-        uint32_t best = 0;
-        for (int b = 31; b >= 16; --b) {
-            const uint32_t cand = best | 1u << b;
-            int here = 0;
-#pragma unroll
-            for (int q = 0; q < Q; ++q) here += __popcll(__ballot(o[q] >= cand));
-            if (here >= k) best = cand;
-        }
-        bound = value_of(best);
-        if (best <= order_of(-3.4028234663852886e38f)) bound = -3.4028234663852886e38f;     // (-inf is no candidate)
-        if constexpr (TEAM > 64) if (threadIdx.x == 0) to.from = bound;
+    // bounds of the wavefront, their upper 16 bits (so a little less than they are), bit by bit
+    constexpr int WAVES = TEAM / 64;
+    const int need = (k + WAVES - 1) / WAVES;
+    const uint32_t o = order_of(lane_max);
+    uint32_t alone = 0, shared = 0;
+    for (int b = 31; b >= 16; --b) {
+        if (__popcll(__ballot(o >= (alone | 1u << b))) >= k) alone |= 1u << b;
+        if (WAVES > 1 && __popcll(__ballot(o >= (shared | 1u << b))) >= need) shared |= 1u << b;
     }
+    if constexpr (WAVES > 1) {
+        if (lane_id() == 0) {
+            to.alone[threadIdx.x >> 6] = alone;
+            to.shared[threadIdx.x >> 6] = shared;
+        }
+    }
+    if (t == 0) to.count = 0;
     team.sync();
-    if constexpr (TEAM > 64) bound = to.from;
+    if constexpr (WAVES > 1) {
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            shared = min(shared, to.shared[w]);
+            alone = max(alone, to.alone[w]);
+        }
+        alone = max(alone, shared);
+    }
+    const float bound = alone <= order_of(-3.4028234663852886e38f) ? -3.4028234663852886e38f : value_of(alone);       // (-inf is no candidate)
     if (lane_max >= bound) collect([&](float f, int32_t) { return f >= bound; });
     team.sync();
     if (to.count <= TopSpace<TEAM>::CAP) return;
@@ -553,13 +563,7 @@ __global__ void __launch_bounds__(THREADS, U == 8 ? 5 : U == 4 ? 7 : 8) logprobs
     const int32_t first = SPLIT ? p * a.piece : 0, len = SPLIT ? min(a.piece, a.classes - first) : a.classes;
     Piece<T, U, TEAM> v;
     v.load(a.z.row<T>(i) + first, len, t);
-    const float mine = v.lane_max();
-    Sums r{team.max(mine), 0.0f, 0.0f};
-    v.renew();
-    v.template add<true>(Exponent(r.m, a.c), r.s, r.h);
-    v.renew();
-    r.s = team.sum(r.s);
-    r.h = team.sum(r.h);
+    const Sums mine = v.template lane_sums<true>(a.c), r = team_sums<true>(mine, a.c, team);
     const float log_s = log2f(r.s);
     if (t == 0) {
         if constexpr (SPLIT) a.parts[i * a.pieces + p] = r;
@@ -567,7 +571,7 @@ __global__ void __launch_bounds__(THREADS, U == 8 ? 5 : U == 4 ? 7 : 8) logprobs
     }
     if (a.k == 0) return;
     TopSpace<TEAM>& top = tops[team.index()];
-    top_candidates(v, mine, first, a.k, top, team);
+    top_candidates(v, mine.m, first, a.k, top, team);
     const int32_t count = min(top.count, TopSpace<TEAM>::CAP);
     auto put = [&](int32_t at, uint64_t key) {
         if constexpr (SPLIT) a.keys[(i * a.pieces + p) * a.k + at] = key;
@@ -650,22 +654,23 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
     for (int32_t e = count + t; e < a.k; e += 256) store_top(a, i, e, 0, r, log_s);
 }
 
-template <typename T, int U>
-__global__ void __launch_bounds__(256) logprobs_grad_kernel(RowsOf z, const int32_t* d_n, int64_t row0, int32_t cap, int32_t classes, int32_t pieces, const int32_t* __restrict__ tokens, float inv_t,
-                                                            const float* __restrict__ lse, const float* __restrict__ entropy, const float* __restrict__ g_logprob,
+template <typename T, int TEAM, int U>
+__global__ void __launch_bounds__(256) logprobs_grad_kernel(RowsOf z, const int32_t* d_n, int64_t row0, int32_t cap, int32_t classes, int32_t pieces, const int32_t* __restrict__ tokens,
+                                                            float inv_t, const float* __restrict__ lse, const float* __restrict__ entropy, const float* __restrict__ g_logprob,
                                                             const float* __restrict__ g_entropy, RowsOf grad) {
-    constexpr int W = Piece<T, U, 256>::W, PIECE = W * U * 256;
-    const int64_t i = row0 + blockIdx.x / (uint32_t)pieces;
-    const int32_t first = (int32_t)(blockIdx.x % (uint32_t)pieces) * PIECE, len = min(PIECE, classes - first);
+    constexpr int W = Piece<T, U, TEAM>::W, PIECE = W * U * TEAM;
+    const int t = Team<TEAM, 256>::lane();
+    const int64_t i = row0 + (TEAM == 256 ? blockIdx.x / (uint32_t)pieces : (int64_t)blockIdx.x * (256 / TEAM) + Team<TEAM, 256>::index());
+    const int32_t first = TEAM == 256 ? (int32_t)(blockIdx.x % (uint32_t)pieces) * PIECE : 0, len = min(PIECE, classes - first);
     if (i >= rows_here(d_n, cap)) return;
-    Piece<T, U, 256> v;
-    v.load(z.row<T>(i) + first, len, threadIdx.x);
+    Piece<T, U, TEAM> v;
+    v.load(z.row<T>(i) + first, len, t);
     const int32_t tok = tokens[i];
     const float l = lse[i], h = entropy[i], gl = g_logprob && tok >= 0 && tok < classes ? g_logprob[i] : 0.0f, gh = g_entropy ? g_entropy[i] : 0.0f;
     RowStore<T, W> store(grad.row<T>(i) + first, len);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int32_t c = v.at(threadIdx.x, u);
+        const int32_t c = v.at(t, u);
         float f[W];
         v.v[u].get(f);
 #pragma unroll
@@ -705,14 +710,14 @@ static int32_t check_teacher(const char* who, int32_t n, const int32_t* ids, con
 // Rows in pieces: as many as fill the chip while rows are few, of a multiple of a block's runs.
 struct Cut {
     int32_t u, piece, pieces;
-    Cut(int32_t n, int32_t classes, int32_t w) {
-        u = 8;
+    Cut(int32_t n, int32_t classes, int32_t w, int32_t most_u) {
+        u = most_u;
         while (u > 1 && (int64_t)n * ceil_div(classes, 256 * w * u) < 1024) u >>= 1;
         piece = 256 * w * u;
         pieces = (int32_t)ceil_div(classes, piece);
     }
 };
-static int32_t most_pieces(int32_t n, int32_t classes) { return Cut(n, classes, 4).pieces; }      // (of either type)
+static int32_t most_pieces(int32_t n, int32_t classes) { return Cut(n, classes, 4, 8).pieces; }      // (of either type: bf16 pieces of 4 runs are as long)
 
 constexpr int64_t FEW_ROWS = 128;       // rows that leave half of the chip idle when each is one block's
 
@@ -738,7 +743,8 @@ static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
         a.pieces = (int32_t)rows;                                                                                             \
         hipLaunchKernelGGL((distill_rows_kernel<T, U>), dim3((unsigned)(rows < 256 ? rows : 256)), dim3(1024), 0, st, a);     \
     })
-    const bool row = !a.lse_in && units <= 16384 && (units <= 2048 || (a.grad.p && a.cap >= FEW_ROWS));
+    // (from a given lse every piece of a row goes by itself, but short rows by wavefronts, which share the work on the teacher's entries)
+    const bool row = a.lse_in ? units <= 256 : units <= 2048 || (units <= 16384 && a.grad.p && a.cap >= FEW_ROWS);
     if (row) {
         if (units <= 64) NO_ROW(64, 256, 1);
         else if (units <= 128) NO_ROW(64, 256, 2);
@@ -753,7 +759,7 @@ static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
     }
 #undef NO_ROW
 #undef NO_ROWS
-    const Cut cut(a.cap, a.classes, W);
+    const Cut cut(a.cap, a.classes, W, 8);
     a.piece = cut.piece;
     a.pieces = cut.pieces;
     a.parts = (Sums*)ws;
@@ -803,10 +809,10 @@ static int32_t logprobs(const char* who, Logprobs a, void* ws, hipStream_t st) {
     else if (units <= 256) NO_ROW(64, 4);
     else if (units <= 512) NO_ROW(256, 2);
     else if (units <= 1024) NO_ROW(256, 4);
-    else if (units <= 2048) NO_ROW(256, 8);
+    else if (W == 4 && units <= 2048) NO_ROW(256, W == 4 ? 8 : 4);
 #undef NO_ROW
     else {
-        const Cut cut(a.cap, a.classes, W);
+        const Cut cut(a.cap, a.classes, W, 32 / W);
         a.piece = cut.piece;
         a.pieces = cut.pieces;
         a.parts = (Sums*)ws;
@@ -814,7 +820,7 @@ static int32_t logprobs(const char* who, Logprobs a, void* ws, hipStream_t st) {
         in_slabs(a.cap, MOST_BLOCKS / a.pieces, [&](int64_t row0, int64_t rows) {
             const dim3 grid((unsigned)(rows * a.pieces));
             a.row0 = row0;
-            if (cut.u == 8) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 8, true>), grid, dim3(256), 0, st, a);
+            if (cut.u == 8) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, W == 4 ? 8 : 4, true>), grid, dim3(256), 0, st, a);
             else if (cut.u == 4) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 4, true>), grid, dim3(256), 0, st, a);
             else if (cut.u == 2) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 2, true>), grid, dim3(256), 0, st, a);
             else hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 1, true>), grid, dim3(256), 0, st, a);
@@ -827,11 +833,19 @@ static int32_t logprobs(const char* who, Logprobs a, void* ws, hipStream_t st) {
 template <typename T>
 static int32_t logprobs_grad(const char* who, const RowsOf& z, const int32_t* d_n, int32_t cap, int32_t classes, const int32_t* tokens, float inv_t, const float* lse,
                              const float* entropy, const float* g_logprob, const float* g_entropy, const RowsOf& grad, hipStream_t st) {
-    const Cut cut(cap, classes, 16 / (int)sizeof(T));
-#define NO_GRAD(U) hipLaunchKernelGGL((logprobs_grad_kernel<T, U>), grid, dim3(256), 0, st, z, d_n, row0, cap, classes, cut.pieces, tokens, inv_t, lse, entropy, g_logprob, g_entropy, grad)
+    const int64_t units = ceil_div(classes, 16 / (int)sizeof(T));
+    const Cut cut(cap, classes, 16 / (int)sizeof(T), 8);
+#define NO_GRAD(TEAM, U) hipLaunchKernelGGL((logprobs_grad_kernel<T, TEAM, U>), grid, dim3(256), 0, st, z, d_n, row0, cap, classes, cut.pieces, tokens, inv_t, lse, entropy, g_logprob, g_entropy, grad)
+    if (units <= 256) {
+        in_slabs(cap, MOST_BLOCKS * 4, [&](int64_t row0, int64_t rows) {
+            const dim3 grid((unsigned)ceil_div(rows, 4));
+            if (units <= 64) NO_GRAD(64, 1); else if (units <= 128) NO_GRAD(64, 2); else NO_GRAD(64, 4);
+        });
+        return launch_status(who);
+    }
     in_slabs(cap, MOST_BLOCKS / cut.pieces, [&](int64_t row0, int64_t rows) {
         const dim3 grid((unsigned)(rows * cut.pieces));
-        if (cut.u == 8) NO_GRAD(8); else if (cut.u == 4) NO_GRAD(4); else if (cut.u == 2) NO_GRAD(2); else NO_GRAD(1);
+        if (cut.u == 8) NO_GRAD(256, 8); else if (cut.u == 4) NO_GRAD(256, 4); else if (cut.u == 2) NO_GRAD(256, 2); else NO_GRAD(256, 1);
     });
 #undef NO_GRAD
     return launch_status(who);

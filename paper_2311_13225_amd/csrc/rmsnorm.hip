@@ -230,25 +230,31 @@ __global__ void __launch_bounds__(256) rmsnorm_wide_parts_kernel(RowsOf s, const
     parts[(int64_t)blockIdx.y * dim + c] = sum;
 }
 
-// A column a lane, the parts shared by a block's sixteen wavefronts.
+// Sixteen columns a block, 64 lanes to a column, so that a lane has eight parts at most and asks for them at once.
 __global__ void __launch_bounds__(1024) rmsnorm_join_kernel(const float* __restrict__ parts, int32_t n_parts, int32_t dim, float* grad_weight) {
-    __shared__ float share[16][64];
-    const int32_t lane = lane_id(), wave = (int32_t)(threadIdx.x >> 6), c = (int32_t)blockIdx.x * 64 + lane;
+    __shared__ float share[64][16];
+    const int32_t col = (int32_t)threadIdx.x & 15, row = (int32_t)threadIdx.x >> 4, c = (int32_t)blockIdx.x * 16 + col;
     float sum = 0.0f;
     if (c < dim) {
-#pragma unroll 8
-        for (int32_t p = wave; p < n_parts; p += 16) sum += parts[(int64_t)p * dim + c];
-    }
-    share[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0 && c < dim) {
 #pragma unroll
-        for (int w = 1; w < 16; ++w) sum += share[w][lane];
-        grad_weight[c] = sum;
+        for (int k = 0; k < NORM_PARTS / 64; ++k) {
+            const int32_t p = row + k * 64;
+            sum += p < n_parts ? parts[(int64_t)p * dim + c] : 0.0f;
+        }
     }
+    share[row][col] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += share[(lane_id() >> 4) * 16 + k][col];
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (threadIdx.x < 16 && c < dim) grad_weight[c] = sum;
 }
 
-// Blocks for n rows: at most what fills the chip, so that a team walks several rows with the weights it holds.
+// Blocks for n rows: at most those that stand on the chip at once (by the kernel's registers), so that a team walks several rows with the weights it holds
+// and all teams end together.
 static inline int64_t norm_blocks(int64_t n, int per_block, int64_t most) {
     const int64_t b = ceil_div(n, per_block);
     return b < most ? b : most;
@@ -277,7 +283,7 @@ extern "C" int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride
     const RowsOf x = rows_of(d_x, x_stride_bytes), r = rows_of(d_residual, residual_stride_bytes), s = rows_of(d_sum, sum_stride_bytes), y = rows_of(d_y, y_stride_bytes);
     hipStream_t st = (hipStream_t)stream;
 #define NO_NORM_AS(T, Y, TEAM, THREADS, U)                                                                                                          \
-    hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, Y, TEAM, THREADS, U>), dim3((unsigned)norm_blocks(n_rows_cap, THREADS / TEAM, THREADS == 256 ? 2048 : 512)), \
+    hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, Y, TEAM, THREADS, U>), dim3((unsigned)norm_blocks(n_rows_cap, THREADS / TEAM, THREADS == 1024 ? 256 : U <= 2 ? 2048 : U == 3 ? 1792 : U == 4 ? 1280 : 768)), \
                        dim3(THREADS), 0, st, x, r, d_weight, eps, d_n_rows, n_rows_cap, dim, s, y, d_row_scale, d_rstd)
 #define NO_NORM(T, Y)                                              \
     do {                                                           \
@@ -286,6 +292,7 @@ extern "C" int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride
         else if (units <= 32) NO_NORM_AS(T, Y, 32, 256, 1);        \
         else if (units <= 64) NO_NORM_AS(T, Y, 64, 256, 1);        \
         else if (units <= 128) NO_NORM_AS(T, Y, 64, 256, 2);       \
+        else if (units <= 192) NO_NORM_AS(T, Y, 64, 256, 3);       \
         else if (units <= 256) NO_NORM_AS(T, Y, 64, 256, 4);       \
         else if (units <= 512) NO_NORM_AS(T, Y, 256, 256, 2);      \
         else if (units <= 1024) NO_NORM_AS(T, Y, 256, 256, 4);     \
@@ -339,6 +346,7 @@ extern "C" int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride
         else if (units <= 32) NO_NORM_AS(T, 32, 256, 1);                                                                                             \
         else if (units <= 64) NO_NORM_AS(T, 64, 256, 1);                                                                                             \
         else if (units <= 128) NO_NORM_AS(T, 64, 256, 2);                                                                                            \
+        else if (units <= 192) NO_NORM_AS(T, 64, 256, 3);                                                                                            \
         else if (units <= 256) NO_NORM_AS(T, 64, 256, 4);                                                                                            \
         else if (units <= 512) NO_NORM_AS(T, 256, 256, 2);                                                                                           \
         else if (units <= 1024) NO_NORM_AS(T, 256, 256, 4);                                                                                          \
@@ -359,6 +367,6 @@ extern "C" int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride
 #undef NO_NORM
 #undef NO_NORM_AS
     if (d_grad_weight && !(direct && n_parts == 1))
-        hipLaunchKernelGGL(rmsnorm_join_kernel, dim3((unsigned)ceil_div(dim, 64)), dim3(1024), 0, st, parts, (int32_t)n_parts, dim, d_grad_weight);
+        hipLaunchKernelGGL(rmsnorm_join_kernel, dim3((unsigned)ceil_div(dim, 16)), dim3(1024), 0, st, parts, (int32_t)n_parts, dim, d_grad_weight);
     return launch_status(who);
 }

@@ -3,6 +3,8 @@
 #pragma once
 #include "primitives.hpp"
 
+#include <type_traits>
+
 namespace no {
 
 typedef __bf16 bf16_t;
@@ -71,6 +73,21 @@ struct Run {
         }
         __builtin_memcpy(v, w, BYTES);
     }
+    // The same from the W values that end at p + here, one request, shifted into place: for rows of W values and more.
+    __device__ __forceinline__ void load_to_end(const T* p, int here, T fill) {
+        load(p + here - W);
+        uint32_t w[WORDS];
+        __builtin_memcpy(w, v, BYTES);
+#pragma unroll 1
+        for (int i = here; i < W; ++i) {
+#pragma unroll
+            for (int j = 0; j < WORDS; ++j) {
+                const uint32_t up = j + 1 < WORDS ? w[j + 1 < WORDS ? j + 1 : 0] : bits(fill);
+                w[j] = BITS == 32 ? up : w[j] >> (BITS & 31) | up << (32 - BITS & 31);
+            }
+        }
+        __builtin_memcpy(v, w, BYTES);
+    }
     __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
         for (int i = 0; i < N; ++i) reinterpret_cast<raw*>(p)[i] = v[i];
@@ -136,6 +153,14 @@ struct Run {
     }
 };
 
+// p + c for a row's address, the same in all lanes, and a place in it: 32 bits of offset, which a request takes beside a scalar address (as 64-bit
+// addresses the places of all of a lane's runs would be kept in registers).
+template <typename T>
+__device__ __forceinline__ T* offset(T* p, int32_t c) {
+    typedef typename std::conditional<std::is_const<T>::value, const char, char>::type byte;
+    return reinterpret_cast<T*>(reinterpret_cast<byte*>(p) + (uint32_t)c * (uint32_t)sizeof(T));
+}
+
 // A row (or a piece of one) of `len` values in the registers of TEAM lanes: run u of lane t covers values [(t + u TEAM) W, + W).
 template <typename T, int W, int U, int TEAM>
 struct RowRegs {
@@ -143,7 +168,7 @@ struct RowRegs {
     __device__ __forceinline__ static int32_t at(int t, int u) { return (t + u * TEAM) * W; }
     // run u, if all of it is there (else `fill`)
     __device__ __forceinline__ void load_run(const T* p, int32_t len, int t, int u, T fill) {
-        if (at(t, u) + W <= len) v[u].load(p + u * TEAM * W + t * W);
+        if (at(t, u) + W <= len) v[u].load(offset(p, at(t, u)));
         else v[u].load(p, 0, fill);
     }
     // the run that the row ends in, by the lane that has it
@@ -152,7 +177,8 @@ struct RowRegs {
         const int32_t c = len / W * W;
         if (len / W % TEAM != t) return;
         Run<T, W> r;
-        r.load(p + c, len - c, fill);
+        if (c > 0) r.load_to_end(p + c, len - c, fill);
+        else r.load(p, len, fill);
 #pragma unroll
         for (int u = 0; u < U; ++u) if (c == at(t, u)) v[u] = r;
     }
@@ -179,7 +205,7 @@ struct RowStore {
     Run<T, W> last;
     __device__ __forceinline__ RowStore(T* p_, int32_t len_) : p(p_), len(len_) {}
     __device__ __forceinline__ void put(int32_t c, const Run<T, W>& r) {
-        if (c + W <= len) r.store(p + c);
+        if (c + W <= len) r.store(offset(p, c));
         else if (c < len) { last = r; end = c; }
     }
     __device__ __forceinline__ void finish() { if (end >= 0) last.store(p + end, len - end); }
