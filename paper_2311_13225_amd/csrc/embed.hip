@@ -58,7 +58,7 @@ static void launch_embed(const RowsOf& table, int64_t n_rows, int32_t dim, const
 // ------------------------------------------------------------------------------------------------------- gradient
 //
 // G[v] = scale * sum over the positions i with ids[i] == v of g[i]. The positions are ordered by id (stable, so by position within an id); then the
-// ordered list is cut into chunks of 8 or 32 positions whatever the ids are, and a lane group walks a chunk with the sum of the id at hand
+// ordered list is cut into chunks of 8 to 64 positions whatever the ids are, and a lane group walks a chunk with the sum of the id at hand
 // in registers: an id that is named a thousand times costs what a thousand rare ones do. Sums of ids that lie inside a chunk go
 // straight to the table; those that reach over a chunk's border go to the workspace and are added up, in chunk order, by a second launch. Rows that no
 // id names are found by a search in the ordered ids and cleared beside the sums. No atomics: the same ids give the same bits.
@@ -72,7 +72,11 @@ struct EmbedPlan {      // the workspace, cut up
     int32_t chunk;
     bool merged, radix;
     size_t keys, pos, keys_tmp, pos_tmp, rank, sort_ws, parts, total;
-    EmbedPlan(int32_t n_, int32_t dim) : n(n_), tiles(ceil_div(n_, EMBED_TILE)), chunk(n_ <= 16384 ? 8 : 32) {
+    EmbedPlan(int32_t n_, int32_t dim) : n(n_), tiles(ceil_div(n_, EMBED_TILE)), chunk(64) {
+        // Long chunks leave few sums to join (65536 positions of 2048 columns: chunks of 32 and 2047 borders 26 us, of 64 half of it), as long as
+        // there are wavefronts for the whole chip, sixteen to a compute unit.
+        const int64_t units = ceil_div(dim, 8), lanes = (int64_t)1 << ilog2_ceil((uint64_t)(units < 64 ? units : 64));
+        while (chunk > 8 && n * ceil_div(units, 64) * lanes / 64 / chunk < 4096) chunk >>= 1;
         chunks = ceil_div(n, chunk);
         radix = n > EMBED_MERGE_MOST;
         merged = !radix && n > EMBED_RANK_MOST;
@@ -127,7 +131,10 @@ __global__ void __launch_bounds__(1024) embed_tile_kernel(const int32_t* __restr
     if (here <= 0) return;
     K x = t < here ? (K)min((uint32_t)ids[base + t], n_rows) << 10 | (K)t : ~(K)0;
     int turn = 0;
+    // (written out: with the distances as constants a step is half of the instructions, which sixteen wavefronts on one compute unit pay for)
+#pragma unroll
     for (int k = 2; k <= EMBED_TILE; k <<= 1)
+#pragma unroll
         for (int j = k >> 1; j > 0; j >>= 1) {
             K o;
             if (j >= 64) {              // (the other half of `held` was read before the barrier of the step between)
@@ -137,7 +144,8 @@ __global__ void __launch_bounds__(1024) embed_tile_kernel(const int32_t* __restr
                 turn ^= 1;
             } else if constexpr (sizeof(K) == 4) o = (K)__shfl_xor((int)x, j, 64);
             else o = (K)__shfl_xor((unsigned long long)x, j, 64);
-            x = (o < x) == (((t & k) == 0) == ((t & j) == 0)) ? o : x;
+            const K small = o < x ? o : x, large = o < x ? x : o;
+            x = ((t & k) == 0) == ((t & j) == 0) ? small : large;
         }
     const bool there = t < here;
     keys[base + t] = there ? (uint32_t)(x >> 10) : ~0u;

@@ -223,8 +223,10 @@ __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_
     }
     store.finish();
     team.sync();
+    // (in a block of sixteen wavefronts by the third and those after it: the first two have the next row's entries and the loss to make)
     if (live)
-        for (int j = t; j < a.k; j += TEAM) {
+        for (int j = TEAM == 1024 ? t - 128 : t; j < a.k; j += TEAM) {
+            if (j < 0) break;
             const int32_t at = te.id[j] - first;
             if (te.id[j] >= 0 && at >= 0 && at < len) {
                 float share = 0.0f;
@@ -284,26 +286,27 @@ __global__ void __launch_bounds__(1024) distill_rows_kernel(Distill a) {
     if (first_wave) {
         e.load(a, i);
         e.load_logits(a.z.row<T>(i), a.classes, 0, a.classes);
+        e.shares(a, teachers[0]);
     }
     for (int turn = 0; i < n; turn ^= 1) {
-        Teacher& te = teachers[turn];
+        const Teacher& te = teachers[turn];
         asm volatile("" : "+v"(t));                 // (what follows from it is made anew in each row, not kept in registers over all of them)
         const int64_t next = i + gridDim.x;
         const T* const next_row = a.z.row<T>(next < n ? next : i);
         const int32_t next_len = next < n ? a.classes : 0;
         const float w = a.weight ? a.weight[i] : 1.0f;
-        if (first_wave) e.shares(a, te);
         v.renew();
         const Sums r = team_sums<false>(v.template lane_sums<false>(a.c), a.c, team);
         v.renew();
-        if (first_wave) distill_loss(a, i, r, w, te);
+        if (threadIdx.x >= 64 && threadIdx.x < 128) distill_loss(a, i, r, w, te);
         distill_grad(a, i, 0, a.classes, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [&](int u) {
             v.load_run(next_row, next_len, t, u, from_f32<T>(-INFINITY));
         });
         v.load_end(next_row, next_len, t, from_f32<T>(-INFINITY));
-        if (first_wave && next < n) {
+        if (first_wave && next < n) {       // (into the other of the two: the last reads of it stand before this row's sums)
             e.load(a, next);
             e.load_logits(next_row, a.classes, 0, a.classes);
+            e.shares(a, teachers[turn ^ 1]);
         }
         i = next;
     }
@@ -385,7 +388,7 @@ struct TopSpace {
     static constexpr int CAP = 512;         // candidates that are ranked against each other
     uint64_t key[CAP];
     int32_t count;
-    uint32_t alone[TEAM / 64], shared[TEAM / 64];
+    uint32_t bound[TEAM / 64];
 };
 
 // The k largest values of a piece, as order keys in `to.key[0 .. min(count, CAP))`, in no order, with others that are smaller among them perhaps: all that reach a bound which
@@ -398,79 +401,47 @@ __device__ __forceinline__ void top_candidates(Piece<T, U, TEAM>& v, float lane_
     constexpr int W = Piece<T, U, TEAM>::W;
     const int t = team.lane();
     const int32_t base = first + t * W;     // class of a lane's first value; those of run u follow at u TEAM W (classes written out would be kept in registers)
-    // The values that `in` takes go to the list. Which runs hold any is found first; then a loop takes those runs, one or two in the lanes that
-    // have any (written out over all of a lane's runs it takes three times the registers).
+    // the values that `in` takes go to the list
     auto collect = [&](auto in) {
-        uint32_t runs = 0;
         v.renew();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float f[W];
             v.v[u].get(f);
-            bool any = false;
-#pragma unroll
-            for (int w = 0; w < W; ++w) any |= in(f[w], u * TEAM * W + w);
-            runs |= any ? 1u << u : 0u;
-        }
-#pragma unroll 1
-        while (runs) {
-            const int at_u = __builtin_ctz(runs);
-            runs &= runs - 1;
-            uint32_t word[4];
-            __builtin_memcpy(word, &v.v[0], 16);
-#pragma unroll
-            for (int u = 1; u < U; ++u) {       // (selected word by word: taken as a whole, the runs would go through memory)
-                uint32_t other[4];
-                __builtin_memcpy(other, &v.v[u], 16);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    asm volatile("" : "+v"(other[j]));
-                    word[j] = u == at_u ? other[j] : word[j];
-                }
-            }
-            Run<T, W> r;
-            __builtin_memcpy(&r, word, 16);
-            float f[W];
-            r.get(f);
-            const int32_t k0 = at_u * TEAM * W;
-            int32_t mine = 0;
-#pragma unroll
-            for (int w = 0; w < W; ++w) mine += in(f[w], k0 + w);
-            int32_t at = atomicAdd(&to.count, mine);
 #pragma unroll
             for (int w = 0; w < W; ++w)
-                if (in(f[w], k0 + w)) {
-                    if (at < TopSpace<TEAM>::CAP) to.key[at] = order_key(f[w], base + k0 + w);
-                    ++at;
+                if (in(f[w], u * TEAM * W + w)) {
+                    const int32_t at = atomicAdd(&to.count, 1);
+                    if (at < TopSpace<TEAM>::CAP) to.key[at] = order_key(f[w], base + u * TEAM * W + w);
                 }
         }
     };
-    // bounds of the wavefront, their upper 16 bits (so a little less than they are), bit by bit
+    // the `need`-th largest lane maximum of the wavefront, its upper 16 bits (so a little less than it is), bit by bit
+    const uint32_t o = order_of(lane_max), lowest = order_of(-3.4028234663852886e38f);
+    auto largest = [&](int need) {
+        uint32_t most = 0;
+        for (int b = 31; b >= 16; --b)
+            if (__popcll(__ballot(o >= (most | 1u << b))) >= need) most |= 1u << b;
+        return most;
+    };
     constexpr int WAVES = TEAM / 64;
-    const int need = (k + WAVES - 1) / WAVES;
-    const uint32_t o = order_of(lane_max);
-    uint32_t alone = 0, shared = 0;
-    for (int b = 31; b >= 16; --b) {
-        if (__popcll(__ballot(o >= (alone | 1u << b))) >= k) alone |= 1u << b;
-        if (WAVES > 1 && __popcll(__ballot(o >= (shared | 1u << b))) >= need) shared |= 1u << b;
-    }
-    if constexpr (WAVES > 1) {
-        if (lane_id() == 0) {
-            to.alone[threadIdx.x >> 6] = alone;
-            to.shared[threadIdx.x >> 6] = shared;
-        }
-    }
+    uint32_t most = largest((k + WAVES - 1) / WAVES);
     if (t == 0) to.count = 0;
-    team.sync();
     if constexpr (WAVES > 1) {
+        if (lane_id() == 0) to.bound[threadIdx.x >> 6] = most;
+        team.sync();
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            shared = min(shared, to.shared[w]);
-            alone = max(alone, to.alone[w]);
+        for (int w = 0; w < WAVES; ++w) most = min(most, to.bound[w]);
+        if (most < lowest) {            // a wavefront with next to nothing: each by itself
+            team.sync();
+            most = largest(k);
+            if (lane_id() == 0) to.bound[threadIdx.x >> 6] = most;
+            team.sync();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) most = max(most, to.bound[w]);
         }
-        alone = max(alone, shared);
-    }
-    const float bound = alone <= order_of(-3.4028234663852886e38f) ? -3.4028234663852886e38f : value_of(alone);       // (-inf is no candidate)
+    } else team.sync();
+    const float bound = value_of(max(most, lowest));       // (-inf is no candidate)
     if (lane_max >= bound) collect([&](float f, int32_t) { return f >= bound; });
     team.sync();
     if (to.count <= TopSpace<TEAM>::CAP) return;
@@ -590,50 +561,52 @@ __global__ void __launch_bounds__(THREADS, U == 8 ? 5 : U == 4 ? 7 : 8) logprobs
 // that do, so the r-th largest of those keys is a bound; the keys that reach it are ranked against each other. (With more lists than lanes a lane
 // takes the largest of several lists' first keys.) Where large values stand in few pieces more keys than there is room for may reach the bound: then
 // every key is ranked by a search in every other list.
-template <typename T>
+template <typename T, int TEAM>
 __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
-    constexpr int CAP = 1024;
+    constexpr int CAP = TEAM * 4, ROWS = 256 / TEAM;
     __shared__ float smem[8];
-    __shared__ uint64_t lane_key[256], cand[CAP], bound;
-    __shared__ int32_t count;
-    Team<256, 256> team(smem);
-    const int64_t i = a.row0 + blockIdx.x;
+    __shared__ uint64_t lane_key[256], cands[ROWS][CAP], bounds[ROWS];
+    __shared__ int32_t counts[ROWS];
+    Team<TEAM, 256> team(smem);
+    const int64_t i = a.row0 + (int64_t)blockIdx.x * ROWS + team.index();
     if (i >= rows_here(a.d_n, a.cap)) return;
-    const int32_t t = threadIdx.x, all = a.pieces * a.k;
+    const int32_t t = team.lane(), all = a.pieces * a.k;
     const uint64_t* const keys = a.keys + i * all;
+    uint64_t *const first = lane_key + team.index() * TEAM, *const cand = cands[team.index()], &bound = bounds[team.index()];
+    int32_t& count = counts[team.index()];
     if (a.k > 0) {
-        const int32_t j = (a.k + a.pieces - 1) / a.pieces, need = (a.k + j - 1) / j, lanes = min(a.pieces, 256);
+        const int32_t j = (a.k + a.pieces - 1) / a.pieces, need = (a.k + j - 1) / j, lanes = min(a.pieces, TEAM);
         uint64_t mine = 0;
-        for (int32_t p = t; p < a.pieces; p += 256) mine = max(mine, keys[p * a.k + j - 1]);
-        lane_key[t] = mine;
+        for (int32_t p = t; p < a.pieces; p += TEAM) mine = max(mine, keys[p * a.k + j - 1]);
+        first[t] = mine;
         if (t == 0) { bound = 1; count = 0; }
-        __syncthreads();
+        team.sync();
         int32_t rank = 0;
-        for (int32_t o = 0; o < lanes; ++o) rank += lane_key[o] > mine;
+        for (int32_t o = 0; o < lanes; ++o) rank += first[o] > mine;
         if (rank == need - 1 && mine != 0) bound = mine;        // (keys are all different; fewer than `need` above 0: all of them)
     }
     const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);
     const float log_s = log2f(r.s);
     if (t == 0) store_row<T>(a, i, r, log_s);
     if (a.k == 0) return;
-    __syncthreads();
-    for (int32_t e = t; e < all; e += 256) {
+    team.sync();
+    for (int32_t e = t; e < all; e += TEAM) {
         const uint64_t key = keys[e];
         if (key >= bound) {
             const int32_t at = atomicAdd(&count, 1);
             if (at < CAP) cand[at] = key;
         }
     }
-    __syncthreads();
+    team.sync();
     if (count <= CAP) {
-        for (int32_t e = t; e < count; e += 256) {
+        for (int32_t e = t; e < count; e += TEAM) {
             const uint64_t key = cand[e];
             int32_t rank = 0;
             for (int32_t o = 0; o < count; ++o) rank += cand[o] > key;
             if (rank < a.k) store_top(a, i, rank, key, r, log_s);
         }
     } else {
-        for (int32_t e = t; e < all; e += 256) {
+        for (int32_t e = t; e < all; e += TEAM) {
             const uint64_t key = keys[e];
             if (key < bound) continue;
             const int32_t own = e / a.k;
@@ -651,7 +624,7 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
             if (rank < a.k) store_top(a, i, rank, key, r, log_s);
         }
     }
-    for (int32_t e = count + t; e < a.k; e += 256) store_top(a, i, e, 0, r, log_s);
+    for (int32_t e = count + t; e < a.k; e += TEAM) store_top(a, i, e, 0, r, log_s);
 }
 
 template <typename T, int TEAM, int U>
@@ -690,7 +663,8 @@ static int32_t check_logits(const char* who, const void* z, no_dtype dt, int64_t
     NO_REQUIRE(dt == NO_F32 || dt == NO_BF16, NO_ERR_INVALID_ARG, "%s: logits are NO_F32 or NO_BF16", who);
     NO_REQUIRE(n >= 0 && classes >= 1, NO_ERR_INVALID_ARG, "%s: bad sizes", who);
     NO_REQUIRE(classes <= NO_MAX_CLASSES, NO_ERR_UNSUPPORTED, "%s: more than %d classes", who, NO_MAX_CLASSES);
-    NO_REQUIRE(temperature > 0.0f && temperature < INFINITY, NO_ERR_INVALID_ARG, "%s: the temperature must be positive and finite", who);
+    NO_REQUIRE(temperature > 0.0f && temperature < INFINITY && LOG2E / temperature < INFINITY, NO_ERR_INVALID_ARG,
+               "%s: the temperature must be positive and finite, and so must its inverse", who);
     return check_rows(who, "z", z, dt, n, classes, stride);
 }
 
@@ -824,7 +798,9 @@ static int32_t logprobs(const char* who, Logprobs a, void* ws, hipStream_t st) {
             else if (cut.u == 4) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 4, true>), grid, dim3(256), 0, st, a);
             else if (cut.u == 2) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 2, true>), grid, dim3(256), 0, st, a);
             else hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 1, true>), grid, dim3(256), 0, st, a);
-            hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)rows), dim3(256), 0, st, a);
+            // many rows of few pieces: a wavefront each, without barriers
+            if (rows >= 256 && a.pieces <= 64) hipLaunchKernelGGL((logprobs_join_kernel<T, 64>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((logprobs_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, a);
         });
     }
     return launch_status(who);

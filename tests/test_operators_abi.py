@@ -61,7 +61,7 @@ def test_distill_refusals(lib):
     rows = [P, 0, 32, None, 4, 8, P, P, 2, 1.0, None]
     common = [({0: None}, INVALID), ({1: 2}, INVALID), ({2: 28}, INVALID), ({2: 33}, INVALID), ({4: -1}, INVALID), ({5: 0}, INVALID), ({5: (1 << 22) + 1, 2: 1 << 25}, UNSUPPORTED),
               ({6: None}, INVALID), ({7: None}, INVALID), ({8: 0}, INVALID), ({8: 257}, UNSUPPORTED), ({9: 0.0}, INVALID), ({9: -1.0}, INVALID),
-              ({9: float("nan")}, INVALID), ({9: float("inf")}, INVALID), ({0: ODD}, INVALID)]
+              ({9: float("nan")}, INVALID), ({9: float("inf")}, INVALID), ({9: 1e-39}, INVALID), ({0: ODD}, INVALID)]
     swept(lib.no_distill_fwd, rows + [P, P, P, 1 << 30, None], common + [({11: None}, INVALID), ({12: None}, INVALID), ({13: None}, INVALID), ({14: 1}, CAPACITY)])
     swept(lib.no_distill_bwd, rows + [P, P, 32, None], common + [({11: None}, INVALID), ({12: None}, INVALID), ({13: 16}, INVALID)])
     swept(lib.no_distill_fwd_bwd, rows + [P, P, P, 32, P, 1 << 30, None], common + [({11: None}, INVALID), ({13: None}, INVALID), ({14: 16}, INVALID), ({15: None}, INVALID), ({15: ODD}, INVALID), ({16: 1}, CAPACITY)])
