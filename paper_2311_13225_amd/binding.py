@@ -455,24 +455,33 @@ def no_gcn_layer_bwd(blk: no_block_view, agg: torch.Tensor, h: torch.Tensor, gra
 
 NO_MAX_EMBED_DIM, NO_MAX_NORM_DIM, NO_MAX_CLASSES, NO_MAX_TEACHER, NO_MAX_ALTERNATIVES = 1 << 20, 65536, 1 << 22, 256, 64
 _OP_DTYPES = {torch.float32: NO_F32, torch.bfloat16: NO_BF16, torch.float8_e4m3fn: NO_E4M3}
+_OP_SIZES = {torch.float32: 4, torch.bfloat16: 2, torch.float8_e4m3fn: 1}
+# These calls take a few microseconds on the device, so their checks ask a tensor for as little as they can.
 
 
 def _stream_of(stream) -> int:
-    """_stream for calls of a few microseconds: the current stream's address without the object around it."""
+    """_stream, with the current stream's address asked for without the object around it."""
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return _stream(stream)
+
+
+def _code(t: torch.Tensor) -> int:
+    return _OP_DTYPES.get(t.dtype, -1)      # (another type is the library's to refuse)
 
 
 def _rows(t: Optional[torch.Tensor], n: int, dim: int, dtype: Optional[torch.dtype] = None):
     """(address, stride in bytes) of a row matrix [n, dim] whose rows are dense; (None, 0) of None."""
     if t is None:
         return None, 0
-    assert t.is_cuda and t.dim() == 2 and t.shape[0] == n and t.shape[1] == dim, "a CUDA tensor [%d, %d] is needed, got %s" % (n, dim, tuple(t.shape))
-    assert t.stride(1) == 1 or dim == 1, "rows must be dense"
-    assert dtype is None or t.dtype == dtype, "%s is needed, got %s" % (dtype, t.dtype)
-    es = t.element_size()
-    return t.data_ptr(), t.stride(0) * es if n > 1 else max(t.stride(0), dim) * es     # (a single row's stride says nothing)
+    dt = t.dtype
+    assert t.is_cuda and t.shape == (n, dim), "a CUDA tensor [%d, %d] is needed, got %s" % (n, dim, tuple(t.shape))
+    assert dtype is None or dt == dtype, "%s is needed, got %s" % (dtype, dt)
+    row, one = t.stride()
+    assert one == 1 or dim == 1, "rows must be dense"
+    if n < 2 and row < dim:
+        row = dim                           # (a single row's stride says nothing)
+    return t.data_ptr(), row * (_OP_SIZES.get(dt) or t.element_size())
 
 
 def _vec(t: Optional[torch.Tensor], n: int, dtype: torch.dtype = torch.float32) -> Optional[int]:
@@ -484,12 +493,12 @@ def _vec(t: Optional[torch.Tensor], n: int, dtype: torch.dtype = torch.float32) 
 
 
 def _count(n: Optional[torch.Tensor]) -> Optional[int]:
-    return _vec(n, 1, torch.int32)
+    return None if n is None else _vec(n, 1, torch.int32)
 
 
 def _ws(ws: torch.Tensor):
     assert ws.is_cuda and ws.is_contiguous()
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
 
 
 def no_embed_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
@@ -499,8 +508,8 @@ def no_embed_fwd(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scal
     v, dim = table.shape
     n = ids.numel()
     (pt, st), (po, so) = _rows(table, v, dim), _rows(out, n, dim)
-    _check(lib().no_embed_fwd(pt, _OP_DTYPES.get(table.dtype, -1), v, dim, st, _vec(row_scale, v), _vec(ids, n, torch.int32),
-                              _count(n_ids), n, scale, po, _OP_DTYPES.get(out.dtype, -1), so, _stream_of(stream)))
+    _check(lib().no_embed_fwd(pt, _code(table), v, dim, st, _vec(row_scale, v), _vec(ids, n, torch.int32),
+                              _count(n_ids), n, scale, po, _code(out), so, _stream_of(stream)))
     return out
 
 
@@ -514,7 +523,7 @@ def no_embed_bwd(grad_out: torch.Tensor, ids: torch.Tensor, grad_table: torch.Te
     v, dim = grad_table.shape
     n = ids.numel()
     (pg, sg), (pt, st), (pw, bw) = _rows(grad_out, n, dim), _rows(grad_table, v, dim, torch.float32), _ws(ws)
-    _check(lib().no_embed_bwd(pg, _OP_DTYPES.get(grad_out.dtype, -1), sg, _vec(ids, n, torch.int32), _count(n_ids), n, scale,
+    _check(lib().no_embed_bwd(pg, _code(grad_out), sg, _vec(ids, n, torch.int32), _count(n_ids), n, scale,
                               1 if accumulate else 0, pt, v, dim, st, pw, bw, _stream_of(stream)))
     return grad_table
 
@@ -527,8 +536,8 @@ def no_rmsnorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float, 
     float8_e4m3fn with the rows' scales in row_scale."""
     n, dim = x.shape
     (px, sx), (pr, sr), (ps, ss), (py, sy) = _rows(x, n, dim), _rows(residual, n, dim, x.dtype), _rows(sum_out, n, dim, x.dtype), _rows(y, n, dim)
-    _check(lib().no_rmsnorm_fwd(px, _OP_DTYPES.get(x.dtype, -1), sx, pr, sr, _vec(weight, dim), eps, _count(n_rows), n, dim, ps, ss,
-                                py, _OP_DTYPES.get(y.dtype, -1), sy, _vec(row_scale, n), _vec(rstd, n), _stream_of(stream)))
+    _check(lib().no_rmsnorm_fwd(px, _code(x), sx, pr, sr, _vec(weight, dim), eps, _count(n_rows), n, dim, ps, ss,
+                                py, _code(y), sy, _vec(row_scale, n), _vec(rstd, n), _stream_of(stream)))
     return y
 
 
@@ -543,7 +552,7 @@ def no_rmsnorm_bwd(s: torch.Tensor, weight: Optional[torch.Tensor], rstd: torch.
     n, dim = s.shape
     (ps, ss), (pg, sg), (pa, sa) = _rows(s, n, dim), _rows(grad_y, n, dim, s.dtype), _rows(grad_sum, n, dim, s.dtype)
     (px, sx), (pw, bw) = _rows(grad_x, n, dim, s.dtype), _ws(ws)
-    _check(lib().no_rmsnorm_bwd(ps, _OP_DTYPES.get(s.dtype, -1), ss, _vec(weight, dim), _vec(rstd, n), pg, sg, pa, sa, _count(n_rows), n,
+    _check(lib().no_rmsnorm_bwd(ps, _code(s), ss, _vec(weight, dim), _vec(rstd, n), pg, sg, pa, sa, _count(n_rows), n,
                                 dim, px, sx, _vec(grad_weight, dim), pw, bw, _stream_of(stream)))
 
 
@@ -552,7 +561,7 @@ def _teacher(z: torch.Tensor, ids: torch.Tensor, logits: torch.Tensor, row_weigh
     k = ids.shape[1]
     assert ids.shape == logits.shape and ids.shape[0] == n
     pz, sz = _rows(z, n, c)
-    return (pz, _OP_DTYPES.get(z.dtype, -1), sz, _count(n_rows), n, c, _vec(ids, n * k, torch.int32), _vec(logits, n * k), k), _vec(row_weight, n)
+    return (pz, _code(z), sz, _count(n_rows), n, c, _vec(ids, n * k, torch.int32), _vec(logits, n * k), k), _vec(row_weight, n)
 
 
 def no_distill_ws_bytes(n_rows_cap: int, n_classes: int) -> int:
@@ -595,7 +604,7 @@ def no_logprobs_fwd(z: torch.Tensor, tokens: torch.Tensor, temperature: float, l
     k = 0 if top_ids is None else top_ids.shape[1]
     assert (top_ids is None) == (top_logprobs is None) and (top_ids is None or tuple(top_ids.shape) == tuple(top_logprobs.shape) == (n, k))
     pz, sz = _rows(z, n, c)
-    _check(lib().no_logprobs_fwd(pz, _OP_DTYPES.get(z.dtype, -1), sz, _count(n_rows), n, c, _vec(tokens, n, torch.int32), temperature,
+    _check(lib().no_logprobs_fwd(pz, _code(z), sz, _count(n_rows), n, c, _vec(tokens, n, torch.int32), temperature,
                                  _vec(logprob, n), _vec(entropy, n), _vec(lse, n), k, _vec(top_ids, n * k, torch.int32),
                                  _vec(top_logprobs, n * k), *_ws(ws), _stream_of(stream)))
 
@@ -606,7 +615,7 @@ def no_logprobs_bwd(z: torch.Tensor, tokens: torch.Tensor, temperature: float, l
     """Gradient of the log probabilities and entropies with respect to the logits."""
     n, c = z.shape
     (pz, sz), (pg, sg) = _rows(z, n, c), _rows(grad_z, n, c, z.dtype)
-    _check(lib().no_logprobs_bwd(pz, _OP_DTYPES.get(z.dtype, -1), sz, _count(n_rows), n, c, _vec(tokens, n, torch.int32), temperature,
+    _check(lib().no_logprobs_bwd(pz, _code(z), sz, _count(n_rows), n, c, _vec(tokens, n, torch.int32), temperature,
                                  _vec(lse, n), _vec(entropy, n), _vec(grad_logprob, n), _vec(grad_entropy, n), pg, sg, _stream_of(stream)))
 
 

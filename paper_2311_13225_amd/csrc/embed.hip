@@ -93,23 +93,35 @@ struct EmbedPlan {      // the workspace, cut up
 };
 
 // The place of a position in the order by id, then by position, is the number of positions before it in that order. n^2 comparisons, but in one
-// launch and from registers: a lane per position, and the sixteen wavefronts of a block share the positions that it is compared with.
+// launch and from registers: a lane per position, and the sixteen wavefronts of a block take the positions it is compared with 64 at a time, which are wholly
+// left of the block's own, its own, or right of them: equal ids count on the left, by lane among its own, and not on the right.
 __global__ void __launch_bounds__(1024) embed_count_kernel(const int32_t* __restrict__ ids, const int32_t* d_n, int32_t cap, uint32_t* keys, uint32_t* pos) {
     __shared__ uint32_t part[16][64];
-    const int32_t n = rows_here(d_n, cap), first = (int32_t)blockIdx.x * 64;
-    if (first >= n) return;
-    const int32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6)), i = first + lane;
+    const int32_t n = rows_here(d_n, cap), own = (int32_t)blockIdx.x;
+    if (own * 64 >= n) return;
+    const int32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6)), i = own * 64 + lane;
     const uint32_t* key = reinterpret_cast<const uint32_t*>(ids);       // ids outside the table are larger than all inside, as unsigned
     const uint32_t mine = i < n ? key[i] : 0u;
-    const int32_t each = (n + 255) / 256 * 16, lo = min(n, wave * each), hi = min(n, lo + each);
     uint32_t before = 0;
-    // equal ids count where they stand earlier: all of those left of this block's positions, none right of it, and among the block's own by lane
-    const int32_t a = min(max(lo, first), hi), b = min(max(lo, first + 64), hi);
-#pragma unroll 16
-    for (int32_t j = lo; j < a; ++j) before += key[j] <= mine;
-    for (int32_t j = a; j < b; ++j) before += key[j] < mine || (key[j] == mine && j < i);
-#pragma unroll 16
-    for (int32_t j = b; j < hi; ++j) before += key[j] < mine;
+    for (int32_t g = wave; g * 64 < n; g += 16) {
+        const uint32_t* const p = key + g * 64;
+        if (g != own && (g + 1) * 64 <= n) {                            // scalar loads: 64 ids in four requests
+            if (g < own) {
+#pragma unroll
+                for (int q = 0; q < 64; ++q) before += p[q] <= mine;
+            } else {
+#pragma unroll
+                for (int q = 0; q < 64; ++q) before += p[q] < mine;
+            }
+        } else {                                                        // its own, or the last ones, behind whose end nothing counts
+            const int32_t here = g * 64 + lane < n ? (int32_t)p[lane] : -1;
+#pragma unroll
+            for (int q = 0; q < 64; ++q) {
+                const uint32_t k = (uint32_t)__builtin_amdgcn_readlane(here, q);
+                before += k < mine || (k == mine && g == own && q < lane);
+            }
+        }
+    }
     part[wave][lane] = before;
     __syncthreads();
     if (wave == 0 && i < n) {
@@ -254,7 +266,7 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
 #pragma unroll
     for (int w = 0; w < W; ++w) acc[w] = 0.0f;
     int32_t start = 0;
-    constexpr int UNR = ADD ? 4 : 8;                // rows requested before the first is added
+    constexpr int UNR = ADD && W == 8 ? 4 : 8;      // rows requested before the first is added
     for (int32_t e = 0; e < len; e += UNR) {
         uint32_t key[UNR + 1], p[UNR];
         Run<T, W> r[UNR];
