@@ -35,7 +35,8 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_
                 for (int w = 0; w < W; ++w) f[w] = there ? f[w] * by : 0.0f;
                 Run<O, W> o;
                 o.set(f);
-                o.store(out.row<O>(r) + c, dim - c);
+                if (c + W <= dim) o.store_once(out.row<O>(r) + c);
+                else o.store(out.row<O>(r) + c, dim - c);
             }
         }
         id = next;
