@@ -23,7 +23,7 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_
 #pragma unroll
             for (int j = 0; j < UNR; ++j) {
                 const int32_t c = (ub + j * g) * W;
-                if (there && c < dim) v[j].load(src + c, dim - c, from_f32<T>(0.0f));
+                if (there && c < dim) v[j].load_at(src, c, dim, from_f32<T>(0.0f));
             }
 #pragma unroll
             for (int j = 0; j < UNR; ++j) {
@@ -64,6 +64,7 @@ static void launch_embed(const RowsOf& table, int64_t n_rows, int32_t dim, const
 // straight to the table; those that reach over a chunk's border go to the workspace and are added up, in chunk order, by a second launch. Rows that no
 // id names are found by a search in the ordered ids and cleared beside the sums. No atomics: the same ids give the same bits.
 
+constexpr int32_t EMBED_FEW = 256;                  // positions that need no order (embed_few_kernel)
 constexpr int EMBED_TILE = 1024;                    // positions that a block orders in LDS
 constexpr int32_t EMBED_RANK_MOST = 8192;           // positions whose places are counted in one launch
 constexpr int32_t EMBED_MERGE_MOST = 131072;        // positions that are ordered by tiles and ranks; more go through the radix sort
@@ -89,7 +90,7 @@ struct EmbedPlan {      // the workspace, cut up
         rank = pos_tmp + (merged || radix ? list : 0);
         sort_ws = rank + (merged ? list : 0);
         parts = sort_ws + (radix ? (size_t)ceil_div((int64_t)radix_ws_bytes(n), 16) * 16 : 0);
-        total = parts + (size_t)chunks * 2 * (size_t)dim * 4 + 16;
+        total = n <= EMBED_FEW ? 16 : parts + (size_t)chunks * 2 * (size_t)dim * 4 + 16;
     }
 };
 
@@ -230,6 +231,87 @@ struct EmbedSums {
     float* parts;       // [chunks][2][dim]: the sum of an id that began in an earlier chunk, and of one that goes on in the next
 };
 
+// Few positions, in one launch and without an order: a wavefront per position and 64 runs of columns looks its id up among all of them; where the position is the id's first it adds
+// the rows of all of its positions, in order. (777 positions take 15 us in three launches; up to 256 the longest run, all positions of one id, still costs no more than that, and
+// 4 us otherwise.)
+// Clears those of the rows [v0, v0 + 16) whose bit is set.
+__device__ __forceinline__ void clear_rows(const EmbedSums& a, int64_t v0, uint32_t empty) {
+    Run<float, 4> zero;
+    const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    zero.set(z);
+    while (empty) {
+        const int32_t at = __builtin_ctz(empty);
+        empty &= empty - 1;
+        float* row = a.table.row<float>(v0 + at);
+        for (int32_t c = lane_id() * 4; c < a.dim; c += 256) zero.store(row + c, a.dim - c);
+    }
+}
+
+template <typename T, int W, bool ADD>
+__global__ void __launch_bounds__(256) embed_few_kernel(EmbedSums a, const int32_t* __restrict__ ids, int32_t col_tiles, uint32_t sum_blocks) {
+    constexpr int Q = EMBED_FEW / 64, UNR = 8;
+    const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6));
+    int32_t id[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) id[q] = lane + q * 64 < n ? ids[lane + q * 64] : -1;
+    for (int64_t v0 = ((int64_t)blockIdx.x - sum_blocks) * 64 + wave * 16; blockIdx.x >= sum_blocks; v0 += ((int64_t)gridDim.x - sum_blocks) * 64) {
+        if (v0 >= a.n_rows) return;
+        uint32_t empty = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            bool named = false;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) named |= id[q] == v0 + r;
+            empty |= v0 + r < a.n_rows && __ballot(named) == 0 ? 1u << r : 0u;
+        }
+        clear_rows(a, v0, empty);
+    }
+    const int32_t item = (int32_t)blockIdx.x * 4 + wave, i = item / col_tiles, col = (item % col_tiles * 64 + lane) * W, width = a.dim - col;
+    if (i >= n) return;
+    const int32_t mine = ids[i];
+    if (mine < 0 || mine >= a.n_rows) return;
+    uint64_t rest[Q];
+    int32_t first = n;
+#pragma unroll
+    for (int q = Q - 1; q >= 0; --q) {
+        rest[q] = __ballot(id[q] == mine);
+        if (rest[q]) first = q * 64 + __builtin_ctzll(rest[q]);
+    }
+    if (first != i || width <= 0) return;
+    float* const to = a.table.row<float>(mine) + col;
+    Run<float, W> out;
+    if (ADD) out.load_at(to - col, col, a.dim, 0.0f);
+    float acc[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) acc[w] = 0.0f;
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+        while (rest[q]) {
+            Run<T, W> r[UNR];
+            int32_t p[UNR];
+#pragma unroll
+            for (int k = 0; k < UNR; ++k) {
+                p[k] = rest[q] ? q * 64 + __builtin_ctzll(rest[q]) : -1;
+                rest[q] &= rest[q] - 1;
+                if (p[k] >= 0) r[k].load_at(a.grad.row<T>(p[k]), col, a.dim, from_f32<T>(0.0f));
+            }
+#pragma unroll
+            for (int k = 0; k < UNR; ++k) {
+                if (p[k] < 0) break;
+                float f[W];
+                r[k].get(f);
+#pragma unroll
+                for (int w = 0; w < W; ++w) acc[w] += f[w];
+            }
+        }
+    float f[W];
+    if (ADD) out.get(f);
+#pragma unroll
+    for (int w = 0; w < W; ++w) f[w] = ADD ? f[w] + a.scale * acc[w] : a.scale * acc[w];
+    out.set(f);
+    out.store(to, width);
+}
+
 template <typename T, int W, bool ADD>
 __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t chunks, int32_t g_log2, int32_t col_tiles, uint32_t sum_blocks) {
     const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id();
@@ -242,16 +324,8 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
             const int32_t mid = lo + ((hi - lo) >> 1);
             if ((int64_t)a.keys[mid] < v) lo = mid + 1; else hi = mid;
         }
-        uint32_t empty = (uint32_t)__ballot(v < a.n_rows && !(lo < n && (int64_t)a.keys[lo] == v)) & 0xffffu;
-        Run<float, 4> zero;
-        const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        zero.set(z);
-        while (empty) {
-            const int32_t at = __builtin_ctz(empty);
-            empty &= empty - 1;
-            float* row = a.table.row<float>(v0 + at);
-            for (int32_t c = lane * 4; c < a.dim; c += 256) zero.store(row + c, a.dim - c);
-        }
+        const uint32_t empty = (uint32_t)__ballot(v < a.n_rows && !(lo < n && (int64_t)a.keys[lo] == v)) & 0xffffu;
+        clear_rows(a, v0, empty);
     }
     const int32_t groups = 64 >> g_log2, u = lane & ((1 << g_log2) - 1);
     const int64_t item = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * groups + (lane >> g_log2);
@@ -281,9 +355,9 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
 #pragma unroll
         for (int k = 0; k < UNR; ++k) {
             if (key[k] >= n_rows) continue;
-            r[k].load(a.grad.row<T>(p[k]) + col, width, from_f32<T>(0.0f));
+            r[k].load_at(a.grad.row<T>(p[k]), col, a.dim, from_f32<T>(0.0f));
             // the row that a run's sum is added to, requested with the run's last gradient
-            if (ADD && key[k + 1] != key[k]) old[ADD ? k : 0].load(a.table.row<float>(key[k]) + col, width, 0.0f);
+            if (ADD && key[k + 1] != key[k]) old[ADD ? k : 0].load_at(a.table.row<float>(key[k]), col, a.dim, 0.0f);
         }
 #pragma unroll
         for (int k = 0; k < UNR; ++k) {
@@ -325,7 +399,7 @@ __global__ void __launch_bounds__(512) embed_join_kernel(EmbedSums a, int64_t ch
 #pragma unroll 8
         for (int64_t p = p0; p < p1; ++p) {
             Run<float, 4> r;
-            r.load(a.parts + ((c + p) * 2 + (p == 0)) * a.dim + col, width, 0.0f);
+            r.load_at(a.parts + ((c + p) * 2 + (p == 0)) * a.dim, col, a.dim, 0.0f);
             float f[4];
             r.get(f);
 #pragma unroll
@@ -337,7 +411,7 @@ __global__ void __launch_bounds__(512) embed_join_kernel(EmbedSums a, int64_t ch
         float* to = a.table.row<float>(key) + col;
         Run<float, 4> out;
         float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (a.accumulate) { out.load(to, width, 0.0f); out.get(f); }
+        if (a.accumulate) { out.load_at(to - col, col, a.dim, 0.0f); out.get(f); }
 #pragma unroll
         for (int w = 0; w < 4; ++w) f[w] += a.scale * sum[w];
         out.set(f);
@@ -390,16 +464,31 @@ __global__ void __launch_bounds__(512) embed_join_kernel(EmbedSums a, int64_t ch
     }
 }
 
+// Blocks that clear rows: 64 rows each, in turn where there are very many.
+static int64_t clear_blocks(const EmbedSums& a) {
+    const int64_t blocks = ceil_div(a.n_rows, 64);
+    return a.accumulate ? 0 : blocks < (1 << 20) ? blocks : 1 << 20;
+}
+
+template <typename T>
+static void launch_few(const EmbedSums& a, const int32_t* ids, hipStream_t st) {
+    constexpr int W = 16 / (int)sizeof(T);
+    const int32_t col_tiles = (int32_t)ceil_div(a.dim, 64 * W);
+    const int64_t sum_blocks = ceil_div((int64_t)a.cap * col_tiles, 4);
+    const dim3 grid((unsigned)(sum_blocks + clear_blocks(a)));
+    if (a.accumulate) hipLaunchKernelGGL((embed_few_kernel<T, W, true>), grid, dim3(256), 0, st, a, ids, col_tiles, (uint32_t)sum_blocks);
+    else hipLaunchKernelGGL((embed_few_kernel<T, W, false>), grid, dim3(256), 0, st, a, ids, col_tiles, (uint32_t)sum_blocks);
+}
+
 template <typename T>
 static void launch_sums(const EmbedSums& a, int64_t chunks, hipStream_t st) {
     constexpr int W = 16 / (int)sizeof(T);
     const int32_t units = (int32_t)ceil_div(a.dim, W), col_tiles = (int32_t)ceil_div(units, 64);
     int g_log2 = 0;
     while ((1 << g_log2) < units && g_log2 < 6) ++g_log2;
-    const int64_t sum_blocks = ceil_div(ceil_div(chunks * col_tiles, 64 >> g_log2), 4), zero_rows = ceil_div(a.n_rows, 64),
-                  zero_blocks = a.accumulate ? 0 : zero_rows < (1 << 20) ? zero_rows : 1 << 20;
-    const dim3 grid((unsigned)(sum_blocks + zero_blocks));
-    if (a.accumulate) { if (sum_blocks) hipLaunchKernelGGL((embed_sums_kernel<T, W, true>), grid, dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks); }
+    const int64_t sum_blocks = ceil_div(ceil_div(chunks * col_tiles, 64 >> g_log2), 4);
+    const dim3 grid((unsigned)(sum_blocks + clear_blocks(a)));
+    if (a.accumulate) hipLaunchKernelGGL((embed_sums_kernel<T, W, true>), grid, dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks);
     else hipLaunchKernelGGL((embed_sums_kernel<T, W, false>), grid, dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks);
 }
 
@@ -449,37 +538,39 @@ extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t gra
     hipStream_t st = (hipStream_t)stream;
     char* ws = (char*)d_ws;
     uint32_t *keys = (uint32_t*)(ws + plan.keys), *pos = (uint32_t*)(ws + plan.pos);
-    if (n_ids_cap > 0) {
-        const unsigned tiles = (unsigned)plan.tiles;
-        if (plan.merged) {
-            uint32_t *k = (uint32_t*)(ws + plan.keys_tmp), *v = (uint32_t*)(ws + plan.pos_tmp), *rank = (uint32_t*)(ws + plan.rank);
-            if (n_rows < (1 << 22)) hipLaunchKernelGGL(embed_tile_kernel<uint32_t>, dim3(tiles), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows, k, v, rank);
-            else hipLaunchKernelGGL(embed_tile_kernel<uint64_t>, dim3(tiles), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows, k, v, rank);
-            // about 512 blocks, two to a compute unit
-            const unsigned groups = (tiles + 3) / 4, wanted = (512 + tiles - 1) / tiles, shares = wanted < groups ? wanted : groups;
-            hipLaunchKernelGGL(embed_rank_kernel, dim3(tiles, shares), dim3(1024), 0, st, k, d_n_ids, n_ids_cap, (int32_t)shares, rank);
-            hipLaunchKernelGGL(embed_place_kernel, dim3(tiles * (EMBED_TILE / 256)), dim3(256), 0, st, k, v, rank, d_n_ids, n_ids_cap, keys, pos);
-        } else if (!plan.radix) {
-            hipLaunchKernelGGL(embed_count_kernel, dim3((unsigned)ceil_div(n_ids_cap, 64)), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, keys, pos);
-        } else {
-            const int bits = ilog2_ceil((uint64_t)n_rows + 1), passes = radix_passes(bits), digit = radix_digit_bits(bits);
-            const RadixPlan radix(n_ids_cap);
-            uint32_t *k[2] = {keys, (uint32_t*)(ws + plan.keys_tmp)}, *v[2] = {pos, (uint32_t*)(ws + plan.pos_tmp)};
-            int to = (passes & 1) ? 0 : 1;          // the last pass ends in the first pair of arrays
-            for (int p = 0; p < passes; ++p, to ^= 1) {
-                const int shift = p * digit, width = bits - shift < digit ? bits - shift : digit;
-                if (p == 0) NO_CHECK(radix_pass(IdSource{d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows}, radix, shift, width, k[to], v[to], ws + plan.sort_ws, st));
-                else NO_CHECK(radix_pass(PairArrays{k[to ^ 1], v[to ^ 1]}, radix, shift, width, k[to], v[to], ws + plan.sort_ws, st));
-            }
-        }
-    }
     const EmbedSums a{keys, pos, d_n_ids, n_ids_cap, scale, accumulate != 0, rows_of(d_grad_out, grad_stride_bytes), rows_of(d_grad_table, table_stride_bytes), n_rows, dim,
                       plan.chunk, (float*)(ws + plan.parts)};
+    if (n_ids_cap <= EMBED_FEW) {
+        if (n_ids_cap == 0 && accumulate) return NO_OK;
+        if (dt == NO_F32) launch_few<float>(a, d_ids, st);
+        else launch_few<bf16_t>(a, d_ids, st);
+        return launch_status(who);
+    }
+    const unsigned tiles = (unsigned)plan.tiles;
+    if (plan.merged) {
+        uint32_t *k = (uint32_t*)(ws + plan.keys_tmp), *v = (uint32_t*)(ws + plan.pos_tmp), *rank = (uint32_t*)(ws + plan.rank);
+        if (n_rows < (1 << 22)) hipLaunchKernelGGL(embed_tile_kernel<uint32_t>, dim3(tiles), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows, k, v, rank);
+        else hipLaunchKernelGGL(embed_tile_kernel<uint64_t>, dim3(tiles), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows, k, v, rank);
+        // about 512 blocks, two to a compute unit
+        const unsigned groups = (tiles + 3) / 4, wanted = (512 + tiles - 1) / tiles, shares = wanted < groups ? wanted : groups;
+        hipLaunchKernelGGL(embed_rank_kernel, dim3(tiles, shares), dim3(1024), 0, st, k, d_n_ids, n_ids_cap, (int32_t)shares, rank);
+        hipLaunchKernelGGL(embed_place_kernel, dim3(tiles * (EMBED_TILE / 256)), dim3(256), 0, st, k, v, rank, d_n_ids, n_ids_cap, keys, pos);
+    } else if (!plan.radix) {
+        hipLaunchKernelGGL(embed_count_kernel, dim3((unsigned)ceil_div(n_ids_cap, 64)), dim3(1024), 0, st, d_ids, d_n_ids, n_ids_cap, keys, pos);
+    } else {
+        const int bits = ilog2_ceil((uint64_t)n_rows + 1), passes = radix_passes(bits), digit = radix_digit_bits(bits);
+        const RadixPlan radix(n_ids_cap);
+        uint32_t *k[2] = {keys, (uint32_t*)(ws + plan.keys_tmp)}, *v[2] = {pos, (uint32_t*)(ws + plan.pos_tmp)};
+        int to = (passes & 1) ? 0 : 1;          // the last pass ends in the first pair of arrays
+        for (int p = 0; p < passes; ++p, to ^= 1) {
+            const int shift = p * digit, width = bits - shift < digit ? bits - shift : digit;
+            if (p == 0) NO_CHECK(radix_pass(IdSource{d_ids, d_n_ids, n_ids_cap, (uint32_t)n_rows}, radix, shift, width, k[to], v[to], ws + plan.sort_ws, st));
+            else NO_CHECK(radix_pass(PairArrays{k[to ^ 1], v[to ^ 1]}, radix, shift, width, k[to], v[to], ws + plan.sort_ws, st));
+        }
+    }
     if (dt == NO_F32) launch_sums<float>(a, plan.chunks, st);
     else launch_sums<bf16_t>(a, plan.chunks, st);
-    if (plan.chunks > 1) {
-        const int64_t eights = ceil_div(plan.chunks - 1, 8);
-        hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(eights < 4096 ? eights : 4096), (unsigned)ceil_div(dim, 256)), dim3(512), 0, st, a, plan.chunks);
-    }
+    const int64_t eights = ceil_div(plan.chunks - 1, 8);
+    hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(eights < 4096 ? eights : 4096), (unsigned)ceil_div(dim, 256)), dim3(512), 0, st, a, plan.chunks);
     return launch_status(who);
 }

@@ -89,11 +89,11 @@ __device__ __forceinline__ Sums join_sums(const Sums* parts, int32_t pieces, flo
 
 // ------------------------------------------------------------------------------------------------------- teacher
 
-// The teacher's entries of a row in LDS: class (-1: left out), share, its logarithm, and the student's logit there. One wavefront makes them, four entries a
-// lane, without a barrier; in blocks of several the others take the row's maximum meanwhile.
+// The teacher's entries of a row in LDS: class (-1: left out), share, its logarithm, the student's logit there, and the class's share over all of its entries. One wavefront
+// makes them, up to four entries a lane, without a barrier; in blocks of several the others take the row's sums meanwhile.
 struct Teacher {
     int32_t id[NO_MAX_TEACHER];
-    float p[NO_MAX_TEACHER], log_p[NO_MAX_TEACHER], z[NO_MAX_TEACHER];
+    float p[NO_MAX_TEACHER], log_p[NO_MAX_TEACHER], z[NO_MAX_TEACHER], whole[NO_MAX_TEACHER];
     int32_t any;        // whether an entry is above -inf
 };
 constexpr int TEACHER_Q = NO_MAX_TEACHER / 64;
@@ -154,12 +154,33 @@ struct Entries {        // a lane's entries as they come from memory
         }
         s = wave.sum(s);
         const float log_s = logf(s);
+        float whole[TEACHER_Q];
+#pragma unroll
+        for (int q = 0; q < TEACHER_Q; ++q) {
+            e[q] = s == 0.0f ? 0.0f : e[q] / s;
+            whole[q] = 0.0f;
+        }
+        if (a.grad.p) {         // each entry in turn to all lanes, in the order of the entries
+#pragma unroll
+            for (int q = 0; q < TEACHER_Q; ++q) {
+                const int here = min(a.k - q * 64, 64);
+                for (int l = 0; l < here; ++l) {
+                    const int32_t c = __builtin_amdgcn_readlane(id[q], l);
+                    const float p = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(e[q]), l));
+                    whole[0] += id[0] == c ? p : 0.0f;
+                    if (a.k > 64)
+#pragma unroll
+                        for (int o = 1; o < TEACHER_Q; ++o) whole[o] += id[o] == c ? p : 0.0f;
+                }
+            }
+        }
 #pragma unroll
         for (int q = 0; q < TEACHER_Q; ++q) {
             const int j = lane_id() + q * 64;
             if (j < a.k) {
                 to.id[j] = id[q];
-                to.p[j] = s == 0.0f ? 0.0f : e[q] / s;
+                to.p[j] = e[q];
+                to.whole[j] = whole[q];
                 to.log_p[j] = (x[q] - from) * a.inv_t - log_s;
                 to.z[j] = z[q];
             }
@@ -229,9 +250,7 @@ __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_
             if (j < 0) break;
             const int32_t at = te.id[j] - first;
             if (te.id[j] >= 0 && at >= 0 && at < len) {
-                float share = 0.0f;
-                for (int o = 0; o < a.k; ++o) share += te.id[o] == te.id[j] ? te.p[o] : 0.0f;
-                out[at] = from_f32<T>(q(te.z[j]) - w * a.temperature * share);
+                out[at] = from_f32<T>(q(te.z[j]) - w * a.temperature * te.whole[j]);
             }
         }
 }
@@ -596,6 +615,7 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
         if (t == 0) { bound = 1; count = 0; }
         team.sync();
         int32_t rank = 0;
+#pragma unroll 8
         for (int32_t o = 0; o < lanes; ++o) rank += first[o] > mine;
         if (rank == need - 1 && mine != 0) bound = mine;        // (keys are all different; fewer than `need` above 0: all of them)
     }
@@ -616,6 +636,7 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
         for (int32_t e = t; e < count; e += TEAM) {
             const uint64_t key = cand[e];
             int32_t rank = 0;
+#pragma unroll 8
             for (int32_t o = 0; o < count; ++o) rank += cand[o] > key;
             if (rank < a.k) store_top(a, i, rank, key, r, log_s);
         }

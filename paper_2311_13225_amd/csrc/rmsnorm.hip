@@ -56,8 +56,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf r
                 if constexpr (KEEP) wk.v[KEEP ? u : 0].get(k);
                 else {
                     Run<float, W> one;
-                    const int32_t c = s.at(t, u);
-                    one.load(weight + min(c, dim), dim - c, 0.0f);
+                    one.load_at(weight, s.at(t, u), dim, 0.0f);
                     one.get(k);
                 }
             }
@@ -335,7 +334,7 @@ extern "C" int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride
     int64_t n_parts = 0;
 #define NO_NORM_AS(T, TEAM, THREADS, U)                                                                                                              \
     do {                                                                                                                                             \
-        n_parts = norm_blocks(n_rows_cap, THREADS / TEAM, NORM_PARTS);                                                                               \
+        n_parts = norm_blocks(n_rows_cap, THREADS / TEAM, THREADS == 1024 ? 256 : NORM_PARTS);                                                       \
         hipLaunchKernelGGL((rmsnorm_bwd_kernel<T, TEAM, THREADS, U>), dim3((unsigned)n_parts), dim3(THREADS), 0, st, s, d_weight, d_rstd, gy, gs, d_n_rows, n_rows_cap, dim, \
                            gx, parts, d_grad_weight);                                                                                                \
     } while (0)

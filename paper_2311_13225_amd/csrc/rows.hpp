@@ -27,8 +27,8 @@ template <> __device__ __forceinline__ e4m3_t from_f32<e4m3_t>(float v) {
     return e4m3_t{(uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, 0.0f, 0, false)};
 }
 
-// Rows that are there: min(*d_n, cap), or cap.
-__device__ __forceinline__ int32_t rows_here(const int32_t* d_n, int32_t cap) { return d_n ? min(*d_n, cap) : cap; }
+// Rows that are there: *d_n within [0, cap], or cap.
+__device__ __forceinline__ int32_t rows_here(const int32_t* d_n, int32_t cap) { return d_n ? min(max(*d_n, 0), cap) : cap; }
 
 // One pointer and stride of a row matrix.
 struct RowsOf {
@@ -61,8 +61,8 @@ struct Run {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const raw*>(p) + i);
     }
-    // The end of a row: a value at a time, in a loop that shifts the run (written out, a branch a value, it costs the kernels more registers than
-    // the rest of them needs).
+    // `here` values and no more, one at a time, in a loop that shifts the run (written out, a branch a value, it costs the kernels more registers than the rest of
+    // them needs). Each waits for memory by itself: for rows shorter than a run.
     __device__ __forceinline__ void load(const T* p, int here, T fill) {
         if (here >= W) return load(p);
         uint32_t w[WORDS], f = bits(fill);
@@ -78,7 +78,8 @@ struct Run {
         }
         __builtin_memcpy(v, w, BYTES);
     }
-    // The same from the W values that end at p + here, one request, shifted into place: for rows of W values and more.
+    // The same from the W values that end at p + here, one request, shifted into place: the end of a row of W values and more. (What it reads of the run before
+    // is shifted out, so that it may be overwritten meanwhile.)
     __device__ __forceinline__ void load_to_end(const T* p, int here, T fill) {
         load(p + here - W);
         uint32_t w[WORDS];
@@ -92,6 +93,12 @@ struct Run {
             }
         }
         __builtin_memcpy(v, w, BYTES);
+    }
+    // values [c, c + W) of a row of `dim`
+    __device__ __forceinline__ void load_at(const T* row, int32_t c, int32_t dim, T fill) {
+        if (c + W <= dim) load(row + c);
+        else if (dim >= W && c < dim) load_to_end(row + c, dim - c, fill);
+        else load(row + (c < dim ? c : 0), dim - c, fill);
     }
     __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
@@ -190,8 +197,7 @@ struct RowRegs {
         const int32_t c = len / W * W;
         if (len / W % TEAM != t) return;
         Run<T, W> r;
-        if (c > 0) r.load_to_end(p + c, len - c, fill);
-        else r.load(p, len, fill);
+        r.load_at(p, c, len, fill);
 #pragma unroll
         for (int u = 0; u < U; ++u) if (c == at(t, u)) v[u] = r;
     }

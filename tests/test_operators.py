@@ -148,7 +148,8 @@ def embed_grad_ref(grad, ids, v, scale):
 @pytest.mark.parametrize("n,v,dim,pad,off,popular", [
     (1, 1, 1, 0, 0, 0.0), (1, 5, 64, 0, 0, 0.0), (2, 3, 100, 1, 1, 1.0), (33, 10, 7, 0, 0, 0.5), (64, 1000, 256, 0, 0, 0.0), (777, 1000, 100, 4, 0, 0.3),
     (1000, 4, 33, 0, 3, 0.2), (4096, 1, 16, 0, 0, 0.0), (4097, 70_000, 130, 2, 1, 0.7), (8193, 300, 64, 0, 0, 0.9), (16_385, 900, 512, 0, 0, 0.5),
-    (40_000, 131_072, 48, 0, 0, 0.4), (100_003, 20_000, 24, 0, 0, 0.95), (300_000, 2, 5, 0, 0, 0.0), (70_000, 100_000, 4, 0, 0, 0.0), (65, 9, 8200, 0, 0, 0.8)])
+    (40_000, 131_072, 48, 0, 0, 0.4), (100_003, 20_000, 24, 0, 0, 0.95), (300_000, 2, 5, 0, 0, 0.0), (70_000, 100_000, 4, 0, 0, 0.0), (65, 9, 8200, 0, 0, 0.8), (256, 40, 300, 0, 0, 1.0), (257, 40, 300, 0, 0, 1.0), (255, 5000, 70, 2, 1, 0.4),
+    (8192, 500, 20, 0, 0, 0.6), (131_073, 5_000_000, 3, 0, 0, 0.5), (20_000, 5_000_000, 3, 0, 0, 0.5)])
 @pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_embed_bwd(n, v, dim, pad, off, popular, dt, accumulate):
@@ -181,13 +182,14 @@ def test_embed_bwd(n, v, dim, pad, off, popular, dt, accumulate):
 
 def test_embed_bwd_counts_and_empty():
     b = nb()
-    for n, here in ((50, 0), (50, 1), (50, 49), (5000, 37), (20_000, 19_999), (70_000, 1000)):
+    for n, here in ((50, 0), (50, 1), (50, 49), (50, -3), (5000, 37), (20_000, 19_999), (70_000, 1000), (140_000, 70_000)):
         g = rng(n)
         grad = randn((n, 20), g)
-        grad[here:] = NAN                                # rows that are not there are not read into anything
+        grad[max(here, 0):] = NAN                                # rows that are not there are not read into anything
         ids = torch.randint(0, 30, (n,), generator=g, device="cuda", dtype=torch.int32)
         table = torch.full((30, 20), MARK, device="cuda")
         b.no_embed_bwd(grad, ids, table, ws_of(b.no_embed_ws_bytes(n, 20)), n_ids=count(here))
+        here = max(here, 0)
         total, size, n_of = embed_grad_ref(grad[:here], ids[:here], 30, 1.0)
         close(table, total, (n_of[:, None] + 3) * U * size)
     table = torch.full((30, 20), MARK, device="cuda")
