@@ -76,9 +76,9 @@ struct EmbedPlan {      // the workspace, cut up
     size_t keys, pos, keys_tmp, pos_tmp, rank, sort_ws, parts, total;
     EmbedPlan(int32_t n_, int32_t dim) : n(n_), tiles(ceil_div(n_, EMBED_TILE)), chunk(64) {
         // Long chunks leave few sums to join (65536 positions of 2048 columns: chunks of 32 and 2047 borders 26 us, of 64 half of it), as long as
-        // there are wavefronts for the whole chip, sixteen to a compute unit.
+        // there are wavefronts for the whole chip, eight to a compute unit with eight rows each on their way.
         const int64_t units = ceil_div(dim, 8), lanes = (int64_t)1 << ilog2_ceil((uint64_t)(units < 64 ? units : 64));
-        while (chunk > 8 && n * ceil_div(units, 64) * lanes / 64 / chunk < 4096) chunk >>= 1;
+        while (chunk > 8 && n * ceil_div(units, 64) * lanes / 64 / chunk < 2048) chunk >>= 1;
         chunks = ceil_div(n, chunk);
         radix = n > EMBED_MERGE_MOST;
         merged = !radix && n > EMBED_RANK_MOST;

@@ -89,11 +89,12 @@ __device__ __forceinline__ Sums join_sums(const Sums* parts, int32_t pieces, flo
 
 // ------------------------------------------------------------------------------------------------------- teacher
 
-// The teacher's entries of a row in LDS: class (-1: left out), share, its logarithm, the student's logit there, and the class's share over all of its entries. One wavefront
-// makes them, up to four entries a lane, without a barrier; in blocks of several the others take the row's sums meanwhile.
+// The teacher's entries of a row in LDS: class (-1: left out) and share side by side, the share's logarithm, and the student's logit there. One wavefront makes them, up to four
+// entries a lane, without a barrier; in blocks of several the others take the row's sums meanwhile.
+struct Entry { int32_t id; float p; };
 struct Teacher {
-    int32_t id[NO_MAX_TEACHER];
-    float p[NO_MAX_TEACHER], log_p[NO_MAX_TEACHER], z[NO_MAX_TEACHER], whole[NO_MAX_TEACHER];
+    Entry of[NO_MAX_TEACHER];
+    float log_p[NO_MAX_TEACHER], z[NO_MAX_TEACHER];
     int32_t any;        // whether an entry is above -inf
 };
 constexpr int TEACHER_Q = NO_MAX_TEACHER / 64;
@@ -154,33 +155,11 @@ struct Entries {        // a lane's entries as they come from memory
         }
         s = wave.sum(s);
         const float log_s = logf(s);
-        float whole[TEACHER_Q];
-#pragma unroll
-        for (int q = 0; q < TEACHER_Q; ++q) {
-            e[q] = s == 0.0f ? 0.0f : e[q] / s;
-            whole[q] = 0.0f;
-        }
-        if (a.grad.p) {         // each entry in turn to all lanes, in the order of the entries
-#pragma unroll
-            for (int q = 0; q < TEACHER_Q; ++q) {
-                const int here = min(a.k - q * 64, 64);
-                for (int l = 0; l < here; ++l) {
-                    const int32_t c = __builtin_amdgcn_readlane(id[q], l);
-                    const float p = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(e[q]), l));
-                    whole[0] += id[0] == c ? p : 0.0f;
-                    if (a.k > 64)
-#pragma unroll
-                        for (int o = 1; o < TEACHER_Q; ++o) whole[o] += id[o] == c ? p : 0.0f;
-                }
-            }
-        }
 #pragma unroll
         for (int q = 0; q < TEACHER_Q; ++q) {
             const int j = lane_id() + q * 64;
             if (j < a.k) {
-                to.id[j] = id[q];
-                to.p[j] = e[q];
-                to.whole[j] = whole[q];
+                to.of[j] = Entry{id[q], s == 0.0f ? 0.0f : e[q] / s};
                 to.log_p[j] = (x[q] - from) * a.inv_t - log_s;
                 to.z[j] = z[q];
             }
@@ -196,7 +175,7 @@ __device__ __forceinline__ void distill_loss(const Distill& a, int64_t i, const 
     if (a.loss) {
         float term = 0.0f;
         for (int j = lane_id(); j < a.k; j += 64)
-            if (te.p[j] != 0.0f) term += te.p[j] * (te.log_p[j] - (r.s == 0.0f ? -INFINITY : (x(te.z[j]) - log_s) * LN2));
+            if (te.of[j].p != 0.0f) term += te.of[j].p * (te.log_p[j] - (r.s == 0.0f ? -INFINITY : (x(te.z[j]) - log_s) * LN2));
         term = Wave(nullptr).sum(term);
         if (lane_id() == 0) a.loss[i] = w == 0.0f || !te.any ? 0.0f : w * a.temperature * a.temperature * term;
     }
@@ -248,10 +227,15 @@ __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_
     if (live)
         for (int j = TEAM == 1024 ? t - 128 : t; j < a.k; j += TEAM) {
             if (j < 0) break;
-            const int32_t at = te.id[j] - first;
-            if (te.id[j] >= 0 && at >= 0 && at < len) {
-                out[at] = from_f32<T>(q(te.z[j]) - w * a.temperature * te.whole[j]);
+            const int32_t id = te.of[j].id, at = id - first;
+            if (id < 0 || at < 0 || at >= len) continue;
+            float share = 0.0f;         // of all entries with this class
+#pragma unroll 8
+            for (int o = 0; o < a.k; ++o) {
+                const Entry other = te.of[o];
+                share += other.id == id ? other.p : 0.0f;
             }
+            out[at] = from_f32<T>(q(te.z[j]) - w * a.temperature * share);
         }
 }
 
@@ -757,8 +741,10 @@ static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
     if (row) {
         if (units <= 64) NO_ROW(64, 256, 1);
         else if (units <= 128) NO_ROW(64, 256, 2);
+        else if (units <= 192) NO_ROW(64, 256, 3);
         else if (units <= 256) NO_ROW(64, 256, 4);
         else if (units <= 512) NO_ROW(256, 256, 2);
+        else if (units <= 768) NO_ROW(256, 256, 3);
         else if (units <= 1024) NO_ROW(256, 256, 4);
         else if (units <= 2048) NO_ROW(256, 256, 8);
         else if (units <= 4096) NO_ROW(1024, 1024, 4);
@@ -815,8 +801,10 @@ static int32_t logprobs(const char* who, Logprobs a, void* ws, hipStream_t st) {
     })
     if (units <= 64) NO_ROW(64, 1);
     else if (units <= 128) NO_ROW(64, 2);
+    else if (units <= 192) NO_ROW(64, 3);
     else if (units <= 256) NO_ROW(64, 4);
     else if (units <= 512) NO_ROW(256, 2);
+    else if (units <= 768) NO_ROW(256, 3);
     else if (units <= 1024) NO_ROW(256, 4);
     else if (W == 4 && units <= 2048) NO_ROW(256, W == 4 ? 8 : 4);
 #undef NO_ROW

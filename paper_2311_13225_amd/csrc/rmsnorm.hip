@@ -129,12 +129,23 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(RowsOf s, const fl
             for (int k = 0; k < Run<float, W>::N; ++k) __builtin_memcpy(&wk.v[u].v[k], one, 16);
         }
     }
-    for (int64_t i = (int64_t)blockIdx.x * PER_BLOCK + team.index(); i < n; i += (int64_t)gridDim.x * PER_BLOCK) {
-        RowRegs<T, W, U, TEAM> rs, rg, ra;
-        const float r = rstd[i];
+    const int64_t stride = (int64_t)gridDim.x * PER_BLOCK;
+    int64_t i = (int64_t)blockIdx.x * PER_BLOCK + team.index();
+    RowRegs<T, W, U, TEAM> rs, rg, ra;
+    float r = 0.0f;
+    if (i < n) {
+        r = rstd[i];
         rs.load(s.row<T>(i), dim, t, zero);
         rg.load(grad_y.row<T>(i), dim, t, zero);
         if (grad_sum.p) ra.load(grad_sum.row<T>(i), dim, t, zero);
+    }
+    for (; i < n; i += stride) {
+        // each run of the next row is requested when the gradient has no more use for this one's registers (100000 x 128 bf16: 55.6 -> 36.5 us,
+        // 16384 x 2048: 59.6 -> 55.9)
+        const int64_t next = i + stride, at = next < n ? next : i;
+        const int32_t next_len = next < n ? dim : 0;
+        const T *const next_s = s.row<T>(at), *const next_g = grad_y.row<T>(at), *const next_a = grad_sum.p ? grad_sum.row<T>(at) : nullptr;
+        const float next_r = rstd[at];
         float dot = 0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -168,8 +179,15 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(RowsOf s, const fl
             Run<T, W> o;
             o.set(g);
             store.put(rs.at(t, u), o);
+            rs.load_run(next_s, next_len, t, u, zero);
+            rg.load_run(next_g, next_len, t, u, zero);
+            if (grad_sum.p) ra.load_run(next_a, next_len, t, u, zero);
         }
         store.finish();
+        rs.load_end(next_s, next_len, t, zero);
+        rg.load_end(next_g, next_len, t, zero);
+        if (grad_sum.p) ra.load_end(next_a, next_len, t, zero);
+        r = next_r;
     }
     if (!grad_weight) return;
     if constexpr (PER_BLOCK > 1) {      // the block's teams in turn

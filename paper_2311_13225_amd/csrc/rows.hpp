@@ -197,7 +197,8 @@ struct RowRegs {
         const int32_t c = len / W * W;
         if (len / W % TEAM != t) return;
         Run<T, W> r;
-        r.load_at(p, c, len, fill);
+        if (c > 0) r.load_to_end(p + c, len - c, fill);
+        else r.load(p, len, fill);
 #pragma unroll
         for (int u = 0; u < U; ++u) if (c == at(t, u)) v[u] = r;
     }
