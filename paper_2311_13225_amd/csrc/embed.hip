@@ -4,11 +4,13 @@
 
 namespace no {
 
-// A group of lanes (a power of two, at most 64) copies a row in runs of W values, W such that the wider side moves 16 or 32 bytes a lane. The next
-// row's id is requested before this row's values, so that a row costs one round trip, its scale beside it.
-template <typename T, typename O, int W, int UNR>
+// out[i] = scale row_scale[id] table[id]: no arithmetic to speak of, bound by the rows' round trips. A group of lanes (a power of two, at most 64) copies a row in runs of
+// W values, 16 bytes a lane or more on the wider side. The next row's id is requested before this row's values, so that a row costs one round trip, its scale beside it.
+// 118000 rows of 256 e4m3 values with scales into bf16: 18.6 us, 4.8 TB/s of the bytes that it cannot do without (runs of 16 values: 22.3). Up to 8192 blocks (2048: 30000 rows of 4096
+// bf16 values 86.0 us for 84.5, 50000 x 1000 bf16 into fp32 65.5 for 59.6). Requests of several runs ahead gain nothing (four: 89.4 us for 83.5).
+template <typename T, typename O, int W, bool SHORT>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_rows, int32_t dim, const float* __restrict__ row_scale, const int32_t* __restrict__ ids,
-                                                        const int32_t* d_n, int32_t cap, float scale, RowsOf out, int32_t units, int32_t g_log2) {
+                                                        const int32_t* d_n, int32_t cap, float scale, RowsOf out, int32_t g_log2) {
     const int32_t n = rows_here(d_n, cap), lane = lane_id(), g = 1 << g_log2, sub = lane >> g_log2, u0 = lane & (g - 1), rows = 64 >> g_log2;
     const int64_t wave = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 6, stride = (int64_t)gridDim.x * 4 * rows;
     int64_t r = wave * rows + sub;
@@ -18,26 +20,18 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_
         const bool there = id >= 0 && id < n_rows;
         const float by = there ? (row_scale ? scale * row_scale[id] : scale) : 0.0f;
         const T* src = table.row<T>(there ? id : 0);
-        for (int32_t ub = u0; ub < units && r < n; ub += g * UNR) {
-            Run<T, W> v[UNR];
+        for (int32_t c = u0 * W; c < dim && r < n; c += g * W) {
+            const Place<W, SHORT> place(c, dim);
+            Run<T, W> v;
+            if (there) place.load(v, src);
+            float f[W];
+            v.get(f);
 #pragma unroll
-            for (int j = 0; j < UNR; ++j) {
-                const int32_t c = (ub + j * g) * W;
-                if (there && c < dim) v[j].load_at(src, c, dim, from_f32<T>(0.0f));
-            }
-#pragma unroll
-            for (int j = 0; j < UNR; ++j) {
-                const int32_t c = (ub + j * g) * W;
-                if (c >= dim) break;
-                float f[W];
-                v[j].get(f);
-#pragma unroll
-                for (int w = 0; w < W; ++w) f[w] = there ? f[w] * by : 0.0f;
-                Run<O, W> o;
-                o.set(f);
-                if (c + W <= dim) o.store_once(out.row<O>(r) + c);
-                else o.store(out.row<O>(r) + c, dim - c);
-            }
+            for (int w = 0; w < W; ++w) f[w] = there ? f[w] * by : 0.0f;
+            Run<O, W> o;
+            o.set(f);
+            if constexpr (SHORT) o.store(out.row<O>(r) + c, dim - c);
+            else o.store_once(out.row<O>(r) + place.at);        // (what two lanes hold, both store)
         }
         id = next;
     }
@@ -46,14 +40,14 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_
 template <typename T, typename O>
 static void launch_embed(const RowsOf& table, int64_t n_rows, int32_t dim, const float* row_scale, const int32_t* ids, const int32_t* d_n, int32_t cap, float scale,
                          const RowsOf& out, hipStream_t st) {
-    constexpr int W = sizeof(T) == 4 && sizeof(O) == 4 ? 4 : sizeof(T) == 1 ? 16 : 8;
+    constexpr int W = sizeof(T) == 4 && sizeof(O) == 4 ? 4 : 8;
     const int32_t units = (int32_t)ceil_div(dim, W);
     int g_log2 = 0;
     while ((1 << g_log2) < units && g_log2 < 6) ++g_log2;
     int64_t blocks = ceil_div(ceil_div(cap, 64 >> g_log2), 4);
-    if (blocks > 2048) blocks = 2048;
-    if (units > 64) hipLaunchKernelGGL((embed_fwd_kernel<T, O, W, 4>), dim3((unsigned)blocks), dim3(256), 0, st, table, n_rows, dim, row_scale, ids, d_n, cap, scale, out, units, g_log2);
-    else hipLaunchKernelGGL((embed_fwd_kernel<T, O, W, 1>), dim3((unsigned)blocks), dim3(256), 0, st, table, n_rows, dim, row_scale, ids, d_n, cap, scale, out, units, g_log2);
+    if (blocks > 8192) blocks = 8192;
+    if (dim >= W) hipLaunchKernelGGL((embed_fwd_kernel<T, O, W, false>), dim3((unsigned)blocks), dim3(256), 0, st, table, n_rows, dim, row_scale, ids, d_n, cap, scale, out, g_log2);
+    else hipLaunchKernelGGL((embed_fwd_kernel<T, O, W, true>), dim3((unsigned)blocks), dim3(256), 0, st, table, n_rows, dim, row_scale, ids, d_n, cap, scale, out, g_log2);
 }
 
 // ------------------------------------------------------------------------------------------------------- gradient
@@ -62,12 +56,19 @@ static void launch_embed(const RowsOf& table, int64_t n_rows, int32_t dim, const
 // ordered list is cut into chunks of 8 to 64 positions whatever the ids are, and a lane group walks a chunk with the sum of the id at hand
 // in registers: an id that is named a thousand times costs what a thousand rare ones do. Sums of ids that lie inside a chunk go
 // straight to the table; those that reach over a chunk's border go to the workspace and are added up, in chunk order, by a second launch. Rows that no
-// id names are found by a search in the ordered ids and cleared beside the sums. No atomics: the same ids give the same bits.
+// id names are found by a search in the ordered ids and cleared beside the sums. No float atomics: the same ids give the same bits.
+// Bound by memory: every gradient row is read once, every table row written once. 65536 rows of 2048 bf16 values, popular ids, into 131072 rows: 295 us, of which order 5.5 + 8.3 + 4.8,
+// sums 265 (1.34 GB, 5.1 TB/s), borders 15.
 
-constexpr int32_t EMBED_FEW = 256;                  // positions that need no order (embed_few_kernel)
 constexpr int EMBED_TILE = 1024;                    // positions that a block orders in LDS
-constexpr int32_t EMBED_RANK_MOST = 8192;           // positions whose places are counted in one launch
-constexpr int32_t EMBED_MERGE_MOST = 131072;        // positions that are ordered by tiles and ranks; more go through the radix sort
+// Positions that need no order (embed_few_kernel), while they have few columns too. 777 positions of 100 columns: 6.3 us for 13.5, all of one id 16.3 for 14.9; 200 of 8000: 12.0 for 14.2;
+// but 1000 of 8000: 37.8 for 26.2.
+constexpr int32_t EMBED_FEW = 1024;
+static inline bool embed_few(int32_t n, int32_t dim) { return n <= 256 || (n <= EMBED_FEW && n * ceil_div(dim, 256) <= 4096); }
+// Positions whose places are counted in one launch; more are ordered by tiles and ranks (6000 of 64 columns: 22.2 us by counting, 20.7 by tiles; 8192: 23.3 and 20.8).
+constexpr int32_t EMBED_RANK_MOST = 4096;
+// More than these go through the radix sort (131072 of 64 columns: 66 us by tiles, 76 by radix; 200000: 129 and 95).
+constexpr int32_t EMBED_MERGE_MOST = 131072;
 
 struct EmbedPlan {      // the workspace, cut up
     int64_t n, tiles, chunks;
@@ -75,7 +76,7 @@ struct EmbedPlan {      // the workspace, cut up
     bool merged, radix;
     size_t keys, pos, keys_tmp, pos_tmp, rank, sort_ws, parts, total;
     EmbedPlan(int32_t n_, int32_t dim) : n(n_), tiles(ceil_div(n_, EMBED_TILE)), chunk(64) {
-        // Long chunks leave few sums to join (65536 positions of 2048 columns: chunks of 32 and 2047 borders 26 us, of 64 half of it), as long as
+        // Long chunks leave few sums to join (65536 positions of 2048 columns: all in all 296 us by chunks of 64, 323 of 16), as long as
         // there are wavefronts for the whole chip, eight to a compute unit with eight rows each on their way.
         const int64_t units = ceil_div(dim, 8), lanes = (int64_t)1 << ilog2_ceil((uint64_t)(units < 64 ? units : 64));
         while (chunk > 8 && n * ceil_div(units, 64) * lanes / 64 / chunk < 2048) chunk >>= 1;
@@ -90,7 +91,7 @@ struct EmbedPlan {      // the workspace, cut up
         rank = pos_tmp + (merged || radix ? list : 0);
         sort_ws = rank + (merged ? list : 0);
         parts = sort_ws + (radix ? (size_t)ceil_div((int64_t)radix_ws_bytes(n), 16) * 16 : 0);
-        total = n <= EMBED_FEW ? 16 : parts + (size_t)chunks * 2 * (size_t)dim * 4 + 16;
+        total = embed_few(n_, dim) ? 16 : parts + (size_t)chunks * 2 * (size_t)dim * 4 + 16;
     }
 };
 
@@ -231,88 +232,117 @@ struct EmbedSums {
     float* parts;       // [chunks][2][dim]: the sum of an id that began in an earlier chunk, and of one that goes on in the next
 };
 
-// Few positions, in one launch and without an order: a wavefront per position and 64 runs of columns looks its id up among all of them; where the position is the id's first it adds
-// the rows of all of its positions, in order. (777 positions take 15 us in three launches; up to 256 the longest run, all positions of one id, still costs no more than that, and
-// 4 us otherwise.)
 // Clears those of the rows [v0, v0 + 16) whose bit is set.
 __device__ __forceinline__ void clear_rows(const EmbedSums& a, int64_t v0, uint32_t empty) {
     Run<float, 4> zero;
     const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     zero.set(z);
+    const bool whole = a.dim >= 4;
     while (empty) {
         const int32_t at = __builtin_ctz(empty);
         empty &= empty - 1;
         float* row = a.table.row<float>(v0 + at);
-        for (int32_t c = lane_id() * 4; c < a.dim; c += 256) zero.store(row + c, a.dim - c);
+        for (int32_t c = lane_id() * 4; c < a.dim; c += 256) {
+            if (whole) zero.store(row + min(c, a.dim - 4));
+            else zero.store(row + c, a.dim - c);
+        }
     }
 }
 
-template <typename T, int W, bool ADD>
+// Few positions, in one launch and without an order: a wavefront per position and 64 runs of columns looks its id up among all of them; where the position is the id's first it adds
+// the rows of all of its positions, in order, and where these are many (more than four rounds of requests) the block's four wavefronts add a quarter each. Bound by the latency of its
+// round trips: ids, the id's rows eight at a time, the table's.
+template <typename T, int W, bool ADD, bool SHORT>
 __global__ void __launch_bounds__(256) embed_few_kernel(EmbedSums a, const int32_t* __restrict__ ids, int32_t col_tiles, uint32_t sum_blocks) {
     constexpr int Q = EMBED_FEW / 64, UNR = 8;
+    constexpr int32_t SHARED = 4 * UNR;
+    __shared__ float part[4][W][64];
+    __shared__ uint16_t list[4][EMBED_FEW];
     const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6));
     int32_t id[Q];
 #pragma unroll
     for (int q = 0; q < Q; ++q) id[q] = lane + q * 64 < n ? ids[lane + q * 64] : -1;
     for (int64_t v0 = ((int64_t)blockIdx.x - sum_blocks) * 64 + wave * 16; blockIdx.x >= sum_blocks; v0 += ((int64_t)gridDim.x - sum_blocks) * 64) {
         if (v0 >= a.n_rows) return;
-        uint32_t empty = 0;
+        uint32_t named = 0;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            bool named = false;
-#pragma unroll
-            for (int q = 0; q < Q; ++q) named |= id[q] == v0 + r;
-            empty |= v0 + r < a.n_rows && __ballot(named) == 0 ? 1u << r : 0u;
+        for (int q = 0; q < Q; ++q) {
+            const int64_t at = id[q] - v0;
+            named |= at >= 0 && at < 16 ? 1u << at : 0u;
         }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) named |= __shfl_xor(named, o, 64);
+        const uint32_t empty = __builtin_amdgcn_readfirstlane(~named & (v0 + 16 <= a.n_rows ? 0xffffu : (1u << (a.n_rows - v0)) - 1u));
         clear_rows(a, v0, empty);
     }
-    const int32_t item = (int32_t)blockIdx.x * 4 + wave, i = item / col_tiles, col = (item % col_tiles * 64 + lane) * W, width = a.dim - col;
-    if (i >= n) return;
-    const int32_t mine = ids[i];
-    if (mine < 0 || mine >= a.n_rows) return;
-    uint64_t rest[Q];
-    int32_t first = n;
+    const int32_t item0 = (int32_t)blockIdx.x * 4, of = lane < 4 && (item0 + lane) / col_tiles < n ? ids[(item0 + lane) / col_tiles] : -1;
+    for (int32_t it = 0; it < 4; ++it) {            // the block's four in turn, the same decisions in each wavefront
+        const int32_t item = item0 + it, i = item / col_tiles, col = (item % col_tiles * 64 + lane) * W, width = a.dim - col;
+        const int32_t mine = __builtin_amdgcn_readlane(of, it);
+        if (mine < 0 || mine >= a.n_rows) continue;
+        int32_t first = n, count = 0;
 #pragma unroll
-    for (int q = Q - 1; q >= 0; --q) {
-        rest[q] = __ballot(id[q] == mine);
-        if (rest[q]) first = q * 64 + __builtin_ctzll(rest[q]);
-    }
-    if (first != i || width <= 0) return;
-    float* const to = a.table.row<float>(mine) + col;
-    Run<float, W> out;
-    if (ADD) out.load_at(to - col, col, a.dim, 0.0f);
-    float acc[W];
+        for (int q = 0; q < Q; ++q) {
+            const uint64_t here = __ballot(id[q] == mine);
+            if (here && count == 0) first = q * 64 + __builtin_ctzll(here);
+            count += __builtin_popcountll(here);
+        }
+        const bool shared = count > SHARED;
+        if (first != i || (!shared && wave != it)) continue;
+        const Place<W, SHORT> place(width > 0 ? col : 0, a.dim);
+        Run<float, W> old;
+        float* const to = a.table.row<float>(mine);
+        if (ADD && wave == it) place.load(old, (const float*)to);
+        // of a shared id's positions those [from, from + share), by their place among them
+        const int32_t share = shared ? (count + 3) / 4 : count, from = shared ? wave * share : 0;
+        float acc[W];
 #pragma unroll
-    for (int w = 0; w < W; ++w) acc[w] = 0.0f;
+        for (int w = 0; w < W; ++w) acc[w] = 0.0f;
+        int32_t before = 0;
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
-        while (rest[q]) {
+        for (int q = 0; q < Q; ++q) {
+            const uint64_t here = __ballot(id[q] == mine);
+            const int32_t at = before + __builtin_popcountll(here & ((1ull << lane) - 1)) - from;
+            if (id[q] == mine && at >= 0 && at < share) list[wave][at] = (uint16_t)(q * 64 + lane);
+            before += __builtin_popcountll(here);
+        }
+        Team<64, 64>::sync();
+        const int32_t len = min(share, count - from);
+        for (int32_t j = 0; j < len; j += UNR) {
             Run<T, W> r[UNR];
             int32_t p[UNR];
 #pragma unroll
-            for (int k = 0; k < UNR; ++k) {
-                p[k] = rest[q] ? q * 64 + __builtin_ctzll(rest[q]) : -1;
-                rest[q] &= rest[q] - 1;
-                if (p[k] >= 0) r[k].load_at(a.grad.row<T>(p[k]), col, a.dim, from_f32<T>(0.0f));
-            }
+            for (int k = 0; k < UNR; ++k) p[k] = list[wave][min(j + k, len - 1)];       // (behind the last the same row again, which does not count)
+#pragma unroll
+            for (int k = 0; k < UNR; ++k) place.load(r[k], (const T*)a.grad.row<T>(__builtin_amdgcn_readfirstlane(p[k])));
 #pragma unroll
             for (int k = 0; k < UNR; ++k) {
-                if (p[k] < 0) break;
                 float f[W];
                 r[k].get(f);
 #pragma unroll
-                for (int w = 0; w < W; ++w) acc[w] += f[w];
+                for (int w = 0; w < W; ++w) acc[w] += j + k < len ? f[w] : 0.0f;
             }
         }
-    float f[W];
-    if (ADD) out.get(f);
+        Team<64, 64>::sync();                               // (the list is read)
+        if (shared) {
+            __syncthreads();                                // (the last shared id's sums are read)
 #pragma unroll
-    for (int w = 0; w < W; ++w) f[w] = ADD ? f[w] + a.scale * acc[w] : a.scale * acc[w];
-    out.set(f);
-    out.store(to, width);
+            for (int w = 0; w < W; ++w) part[wave][w][lane] = acc[w];
+            __syncthreads();
+            if (wave != it) continue;
+#pragma unroll
+            for (int w = 0; w < W; ++w) acc[w] = ((part[0][w][lane] + part[1][w][lane]) + part[2][w][lane]) + part[3][w][lane];
+        }
+        if (width <= 0) continue;
+        float f[W];
+        if (ADD) old.get(f);
+#pragma unroll
+        for (int w = 0; w < W; ++w) f[w] = ADD ? f[w] + a.scale * acc[w] : a.scale * acc[w];
+        place.store(f, to);
+    }
 }
 
-template <typename T, int W, bool ADD>
+template <typename T, int W, bool ADD, bool SHORT>
 __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t chunks, int32_t g_log2, int32_t col_tiles, uint32_t sum_blocks) {
     const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id();
     for (int64_t v0 = ((int64_t)blockIdx.x - sum_blocks) * 64 + (threadIdx.x >> 6) * 16; blockIdx.x >= sum_blocks;
@@ -335,7 +365,8 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
     if (chunk >= chunks || e0 >= n || width <= 0) return;
     const int32_t len = (int32_t)min((int64_t)a.chunk, n - e0);
     const uint32_t before = chunk ? a.keys[e0 - 1] : ~0u, after = e0 + len < n ? a.keys[e0 + len] : ~0u;
-    float* const parts = a.parts + chunk * 2 * a.dim + col;
+    const Place<W, SHORT> place(col, a.dim);
+    float* const parts = a.parts + chunk * 2 * a.dim;
     const uint32_t n_rows = (uint32_t)a.n_rows;     // (fewer than 2^31)
     float acc[W];
 #pragma unroll
@@ -355,9 +386,9 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
 #pragma unroll
         for (int k = 0; k < UNR; ++k) {
             if (key[k] >= n_rows) continue;
-            r[k].load_at(a.grad.row<T>(p[k]), col, a.dim, from_f32<T>(0.0f));
+            place.load(r[k], (const T*)a.grad.row<T>(p[k]));
             // the row that a run's sum is added to, requested with the run's last gradient
-            if (ADD && key[k + 1] != key[k]) old[ADD ? k : 0].load_at(a.table.row<float>(key[k]), col, a.dim, 0.0f);
+            if (ADD && key[k + 1] != key[k]) place.load(old[ADD ? k : 0], (const float*)a.table.row<float>(key[k]));
         }
 #pragma unroll
         for (int k = 0; k < UNR; ++k) {
@@ -367,16 +398,14 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
 #pragma unroll
             for (int w = 0; w < W; ++w) acc[w] += f[w];
             if (key[k + 1] == key[k]) continue;     // (an id at the chunk's end goes on in the next, or does not: its sum is stored either way)
-            Run<float, W> out;
             const bool last = e + k + 1 == len;
-            if (start == 0 && key[k] == before) { out.set(acc); out.store(parts, width); }
-            else if (last && key[k] == after) { out.set(acc); out.store(parts + a.dim, width); }
+            if (start == 0 && key[k] == before) place.store(acc, parts);
+            else if (last && key[k] == after) place.store(acc, parts + a.dim);
             else {
                 if constexpr (ADD) old[ADD ? k : 0].get(f);
 #pragma unroll
                 for (int w = 0; w < W; ++w) f[w] = ADD ? f[w] + a.scale * acc[w] : a.scale * acc[w];
-                out.set(f);
-                out.store(a.table.row<float>(key[k]) + col, width);
+                place.store(f, a.table.row<float>(key[k]));
             }
             start = e + k + 1;
 #pragma unroll
@@ -387,6 +416,7 @@ __global__ void __launch_bounds__(256) embed_sums_kernel(EmbedSums a, int64_t ch
 
 // Adds up the sums that reach over borders: the chunk where such an id begins owns it. A wavefront looks at a chunk, counts the id's later chunks 64 at a time, and adds their
 // parts by itself where they are few; the parts of an id with many are shared by the block's eight wavefronts.
+template <bool SHORT>
 __global__ void __launch_bounds__(512) embed_join_kernel(EmbedSums a, int64_t chunks) {
     constexpr int64_t FEW = 16;
     __shared__ float share[8][64][4];
@@ -394,12 +424,12 @@ __global__ void __launch_bounds__(512) embed_join_kernel(EmbedSums a, int64_t ch
     const int32_t n = rows_here(a.d_n, a.cap), lane = lane_id(), wave = (int32_t)(threadIdx.x >> 6), ch = a.chunk;
     const int32_t col = ((int32_t)blockIdx.y * 64 + lane) * 4, width = a.dim - col;
     const int64_t here = min(chunks, ceil_div(n, ch));
+    const Place<4, SHORT> place(width > 0 ? col : 0, a.dim);
     auto add = [&](int64_t c, int64_t p0, int64_t p1, float (&acc)[4]) {
-        if (width <= 0) return;
 #pragma unroll 8
         for (int64_t p = p0; p < p1; ++p) {
             Run<float, 4> r;
-            r.load_at(a.parts + ((c + p) * 2 + (p == 0)) * a.dim, col, a.dim, 0.0f);
+            place.load(r, (const float*)a.parts + ((c + p) * 2 + (p == 0)) * a.dim);
             float f[4];
             r.get(f);
 #pragma unroll
@@ -408,14 +438,16 @@ __global__ void __launch_bounds__(512) embed_join_kernel(EmbedSums a, int64_t ch
     };
     auto put = [&](uint32_t key, const float (&sum)[4]) {
         if (width <= 0) return;
-        float* to = a.table.row<float>(key) + col;
-        Run<float, 4> out;
+        float* to = a.table.row<float>(key);
         float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (a.accumulate) { out.load_at(to - col, col, a.dim, 0.0f); out.get(f); }
+        if (a.accumulate) {
+            Run<float, 4> old;
+            place.load(old, (const float*)to);
+            old.get(f);
+        }
 #pragma unroll
         for (int w = 0; w < 4; ++w) f[w] += a.scale * sum[w];
-        out.set(f);
-        out.store(to, width);
+        place.store(f, to);
     };
     for (int64_t c0 = (int64_t)blockIdx.x * 8; c0 + 1 < here; c0 += (int64_t)gridDim.x * 8) {
         const int64_t c = c0 + wave;
@@ -476,8 +508,10 @@ static void launch_few(const EmbedSums& a, const int32_t* ids, hipStream_t st) {
     const int32_t col_tiles = (int32_t)ceil_div(a.dim, 64 * W);
     const int64_t sum_blocks = ceil_div((int64_t)a.cap * col_tiles, 4);
     const dim3 grid((unsigned)(sum_blocks + clear_blocks(a)));
-    if (a.accumulate) hipLaunchKernelGGL((embed_few_kernel<T, W, true>), grid, dim3(256), 0, st, a, ids, col_tiles, (uint32_t)sum_blocks);
-    else hipLaunchKernelGGL((embed_few_kernel<T, W, false>), grid, dim3(256), 0, st, a, ids, col_tiles, (uint32_t)sum_blocks);
+#define NO_AS(ADD, SHORT) hipLaunchKernelGGL((embed_few_kernel<T, W, ADD, SHORT>), grid, dim3(256), 0, st, a, ids, col_tiles, (uint32_t)sum_blocks)
+    if (a.accumulate) { if (a.dim >= W) NO_AS(true, false); else NO_AS(true, true); }
+    else { if (a.dim >= W) NO_AS(false, false); else NO_AS(false, true); }
+#undef NO_AS
 }
 
 template <typename T>
@@ -488,8 +522,10 @@ static void launch_sums(const EmbedSums& a, int64_t chunks, hipStream_t st) {
     while ((1 << g_log2) < units && g_log2 < 6) ++g_log2;
     const int64_t sum_blocks = ceil_div(ceil_div(chunks * col_tiles, 64 >> g_log2), 4);
     const dim3 grid((unsigned)(sum_blocks + clear_blocks(a)));
-    if (a.accumulate) hipLaunchKernelGGL((embed_sums_kernel<T, W, true>), grid, dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks);
-    else hipLaunchKernelGGL((embed_sums_kernel<T, W, false>), grid, dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks);
+#define NO_AS(ADD, SHORT) hipLaunchKernelGGL((embed_sums_kernel<T, W, ADD, SHORT>), grid, dim3(256), 0, st, a, chunks, g_log2, col_tiles, (uint32_t)sum_blocks)
+    if (a.accumulate) { if (a.dim >= W) NO_AS(true, false); else NO_AS(true, true); }
+    else { if (a.dim >= W) NO_AS(false, false); else NO_AS(false, true); }
+#undef NO_AS
 }
 
 }  // namespace no
@@ -540,7 +576,7 @@ extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t gra
     uint32_t *keys = (uint32_t*)(ws + plan.keys), *pos = (uint32_t*)(ws + plan.pos);
     const EmbedSums a{keys, pos, d_n_ids, n_ids_cap, scale, accumulate != 0, rows_of(d_grad_out, grad_stride_bytes), rows_of(d_grad_table, table_stride_bytes), n_rows, dim,
                       plan.chunk, (float*)(ws + plan.parts)};
-    if (n_ids_cap <= EMBED_FEW) {
+    if (embed_few(n_ids_cap, dim)) {
         if (n_ids_cap == 0 && accumulate) return NO_OK;
         if (dt == NO_F32) launch_few<float>(a, d_ids, st);
         else launch_few<bf16_t>(a, d_ids, st);
@@ -571,6 +607,8 @@ extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t gra
     if (dt == NO_F32) launch_sums<float>(a, plan.chunks, st);
     else launch_sums<bf16_t>(a, plan.chunks, st);
     const int64_t eights = ceil_div(plan.chunks - 1, 8);
-    hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(eights < 4096 ? eights : 4096), (unsigned)ceil_div(dim, 256)), dim3(512), 0, st, a, plan.chunks);
+    const dim3 grid((unsigned)(eights < 4096 ? eights : 4096), (unsigned)ceil_div(dim, 256));
+    if (dim >= 4) hipLaunchKernelGGL(embed_join_kernel<false>, grid, dim3(512), 0, st, a, plan.chunks);
+    else hipLaunchKernelGGL(embed_join_kernel<true>, grid, dim3(512), 0, st, a, plan.chunks);
     return launch_status(who);
 }

@@ -197,11 +197,10 @@ struct ShareByLse {
 };
 
 // The gradient of values [first, first + len) of a row, held in `v`: w T q everywhere, then the classes that the teacher names once more with
-// their shares taken off (the barrier orders the two stores; an entry that stands twice stores the same value twice). `after(u)` follows the last use of
-// run u.
-template <typename T, int U, int TEAM, int THREADS, bool ONCE, typename Q, typename After>
+// their shares taken off (the barrier orders the two stores; an entry that stands twice stores the same value twice).
+template <typename T, int U, int TEAM, int THREADS, bool ONCE, typename Q>
 __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_t first, int32_t len, Piece<T, U, TEAM, ONCE>& v, const Q& q, float w, const Teacher& te,
-                                             Team<TEAM, THREADS>& team, After after) {
+                                             Team<TEAM, THREADS>& team) {
     constexpr int W = Piece<T, U, TEAM>::W;
     int t = team.lane();
     asm volatile("" : "+v"(t));
@@ -219,14 +218,11 @@ __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_
             o.set(f);
         } else o.v[0] = 0;
         store.put(v.at(t, u), o);
-        after(u);
     }
     store.finish();
     team.sync();
-    // (in a block of sixteen wavefronts by the third and those after it: the first two have the next row's entries and the loss to make)
     if (live)
-        for (int j = TEAM == 1024 ? t - 128 : t; j < a.k; j += TEAM) {
-            if (j < 0) break;
+        for (int j = t; j < a.k; j += TEAM) {
             const int32_t id = te.of[j].id, at = id - first;
             if (id < 0 || at < 0 || at >= len) continue;
             float share = 0.0f;         // of all entries with this class
@@ -239,7 +235,9 @@ __device__ __forceinline__ void distill_grad(const Distill& a, int64_t i, int32_
         }
 }
 
-// Whole rows in a team's registers: everything in one read.
+// Whole rows in a team's registers: everything in one read and one write, which bound it; the largest take a compute unit's register file. 1024 x 172 fp32 with 8 entries: 5.6 us, a row's
+// round trips; 16384 x 32768 bf16: 403 us, 5.3 TB/s; 4096 x 131072 bf16 with 64 entries: 410 us, 5.2 TB/s (sums and gradients in two launches: 554; a block that walks rows and
+// asks for each run of the next one as soon as the gradient has no more use for its registers: 452).
 template <typename T, int TEAM, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) distill_row_kernel(Distill a) {
     __shared__ float smem[2 * THREADS / 64];
@@ -252,7 +250,7 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(Distill a) {
     const bool first_wave = TEAM == 64 || threadIdx.x < 64;
     Entries e;
     if (first_wave) e.load(a, i);
-    Piece<T, U, TEAM> v;
+    Piece<T, U, TEAM, (TEAM == 1024 && U > 4)> v;
     v.load(z, a.classes, team.lane());
     const float w = a.weight ? a.weight[i] : 1.0f;
     if (first_wave) {
@@ -261,61 +259,17 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(Distill a) {
     }
     if (a.lse_in) {
         team.sync();
-        distill_grad(a, i, 0, a.classes, v, ShareByLse(a.inv_t, a.lse_in[i], w * a.temperature), w, te, team, [](int) {});
+        distill_grad(a, i, 0, a.classes, v, ShareByLse(a.inv_t, a.lse_in[i], w * a.temperature), w, te, team);
         return;
     }
     const Sums r = team_sums<false>(v.template lane_sums<false>(a.c), a.c, team);
     v.renew();
     if constexpr (TEAM == 64) team.sync();      // (the entries; in larger teams a sum's barrier stood between)
     if (first_wave) distill_loss(a, i, r, w, te);
-    if (a.grad.p) distill_grad(a, i, 0, a.classes, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [](int) {});
+    if (a.grad.p) distill_grad(a, i, 0, a.classes, v, ShareBySums(r, a.c, w * a.temperature), w, te, team);
 }
 
-// The same for rows that fill the register file of a compute unit, one block to each: the block walks rows, and each run of the next row is requested when this
-// row's gradient has no more use for its registers, so that reading goes on beside the arithmetic and the stores.
-template <typename T, int U>
-__global__ void __launch_bounds__(1024) distill_rows_kernel(Distill a) {
-    __shared__ float smem[2 * 1024 / 64];
-    __shared__ Teacher teachers[2];
-    Team<1024, 1024> team(smem);
-    const int64_t n = min((int64_t)rows_here(a.d_n, a.cap), a.row0 + a.pieces);     // (pieces: the launch's rows)
-    const bool first_wave = threadIdx.x < 64;
-    int64_t i = a.row0 + blockIdx.x;
-    if (i >= n) return;
-    int t = threadIdx.x;
-    Entries e;
-    Piece<T, U, 1024, U == 16> v;
-    v.load(a.z.row<T>(i), a.classes, t);
-    if (first_wave) {
-        e.load(a, i);
-        e.load_logits(a.z.row<T>(i), a.classes, 0, a.classes);
-        e.shares(a, teachers[0]);
-    }
-    for (int turn = 0; i < n; turn ^= 1) {
-        const Teacher& te = teachers[turn];
-        asm volatile("" : "+v"(t));                 // (what follows from it is made anew in each row, not kept in registers over all of them)
-        const int64_t next = i + gridDim.x;
-        const T* const next_row = a.z.row<T>(next < n ? next : i);
-        const int32_t next_len = next < n ? a.classes : 0;
-        const float w = a.weight ? a.weight[i] : 1.0f;
-        v.renew();
-        const Sums r = team_sums<false>(v.template lane_sums<false>(a.c), a.c, team);
-        v.renew();
-        if (threadIdx.x >= 64 && threadIdx.x < 128) distill_loss(a, i, r, w, te);
-        distill_grad(a, i, 0, a.classes, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [&](int u) {
-            v.load_run(next_row, next_len, t, u, from_f32<T>(-INFINITY));
-        });
-        v.load_end(next_row, next_len, t, from_f32<T>(-INFINITY));
-        if (first_wave && next < n) {       // (into the other of the two: the last reads of it stand before this row's sums)
-            e.load(a, next);
-            e.load_logits(next_row, a.classes, 0, a.classes);
-            e.shares(a, teachers[turn ^ 1]);
-        }
-        i = next;
-    }
-}
-
-// Sums of one piece of a row.
+// Sums of one piece of a row. 16384 x 32768 bf16: 174 us, 6.2 TB/s.
 template <typename T, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) distill_sums_kernel(Distill a) {
     __shared__ float smem[2 * THREADS / 64];
@@ -329,7 +283,7 @@ __global__ void __launch_bounds__(THREADS) distill_sums_kernel(Distill a) {
     if (threadIdx.x == 0) a.parts[i * a.pieces + p] = r;
 }
 
-// One piece of a row's gradient, from the sums of the row's pieces or from a given lse. The gradient may go over the logits, so the loss, which
+// One piece of a row's gradient, from the sums of the row's pieces or from a given lse (16384 x 32768 bf16: 373 us, 5.8 TB/s). The gradient may go over the logits, so the loss, which
 // reads them all over the row, is made by a launch before this one (distill_loss_kernel).
 template <typename T, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) distill_grad_kernel(Distill a) {
@@ -351,10 +305,10 @@ __global__ void __launch_bounds__(THREADS) distill_grad_kernel(Distill a) {
     }
     if (a.lse_in) {
         team.sync();
-        distill_grad(a, i, first, len, v, ShareByLse(a.inv_t, a.lse_in[i], w * a.temperature), w, te, team, [](int) {});
+        distill_grad(a, i, first, len, v, ShareByLse(a.inv_t, a.lse_in[i], w * a.temperature), w, te, team);
     } else {
         const Sums r = join_sums(a.parts + i * a.pieces, a.pieces, a.c, team);      // (its barriers stand behind the entries)
-        distill_grad(a, i, first, len, v, ShareBySums(r, a.c, w * a.temperature), w, te, team, [](int) {});
+        distill_grad(a, i, first, len, v, ShareBySums(r, a.c, w * a.temperature), w, te, team);
     }
 }
 
@@ -533,6 +487,9 @@ __device__ __forceinline__ void store_top(const Logprobs& a, int64_t i, int32_t 
     a.top_logprobs[i * a.k + at] = r.s != r.s ? NAN : none ? -INFINITY : log_share(a, r, log_s, value_of((uint32_t)(key >> 32)));
 }
 
+// A row, or a piece of one: sums, and the largest values. 4096 x 50001 fp32 with 20 alternatives: 148 us, 5.5 TB/s, the join in it 13 to 15; one row of 131072 bf16
+// in 64 pieces 5 us and 5, the round trips of either launch; 4096 x 131072 bf16 204 us without alternatives (5.3 TB/s), 259 with 20, whose search holds a block's place longer than
+// its share of memory takes.
 template <typename T, int TEAM, int THREADS, int U, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, U == 8 ? 5 : U == 4 ? 7 : 8) logprobs_kernel(Logprobs a) {
     __shared__ float smem[2 * THREADS / 64];
@@ -646,6 +603,7 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
     for (int32_t e = count + t; e < a.k; e += TEAM) store_top(a, i, e, 0, r, log_s);
 }
 
+// The gradient of log probability and entropy: one read, one write. 4096 x 32000 bf16: 94 us, 5.6 TB/s.
 template <typename T, int TEAM, int U>
 __global__ void __launch_bounds__(256) logprobs_grad_kernel(RowsOf z, const int32_t* d_n, int64_t row0, int32_t cap, int32_t classes, int32_t pieces, const int32_t* __restrict__ tokens,
                                                             float inv_t, const float* __restrict__ lse, const float* __restrict__ entropy, const float* __restrict__ g_logprob,
@@ -700,7 +658,7 @@ static int32_t check_teacher(const char* who, int32_t n, const int32_t* ids, con
     return NO_OK;
 }
 
-// Rows in pieces: as many as fill the chip while rows are few, of a multiple of a block's runs.
+// Rows in pieces: as many as fill the chip while rows are few, of a multiple of a block's runs. (100 x 50001 fp32, log probabilities: at least 1024 blocks 14.8 us, 512 or 2048 16.1.)
 struct Cut {
     int32_t u, piece, pieces;
     Cut(int32_t n, int32_t classes, int32_t w, int32_t most_u) {
@@ -712,7 +670,10 @@ struct Cut {
 };
 static int32_t most_pieces(int32_t n, int32_t classes) { return Cut(n, classes, 4, 8).pieces; }      // (of either type: bf16 pieces of 4 runs are as long)
 
-constexpr int64_t FEW_ROWS = 128;       // rows that leave half of the chip idle when each is one block's
+// Rows of more values than MANY, whose arithmetic takes one block long, and fewer than FEW_ROWS of them: in pieces all over the chip (48 x 131072 bf16: 17.0 us, a block a row 19.3; 64: 19.0 and 19.8;
+// 96: 22.1 and 21.2; but 20 x 50000 bf16 13.5 and 10.9, 48 x 50000 fp32 15.5 and 11.5).
+constexpr int64_t FEW_ROWS = 64;
+constexpr int32_t MANY = 65536;
 
 // A launch holds fewer than 2^32 threads, 2^21 blocks of 1024 among them: more rows go in several.
 template <typename F>
@@ -730,14 +691,10 @@ static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
         a.row0 = row0;                                                                                                                            \
         hipLaunchKernelGGL((distill_row_kernel<T, TEAM, THREADS, U>), dim3((unsigned)ceil_div(rows, THREADS / TEAM)), dim3(THREADS), 0, st, a);   \
     })
-#define NO_ROWS(U)                                                                                                            \
-    in_slabs(a.cap, MOST_BLOCKS, [&](int64_t row0, int64_t rows) {                                                            \
-        a.row0 = row0;                                                                                                        \
-        a.pieces = (int32_t)rows;                                                                                             \
-        hipLaunchKernelGGL((distill_rows_kernel<T, U>), dim3((unsigned)(rows < 256 ? rows : 256)), dim3(1024), 0, st, a);     \
-    })
     // (from a given lse every piece of a row goes by itself, but short rows by wavefronts, which share the work on the teacher's entries)
-    const bool row = a.lse_in ? units <= 256 : units <= 2048 || (units <= 16384 && a.grad.p && a.cap >= FEW_ROWS);
+    // Runs a lane: as few as hold the row, where a step less was measured to pay (50000 x 602 fp32: three runs 59.3 us, four 62.1; 32000 x 10000 bf16: three runs of 512 lanes 246, four 263;
+    // 8000 x 80000 bf16: ten of 1024 lanes 518, sixteen 596).
+    const bool row = a.lse_in ? units <= 256 : units <= 2048 || (units <= 16384 && a.grad.p && (a.classes <= MANY || a.cap >= FEW_ROWS));
     if (row) {
         if (units <= 64) NO_ROW(64, 256, 1);
         else if (units <= 128) NO_ROW(64, 256, 2);
@@ -746,14 +703,17 @@ static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
         else if (units <= 512) NO_ROW(256, 256, 2);
         else if (units <= 768) NO_ROW(256, 256, 3);
         else if (units <= 1024) NO_ROW(256, 256, 4);
-        else if (units <= 2048) NO_ROW(256, 256, 8);
+        else if (units <= 1536) NO_ROW(512, 512, 3);
+        else if (units <= 2048) NO_ROW(512, 512, 4);
         else if (units <= 4096) NO_ROW(1024, 1024, 4);
-        else if (units <= 8192) NO_ROWS(8);
-        else NO_ROWS(16);
+        else if (units <= 8192) NO_ROW(1024, 1024, 8);
+        else if (units <= 10240) NO_ROW(1024, 1024, 10);
+        else if (units <= 12288) NO_ROW(1024, 1024, 12);
+        else if (units <= 14336) NO_ROW(1024, 1024, 14);
+        else NO_ROW(1024, 1024, 16);
         return launch_status(who);
     }
 #undef NO_ROW
-#undef NO_ROWS
     const Cut cut(a.cap, a.classes, W, 8);
     a.piece = cut.piece;
     a.pieces = cut.pieces;
@@ -821,7 +781,7 @@ static int32_t logprobs(const char* who, Logprobs a, void* ws, hipStream_t st) {
             else if (cut.u == 4) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 4, true>), grid, dim3(256), 0, st, a);
             else if (cut.u == 2) hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 2, true>), grid, dim3(256), 0, st, a);
             else hipLaunchKernelGGL((logprobs_kernel<T, 256, 256, 1, true>), grid, dim3(256), 0, st, a);
-            // many rows of few pieces: a wavefront each, without barriers
+            // many rows of few pieces: a wavefront each, without barriers (4096 x 50001: 149.1 us in all, by blocks 151.1; one row of 64 pieces 10.3 and 10.0)
             if (rows >= 256 && a.pieces <= 64) hipLaunchKernelGGL((logprobs_join_kernel<T, 64>), dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, st, a);
             else hipLaunchKernelGGL((logprobs_join_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, a);
         });

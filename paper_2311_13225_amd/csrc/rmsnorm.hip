@@ -5,8 +5,10 @@ namespace no {
 
 constexpr float E4M3_MOST = 448.0f, SMALLEST_MOST = 0x1p-100f;
 
-// A team of lanes holds a row in registers, U runs of 16 bytes a lane, and walks rows with a stride of all teams, the weights in registers too where they fit. The
-// row is read once and written once.
+// y = s / sqrt(mean(s^2) + eps) weight of s = x + residual. A team of lanes holds a row in registers, U runs of 16 bytes a lane, so that the row is read once and written once, which is
+// what bounds it: 16384 x 4096 bf16 with a residual 92 us, 5.8 TB/s; 50001 x 602 fp32 into e4m3 33 us, 4.6 TB/s (three runs a lane; four, of which 41 % are empty: 35.2).
+// What it writes goes past the caches (94.8 -> 91.1 us, 4096 x 4096 27.8 -> 21.8); what it reads does not, since the launch before may have left it there (4096 x 4096: 25.7, but
+// 50000 x 2048 138.9 -> 134.1).
 template <typename T, typename Y, int TEAM, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf residual, const float* __restrict__ weight, float eps, const int32_t* d_n, int32_t cap,
                                                               int32_t dim, RowsOf sum, RowsOf y, float* row_scale, float* rstd_out) {
@@ -43,7 +45,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf r
             for (int w = 0; w < W; ++w) ss += f[w] * f[w];
         }
         if (sum.p) {
-            RowStore<T, W> store(sum.row<T>(i), dim);
+            RowStore<T, W, true> store(sum.row<T>(i), dim);
 #pragma unroll
             for (int u = 0; u < U; ++u) store.put(s.at(t, u), s.v[u]);
             store.finish();
@@ -80,7 +82,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf r
             inv = 1.0f / scale;
         }
         s.renew();
-        RowStore<Y, W> store(y.row<Y>(i), dim);
+        RowStore<Y, W, true> store(y.row<Y>(i), dim);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float f[W];
@@ -103,9 +105,10 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf r
 // ------------------------------------------------------------------------------------------------------- gradients
 //
 // The weight's gradient is a sum over rows for every column: a team adds its rows' terms in registers while it makes their input gradients, a block joins its
-// teams' sums in LDS and stores one row of parts, and a second launch adds the blocks' parts in order.
+// teams' sums in LDS and stores one row of parts, and a second launch adds the blocks' parts in order. Bound by memory: 16384 x 2048 bf16 with the residual's gradient 53 us,
+// 5.0 TB/s, of which the second launch takes 4.8; 16384 x 4096 97 us, 5.5 TB/s.
 
-constexpr int32_t NORM_PARTS = 512;     // rows of parts, at most
+constexpr int32_t NORM_PARTS = 512;     // rows of parts, at most (50000 x 602 fp32: 101 us; 256: 132, 1024: 121)
 
 template <typename T, int TEAM, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(RowsOf s, const float* __restrict__ weight, const float* __restrict__ rstd, RowsOf grad_y, RowsOf grad_sum,
@@ -131,7 +134,8 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(RowsOf s, const fl
     }
     const int64_t stride = (int64_t)gridDim.x * PER_BLOCK;
     int64_t i = (int64_t)blockIdx.x * PER_BLOCK + team.index();
-    RowRegs<T, W, U, TEAM> rs, rg, ra;
+    // Long rows past the caches (16384 x 4096 bf16 103 -> 95 us, 4000 x 16384 fp32 214 -> 196); short ones share cache lines with the rows beside them (50000 x 602 fp32: 102 -> 115).
+    RowRegs<T, W, U, TEAM, U * TEAM >= 256> rs, rg, ra;
     float r = 0.0f;
     if (i < n) {
         r = rstd[i];
@@ -163,7 +167,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(RowsOf s, const fl
         const float mean = team.sum(dot) / (float)dim;
         rs.renew();
         rg.renew();
-        RowStore<T, W> store(grad_x.row<T>(i), dim);
+        RowStore<T, W, true> store(grad_x.row<T>(i), dim);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[W], g[W], k[W], a[W];
@@ -270,8 +274,9 @@ __global__ void __launch_bounds__(1024) rmsnorm_join_kernel(const float* __restr
     if (threadIdx.x < 16 && c < dim) grad_weight[c] = sum;
 }
 
-// Blocks for n rows: at most those that stand on the chip at once (by the kernel's registers), so that a team walks several rows with the weights it holds
-// and all teams end together.
+// Blocks for n rows, `most` at most, behind which a team walks several rows with the weights it holds. The forward pass has a team for every row (16384 x 4096 bf16 94.8 us; 2048 blocks
+// 105.8), but for rows of part of a wavefront (200000 x 128 bf16: 2048 blocks 47 us, all 56), for fp32 into e4m3, whose arithmetic is most (50001 x 602: 4096 blocks 32.7, all 36.1; 100000 x 256:
+// 33.7 and 39.4), and for blocks of 1024 lanes (4000 x 30000 fp32: 256 blocks 347, all 382).
 static inline int64_t norm_blocks(int64_t n, int per_block, int64_t most) {
     const int64_t b = ceil_div(n, per_block);
     return b < most ? b : most;
@@ -300,7 +305,7 @@ extern "C" int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride
     const RowsOf x = rows_of(d_x, x_stride_bytes), r = rows_of(d_residual, residual_stride_bytes), s = rows_of(d_sum, sum_stride_bytes), y = rows_of(d_y, y_stride_bytes);
     hipStream_t st = (hipStream_t)stream;
 #define NO_NORM_AS(T, Y, TEAM, THREADS, U)                                                                                                          \
-    hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, Y, TEAM, THREADS, U>), dim3((unsigned)norm_blocks(n_rows_cap, THREADS / TEAM, THREADS == 1024 ? 256 : U <= 2 ? 2048 : U == 3 ? 1792 : U == 4 ? 1280 : 768)), \
+    hipLaunchKernelGGL((rmsnorm_fwd_kernel<T, Y, TEAM, THREADS, U>), dim3((unsigned)norm_blocks(n_rows_cap, THREADS / TEAM, THREADS == 1024 ? 256 : TEAM < 64 ? 2048 : sizeof(T) == 4 && sizeof(Y) == 1 ? 4096 : 1 << 20)), \
                        dim3(THREADS), 0, st, x, r, d_weight, eps, d_n_rows, n_rows_cap, dim, s, y, d_row_scale, d_rstd)
 #define NO_NORM(T, Y)                                              \
     do {                                                           \

@@ -169,6 +169,31 @@ struct Run {
     }
 };
 
+// Where a lane's run of a row begins: at its own columns [c, c + W), or W values before the row's end, so that the requests of every lane are whole and nothing branches; the
+// last two lanes of such a row hold some values twice. Rows shorter than a run (SHORT) go value by value.
+template <int W, bool SHORT>
+struct Place {
+    int32_t at, skip;       // skip: values of the run that are the lane before's
+    int32_t dim;
+    __device__ __forceinline__ Place(int32_t c, int32_t dim_) : at(SHORT ? c : min(c, dim_ - W)), skip(c - at), dim(dim_) {}
+    template <typename T>
+    __device__ __forceinline__ void load(Run<T, W>& r, const T* row) const {
+        if constexpr (SHORT) r.load_at(row, at, dim, from_f32<T>(0.0f));
+        else r.load(row + at);
+    }
+    __device__ __forceinline__ void store(const float (&f)[W], float* row) const {      // of a lane inside the row
+        if (SHORT || skip == 0) {
+            Run<float, W> o;
+            o.set(f);
+            if constexpr (SHORT) o.store(row + at, dim - at);
+            else o.store(row + at);
+        } else {
+#pragma unroll
+            for (int w = 1; w < W; ++w) if (w >= skip) row[at + w] = f[w];
+        }
+    }
+};
+
 // p + c for a row's address, the same in all lanes, and a place in it: 32 bits of offset, which a request takes beside a scalar address (as 64-bit
 // addresses the places of all of a lane's runs would be kept in registers).
 template <typename T>
@@ -178,8 +203,8 @@ __device__ __forceinline__ T* offset(T* p, int32_t c) {
 }
 
 // A row (or a piece of one) of `len` values in the registers of TEAM lanes: run u of lane t covers values [(t + u TEAM) W, + W). ONCE: by requests that leave the caches
-// to others. Measured kernel by kernel: sums of 16384 x 32768 bf16 logits 198 -> 178 us, their gradient from an lse 403 -> 373, the gradient of log probabilities 101 -> 95, rows by
-// id (stores) 103 -> 94, rows of 131072 logits in a block 467 -> 454; but norms, table gradients and shorter rows of logits up to 8 % slower.
+// to others. Measured kernel by kernel: sums of 16384 x 32768 bf16 logits 198 -> 178 us, their gradient from an lse 403 -> 373, the gradient of log probabilities 101 -> 95, rows
+// of 131072 bf16 logits in a block 426 -> 410, of 20000 fp32 ones 242 -> 215; but short rows of logits slower (100000 x 600 fp32 99 -> 152), and what fits the caches (see the norms).
 template <typename T, int W, int U, int TEAM, bool ONCE = false>
 struct RowRegs {
     Run<T, W> v[U];

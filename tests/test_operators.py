@@ -148,7 +148,7 @@ def embed_grad_ref(grad, ids, v, scale):
 @pytest.mark.parametrize("n,v,dim,pad,off,popular", [
     (1, 1, 1, 0, 0, 0.0), (1, 5, 64, 0, 0, 0.0), (2, 3, 100, 1, 1, 1.0), (33, 10, 7, 0, 0, 0.5), (64, 1000, 256, 0, 0, 0.0), (777, 1000, 100, 4, 0, 0.3),
     (1000, 4, 33, 0, 3, 0.2), (4096, 1, 16, 0, 0, 0.0), (4097, 70_000, 130, 2, 1, 0.7), (8193, 300, 64, 0, 0, 0.9), (16_385, 900, 512, 0, 0, 0.5),
-    (40_000, 131_072, 48, 0, 0, 0.4), (100_003, 20_000, 24, 0, 0, 0.95), (300_000, 2, 5, 0, 0, 0.0), (70_000, 100_000, 4, 0, 0, 0.0), (65, 9, 8200, 0, 0, 0.8), (256, 40, 300, 0, 0, 1.0), (257, 40, 300, 0, 0, 1.0), (255, 5000, 70, 2, 1, 0.4),
+    (40_000, 131_072, 48, 0, 0, 0.4), (100_003, 20_000, 24, 0, 0, 0.95), (300_000, 2, 5, 0, 0, 0.0), (70_000, 100_000, 4, 0, 0, 0.0), (65, 9, 8200, 0, 0, 0.8), (256, 40, 300, 0, 0, 1.0), (257, 40, 300, 0, 0, 1.0), (255, 5000, 70, 2, 1, 0.4), (1024, 300, 130, 0, 0, 0.9), (1024, 1, 70, 3, 0, 0.0), (1025, 3, 70, 0, 2, 0.5), (1000, 2, 530, 1, 0, 0.7),
     (8192, 500, 20, 0, 0, 0.6), (131_073, 5_000_000, 3, 0, 0, 0.5), (20_000, 5_000_000, 3, 0, 0, 0.5)])
 @pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("accumulate", [False, True])
@@ -384,7 +384,8 @@ def test_rmsnorm_gradient_against_differences():
 
 CLASSES = [(1, 1, 0, 0), (5, 2, 0, 0), (9, 7, 1, 1), (300, 47, 0, 0), (33, 64, 0, 0), (1025, 172, 4, 0), (17, 513, 0, 3), (12, 2048, 0, 0), (6, 4099, 0, 0),
            (600, 5000, 8, 8), (3, 16_385, 1, 0), (2, 32_768, 0, 0), (5, 50_001, 0, 0), (1, 131_072, 0, 0), (2, 131_073, 0, 1), (1, 300_001, 0, 0),
-           (270, 40_003, 0, 0), (20_000, 10, 0, 0)]
+           (270, 40_003, 0, 0), (20_000, 10, 0, 0), (4, 8005, 0, 0), (3, 10_007, 1, 0), (4, 15_000, 0, 0), (9, 36_001, 0, 0), (2, 45_001, 0, 1), (3, 55_555, 0, 0),
+           (70, 76_001, 0, 0), (66, 90_001, 1, 0), (65, 110_007, 0, 0), (64, 131_072, 0, 0), (63, 131_072, 0, 0)]
 
 
 def logits(n, c, pad, off, dt, g, masked=True):
