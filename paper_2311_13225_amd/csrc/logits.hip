@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(THREADS) distill_sums_kernel(Distill a) {
     if (threadIdx.x == 0) a.parts[i * a.pieces + p] = r;
 }
 
-// One piece of a row's gradient, from the sums of the row's pieces or from a given lse (16384 x 32768 bf16: 373 us, 5.8 TB/s). The gradient may go over the logits, so the loss, which
+// One piece of a row's gradient, from the sums of the row's pieces or from a given lse (4096 x 131072 bf16: 367 us, 5.9 TB/s). The gradient may go over the logits, so the loss, which
 // reads them all over the row, is made by a launch before this one (distill_loss_kernel).
 template <typename T, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) distill_grad_kernel(Distill a) {
@@ -603,7 +603,7 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(Logprobs a) {
     for (int32_t e = count + t; e < a.k; e += TEAM) store_top(a, i, e, 0, r, log_s);
 }
 
-// The gradient of log probability and entropy: one read, one write. 4096 x 32000 bf16: 94 us, 5.6 TB/s.
+// The gradient of log probability and entropy: one read, one write. 4096 x 32000 bf16: 91 us, 5.8 TB/s.
 template <typename T, int TEAM, int U>
 __global__ void __launch_bounds__(256) logprobs_grad_kernel(RowsOf z, const int32_t* d_n, int64_t row0, int32_t cap, int32_t classes, int32_t pieces, const int32_t* __restrict__ tokens,
                                                             float inv_t, const float* __restrict__ lse, const float* __restrict__ entropy, const float* __restrict__ g_logprob,
@@ -671,7 +671,8 @@ struct Cut {
 static int32_t most_pieces(int32_t n, int32_t classes) { return Cut(n, classes, 4, 8).pieces; }      // (of either type: bf16 pieces of 4 runs are as long)
 
 // Rows of more values than MANY, whose arithmetic takes one block long, and fewer than FEW_ROWS of them: in pieces all over the chip (48 x 131072 bf16: 17.0 us, a block a row 19.3; 64: 19.0 and 19.8;
-// 96: 22.1 and 21.2; but 20 x 50000 bf16 13.5 and 10.9, 48 x 50000 fp32 15.5 and 11.5).
+// 96: 22.1 and 21.2; but 20 x 50000 bf16 13.5 and 10.9, 48 x 50000 fp32 15.5 and 11.5). For the loss alone pieces do where there are rows for the chip (16384 x 32768 bf16:
+// 6.2 TB/s), and a block a row where there are not (200 x 30000 fp32: 8.1 us, pieces 10.9).
 constexpr int64_t FEW_ROWS = 64;
 constexpr int32_t MANY = 65536;
 
@@ -694,7 +695,7 @@ static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
     // (from a given lse every piece of a row goes by itself, but short rows by wavefronts, which share the work on the teacher's entries)
     // Runs a lane: as few as hold the row, where a step less was measured to pay (50000 x 602 fp32: three runs 59.3 us, four 62.1; 32000 x 10000 bf16: three runs of 512 lanes 246, four 263;
     // 8000 x 80000 bf16: ten of 1024 lanes 518, sixteen 596).
-    const bool row = a.lse_in ? units <= 256 : units <= 2048 || (units <= 16384 && a.grad.p && (a.classes <= MANY || a.cap >= FEW_ROWS));
+    const bool row = a.lse_in ? units <= 256 : units <= 2048 || (units <= 16384 && (a.grad.p ? a.classes <= MANY || a.cap >= FEW_ROWS : a.classes <= MANY && a.cap < 256));
     if (row) {
         if (units <= 64) NO_ROW(64, 256, 1);
         else if (units <= 128) NO_ROW(64, 256, 2);
@@ -714,7 +715,8 @@ static int32_t distill(const char* who, Distill a, void* ws, hipStream_t st) {
         return launch_status(who);
     }
 #undef NO_ROW
-    const Cut cut(a.cap, a.classes, W, 8);
+    // (from a given lse, which needs no sums of the pieces, of four runs a lane: 4096 x 50001 fp32 286 us, of eight 304)
+    const Cut cut(a.cap, a.classes, W, a.lse_in ? 4 : 8);
     a.piece = cut.piece;
     a.pieces = cut.pieces;
     a.parts = (Sums*)ws;
@@ -793,7 +795,8 @@ template <typename T>
 static int32_t logprobs_grad(const char* who, const RowsOf& z, const int32_t* d_n, int32_t cap, int32_t classes, const int32_t* tokens, float inv_t, const float* lse,
                              const float* entropy, const float* g_logprob, const float* g_entropy, const RowsOf& grad, hipStream_t st) {
     const int64_t units = ceil_div(classes, 16 / (int)sizeof(T));
-    const Cut cut(cap, classes, 16 / (int)sizeof(T), 8);
+    // (pieces of four runs a lane: 4096 x 32000 bf16 91 us, 4096 x 50001 fp32 287, 20000 x 3000 fp32 85; of eight 95, 313 and 85; of two 91, 278 and 94)
+    const Cut cut(cap, classes, 16 / (int)sizeof(T), 4);
 #define NO_GRAD(TEAM, U) hipLaunchKernelGGL((logprobs_grad_kernel<T, TEAM, U>), grid, dim3(256), 0, st, z, d_n, row0, cap, classes, cut.pieces, tokens, inv_t, lse, entropy, g_logprob, g_entropy, grad)
     if (units <= 256) {
         in_slabs(cap, MOST_BLOCKS * 4, [&](int64_t row0, int64_t rows) {
@@ -804,7 +807,7 @@ static int32_t logprobs_grad(const char* who, const RowsOf& z, const int32_t* d_
     }
     in_slabs(cap, MOST_BLOCKS / cut.pieces, [&](int64_t row0, int64_t rows) {
         const dim3 grid((unsigned)(rows * cut.pieces));
-        if (cut.u == 8) NO_GRAD(256, 8); else if (cut.u == 4) NO_GRAD(256, 4); else if (cut.u == 2) NO_GRAD(256, 2); else NO_GRAD(256, 1);
+        if (cut.u == 4) NO_GRAD(256, 4); else if (cut.u == 2) NO_GRAD(256, 2); else NO_GRAD(256, 1);
     });
 #undef NO_GRAD
     return launch_status(who);
