@@ -311,6 +311,7 @@ extern "C" int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride
     do {                                                           \
         const int64_t units = ceil_div(dim, 16 / (int)sizeof(T));  \
         if (units <= 8) NO_NORM_AS(T, Y, 8, 256, 1);               \
+        else if (units <= 16) NO_NORM_AS(T, Y, 16, 256, 1);        \
         else if (units <= 32) NO_NORM_AS(T, Y, 32, 256, 1);        \
         else if (units <= 64) NO_NORM_AS(T, Y, 64, 256, 1);        \
         else if (units <= 128) NO_NORM_AS(T, Y, 64, 256, 2);       \
@@ -365,6 +366,7 @@ extern "C" int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride
     do {                                                                                                                                             \
         const int64_t units = ceil_div(dim, 16 / (int)sizeof(T));                                                                                    \
         if (units <= 8) NO_NORM_AS(T, 8, 256, 1);                                                                                                    \
+        else if (units <= 16) NO_NORM_AS(T, 16, 256, 1);                                                                                             \
         else if (units <= 32) NO_NORM_AS(T, 32, 256, 1);                                                                                             \
         else if (units <= 64) NO_NORM_AS(T, 64, 256, 1);                                                                                             \
         else if (units <= 128) NO_NORM_AS(T, 64, 256, 2);                                                                                            \
