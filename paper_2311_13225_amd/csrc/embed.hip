@@ -77,9 +77,10 @@ struct EmbedPlan {      // the workspace, cut up
     size_t keys, pos, keys_tmp, pos_tmp, rank, sort_ws, parts, total;
     EmbedPlan(int32_t n_, int32_t dim) : n(n_), tiles(ceil_div(n_, EMBED_TILE)), chunk(64) {
         // Long chunks leave few sums to join (65536 positions of 2048 columns: all in all 296 us by chunks of 64, 323 of 16), as long as
-        // there are wavefronts for the whole chip, eight to a compute unit with eight rows each on their way.
+        // there are wavefronts for the whole chip, four to a compute unit with eight rows each on their way (107952 x 65 bf16: 48.5 us, for eight to a compute unit 57.1, for two 47.7; 18834 x 176:
+        // 25.0, 25.0 and 26.9).
         const int64_t units = ceil_div(dim, 8), lanes = (int64_t)1 << ilog2_ceil((uint64_t)(units < 64 ? units : 64));
-        while (chunk > 8 && n * ceil_div(units, 64) * lanes / 64 / chunk < 2048) chunk >>= 1;
+        while (chunk > 8 && n * ceil_div(units, 64) * lanes / 64 / chunk < 1024) chunk >>= 1;
         chunks = ceil_div(n, chunk);
         radix = n > EMBED_MERGE_MOST;
         merged = !radix && n > EMBED_RANK_MOST;
@@ -453,22 +454,35 @@ __global__ void __launch_bounds__(512) embed_join_kernel(EmbedSums a, int64_t ch
         const int64_t c = c0 + wave;
         int64_t parts = 0;
         uint32_t key = 0;
+        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (c + 1 < here) {
+            // everything that most borders need at once, before it is known whether an id reaches over this one: the ids around it, the next chunks' first ids, the first two parts
             const uint32_t first = a.keys[c * ch], next = a.keys[(c + 1) * ch], prior = c > 0 ? a.keys[c * ch - 1] : ~0u;
             key = a.keys[(c + 1) * ch - 1];
+            uint32_t ahead = a.keys[min(c + 2 + lane, here - 1) * ch];
+            Run<float, 4> two[2];
+            place.load(two[0], (const float*)a.parts + (c * 2 + 1) * a.dim);
+            place.load(two[1], (const float*)a.parts + (c + 1) * 2 * a.dim);
             if ((int64_t)key < a.n_rows && next == key && !(first == key && prior == key)) {
                 int64_t end = c + 2;            // the first chunk that does not begin with this id
                 for (;;) {
-                    const uint64_t same = __ballot(end + lane < here && a.keys[min(end + lane, here - 1) * ch] == key);
+                    const uint64_t same = __ballot(end + lane < here && ahead == key);
                     end += same == ~0ull ? 64 : __builtin_ctzll(~same);
                     if (same != ~0ull) break;
+                    ahead = a.keys[min(end + lane, here - 1) * ch];
                 }
                 parts = end - c;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    float f[4];
+                    two[p].get(f);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) acc[w] += f[w];
+                }
             }
         }
         if (parts > 0 && parts <= FEW) {
-            float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            add(c, 0, parts, acc);
+            add(c, 2, parts, acc);
             put(key, acc);
         }
         if (lane == 0) many[wave] = parts > FEW ? parts : 0;
