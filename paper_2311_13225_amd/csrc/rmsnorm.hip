@@ -105,8 +105,8 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf r
 // ------------------------------------------------------------------------------------------------------- gradients
 //
 // The weight's gradient is a sum over rows for every column: a team adds its rows' terms in registers while it makes their input gradients, a block joins its
-// teams' sums in LDS and stores one row of parts, and a second launch adds the blocks' parts in order. Bound by memory: 16384 x 2048 bf16 with the residual's gradient 53 us,
-// 5.0 TB/s, of which the second launch takes 4.8; 16384 x 4096 97 us, 5.5 TB/s.
+// teams' sums in LDS and stores one row of parts, and a second launch adds the blocks' parts in order. Bound by memory: 16384 x 2048 bf16 with the residual's gradient 51 us,
+// the first launch 47 of them (5.7 TB/s); 16384 x 4096 97 us, 5.5 TB/s.
 
 constexpr int32_t NORM_PARTS = 512;     // rows of parts, at most (50000 x 602 fp32: 101 us; 256: 132, 1024: 121)
 
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(1024) rmsnorm_join_kernel(const float* __restr
 }
 
 // Blocks for n rows, `most` at most, behind which a team walks several rows with the weights it holds. The forward pass has a team for every row (16384 x 4096 bf16 94.8 us; 2048 blocks
-// 105.8), but for rows of part of a wavefront (200000 x 128 bf16: 2048 blocks 47 us, all 56), for fp32 into e4m3, whose arithmetic is most (50001 x 602: 4096 blocks 32.7, all 36.1; 100000 x 256:
+// 105.8), but for rows of part of a wavefront (200000 x 128 bf16 by 32 lanes: 2048 blocks 47 us, all 56; by 16, which hold it, 37), for fp32 into e4m3, whose arithmetic is most (50001 x 602: 4096 blocks 32.7, all 36.1; 100000 x 256:
 // 33.7 and 39.4), and for blocks of 1024 lanes (4000 x 30000 fp32: 256 blocks 347, all 382).
 static inline int64_t norm_blocks(int64_t n, int per_block, int64_t most) {
     const int64_t b = ceil_div(n, per_block);
