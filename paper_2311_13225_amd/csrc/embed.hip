@@ -6,7 +6,7 @@ namespace no {
 
 // out[i] = scale row_scale[id] table[id]: no arithmetic to speak of, bound by the rows' round trips. A group of lanes (a power of two, at most 64) copies a row in runs of
 // W values, 16 bytes a lane or more on the wider side. The next row's id is requested before this row's values, so that a row costs one round trip, its scale beside it.
-// 118000 rows of 256 e4m3 values with scales into bf16: 18.6 us, 4.8 TB/s of the bytes that it cannot do without (runs of 16 values: 22.3). Up to 8192 blocks (2048: 30000 rows of 4096
+// 118000 rows of 256 e4m3 values with scales into bf16: 18.6 us, 4.8 TB/s of the bytes that it cannot do without (runs of 16 values: 22.3). Stores go past the caches (by them 26.9 us; read next, all in all 46.4 and 44.7). Up to 8192 blocks (2048: 30000 rows of 4096
 // bf16 values 86.0 us for 84.5, 50000 x 1000 bf16 into fp32 65.5 for 59.6). Requests of several runs ahead gain nothing (four: 89.4 us for 83.5).
 template <typename T, typename O, int W, bool SHORT>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(RowsOf table, int64_t n_rows, int32_t dim, const float* __restrict__ row_scale, const int32_t* __restrict__ ids,

@@ -8,7 +8,7 @@ constexpr float E4M3_MOST = 448.0f, SMALLEST_MOST = 0x1p-100f;
 // y = s / sqrt(mean(s^2) + eps) weight of s = x + residual. A team of lanes holds a row in registers, U runs of 16 bytes a lane, so that the row is read once and written once, which is
 // what bounds it: 16384 x 4096 bf16 with a residual 92 us, 5.8 TB/s; 50001 x 602 fp32 into e4m3 33 us, 4.6 TB/s (three runs a lane; four, of which 41 % are empty: 35.2).
 // What it writes goes past the caches (94.8 -> 91.1 us, 4096 x 4096 27.8 -> 21.8); what it reads does not, since the launch before may have left it there (4096 x 4096: 25.7, but
-// 50000 x 2048 138.9 -> 134.1).
+// 50000 x 2048 138.9 -> 134.1). A next launch that reads small outputs at once pays some of it back (with both read next, 4096 x 4096 50.0 us, by the caches 48.6).
 template <typename T, typename Y, int TEAM, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf residual, const float* __restrict__ weight, float eps, const int32_t* d_n, int32_t cap,
                                                               int32_t dim, RowsOf sum, RowsOf y, float* row_scale, float* rstd_out) {
@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(RowsOf s, const fl
     }
     const int64_t stride = (int64_t)gridDim.x * PER_BLOCK;
     int64_t i = (int64_t)blockIdx.x * PER_BLOCK + team.index();
-    // Long rows past the caches (16384 x 4096 bf16 103 -> 95 us, 4000 x 16384 fp32 214 -> 196); short ones share cache lines with the rows beside them (50000 x 602 fp32: 102 -> 115).
+    // Stores past the caches but for rows of a wavefront (16384 x 2048 bf16 51.5 us so, 48.8 by the caches; 16384 x 4096 96.4 and 100.0; 100000 x 128 22.6 and 25.4).
+    // Requests: long rows past the caches (16384 x 4096 bf16 103 -> 95 us, 4000 x 16384 fp32 214 -> 196); short ones share cache lines with the rows beside them (50000 x 602 fp32: 102 -> 115).
     RowRegs<T, W, U, TEAM, U * TEAM >= 256> rs, rg, ra;
     float r = 0.0f;
     if (i < n) {
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_bwd_kernel(RowsOf s, const fl
         const float mean = team.sum(dot) / (float)dim;
         rs.renew();
         rg.renew();
-        RowStore<T, W, true> store(grad_x.row<T>(i), dim);
+        RowStore<T, W, TEAM != 64> store(grad_x.row<T>(i), dim);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[W], g[W], k[W], a[W];
