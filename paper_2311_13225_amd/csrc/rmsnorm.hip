@@ -105,8 +105,8 @@ __global__ void __launch_bounds__(THREADS) rmsnorm_fwd_kernel(RowsOf x, RowsOf r
 // ------------------------------------------------------------------------------------------------------- gradients
 //
 // The weight's gradient is a sum over rows for every column: a team adds its rows' terms in registers while it makes their input gradients, a block joins its
-// teams' sums in LDS and stores one row of parts, and a second launch adds the blocks' parts in order. Bound by memory: 16384 x 2048 bf16 with the residual's gradient 51 us,
-// the first launch 47 of them (5.7 TB/s); 16384 x 4096 97 us, 5.5 TB/s.
+// teams' sums in LDS and stores one row of parts, and a second launch adds the blocks' parts in order. Bound by memory: 16384 x 2048 bf16 with the residual's gradient 48 us,
+// the first launch 45 (5.9 TB/s) and the second under 5 under the profiler; 16384 x 4096 97 us, 5.5 TB/s.
 
 constexpr int32_t NORM_PARTS = 512;     // rows of parts, at most (50000 x 602 fp32: 101 us; 256: 132, 1024: 121)
 
