@@ -23,11 +23,12 @@ struct Exponent {
 // Sums of a row, a piece or a lane's values: largest logit (-inf: there is none above), sum of 2^x, sum of x 2^x.
 struct Sums {
     float m, s, h;
-    // s and h as they are under another maximum, no smaller than m
+    // s and h as they are under another maximum, no smaller than m. Where d lies below -1000 the exponential is 0, and d held there keeps its product with s, and so h, finite:
+    // under masks of a type's lowest value d itself is about -3e38, or -inf (and +inf of a lane without values, whose s is 0).
     template <bool ENTROPY>
     __device__ __forceinline__ void move(const Exponent& to) {
         const float d = to(above(m)), e = s == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(d);
-        if constexpr (ENTROPY) h = e * (h + fmaxf(d, -3.0e38f) * s);
+        if constexpr (ENTROPY) h = e * (h + __builtin_amdgcn_fmed3f(d, -1000.0f, 0.0f) * s);
         s *= e;
     }
 };

@@ -1,0 +1,74 @@
+"""Log probabilities and distillation of rows whose classes are masked with finite values: the lowest of the type, -1e38, -1e35, -1e9.
+
+References take the row's largest logit off first, in 64 bits, so that a row that is masked throughout keeps its shares there. Bounds: a sum of C
+exponentials is off by its chain and tree, C / 256 + 64 roundings with those of its exponents (at most 3 log2 C + 2 on the average under the shares themselves); its
+logarithm and the differences around it by 8 more of 1 + |log p|; the entropy is made of two such sums."""
+import pytest
+import torch
+
+from .test_operators import BF16, F32, INF, NAN, TINY, U, close, half, nb, randn, rng, teacher, ws_of
+
+pytestmark = pytest.mark.gpu
+
+LOW = {F32: torch.finfo(F32).min, BF16: torch.finfo(BF16).min}
+# rows of a wavefront, of a block, in pieces joined by a block and by a wavefront a row, in the shortest pieces; ends inside a run
+ROUTES = [(10, 172), (10, 1003), (10, 5003), (10, 40_003), (300, 33_001), (10, 131_072)]
+
+
+def masked_rows(n, c, dt, low, g):
+    """Rows 0 .. 8 masked in nine ways, the others like row 0: (logits, classes that are left in all but rows 5 and 6)."""
+    z = randn((n, c), g, dt)
+    z[:, c - 8:] = low                              # one aligned run and what is around it
+    z[1, : c // 4] = low                            # the front, so that a lane begins with nothing else
+    left = torch.randperm(c - 8, generator=g, device="cuda")[:10]
+    keep = z[2, left].clone()
+    z[2] = low
+    z[2, left] = keep                               # all but ten
+    z[3, c // 8: 7 * c // 8] = low                  # whole pieces
+    z[4, ::2] = low                                 # every other class
+    z[5] = low                                      # nothing is left
+    z[6], z[6, : c // 2] = low, -INF                # ... and half of it is -inf
+    z[7, : c // 2] = -INF                           # both kinds
+    z[8, : c - 9] = low                             # one class is left
+    return z
+
+
+def exact_rows(z, t):
+    """(log p, entropy, lse) in 64 bits."""
+    x = z.double()
+    m = x.amax(1, keepdim=True)
+    d = (x - m) / t
+    log_s = d.exp().sum(1, keepdim=True).log()
+    log_p = d - log_s
+    p = log_p.exp()
+    return log_p, -torch.where(p > 0, p * log_p, 0.0).sum(1), (m / t + log_s)[:, 0]
+
+
+def sum_bound(c):
+    return (c / 256 + 64) * U
+
+
+def answers_of(z, tok, t, k=0):
+    b, (n, c) = nb(), z.shape
+    lp, ent, lse, top = (torch.full(s, 77.0, device="cuda") for s in ((n,), (n,), (n,), (n, k)))
+    ids = torch.full((n, k), 77, dtype=torch.int32, device="cuda")
+    b.no_logprobs_fwd(z, tok, t, lp, ent, lse, ws_of(b.no_logprobs_ws_bytes(n, c, k)), top_ids=ids if k else None, top_logprobs=top if k else None)
+    return lp, ent, lse, ids, top
+
+
+@pytest.mark.parametrize("n,c", ROUTES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("low", [None, -1e38, -1e35, -1e9], ids=["lowest", "-1e38", "-1e35", "-1e9"])
+@pytest.mark.parametrize("t", [1.0, 2.0, 0.7])
+def test_entropy_of_rows_with_finite_masks(n, c, dt, low, t):
+    g = rng(c)
+    z = masked_rows(n, c, dt, LOW[dt] if low is None else low, g)
+    tok = z.float().argmax(1).to(torch.int32)       # (a class that is left, where one is)
+    log_p, want, want_lse = exact_rows(z, t)
+    for k in (0, 8):
+        lp, ent, lse, _, _ = answers_of(z, tok, t, k)
+        want_lp = log_p.gather(1, tok.long()[:, None])[:, 0]
+        close(ent, want, 5 * sum_bound(c) * (1 + want) + 16 * U * want, "entropy")
+        close(lp, want_lp, sum_bound(c) + 8 * U * (1 + want_lp.abs()), "logprob")
+        m = z.double().amax(1).abs() / t
+        close(lse, want_lse.float(), sum_bound(c) + 4 * U * (m + want_lse.abs()), "lse")
