@@ -3,8 +3,8 @@
 // A team of lanes (a wavefront or a block) holds a row, or a piece of one, in registers, U runs of 16 bytes a lane, and takes the maximum, the sum of
 // exponentials and whatever follows from there. Rows that are longer than a team's registers, and rows that are too few to fill the chip, are cut into pieces whose sums a
 // second launch joins. Exponentials are 2^x with x = (z - m) c, c = log2(e) / T, m the row's maximum, the difference taken first: it is exact next to the maximum,
-// where the exponentials are large, so that its rounding costs nothing there, and it stays in range for every logit. (fma(z, c, -mc) saves one instruction of
-// twelve, but is off by the rounding of mc = m c, which is no smaller than the result where |m c| passes 2^24: logits of 1e8, or a small T.)
+// where the exponentials are large, so that its rounding costs nothing there; where x leaves fp32 its exponential is 0 long since, and log p itself is made in natural units.
+// (fma(z, c, -mc) saves one instruction of twelve, but is off by the rounding of mc = m c, which is no smaller than the result where |m c| passes 2^24: logits of 1e8, or a small T.)
 #include "rows.hpp"
 
 namespace no {
@@ -32,6 +32,13 @@ struct Sums {
         s *= e;
     }
 };
+
+// log p of a logit from its row's sums and the logarithm (to base 2) of their s. In natural units: to base 2 the difference of a masked class (a type's lowest value) leaves
+// fp32 where log p itself does not. A difference that leaves it before its division by T is taken after that; its two parts have one sign then, so that nothing cancels.
+__device__ __forceinline__ float log_ratio(const Sums& r, float inv_t, float log_s, float z) {
+    const float from = above(r.m), d = z - from;
+    return (fabsf(d) < INFINITY ? d * inv_t : z * inv_t - from * inv_t) - log_s * LN2;
+}
 
 template <typename T, int U, int TEAM, bool ONCE = false>
 struct Piece : RowRegs<T, 16 / (int)sizeof(T), U, TEAM, ONCE> {      // logits of a row or a piece of one, in a lane's registers; -inf behind its end
@@ -169,18 +176,18 @@ struct Entries {        // a lane's entries as they come from memory
     }
 };
 
-// Loss and lse of a row whose sums are known, by one wavefront.
+// Loss and lse of a row whose sums are known, by one wavefront. The terms are T p (log p - log q) with T log q = (z - m) - T log s, so that masked classes (a type's lowest
+// value) that the teacher names leave the loss finite, where z / T, z - m or the sum of terms would leave fp32: halves of the terms do not.
 __device__ __forceinline__ void distill_loss(const Distill& a, int64_t i, const Sums& r, float w, const Teacher& te) {
-    const Exponent x(r.m, a.c);
-    const float log_s = log2f(r.s);
+    const float from = above(r.m), ln_s = log2f(r.s) * LN2;
     if (a.loss) {
         float term = 0.0f;
         for (int j = lane_id(); j < a.k; j += 64)
-            if (te.of[j].p != 0.0f) term += te.of[j].p * (te.log_p[j] - (r.s == 0.0f ? -INFINITY : (x(te.z[j]) - log_s) * LN2));
+            if (te.of[j].p != 0.0f) term += te.of[j].p * (r.s == 0.0f ? INFINITY : 0.5f * a.temperature * (te.log_p[j] + ln_s) - (0.5f * te.z[j] - 0.5f * from));
         term = Wave(nullptr).sum(term);
-        if (lane_id() == 0) a.loss[i] = w == 0.0f || !te.any ? 0.0f : w * a.temperature * a.temperature * term;
+        if (lane_id() == 0) a.loss[i] = w == 0.0f || !te.any ? 0.0f : 2.0f * (w * a.temperature * term);
     }
-    if (a.lse_out && lane_id() == 0) a.lse_out[i] = x.from * a.inv_t + log_s * LN2;
+    if (a.lse_out && lane_id() == 0) a.lse_out[i] = from * a.inv_t + ln_s;
 }
 
 // A class's share in the student's row, times `by`: from the row's sums, or from its lse. (A row of -inf alone has no share anywhere: the factor is 0
@@ -457,10 +464,9 @@ struct Logprobs {
     int32_t pieces, piece;
 };
 
-// log p of a logit, from the row's sums and the logarithm (to base 2) of their s
 __device__ __forceinline__ float log_share(const Logprobs& a, const Sums& r, float log_s, float z) {
     if (r.s != r.s) return NAN;
-    return z == -INFINITY ? -INFINITY : (Exponent(r.m, a.c)(z) - log_s) * LN2;
+    return z == -INFINITY ? -INFINITY : log_ratio(r, a.inv_t, log_s, z);
 }
 
 // A row's answer and its logit, requested before the sums that they wait for.

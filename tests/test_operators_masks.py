@@ -72,3 +72,70 @@ def test_entropy_of_rows_with_finite_masks(n, c, dt, low, t):
         close(lp, want_lp, sum_bound(c) + 8 * U * (1 + want_lp.abs()), "logprob")
         m = z.double().amax(1).abs() / t
         close(lse, want_lse.float(), sum_bound(c) + 4 * U * (m + want_lse.abs()), "lse")
+
+
+@pytest.mark.parametrize("n,c", ROUTES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("low", [None, -2.5e38, -1e9], ids=["lowest", "-2.5e38", "-1e9"])
+@pytest.mark.parametrize("t", [1.0, 2.0, 0.7])
+def test_log_probabilities_of_masked_classes(n, c, dt, low, t):
+    """A finite logit has a finite log probability wherever fp32 holds it: of an answer, and of an alternative."""
+    g = rng(c + 1)
+    z = masked_rows(n, c, dt, LOW[dt] if low is None else low, g)
+    z[9 % n] = LOW[dt]
+    z[9 % n, 3] = -LOW[dt]                          # differences that leave fp32 before their division by T
+    tok = torch.full((n,), c - 5, dtype=torch.int32, device="cuda")     # masked, but in a row with nothing left
+    log_p, _, _ = exact_rows(z, t)
+    k = 20
+    lp, _, _, ids, top = answers_of(z, tok, t, k)
+    bound = lambda want: sum_bound(c) + 8 * U * (1 + torch.where(want.isfinite(), want.abs(), 0.0))  # noqa: E731
+    want = log_p[:, c - 5].float()
+    close(lp, want, bound(want.double()), "logprob")
+    value, at = torch.sort(z.float(), dim=1, descending=True, stable=True)
+    want_ids = torch.where(value[:, :k] > -INF, at[:, :k], -1).to(torch.int32)
+    assert torch.equal(ids, want_ids)
+    want = log_p.gather(1, at[:, :k]).float()
+    close(top, want, bound(want.double()), "top")
+
+
+@pytest.mark.parametrize("n,c", ROUTES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("low", [None, -2.5e38, -1e9], ids=["lowest", "-2.5e38", "-1e9"])
+@pytest.mark.parametrize("t", [1.0, 2.0, 0.7])
+def test_losses_against_a_teacher_that_names_masked_classes(n, c, dt, low, t):
+    b, g = nb(), rng(c + 2)
+    z = masked_rows(n, c, dt, LOW[dt] if low is None else low, g)
+    k = 6
+    ids, tl = teacher(n, c, k, g)
+    ids[:, 0] = c - 5                               # masked, but in a row with nothing left
+    ids[:, 1:] = torch.randperm(c - 9, generator=g, device="cuda")[:k - 1].to(torch.int32)      # some of them masked too
+    log_q, _, want_lse = exact_rows(z, t)
+    log_p = torch.log_softmax(tl.double() / t, 1)
+    p, at = log_p.exp(), ids.long()
+    w = torch.rand((n,), generator=g, device="cuda") * 0.4 + 0.1
+    ql = log_q.gather(1, at)
+    by = w.double() * t * t
+    want = by * (p * (log_p - ql)).sum(1)
+    # a share's exponent, sum, quotient; its logarithm; the difference; the sum of k; log q's own sum
+    size = (p * (log_p.abs() + ql.abs())).sum(1)
+    tol = by * ((2 * k + 32) * U * size.nan_to_num(0.0, 0.0, 0.0) + sum_bound(c) + 8 * U)
+    loss, lse, grad = torch.empty((n,), device="cuda"), torch.empty((n,), device="cuda"), torch.empty_like(z)
+    ws = ws_of(b.no_distill_ws_bytes(n, c))
+    # the gradient, from the row's own sums: three roundings of an exponent, the sum's, quotient and products; the teacher's shares likewise
+    q = log_q.exp()
+    dense = torch.zeros_like(q).scatter_add_(1, at, p)
+    dense_size = torch.zeros_like(q).scatter_add_(1, at, p * (2 * k + 16 + 8 * log_p.abs()))
+    want_grad = (w.double() * t)[:, None] * (q - dense)
+    exponent = torch.where(q > 0, log_q, 0.0).abs()
+    grad_tol = (w.double() * t)[:, None] * (q * (sum_bound(c) + 8 * U * (1 + exponent)) + U * dense_size) + 2 * U * want_grad.abs() + TINY
+    for both in (True, False):
+        loss.fill_(77.0)
+        lse.fill_(77.0)
+        if both:
+            b.no_distill_fwd_bwd(z, ids, tl, t, w, loss, lse, grad, ws)
+            close(grad, want_grad, grad_tol + half(dt) * (want_grad.abs() + grad_tol), "grad")
+        else:
+            b.no_distill_fwd(z, ids, tl, t, w, loss, lse, ws)
+        close(loss, torch.where(want.isnan(), INF, want).float(), tol, "loss")
+        m = z.double().amax(1).abs() / t
+        close(lse, want_lse.float(), sum_bound(c) + 4 * U * (m + want_lse.abs()), "lse")
