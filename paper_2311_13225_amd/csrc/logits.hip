@@ -623,7 +623,8 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(RowsOf z, const int3
     Piece<T, U, TEAM, true> v;
     v.load(z.row<T>(i) + first, len, t);
     const int32_t tok = tokens[i];
-    const float l = lse[i], h = entropy[i], gl = g_logprob && tok >= 0 && tok < classes ? g_logprob[i] : 0.0f, gh = g_entropy ? g_entropy[i] : 0.0f;
+    const float l = lse[i], gl = g_logprob && tok >= 0 && tok < classes ? g_logprob[i] : 0.0f, gh = g_entropy ? g_entropy[i] : 0.0f;
+    const float h = g_entropy ? entropy[i] : 0.0f;      // (0 times an entropy that is not finite would be NaN)
     RowStore<T, W, true> store(grad.row<T>(i) + first, len);
 #pragma unroll
     for (int u = 0; u < U; ++u) {

@@ -139,3 +139,17 @@ def test_losses_against_a_teacher_that_names_masked_classes(n, c, dt, low, t):
         close(loss, torch.where(want.isnan(), INF, want).float(), tol, "loss")
         m = z.double().amax(1).abs() / t
         close(lse, want_lse.float(), sum_bound(c) + 4 * U * (m + want_lse.abs()), "lse")
+
+
+@pytest.mark.parametrize("n,c", ROUTES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_gradient_of_log_probabilities_does_not_read_an_entropy_without_a_gradient(n, c, dt):
+    b, g = nb(), rng(c + 3)
+    z = randn((n, c), g, dt)
+    tok = torch.randint(0, c, (n,), generator=g, device="cuda", dtype=torch.int32)
+    _, ent, lse, _, _ = answers_of(z, tok, 1.0)
+    gl, want, got = randn((n,), g), torch.empty_like(z), torch.empty_like(z)
+    b.no_logprobs_bwd(z, tok, 1.0, lse, ent, gl, torch.zeros_like(gl), want)
+    for other in (NAN, INF):
+        b.no_logprobs_bwd(z, tok, 1.0, lse, torch.full_like(ent, other), gl, None, got)
+        assert torch.equal(got, want)
