@@ -623,7 +623,10 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(RowsOf z, const int3
     Piece<T, U, TEAM, true> v;
     v.load(z.row<T>(i) + first, len, t);
     const int32_t tok = tokens[i];
-    const float l = lse[i], gl = g_logprob && tok >= 0 && tok < classes ? g_logprob[i] : 0.0f, gh = g_entropy ? g_entropy[i] : 0.0f;
+    // A row's lse is rounded: where that is more than a share's logarithm (rows masked throughout, by -1e9 or less) z / T - lse may come out far above 0, and beyond fp32 as inf - inf. No
+    // share is larger than 1, so no logarithm is above 0; an lse of -inf leaves no share. (The minimum drops a NaN: a row whose lse is one takes it from gl.)
+    const float given = lse[i], l = given == -INFINITY ? INFINITY : given, gh = g_entropy ? g_entropy[i] : 0.0f;
+    const float gl = given != given ? NAN : g_logprob && tok >= 0 && tok < classes ? g_logprob[i] : 0.0f;
     const float h = g_entropy ? entropy[i] : 0.0f;      // (0 times an entropy that is not finite would be NaN)
     RowStore<T, W, true> store(grad.row<T>(i) + first, len);
 #pragma unroll
@@ -633,7 +636,7 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(RowsOf z, const int3
         v.v[u].get(f);
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const float log_p = f[w] * inv_t - l, p = f[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(log_p * LOG2E);
+            const float log_p = fminf(f[w] * inv_t - l, 0.0f), p = __builtin_amdgcn_exp2f(log_p * LOG2E);
             const float d = p == 0.0f ? 0.0f : -(p * (gl + gh * (log_p + h)));
             f[w] = (first + c + w == tok ? gl + d : d) * inv_t;
         }

@@ -153,3 +153,42 @@ def test_gradient_of_log_probabilities_does_not_read_an_entropy_without_a_gradie
     for other in (NAN, INF):
         b.no_logprobs_bwd(z, tok, 1.0, lse, torch.full_like(ent, other), gl, None, got)
         assert torch.equal(got, want)
+
+
+def given_shares(z, lse, t):
+    """(log p, bound of p's relative error) by a stored lse, which stands rounded: exponents are off by its rounding and theirs."""
+    log_p = (z.double() / t - lse.double()[:, None]).clamp(max=0.0)
+    there = log_p > -200
+    size = torch.where(there, (z.double() / t).nan_to_num(0.0, 0.0, 0.0).abs() + lse.double().nan_to_num(0.0, 0.0, 0.0).abs()[:, None] + log_p.abs(), 0.0)
+    return log_p, 4 * U * size + 8 * U
+
+
+@pytest.mark.parametrize("n,c", ROUTES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("low", [None, -1e38, -1e9], ids=["lowest", "-1e38", "-1e9"])
+@pytest.mark.parametrize("t", [1.0, 2.0, 0.7])
+def test_gradient_of_log_probabilities_of_masked_rows(n, c, dt, low, t):
+    """Rows with classes left have their gradient; rows without, whose lse is rounded by more than their shares' logarithm or leaves fp32, stay within what shares of at most
+    1 can give."""
+    b, g = nb(), rng(c + 4)
+    z = masked_rows(n, c, dt, LOW[dt] if low is None else low, g)
+    tok = z.float().argmax(1).to(torch.int32)
+    _, ent, lse, _, _ = answers_of(z, tok, t)
+    gl, gh, grad = randn((n,), g), randn((n,), g), torch.empty_like(z)
+    for entropy in (True, False):
+        grad.fill_(77.0)
+        b.no_logprobs_bwd(z, tok, t, lse, ent, gl, gh if entropy else None, grad)
+        e, h = (gh.double()[:, None], ent.double()[:, None]) if entropy else (torch.zeros((n, 1), device="cuda", dtype=torch.float64),) * 2
+        l = gl.double()[:, None]
+        assert grad.isfinite().all()
+        most = (l.abs() + (l.abs() + e.abs() * (1 + h))).expand(n, c) / t
+        assert (grad.double().abs()[5:7] <= most[5:7] * (1 + half(dt) + 16 * U) + TINY).all()
+        rows = [i for i in range(n) if i not in (5, 6)]
+        log_p, rel = given_shares(z[rows], lse[rows], t)
+        p = log_p.exp()
+        hit = torch.zeros_like(p).scatter_(1, tok[rows].long()[:, None], 1.0)
+        lp = torch.where(p > 0, log_p, 0.0)
+        ref = (l[rows] * (hit - p) - e[rows] * p * (lp + h[rows])) / t
+        size = (l[rows].abs() * (hit + p) + e[rows].abs() * p * (lp.abs() + h[rows])) / t
+        tol = (rel + 8 * U) * size + rel * p * e[rows].abs() / t + TINY
+        close(grad[rows], ref, tol + half(dt) * (ref.abs() + tol), "grad")
