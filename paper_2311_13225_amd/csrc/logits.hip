@@ -198,10 +198,12 @@ struct ShareBySums {
     __device__ __forceinline__ ShareBySums(const Sums& r, float c, float by_) : x(r.m, c), by(r.s == 0.0f ? 0.0f : by_ / r.s) {}
     __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f(x(z)) * by; }
 };
+// (An lse is rounded, which may be more than a share's logarithm where a row is masked throughout, by -1e9 or less: no share is larger than 1, so no exponent is above 0. The
+// minimum drops a NaN; a row whose lse is one takes it from the factor.)
 struct ShareByLse {
     float inv_t, lse, by;
-    __device__ __forceinline__ ShareByLse(float inv_t_, float lse_, float by_) : inv_t(inv_t_), lse(lse_ == -INFINITY ? INFINITY : lse_), by(by_) {}
-    __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z * inv_t - lse) * LOG2E) * by; }
+    __device__ __forceinline__ ShareByLse(float inv_t_, float lse_, float by_) : inv_t(inv_t_), lse(lse_ == -INFINITY ? INFINITY : lse_), by(lse_ != lse_ ? NAN : by_) {}
+    __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f(fminf(z * inv_t - lse, 0.0f) * LOG2E) * by; }
 };
 
 // The gradient of values [first, first + len) of a row, held in `v`: w T q everywhere, then the classes that the teacher names once more with

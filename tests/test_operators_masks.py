@@ -192,3 +192,30 @@ def test_gradient_of_log_probabilities_of_masked_rows(n, c, dt, low, t):
         size = (l[rows].abs() * (hit + p) + e[rows].abs() * p * (lp.abs() + h[rows])) / t
         tol = (rel + 8 * U) * size + rel * p * e[rows].abs() / t + TINY
         close(grad[rows], ref, tol + half(dt) * (ref.abs() + tol), "grad")
+
+
+@pytest.mark.parametrize("n,c", ROUTES)
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("low", [None, -1e38, -1e9], ids=["lowest", "-1e38", "-1e9"])
+@pytest.mark.parametrize("t", [1.0, 2.0, 0.7])
+def test_gradient_of_the_loss_of_masked_rows_from_an_lse(n, c, dt, low, t):
+    b, g = nb(), rng(c + 5)
+    z = masked_rows(n, c, dt, LOW[dt] if low is None else low, g)
+    k = 6
+    ids, tl = teacher(n, c, k, g)
+    w = torch.rand((n,), generator=g, device="cuda") * 0.4 + 0.1
+    loss, lse, grad = torch.empty((n,), device="cuda"), torch.empty((n,), device="cuda"), torch.full_like(z, 77.0)
+    b.no_distill_fwd(z, ids, tl, t, w, loss, lse, ws_of(b.no_distill_ws_bytes(n, c)))
+    b.no_distill_bwd(z, ids, tl, t, w, lse, grad)
+    assert grad.isfinite().all()
+    log_p = torch.log_softmax(tl.double() / t, 1)
+    dense = torch.zeros_like(z, dtype=torch.float64).scatter_add_(1, ids.long(), log_p.exp())
+    dense_size = torch.zeros_like(dense).scatter_add_(1, ids.long(), log_p.exp() * (2 * k + 16 + 8 * log_p.abs()))
+    by = (w.double() * t)[:, None]
+    assert (grad.double().abs()[5:7] <= (by * (1 + dense))[5:7] * (1 + half(dt) + 128 * U)).all()      # nothing left: shares of at most 1
+    rows = [i for i in range(n) if i not in (5, 6)]
+    log_q, rel = given_shares(z[rows], lse[rows], t)
+    q = log_q.exp()
+    ref = by[rows] * (q - dense[rows])
+    tol = by[rows] * (rel * q + U * dense_size[rows]) + 2 * U * ref.abs() + TINY
+    close(grad[rows], ref, tol + half(dt) * (ref.abs() + tol), "grad")
