@@ -332,11 +332,12 @@ int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride_bytes, con
                        float* d_grad_weight, void* d_ws, size_t ws_bytes, void* stream);
 
 /* Distillation from a teacher's top logits. A row has k entries (d_teacher_ids int32 [n, k], d_teacher_logits fp32 [n, k], dense); an entry whose id
- * lies outside [0, n_classes) is left out. p = softmax(teacher logits / T) over the row's entries (an id may stand twice: its shares add up),
+ * lies outside [0, n_classes) is left out. p_j = softmax(teacher logits / T) over the row's entries j,
  * log q = z / T - lse, lse = log sum exp(z / T) over all classes of the student's row d_z (dt: NO_F32 or NO_BF16), and with the row's weight w
  * (d_row_weight fp32 [n], NULL: 1):
- *   d_loss[i] = w T^2 sum p (log p - log q)        d_grad_z[i, c] = w T (q_c - p_c), of type dt
- * The factor T^2 keeps the gradient's size as T grows. A row of weight 0 has loss 0 and gradient 0 whatever it holds, and so has a row without
+ *   d_loss[i] = w T^2 sum over j of p_j (log p_j - log q_(id_j))        d_grad_z[i, c] = w T (q_c - sum of p_j over the j with id_j = c), of type dt
+ * The factor T^2 keeps the gradient's size as T grows. An id may stand twice in a row: its shares add up in the gradient, while the loss counts entry by entry, which is
+ * less than the divergence from the added shares by w T^2 times the entropy of the split (so it may be negative), a number that no logit changes. A row of weight 0 has loss 0 and gradient 0 whatever it holds, and so has a row without
  * entries above -inf. A logit of -inf takes part in nothing (q = 0): the loss is +inf where the teacher gives it a share. +inf or NaN in a row
  * make the row's results NaN.
  * no_distill_fwd stores d_loss and d_lse (fp32 [n]); no_distill_bwd takes that d_lse (an upstream gradient of the losses goes into the

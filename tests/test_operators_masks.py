@@ -219,3 +219,30 @@ def test_gradient_of_the_loss_of_masked_rows_from_an_lse(n, c, dt, low, t):
     ref = by[rows] * (q - dense[rows])
     tol = by[rows] * (rel * q + U * dense_size[rows]) + 2 * U * ref.abs() + TINY
     close(grad[rows], ref, tol + half(dt) * (ref.abs() + tol), "grad")
+
+
+@pytest.mark.parametrize("n,c", [(10, 172), (10, 40_003), (2, 131_072), (3, 200_001)])
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_an_id_that_stands_twice_counts_entry_by_entry_in_the_loss_and_once_in_the_gradient(n, c, dt):
+    """Halved shares of the same classes: the gradient of the whole shares, and a loss that is less by log 2, whatever the logits."""
+    b, g, t = nb(), rng(c + 6), 2.0
+    z, k = randn((n, c), g, dt), 4
+    ids, tl = teacher(n, c, k, g)
+    w = torch.rand((n,), generator=g, device="cuda") + 0.5
+    ws = ws_of(b.no_distill_ws_bytes(n, c))
+    loss, grad = [torch.empty((n,), device="cuda") for _ in range(2)], [torch.empty_like(z) for _ in range(2)]
+    b.no_distill_fwd_bwd(z, ids, tl, t, w, loss[0], None, grad[0], ws)
+    b.no_distill_fwd_bwd(z, ids.repeat(1, 2).contiguous(), tl.repeat(1, 2).contiguous(), t, w, loss[1], None, grad[1], ws)
+    log_q, _, _ = exact_rows(z, t)
+    log_p = torch.log_softmax(tl.double() / t, 1)
+    p, ql = log_p.exp(), log_q.gather(1, ids.long())
+    by = w.double() * t * t
+    want = by * (p * (log_p - ql)).sum(1)
+    tol = by * ((4 * k + 32) * U * (p * (log_p.abs() + 1 + ql.abs())).sum(1) + sum_bound(c) + 8 * U)
+    close(loss[0], want, tol, "loss")
+    close(loss[1], want - by * torch.log(torch.tensor(2.0, dtype=torch.float64)), tol, "loss of halved shares")
+    # each of the two gradients: its own bound around the same value
+    size = (w.double() * t)[:, None] * (log_q.exp() * (sum_bound(c) + 8 * U * (1 + log_q.abs())) + U * torch.zeros_like(log_q).scatter_add_(1, ids.long(), p * (4 * k + 16 + 8 * (log_p.abs() + 1))))
+    ref = (w.double() * t)[:, None] * (log_q.exp() - torch.zeros_like(log_q).scatter_add_(1, ids.long(), p))
+    for at in (0, 1):
+        close(grad[at], ref, size + 2 * U * ref.abs() + half(dt) * (ref.abs() + size) + TINY, "grad")
