@@ -303,8 +303,8 @@ int32_t no_embed_fwd(const void* d_table, no_dtype dt, int64_t n_rows, int32_t d
 /* Its gradient: d_grad_table[v, :] = scale * sum of d_grad_out[i, :] over the i < n with d_ids[i] == v, fp32; rows that no id names become zeros,
  * or, with accumulate != 0, the sum is added to what is there and other rows are left alone. (With accumulate, scale = -learning rate
  * times the forward scale and d_grad_table an fp32 table itself, the call is the update of plain SGD.) Ids outside [0, n_rows) add nothing.
- * dt: type of d_grad_out, NO_F32 or NO_BF16. The order of a row's sum is that of the positions i, in runs whose
- * length depends on the sizes alone: the same ids give the same bits. */
+ * dt: type of d_grad_out, NO_F32 or NO_BF16. A row's sum takes its positions i in ascending order, in runs that are added up in order; where the runs end depends on
+ * the sizes and on the ids (how many positions a row has, and where they stand among all), not on timing: the same ids give the same bits. */
 size_t no_embed_ws_bytes(int32_t n_ids_cap, int32_t dim);
 int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t grad_stride_bytes, const int32_t* d_ids, const int32_t* d_n_ids,
                      int32_t n_ids_cap, float scale, int32_t accumulate, float* d_grad_table, int64_t n_rows, int32_t dim,
