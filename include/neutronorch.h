@@ -315,7 +315,8 @@ int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t grad_stride_by
  * Outputs: d_sum (NULL: not stored) takes s; d_rstd fp32 [n] (may be NULL); d_y of dt_y: NO_F32, NO_BF16, or NO_E4M3, then
  * d_row_scale fp32 [n] takes max(max |y|, 2^-100) / 448 of each row and d_y holds y divided by it (NULL otherwise). d_sum may be d_x or d_residual
  * itself, and so may d_y where dt_y == dt (same address and stride; two outputs never share an array); no other overlap. A row whose
- * squares leave fp32 (|s| beyond 1.8e19, infinities, NaN) has rstd 0 or NaN and y = s * rstd * weight by that; in NO_E4M3 all of it is NaN, its scale too. */
+ * squares leave fp32 (|s| beyond 1.8e19, infinities, NaN) has rstd 0 or NaN and y = s * rstd * weight by that; in NO_E4M3 all of it is NaN, its scale too.
+ * With eps == 0 the rstd of a row of zeros, or of values whose squares vanish in fp32 (|s| below 1e-23), is infinite. */
 int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_residual, int64_t residual_stride_bytes,
                        const float* d_weight, float eps, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t dim, void* d_sum,
                        int64_t sum_stride_bytes, void* d_y, no_dtype dt_y, int64_t y_stride_bytes, float* d_row_scale, float* d_rstd,
@@ -324,7 +325,7 @@ int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, con
 /* Its gradients: with u = d_s * d_rstd and wg = d_weight * d_grad_y: d_grad_x = d_rstd (wg - u * mean(wg * u)) + d_grad_sum, the gradient of x and
  * of the residual alike (d_grad_sum: the gradient that reaches s itself, NULL: none); d_grad_weight fp32 [dim] = sum over the rows of d_grad_y * u
  * (overwritten; NULL: not computed). d_s is what the forward pass stored in d_sum (or its d_x). dt: type of d_s, d_grad_y, d_grad_sum and
- * d_grad_x. d_grad_x may be d_grad_y, d_grad_sum or d_s itself (same address and stride). */
+ * d_grad_x. d_grad_x may be d_grad_y, d_grad_sum or d_s itself (same address and stride). The workspace is asked for whether d_grad_weight is NULL or not. */
 size_t no_rmsnorm_ws_bytes(int32_t n_rows_cap, int32_t dim);
 int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride_bytes, const float* d_weight, const float* d_rstd,
                        const void* d_grad_y, int64_t grad_y_stride_bytes, const void* d_grad_sum, int64_t grad_sum_stride_bytes,
@@ -341,7 +342,10 @@ int32_t no_rmsnorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride_bytes, con
  * entries above -inf. A logit of -inf takes part in nothing (q = 0): the loss is +inf where the teacher gives it a share. +inf or NaN in a row
  * make the row's results NaN.
  * no_distill_fwd stores d_loss and d_lse (fp32 [n]); no_distill_bwd takes that d_lse (an upstream gradient of the losses goes into the
- * weights); no_distill_fwd_bwd makes all of it at once (d_lse may be NULL). d_grad_z may be d_z itself (same stride). */
+ * weights); no_distill_fwd_bwd makes all of it at once (d_lse may be NULL). d_grad_z may be d_z itself (same stride).
+ * Large negative finite masks are logits like others: loss, lse and the gradient of fwd_bwd are right under them, also where a row holds nothing else. The gradient from an lse
+ * takes q as exp(z / T - lse), at most 1, so its rows are as good as the lse's rounding: a row masked throughout by -1e9 or less has shares between 0 and 1 there, not 1 / n_classes, and
+ * none at all where its lse is -inf, beyond fp32. */
 size_t no_distill_ws_bytes(int32_t n_rows_cap, int32_t n_classes);
 int32_t no_distill_fwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
                        const int32_t* d_teacher_ids, const float* d_teacher_logits, int32_t k, float temperature, const float* d_row_weight,
@@ -361,7 +365,8 @@ int32_t no_distill_fwd_bwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes,
  *   ascending class. Logits of -inf are no alternatives: places left over hold -1 and -inf.
  * A row of -inf alone has lse = -inf, log p = -inf and entropy 0; +inf or NaN in a row make its numbers NaN and its alternatives -1.
  * Backward: d_grad_z[i, c] = (g_lp ([c == token] - p_c) - g_H p_c (log p_c + H)) / T with the forward pass's d_lse and d_entropy and the gradients
- * d_grad_logprob, d_grad_entropy (either may be NULL: 0); a position without an answer takes no g_lp. d_grad_z (of dt) may be d_z itself. */
+ * d_grad_logprob, d_grad_entropy (either may be NULL: 0; the entropies are not read without a gradient of theirs); a position without an answer takes no g_lp. d_grad_z (of dt)
+ * may be d_z itself. Finite masks: as for no_distill_*; p from the rounded lse is at most 1, and 0 where that is -inf. */
 size_t no_logprobs_ws_bytes(int32_t n_rows_cap, int32_t n_classes, int32_t k);
 int32_t no_logprobs_fwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
                         const int32_t* d_tokens, float temperature, float* d_logprob, float* d_entropy, float* d_lse, int32_t k,
