@@ -315,7 +315,7 @@ int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t grad_stride_by
  * Outputs: d_sum (NULL: not stored) takes s; d_rstd fp32 [n] (may be NULL); d_y of dt_y: NO_F32, NO_BF16, or NO_E4M3, then
  * d_row_scale fp32 [n] takes max(max |y|, 2^-100) / 448 of each row and d_y holds y divided by it (NULL otherwise). d_sum may be d_x or d_residual
  * itself, and so may d_y where dt_y == dt (same address and stride; two outputs never share an array); no other overlap. A row whose
- * squares leave fp32 (|s| beyond 1.8e19, infinities, NaN) has rstd 0 or NaN and y = s * rstd * weight by that; in NO_E4M3 all of it is NaN, its scale too.
+ * sum of squares leaves fp32 (beyond 3.4e38; infinities, NaN) has rstd 0 or NaN and y = s * rstd * weight by that; in NO_E4M3 all of it is NaN, its scale too.
  * With eps == 0 the rstd of a row of zeros, or of values whose squares vanish in fp32 (|s| below 1e-23), is infinite. */
 int32_t no_rmsnorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_residual, int64_t residual_stride_bytes,
                        const float* d_weight, float eps, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t dim, void* d_sum,
