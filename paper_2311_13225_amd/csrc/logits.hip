@@ -180,14 +180,14 @@ struct Entries {        // a lane's entries as they come from memory
 // value) that the teacher names leave the loss finite, where z / T, z - m or the sum of terms would leave fp32: halves of the terms do not.
 __device__ __forceinline__ void distill_loss(const Distill& a, int64_t i, const Sums& r, float w, const Teacher& te) {
     const float from = above(r.m), ln_s = log2f(r.s) * LN2;
-    if (a.loss) {
-        float term = 0.0f;
-        for (int j = lane_id(); j < a.k; j += 64)
-            if (te.of[j].p != 0.0f) term += te.of[j].p * (r.s == 0.0f ? INFINITY : 0.5f * a.temperature * (te.log_p[j] + ln_s) - (0.5f * te.z[j] - 0.5f * from));
-        term = Wave(nullptr).sum(term);
-        if (lane_id() == 0) a.loss[i] = w == 0.0f || !te.any ? 0.0f : 2.0f * (w * a.temperature * term);
+    float term = 0.0f;
+    for (int j = lane_id(); j < a.k; j += 64)
+        if (te.of[j].p != 0.0f) term += te.of[j].p * (r.s == 0.0f ? INFINITY : 0.5f * a.temperature * (te.log_p[j] + ln_s) - (0.5f * te.z[j] - 0.5f * from));
+    term = Wave(nullptr).sum(term);
+    if (lane_id() == 0) {
+        a.loss[i] = w == 0.0f || !te.any ? 0.0f : 2.0f * (w * a.temperature * term);
+        if (a.lse_out) a.lse_out[i] = from * a.inv_t + ln_s;
     }
-    if (a.lse_out && lane_id() == 0) a.lse_out[i] = from * a.inv_t + ln_s;
 }
 
 // A class's share in the student's row, times `by`: from the row's sums, or from its lse. (A row of -inf alone has no share anywhere: the factor is 0
@@ -267,11 +267,12 @@ __global__ void __launch_bounds__(THREADS) distill_row_kernel(Distill a) {
         e.load_logits(z, a.classes, 0, a.classes);
         e.shares(a, te);
     }
-    if (a.lse_in) {
-        team.sync();
-        distill_grad(a, i, 0, a.classes, v, ShareByLse(a.inv_t, a.lse_in[i], w * a.temperature), w, te, team);
-        return;
-    }
+    if constexpr (TEAM == 64)       // (longer rows go in pieces where an lse is given)
+        if (a.lse_in) {
+            team.sync();
+            distill_grad(a, i, 0, a.classes, v, ShareByLse(a.inv_t, a.lse_in[i], w * a.temperature), w, te, team);
+            return;
+        }
     const Sums r = team_sums<false>(v.template lane_sums<false>(a.c), a.c, team);
     v.renew();
     if constexpr (TEAM == 64) team.sync();      // (the entries; in larger teams a sum's barrier stood between)

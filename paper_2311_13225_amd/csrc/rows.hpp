@@ -19,7 +19,6 @@ static inline int32_t size_of(no_dtype dt) { return dt == NO_F32 ? 4 : dt == NO_
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(bf16_t v) { return (float)v; }
-__device__ __forceinline__ float to_f32(e4m3_t v) { return __builtin_amdgcn_cvt_f32_fp8((int)v.bits, 0); }
 template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float v) { return (bf16_t)v; }
