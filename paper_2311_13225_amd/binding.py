@@ -459,10 +459,14 @@ _OP_SIZES = {torch.float32: 4, torch.bfloat16: 2, torch.float8_e4m3fn: 1}
 # These calls take a few microseconds on the device, so their checks ask a tensor for as little as they can.
 
 
+# The current stream's address without the object around it, where this torch has that (the name is not a public one).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_of(stream) -> int:
-    """_stream, with the current stream's address asked for without the object around it."""
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    """_stream, with the current stream's address asked for without the object around it if that can be."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return _stream(stream)
 
 

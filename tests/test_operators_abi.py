@@ -93,3 +93,15 @@ def test_binding_refuses_other_types_and_shapes():
         b.no_logprobs_bwd(x, torch.zeros(3, dtype=torch.int32), 1.0, x[:, 0], x[:, 0], None, None, x)
     with pytest.raises(AssertionError):
         b.no_distill_fwd(x, torch.zeros((3, 1), dtype=torch.int32), torch.zeros((3, 1)), 1.0, None, x[:, 0], x[:, 0], x)
+
+
+def test_binding_finds_the_current_stream_with_public_names_alone(monkeypatch):
+    """torch's shorter way to the stream's address is taken where it exists, and not needed."""
+    from paper_2311_13225_amd import binding as b
+    asked = []
+    monkeypatch.setattr(b, "_stream", lambda stream=None: asked.append(stream) or 11)
+    monkeypatch.setattr(b, "_raw_stream", None)
+    assert b._stream_of(None) == 11 and b._stream_of("a stream") == 11 and asked == [None, "a stream"]
+    monkeypatch.setattr(b.torch.cuda, "current_device", lambda: 5)
+    monkeypatch.setattr(b, "_raw_stream", lambda device: 100 + device)
+    assert b._stream_of(None) == 105 and b._stream_of("a stream") == 11
