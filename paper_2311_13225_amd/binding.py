@@ -459,14 +459,16 @@ _OP_SIZES = {torch.float32: 4, torch.bfloat16: 2, torch.float8_e4m3fn: 1}
 # These calls take a few microseconds on the device, so their checks ask a tensor for as little as they can.
 
 
-# The current stream's address without the object around it, where this torch has that (the name is not a public one).
+# The current stream's address without the object around it, and the device without a look at whether CUDA is up, where this torch has them (the names are not public ones): 0.22 us a
+# call, by the public device 0.37, by the stream's object 2.9.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream_of(stream) -> int:
     """_stream, with the current stream's address asked for without the object around it if that can be."""
     if stream is None and _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_current_device())
     return _stream(stream)
 
 

@@ -102,6 +102,6 @@ def test_binding_finds_the_current_stream_with_public_names_alone(monkeypatch):
     monkeypatch.setattr(b, "_stream", lambda stream=None: asked.append(stream) or 11)
     monkeypatch.setattr(b, "_raw_stream", None)
     assert b._stream_of(None) == 11 and b._stream_of("a stream") == 11 and asked == [None, "a stream"]
-    monkeypatch.setattr(b.torch.cuda, "current_device", lambda: 5)
+    monkeypatch.setattr(b, "_current_device", lambda: 5)
     monkeypatch.setattr(b, "_raw_stream", lambda device: 100 + device)
     assert b._stream_of(None) == 105 and b._stream_of("a stream") == 11
