@@ -287,7 +287,7 @@ int32_t no_gcn_layer_bwd(const no_block_view* blk, no_arch form, int32_t d_in, c
 
 enum {
     NO_MAX_EMBED_DIM = 1 << 20,    /* widest row of no_embed_* */
-    NO_MAX_NORM_DIM = 65536,       /* widest row of no_rmsnorm_* */
+    NO_MAX_NORM_DIM = 65536,       /* widest row of no_rmsnorm_* and no_layernorm_* */
     NO_MAX_CLASSES = 1 << 22,      /* widest row of no_distill_* and no_logprobs_* */
     NO_MAX_TEACHER = 256,          /* teacher entries a row */
     NO_MAX_ALTERNATIVES = 64       /* alternatives a row */
@@ -374,6 +374,59 @@ int32_t no_logprobs_fwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, co
 int32_t no_logprobs_bwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
                         const int32_t* d_tokens, float temperature, const float* d_lse, const float* d_entropy,
                         const float* d_grad_logprob, const float* d_grad_entropy, void* d_grad_z, int64_t grad_stride_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Operators of a dense block and of its update: layer norm, the dense layer by itself, orthogonalised updates
+ *
+ * They keep to what the operators above have in common.
+ * ---------------------------------------------------------------------------------------- */
+
+enum {
+    NO_MAX_LINEAR_DIM = 1 << 20,   /* longest side of a matrix of no_linear_* */
+    NO_MAX_UPDATE_DIM = 32768      /* longest side of a matrix of no_orthogonalise and no_muon_step */
+};
+
+/* Layer norm of rows: s = d_x + d_residual rounded to dt (s = d_x where d_residual is NULL), mean of s, rstd = 1 / sqrt(mean of (s - mean)^2 + eps),
+ * y = (s - mean) * rstd * d_weight + d_bias (1 and 0 where they are NULL). dt: type of d_x, d_residual and d_sum, dt_y: type of d_y: NO_F32 or NO_BF16.
+ * Outputs: d_sum (NULL: not stored) takes s; d_mean and d_rstd fp32 [n] (either may be NULL); d_y. d_sum may be d_x or d_residual itself, and so may d_y where
+ * dt_y == dt (same address and stride; two outputs never share an array); no other overlap. The mean is subtracted before the squares are summed, so a row's level does not cost
+ * digits. A row whose sum or sum of squares leaves fp32 (infinities, NaN) has results that are NaN or 0 by that. With eps == 0 the rstd of a row of equal values is infinite and its y NaN. */
+int32_t no_layernorm_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_residual, int64_t residual_stride_bytes,
+                         const float* d_weight, const float* d_bias, float eps, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t dim,
+                         void* d_sum, int64_t sum_stride_bytes, void* d_y, no_dtype dt_y, int64_t y_stride_bytes, float* d_mean,
+                         float* d_rstd, void* stream);
+
+/* Its gradients: with u = (d_s - d_mean) * d_rstd and wg = d_weight * d_grad_y: d_grad_x = d_rstd (wg - mean(wg) - u * mean(wg * u)) + d_grad_sum, the gradient of x and of the
+ * residual alike (d_grad_sum: the gradient that reaches s itself, NULL: none); d_grad_weight fp32 [dim] = sum over the rows of d_grad_y * u, d_grad_bias fp32 [dim] = sum of d_grad_y
+ * (overwritten; NULL: not computed). d_s is what the forward pass stored in d_sum (or its d_x). dt: type of d_s, d_grad_y, d_grad_sum and d_grad_x. d_grad_x may be d_grad_y, d_grad_sum
+ * or d_s itself (same address and stride). The workspace is asked for whichever gradients are wanted. */
+size_t no_layernorm_ws_bytes(int32_t n_rows_cap, int32_t dim);
+int32_t no_layernorm_bwd(const void* d_s, no_dtype dt, int64_t s_stride_bytes, const float* d_weight, const float* d_mean, const float* d_rstd,
+                         const void* d_grad_y, int64_t grad_y_stride_bytes, const void* d_grad_sum, int64_t grad_sum_stride_bytes,
+                         const int32_t* d_n_rows, int32_t n_rows_cap, int32_t dim, void* d_grad_x, int64_t grad_x_stride_bytes,
+                         float* d_grad_weight, float* d_grad_bias, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Activations. NO_ACT_GELU: z times the standard normal distribution's share below z (by the error function); NO_ACT_SILU: z / (1 + exp(-z)). */
+typedef enum { NO_ACT_NONE = 0, NO_ACT_RELU = 1, NO_ACT_GELU = 2, NO_ACT_SILU = 3 } no_act;
+
+/* Dense layer: z = d_x * d_w + d_bias, y = act(z) + d_residual, for rows d_x [n, d_in] and a matrix d_w [d_in, d_out]. dt: type of d_x, d_w, d_residual, d_z and d_y, NO_F32 or NO_BF16;
+ * d_bias fp32 [d_out] (NULL: 0). d_z (NULL: not stored) takes z for the backward pass; the activation is taken of the sums before that rounding. d_y and d_z may not overlap what
+ * the call reads, but d_y may be d_residual itself (same address and stride). bf16 operands are multiplied as they are and summed in fp32. fp32 operands are multiplied in three bf16 pieces
+ * each (the six largest of nine products, summed in fp32), no less exact than in fp32; there an operand that is infinite, NaN or above 3.38e38 makes the sums that it meets NaN, and one below 2^-110 is taken
+ * with fewer digits. The few-row form (up to 8 rows) multiplies in fp32.
+ * One workspace size holds for the forward and the backward call. */
+size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_in, int32_t d_out);
+int32_t no_linear_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_w, int64_t w_stride_bytes, const float* d_bias, no_act act,
+                      const void* d_residual, int64_t residual_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t d_in, int32_t d_out,
+                      void* d_z, int64_t z_stride_bytes, void* d_y, int64_t y_stride_bytes, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Its gradients: gz = d_grad_y * act'(d_z) (rounded to bf16 where dt is NO_BF16, as the operand of both products; d_z may be NULL for NO_ACT_NONE; at z == 0 the slope of NO_ACT_RELU is 0);
+ * d_grad_x [n, d_in] = gz * d_w^T, d_grad_w [d_in, d_out] = d_x^T * gz, both of dt; d_grad_bias fp32 [d_out] = column sums of gz before it is rounded. Each may be NULL (not computed; d_w is
+ * read for d_grad_x alone, d_x for d_grad_w alone) and is overwritten. The residual's gradient is d_grad_y. With no rows d_grad_w and d_grad_bias are zeros. Outputs overlap nothing. */
+int32_t no_linear_bwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_w, int64_t w_stride_bytes, no_act act, const void* d_z,
+                      int64_t z_stride_bytes, const void* d_grad_y, int64_t grad_y_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t d_in,
+                      int32_t d_out, void* d_grad_x, int64_t grad_x_stride_bytes, void* d_grad_w, int64_t grad_w_stride_bytes, float* d_grad_bias, void* d_ws,
+                      size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
  * Whole step (loop body of Algorithm 1 with plain SGD, plus hot-embedding reuse)

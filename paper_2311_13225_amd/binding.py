@@ -20,6 +20,8 @@ LIB_PATH = os.path.join(_HERE, "libneutronorch.so")
 NO_F32, NO_BF16, NO_E4M3 = 0, 1, 2
 NO_ARCH_SAGE_MEAN, NO_ARCH_GCN, NO_ARCH_GCN_SUM, NO_ARCH_GCN_SYM = 0, 1, 2, 3
 ARCH_OF_NAME = {"sage": NO_ARCH_SAGE_MEAN, "gcn": NO_ARCH_GCN, "gcn_sum": NO_ARCH_GCN_SUM, "gcn_sym": NO_ARCH_GCN_SYM}
+NO_ACT_NONE, NO_ACT_RELU, NO_ACT_GELU, NO_ACT_SILU = 0, 1, 2, 3
+ACT_OF_NAME = {"none": NO_ACT_NONE, "relu": NO_ACT_RELU, "gelu": NO_ACT_GELU, "silu": NO_ACT_SILU}
 NO_CSR_INPUT_ON_DEVICE, NO_CSR_IDS_64, NO_CSR_SYMMETRISE, NO_CSR_DEDUP = 1, 2, 4, 8
 NO_MAX_LAYERS = 8
 ERROR_NAMES = {0: "NO_OK", -1: "NO_ERR_INVALID_ARG", -2: "NO_ERR_OUT_OF_RANGE", -3: "NO_ERR_CAPACITY",
@@ -82,6 +84,12 @@ _SIGNATURES = {
     "no_rmsnorm_fwd": (_I32, [_P, _I32, _I64, _P, _I64, _P, C.c_float, _P, _I32, _I32, _P, _I64, _P, _I32, _I64, _P, _P, _P]),
     "no_rmsnorm_ws_bytes": (C.c_size_t, [_I32, _I32]),
     "no_rmsnorm_bwd": (_I32, [_P, _I32, _I64, _P, _P, _P, _I64, _P, _I64, _P, _I32, _I32, _P, _I64, _P, _P, C.c_size_t, _P]),
+    "no_layernorm_fwd": (_I32, [_P, _I32, _I64, _P, _I64, _P, _P, C.c_float, _P, _I32, _I32, _P, _I64, _P, _I32, _I64, _P, _P, _P]),
+    "no_layernorm_ws_bytes": (C.c_size_t, [_I32, _I32]),
+    "no_layernorm_bwd": (_I32, [_P, _I32, _I64, _P, _P, _P, _P, _I64, _P, _I64, _P, _I32, _I32, _P, _I64, _P, _P, _P, C.c_size_t, _P]),
+    "no_linear_ws_bytes": (C.c_size_t, [_I32, _I32, _I32, _I32]),
+    "no_linear_fwd": (_I32, [_P, _I32, _I64, _P, _I64, _P, _I32, _P, _I64, _P, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, C.c_size_t, _P]),
+    "no_linear_bwd": (_I32, [_P, _I32, _I64, _P, _I64, _I32, _P, _I64, _P, _I64, _P, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, C.c_size_t, _P]),
     "no_distill_ws_bytes": (C.c_size_t, [_I32, _I32]),
     "no_distill_fwd": (_I32, [_P, _I32, _I64, _P, _I32, _I32, _P, _P, _I32, C.c_float, _P, _P, _P, _P, C.c_size_t, _P]),
     "no_distill_bwd": (_I32, [_P, _I32, _I64, _P, _I32, _I32, _P, _P, _I32, C.c_float, _P, _P, _P, _I64, _P]),
@@ -623,6 +631,68 @@ def no_logprobs_bwd(z: torch.Tensor, tokens: torch.Tensor, temperature: float, l
     (pz, sz), (pg, sg) = _rows(z, n, c), _rows(grad_z, n, c, z.dtype)
     _check(lib().no_logprobs_bwd(pz, _code(z), sz, _count(n_rows), n, c, _vec(tokens, n, torch.int32), temperature,
                                  _vec(lse, n), _vec(entropy, n), _vec(grad_logprob, n), _vec(grad_entropy, n), pg, sg, _stream_of(stream)))
+
+
+# ------------------------------------------------------------------------------------------ dense block and its update
+
+NO_MAX_LINEAR_DIM, NO_MAX_UPDATE_DIM = 1 << 20, 32768
+
+
+def no_layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], eps: float, y: torch.Tensor,
+                     residual: Optional[torch.Tensor] = None, sum_out: Optional[torch.Tensor] = None,
+                     mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                     n_rows: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """s = x + residual (rounded to x's type, stored in sum_out), y = (s - mean) * rstd * weight + bias in y's type, float32 or bfloat16."""
+    n, dim = x.shape
+    (px, sx), (pr, sr), (ps, ss), (py, sy) = _rows(x, n, dim), _rows(residual, n, dim, x.dtype), _rows(sum_out, n, dim, x.dtype), _rows(y, n, dim)
+    _check(lib().no_layernorm_fwd(px, _code(x), sx, pr, sr, _vec(weight, dim), _vec(bias, dim), eps, _count(n_rows), n, dim, ps, ss,
+                                  py, _code(y), sy, _vec(mean, n), _vec(rstd, n), _stream_of(stream)))
+    return y
+
+
+def no_layernorm_ws_bytes(n_rows_cap: int, dim: int) -> int:
+    return int(lib().no_layernorm_ws_bytes(n_rows_cap, dim))
+
+
+def no_layernorm_bwd(s: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor, grad_y: torch.Tensor,
+                     grad_x: torch.Tensor, grad_weight: Optional[torch.Tensor], grad_bias: Optional[torch.Tensor], ws: torch.Tensor,
+                     grad_sum: Optional[torch.Tensor] = None, n_rows: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of no_layernorm_fwd: grad_x (of x and of the residual alike, grad_sum added), grad_weight and grad_bias."""
+    n, dim = s.shape
+    (ps, ss), (pg, sg), (pa, sa) = _rows(s, n, dim), _rows(grad_y, n, dim, s.dtype), _rows(grad_sum, n, dim, s.dtype)
+    (px, sx), (pw, bw) = _rows(grad_x, n, dim, s.dtype), _ws(ws)
+    _check(lib().no_layernorm_bwd(ps, _code(s), ss, _vec(weight, dim), _vec(mean, n), _vec(rstd, n), pg, sg, pa, sa, _count(n_rows), n,
+                                  dim, px, sx, _vec(grad_weight, dim), _vec(grad_bias, dim), pw, bw, _stream_of(stream)))
+
+
+def no_linear_ws_bytes(dtype: torch.dtype, n_rows_cap: int, d_in: int, d_out: int) -> int:
+    return int(lib().no_linear_ws_bytes(_OP_DTYPES.get(dtype, -1), n_rows_cap, d_in, d_out))
+
+
+def no_linear_fwd(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], act: int, y: torch.Tensor, ws: torch.Tensor,
+                  residual: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None, n_rows: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """y = act(x w + bias) + residual for rows x [n, d_in] and a matrix w [d_in, d_out], float32 or bfloat16 throughout (bias float32);
+    z takes the pre-activation for no_linear_bwd. act: one of NO_ACT_*."""
+    (n, d_in), d_out = x.shape, w.shape[1]
+    dt = x.dtype
+    (px, sx), (pw, sw), (pr, sr) = _rows(x, n, d_in), _rows(w, d_in, d_out, dt), _rows(residual, n, d_out, dt)
+    (pz, sz), (py, sy), (pb, bb) = _rows(z, n, d_out, dt), _rows(y, n, d_out, dt), _ws(ws)
+    _check(lib().no_linear_fwd(px, _code(x), sx, pw, sw, _vec(bias, d_out), act, pr, sr, _count(n_rows), n, d_in, d_out, pz, sz, py, sy,
+                               pb, bb, _stream_of(stream)))
+    return y
+
+
+def no_linear_bwd(x: torch.Tensor, w: torch.Tensor, act: int, z: Optional[torch.Tensor], grad_y: torch.Tensor,
+                  grad_x: Optional[torch.Tensor], grad_w: Optional[torch.Tensor], grad_bias: Optional[torch.Tensor], ws: torch.Tensor,
+                  n_rows: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of no_linear_fwd from the pre-activation z that it stored (None for NO_ACT_NONE); each of the three may be None."""
+    (n, d_in), d_out = x.shape, w.shape[1]
+    dt = x.dtype
+    (px, sx), (pw, sw), (pz, sz), (pg, sg) = _rows(x, n, d_in), _rows(w, d_in, d_out, dt), _rows(z, n, d_out, dt), _rows(grad_y, n, d_out, dt)
+    (pgx, sgx), (pgw, sgw), (pb, bb) = _rows(grad_x, n, d_in, dt), _rows(grad_w, d_in, d_out, dt), _ws(ws)
+    _check(lib().no_linear_bwd(px, _code(x), sx, pw, sw, act, pz, sz, pg, sg, _count(n_rows), n, d_in, d_out, pgx, sgx, pgw, sgw,
+                               _vec(grad_bias, d_out), pb, bb, _stream_of(stream)))
 
 
 # ------------------------------------------------------------------------------------------ model / step

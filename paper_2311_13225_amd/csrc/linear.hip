@@ -1,0 +1,495 @@
+// no_linear_fwd / no_linear_bwd: rows times a matrix, with bias, activation and residual, and the gradients.
+#include "dense.hpp"
+
+namespace no {
+
+template <int ACT> __device__ __forceinline__ float act_of(float z) {
+    if (ACT == NO_ACT_RELU) return z > 0.0f ? z : z != z ? z : 0.0f;
+    if (ACT == NO_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    if (ACT == NO_ACT_SILU) return z / (1.0f + expf(-z));
+    return z;
+}
+// derivative of the activation
+__device__ __forceinline__ float slope_of(int act, float z) {
+    if (act == NO_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (act == NO_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * expf(-0.5f * z * z) * 0.39894228f;
+    if (act == NO_ACT_SILU) {
+        const float p = 1.0f / (1.0f + expf(-z));
+        return p * (1.0f + z * (1.0f - p));
+    }
+    return 1.0f;
+}
+
+// What follows the sums of the forward pass: z = sum + bias, y = act(z) + residual.
+struct LinearEnd {
+    const float* bias;
+    RowsOf residual, z, y;
+    int32_t act;
+};
+
+template <typename T, int ACT, int W>
+__device__ __forceinline__ void linear_end(const LinearEnd& e, int64_t m, int32_t n, int32_t here, float (&v)[W]) {
+    if (e.bias) {
+        Run<float, W> b;
+        float f[W];
+        b.load(e.bias + n, here, 0.0f);
+        b.get(f);
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[w] += f[w];
+    }
+    Run<T, W> o;
+    if (e.z.p) {
+        o.set(v);
+        o.store(e.z.row<T>(m) + n, here);
+    }
+    if (ACT != NO_ACT_NONE)
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[w] = act_of<ACT>(v[w]);
+    if (e.residual.p) {
+        float f[W];
+        o.load(e.residual.row<T>(m) + n, here, from_f32<T>(0.0f));
+        o.get(f);
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[w] += f[w];
+    }
+    o.set(v);
+    o.store(e.y.row<T>(m) + n, here);
+}
+
+template <typename T, int W>
+__device__ __forceinline__ void linear_end_of(const LinearEnd& e, int64_t m, int32_t n, int32_t here, float (&v)[W]) {
+    switch (e.act) {
+        case NO_ACT_RELU: return linear_end<T, NO_ACT_RELU, W>(e, m, n, here, v);
+        case NO_ACT_GELU: return linear_end<T, NO_ACT_GELU, W>(e, m, n, here, v);
+        case NO_ACT_SILU: return linear_end<T, NO_ACT_SILU, W>(e, m, n, here, v);
+        default: return linear_end<T, NO_ACT_NONE, W>(e, m, n, here, v);
+    }
+}
+
+template <typename T>
+struct LinearOut {
+    struct Args { LinearEnd end; float* parts; };      // parts: sums of a split reduction [split][M][N] instead
+    static constexpr bool MIRROR = false;
+    __device__ static __forceinline__ bool wanted(const Args&, int, int) { return true; }
+    __device__ static __forceinline__ void put(const Args& e, const DenseArgs& g, int32_t m, int32_t n, int32_t here, float (&v)[8]) {
+        if (e.parts) {
+            Run<float, 8> o;
+            o.set(v);
+            o.store(e.parts + ((int64_t)blockIdx.y * g.M + m) * g.N + n, here);
+        } else linear_end_of<T, 8>(e.end, m, n, here, v);
+    }
+    __device__ static __forceinline__ void mirror(const Args&, const DenseArgs&, int32_t, int32_t, int32_t, float (&)[8]) {}
+};
+
+// The parts of a split reduction added in order, four columns a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) linear_join_kernel(const float* __restrict__ parts, int32_t splits, int32_t M, const int32_t* d_M, int32_t N, LinearEnd e) {
+    const int64_t per_row = ceil_div(N, 4), i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / per_row;
+    if (m >= rows_here(d_M, M)) return;
+    const int32_t n = (int32_t)(i - m * per_row) * 4, here = min(4, N - n);
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t s = 0; s < splits; ++s) {
+        Run<float, 4> r;
+        float f[4];
+        r.load(parts + ((int64_t)s * M + m) * N + n, here, 0.0f);
+        r.get(f);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] += f[w];
+    }
+    linear_end_of<T, 4>(e, m, n, here, v);
+}
+
+// ------------------------------------------------------------------------------------------------------- operands
+//
+// A product takes rows of whole 16 bytes. bf16 rows that are none are copied into rows of a multiple of 8 values, zeros at the end; fp32 rows are cut into three bf16 planes whose sum is
+// the value, x = h + m + l, rounded each time to the nearest (8 bits each, so nothing of the 24 is left over while the pieces are in range).
+__device__ __forceinline__ void dense_cut(float x, float& h, float& m, float& l) {
+    h = to_f32(from_f32<bf16_t>(x));
+    const bool fine = fabsf(h) < INFINITY;      // (an infinity or NaN is all in the first piece)
+    m = fine ? to_f32(from_f32<bf16_t>(x - h)) : 0.0f;
+    l = fine ? x - h - m : 0.0f;
+}
+
+template <typename T>
+__device__ __forceinline__ void dense_put(const float (&f)[8], char* to, int64_t plane) {
+    Run<bf16_t, 8> o;
+    if constexpr (sizeof(T) == 2) {
+        o.set(f);
+        o.store(reinterpret_cast<bf16_t*>(to));
+    } else {
+        float p[3][8];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) dense_cut(f[w], p[0][w], p[1][w], p[2][w]);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            o.set(p[q]);
+            o.store(reinterpret_cast<bf16_t*>(to + q * plane));
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) linear_pack_kernel(RowsOf x, const int32_t* d_n, int32_t cap, int32_t dim, char* out, int64_t pitch, int64_t plane) {
+    const int32_t units = (dim + 7) / 8, n = rows_here(d_n, cap);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * units; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / units;
+        const int32_t c = (int32_t)(i - r * units) * 8;
+        Run<T, 8> v;
+        float f[8];
+        v.load_at(x.row<T>(r), c, dim, from_f32<T>(0.0f));
+        v.get(f);
+        dense_put<T>(f, out + r * pitch + c * 2, plane);
+    }
+}
+
+// The gradient of the pre-activation, gz = grad_y act'(z), laid out as an operand (gz NULL: grad_y is one as it stands), and its column sums over `per` rows a block, added in order of
+// the rows by eight threads a column.
+template <typename T>
+__global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z, int32_t act, const int32_t* d_n, int32_t cap, int32_t dim, int32_t per, char* gz, int64_t pitch,
+                                                        int64_t plane, float* parts) {
+    __shared__ float share[8][32 * 8];
+    const int32_t n = rows_here(d_n, cap), lane = (int32_t)threadIdx.x & 31, line = (int32_t)threadIdx.x >> 5, c = ((int32_t)blockIdx.x * 32 + lane) * 8;
+    const int64_t first = (int64_t)blockIdx.y * per, last = first + per < n ? first + per : n;
+    float sum[8] = {};
+    if (c < dim) {
+        for (int64_t r = first + line; r < last; r += 8) {
+            Run<T, 8> v;
+            float f[8], s[8];
+            v.load_at(grad_y.row<T>(r), c, dim, from_f32<T>(0.0f));
+            v.get(f);
+            if (z.p) {
+                v.load_at(z.row<T>(r), c, dim, from_f32<T>(0.0f));
+                v.get(s);
+#pragma unroll
+                for (int w = 0; w < 8; ++w) f[w] *= slope_of(act, s[w]);
+            }
+            if (gz) dense_put<T>(f, gz + r * pitch + c * 2, plane);
+#pragma unroll
+            for (int w = 0; w < 8; ++w) sum[w] += f[w];
+        }
+    }
+    if (!parts) return;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) share[line][lane * 8 + w] = sum[w];
+    __syncthreads();
+    const int32_t at = (int32_t)blockIdx.x * 256 + (int32_t)threadIdx.x;
+    if (at >= dim) return;
+    float total = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) total += share[k][threadIdx.x];
+    parts[(int64_t)blockIdx.y * dim + at] = total;
+}
+
+// Sixteen columns a block, sixteen threads to a column.
+__global__ void __launch_bounds__(256) linear_bias_kernel(const float* __restrict__ parts, int32_t n_parts, int32_t dim, float* grad_bias) {
+    __shared__ float share[16][17];
+    const int32_t col = (int32_t)threadIdx.x & 15, row = (int32_t)threadIdx.x >> 4, c = (int32_t)blockIdx.x * 16 + col;
+    float sum = 0.0f;
+    if (c < dim)
+        for (int32_t p = row; p < n_parts; p += 16) sum += parts[(int64_t)p * dim + c];
+    share[row][col] = sum;
+    __syncthreads();
+    if (row > 0 || c >= dim) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += share[k][col];
+    grad_bias[c] = sum;
+}
+
+// ------------------------------------------------------------------------------------------------------- few rows
+//
+// Up to LINEAR_FEW rows: the matrix is read once, in its own order, and that bounds it. A thread has 16 bytes of columns and every 64th row of the block's share of the reduction, for all
+// of the rows at once; rows of x stand in LDS as fp32.
+constexpr int LINEAR_FEW = 8, LINEAR_FEW_K = 1024;      // rows; reduction indices in LDS at a time
+
+template <typename T, int MR>
+__global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int32_t K, int32_t N, int32_t splits, LinearEnd e, float* parts) {
+    constexpr int W = 16 / (int)sizeof(T), LANES = 8, LINES = 512 / LANES;
+    __shared__ __attribute__((aligned(16))) float xs[LINEAR_FEW_K * MR];
+    __shared__ float share[8][MR][LANES * W];
+    const int32_t n = rows_here(d_n, cap);
+    const int lane = (int)threadIdx.x & (LANES - 1), line = (int)threadIdx.x / LANES;
+    const int32_t c = ((int32_t)blockIdx.x * LANES + lane) * W;
+    const int32_t k0 = (int32_t)((int64_t)K * blockIdx.y / splits), k1 = (int32_t)((int64_t)K * (blockIdx.y + 1) / splits);
+    float acc[MR][W] = {};
+    for (int32_t kb = k0; kb < k1; kb += LINEAR_FEW_K) {
+        const int32_t here = min(LINEAR_FEW_K, k1 - kb);
+        __syncthreads();
+        for (int32_t i = (int32_t)threadIdx.x; i < here * MR; i += 512) {
+            const int32_t r = i / here, k = i - r * here;
+            xs[k * MR + r] = r < n ? to_f32(x.row<T>(r)[kb + k]) : 0.0f;
+        }
+        __syncthreads();
+        if (c < N) {
+            auto add = [&](const Run<T, W>& v, int32_t k) {
+                float f[W];
+                v.get(f);
+#pragma unroll
+                for (int r = 0; r < MR; ++r)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) acc[r][j] += xs[k * MR + r] * f[j];
+            };
+            constexpr int AHEAD = 8;        // rows of the matrix requested at once
+            int32_t k = line;
+            for (; k + (AHEAD - 1) * LINES < here; k += AHEAD * LINES) {
+                Run<T, W> v[AHEAD];
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) v[a].load_at(w.row<T>(kb + k + a * LINES), c, N, from_f32<T>(0.0f));
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) add(v[a], k + a * LINES);
+            }
+            for (; k < here; k += LINES) {
+                Run<T, W> v;
+                v.load_at(w.row<T>(kb + k), c, N, from_f32<T>(0.0f));
+                add(v, k);
+            }
+        }
+    }
+    // eight lines of a wavefront, then its eight wavefronts
+#pragma unroll
+    for (int r = 0; r < MR; ++r)
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            float s = acc[r][j];
+#pragma unroll
+            for (int o = LANES; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
+            if (lane_id() < LANES) share[threadIdx.x >> 6][r][lane * W + j] = s;
+        }
+    __syncthreads();
+    constexpr int UNITS = LANES * W / 4;
+    const int r = (int)threadIdx.x / UNITS, u = (int)threadIdx.x % UNITS;
+    const int32_t col = (int32_t)blockIdx.x * LANES * W + u * 4;
+    if (r >= MR || r >= n || col >= N) return;
+    float v[4] = {};
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += share[s][r][u * 4 + j];
+    const int32_t here = min(4, N - col);
+    if (parts) {
+        Run<float, 4> o;
+        o.set(v);
+        o.store(parts + ((int64_t)blockIdx.y * cap + r) * N + col, here);
+    } else linear_end_of<T, 4>(e, r, col, here, v);
+}
+
+// ------------------------------------------------------------------------------------------------------- plans
+
+constexpr size_t LINEAR_PARTS_MOST = (size_t)128 << 20;      // bytes of parts, at most
+
+struct LinearPlan { int tile, splits; };
+
+// Tile and splits of a product of M x N over `steps` steps: the shortest estimate, in units of a 256-wide tile's step. A compute unit holds one block of 256-wide tiles, two of
+// 128-wide or five of 64-wide ones.
+static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int pairs) {
+    const int64_t steps = ceil_div(K < 1 ? 1 : K, DENSE_BK) * pairs;
+    struct { int tile, slots; double step, start; } kinds[3] = {{256, 256, 1.0, 3.0}, {128, 512, 0.65, 3.0}, {64, 1024, 0.45, 3.0}};
+    LinearPlan best{64, 1};
+    double least = 1e300;
+    for (auto& k : kinds) {
+        const int64_t tiles = ceil_div(M < 1 ? 1 : M, k.tile) * ceil_div(N, k.tile);
+        for (int splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 2) {
+            if (splits > 1 && (steps < splits * 4 || (size_t)splits * M * N * 4 > LINEAR_PARTS_MOST)) break;
+            const double rounds = (double)ceil_div(tiles * splits, k.slots);
+            double t = rounds * (ceil_div(steps, splits) * k.step + k.start);
+            if (splits > 1) t += 4.0 + (double)splits * M * N * 8 / 4e6;
+            if (t < least) { least = t; best = LinearPlan{k.tile, splits}; }
+        }
+    }
+    return best;
+}
+static int linear_few_splits(int64_t K, int64_t N, int es) {
+    const int64_t blocks = ceil_div(N, 8 * 16 / es);
+    int splits = 1;
+    while (splits < 32 && blocks * splits < 128 && K / (splits * 2) >= 256) splits *= 2;
+    return splits;
+}
+static size_t linear_parts_bytes(const LinearPlan& p, int64_t M, int64_t N) { return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0; }
+
+static inline size_t round_256(size_t b) { return (b + 255) / 256 * 256; }
+static inline int64_t wide_of(int64_t dim) { return (dim + 7) / 8 * 8; }
+static inline int planes_of_type(no_dtype dt) { return dt == NO_F32 ? 3 : 1; }
+static inline size_t operand_bytes(no_dtype dt, int64_t rows, int64_t dim) { return round_256((size_t)rows * wide_of(dim) * 2 * planes_of_type(dt)); }
+
+constexpr int32_t LINEAR_GZ_ROWS = 64;      // rows a block of linear_gz_kernel, at least
+static inline int64_t gz_blocks(int64_t n) {
+    const int64_t b = ceil_div(n, LINEAR_GZ_ROWS);
+    return b < 1 ? 1 : b < 512 ? b : 512;
+}
+
+// Pairs of planes of fp32 operands, smallest products first: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0); what is left out is below 2^-24 of the product.
+constexpr uint32_t CUT_PAIRS_A = 0x001102u, CUT_PAIRS_B = 0x010120u;
+
+struct LinearRoom { char* p; size_t left; char* take(size_t b) { char* r = p; p += round_256(b); return r; } };
+
+// The operand that holds `rows` rows of `dim` values: the matrix itself where a product can take it, else a copy (fp32: planes).
+template <typename T>
+static DenseOperand linear_operand(RowsOf x, const int32_t* d_n, int64_t rows, int32_t dim, LinearRoom& room, hipStream_t st) {
+    DenseOperand o;
+    if (sizeof(T) == 2 && (uintptr_t)x.p % 16 == 0 && x.stride % 16 == 0 && dim % 8 == 0 && x.stride <= (int64_t)1 << 22) {
+        o = DenseOperand{x.p, x.stride, 0, 0, 0};
+        return o;
+    }
+    const int64_t pitch = wide_of(dim) * 2, plane = pitch * rows;
+    char* to = room.take(operand_bytes(TypeOf<T>::code, rows, dim));
+    if (rows > 0) {
+        const int64_t blocks = ceil_div(rows * ((dim + 7) / 8), 256);
+        hipLaunchKernelGGL(linear_pack_kernel<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, x, d_n, (int32_t)rows, dim, to, pitch, plane);
+    }
+    return DenseOperand{to, pitch, plane, 0, 0};
+}
+
+template <typename T, bool AL, bool BL>
+static void linear_product(DenseArgs g, const LinearEnd& end, float* parts, hipStream_t st) {
+    g.n_pairs = sizeof(T) == 4 ? 6 : 1;
+    g.pairs_a = sizeof(T) == 4 ? CUT_PAIRS_A : 0;
+    g.pairs_b = sizeof(T) == 4 ? CUT_PAIRS_B : 0;
+    const LinearPlan p = linear_plan(g.M, g.N, g.K, g.n_pairs);
+    g.splits = p.splits;
+    g.tiles_m = (int32_t)ceil_div(g.M, p.tile);
+    g.tiles_n = (int32_t)ceil_div(g.N, p.tile);
+    const typename LinearOut<T>::Args e{end, p.splits > 1 ? parts : nullptr};
+    const dim3 grid((unsigned)(ceil_div((int64_t)g.tiles_m * g.tiles_n, 8) * 8), (unsigned)p.splits);
+    if (p.tile == 256) hipLaunchKernelGGL((dense_kernel<__bf16, AL, BL, 256, 256, 2, 4, LinearOut<T>>), grid, dim3(512), 0, st, g, e);
+    else if (p.tile == 128) hipLaunchKernelGGL((dense_kernel<__bf16, AL, BL, 128, 128, 2, 2, LinearOut<T>>), grid, dim3(256), 0, st, g, e);
+    else hipLaunchKernelGGL((dense_kernel<__bf16, AL, BL, 64, 64, 2, 2, LinearOut<T>>), grid, dim3(256), 0, st, g, e);
+    if (p.splits > 1)
+        hipLaunchKernelGGL(linear_join_kernel<T>, dim3((unsigned)ceil_div((int64_t)g.M * ceil_div(g.N, 4), 256)), dim3(256), 0, st, parts, p.splits, g.M, g.d_M, g.N, end);
+}
+
+template <typename T>
+static void linear_fwd(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int32_t d_in, int32_t d_out, const LinearEnd& end, char* ws, hipStream_t st) {
+    LinearRoom room{ws, 0};
+    if (cap <= LINEAR_FEW) {
+        const int splits = linear_few_splits(d_in, d_out, sizeof(T));
+        float* parts = splits > 1 ? (float*)ws : nullptr;
+        const dim3 grid((unsigned)ceil_div(d_out, 8 * 16 / (int)sizeof(T)), (unsigned)splits);
+        if (cap <= 1) hipLaunchKernelGGL((linear_few_kernel<T, 1>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts);
+        else if (cap <= 2) hipLaunchKernelGGL((linear_few_kernel<T, 2>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts);
+        else if (cap <= 4) hipLaunchKernelGGL((linear_few_kernel<T, 4>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts);
+        else hipLaunchKernelGGL((linear_few_kernel<T, 8>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts);
+        if (splits > 1)
+            hipLaunchKernelGGL(linear_join_kernel<T>, dim3((unsigned)ceil_div(cap * ceil_div(d_out, 4), 256)), dim3(256), 0, st, parts, splits, cap, d_n, d_out, end);
+        return;
+    }
+    DenseArgs g{};
+    g.a = linear_operand<T>(x, d_n, cap, d_in, room, st);
+    g.b = linear_operand<T>(w, nullptr, d_in, d_out, room, st);
+    g.a.extent = cap;
+    g.b.extent = (int32_t)wide_of(d_out);
+    g.M = cap; g.N = d_out; g.K = d_in;
+    g.d_M = d_n;
+    linear_product<T, true, false>(g, end, (float*)room.p, st);
+}
+
+template <typename T>
+static void linear_bwd(RowsOf x, RowsOf w, int32_t act, RowsOf z, RowsOf grad_y, const int32_t* d_n, int32_t cap, int32_t d_in, int32_t d_out, RowsOf grad_x, RowsOf grad_w,
+                       float* grad_bias, char* ws, hipStream_t st) {
+    LinearRoom room{ws, 0};
+    const bool products = grad_x.p || grad_w.p;
+    const bool as_is = act == NO_ACT_NONE && sizeof(T) == 2 && (uintptr_t)grad_y.p % 16 == 0 && grad_y.stride % 16 == 0 && d_out % 8 == 0 && grad_y.stride <= (int64_t)1 << 22;
+    DenseOperand gz{grad_y.p, grad_y.stride, 0, 0, 0};
+    char* to = nullptr;
+    if (products && !as_is) {
+        to = room.take(operand_bytes(TypeOf<T>::code, cap, d_out));
+        gz = DenseOperand{to, wide_of(d_out) * 2, wide_of(d_out) * 2 * cap, 0, 0};
+    }
+    const int64_t blocks = gz_blocks(cap);
+    float* sums = (float*)room.take(blocks * d_out * 4);
+    if (to || grad_bias) {
+        hipLaunchKernelGGL(linear_gz_kernel<T>, dim3((unsigned)ceil_div(d_out, 256), (unsigned)blocks), dim3(256), 0, st, grad_y, act == NO_ACT_NONE ? RowsOf{nullptr, 0} : z, act, d_n,
+                           cap, d_out, (int32_t)ceil_div(cap, blocks), to, gz.pitch, gz.plane, grad_bias ? (blocks == 1 ? grad_bias : sums) : nullptr);
+        if (grad_bias && blocks > 1) hipLaunchKernelGGL(linear_bias_kernel, dim3((unsigned)ceil_div(d_out, 16)), dim3(256), 0, st, sums, (int32_t)blocks, d_out, grad_bias);
+    }
+    DenseOperand ow{}, ox{};
+    if (grad_x.p) ow = linear_operand<T>(w, nullptr, d_in, d_out, room, st);
+    if (grad_w.p) ox = linear_operand<T>(x, d_n, cap, d_in, room, st);
+    if (grad_x.p && cap > 0) {
+        DenseArgs g{};
+        g.a = gz; g.b = ow;
+        g.a.extent = cap;
+        g.b.extent = d_in;
+        g.M = cap; g.N = d_in; g.K = d_out;
+        g.d_M = d_n;
+        linear_product<T, true, true>(g, LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_x, NO_ACT_NONE}, (float*)room.p, st);
+    }
+    if (grad_w.p) {
+        DenseArgs g{};
+        g.a = ox; g.b = gz;
+        g.a.extent = (int32_t)wide_of(d_in);
+        g.b.extent = (int32_t)wide_of(d_out);
+        g.M = d_in; g.N = d_out; g.K = cap;
+        g.d_K = d_n;
+        linear_product<T, false, false>(g, LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_w, NO_ACT_NONE}, (float*)room.p, st);
+    }
+}
+
+static int32_t linear_sizes(const char* who, no_dtype dt, int32_t act, int32_t cap, int32_t d_in, int32_t d_out) {
+    NO_REQUIRE(dt == NO_F32 || dt == NO_BF16, NO_ERR_INVALID_ARG, "%s: values are NO_F32 or NO_BF16", who);
+    NO_REQUIRE(act >= NO_ACT_NONE && act <= NO_ACT_SILU, NO_ERR_INVALID_ARG, "%s: unknown activation", who);
+    NO_REQUIRE(cap >= 0 && d_in >= 1 && d_out >= 1, NO_ERR_INVALID_ARG, "%s: bad sizes", who);
+    NO_REQUIRE(d_in <= NO_MAX_LINEAR_DIM && d_out <= NO_MAX_LINEAR_DIM, NO_ERR_UNSUPPORTED, "%s: a side of more than %d", who, NO_MAX_LINEAR_DIM);
+    return NO_OK;
+}
+
+}  // namespace no
+
+using namespace no;
+
+extern "C" size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_in, int32_t d_out) {
+    if ((dt != NO_F32 && dt != NO_BF16) || n_rows_cap < 0 || d_in < 1 || d_out < 1 || d_in > NO_MAX_LINEAR_DIM || d_out > NO_MAX_LINEAR_DIM) return 0;
+    const int pairs = dt == NO_F32 ? 6 : 1;
+    const int64_t n = n_rows_cap;
+    size_t parts = linear_parts_bytes(linear_plan(n, d_out, d_in, pairs), n, d_out);
+    const size_t px = linear_parts_bytes(linear_plan(n, d_in, d_out, pairs), n, d_in), pw = linear_parts_bytes(linear_plan(d_in, d_out, n, pairs), d_in, d_out);
+    if (px > parts) parts = px;
+    if (pw > parts) parts = pw;
+    if (n <= LINEAR_FEW) {
+        const size_t few = (size_t)linear_few_splits(d_in, d_out, dt == NO_F32 ? 4 : 2) * n * d_out * 4;
+        if (few > parts) parts = few;
+    }
+    return 256 + operand_bytes(dt, n, d_in) + operand_bytes(dt, d_in, d_out) + operand_bytes(dt, n, d_out) + round_256((size_t)gz_blocks(n) * d_out * 4) + round_256(parts);
+}
+
+extern "C" int32_t no_linear_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_w, int64_t w_stride_bytes, const float* d_bias, no_act act,
+                                 const void* d_residual, int64_t residual_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t d_in, int32_t d_out,
+                                 void* d_z, int64_t z_stride_bytes, void* d_y, int64_t y_stride_bytes, void* d_ws, size_t ws_bytes, void* stream) {
+    clear_error();
+    const char* who = "no_linear_fwd";
+    NO_CHECK(linear_sizes(who, dt, act, n_rows_cap, d_in, d_out));
+    NO_CHECK(check_rows(who, "x", d_x, dt, n_rows_cap, d_in, x_stride_bytes));
+    NO_CHECK(check_rows(who, "w", d_w, dt, d_in, d_out, w_stride_bytes));
+    if (d_residual) NO_CHECK(check_rows(who, "residual", d_residual, dt, n_rows_cap, d_out, residual_stride_bytes));
+    if (d_z) NO_CHECK(check_rows(who, "z", d_z, dt, n_rows_cap, d_out, z_stride_bytes));
+    NO_CHECK(check_rows(who, "y", d_y, dt, n_rows_cap, d_out, y_stride_bytes));
+    NO_REQUIRE(d_ws && (uintptr_t)d_ws % 16 == 0, NO_ERR_INVALID_ARG, "%s: the workspace is NULL or misaligned", who);
+    NO_REQUIRE(ws_bytes >= no_linear_ws_bytes(dt, n_rows_cap, d_in, d_out), NO_ERR_CAPACITY, "%s: workspace too small", who);
+    if (n_rows_cap == 0) return NO_OK;
+    const LinearEnd end{d_bias, rows_of(d_residual, residual_stride_bytes), rows_of(d_z, z_stride_bytes), rows_of(d_y, y_stride_bytes), (int32_t)act};
+    const RowsOf x = rows_of(d_x, x_stride_bytes), w = rows_of(d_w, w_stride_bytes);
+    if (dt == NO_F32) linear_fwd<float>(x, w, d_n_rows, n_rows_cap, d_in, d_out, end, (char*)d_ws, (hipStream_t)stream);
+    else linear_fwd<bf16_t>(x, w, d_n_rows, n_rows_cap, d_in, d_out, end, (char*)d_ws, (hipStream_t)stream);
+    return launch_status(who);
+}
+
+extern "C" int32_t no_linear_bwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_w, int64_t w_stride_bytes, no_act act, const void* d_z,
+                                 int64_t z_stride_bytes, const void* d_grad_y, int64_t grad_y_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t d_in,
+                                 int32_t d_out, void* d_grad_x, int64_t grad_x_stride_bytes, void* d_grad_w, int64_t grad_w_stride_bytes, float* d_grad_bias, void* d_ws,
+                                 size_t ws_bytes, void* stream) {
+    clear_error();
+    const char* who = "no_linear_bwd";
+    NO_CHECK(linear_sizes(who, dt, act, n_rows_cap, d_in, d_out));
+    if (d_grad_w) NO_CHECK(check_rows(who, "x", d_x, dt, n_rows_cap, d_in, x_stride_bytes));
+    if (d_grad_x) NO_CHECK(check_rows(who, "w", d_w, dt, d_in, d_out, w_stride_bytes));
+    if (act != NO_ACT_NONE) NO_CHECK(check_rows(who, "z", d_z, dt, n_rows_cap, d_out, z_stride_bytes));
+    NO_CHECK(check_rows(who, "grad_y", d_grad_y, dt, n_rows_cap, d_out, grad_y_stride_bytes));
+    if (d_grad_x) NO_CHECK(check_rows(who, "grad_x", d_grad_x, dt, n_rows_cap, d_in, grad_x_stride_bytes));
+    if (d_grad_w) NO_CHECK(check_rows(who, "grad_w", d_grad_w, dt, d_in, d_out, grad_w_stride_bytes));
+    NO_REQUIRE(d_ws && (uintptr_t)d_ws % 16 == 0, NO_ERR_INVALID_ARG, "%s: the workspace is NULL or misaligned", who);
+    NO_REQUIRE(ws_bytes >= no_linear_ws_bytes(dt, n_rows_cap, d_in, d_out), NO_ERR_CAPACITY, "%s: workspace too small", who);
+    const RowsOf x = rows_of(d_x, x_stride_bytes), w = rows_of(d_w, w_stride_bytes), z = rows_of(d_z, z_stride_bytes), gy = rows_of(d_grad_y, grad_y_stride_bytes),
+                 gx = rows_of(d_grad_x, grad_x_stride_bytes), gw = rows_of(d_grad_w, grad_w_stride_bytes);
+    if (dt == NO_F32) linear_bwd<float>(x, w, act, z, gy, d_n_rows, n_rows_cap, d_in, d_out, gx, gw, d_grad_bias, (char*)d_ws, (hipStream_t)stream);
+    else linear_bwd<bf16_t>(x, w, act, z, gy, d_n_rows, n_rows_cap, d_in, d_out, gx, gw, d_grad_bias, (char*)d_ws, (hipStream_t)stream);
+    return launch_status(who);
+}

@@ -1,4 +1,4 @@
-// Rows of fp32, bf16 or e4m3 values for the operators on learned inputs and large answers (embed.hip, rmsnorm.hip, logits.hip): types,
+// Rows of fp32, bf16 or e4m3 values for the operators on learned inputs and large answers (embed.hip, rmsnorm.hip, layernorm.hip, logits.hip): types,
 // 16-byte units of a row at any alignment, reductions over the lanes that share a row.
 #pragma once
 #include "primitives.hpp"
@@ -263,7 +263,7 @@ template <int TEAM, int THREADS>
 struct Team {
     static_assert(TEAM <= 64 || TEAM == THREADS, "a team is a part of a wavefront or the block");
     static constexpr int WAVES = TEAM <= 64 ? 1 : TEAM / 64, PER_BLOCK = THREADS / TEAM;
-    float* smem;        // [2][WAVES] where a team spans wavefronts
+    float* smem;        // [2][WAVES] where a team spans wavefronts; [4][WAVES] for sum_two
     int turn = 0;
     __device__ __forceinline__ explicit Team(float* s) : smem(s) {}
     __device__ __forceinline__ static int lane() { return (int)threadIdx.x & (TEAM - 1); }
@@ -293,6 +293,30 @@ struct Team {
         }
     }
     __device__ __forceinline__ float sum(float v) { return reduce(v, [](float a, float b) { return a + b; }); }
+    // two sums for one barrier; a kernel that calls this calls nothing else of the team's across its wavefronts
+    __device__ __forceinline__ void sum_two(float& a, float& b) {
+#pragma unroll
+        for (int o = (TEAM < 64 ? TEAM : 64) / 2; o > 0; o >>= 1) {
+            a += __shfl_xor(a, o, 64);
+            b += __shfl_xor(b, o, 64);
+        }
+        if constexpr (TEAM > 64) {
+            float* s = smem + turn * 2 * WAVES;
+            turn ^= 1;
+            if (lane_id() == 0) {
+                s[threadIdx.x >> 6] = a;
+                s[WAVES + (threadIdx.x >> 6)] = b;
+            }
+            __syncthreads();
+            a = s[0];
+            b = s[WAVES];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                a += s[w];
+                b += s[WAVES + w];
+            }
+        }
+    }
     __device__ __forceinline__ float max(float v) { return reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
 };
 
