@@ -428,6 +428,22 @@ int32_t no_linear_bwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, cons
                       int32_t d_out, void* d_grad_x, int64_t grad_x_stride_bytes, void* d_grad_w, int64_t grad_w_stride_bytes, float* d_grad_bias, void* d_ws,
                       size_t ws_bytes, void* stream);
 
+/* Matrices made nearly orthogonal by Newton-Schulz products (the update of the Muon optimiser). For each of n_matrices matrices of rows x cols: X = d_x / |d_x| (Frobenius norm, in 64 bits; a
+ * matrix of zeros stays one), then `steps` times (1 to 100; 5 is usual) X <- a X + (b G + c G G) X with G = X X^T where rows <= cols, else X <- a X + X (b G + c G G) with G = X^T X, and
+ * (a, b, c) = (3.4445, -4.7750, 2.0315): a singular value s goes to a s + b s^3 + c s^5 each time, and d_out takes the last X, of type dt_out. Products are of values held to 22 bits, summed in fp32.
+ * dt, dt_out: NO_F32 or NO_BF16. Matrices lie x_matrix_bytes apart (not read for a single one), rows x_stride_bytes. d_out may be d_x itself (same type, address and strides). A matrix with an infinity or
+ * NaN gives NaN throughout; others beside it are not touched by that. */
+size_t no_orthogonalise_ws_bytes(int32_t n_matrices, int32_t rows, int32_t cols);
+int32_t no_orthogonalise(const void* d_x, no_dtype dt, int64_t x_stride_bytes, int64_t x_matrix_bytes, int32_t n_matrices, int32_t rows, int32_t cols, int32_t steps,
+                         void* d_out, no_dtype dt_out, int64_t out_stride_bytes, int64_t out_matrix_bytes, void* d_ws, size_t ws_bytes, void* stream);
+
+/* A step of such an optimiser, in place: d_momentum <- beta d_momentum + d_grad; U = d_grad + beta d_momentum (nesterov != 0) or d_momentum; X from U as no_orthogonalise does;
+ * d_w <- (1 - lr weight_decay) d_w - lr scale X. Weights and momentum are fp32, d_grad of dt. `scale` is the caller's (sqrt(max(1, rows / cols)) is usual). The workspace is that of
+ * no_orthogonalise_ws_bytes. The three overlap nowhere. */
+int32_t no_muon_step(float* d_w, int64_t w_stride_bytes, int64_t w_matrix_bytes, float* d_momentum, int64_t momentum_stride_bytes, int64_t momentum_matrix_bytes,
+                     const void* d_grad, no_dtype dt, int64_t grad_stride_bytes, int64_t grad_matrix_bytes, int32_t n_matrices, int32_t rows, int32_t cols, float lr,
+                     float beta, int32_t nesterov, int32_t steps, float weight_decay, float scale, void* d_ws, size_t ws_bytes, void* stream);
+
 /* ------------------------------------------------------------------------------------------
  * Whole step (loop body of Algorithm 1 with plain SGD, plus hot-embedding reuse)
  * ---------------------------------------------------------------------------------------- */

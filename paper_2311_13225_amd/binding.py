@@ -90,6 +90,10 @@ _SIGNATURES = {
     "no_linear_ws_bytes": (C.c_size_t, [_I32, _I32, _I32, _I32]),
     "no_linear_fwd": (_I32, [_P, _I32, _I64, _P, _I64, _P, _I32, _P, _I64, _P, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, C.c_size_t, _P]),
     "no_linear_bwd": (_I32, [_P, _I32, _I64, _P, _I64, _I32, _P, _I64, _P, _I64, _P, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, C.c_size_t, _P]),
+    "no_orthogonalise_ws_bytes": (C.c_size_t, [_I32, _I32, _I32]),
+    "no_orthogonalise": (_I32, [_P, _I32, _I64, _I64, _I32, _I32, _I32, _I32, _P, _I32, _I64, _I64, _P, C.c_size_t, _P]),
+    "no_muon_step": (_I32, [_P, _I64, _I64, _P, _I64, _I64, _P, _I32, _I64, _I64, _I32, _I32, _I32, C.c_float, C.c_float, _I32, _I32, C.c_float, C.c_float,
+                            _P, C.c_size_t, _P]),
     "no_distill_ws_bytes": (C.c_size_t, [_I32, _I32]),
     "no_distill_fwd": (_I32, [_P, _I32, _I64, _P, _I32, _I32, _P, _P, _I32, C.c_float, _P, _P, _P, _P, C.c_size_t, _P]),
     "no_distill_bwd": (_I32, [_P, _I32, _I64, _P, _I32, _I32, _P, _P, _I32, C.c_float, _P, _P, _P, _I64, _P]),
@@ -693,6 +697,44 @@ def no_linear_bwd(x: torch.Tensor, w: torch.Tensor, act: int, z: Optional[torch.
     (pgx, sgx), (pgw, sgw), (pb, bb) = _rows(grad_x, n, d_in, dt), _rows(grad_w, d_in, d_out, dt), _ws(ws)
     _check(lib().no_linear_bwd(px, _code(x), sx, pw, sw, act, pz, sz, pg, sg, _count(n_rows), n, d_in, d_out, pgx, sgx, pgw, sgw,
                                _vec(grad_bias, d_out), pb, bb, _stream_of(stream)))
+
+
+def _matrices(t: torch.Tensor, shape, dtype: Optional[torch.dtype] = None):
+    """(address, row stride, matrix stride in bytes) of matrices [n, rows, cols], or of one [rows, cols], whose rows are dense."""
+    assert t.is_cuda and t.shape == shape, "a CUDA tensor %s is needed, got %s" % (tuple(shape), tuple(t.shape))
+    assert dtype is None or t.dtype == dtype, "%s is needed, got %s" % (dtype, t.dtype)
+    rows, cols = shape[-2:]
+    assert t.stride(-1) == 1 or cols == 1, "rows must be dense"
+    size, row = _OP_SIZES.get(t.dtype) or t.element_size(), t.stride(-2)
+    if rows < 2 and row < cols:
+        row = cols                          # (a single row's stride says nothing)
+    return t.data_ptr(), row * size, (t.stride(0) if t.dim() == 3 else 0) * size
+
+
+def _matrix_sizes(t: torch.Tensor):
+    assert t.dim() in (2, 3), "matrices [n, rows, cols] or one [rows, cols] are needed"
+    return (t.shape[0] if t.dim() == 3 else 1, t.shape[-2], t.shape[-1])
+
+
+def no_orthogonalise_ws_bytes(n_matrices: int, rows: int, cols: int) -> int:
+    return int(lib().no_orthogonalise_ws_bytes(n_matrices, rows, cols))
+
+
+def no_orthogonalise(x: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, steps: int = 5, stream=None) -> torch.Tensor:
+    """out = x [n, rows, cols] (or one matrix) made nearly orthogonal, matrix by matrix, by `steps` Newton-Schulz steps; float32 or bfloat16."""
+    (px, sx, mx), (po, so, mo), (pw, bw) = _matrices(x, x.shape), _matrices(out, x.shape), _ws(ws)
+    _check(lib().no_orthogonalise(px, _code(x), sx, mx, *_matrix_sizes(x), steps, po, _code(out), so, mo, pw, bw, _stream_of(stream)))
+    return out
+
+
+def no_muon_step(w: torch.Tensor, momentum: torch.Tensor, grad: torch.Tensor, lr: float, beta: float, ws: torch.Tensor, nesterov: bool = True,
+                 steps: int = 5, weight_decay: float = 0.0, scale: float = 1.0, stream=None):
+    """momentum = beta momentum + grad; w = (1 - lr weight_decay) w - lr scale orthogonalise(grad + beta momentum, or momentum without nesterov), in place.
+    w, momentum: float32 [n, rows, cols] or one matrix; grad: float32 or bfloat16. ws: of no_orthogonalise_ws_bytes."""
+    (p0, s0, m0), (p1, s1, m1), (p2, s2, m2) = _matrices(w, w.shape, torch.float32), _matrices(momentum, w.shape, torch.float32), _matrices(grad, w.shape)
+    (pw, bw) = _ws(ws)
+    _check(lib().no_muon_step(p0, s0, m0, p1, s1, m1, p2, _code(grad), s2, m2, *_matrix_sizes(w), lr, beta, 1 if nesterov else 0, steps, weight_decay,
+                              scale, pw, bw, _stream_of(stream)))
 
 
 # ------------------------------------------------------------------------------------------ model / step

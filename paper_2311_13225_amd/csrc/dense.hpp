@@ -27,6 +27,9 @@ struct DenseArgs {
     int32_t n_pairs, splits, tiles_m, tiles_n;
 };
 
+static inline size_t round_256(size_t b) { return (b + 255) / 256 * 256; }
+static inline int64_t wide_of(int64_t dim) { return (dim + 7) / 8 * 8; }       // values of a row of whole 16 bytes
+
 constexpr int DENSE_BK = 64;            // reduction indices a step
 constexpr uint32_t DENSE_NOWHERE = 0x80000000u;      // past every buffer's range: reads as 0
 
@@ -96,10 +99,20 @@ template <> __device__ __forceinline__ f32x4 dense_mfma<_Float16>(s16x8 a, s16x8
 }
 
 // A block's place: tiles are dealt to the dies in runs, and walked in bands of `band` tile rows, so that a die's blocks share rows and columns in its L2.
+// HALF: the tiles on and above the diagonal of a square alone.
+static inline unsigned dense_grid(int64_t tiles_m, int64_t tiles_n, bool half) { return (unsigned)(ceil_div(half ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n, 8) * 8); }
+template <bool HALF>
 __device__ __forceinline__ bool dense_place(const DenseArgs& g, int band, int& tm, int& tn) {
-    const int total = g.tiles_m * g.tiles_n, padded = (int)gridDim.x;
+    const int total = HALF ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n, padded = (int)gridDim.x;
     const int id = ((int)blockIdx.x % 8) * (padded / 8) + (int)blockIdx.x / 8;
     if (id >= total) return false;
+    if (HALF) {         // column tn begins behind tn (tn + 1) / 2 tiles (fewer than 2^24 of them, so the root is off by one at most)
+        tn = (int)((sqrtf(8.0f * (float)id + 1.0f) - 1.0f) * 0.5f);
+        tn += (tn + 1) * (tn + 2) / 2 <= id ? 1 : 0;
+        tn -= tn * (tn + 1) / 2 > id ? 1 : 0;
+        tm = id - tn * (tn + 1) / 2;
+        return true;
+    }
     const int per = band * g.tiles_n, b = id / per, rest = id - b * per, rows = min(band, g.tiles_m - b * band);
     tm = b * band + rest % rows;
     tn = rest / rows;
@@ -115,9 +128,9 @@ __global__ void __launch_bounds__(64 * WM * WN) dense_kernel(const DenseArgs g, 
     typedef DenseTile<BL, BN, T> TB;
     __shared__ __attribute__((aligned(1024))) char lds[2 * (TA::BYTES + TB::BYTES)];
     int tm, tn;
-    if (!dense_place(g, 8, tm, tn)) return;
+    if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
     const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * BM, n0 = tn * BN;
-    if (m0 >= M || !E::wanted(e, m0, n0)) return;
+    if (m0 >= M) return;
     const int wave = (int)threadIdx.x >> 6, wm = wave / WN, wn = wave % WN, l = (int)threadIdx.x & 63;
     TA ta;
     TB tb;
@@ -188,6 +201,7 @@ __global__ void __launch_bounds__(64 * WM * WN) dense_kernel(const DenseArgs g, 
             E::put(e, g, m, n, min(8, g.N - n), v);
         }
         if constexpr (E::MIRROR) {          // the same values as C[n, m], eight consecutive m a lane
+            if (tm == tn) continue;
 #pragma unroll 1
             for (int c = l / (ROWS / 8); c < COLS; c += 64 / (ROWS / 8)) {
                 const int32_t n = nw + c, m = mw + l % (ROWS / 8) * 8;

@@ -70,7 +70,6 @@ template <typename T>
 struct LinearOut {
     struct Args { LinearEnd end; float* parts; };      // parts: sums of a split reduction [split][M][N] instead
     static constexpr bool MIRROR = false;
-    __device__ static __forceinline__ bool wanted(const Args&, int, int) { return true; }
     __device__ static __forceinline__ void put(const Args& e, const DenseArgs& g, int32_t m, int32_t n, int32_t here, float (&v)[8]) {
         if (e.parts) {
             Run<float, 8> o;
@@ -78,7 +77,6 @@ struct LinearOut {
             o.store(e.parts + ((int64_t)blockIdx.y * g.M + m) * g.N + n, here);
         } else linear_end_of<T, 8>(e.end, m, n, here, v);
     }
-    __device__ static __forceinline__ void mirror(const Args&, const DenseArgs&, int32_t, int32_t, int32_t, float (&)[8]) {}
 };
 
 // The parts of a split reduction added in order, four columns a thread.
@@ -306,8 +304,6 @@ static int linear_few_splits(int64_t K, int64_t N, int es) {
 }
 static size_t linear_parts_bytes(const LinearPlan& p, int64_t M, int64_t N) { return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0; }
 
-static inline size_t round_256(size_t b) { return (b + 255) / 256 * 256; }
-static inline int64_t wide_of(int64_t dim) { return (dim + 7) / 8 * 8; }
 static inline int planes_of_type(no_dtype dt) { return dt == NO_F32 ? 3 : 1; }
 static inline size_t operand_bytes(no_dtype dt, int64_t rows, int64_t dim) { return round_256((size_t)rows * wide_of(dim) * 2 * planes_of_type(dt)); }
 
@@ -349,7 +345,7 @@ static void linear_product(DenseArgs g, const LinearEnd& end, float* parts, hipS
     g.tiles_m = (int32_t)ceil_div(g.M, p.tile);
     g.tiles_n = (int32_t)ceil_div(g.N, p.tile);
     const typename LinearOut<T>::Args e{end, p.splits > 1 ? parts : nullptr};
-    const dim3 grid((unsigned)(ceil_div((int64_t)g.tiles_m * g.tiles_n, 8) * 8), (unsigned)p.splits);
+    const dim3 grid(dense_grid(g.tiles_m, g.tiles_n, false), (unsigned)p.splits);
     if (p.tile == 256) hipLaunchKernelGGL((dense_kernel<__bf16, AL, BL, 256, 256, 2, 4, LinearOut<T>>), grid, dim3(512), 0, st, g, e);
     else if (p.tile == 128) hipLaunchKernelGGL((dense_kernel<__bf16, AL, BL, 128, 128, 2, 2, LinearOut<T>>), grid, dim3(256), 0, st, g, e);
     else hipLaunchKernelGGL((dense_kernel<__bf16, AL, BL, 64, 64, 2, 2, LinearOut<T>>), grid, dim3(256), 0, st, g, e);

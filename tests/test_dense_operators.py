@@ -383,3 +383,124 @@ def test_linear_gradient_against_differences():
                 up, down = list(args), list(args)
                 up[at], down[at] = args[at] + d.view_as(args[at]), args[at] - d.view_as(args[at])
                 assert abs((f(*up) - f(*down)) / (2 * h) - got.view(-1)[place].item()) < 1e-4, (act, at)
+
+
+# ------------------------------------------------------------------------------------------------------- orthogonalised updates
+
+A, B, C = 3.4445, -4.7750, 2.0315
+
+
+def steps_ref(x, steps):
+    """The polynomial's steps in x's own type, matrix by matrix."""
+    made = []
+    for m in x:
+        tall = m.shape[0] > m.shape[1]
+        m = m.t().contiguous() if tall else m
+        norm = torch.linalg.norm(m.double())
+        m = (m.double() / norm).to(x.dtype) if norm > 0 else m
+        for _ in range(steps):
+            g = m @ m.t().contiguous()
+            m = A * m + (B * g + C * (g @ g)) @ m
+        made.append(m.t() if tall else m)
+    return torch.stack(made)
+
+
+def apart(got, ref):
+    return ((got.double() - ref).norm() / ref.norm()).item()
+
+
+# A step's rounding, in parts of |X|: a x, b G x and c G G x of singular values up to 1.21 add up to 34 |X| in magnitude, their factors are off by 2^-22 and the sums over k by 2 u sqrt(k), random in
+# sign. Over five steps a perturbation grows up to 3.9-fold in each, which is no bound worth having; there the same formula in fp32 is the measure: its operands are held to 2^-24 and its
+# sums rounded alike, so twice its error, and 8 x 2^-22 where that is smaller.
+def one_step_tol(k):
+    return 34 * (2.0 ** -22 + 2 * U * math.sqrt(k + 64))
+
+
+@pytest.mark.parametrize("n,rows,cols", [(1, 1, 1), (2, 1, 9), (3, 9, 1), (1, 7, 5), (2, 64, 64), (3, 65, 130), (2, 130, 65), (1, 256, 602), (2, 602, 256), (1, 100, 1001), (4, 300, 41),
+                                         (1, 1030, 1500), (1, 1500, 1030), (2, 520, 2048), (1, 2050, 2050)])
+@BOTH
+def test_orthogonalise(n, rows, cols, dt):
+    b, g = nb(), rng(rows + cols)
+    x = randn((n, rows, cols), g, dt, 0.01)
+    x[0, 0] *= 30                           # a strong direction
+    ws = ws_of(b.no_orthogonalise_ws_bytes(n, rows, cols))
+    small = min(rows, cols)
+    for steps in (1, 5):
+        out = torch.empty_like(x)
+        wide = torch.empty((n, rows, cols), device="cuda")
+        b.no_orthogonalise(x, out, ws, steps=steps)
+        ws.fill_(0x3C)
+        b.no_orthogonalise(x, wide, ws, steps=steps)
+        ref = steps_ref(x.double(), steps)
+        tol = one_step_tol(max(rows, cols)) if steps == 1 else max(2 * apart(steps_ref(x.float(), steps), ref), 8 * 2.0 ** -22)
+        assert apart(wide, ref) <= tol, (steps, apart(wide, ref), tol)
+        assert torch.equal(out, wide.to(dt))
+    # what it is for: every singular value of x / |x| went through the polynomial five times (a matrix of small difference has singular values that differ by no more than its norm)
+    sv = torch.linalg.svdvals(x.double())
+    sv = sv / sv.norm(dim=1, keepdim=True)
+    for _ in range(5):
+        sv = A * sv + B * sv ** 3 + C * sv ** 5
+    diff = torch.linalg.svdvals(wide.double()).sort().values - sv.sort().values
+    assert diff.abs().max() <= tol * ref.norm() + 1e-9 and sv.max() < 1.21
+    again = x.clone()
+    b.no_orthogonalise(again, again, ws)
+    assert torch.equal(again, out)
+    one = torch.empty((rows, cols), device="cuda")
+    b.no_orthogonalise(x[n - 1], one, ws_of(b.no_orthogonalise_ws_bytes(1, rows, cols)))
+    assert apart(one, wide[n - 1].double()) <= 2 * tol
+
+
+@BOTH
+def test_orthogonalise_strides_and_extremes(dt):
+    b, g = nb(), rng(2)
+    rows, cols = 40, 67
+    base = randn((3, rows + 2, cols + 5), g, dt)
+    x = base[:, 1:rows + 1, 3:cols + 3]
+    marked = torch.full((3, rows + 2, cols + 5), MARK, device="cuda", dtype=dt)
+    out = marked[:, 1:rows + 1, 3:cols + 3]
+    ws = ws_of(b.no_orthogonalise_ws_bytes(3, rows, cols))
+    b.no_orthogonalise(x, out, ws)
+    dense = torch.empty((3, rows, cols), device="cuda", dtype=dt)
+    b.no_orthogonalise(x.contiguous(), dense, ws)
+    assert torch.equal(out, dense)
+    marked[:, 1:rows + 1, 3:cols + 3] = MARK
+    assert (marked == MARK).all()
+    b.no_orthogonalise(x.contiguous() * 2.0 ** -60, out, ws)                # the size of a matrix does not count
+    assert torch.equal(out, dense)
+    if dt == F32:
+        b.no_orthogonalise(x.contiguous() * 2.0 ** 100, out, ws)            # (squares beyond fp32)
+        assert torch.equal(out, dense)
+    y = x.contiguous()
+    y[0], y[1, 3, 4] = 0.0, NAN
+    b.no_orthogonalise(y, out, ws)
+    assert (out[0] == 0).all() and out[1].isnan().all() and torch.equal(out[2], dense[2])
+    y[1, 3, 4] = INF
+    b.no_orthogonalise(y, out, ws)
+    assert out[1].isnan().all() and torch.equal(out[2], dense[2])
+    b.no_orthogonalise(y[:0], out[:0], ws_of(b.no_orthogonalise_ws_bytes(0, rows, cols)))
+
+
+@pytest.mark.parametrize("n,rows,cols", [(1, 1, 3), (2, 602, 256), (3, 41, 300), (1, 777, 777)])
+@BOTH
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_muon_step(n, rows, cols, dt, nesterov):
+    b, g = nb(), rng(rows + 1)
+    w, m = randn((n, rows, cols), g), randn((n, rows, cols), g, F32, 0.1)
+    ws = ws_of(b.no_orthogonalise_ws_bytes(n, rows, cols))
+    lr, beta, decay, scale = 0.05, 0.9, 0.1, 1.5
+    for _ in range(3):
+        grad = randn((n, rows, cols), g, dt)
+        w0, m0, g0 = w.double(), m.double(), grad.double()
+        b.no_muon_step(w, m, grad, lr, beta, ws, nesterov=nesterov, weight_decay=decay, scale=scale)
+        beta32, keep, step = (torch.tensor(v, dtype=F32).item() for v in (beta, 1 - lr * decay, lr * scale))
+        ref_m = beta32 * m0 + g0
+        close(m, ref_m, 2 * U * ((beta32 * m0).abs() + ref_m.abs()), "momentum")
+        u = (g0 + beta32 * m.double()) if nesterov else m.double()
+        ref_o = steps_ref(u, 5)
+        tol = max(2 * apart(steps_ref(u.float(), 5), ref_o), 8 * 2.0 ** -22)
+        got = (w0 * keep - w.double()) / step
+        # the update by difference: the weights' own rounding besides (three operations, and their constants)
+        assert (got - ref_o).norm() <= tol * ref_o.norm() + 4 * U * w0.norm() / step
+    one_w, one_m = w[0].clone(), m[0].clone()
+    b.no_muon_step(one_w, one_m, grad[0], 0.0, 0.0, ws, nesterov=nesterov)
+    assert torch.equal(one_w, w[0]) and torch.equal(one_m, grad[0].float())
