@@ -109,7 +109,7 @@ __device__ __forceinline__ void dense_cut(float x, float& h, float& m, float& l)
 }
 
 template <typename T>
-__device__ __forceinline__ void dense_put(const float (&f)[8], char* to, int64_t plane) {
+__device__ __forceinline__ void dense_put(const float (&f)[8], char* to, int32_t plane) {
     Run<bf16_t, 8> o;
     if constexpr (sizeof(T) == 2) {
         o.set(f);
@@ -127,7 +127,7 @@ __device__ __forceinline__ void dense_put(const float (&f)[8], char* to, int64_t
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) linear_pack_kernel(RowsOf x, const int32_t* d_n, int32_t cap, int32_t dim, char* out, int64_t pitch, int64_t plane) {
+__global__ void __launch_bounds__(256) linear_pack_kernel(RowsOf x, const int32_t* d_n, int32_t cap, int32_t dim, char* out, int64_t pitch, int32_t plane) {
     const int32_t units = (dim + 7) / 8, n = rows_here(d_n, cap);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * units; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / units;
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(256) linear_pack_kernel(RowsOf x, const int32_
 // the rows by eight threads a column.
 template <typename T>
 __global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z, int32_t act, const int32_t* d_n, int32_t cap, int32_t dim, int32_t per, char* gz, int64_t pitch,
-                                                        int64_t plane, float* parts) {
+                                                        int32_t plane, float* parts) {
     __shared__ float share[8][32 * 8];
     const int32_t n = rows_here(d_n, cap), lane = (int32_t)threadIdx.x & 31, line = (int32_t)threadIdx.x >> 5, c = ((int32_t)blockIdx.x * 32 + lane) * 8;
     const int64_t first = (int64_t)blockIdx.y * per, last = first + per < n ? first + per : n;
@@ -275,23 +275,23 @@ __global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, con
 
 constexpr size_t LINEAR_PARTS_MOST = (size_t)128 << 20;      // bytes of parts, at most
 
-struct LinearPlan { int tile, splits; };
+struct LinearPlan { int bm, bn, splits; };
 
-// Tile and splits of a product of M x N over `steps` steps: the shortest estimate, in units of a 256-wide tile's step. A compute unit holds one block of 256-wide tiles, two of
-// 128-wide or five of 64-wide ones.
-static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int pairs) {
-    const int64_t steps = ceil_div(K < 1 ? 1 : K, DENSE_BK) * pairs;
-    struct { int tile, slots; double step, start; } kinds[3] = {{256, 256, 1.0, 3.0}, {128, 512, 0.65, 3.0}, {64, 1024, 0.45, 3.0}};
-    LinearPlan best{64, 1};
+// Tile and splits of a product of M x N over K of P pieces: the shortest estimate in microseconds. A step's time is that of a full chip, so a kind of tile takes rounds x (steps x step + start).
+static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int P) {
+    const int64_t steps = ceil_div(K < 1 ? 1 : K, dense_bk(P));
+    struct Kind { int bm, bn, slots; double step, start; };
+    static const Kind one[3] = {{256, 256, 256, 1.0, 5.0}, {128, 128, 512, 0.65, 4.0}, {64, 64, 1024, 0.45, 4.0}}, three[3] = {{256, 128, 256, 1.7, 5.0}, {128, 128, 256, 1.0, 4.0}, {64, 64, 768, 0.9, 4.0}};
+    LinearPlan best{64, 64, 1};
     double least = 1e300;
-    for (auto& k : kinds) {
-        const int64_t tiles = ceil_div(M < 1 ? 1 : M, k.tile) * ceil_div(N, k.tile);
+    for (const Kind& k : P == 1 ? one : three) {
+        const int64_t tiles = ceil_div(M < 1 ? 1 : M, k.bm) * ceil_div(N, k.bn);
         for (int splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 2) {
             if (splits > 1 && (steps < splits * 4 || (size_t)splits * M * N * 4 > LINEAR_PARTS_MOST)) break;
             const double rounds = (double)ceil_div(tiles * splits, k.slots);
             double t = rounds * (ceil_div(steps, splits) * k.step + k.start);
             if (splits > 1) t += 4.0 + (double)splits * M * N * 8 / 4e6;
-            if (t < least) { least = t; best = LinearPlan{k.tile, splits}; }
+            if (t < least) { least = t; best = LinearPlan{k.bm, k.bn, splits}; }
         }
     }
     return best;
@@ -313,9 +313,6 @@ static inline int64_t gz_blocks(int64_t n) {
     return b < 1 ? 1 : b < 512 ? b : 512;
 }
 
-// Pairs of planes of fp32 operands, smallest products first: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0); what is left out is below 2^-24 of the product.
-constexpr uint32_t CUT_PAIRS_A = 0x001102u, CUT_PAIRS_B = 0x010120u;
-
 struct LinearRoom { char* p; size_t left; char* take(size_t b) { char* r = p; p += round_256(b); return r; } };
 
 // The operand that holds `rows` rows of `dim` values: the matrix itself where a product can take it, else a copy (fp32: planes).
@@ -326,29 +323,30 @@ static DenseOperand linear_operand(RowsOf x, const int32_t* d_n, int64_t rows, i
         o = DenseOperand{x.p, x.stride, 0, 0, 0};
         return o;
     }
-    const int64_t pitch = wide_of(dim) * 2, plane = pitch * rows;
+    const int32_t plane = (int32_t)wide_of(dim) * 2;
+    const int64_t pitch = (int64_t)plane * planes_of_type(TypeOf<T>::code);
     char* to = room.take(operand_bytes(TypeOf<T>::code, rows, dim));
     if (rows > 0) {
         const int64_t blocks = ceil_div(rows * ((dim + 7) / 8), 256);
         hipLaunchKernelGGL(linear_pack_kernel<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, x, d_n, (int32_t)rows, dim, to, pitch, plane);
     }
-    return DenseOperand{to, pitch, plane, 0, 0};
+    return DenseOperand{to, pitch, 0, plane, 0};
 }
 
 template <typename T, bool AL, bool BL>
 static void linear_product(DenseArgs g, const LinearEnd& end, float* parts, hipStream_t st) {
-    g.n_pairs = sizeof(T) == 4 ? 6 : 1;
-    g.pairs_a = sizeof(T) == 4 ? CUT_PAIRS_A : 0;
-    g.pairs_b = sizeof(T) == 4 ? CUT_PAIRS_B : 0;
-    const LinearPlan p = linear_plan(g.M, g.N, g.K, g.n_pairs);
+    constexpr int P = sizeof(T) == 4 ? 3 : 1;
+    const LinearPlan p = linear_plan(g.M, g.N, g.K, P);
     g.splits = p.splits;
-    g.tiles_m = (int32_t)ceil_div(g.M, p.tile);
-    g.tiles_n = (int32_t)ceil_div(g.N, p.tile);
+    g.tiles_m = (int32_t)ceil_div(g.M, p.bm);
+    g.tiles_n = (int32_t)ceil_div(g.N, p.bn);
     const typename LinearOut<T>::Args e{end, p.splits > 1 ? parts : nullptr};
     const dim3 grid(dense_grid(g.tiles_m, g.tiles_n, false), (unsigned)p.splits);
-    if (p.tile == 256) hipLaunchKernelGGL((dense_kernel<__bf16, AL, BL, 256, 256, 2, 4, LinearOut<T>>), grid, dim3(512), 0, st, g, e);
-    else if (p.tile == 128) hipLaunchKernelGGL((dense_kernel<__bf16, AL, BL, 128, 128, 2, 2, LinearOut<T>>), grid, dim3(256), 0, st, g, e);
-    else hipLaunchKernelGGL((dense_kernel<__bf16, AL, BL, 64, 64, 2, 2, LinearOut<T>>), grid, dim3(256), 0, st, g, e);
+    if (p.bm == 256) {
+        if constexpr (P == 1) hipLaunchKernelGGL((dense_large_kernel<__bf16, P, AL, BL, LinearOut<T>>), grid, dim3(256), 0, st, g, e);
+        else hipLaunchKernelGGL((dense_kernel<__bf16, P, AL, BL, 256, 128, 4, 2, LinearOut<T>>), grid, dim3(512), 0, st, g, e);
+    } else if (p.bm == 128) hipLaunchKernelGGL((dense_kernel<__bf16, P, AL, BL, 128, 128, 2, 2, LinearOut<T>>), grid, dim3(256), 0, st, g, e);
+    else hipLaunchKernelGGL((dense_kernel<__bf16, P, AL, BL, 64, 64, 2, 2, LinearOut<T>>), grid, dim3(256), 0, st, g, e);
     if (p.splits > 1)
         hipLaunchKernelGGL(linear_join_kernel<T>, dim3((unsigned)ceil_div((int64_t)g.M * ceil_div(g.N, 4), 256)), dim3(256), 0, st, parts, p.splits, g.M, g.d_M, g.N, end);
 }
@@ -388,7 +386,7 @@ static void linear_bwd(RowsOf x, RowsOf w, int32_t act, RowsOf z, RowsOf grad_y,
     char* to = nullptr;
     if (products && !as_is) {
         to = room.take(operand_bytes(TypeOf<T>::code, cap, d_out));
-        gz = DenseOperand{to, wide_of(d_out) * 2, wide_of(d_out) * 2 * cap, 0, 0};
+        gz = DenseOperand{to, wide_of(d_out) * 2 * planes_of_type(TypeOf<T>::code), 0, (int32_t)wide_of(d_out) * 2, 0};
     }
     const int64_t blocks = gz_blocks(cap);
     float* sums = (float*)room.take(blocks * d_out * 4);
@@ -434,10 +432,10 @@ using namespace no;
 
 extern "C" size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_in, int32_t d_out) {
     if ((dt != NO_F32 && dt != NO_BF16) || n_rows_cap < 0 || d_in < 1 || d_out < 1 || d_in > NO_MAX_LINEAR_DIM || d_out > NO_MAX_LINEAR_DIM) return 0;
-    const int pairs = dt == NO_F32 ? 6 : 1;
+    const int pieces = planes_of_type(dt);
     const int64_t n = n_rows_cap;
-    size_t parts = linear_parts_bytes(linear_plan(n, d_out, d_in, pairs), n, d_out);
-    const size_t px = linear_parts_bytes(linear_plan(n, d_in, d_out, pairs), n, d_in), pw = linear_parts_bytes(linear_plan(d_in, d_out, n, pairs), d_in, d_out);
+    size_t parts = linear_parts_bytes(linear_plan(n, d_out, d_in, pieces), n, d_out);
+    const size_t px = linear_parts_bytes(linear_plan(n, d_in, d_out, pieces), n, d_in), pw = linear_parts_bytes(linear_plan(d_in, d_out, n, pieces), d_in, d_out);
     if (px > parts) parts = px;
     if (pw > parts) parts = pw;
     if (n <= LINEAR_FEW) {

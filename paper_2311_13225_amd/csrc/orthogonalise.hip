@@ -11,10 +11,9 @@ namespace no {
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float NS_HELD = 0x1p14f, NS_VALUE = 0x1p-14f;
-constexpr uint32_t NS_PAIRS_A = 0x001u, NS_PAIRS_B = 0x010u;       // (1, 0), (0, 1), (0, 0): smallest first
 
 // Eight values of one row in pieces, and back.
-__device__ __forceinline__ void ns_store(const float (&f)[8], char* to, int64_t plane) {
+__device__ __forceinline__ void ns_store(const float (&f)[8], char* to, int32_t plane) {
     f16x8 h, l;
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
@@ -24,16 +23,17 @@ __device__ __forceinline__ void ns_store(const float (&f)[8], char* to, int64_t 
     *reinterpret_cast<f16x8*>(to) = h;
     *reinterpret_cast<f16x8*>(to + plane) = l;
 }
-__device__ __forceinline__ void ns_load(const char* from, int64_t plane, float (&f)[8]) {
+__device__ __forceinline__ void ns_load(const char* from, int32_t plane, float (&f)[8]) {
     const f16x8 h = *reinterpret_cast<const f16x8*>(from), l = *reinterpret_cast<const f16x8*>(from + plane);
 #pragma unroll
     for (int w = 0; w < 8; ++w) f[w] = (float)h[w] + (float)l[w];
 }
 
-// A matrix in pieces: rows of a multiple of 8 values, zeros past the columns.
+// A matrix in pieces: rows of a multiple of 8 values, zeros past the columns, the second pieces of a row behind the first.
 struct NsMatrix {
     char* p;
-    int64_t pitch, plane, matrix;
+    int64_t pitch, matrix;
+    int32_t plane;
 };
 struct NsRows {           // rows of the caller's matrices
     RowsOf rows;
@@ -170,8 +170,8 @@ __global__ void __launch_bounds__(256) ns_pieces_kernel(NsSource<T> u, int32_t r
 // ------------------------------------------------------------------------------------------------------- products
 
 static int ns_tile(int64_t M, int64_t N, int64_t K, int64_t matrices, bool half) {
-    const int64_t steps = ceil_div(K, DENSE_BK) * 3;
-    struct { int tile, slots; double step, start; } kinds[3] = {{256, 256, 1.0, 3.0}, {128, 512, 0.65, 3.0}, {64, 1024, 0.45, 3.0}};
+    const int64_t steps = ceil_div(K, dense_bk(2));
+    struct { int tile, slots; double step, start; } kinds[3] = {{256, 256, 1.5, 5.0}, {128, 512, 0.95, 4.0}, {64, 1024, 0.65, 4.0}};
     int best = 64;
     double least = 1e300;
     for (auto& k : kinds) {
@@ -186,20 +186,17 @@ template <bool AL, bool BL, bool HALF>
 static void ns_product(const NsMatrix& a, int32_t a_extent, const NsMatrix& b, int32_t b_extent, int32_t M, int32_t N, int32_t K, int32_t matrices, const typename NsEnd<HALF>::Args& e,
                        hipStream_t st) {
     DenseArgs g{};
-    g.a = DenseOperand{a.p, a.pitch, a.plane, a.matrix, a_extent};
-    g.b = DenseOperand{b.p, b.pitch, b.plane, b.matrix, b_extent};
+    g.a = DenseOperand{a.p, a.pitch, a.matrix, a.plane, a_extent};
+    g.b = DenseOperand{b.p, b.pitch, b.matrix, b.plane, b_extent};
     g.M = M; g.N = N; g.K = K;
-    g.pairs_a = NS_PAIRS_A;
-    g.pairs_b = NS_PAIRS_B;
-    g.n_pairs = 3;
     g.splits = 1;
     const int tile = ns_tile(M, N, K, matrices, HALF);
     g.tiles_m = (int32_t)ceil_div(M, tile);
     g.tiles_n = (int32_t)ceil_div(N, tile);
     const dim3 grid(dense_grid(g.tiles_m, g.tiles_n, HALF), 1, (unsigned)matrices);
-    if (tile == 256) hipLaunchKernelGGL((dense_kernel<_Float16, AL, BL, 256, 256, 2, 4, NsEnd<HALF>>), grid, dim3(512), 0, st, g, e);
-    else if (tile == 128) hipLaunchKernelGGL((dense_kernel<_Float16, AL, BL, 128, 128, 2, 2, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e);
-    else hipLaunchKernelGGL((dense_kernel<_Float16, AL, BL, 64, 64, 2, 2, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e);
+    if (tile == 256) hipLaunchKernelGGL((dense_large_kernel<_Float16, 2, AL, BL, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e);
+    else if (tile == 128) hipLaunchKernelGGL((dense_kernel<_Float16, 2, AL, BL, 128, 128, 2, 2, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e);
+    else hipLaunchKernelGGL((dense_kernel<_Float16, 2, AL, BL, 64, 64, 2, 2, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e);
 }
 
 struct NsRoom {
@@ -209,9 +206,9 @@ struct NsRoom {
 };
 
 static NsMatrix ns_matrix(char*& p, int64_t matrices, int64_t rows, int64_t cols) {
-    const int64_t pitch = wide_of(cols) * 2, plane = pitch * rows;
-    const NsMatrix m{p, pitch, plane, 2 * plane};
-    p += round_256((size_t)(matrices * 2 * plane));
+    const int32_t plane = (int32_t)wide_of(cols) * 2;
+    const NsMatrix m{p, 2 * plane, 2 * plane * rows, plane};
+    p += round_256((size_t)(matrices * m.matrix));
     return m;
 }
 static NsRoom ns_room(char* ws, int64_t matrices, int64_t rows, int64_t cols) {
