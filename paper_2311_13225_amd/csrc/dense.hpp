@@ -81,22 +81,24 @@ struct DenseTile {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + (i * T + wave * 64) * 16), 16, at, 0, 0, 0);
         }
     }
-    // Request i of step s alone, by hand: the compiler takes a request for a write of LDS that every later read of LDS has to wait for, and cannot know that the two go to different
-    // copies. What it fills is waited for in dense_meet().
-    __device__ __forceinline__ int32_t unit_k() const {      // the reduction index of request 0
-        int line, unit;
-        which(0, line, unit);
-        return ALONG ? (P == 1 ? unit : unit & 3) * 8 : P == 1 ? line : line & 31;
-    }
+    // Request i alone, by hand: the compiler takes a request for a write of LDS that every later read of LDS has to wait for, and cannot know that the two go to different copies. What it
+    // fills is waited for in dense_meet(). Nothing is masked here: cut() comes before the first step that is not whole.
     __device__ __forceinline__ i32x4 source(int32_t s) const {
         const uint64_t at = (uint64_t)(base + (int64_t)s * step);
         return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), 0x7fffffff, 0x00020000};
     }
-    __device__ __forceinline__ void request_one(int i, i32x4 rsrc, int32_t left, int32_t k0, uint32_t to) const {
-        static_assert(!ALONG || (P < 3 && T % (8 * PER_ROW) == 0), "a thread's requests of a row operand share their unit");
-        const int32_t k = ALONG ? k0 : P == 1 ? k0 + i * (T / PER_ROW) : (k0 + i * (T / PER_ROW)) & 31;
-        const uint32_t at = k < left ? off[i] : DENSE_NOWHERE;
-        asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(at), "s"(rsrc), "s"(to + i * T * 16) : "memory");
+    __device__ __forceinline__ void request_one(int i, i32x4 rsrc, uint32_t to) const {
+        asm volatile("s_add_u32 m0, %2, %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(off[i]), "s"(rsrc), "s"(to), "i"(i * T * 16) : "memory", "scc");
+    }
+    // From here on only the first `left` reduction indices of a step are asked for.
+    __device__ __forceinline__ void cut(int32_t left) {
+#pragma unroll
+        for (int i = 0; i < REQ; ++i) {
+            int line, unit;
+            which(i, line, unit);
+            const int k = ALONG ? (P == 1 ? unit : unit & 3) * 8 : P == 1 ? line : line & 31;
+            if (k >= left) off[i] = DENSE_NOWHERE;
+        }
     }
     // The fragment of 16 rows (columns) from 16 q on, slab h: lane l has row l % 16 and indices 8 (l / 16) + [0, 8).
     __device__ __forceinline__ static s16x8 fragment(const char* from, int q, int h) {
@@ -340,80 +342,87 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             asm volatile("" : "+a"(acc[i][j]));
         }
-    constexpr uint32_t COPY = TA::BYTES + TB::BYTES;
-    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + (uint32_t)wave * 1024u);
-    const int32_t ka = ta.unit_k(), kb = tb.unit_k();
-    uint32_t now = 0;
-    // (steps past K are zeros, those past `last` are loaded and not used)
-    auto request = [&](int n, int32_t s, uint32_t copy) {       // request n of the step's TA::REQ + TB::REQ
-        const int32_t left = K - s * TA::BK;
-        if (n < TA::REQ) ta.request_one(n, ta.source(s), AL ? (left + 7) & ~7 : left, ka, lds0 + copy);
-        else tb.request_one(n - TA::REQ, tb.source(s), BL ? (left + 7) & ~7 : left, kb, lds0 + copy + TA::BYTES);
-    };
-    auto take = [&](int n, s16x8 (&a)[I], int ha, s16x8 (&b)[J], int hb, uint32_t copy) {       // fragment n of the sixteen: as the products want them
-        if (n < 4) b[n] = TB::fragment(lds + copy + TA::BYTES, wn * J + n, hb);
-        else if (n == 4) a[0] = TA::fragment(lds + copy, wm * I, ha);
-        else if (n < 9) b[n - 1] = TB::fragment(lds + copy + TA::BYTES, wn * J + n - 1, hb);
-        else a[n - 8] = TA::fragment(lds + copy, wm * I + n - 8, ha);
-    };
-    auto four = [&](int n, s16x8 (&a)[I], s16x8 (&b)[J]) {      // products 4 n to 4 n + 3 of 64
-#pragma unroll
-        for (int j = 0; j < 4; ++j) dense_mfma_in_place<H>(acc[n >> 1][(n & 1) * 4 + j], b[(n & 1) * 4 + j], a[n >> 1]);
-    };
-    constexpr int REQ = TA::REQ + TB::REQ;
+    constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
     static_assert(REQ == 16, "one request for four products");
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + (uint32_t)wave * 1024u);
+    const int32_t whole = K / TA::BK;
+    i32x4 ra, rb;
+    // what comes before the requests of step s (those past K are zeros, those past `last` are loaded and not used)
+    auto aim = [&](int32_t s) {
+        if (s >= whole) {
+            const int32_t left = K - s * TA::BK;
+            ta.cut(AL ? (left + 7) & ~7 : left);
+            tb.cut(BL ? (left + 7) & ~7 : left);
+        }
+        ra = ta.source(s);
+        rb = tb.source(s);
+    };
+    auto request = [&](int n, int copy) {
+        if (n < TA::REQ) ta.request_one(n, ra, lds0 + copy * COPY);
+        else tb.request_one(n - TA::REQ, rb, lds0 + copy * COPY + TA::BYTES);
+    };
+    auto take = [&](int n, s16x8 (&a)[I], int ha, s16x8 (&b)[J], int hb, int copy) {       // fragment n of the sixteen: in the order in which the products want them
+        if (n < 4) b[n] = TB::fragment(lds + copy * COPY + TA::BYTES, wn * J + n, hb);
+        else if (n == 4) a[0] = TA::fragment(lds + copy * COPY, wm * I, ha);
+        else if (n < 9) b[n - 1] = TB::fragment(lds + copy * COPY + TA::BYTES, wn * J + n - 1, hb);
+        else a[n - 8] = TA::fragment(lds + copy * COPY, wm * I + n - 8, ha);
+    };
+    // Product n of 64, and the end of what may stand beside it: a wavefront issues in order, and while a product is at work the next one waits, so that other instructions are free only
+    // one or two at a time, between products (four products and then what four of them need: 503 us for what takes 400 so).
+    auto one = [&](int n, s16x8 (&a)[I], s16x8 (&b)[J]) {
+        dense_mfma_in_place<H>(acc[n >> 3][n & 7], b[n & 7], a[n >> 3]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    aim(first);
 #pragma unroll
-    for (int n = 0; n < REQ; ++n) request(n, first, 0);
+    for (int n = 0; n < REQ; ++n) request(n, 0);
+    aim(first + 1);
 #pragma unroll
-    for (int n = 0; n < REQ; ++n) request(n, first + 1, COPY);
+    for (int n = 0; n < REQ; ++n) request(n, 1);
     dense_meet();
     s16x8 a0[I], a1[I], b0[J], b1[J];
-    if constexpr (P == 1) {
+    auto step = [&](auto copy_of, int32_t s) {
+        constexpr int now = decltype(copy_of)::value;
+        if constexpr (P == 1) {
 #pragma unroll
-        for (int n = 0; n < 16; ++n) take(n, a0, 0, b0, 0, now);
-        for (int32_t s = first; s < last; ++s) {
-#pragma unroll
-            for (int n = 0; n < 16; ++n) {
-                if (n < 8) { take(2 * n, a1, 1, b1, 1, now); take(2 * n + 1, a1, 1, b1, 1, now); }
-                four(n, a0, b0);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int n = 0; n < 64; ++n) {
+                if (n % 2 == 0 && n < 32) take(n / 2, a1, 1, b1, 1, now);
+                one(n, a0, b0);
             }
+            aim(s + 2);
             dense_meet();
 #pragma unroll
-            for (int n = 0; n < 16; ++n) {
-                request(n, s + 2, now);
-                take(n, a0, 0, b0, 0, now ^ COPY);
-                four(n, a1, b1);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int n = 0; n < 64; ++n) {
+                if (n % 4 == 0) take(n / 4, a0, 0, b0, 0, now ^ 1);
+                if (n % 4 == 2) request(n / 4, now);
+                one(n, a1, b1);
             }
-            now ^= COPY;
-        }
-    } else {
+        } else {
 #pragma unroll
-        for (int n = 0; n < 16; ++n) take(n, a1, 1, b0, 0, now);
-        for (int32_t s = first; s < last; ++s) {
-#pragma unroll
-            for (int n = 0; n < 16; ++n) {
-                take(n, a0, 0, b1, 1, now);
-                four(n, a1, b0);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int n = 0; n < 64; ++n) {
+                if (n % 4 == 0) take(n / 4, a0, 0, b1, 1, now);
+                one(n, a1, b0);
             }
 #pragma unroll
-            for (int n = 0; n < 16; ++n) {
-                four(n, a0, b0);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int n = 0; n < 64; ++n) one(n, a0, b0);
+            aim(s + 2);
             dense_meet();
 #pragma unroll
-            for (int n = 0; n < 16; ++n) {
-                request(n, s + 2, now);
-                take(n, a1, 1, b0, 0, now ^ COPY);
-                four(n, a0, b1);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int n = 0; n < 64; ++n) {
+                if (n % 4 == 0) take(n / 4, a1, 1, b0, 0, now ^ 1);
+                if (n % 4 == 2) request(n / 4, now);
+                one(n, a0, b1);
             }
-            now ^= COPY;
         }
+    };
+#pragma unroll
+    for (int n = 0; n < 16; ++n) take(n, P == 1 ? a0 : a1, P == 1 ? 0 : 1, b0, 0, 0);
+    int32_t s = first;
+    for (; s + 1 < last; s += 2) {
+        step(std::integral_constant<int, 0>{}, s);
+        step(std::integral_constant<int, 1>{}, s + 1);
     }
+    if (s < last) step(std::integral_constant<int, 0>{}, s);
     dense_settle();
     dense_meet();
     dense_finish<B, B, 2, 2, E>(g, e, tm, tn, M, acc, lds);
