@@ -64,23 +64,6 @@ struct DenseTile {
         base = o.p + matrix * o.matrix + (ALONG ? (int64_t)first * o.pitch : (int64_t)first * 2);
         step = ALONG ? BK * 2 : BK * o.pitch;
     }
-    // step s of K reduction indices, into `to`; what lies past them is 0
-    __device__ __forceinline__ void request(int32_t s, int32_t K, char* to) const {
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)s * step), 0, 0x7fffffff, 0x00020000);
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-        const int32_t left = K - s * BK;
-#pragma unroll
-        for (int i = 0; i < REQ; ++i) {
-            uint32_t at = off[i];
-            if (left < BK) {
-                int line, unit;
-                which(i, line, unit);
-                const int k = ALONG ? (P == 1 ? unit : unit & 3) * 8 : P == 1 ? line : line & 31;
-                at = k < left ? at : DENSE_NOWHERE;
-            }
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + (i * T + wave * 64) * 16), 16, at, 0, 0, 0);
-        }
-    }
     // Request i alone, by hand: the compiler takes a request for a write of LDS that every later read of LDS has to wait for, and cannot know that the two go to different copies. What it
     // fills is waited for in dense_meet(). Nothing is masked here: cut() comes before the first step that is not whole.
     __device__ __forceinline__ i32x4 source(int32_t s) const {
@@ -197,19 +180,30 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
     }
 }
 
-constexpr int dense_shared(int P, int BM, int BN, int WM, int WN) {
-    const int tiles = 2 * (BM + BN) * dense_slabs(P) * 64, rows = WM * WN * (BM / WM < 32 ? BM / WM : 32) * (BN / WN + 4) * 4;
+constexpr int dense_shared(int P, int BM, int BN, int WM, int WN, int STAGES) {
+    const int tiles = STAGES * (BM + BN) * dense_slabs(P) * 64, rows = WM * WN * (BM / WM < 32 ? BM / WM : 32) * (BN / WN + 4) * 4;
     return tiles > rows ? tiles : rows;
 }
 
-// C's tile of BM x BN by WM x WN wavefronts, each BM/WM x BN/WN of it in fragments of 16 x 16; two LDS copies, the next step's on its way while this one's is multiplied. For tiles of which
-// a compute unit holds several blocks, or a wavefront's registers do not hold the next fragments beside these.
-template <typename H, int P, bool AL, bool BL, int BM, int BN, int WM, int WN, typename E>
+// Waits for this wavefront's requests but the youngest YOUNG and for its LDS reads, then for the block: what those requests filled stands in LDS for all, and what was read before may be
+// overwritten.
+template <int YOUNG>
+__device__ __forceinline__ void dense_meet() {
+    static_assert(YOUNG < 64, "the counter's range");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(YOUNG) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// C's tile of BM x BN by WM x WN wavefronts, each BM/WM x BN/WN of it in fragments of 16 x 16, and STAGES copies in LDS: while a step is multiplied, the next STAGES - 1 are on their way.
+// For tiles of which a compute unit holds several blocks (two copies), for grids that leave it but one (four: the memory's latency is then what a step costs), and for values in three pieces.
+template <typename H, int P, bool AL, bool BL, int BM, int BN, int WM, int WN, int STAGES, typename E>
 __global__ void __launch_bounds__(64 * WM * WN) dense_kernel(const DenseArgs g, const typename E::Args e) {
     constexpr int T = 64 * WM * WN, I = BM / WM / 16, J = BN / WN / 16;
     typedef DenseTile<P, AL, BM, T> TA;
     typedef DenseTile<P, BL, BN, T> TB;
-    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, WM, WN)];
+    constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
+    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, WM, WN, STAGES)];
     int tm, tn;
     if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
     const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * BM, n0 = tn * BN;
@@ -222,7 +216,8 @@ __global__ void __launch_bounds__(64 * WM * WN) dense_kernel(const DenseArgs g, 
     ta.open(oa, blockIdx.z, m0);
     tb.open(g.b, blockIdx.z, n0);
     const int32_t steps = (K + TA::BK - 1) / TA::BK, first = (int32_t)((int64_t)steps * blockIdx.y / g.splits), last = (int32_t)((int64_t)steps * (blockIdx.y + 1) / g.splits);
-    const int32_t KA = AL ? (K + 7) & ~7 : K, KB = BL ? (K + 7) & ~7 : K;
+    const int32_t whole = K / TA::BK;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + (uint32_t)wave * 1024u);
     f32x4 acc[I][J];
     f32x4 big[P == 3 ? I : 1][P == 3 ? J : 1];       // of three pieces: the largest product's sums apart from the other five's
 #pragma unroll
@@ -232,17 +227,26 @@ __global__ void __launch_bounds__(64 * WM * WN) dense_kernel(const DenseArgs g, 
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             if constexpr (P == 3) big[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-    char* now = lds;
-    char* then = lds + TA::BYTES + TB::BYTES;
-    auto request = [&](int32_t s, char* to) {
-        ta.request(s, KA, to);
-        tb.request(s, KB, to + TA::BYTES);
+    // (steps past K are zeros, those past `last` are loaded and not used)
+    auto request = [&](int32_t s, uint32_t copy) {
+        if (s >= whole) {
+            const int32_t left = K - s * TA::BK;
+            ta.cut(AL ? (left + 7) & ~7 : left);
+            tb.cut(BL ? (left + 7) & ~7 : left);
+        }
+        const i32x4 ra = ta.source(s), rb = tb.source(s);
+#pragma unroll
+        for (int i = 0; i < TA::REQ; ++i) ta.request_one(i, ra, lds0 + copy);
+#pragma unroll
+        for (int i = 0; i < TB::REQ; ++i) tb.request_one(i, rb, lds0 + copy + TA::BYTES);
     };
-    if (first < last) request(first, now);
+#pragma unroll
+    for (int c = 0; c < STAGES - 1; ++c) request(first + c, c * COPY);
+    uint32_t at = 0;
     for (int32_t s = first; s < last; ++s) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0): this step's operands have arrived
-        __syncthreads();
-        if (s + 1 < last) request(s + 1, then);
+        dense_meet<REQ * (STAGES - 2)>();
+        request(s + STAGES - 1, at == 0 ? (STAGES - 1) * COPY : at - COPY);        // into the copy of the step before
+        const char* now = lds + at;
         auto take_a = [&](s16x8 (&a)[I], int h) {
 #pragma unroll
             for (int i = 0; i < I; ++i) a[i] = TA::fragment(now, wm * I + i, h);
@@ -284,23 +288,17 @@ __global__ void __launch_bounds__(64 * WM * WN) dense_kernel(const DenseArgs g, 
             dense_multiply<H>(acc, a[1], b[0]);
             dense_multiply<H>(acc, a[0], b[1]);
         }
-        char* t = now; now = then; then = t;
+        at = at == (STAGES - 1) * COPY ? 0 : at + COPY;
     }
     if constexpr (P == 3)
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
             for (int j = 0; j < J; ++j) acc[i][j] += big[i][j];
-    __syncthreads();
+    dense_meet<0>();
     dense_finish<BM, BN, WM, WN, E>(g, e, tm, tn, M, acc, lds);
 }
 
-// Waits for this wavefront's requests and LDS reads, then for the block: what was requested before stands in LDS for all, and what was read before may be overwritten.
-__device__ __forceinline__ void dense_meet() {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
 // One product into accumulation registers. (Left to the compiler, sums that fill half of a wavefront's registers are moved to and fro between the two kinds in every step.) Operands come from
 // LDS reads, which the compiler waits for; after the last one dense_settle() has to stand before the sums are read.
 template <typename H> __device__ __forceinline__ void dense_mfma_in_place(f32x4& c, s16x8 b, s16x8 a);
@@ -321,7 +319,7 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
     constexpr int B = 256, T = 256, I = 8, J = 8;
     typedef DenseTile<P, AL, B, T> TA;
     typedef DenseTile<P, BL, B, T> TB;
-    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, B, B, 2, 2)];
+    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, B, B, 2, 2, 2)];
     int tm, tn;
     if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
     const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * B, n0 = tn * B;
@@ -379,7 +377,7 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
     aim(first + 1);
 #pragma unroll
     for (int n = 0; n < REQ; ++n) request(n, 1);
-    dense_meet();
+    dense_meet<0>();
     s16x8 a0[I], a1[I], b0[J], b1[J];
     auto step = [&](auto copy_of, int32_t s) {
         constexpr int now = decltype(copy_of)::value;
@@ -390,7 +388,7 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
                 one(n, a0, b0);
             }
             aim(s + 2);
-            dense_meet();
+            dense_meet<0>();
 #pragma unroll
             for (int n = 0; n < 64; ++n) {
                 if (n % 4 == 0) take(n / 4, a0, 0, b0, 0, now ^ 1);
@@ -406,7 +404,7 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
 #pragma unroll
             for (int n = 0; n < 64; ++n) one(n, a0, b0);
             aim(s + 2);
-            dense_meet();
+            dense_meet<0>();
 #pragma unroll
             for (int n = 0; n < 64; ++n) {
                 if (n % 4 == 0) take(n / 4, a1, 1, b0, 0, now ^ 1);
@@ -424,7 +422,7 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
     }
     if (s < last) step(std::integral_constant<int, 0>{}, s);
     dense_settle();
-    dense_meet();
+    dense_meet<0>();
     dense_finish<B, B, 2, 2, E>(g, e, tm, tn, M, acc, lds);
 }
 

@@ -194,9 +194,13 @@ static void ns_product(const NsMatrix& a, int32_t a_extent, const NsMatrix& b, i
     g.tiles_m = (int32_t)ceil_div(M, tile);
     g.tiles_n = (int32_t)ceil_div(N, tile);
     const dim3 grid(dense_grid(g.tiles_m, g.tiles_n, HALF), 1, (unsigned)matrices);
+#define NO_DENSE(B, STAGES) hipLaunchKernelGGL((dense_kernel<_Float16, 2, AL, BL, B, B, 2, 2, STAGES, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e)
+    const int64_t blocks = (int64_t)grid.x * matrices;
     if (tile == 256) hipLaunchKernelGGL((dense_large_kernel<_Float16, 2, AL, BL, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e);
-    else if (tile == 128) hipLaunchKernelGGL((dense_kernel<_Float16, 2, AL, BL, 128, 128, 2, 2, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e);
-    else hipLaunchKernelGGL((dense_kernel<_Float16, 2, AL, BL, 64, 64, 2, 2, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e);
+    else if (tile == 128) { if (blocks <= 256) NO_DENSE(128, 4); else NO_DENSE(128, 2); }
+    else if (blocks <= 512) NO_DENSE(64, 4);
+    else NO_DENSE(64, 2);
+#undef NO_DENSE
 }
 
 struct NsRoom {
