@@ -42,14 +42,14 @@ constexpr uint32_t DENSE_NOWHERE = 0x80000000u;      // past every buffer's rang
 template <int P, bool ALONG, int R, int T>
 struct DenseTile {
     static constexpr int SLABS = dense_slabs(P), BK = dense_bk(P), PER_ROW = ALONG ? SLABS * 4 : R / 8, BYTES = R * SLABS * 64, REQ = BYTES / (16 * T);
-    static_assert(BYTES % (16 * T) == 0 && (ALONG || (R >= 64 && T % PER_ROW == 0)), "whole requests");
+    static_assert(BYTES % (16 * T) == 0 && (ALONG || (R >= 32 && T % PER_ROW == 0)), "whole requests");
     uint32_t off[REQ];
     const char* base;                   // the tile's origin in the matrix
     int64_t step;                       // bytes from one step to the next
     __device__ __forceinline__ static int mix(int k) { return ((k & 3) | (k >> 3 & 1) << 2) & (R / 16 - 1); }
     // what request i of this thread asks for: line of the tile, unit of the line
     __device__ __forceinline__ static void which(int i, int& line, int& unit) {
-        const int c = i * T + (int)threadIdx.x, place = c % PER_ROW;
+        const int c = i * T + ((int)threadIdx.x & (T - 1)), place = c % PER_ROW;
         line = c / PER_ROW;
         unit = !ALONG ? ((place >> 1) ^ mix(line)) << 1 | (place & 1) : P == 3 ? place ^ (line >> 2 & 3) : place ^ (line & 7);
     }
@@ -180,8 +180,8 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
     }
 }
 
-constexpr int dense_shared(int P, int BM, int BN, int WM, int WN, int STAGES) {
-    const int tiles = STAGES * (BM + BN) * dense_slabs(P) * 64, rows = WM * WN * (BM / WM < 32 ? BM / WM : 32) * (BN / WN + 4) * 4;
+constexpr int dense_shared(int P, int BM, int BN, int WM, int WN, int STAGES, int GROUPS = 1) {
+    const int tiles = GROUPS * STAGES * (BM + BN) * dense_slabs(P) * 64, rows = WM * WN * (BM / WM < 32 ? BM / WM : 32) * (BN / WN + 4) * 4;
     return tiles > rows ? tiles : rows;
 }
 
@@ -195,110 +195,6 @@ __device__ __forceinline__ void dense_meet() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// C's tile of BM x BN by WM x WN wavefronts, each BM/WM x BN/WN of it in fragments of 16 x 16, and STAGES copies in LDS: while a step is multiplied, the next STAGES - 1 are on their way.
-// For tiles of which a compute unit holds several blocks (two copies), for grids that leave it but one (four: the memory's latency is then what a step costs), and for values in three pieces.
-template <typename H, int P, bool AL, bool BL, int BM, int BN, int WM, int WN, int STAGES, typename E>
-__global__ void __launch_bounds__(64 * WM * WN) dense_kernel(const DenseArgs g, const typename E::Args e) {
-    constexpr int T = 64 * WM * WN, I = BM / WM / 16, J = BN / WN / 16;
-    typedef DenseTile<P, AL, BM, T> TA;
-    typedef DenseTile<P, BL, BN, T> TB;
-    constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
-    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, WM, WN, STAGES)];
-    int tm, tn;
-    if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
-    const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * BM, n0 = tn * BN;
-    if (m0 >= M) return;
-    const int wave = (int)threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
-    TA ta;
-    TB tb;
-    DenseOperand oa = g.a;
-    if (AL) oa.extent = min(oa.extent, M);
-    ta.open(oa, blockIdx.z, m0);
-    tb.open(g.b, blockIdx.z, n0);
-    const int32_t steps = (K + TA::BK - 1) / TA::BK, first = (int32_t)((int64_t)steps * blockIdx.y / g.splits), last = (int32_t)((int64_t)steps * (blockIdx.y + 1) / g.splits);
-    const int32_t whole = K / TA::BK;
-    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + (uint32_t)wave * 1024u);
-    f32x4 acc[I][J];
-    f32x4 big[P == 3 ? I : 1][P == 3 ? J : 1];       // of three pieces: the largest product's sums apart from the other five's
-#pragma unroll
-    for (int i = 0; i < I; ++i)
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if constexpr (P == 3) big[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        }
-    // (steps past K are zeros, those past `last` are loaded and not used)
-    auto request = [&](int32_t s, uint32_t copy) {
-        if (s >= whole) {
-            const int32_t left = K - s * TA::BK;
-            ta.cut(AL ? (left + 7) & ~7 : left);
-            tb.cut(BL ? (left + 7) & ~7 : left);
-        }
-        const i32x4 ra = ta.source(s), rb = tb.source(s);
-#pragma unroll
-        for (int i = 0; i < TA::REQ; ++i) ta.request_one(i, ra, lds0 + copy);
-#pragma unroll
-        for (int i = 0; i < TB::REQ; ++i) tb.request_one(i, rb, lds0 + copy + TA::BYTES);
-    };
-#pragma unroll
-    for (int c = 0; c < STAGES - 1; ++c) request(first + c, c * COPY);
-    uint32_t at = 0;
-    for (int32_t s = first; s < last; ++s) {
-        dense_meet<REQ * (STAGES - 2)>();
-        request(s + STAGES - 1, at == 0 ? (STAGES - 1) * COPY : at - COPY);        // into the copy of the step before
-        const char* now = lds + at;
-        auto take_a = [&](s16x8 (&a)[I], int h) {
-#pragma unroll
-            for (int i = 0; i < I; ++i) a[i] = TA::fragment(now, wm * I + i, h);
-        };
-        auto take_b = [&](s16x8 (&b)[J], int h) {
-#pragma unroll
-            for (int j = 0; j < J; ++j) b[j] = TB::fragment(now + TA::BYTES, wn * J + j, h);
-        };
-        if constexpr (P == 1) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                s16x8 a[I], b[J];
-                take_b(b, h);
-                take_a(a, h);
-                dense_multiply<H>(acc, a, b);
-            }
-        } else if constexpr (P == 2) {
-            s16x8 a0[I], a1[I], b0[J], b1[J];
-            take_b(b0, 0);
-            take_a(a1, 1);
-            dense_multiply<H>(acc, a1, b0);
-            take_b(b1, 1);
-            take_a(a0, 0);
-            dense_multiply<H>(acc, a0, b1);
-            dense_multiply<H>(acc, a0, b0);
-        } else {
-            // (a2 b0) (a0 b2) (a1 b1) (a1 b0) (a0 b1), and (a0 b0) apart
-            s16x8 a[3][I], b[3][J];
-            take_b(b[0], 0);
-            take_a(a[2], 2);
-            dense_multiply<H>(acc, a[2], b[0]);
-            take_a(a[0], 0);
-            dense_multiply<H>(big, a[0], b[0]);
-            take_b(b[2], 2);
-            dense_multiply<H>(acc, a[0], b[2]);
-            take_b(b[1], 1);
-            take_a(a[1], 1);
-            dense_multiply<H>(acc, a[1], b[1]);
-            dense_multiply<H>(acc, a[1], b[0]);
-            dense_multiply<H>(acc, a[0], b[1]);
-        }
-        at = at == (STAGES - 1) * COPY ? 0 : at + COPY;
-    }
-    if constexpr (P == 3)
-#pragma unroll
-        for (int i = 0; i < I; ++i)
-#pragma unroll
-            for (int j = 0; j < J; ++j) acc[i][j] += big[i][j];
-    dense_meet<0>();
-    dense_finish<BM, BN, WM, WN, E>(g, e, tm, tn, M, acc, lds);
-}
-
 // One product into accumulation registers. (Left to the compiler, sums that fill half of a wavefront's registers are moved to and fro between the two kinds in every step.) Operands come from
 // LDS reads, which the compiler waits for; after the last one dense_settle() has to stand before the sums are read.
 template <typename H> __device__ __forceinline__ void dense_mfma_in_place(f32x4& c, s16x8 b, s16x8 a);
@@ -308,21 +204,159 @@ template <> __device__ __forceinline__ void dense_mfma_in_place<__bf16>(f32x4& c
 template <> __device__ __forceinline__ void dense_mfma_in_place<_Float16>(f32x4& c, s16x8 b, s16x8 a) {
     asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(b), "v"(a));
 }
-__device__ __forceinline__ void dense_settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+template <int I, int J>
+__device__ __forceinline__ void dense_settle(f32x4 (&acc)[I][J]) {
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) asm volatile("" : "+a"(acc[i][j]));      // (nothing reads them from before)
+}
 
-// The same for large products: a tile of 256 x 256 by four wavefronts of 128 x 128, one a SIMD, whose registers hold the next fragments beside the ones that are multiplied, so that reads of LDS,
-// requests and products go on together, and the block meets once a step. A copy of LDS is free when its last fragments are in registers: the step after next is requested right then, and has a
-// whole step's time to arrive. LDS is read 16 bytes for 8192 multiplications (by eight wavefronts of 128 x 64: 24 bytes, which takes LDS as long as the products).
-template <typename H, int P, bool AL, bool BL, typename E>
-__global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, const typename E::Args e) {
-    static_assert(P <= 2, "three pieces do not fit the registers");
-    constexpr int B = 256, T = 256, I = 8, J = 8;
-    typedef DenseTile<P, AL, B, T> TA;
-    typedef DenseTile<P, BL, B, T> TB;
-    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, B, B, 2, 2, 2)];
+// C's tile of BM x BN by WM x WN wavefronts, each BM/WM x BN/WN of it in fragments of 16 x 16, and STAGES copies in LDS. While a step is multiplied, the fragments of the next are read into the
+// other half of a wavefront's registers, and the step STAGES further on is requested into the copy whose fragments are being multiplied. The block meets once a step.
+// GROUPS of so many wavefronts take the steps in turn, each with copies of its own, and the first adds up the others' sums in order: for products so small that the steps' number is what they last.
+template <typename H, int P, bool AL, bool BL, int BM, int BN, int WM, int WN, int STAGES, int GROUPS, typename E>
+__global__ void __launch_bounds__(64 * WM * WN * GROUPS) dense_kernel(const DenseArgs g, const typename E::Args e) {
+    constexpr int T = 64 * WM * WN, I = BM / WM / 16, J = BN / WN / 16, S = dense_slabs(P), PAIRS = P == 1 ? 2 : P == 2 ? 3 : 6;
+    typedef DenseTile<P, AL, BM, T> TA;
+    typedef DenseTile<P, BL, BN, T> TB;
+    constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
+    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, WM, WN, STAGES, GROUPS)];
     int tm, tn;
     if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
-    const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * B, n0 = tn * B;
+    const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * BM, n0 = tn * BN;
+    if (m0 >= M) return;
+    const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / T), wave = ((int)threadIdx.x & (T - 1)) >> 6, wm = wave / WN, wn = wave % WN;
+    char* const mine = lds + group * STAGES * COPY;
+    TA ta;
+    TB tb;
+    DenseOperand oa = g.a;
+    if (AL) oa.extent = min(oa.extent, M);
+    ta.open(oa, blockIdx.z, m0);
+    tb.open(g.b, blockIdx.z, n0);
+    const int32_t steps = (K + TA::BK - 1) / TA::BK, first = (int32_t)((int64_t)steps * blockIdx.y / g.splits), last = (int32_t)((int64_t)steps * (blockIdx.y + 1) / g.splits);
+    const int32_t end = min(K, last * TA::BK), whole = end / TA::BK;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine + (uint32_t)wave * 1024u);
+    f32x4 acc[I][J];
+    f32x4 big[P == 3 ? I : 1][P == 3 ? J : 1];       // of three pieces: the largest product's sums apart from the other five's
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            asm volatile("" : "+a"(acc[i][j]));
+            if constexpr (P == 3) {
+                big[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                asm volatile("" : "+a"(big[i][j]));
+            }
+        }
+    i32x4 ra, rb;
+    // what comes before the requests of step s (those past `last` are zeros)
+    auto aim = [&](int32_t s) {
+        if (s >= whole) {
+            const int32_t left = end - s * TA::BK;
+            ta.cut(AL ? (left + 7) & ~7 : left);
+            tb.cut(BL ? (left + 7) & ~7 : left);
+        }
+        ra = ta.source(s);
+        rb = tb.source(s);
+    };
+    auto request = [&](int n, uint32_t copy) {
+        if (n < TA::REQ) ta.request_one(n, ra, lds0 + copy);
+        else tb.request_one(n - TA::REQ, rb, lds0 + copy + TA::BYTES);
+    };
+    s16x8 fa[2][S][I], fb[2][S][J];
+    // the pairs of slabs that are multiplied, in order; of pieces the smallest products first
+    constexpr int PA[3][6] = {{0, 1}, {1, 0, 0}, {2, 0, 1, 1, 0, 0}}, PB[3][6] = {{0, 1}, {0, 1, 0}, {0, 2, 1, 0, 1, 0}};
+    // fragment n of a step's, in the order in which the pairs want them: b before a, slab by slab
+    auto take = [&](int n, s16x8 (&a)[S][I], s16x8 (&b)[S][J], const char* from) {
+        constexpr int OA[3][3] = {{0, 1}, {1, 0}, {2, 0, 1}}, OB[3][3] = {{0, 1}, {0, 1}, {0, 2, 1}};
+        const int h = n / (I + J), k = n % (I + J);
+        if (k < J) b[OB[P - 1][h]][k] = TB::fragment(from + TA::BYTES, wn * J + k, OB[P - 1][h]);
+        else a[OA[P - 1][h]][k - J] = TA::fragment(from, wm * I + k - J, OA[P - 1][h]);
+    };
+    constexpr int PRODUCTS = PAIRS * I * J, READS = S * (I + J), ITEMS = READS + REQ;
+    uint32_t at = 0;        // the copy of the step that is multiplied
+    auto step = [&](auto half_of, int32_t s) {
+        constexpr int half = decltype(half_of)::value;
+        dense_meet<REQ * (STAGES - 2)>();
+        const uint32_t next = at == (STAGES - 1) * COPY ? 0 : at + COPY;
+        aim(s + STAGES * GROUPS);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < PRODUCTS; ++n) {
+#pragma unroll
+            for (int k = n * ITEMS / PRODUCTS; k < (n + 1) * ITEMS / PRODUCTS; ++k) {
+                if (k < READS) take(k, fa[half ^ 1], fb[half ^ 1], mine + next);
+                else request(k - READS, at);
+            }
+            const int pair = n / (I * J), i = n / J % I, j = n % J;
+            if (P == 3 && pair == 5) dense_mfma_in_place<H>(big[P == 3 ? i : 0][P == 3 ? j : 0], fb[half][PB[P - 1][pair]][j], fa[half][PA[P - 1][pair]][i]);
+            else dense_mfma_in_place<H>(acc[i][j], fb[half][PB[P - 1][pair]][j], fa[half][PA[P - 1][pair]][i]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        at = next;
+    };
+#pragma unroll
+    for (int c = 0; c < STAGES; ++c) {
+        aim(first + group + c * GROUPS);
+#pragma unroll
+        for (int n = 0; n < REQ; ++n) request(n, c * COPY);
+    }
+    dense_meet<REQ * (STAGES - 1)>();
+#pragma unroll
+    for (int n = 0; n < READS; ++n) take(n, fa[0], fb[0], mine);
+    const int32_t turns = (last - first + GROUPS - 1) / GROUPS;      // (as many for every group: steps past `last` are zeros)
+    int32_t turn = 0;
+    for (; turn + 1 < turns; turn += 2) {
+        step(std::integral_constant<int, 0>{}, first + group + turn * GROUPS);
+        step(std::integral_constant<int, 1>{}, first + group + (turn + 1) * GROUPS);
+    }
+    if (turn < turns) step(std::integral_constant<int, 0>{}, first + group + turn * GROUPS);
+    dense_settle(acc);
+    if constexpr (P == 3) dense_settle(big);
+    if constexpr (P == 3)
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < J; ++j) acc[i][j] += big[i][j];
+    dense_meet<0>();
+    if constexpr (GROUPS > 1) {
+        static_assert((GROUPS - 1) * I * J * T * 16 <= (int)sizeof(lds), "room for the other groups' sums");
+        f32x4* sums = reinterpret_cast<f32x4*>(lds) + ((int)threadIdx.x & (T - 1));
+        if (group > 0)
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int j = 0; j < J; ++j) sums[((group - 1) * I * J + i * J + j) * T] = acc[i][j];
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+            for (int k = 1; k < GROUPS; ++k)
+#pragma unroll
+                for (int i = 0; i < I; ++i)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) acc[i][j] += sums[((k - 1) * I * J + i * J + j) * T];
+        __syncthreads();
+        if (group > 0) return;
+    }
+    dense_finish<BM, BN, WM, WN, E>(g, e, tm, tn, M, acc, lds);
+}
+
+// The same for large products: a tile of 256 x 256 (three pieces: 256 x 128) by four wavefronts of a quarter each, one a SIMD, whose sums fill the accumulation registers; the others hold one set of
+// fragments a slab, and a set is read again when the products that want it are done. A copy of LDS is free when its last fragments are in registers: the step after next is requested right then, and
+// has a whole step's time to arrive. LDS is read 16 bytes for 8192 multiplications (by eight wavefronts of 128 x 64: 24 bytes, which takes LDS as long as the products).
+template <typename H, int P, bool AL, bool BL, typename E>
+__global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, const typename E::Args e) {
+    constexpr int BM = 256, BN = P < 3 ? 256 : 128, T = 256, I = 8, J = BN / 32, S = dense_slabs(P), N = I * J;
+    typedef DenseTile<P, AL, BM, T> TA;
+    typedef DenseTile<P, BL, BN, T> TB;
+    constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
+    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, 2, 2, 2)];
+    int tm, tn;
+    if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
+    const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * BM, n0 = tn * BN;
     if (m0 >= M) return;
     const int wave = (int)threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
     TA ta;
@@ -333,22 +367,25 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
     tb.open(g.b, blockIdx.z, n0);
     const int32_t steps = (K + TA::BK - 1) / TA::BK, first = (int32_t)((int64_t)steps * blockIdx.y / g.splits), last = (int32_t)((int64_t)steps * (blockIdx.y + 1) / g.splits);
     f32x4 acc[I][J];
+    f32x4 big[P == 3 ? I : 1][P == 3 ? J : 1];
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             asm volatile("" : "+a"(acc[i][j]));
+            if constexpr (P == 3) {
+                big[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                asm volatile("" : "+a"(big[i][j]));
+            }
         }
-    constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
-    static_assert(REQ == 16, "one request for four products");
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + (uint32_t)wave * 1024u);
-    const int32_t whole = K / TA::BK;
+    const int32_t end = min(K, last * TA::BK), whole = end / TA::BK;
     i32x4 ra, rb;
-    // what comes before the requests of step s (those past K are zeros, those past `last` are loaded and not used)
+    // what comes before the requests of step s (those past `last` are zeros)
     auto aim = [&](int32_t s) {
         if (s >= whole) {
-            const int32_t left = K - s * TA::BK;
+            const int32_t left = end - s * TA::BK;
             ta.cut(AL ? (left + 7) & ~7 : left);
             tb.cut(BL ? (left + 7) & ~7 : left);
         }
@@ -359,71 +396,179 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
         if (n < TA::REQ) ta.request_one(n, ra, lds0 + copy * COPY);
         else tb.request_one(n - TA::REQ, rb, lds0 + copy * COPY + TA::BYTES);
     };
-    auto take = [&](int n, s16x8 (&a)[I], int ha, s16x8 (&b)[J], int hb, int copy) {       // fragment n of the sixteen: in the order in which the products want them
-        if (n < 4) b[n] = TB::fragment(lds + copy * COPY + TA::BYTES, wn * J + n, hb);
-        else if (n == 4) a[0] = TA::fragment(lds + copy * COPY, wm * I, ha);
-        else if (n < 9) b[n - 1] = TB::fragment(lds + copy * COPY + TA::BYTES, wn * J + n - 1, hb);
-        else a[n - 8] = TA::fragment(lds + copy * COPY, wm * I + n - 8, ha);
-    };
-    // Product n of 64, and the end of what may stand beside it: a wavefront issues in order, and while a product is at work the next one waits, so that other instructions are free only
-    // one or two at a time, between products (four products and then what four of them need: 503 us for what takes 400 so).
-    auto one = [&](int n, s16x8 (&a)[I], s16x8 (&b)[J]) {
-        dense_mfma_in_place<H>(acc[n >> 3][n & 7], b[n & 7], a[n >> 3]);
+    s16x8 fa[S][I], fb[S][J];
+    auto take_a = [&](int h, int i, int copy) { fa[h][i] = TA::fragment(lds + copy * COPY, wm * I + i, h); };
+    auto take_b = [&](int h, int j, int copy) { fb[h][j] = TB::fragment(lds + copy * COPY + TA::BYTES, wn * J + j, h); };
+    // Product n of the N of two slabs, and the end of what may stand beside it: a wavefront issues in order, and while a product is at work the next one waits, so that other instructions are
+    // free only one or two at a time, between products (four products and then what four of them need: 503 us for what takes 465 so).
+    auto one = [&](int n, int ha, int hb, f32x4 (&c)[I][J]) {
+        dense_mfma_in_place<H>(c[n / J][n % J], fb[hb][n % J], fa[ha][n / J]);
         __builtin_amdgcn_sched_barrier(0);
     };
+    // `items` things spread over the N products, from `begin` on, the last of them no later than `until` of N
+    auto here = [](int n, int items, int until) { return n < until ? (n + 1) * items / until : items; };
+    auto begun = [](int n, int items, int until) { return n < until ? n * items / until : items; };
     aim(first);
 #pragma unroll
     for (int n = 0; n < REQ; ++n) request(n, 0);
     aim(first + 1);
 #pragma unroll
     for (int n = 0; n < REQ; ++n) request(n, 1);
-    dense_meet<0>();
-    s16x8 a0[I], a1[I], b0[J], b1[J];
+    dense_meet<REQ>();
     auto step = [&](auto copy_of, int32_t s) {
         constexpr int now = decltype(copy_of)::value;
         if constexpr (P == 1) {
 #pragma unroll
-            for (int n = 0; n < 64; ++n) {
-                if (n % 2 == 0 && n < 32) take(n / 2, a1, 1, b1, 1, now);
-                one(n, a0, b0);
+            for (int n = 0; n < N; ++n) {       // the second slab, b and a in turn
+#pragma unroll
+                for (int k = begun(n, I + J, N / 2); k < here(n, I + J, N / 2); ++k)
+                    if (k % 2) take_a(1, k / 2, now);
+                    else take_b(1, k / 2, now);
+                one(n, 0, 0, acc);
             }
             aim(s + 2);
             dense_meet<0>();
 #pragma unroll
-            for (int n = 0; n < 64; ++n) {
-                if (n % 4 == 0) take(n / 4, a0, 0, b0, 0, now ^ 1);
+            for (int n = 0; n < N; ++n) {
+                if (n % 4 == 0) { if (n / 4 < J) take_b(0, n / 4, now ^ 1); else take_a(0, n / 4 - J, now ^ 1); }
                 if (n % 4 == 2) request(n / 4, now);
-                one(n, a1, b1);
+                one(n, 1, 1, acc);
+            }
+        } else if constexpr (P == 2) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                if (n % 4 == 0) { if (n / 4 < I) take_a(0, n / 4, now); else take_b(1, n / 4 - I, now); }
+                one(n, 1, 0, acc);
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) one(n, 0, 0, acc);
+            aim(s + 2);
+            dense_meet<0>();
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                if (n % 4 == 0) { if (n / 4 < J) take_b(0, n / 4, now ^ 1); else take_a(1, n / 4 - J, now ^ 1); }
+                if (n % 4 == 2) request(n / 4, now);
+                one(n, 0, 1, acc);
             }
         } else {
 #pragma unroll
-            for (int n = 0; n < 64; ++n) {
-                if (n % 4 == 0) take(n / 4, a0, 0, b1, 1, now);
-                one(n, a1, b0);
+            for (int n = 0; n < N; ++n) {
+                if (n % 3 == 0 && n / 3 < I) take_a(0, n / 3, now);
+                one(n, 2, 0, acc);
             }
 #pragma unroll
-            for (int n = 0; n < 64; ++n) one(n, a0, b0);
+            for (int n = 0; n < N; ++n) {
+                if (n % 4 == 0 && n / 4 < J) take_b(2, n / 4, now);
+                one(n, 0, 0, big);
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                if (n % 3 == 0 && n / 3 < I) take_a(1, n / 3, now);
+                one(n, 0, 2, acc);
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                if (n % 4 == 0 && n / 4 < J) take_b(1, n / 4, now);
+                one(n, 1, 0, acc);
+            }
             aim(s + 2);
             dense_meet<0>();
 #pragma unroll
-            for (int n = 0; n < 64; ++n) {
-                if (n % 4 == 0) take(n / 4, a1, 1, b0, 0, now ^ 1);
-                if (n % 4 == 2) request(n / 4, now);
-                one(n, a0, b1);
+            for (int n = 0; n < N; ++n) {
+                if (n % 3 == 0 && n / 3 < I) take_a(2, n / 3, now ^ 1);
+                if (n % 3 == 1 && n / 3 < REQ / 2) request(n / 3, now);
+                one(n, 1, 1, acc);
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                if (n % 4 == 0 && n / 4 < J) take_b(0, n / 4, now ^ 1);
+                if (n % 3 == 1 && REQ / 2 + n / 3 < REQ) request(REQ / 2 + n / 3, now);
+                one(n, 0, 1, acc);
             }
         }
     };
+    static_assert(P == 3 ? REQ / 2 <= N / 3 && REQ - REQ / 2 <= N / 3 : REQ == N / 4, "a place for every request");
 #pragma unroll
-    for (int n = 0; n < 16; ++n) take(n, P == 1 ? a0 : a1, P == 1 ? 0 : 1, b0, 0, 0);
+    for (int j = 0; j < J; ++j) take_b(0, j, 0);
+#pragma unroll
+    for (int i = 0; i < I; ++i) take_a(P - 1, i, 0);
     int32_t s = first;
     for (; s + 1 < last; s += 2) {
         step(std::integral_constant<int, 0>{}, s);
         step(std::integral_constant<int, 1>{}, s + 1);
     }
     if (s < last) step(std::integral_constant<int, 0>{}, s);
-    dense_settle();
+    dense_settle(acc);
+    if constexpr (P == 3) {
+        dense_settle(big);
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < J; ++j) acc[i][j] += big[i][j];
+    }
     dense_meet<0>();
-    dense_finish<B, B, 2, 2, E>(g, e, tm, tn, M, acc, lds);
+    dense_finish<BM, BN, 2, 2, E>(g, e, tm, tn, M, acc, lds);
+}
+
+// ------------------------------------------------------------------------------------------------------- plans
+
+// Kinds of tiles: sides, blocks of which a compute unit holds at most `per_unit` (by their LDS), and an estimate of their time in microseconds: `start` for each round of blocks, and for each step `one`
+// where a compute unit has one block, `more` for each block beside it. Measured with all kinds in turn at sides from 64 to 4096, sums of 256 to 4096, one to eight products; the estimates are
+// within 20 % of those times, mostly. bf16, us, large / 128 / 128 deep / 64 / 64 deep / 64 in groups / 32: 4096^3 103 / 128 / 152 / 178 / 198 / 248 / 629; 2048 x 4096 x 2048
+// 51 / 36 / 46 / 52 / 58 / 75 / 211; 1024 x 1024 x 4096 78 / 54 / 33 / 37 / 18 / 19 / 41; 256 x 256 x 4096 77 / 38 / 32 / 24 / 17 / 15 / 10.
+struct DenseKind { int bm, bn, per_unit; double one, more, start; };
+struct DensePlan { int kind, splits; };
+enum { DENSE_LARGE, DENSE_128, DENSE_128_DEEP, DENSE_64, DENSE_64_DEEP, DENSE_64_GROUPS, DENSE_32, DENSE_KINDS };
+
+static const DenseKind DENSE_KIND[3][DENSE_KINDS] = {      // of one, two and three pieces
+    {{256, 256, 1, 1.35, 0, 8}, {128, 128, 2, 0.6, 0.35, 5}, {128, 128, 1, 0.5, 0, 5.5}, {64, 64, 5, 0.3, 0.12, 4}, {64, 64, 2, 0.21, 0.13, 3.7}, {64, 64, 1, 0.17, 0, 4.8}, {32, 32, 1, 0.08, 0, 4.8}},
+    {{256, 256, 1, 2.1, 0, 8}, {128, 128, 2, 0.95, 0.7, 5}, {128, 128, 1, 0.75, 0, 5}, {64, 64, 5, 0.42, 0.24, 4.5}, {64, 64, 2, 0.27, 0.17, 4}, {64, 64, 1, 0.24, 0, 5}, {32, 32, 1, 0.09, 0, 5.2}},
+    {{256, 128, 1, 1.9, 0, 8}, {128, 128, 1, 1.3, 0, 5}, {128, 128, 0, 0, 0, 0}, {64, 64, 3, 0.75, 0.25, 3}, {64, 64, 1, 0.42, 0, 3}, {64, 64, 0, 0, 0, 0}, {32, 32, 1, 0.25, 0, 3}}};
+
+// The kind of tile and the number of parts of the reduction that promise the shortest time; the parts' sums take at most `parts_most` bytes and a launch that joins them.
+static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matrices, bool half, size_t parts_most) {
+    const int64_t steps = ceil_div(K < 1 ? 1 : K, dense_bk(P));
+    DensePlan best{DENSE_64, 1};
+    double least = 1e300;
+    for (int kind = 0; kind < DENSE_KINDS; ++kind) {
+        const DenseKind& k = DENSE_KIND[P - 1][kind];
+        if (k.per_unit == 0) continue;
+        const int64_t a = ceil_div(M < 1 ? 1 : M, k.bm), b = ceil_div(N, k.bn), tiles = (half ? a * (a + 1) / 2 : a * b) * matrices;
+        for (int splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 2) {
+            if (splits > 1 && (steps < splits * 4 || (size_t)splits * M * N * 4 > parts_most)) break;
+            const int64_t units = ceil_div(tiles * splits, 256), rounds = ceil_div(units, k.per_unit);
+            double t = (double)rounds * ((double)ceil_div(steps, splits) * (k.one + k.more * (double)((rounds > 1 ? k.per_unit : units) - 1)) + k.start);
+            if (splits > 1) t += 4.0 + (double)splits * M * N * 8 / 4e6;
+            if (t < least) { least = t; best = DensePlan{kind, splits}; }
+        }
+    }
+    return best;
+}
+
+template <typename H, int P, bool AL, bool BL, typename E>
+static void dense_launch(DenseArgs g, const typename E::Args& e, const DensePlan& p, int64_t matrices, hipStream_t st) {
+    const DenseKind& k = DENSE_KIND[P - 1][p.kind];
+    g.splits = p.splits;
+    g.tiles_m = (int32_t)ceil_div(g.M, k.bm);
+    g.tiles_n = (int32_t)ceil_div(g.N, k.bn);
+    const dim3 grid(dense_grid(g.tiles_m, g.tiles_n, E::MIRROR), (unsigned)p.splits, (unsigned)matrices);
+#define NO_DENSE(BM, BN, WM, WN, STAGES, GROUPS) hipLaunchKernelGGL((dense_kernel<H, P, AL, BL, BM, BN, WM, WN, STAGES, GROUPS, E>), grid, dim3(64 * WM * WN * GROUPS), 0, st, g, e)
+    switch (p.kind) {
+        case DENSE_LARGE:
+            hipLaunchKernelGGL((dense_large_kernel<H, P, AL, BL, E>), grid, dim3(256), 0, st, g, e);
+            break;
+        case DENSE_128: NO_DENSE(128, 128, 2, 2, P < 3 ? 2 : 3, 1); break;
+        case DENSE_128_DEEP:
+            if constexpr (P < 3) NO_DENSE(128, 128, 2, 2, 4, 1);
+            break;
+        case DENSE_64: NO_DENSE(64, 64, 2, 2, 2, 1); break;
+        case DENSE_64_DEEP: NO_DENSE(64, 64, 2, 2, 4, 1); break;
+        case DENSE_64_GROUPS:
+            if constexpr (P < 3) NO_DENSE(64, 64, 2, 2, 4, 2);
+            break;
+        default: NO_DENSE(32, 32, 1, 1, P < 3 ? 4 : 3, 4); break;
+    }
+#undef NO_DENSE
 }
 
 }  // namespace no

@@ -297,6 +297,16 @@ static inline int64_t layernorm_blocks(int64_t n, int per_block, int64_t most) {
     return b < most ? b : most;
 }
 
+// The forward pass's most blocks. A block that walks several rows reads weights and biases (twice the bytes of a bf16 row) once: 50001 x 602 fp32 into bf16 40.3 us with 1024 blocks, 54.7 with one for every four rows;
+// 16384 x 4096 bf16 with residual 95.4 with 8192, 97 with 4096 and 101 with 16384; 8000 x 8192 62.4 with 4096, 75.6 with 1024; 4000 x 16384 101 with 1024, 109 with all. Rows of 512 or 1024 values are no faster so (30000 x
+// 1024 bf16 42.8, 43.5 with 1024; 100000 x 256 fp32 71.5 and 79.1).
+static inline int64_t layernorm_most(int team, int u) {
+    if (team == 1024) return 256;
+    if (team < 64) return 2048;
+    if (team == 64) return u >= 3 ? 1024 : 1 << 20;
+    return u == 2 ? 8192 : u == 4 ? 4096 : 1024;
+}
+
 }  // namespace no
 
 using namespace no;
@@ -319,7 +329,7 @@ extern "C" int32_t no_layernorm_fwd(const void* d_x, no_dtype dt, int64_t x_stri
     const RowsOf x = rows_of(d_x, x_stride_bytes), r = rows_of(d_residual, residual_stride_bytes), s = rows_of(d_sum, sum_stride_bytes), y = rows_of(d_y, y_stride_bytes);
     hipStream_t st = (hipStream_t)stream;
 #define NO_NORM_AS(T, Y, TEAM, THREADS, U)                                                                                                                           \
-    hipLaunchKernelGGL((layernorm_fwd_kernel<T, Y, TEAM, THREADS, U>), dim3((unsigned)layernorm_blocks(n_rows_cap, THREADS / TEAM, THREADS == 1024 ? 256 : TEAM < 64 ? 2048 : 1 << 20)), \
+    hipLaunchKernelGGL((layernorm_fwd_kernel<T, Y, TEAM, THREADS, U>), dim3((unsigned)layernorm_blocks(n_rows_cap, THREADS / TEAM, layernorm_most(TEAM, U))), \
                        dim3(THREADS), 0, st, x, r, d_weight, d_bias, eps, d_n_rows, n_rows_cap, dim, s, y, d_mean, d_rstd)
 #define NO_NORM(T, Y)                                              \
     do {                                                           \
@@ -393,7 +403,8 @@ extern "C" int32_t no_layernorm_bwd(const void* d_s, no_dtype dt, int64_t s_stri
         else if (units <= 64) NO_NORM_AS(T, 64, 256, 1);                                                                                             \
         else if (units <= 128) NO_NORM_AS(T, 64, 256, 2);                                                                                            \
         else if (units <= 192) NO_NORM_AS(T, 64, 256, 3);                                                                                            \
-        else if (units <= 256) NO_NORM_AS(T, 64, 256, 4);                                                                                            \
+        /* (16384 x 2048 bf16 with grad_sum 63.0 us by a block a row, 66.2 by a wavefront, whose sums leave no registers for the next row; fp32 rows of as many bytes 93.7 and 92.6) */ \
+        else if (units <= 256) NO_NORM_AS(T, (sizeof(T) == 2 ? 256 : 64), 256, (sizeof(T) == 2 ? 1 : 4));                                            \
         else if (units <= 512) NO_NORM_AS(T, 256, 256, 2);                                                                                           \
         else if (units <= 1024) NO_NORM_AS(T, 256, 256, 4);                                                                                          \
         else if (units <= 2048) NO_NORM_AS(T, 1024, 1024, 2);                                                                                        \

@@ -105,10 +105,34 @@ struct LinearOut {
     }
 };
 
-// The parts of a split reduction added up, four columns a thread; LANES > 1: that many threads to a place, each with every LANES-th part, whose sums are added in order.
+// Column sums of gz from their parts: sixteen columns a block, sixteen threads to a column.
+struct BiasJob {
+    const float* parts;
+    int32_t n_parts, dim;
+    float* grad_bias;
+};
+__device__ __forceinline__ void bias_block(const BiasJob& j, int32_t block) {
+    __shared__ float share[16][17];
+    const int32_t col = (int32_t)threadIdx.x & 15, row = (int32_t)threadIdx.x >> 4, c = block * 16 + col;
+    float sum = 0.0f;
+    if (c < j.dim)
+#pragma unroll 4
+        for (int32_t p = row; p < j.n_parts; p += 16) sum += j.parts[(int64_t)p * j.dim + c];
+    share[row][col] = sum;
+    __syncthreads();
+    if (row > 0 || c >= j.dim) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += share[k][col];
+    j.grad_bias[c] = sum;
+}
+__global__ void __launch_bounds__(256) linear_bias_kernel(BiasJob j) { bias_block(j, (int32_t)blockIdx.x); }
+
+// The parts of a split reduction added up (the launch's other blocks: column sums), four columns a thread; LANES > 1: that many threads to a place, each with every LANES-th part, whose sums are added in order.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(256) linear_join_kernel(const float* __restrict__ parts, int32_t splits, int32_t M, const int32_t* d_M, int32_t N, LinearEnd e) {
+__global__ void __launch_bounds__(256) linear_join_kernel(const float* __restrict__ parts, int32_t splits, int32_t M, const int32_t* d_M, int32_t N, LinearEnd e, int32_t blocks, BiasJob bias) {
     constexpr int PLACES = 256 / LANES;
+    if ((int32_t)blockIdx.x >= blocks) return bias_block(bias, (int32_t)blockIdx.x - blocks);
     __shared__ float share[LANES][PLACES][4];
     const int place = (int)threadIdx.x % PLACES, lane = (int)threadIdx.x / PLACES;
     const int64_t per_row = ceil_div(N, 4), i = (int64_t)blockIdx.x * PLACES + place, m = i / per_row;
@@ -142,11 +166,12 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* __restric
     if (there) linear_end_of<T, 4>(e, m, n, here, v);
 }
 template <typename T>
-static void linear_join(const float* parts, int32_t splits, int32_t M, const int32_t* d_M, int32_t N, const LinearEnd& end, hipStream_t st) {
-    const int64_t places = (int64_t)M * ceil_div(N, 4);
-    if (splits >= 8 && places <= 65536)
-        hipLaunchKernelGGL((linear_join_kernel<T, 16>), dim3((unsigned)ceil_div(places, 16)), dim3(256), 0, st, parts, splits, M, d_M, N, end);
-    else hipLaunchKernelGGL((linear_join_kernel<T, 1>), dim3((unsigned)ceil_div(places, 256)), dim3(256), 0, st, parts, splits, M, d_M, N, end);
+static void linear_join(const float* parts, int32_t splits, int32_t M, const int32_t* d_M, int32_t N, const LinearEnd& end, const BiasJob& bias, hipStream_t st) {
+    const int64_t places = (int64_t)M * ceil_div(N, 4), more = bias.grad_bias ? ceil_div(bias.dim, 16) : 0;
+    const bool few = splits >= 8 && places <= 65536;
+    const int64_t blocks = ceil_div(places, few ? 16 : 256);
+    if (few) hipLaunchKernelGGL((linear_join_kernel<T, 16>), dim3((unsigned)(blocks + more)), dim3(256), 0, st, parts, splits, M, d_M, N, end, (int32_t)blocks, bias);
+    else hipLaunchKernelGGL((linear_join_kernel<T, 1>), dim3((unsigned)(blocks + more)), dim3(256), 0, st, parts, splits, M, d_M, N, end, (int32_t)blocks, bias);
 }
 
 // ------------------------------------------------------------------------------------------------------- operands
@@ -178,29 +203,50 @@ __device__ __forceinline__ void dense_put(const float (&f)[8], char* to, int32_t
     }
 }
 
+struct PackJob {
+    RowsOf x;
+    const int32_t* d_n;
+    int32_t cap, dim;
+    char* out;              // NULL: nothing to do
+    int64_t pitch;
+    int32_t plane, blocks;
+};
 template <typename T>
-__global__ void __launch_bounds__(256) linear_pack_kernel(RowsOf x, const int32_t* d_n, int32_t cap, int32_t dim, char* out, int64_t pitch, int32_t plane) {
-    const int32_t units = (dim + 7) / 8, n = rows_here(d_n, cap);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * units; i += (int64_t)gridDim.x * 256) {
+__device__ __forceinline__ void pack_block(const PackJob& j, int32_t block) {
+    const int32_t units = (j.dim + 7) / 8, n = rows_here(j.d_n, j.cap);
+    for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < (int64_t)n * units; i += (int64_t)j.blocks * 256) {
         const int64_t r = i / units;
         const int32_t c = (int32_t)(i - r * units) * 8;
         Run<T, 8> v;
         float f[8];
-        v.load_at(x.row<T>(r), c, dim, from_f32<T>(0.0f));
+        v.load_at(j.x.row<T>(r), c, j.dim, from_f32<T>(0.0f));
         v.get(f);
-        dense_put<T>(f, out + r * pitch + c * 2, plane);
+        dense_put<T>(f, j.out + r * j.pitch + c * 2, j.plane);
     }
+}
+template <typename T>
+__global__ void __launch_bounds__(256) linear_pack_kernel(PackJob a, PackJob b) {
+    if ((int32_t)blockIdx.x < a.blocks) pack_block<T>(a, (int32_t)blockIdx.x);
+    else pack_block<T>(b, (int32_t)blockIdx.x - a.blocks);
 }
 
 // The gradient of the pre-activation, gz = grad_y act'(z), laid out as an operand (gz NULL: grad_y is one as it stands), and its column sums over `per` rows a block: LANES threads along a
 // row, each with eight columns, and 256 / LANES rows at a time, whose sums are added in order; four of a thread's rows are requested at once.
+// The launch's other blocks lay out the rows of x and the matrix for the products behind it.
 template <typename T, int ACT, int LANES>
-__global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z, const int32_t* d_n, int32_t cap, int32_t dim, int32_t per, char* gz, int64_t pitch, int32_t plane,
-                                                        float* parts) {
+__global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z, const int32_t* d_n, int32_t cap, int32_t dim, int32_t per, int32_t wide, int32_t blocks, char* gz,
+                                                        int64_t pitch, int32_t plane, float* parts, PackJob a, PackJob b) {
     constexpr int LINES = 256 / LANES, AHEAD = 4;
     __shared__ float share[LINES][LANES * 8 + 4];
-    const int32_t n = rows_here(d_n, cap), lane = (int32_t)threadIdx.x % LANES, line = (int32_t)threadIdx.x / LANES, c = ((int32_t)blockIdx.x * LANES + lane) * 8;
-    const int64_t first = (int64_t)blockIdx.y * per, last = first + per < n ? first + per : n;
+    if ((int32_t)blockIdx.x >= blocks) {
+        const int32_t k = (int32_t)blockIdx.x - blocks;
+        if (k < a.blocks) pack_block<T>(a, k);
+        else pack_block<T>(b, k - a.blocks);
+        return;
+    }
+    const int32_t bx = (int32_t)blockIdx.x % wide, by = (int32_t)blockIdx.x / wide;
+    const int32_t n = rows_here(d_n, cap), lane = (int32_t)threadIdx.x % LANES, line = (int32_t)threadIdx.x / LANES, c = (bx * LANES + lane) * 8;
+    const int64_t first = (int64_t)by * per, last = first + per < n ? first + per : n;
     float sum[8] = {};
     if (c < dim) {
         for (int64_t r0 = first + line; r0 < last; r0 += AHEAD * LINES) {
@@ -232,28 +278,12 @@ __global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z,
 #pragma unroll
     for (int w = 0; w < 8; ++w) share[line][lane * 8 + w] = sum[w];
     __syncthreads();
-    const int32_t at = (int32_t)blockIdx.x * LANES * 8 + (int32_t)threadIdx.x;
+    const int32_t at = bx * LANES * 8 + (int32_t)threadIdx.x;
     if ((int32_t)threadIdx.x >= LANES * 8 || at >= dim) return;
     float total = 0.0f;
 #pragma unroll
     for (int k = 0; k < LINES; ++k) total += share[k][threadIdx.x];
-    parts[(int64_t)blockIdx.y * dim + at] = total;
-}
-
-// Sixteen columns a block, sixteen threads to a column.
-__global__ void __launch_bounds__(256) linear_bias_kernel(const float* __restrict__ parts, int32_t n_parts, int32_t dim, float* grad_bias) {
-    __shared__ float share[16][17];
-    const int32_t col = (int32_t)threadIdx.x & 15, row = (int32_t)threadIdx.x >> 4, c = (int32_t)blockIdx.x * 16 + col;
-    float sum = 0.0f;
-    if (c < dim)
-        for (int32_t p = row; p < n_parts; p += 16) sum += parts[(int64_t)p * dim + c];
-    share[row][col] = sum;
-    __syncthreads();
-    if (row > 0 || c >= dim) return;
-    sum = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) sum += share[k][col];
-    grad_bias[c] = sum;
+    parts[(int64_t)by * dim + at] = total;
 }
 
 // ------------------------------------------------------------------------------------------------------- few rows
@@ -337,32 +367,20 @@ __global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, con
 
 constexpr size_t LINEAR_PARTS_MOST = (size_t)128 << 20;      // bytes of parts, at most
 
-struct LinearPlan { int bm, bn, splits; };
+struct LinearPlan { int kind, splits; };
 
-// Tile and splits of a product of M x N over K of P pieces: the shortest estimate in microseconds. A step's time is that of a full chip, so a kind of tile takes rounds x (steps x step + start).
 static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int P) {
-    const int64_t steps = ceil_div(K < 1 ? 1 : K, dense_bk(P));
-    struct Kind { int bm, bn, slots; double step, start; };
-    static const Kind one[3] = {{256, 256, 256, 1.0, 5.0}, {128, 128, 512, 0.65, 4.0}, {64, 64, 1024, 0.45, 4.0}}, three[3] = {{256, 128, 256, 1.7, 5.0}, {128, 128, 256, 1.0, 4.0}, {64, 64, 768, 0.9, 4.0}};
-    LinearPlan best{64, 64, 1};
-    double least = 1e300;
-    for (const Kind& k : P == 1 ? one : three) {
-        const int64_t tiles = ceil_div(M < 1 ? 1 : M, k.bm) * ceil_div(N, k.bn);
-        for (int splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 2) {
-            if (splits > 1 && (steps < splits * 4 || (size_t)splits * M * N * 4 > LINEAR_PARTS_MOST)) break;
-            const double rounds = (double)ceil_div(tiles * splits, k.slots);
-            double t = rounds * (ceil_div(steps, splits) * k.step + k.start);
-            if (splits > 1) t += 4.0 + (double)splits * M * N * 8 / 4e6;
-            if (t < least) { least = t; best = LinearPlan{k.bm, k.bn, splits}; }
-        }
-    }
-    return best;
+    const DensePlan p = dense_plan(M, N, K, P, 1, false, LINEAR_PARTS_MOST);
+    return LinearPlan{p.kind, p.splits};
 }
-static int linear_few_splits(int64_t K, int64_t N, int es) {
-    const int64_t blocks = ceil_div(N, 8 * 16 / es);
+// Parts of the reduction: blocks with 128 KB of the matrix each, but where two parts would do so for few rows, whose join costs what it saves. us by 1 / 2 / 4 / 8 / 16 parts: one bf16 row, 8192
+// columns, K = 2048 11.2 / 11.9 / 11.6 / 13.9; 2048 columns, K = 8192 31.6 / 20.7 / 13.6 / 11.7 / 11.5; 4096 x 4096 16.8 / 13.9 / 11.9 / 11.5 / 13.8; eight rows, 8192 columns, K = 2048 29.6 / 24.3 / 31.7;
+// 2048 columns, K = 8192 88 / 54 / 33 / 24 / 32. Half of the columns a block (64 bytes of a row, not 128): 15.1 for 11.2, 33 for 30.
+static int linear_few_splits(int64_t K, int64_t N, int64_t rows, int es) {
+    const int64_t most = K / 128 < 1 ? 1 : K / 128, bytes = K * (N < 128 / es ? N : 128 / es) * es;
     int splits = 1;
-    while (splits < 32 && blocks * splits < 128 && K / (splits * 2) >= 256) splits *= 2;
-    return splits;
+    while (splits < 32 && splits * 2 <= most && bytes > splits * (128 << 10)) splits *= 2;
+    return splits == 2 && rows < 4 ? 1 : splits;
 }
 static size_t linear_parts_bytes(const LinearPlan& p, int64_t M, int64_t N) { return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0; }
 
@@ -377,71 +395,59 @@ static inline int64_t gz_blocks(int64_t n) {
 
 struct LinearRoom { char* p; size_t left; char* take(size_t b) { char* r = p; p += round_256(b); return r; } };
 
-// The operand that holds `rows` rows of `dim` values: the matrix itself where a product can take it, else a copy (fp32: planes).
+// The operand that holds `rows` rows of `dim` values: the matrix itself where a product can take it, else a copy (fp32: pieces) that `job` makes.
 template <typename T>
-static DenseOperand linear_operand(RowsOf x, const int32_t* d_n, int64_t rows, int32_t dim, LinearRoom& room, hipStream_t st) {
-    DenseOperand o;
-    if (sizeof(T) == 2 && (uintptr_t)x.p % 16 == 0 && x.stride % 16 == 0 && dim % 8 == 0 && x.stride <= (int64_t)1 << 22) {
-        o = DenseOperand{x.p, x.stride, 0, 0, 0};
-        return o;
-    }
-    const int32_t plane = (int32_t)wide_of(dim) * 2;
-    const int64_t pitch = (int64_t)plane * planes_of_type(TypeOf<T>::code);
-    char* to = room.take(operand_bytes(TypeOf<T>::code, rows, dim));
-    if (rows > 0) {
-        const int64_t blocks = ceil_div(rows * ((dim + 7) / 8), 256);
-        hipLaunchKernelGGL(linear_pack_kernel<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, x, d_n, (int32_t)rows, dim, to, pitch, plane);
-    }
-    return DenseOperand{to, pitch, 0, plane, 0};
+static DenseOperand linear_operand(RowsOf x, const int32_t* d_n, int64_t rows, int32_t dim, LinearRoom& room, PackJob& job) {
+    job = PackJob{x, d_n, (int32_t)rows, dim, nullptr, 0, 0, 0};
+    if (sizeof(T) == 2 && (uintptr_t)x.p % 16 == 0 && x.stride % 16 == 0 && dim % 8 == 0 && x.stride <= (int64_t)1 << 22) return DenseOperand{x.p, x.stride, 0, 0, 0};
+    job.plane = (int32_t)wide_of(dim) * 2;
+    job.pitch = (int64_t)job.plane * planes_of_type(TypeOf<T>::code);
+    job.out = room.take(operand_bytes(TypeOf<T>::code, rows, dim));
+    const int64_t blocks = ceil_div(rows * ((dim + 7) / 8), 256);
+    job.blocks = (int32_t)(blocks < 8192 ? blocks : 8192);
+    return DenseOperand{job.out, job.pitch, 0, job.plane, 0};
+}
+template <typename T>
+static void linear_pack(const PackJob& a, const PackJob& b, hipStream_t st) {
+    if (a.blocks + b.blocks > 0) hipLaunchKernelGGL(linear_pack_kernel<T>, dim3((unsigned)(a.blocks + b.blocks)), dim3(256), 0, st, a, b);
 }
 
 template <typename T, bool AL, bool BL>
-static void linear_product(DenseArgs g, const LinearEnd& end, float* parts, hipStream_t st) {
+static bool linear_product(DenseArgs g, const LinearEnd& end, float* parts, const BiasJob& bias, hipStream_t st) {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;
     const LinearPlan p = linear_plan(g.M, g.N, g.K, P);
-    g.splits = p.splits;
-    g.tiles_m = (int32_t)ceil_div(g.M, p.bm);
-    g.tiles_n = (int32_t)ceil_div(g.N, p.bn);
     const typename LinearOut<T>::Args e{end, p.splits > 1 ? parts : nullptr};
-    const dim3 grid(dense_grid(g.tiles_m, g.tiles_n, false), (unsigned)p.splits);
-#define NO_DENSE(BM, BN, WM, WN, STAGES) hipLaunchKernelGGL((dense_kernel<__bf16, P, AL, BL, BM, BN, WM, WN, STAGES, LinearOut<T>>), grid, dim3(64 * WM * WN), 0, st, g, e)
-    const int64_t blocks = (int64_t)g.tiles_m * g.tiles_n * p.splits;
-    if (p.bm == 256) {
-        if constexpr (P == 1) hipLaunchKernelGGL((dense_large_kernel<__bf16, P, AL, BL, LinearOut<T>>), grid, dim3(256), 0, st, g, e);
-        else NO_DENSE(256, 128, 4, 2, 2);
-    } else if (p.bm == 128) {
-        if (P == 1 && blocks <= 256) NO_DENSE(128, 128, 2, 2, P == 1 ? 4 : 3);
-        else NO_DENSE(128, 128, 2, 2, P == 1 ? 2 : 3);
-    } else if (blocks <= (P == 1 ? 512 : 256)) NO_DENSE(64, 64, 2, 2, 4);
-    else NO_DENSE(64, 64, 2, 2, 2);
-#undef NO_DENSE
-    if (p.splits > 1)
-        linear_join<T>(parts, p.splits, g.M, g.d_M, g.N, end, st);
+    dense_launch<__bf16, P, AL, BL, LinearOut<T>>(g, e, DensePlan{p.kind, p.splits}, 1, st);
+    if (p.splits > 1) linear_join<T>(parts, p.splits, g.M, g.d_M, g.N, end, bias, st);
+    return p.splits > 1;        // (the column sums went along)
 }
 
 template <typename T>
 static void linear_fwd(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int32_t d_in, int32_t d_out, const LinearEnd& end, char* ws, hipStream_t st) {
     LinearRoom room{ws, 0};
     if (cap <= LINEAR_FEW) {
-        const int splits = linear_few_splits(d_in, d_out, sizeof(T));
+        const int splits = linear_few_splits(d_in, d_out, cap, sizeof(T));
         float* parts = splits > 1 ? (float*)ws : nullptr;
-        const dim3 grid((unsigned)ceil_div(d_out, 8 * 16 / (int)sizeof(T)), (unsigned)splits);
-        if (cap <= 1) hipLaunchKernelGGL((linear_few_kernel<T, 1>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts);
-        else if (cap <= 2) hipLaunchKernelGGL((linear_few_kernel<T, 2>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts);
-        else if (cap <= 4) hipLaunchKernelGGL((linear_few_kernel<T, 4>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts);
-        else hipLaunchKernelGGL((linear_few_kernel<T, 8>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts);
-        if (splits > 1)
-            linear_join<T>(parts, splits, cap, d_n, d_out, end, st);
+        const dim3 grid((unsigned)ceil_div(d_out, 128 / (int)sizeof(T)), (unsigned)splits);
+#define NO_FEW(MR) hipLaunchKernelGGL((linear_few_kernel<T, MR>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts)
+        if (cap <= 1) NO_FEW(1);
+        else if (cap <= 2) NO_FEW(2);
+        else if (cap <= 4) NO_FEW(4);
+        else NO_FEW(8);
+#undef NO_FEW
+        if (splits > 1) linear_join<T>(parts, splits, cap, d_n, d_out, end, BiasJob{}, st);
         return;
     }
     DenseArgs g{};
-    g.a = linear_operand<T>(x, d_n, cap, d_in, room, st);
-    g.b = linear_operand<T>(w, nullptr, d_in, d_out, room, st);
+    PackJob jx, jw;
+    g.a = linear_operand<T>(x, d_n, cap, d_in, room, jx);
+    g.b = linear_operand<T>(w, nullptr, d_in, d_out, room, jw);
+    linear_pack<T>(jx, jw, st);
     g.a.extent = cap;
     g.b.extent = (int32_t)wide_of(d_out);
     g.M = cap; g.N = d_out; g.K = d_in;
     g.d_M = d_n;
-    linear_product<T, true, false>(g, end, (float*)room.p, st);
+    linear_product<T, true, false>(g, end, (float*)room.p, BiasJob{}, st);
 }
 
 template <typename T>
@@ -456,25 +462,28 @@ static void linear_bwd(RowsOf x, RowsOf w, int32_t act, RowsOf z, RowsOf grad_y,
         to = room.take(operand_bytes(TypeOf<T>::code, cap, d_out));
         gz = DenseOperand{to, wide_of(d_out) * 2 * planes_of_type(TypeOf<T>::code), 0, (int32_t)wide_of(d_out) * 2, 0};
     }
-    const int64_t blocks = gz_blocks(cap);
+    const int64_t blocks = gz_blocks(cap), lanes = d_out <= 64 ? 8 : 32, wide = ceil_div(d_out, lanes * 8);
     float* sums = (float*)room.take(blocks * d_out * 4);
+    PackJob jw{}, jx{};
+    DenseOperand ow{}, ox{};
+    if (grad_x.p && cap > 0) ow = linear_operand<T>(w, nullptr, d_in, d_out, room, jw);
+    if (grad_w.p) ox = linear_operand<T>(x, d_n, cap, d_in, room, jx);
+    BiasJob bias{sums, (int32_t)blocks, d_out, blocks > 1 ? grad_bias : nullptr};
     if (to || grad_bias) {
         const int32_t per = (int32_t)ceil_div(cap, blocks);
         float* parts = grad_bias ? (blocks == 1 ? grad_bias : sums) : nullptr;
-#define NO_GZ_AS(ACT, LANES) \
-    hipLaunchKernelGGL((linear_gz_kernel<T, ACT, LANES>), dim3((unsigned)ceil_div(d_out, LANES * 8), (unsigned)blocks), dim3(256), 0, st, grad_y, z, d_n, cap, d_out, per, to, gz.pitch, gz.plane, parts)
-#define NO_GZ(ACT) do { if (d_out <= 64) NO_GZ_AS(ACT, 8); else NO_GZ_AS(ACT, 32); } while (0)
+#define NO_GZ_AS(ACT, LANES)                                                                                                                                                           \
+    hipLaunchKernelGGL((linear_gz_kernel<T, ACT, LANES>), dim3((unsigned)(wide * blocks + jw.blocks + jx.blocks)), dim3(256), 0, st, grad_y, z, d_n, cap, d_out, per, (int32_t)wide,   \
+                       (int32_t)(wide * blocks), to, gz.pitch, gz.plane, parts, jw, jx)
+#define NO_GZ(ACT) do { if (lanes == 8) NO_GZ_AS(ACT, 8); else NO_GZ_AS(ACT, 32); } while (0)
         if (act == NO_ACT_RELU) NO_GZ(NO_ACT_RELU);
         else if (act == NO_ACT_GELU) NO_GZ(NO_ACT_GELU);
         else if (act == NO_ACT_SILU) NO_GZ(NO_ACT_SILU);
         else NO_GZ(NO_ACT_NONE);
 #undef NO_GZ
 #undef NO_GZ_AS
-        if (grad_bias && blocks > 1) hipLaunchKernelGGL(linear_bias_kernel, dim3((unsigned)ceil_div(d_out, 16)), dim3(256), 0, st, sums, (int32_t)blocks, d_out, grad_bias);
-    }
-    DenseOperand ow{}, ox{};
-    if (grad_x.p) ow = linear_operand<T>(w, nullptr, d_in, d_out, room, st);
-    if (grad_w.p) ox = linear_operand<T>(x, d_n, cap, d_in, room, st);
+    } else linear_pack<T>(jw, jx, st);
+    auto joined = [&](bool went) { if (went) bias.grad_bias = nullptr; };
     if (grad_x.p && cap > 0) {
         DenseArgs g{};
         g.a = gz; g.b = ow;
@@ -482,7 +491,7 @@ static void linear_bwd(RowsOf x, RowsOf w, int32_t act, RowsOf z, RowsOf grad_y,
         g.b.extent = d_in;
         g.M = cap; g.N = d_in; g.K = d_out;
         g.d_M = d_n;
-        linear_product<T, true, true>(g, LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_x, NO_ACT_NONE}, (float*)room.p, st);
+        joined(linear_product<T, true, true>(g, LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_x, NO_ACT_NONE}, (float*)room.p, bias, st));
     }
     if (grad_w.p) {
         DenseArgs g{};
@@ -491,8 +500,9 @@ static void linear_bwd(RowsOf x, RowsOf w, int32_t act, RowsOf z, RowsOf grad_y,
         g.b.extent = (int32_t)wide_of(d_out);
         g.M = d_in; g.N = d_out; g.K = cap;
         g.d_K = d_n;
-        linear_product<T, false, false>(g, LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_w, NO_ACT_NONE}, (float*)room.p, st);
+        joined(linear_product<T, false, false>(g, LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_w, NO_ACT_NONE}, (float*)room.p, bias, st));
     }
+    if (bias.grad_bias) hipLaunchKernelGGL(linear_bias_kernel, dim3((unsigned)ceil_div(d_out, 16)), dim3(256), 0, st, bias);
 }
 
 static int32_t linear_sizes(const char* who, no_dtype dt, int32_t act, int32_t cap, int32_t d_in, int32_t d_out) {
@@ -516,7 +526,7 @@ extern "C" size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_
     if (px > parts) parts = px;
     if (pw > parts) parts = pw;
     if (n <= LINEAR_FEW) {
-        const size_t few = (size_t)linear_few_splits(d_in, d_out, dt == NO_F32 ? 4 : 2) * n * d_out * 4;
+        const size_t few = (size_t)linear_few_splits(d_in, d_out, n, dt == NO_F32 ? 4 : 2) * n * d_out * 4;
         if (few > parts) parts = few;
     }
     return 256 + operand_bytes(dt, n, d_in) + operand_bytes(dt, d_in, d_out) + operand_bytes(dt, n, d_out) + round_256((size_t)gz_blocks(n) * d_out * 4) + round_256(parts);

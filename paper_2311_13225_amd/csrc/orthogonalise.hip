@@ -169,19 +169,6 @@ __global__ void __launch_bounds__(256) ns_pieces_kernel(NsSource<T> u, int32_t r
 
 // ------------------------------------------------------------------------------------------------------- products
 
-static int ns_tile(int64_t M, int64_t N, int64_t K, int64_t matrices, bool half) {
-    const int64_t steps = ceil_div(K, dense_bk(2));
-    struct { int tile, slots; double step, start; } kinds[3] = {{256, 256, 1.5, 5.0}, {128, 512, 0.95, 4.0}, {64, 1024, 0.65, 4.0}};
-    int best = 64;
-    double least = 1e300;
-    for (auto& k : kinds) {
-        const int64_t a = ceil_div(M, k.tile), b = ceil_div(N, k.tile), tiles = (half ? a * (a + 1) / 2 : a * b) * matrices;
-        const double t = (double)ceil_div(tiles, k.slots) * (steps * k.step + k.start);
-        if (t < least) { least = t; best = k.tile; }
-    }
-    return best;
-}
-
 template <bool AL, bool BL, bool HALF>
 static void ns_product(const NsMatrix& a, int32_t a_extent, const NsMatrix& b, int32_t b_extent, int32_t M, int32_t N, int32_t K, int32_t matrices, const typename NsEnd<HALF>::Args& e,
                        hipStream_t st) {
@@ -189,18 +176,7 @@ static void ns_product(const NsMatrix& a, int32_t a_extent, const NsMatrix& b, i
     g.a = DenseOperand{a.p, a.pitch, a.matrix, a.plane, a_extent};
     g.b = DenseOperand{b.p, b.pitch, b.matrix, b.plane, b_extent};
     g.M = M; g.N = N; g.K = K;
-    g.splits = 1;
-    const int tile = ns_tile(M, N, K, matrices, HALF);
-    g.tiles_m = (int32_t)ceil_div(M, tile);
-    g.tiles_n = (int32_t)ceil_div(N, tile);
-    const dim3 grid(dense_grid(g.tiles_m, g.tiles_n, HALF), 1, (unsigned)matrices);
-#define NO_DENSE(B, STAGES) hipLaunchKernelGGL((dense_kernel<_Float16, 2, AL, BL, B, B, 2, 2, STAGES, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e)
-    const int64_t blocks = (int64_t)grid.x * matrices;
-    if (tile == 256) hipLaunchKernelGGL((dense_large_kernel<_Float16, 2, AL, BL, NsEnd<HALF>>), grid, dim3(256), 0, st, g, e);
-    else if (tile == 128) { if (blocks <= 256) NO_DENSE(128, 4); else NO_DENSE(128, 2); }
-    else if (blocks <= 512) NO_DENSE(64, 4);
-    else NO_DENSE(64, 2);
-#undef NO_DENSE
+    dense_launch<_Float16, 2, AL, BL, NsEnd<HALF>>(g, e, dense_plan(M, N, K, 2, matrices, HALF, 0), matrices, st);
 }
 
 struct NsRoom {
