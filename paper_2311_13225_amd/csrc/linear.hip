@@ -288,8 +288,9 @@ __global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z,
 
 // ------------------------------------------------------------------------------------------------------- few rows
 //
-// Up to LINEAR_FEW rows: the matrix is read once, in its own order, and that bounds it. A thread has 16 bytes of columns and every 64th row of the block's share of the reduction, for all
-// of the rows at once; rows of x stand in LDS as fp32.
+// Up to LINEAR_FEW rows of fp32, or with a bf16 matrix that a product cannot take as it is: the matrix would be copied for a single use, so it is read once, in its own order, and multiplied in
+// fp32. A thread has 16 bytes of columns and every 64th row of the block's share of the reduction, for all of the rows at once; rows of x stand in LDS as fp32. (One row, 2048 x 8192 bf16 11.2 us, one launch of
+// tiles of 32 x 32 8.6, eight rows 24 and 8.6; fp32, one row 13.9, eight of 2048 x 2048 13.2, where copy and tiles of nine rows of 8192 x 2048 take 48.)
 constexpr int LINEAR_FEW = 8, LINEAR_FEW_K = 1024;      // rows; reduction indices in LDS at a time
 
 template <typename T, int MR>
@@ -395,11 +396,17 @@ static inline int64_t gz_blocks(int64_t n) {
 
 struct LinearRoom { char* p; size_t left; char* take(size_t b) { char* r = p; p += round_256(b); return r; } };
 
+// bf16 rows of whole, aligned 16 bytes (and not so far apart that a tile's offsets leave 31 bits).
+template <typename T>
+static bool taken_as_it_is(const RowsOf& x, int32_t dim) {
+    return sizeof(T) == 2 && (uintptr_t)x.p % 16 == 0 && x.stride % 16 == 0 && dim % 8 == 0 && x.stride <= (int64_t)1 << 22;
+}
+
 // The operand that holds `rows` rows of `dim` values: the matrix itself where a product can take it, else a copy (fp32: pieces) that `job` makes.
 template <typename T>
 static DenseOperand linear_operand(RowsOf x, const int32_t* d_n, int64_t rows, int32_t dim, LinearRoom& room, PackJob& job) {
     job = PackJob{x, d_n, (int32_t)rows, dim, nullptr, 0, 0, 0};
-    if (sizeof(T) == 2 && (uintptr_t)x.p % 16 == 0 && x.stride % 16 == 0 && dim % 8 == 0 && x.stride <= (int64_t)1 << 22) return DenseOperand{x.p, x.stride, 0, 0, 0};
+    if (taken_as_it_is<T>(x, dim)) return DenseOperand{x.p, x.stride, 0, 0, 0};
     job.plane = (int32_t)wide_of(dim) * 2;
     job.pitch = (int64_t)job.plane * planes_of_type(TypeOf<T>::code);
     job.out = room.take(operand_bytes(TypeOf<T>::code, rows, dim));
@@ -425,7 +432,7 @@ static bool linear_product(DenseArgs g, const LinearEnd& end, float* parts, cons
 template <typename T>
 static void linear_fwd(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int32_t d_in, int32_t d_out, const LinearEnd& end, char* ws, hipStream_t st) {
     LinearRoom room{ws, 0};
-    if (cap <= LINEAR_FEW) {
+    if (cap <= LINEAR_FEW && !taken_as_it_is<T>(w, d_out)) {
         const int splits = linear_few_splits(d_in, d_out, cap, sizeof(T));
         float* parts = splits > 1 ? (float*)ws : nullptr;
         const dim3 grid((unsigned)ceil_div(d_out, 128 / (int)sizeof(T)), (unsigned)splits);
@@ -455,7 +462,7 @@ static void linear_bwd(RowsOf x, RowsOf w, int32_t act, RowsOf z, RowsOf grad_y,
                        float* grad_bias, char* ws, hipStream_t st) {
     LinearRoom room{ws, 0};
     const bool products = grad_x.p || grad_w.p;
-    const bool as_is = act == NO_ACT_NONE && sizeof(T) == 2 && (uintptr_t)grad_y.p % 16 == 0 && grad_y.stride % 16 == 0 && d_out % 8 == 0 && grad_y.stride <= (int64_t)1 << 22;
+    const bool as_is = act == NO_ACT_NONE && taken_as_it_is<T>(grad_y, d_out);
     DenseOperand gz{grad_y.p, grad_y.stride, 0, 0, 0};
     char* to = nullptr;
     if (products && !as_is) {
