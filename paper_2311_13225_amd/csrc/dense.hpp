@@ -135,54 +135,84 @@ __device__ __forceinline__ bool dense_place(const DenseArgs& g, int band, int& t
 }
 
 // The sums of a block's tile to the epilogue: through LDS, 32 rows of a wavefront at a time, so that eight consecutive columns of a row meet in a lane and the lanes beside it go on along
-// the row: E::put(epilogue's arguments, product's, m, n, columns there, sums).
+// the row. What the epilogue reads of those rows is asked for at once, before the first of them, and waits in LDS for its row (asked for row by row, 16384 x 8192 x 2048 bf16 with a residual lost 35 us of 250 a
+// tile): E::ahead(epilogue's arguments, m, n, columns there), then E::put(arguments, m, n, columns there, sums, what was read, M), which leaves in the sums what it stored; E::MIRROR: that
+// is stored as C[n, m], too.
+template <int BM, int BN, int WM, int WN>
+struct DenseFinish {
+    static constexpr int T = 64 * WM * WN, COLS = BN / WN, PITCH = COLS + 4, LANES = COLS / 8, ROWS = BM / WM < 32 ? BM / WM : 32, PASS = 64 / LANES, TURNS = ROWS / PASS, AHEAD = 32;
+    static constexpr int SUMS = WM * WN * ROWS * PITCH * 4, BYTES = SUMS + (TURNS > 2 ? T * TURNS * AHEAD : 0);
+    static_assert(ROWS % PASS == 0, "whole passes");
+};
 template <int BM, int BN, int WM, int WN, typename E, int I, int J>
 __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename E::Args& e, int tm, int tn, int32_t M, f32x4 (&acc)[I][J], char* lds) {
-    constexpr int T = 64 * WM * WN, COLS = BN / WN, PITCH = COLS + 4, LANES = COLS / 8, RI = I < 2 ? I : 2, ROWS = RI * 16, PASS = 64 / LANES;
-    static_assert(I % RI == 0 && ROWS % PASS == 0, "whole passes");
-    const int wave = (int)threadIdx.x >> 6, wm = wave / WN, wn = wave % WN, l = (int)threadIdx.x & 63;
-    const int32_t m0 = tm * BM, n0 = tn * BN;
+    typedef DenseFinish<BM, BN, WM, WN> F;
+    constexpr int COLS = F::COLS, PITCH = F::PITCH, LANES = F::LANES, ROWS = F::ROWS, RI = ROWS / 16, PASS = F::PASS, TURNS = F::TURNS;
+    constexpr bool HELD = TURNS > 2;
+    typedef typename E::Ahead Ahead;
+    static_assert(I % RI == 0 && sizeof(Ahead) <= F::AHEAD, "whole rounds");
+    const int wave = ((int)threadIdx.x & (F::T - 1)) >> 6, wm = wave / WN, wn = wave % WN, l = (int)threadIdx.x & 63;
+    const int32_t nw = tn * BN + wn * COLS, n = nw + l % LANES * 8, here = min(8, g.N - n);
     float* mine = reinterpret_cast<float*>(lds) + wave * ROWS * PITCH;
+    Ahead* held = reinterpret_cast<Ahead*>(lds + F::SUMS) + (wave * 64 + l);
 #pragma unroll
     for (int i0 = 0; i0 < I; i0 += RI) {
-        Team<64, T>::sync();
+        const int32_t mw = tm * BM + (wm * I + i0) * 16, mine0 = mw + l / LANES;
+        Ahead ahead[TURNS];
+#pragma unroll
+        for (int t = 0; t < TURNS; ++t)
+            if (mine0 + t * PASS < M && here > 0) ahead[t] = E::ahead(e, mine0 + t * PASS, n, here);
+        Team<64, F::T>::sync();
 #pragma unroll
         for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < J; ++j) *reinterpret_cast<f32x4*>(mine + (i * 16 + (l & 15)) * PITCH + j * 16 + (l >> 4) * 4) = acc[i0 + i][j];
-        Team<64, T>::sync();
-        const int32_t mw = m0 + (wm * I + i0) * 16, nw = n0 + wn * COLS;
-#pragma unroll 1
-        for (int r = l / LANES; r < ROWS; r += PASS) {
-            const int32_t m = mw + r, n = nw + l % LANES * 8;
-            if (m >= M || n >= g.N) continue;
+        if constexpr (HELD)
+#pragma unroll
+            for (int t = 0; t < TURNS; ++t) held[t * F::T] = ahead[t];
+        Team<64, F::T>::sync();
+        auto turn = [&](int t, const Ahead& a) {
+            const int32_t m = mine0 + t * PASS;
+            if (m >= M || here <= 0) return;
             float v[8];
+            f32x4* at = reinterpret_cast<f32x4*>(mine + (l / LANES + t * PASS) * PITCH + l % LANES * 8);
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const f32x4 x = *reinterpret_cast<const f32x4*>(mine + r * PITCH + l % LANES * 8 + q * 4);
+                const f32x4 x = at[q];
 #pragma unroll
                 for (int w = 0; w < 4; ++w) v[4 * q + w] = x[w];
             }
-            E::put(e, g, m, n, min(8, g.N - n), v);
+            E::put(e, m, n, here, v, a, g.M);
+            if constexpr (E::MIRROR)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) at[q] = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        };
+        if constexpr (HELD) {
+#pragma unroll 1
+            for (int t = 0; t < TURNS; ++t) turn(t, held[t * F::T]);
+        } else {
+#pragma unroll
+            for (int t = 0; t < TURNS; ++t) turn(t, ahead[t]);
         }
-        if constexpr (E::MIRROR) {          // the same values as C[n, m], eight consecutive m a lane
+        if constexpr (E::MIRROR) {          // eight consecutive m a lane
             if (tm == tn) continue;
+            Team<64, F::T>::sync();
 #pragma unroll 1
             for (int c = l / (ROWS / 8); c < COLS; c += 64 / (ROWS / 8)) {
-                const int32_t n = nw + c, m = mw + l % (ROWS / 8) * 8;
-                if (m >= M || n >= g.N) continue;
+                const int32_t n2 = nw + c, m = mw + l % (ROWS / 8) * 8;
+                if (m >= M || n2 >= g.N) continue;
                 float v[8];
 #pragma unroll
-                for (int w = 0; w < 8; ++w) v[w] = mine[(l % (ROWS / 8) * 8 + w) * PITCH + c];
-                E::mirror(e, g, n, m, min(8, M - m), v);
+                for (int w = 0; w < 8; ++w) v[w] = m + w < M ? mine[(l % (ROWS / 8) * 8 + w) * PITCH + c] : 0.0f;
+                E::mirror(e, n2, m, v);
             }
         }
     }
 }
 
-constexpr int dense_shared(int P, int BM, int BN, int WM, int WN, int STAGES, int GROUPS = 1) {
-    const int tiles = GROUPS * STAGES * (BM + BN) * dense_slabs(P) * 64, rows = WM * WN * (BM / WM < 32 ? BM / WM : 32) * (BN / WN + 4) * 4;
-    return tiles > rows ? tiles : rows;
+constexpr int dense_shared(int P, int BM, int BN, int STAGES, int GROUPS, int finish) {
+    const int tiles = GROUPS * STAGES * (BM + BN) * dense_slabs(P) * 64;
+    return tiles > finish ? tiles : finish;
 }
 
 // Waits for this wavefront's requests but the youngest YOUNG and for its LDS reads, then for the block: what those requests filled stands in LDS for all, and what was read before may be
@@ -222,7 +252,7 @@ __global__ void __launch_bounds__(64 * WM * WN * GROUPS) dense_kernel(const Dens
     typedef DenseTile<P, AL, BM, T> TA;
     typedef DenseTile<P, BL, BN, T> TB;
     constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
-    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, WM, WN, STAGES, GROUPS)];
+    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, STAGES, GROUPS, DenseFinish<BM, BN, WM, WN>::BYTES)];
     int tm, tn;
     if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
     const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * BM, n0 = tn * BN;
@@ -353,7 +383,7 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
     typedef DenseTile<P, AL, BM, T> TA;
     typedef DenseTile<P, BL, BN, T> TB;
     constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
-    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, 2, 2, 2)];
+    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, 2, 1, DenseFinish<BM, BN, 2, 2>::BYTES)];
     int tm, tn;
     if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
     const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * BM, n0 = tn * BN;

@@ -53,8 +53,19 @@ struct LinearEnd {
     int32_t act;
 };
 
-template <typename T, int ACT, int W>
-__device__ __forceinline__ void linear_end(const LinearEnd& e, int64_t m, int32_t n, int32_t here, float (&v)[W]) {
+template <typename T, int W>
+__device__ __forceinline__ Run<T, W> linear_ahead(const LinearEnd& e, int64_t m, int32_t n, int32_t here) {
+    Run<T, W> r;
+    if (e.residual.p) r.load(e.residual.row<T>(m) + n, here, from_f32<T>(0.0f));
+    return r;
+}
+template <int ACT, int W>
+__device__ __forceinline__ void activate(float (&v)[W]) {
+#pragma unroll
+    for (int w = 0; w < W; ++w) v[w] = act_of<ACT>(v[w]);
+}
+template <typename T, int W>
+__device__ __forceinline__ void linear_end(const LinearEnd& e, int64_t m, int32_t n, int32_t here, float (&v)[W], const Run<T, W>& residual) {
     if (e.bias) {
         Run<float, W> b;
         float f[W];
@@ -68,13 +79,12 @@ __device__ __forceinline__ void linear_end(const LinearEnd& e, int64_t m, int32_
         o.set(v);
         o.store(e.z.row<T>(m) + n, here);
     }
-    if (ACT != NO_ACT_NONE)
-#pragma unroll
-        for (int w = 0; w < W; ++w) v[w] = act_of<ACT>(v[w]);
+    if (e.act == NO_ACT_RELU) activate<NO_ACT_RELU>(v);
+    else if (e.act == NO_ACT_GELU) activate<NO_ACT_GELU>(v);
+    else if (e.act == NO_ACT_SILU) activate<NO_ACT_SILU>(v);
     if (e.residual.p) {
         float f[W];
-        o.load(e.residual.row<T>(m) + n, here, from_f32<T>(0.0f));
-        o.get(f);
+        residual.get(f);
 #pragma unroll
         for (int w = 0; w < W; ++w) v[w] += f[w];
     }
@@ -82,26 +92,18 @@ __device__ __forceinline__ void linear_end(const LinearEnd& e, int64_t m, int32_
     o.store(e.y.row<T>(m) + n, here);
 }
 
-template <typename T, int W>
-__device__ __forceinline__ void linear_end_of(const LinearEnd& e, int64_t m, int32_t n, int32_t here, float (&v)[W]) {
-    switch (e.act) {
-        case NO_ACT_RELU: return linear_end<T, NO_ACT_RELU, W>(e, m, n, here, v);
-        case NO_ACT_GELU: return linear_end<T, NO_ACT_GELU, W>(e, m, n, here, v);
-        case NO_ACT_SILU: return linear_end<T, NO_ACT_SILU, W>(e, m, n, here, v);
-        default: return linear_end<T, NO_ACT_NONE, W>(e, m, n, here, v);
-    }
-}
-
 template <typename T>
 struct LinearOut {
-    struct Args { LinearEnd end; float* parts; };      // parts: sums of a split reduction [split][M][N] instead
+    struct Args { LinearEnd end; float* parts; int32_t N; };      // parts: sums of a split reduction [split][M][N] instead
     static constexpr bool MIRROR = false;
-    __device__ static __forceinline__ void put(const Args& e, const DenseArgs& g, int32_t m, int32_t n, int32_t here, float (&v)[8]) {
+    typedef Run<T, 8> Ahead;
+    __device__ static __forceinline__ Ahead ahead(const Args& e, int32_t m, int32_t n, int32_t here) { return linear_ahead<T, 8>(e.end, m, n, here); }
+    __device__ static __forceinline__ void put(const Args& e, int32_t m, int32_t n, int32_t here, float (&v)[8], const Ahead& residual, int32_t M) {
         if (e.parts) {
             Run<float, 8> o;
             o.set(v);
-            o.store(e.parts + ((int64_t)blockIdx.y * g.M + m) * g.N + n, here);
-        } else linear_end_of<T, 8>(e.end, m, n, here, v);
+            o.store(e.parts + ((int64_t)blockIdx.y * M + m) * e.N + n, here);
+        } else linear_end<T, 8>(e.end, m, n, here, v, residual);
     }
 };
 
@@ -163,7 +165,7 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* __restric
 #pragma unroll
             for (int w = 0; w < 4; ++w) v[w] += share[k][place][w];
     }
-    if (there) linear_end_of<T, 4>(e, m, n, here, v);
+    if (there) linear_end<T, 4>(e, m, n, here, v, linear_ahead<T, 4>(e, m, n, here));
 }
 template <typename T>
 static void linear_join(const float* parts, int32_t splits, int32_t M, const int32_t* d_M, int32_t N, const LinearEnd& end, const BiasJob& bias, hipStream_t st) {
@@ -361,7 +363,7 @@ __global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, con
         Run<float, 4> o;
         o.set(v);
         o.store(parts + ((int64_t)blockIdx.y * cap + r) * N + col, here);
-    } else linear_end_of<T, 4>(e, r, col, here, v);
+    } else linear_end<T, 4>(e, r, col, here, v, linear_ahead<T, 4>(e, r, col, here));
 }
 
 // ------------------------------------------------------------------------------------------------------- plans
@@ -423,7 +425,7 @@ template <typename T, bool AL, bool BL>
 static bool linear_product(DenseArgs g, const LinearEnd& end, float* parts, const BiasJob& bias, hipStream_t st) {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;
     const LinearPlan p = linear_plan(g.M, g.N, g.K, P);
-    const typename LinearOut<T>::Args e{end, p.splits > 1 ? parts : nullptr};
+    const typename LinearOut<T>::Args e{p.splits > 1 ? LinearEnd{} : end, p.splits > 1 ? parts : nullptr, g.N};
     dense_launch<__bf16, P, AL, BL, LinearOut<T>>(g, e, DensePlan{p.kind, p.splits}, 1, st);
     if (p.splits > 1) linear_join<T>(parts, p.splits, g.M, g.d_M, g.N, end, bias, st);
     return p.splits > 1;        // (the column sums went along)

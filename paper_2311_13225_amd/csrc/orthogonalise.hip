@@ -12,7 +12,7 @@ namespace no {
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float NS_HELD = 0x1p14f, NS_VALUE = 0x1p-14f;
 
-// Eight values of one row in pieces, and back.
+// Eight values of one row in pieces.
 __device__ __forceinline__ void ns_store(const float (&f)[8], char* to, int32_t plane) {
     f16x8 h, l;
 #pragma unroll
@@ -22,11 +22,6 @@ __device__ __forceinline__ void ns_store(const float (&f)[8], char* to, int32_t 
     }
     *reinterpret_cast<f16x8*>(to) = h;
     *reinterpret_cast<f16x8*>(to + plane) = l;
-}
-__device__ __forceinline__ void ns_load(const char* from, int32_t plane, float (&f)[8]) {
-    const f16x8 h = *reinterpret_cast<const f16x8*>(from), l = *reinterpret_cast<const f16x8*>(from + plane);
-#pragma unroll
-    for (int w = 0; w < 8; ++w) f[w] = (float)h[w] + (float)l[w];
 }
 
 // A matrix in pieces: rows of a multiple of 8 values, zeros past the columns, the second pieces of a row behind the first.
@@ -53,40 +48,48 @@ struct NsEnd {
         float keep, step;
     };
     static constexpr bool MIRROR = SYMMETRIC;
-    __device__ static __forceinline__ void put(const Args& e, const DenseArgs& g, int32_t m, int32_t n, int32_t here, float (&v)[8]) {
-        const int64_t z = blockIdx.z;
-        float f[8];
-        if (e.from.p) ns_load(e.from.p + z * e.from.matrix + m * e.from.pitch + n * 2, e.from.plane, f);
+    struct Ahead { f16x8 h, l; };
+    __device__ static __forceinline__ Ahead ahead(const Args& e, int32_t m, int32_t n, int32_t) {
+        Ahead a;
+        if (e.from.p) {
+            const char* from = e.from.p + (int64_t)blockIdx.z * e.from.matrix + m * e.from.pitch + n * 2;
+            a.h = *reinterpret_cast<const f16x8*>(from);
+            a.l = *reinterpret_cast<const f16x8*>(from + e.from.plane);
+        }
+        return a;
+    }
+    __device__ static __forceinline__ void pieces(const Args& e, int32_t m, int32_t n, const float (&v)[8]) {
+        ns_store(v, e.to.p + (int64_t)blockIdx.z * e.to.matrix + m * e.to.pitch + n * 2, e.to.plane);
+    }
+    __device__ static __forceinline__ void put(const Args& e, int32_t m, int32_t n, int32_t here, float (&v)[8], const Ahead& a, int32_t) {
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
             v[w] *= e.by;
-            if (e.from.p) v[w] += e.own * f[w];
+            if (e.from.p) v[w] += e.own * ((float)a.h[w] + (float)a.l[w]);
             if (w >= here) v[w] = 0.0f;
         }
-        if (SYMMETRIC || e.kind == NS_PIECES) {
-            ns_store(v, e.to.p + z * e.to.matrix + m * e.to.pitch + n * 2, e.to.plane);
-            return;
-        }
+        if (SYMMETRIC || e.kind == NS_PIECES) return pieces(e, m, n, v);
 #pragma unroll
         for (int w = 0; w < 8; ++w) v[w] *= NS_VALUE;
+        const RowsOf out = e.out.of(blockIdx.z);
         if (e.kind == NS_OUT_BF16) {
             Run<bf16_t, 8> o;
             o.set(v);
-            o.store(e.out.of(z).template row<bf16_t>(m) + n, here);
+            o.store(out.row<bf16_t>(m) + n, here);
             return;
         }
-        float* to = e.out.of(z).template row<float>(m) + n;
         Run<float, 8> o;
         if (e.kind == NS_WEIGHTS) {
-            o.load(to, here, 0.0f);
+            float f[8];
+            o.load(out.row<float>(m) + n, here, 0.0f);
             o.get(f);
 #pragma unroll
             for (int w = 0; w < 8; ++w) v[w] = f[w] * e.keep - v[w] * e.step;
         }
         o.set(v);
-        o.store(to, here);
+        o.store(out.row<float>(m) + n, here);
     }
-    __device__ static __forceinline__ void mirror(const Args& e, const DenseArgs& g, int32_t m, int32_t n, int32_t here, float (&v)[8]) { put(e, g, m, n, here, v); }
+    __device__ static __forceinline__ void mirror(const Args& e, int32_t m, int32_t n, const float (&v)[8]) { pieces(e, m, n, v); }
 };
 
 // ------------------------------------------------------------------------------------------------------- before the products
