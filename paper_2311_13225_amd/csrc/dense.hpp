@@ -37,16 +37,16 @@ constexpr uint32_t DENSE_NOWHERE = 0x80000000u;      // past every buffer's rang
 
 // One operand's tile of R rows (or columns) and a step's slabs in LDS, loaded by T threads in requests of 16 bytes that go straight to LDS. A request's 64 lanes fill 1 KB in lane
 // order, so the order of the units in LDS is made by which unit a lane asks for: ALONG, unit u of row r stands at place u ^ (r & 7) of its 128 bytes (three pieces: at
-// u ^ (r >> 2 & 3) of its 192); across, the 32 bytes of 16 columns of line k stand at place c ^ f(k), f(k) = (k & 3) | (k >> 3 & 1) << 2. Then the 64 lanes of a fragment's read meet every
-// bank equally often.
+// u ^ (r >> 2 & 3) of its 192); across, the 32 bytes of 16 columns of line k stand at place c ^ f(k), f(k) = (k & 3) | (k >> 3 & 1) << 2 (192 columns, whose lines begin half of the banks apart: (k >> 1 & 1) |
+// (k >> 3 & 1) << 1). Then the 64 lanes of a fragment's read meet every bank equally often (SQ_LDS_BANK_CONFLICT 0).
 template <int P, bool ALONG, int R, int T>
 struct DenseTile {
     static constexpr int SLABS = dense_slabs(P), BK = dense_bk(P), PER_ROW = ALONG ? SLABS * 4 : R / 8, BYTES = R * SLABS * 64, REQ = BYTES / (16 * T);
-    static_assert(BYTES % (16 * T) == 0 && (ALONG || (R >= 32 && T % PER_ROW == 0)), "whole requests");
+    static_assert(BYTES % (16 * T) == 0 && R >= 32, "whole requests");
     uint32_t off[REQ];
     const char* base;                   // the tile's origin in the matrix
     int64_t step;                       // bytes from one step to the next
-    __device__ __forceinline__ static int mix(int k) { return ((k & 3) | (k >> 3 & 1) << 2) & (R / 16 - 1); }
+    __device__ __forceinline__ static int mix(int k) { return R == 192 ? (k >> 1 & 1) | (k >> 3 & 1) << 1 : ((k & 3) | (k >> 3 & 1) << 2) & (R / 16 - 1); }
     // what request i of this thread asks for: line of the tile, unit of the line
     __device__ __forceinline__ static void which(int i, int& line, int& unit) {
         const int c = i * T + ((int)threadIdx.x & (T - 1)), place = c % PER_ROW;
@@ -140,7 +140,7 @@ __device__ __forceinline__ bool dense_place(const DenseArgs& g, int band, int& t
 // is stored as C[n, m], too.
 template <int BM, int BN, int WM, int WN>
 struct DenseFinish {
-    static constexpr int T = 64 * WM * WN, COLS = BN / WN, PITCH = COLS + 4, LANES = COLS / 8, ROWS = BM / WM < 32 ? BM / WM : 32, PASS = 64 / LANES, TURNS = ROWS / PASS, AHEAD = 32;
+    static constexpr int T = 64 * WM * WN, COLS = BN / WN, PITCH = COLS + 4, LANES = COLS == 96 ? 16 : COLS / 8, ROWS = BM / WM < 32 ? BM / WM : 32, PASS = 64 / LANES, TURNS = ROWS / PASS, AHEAD = 32;
     static constexpr int SUMS = WM * WN * ROWS * PITCH * 4, BYTES = SUMS + (TURNS > 2 ? T * TURNS * AHEAD : 0);
     static_assert(ROWS % PASS == 0, "whole passes");
 };
@@ -152,7 +152,7 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
     typedef typename E::Ahead Ahead;
     static_assert(I % RI == 0 && sizeof(Ahead) <= F::AHEAD, "whole rounds");
     const int wave = ((int)threadIdx.x & (F::T - 1)) >> 6, wm = wave / WN, wn = wave % WN, l = (int)threadIdx.x & 63;
-    const int32_t nw = tn * BN + wn * COLS, n = nw + l % LANES * 8, here = min(8, g.N - n);
+    const int32_t nw = tn * BN + wn * COLS, n = nw + l % LANES * 8, here = l % LANES * 8 < COLS ? min(8, g.N - n) : 0;      // (of 16 lanes to 96 columns four have none)
     float* mine = reinterpret_cast<float*>(lds) + wave * ROWS * PITCH;
     Ahead* held = reinterpret_cast<Ahead*>(lds + F::SUMS) + (wave * 64 + l);
 #pragma unroll
@@ -374,12 +374,12 @@ __global__ void __launch_bounds__(64 * WM * WN * GROUPS) dense_kernel(const Dens
     dense_finish<BM, BN, WM, WN, E>(g, e, tm, tn, M, acc, lds);
 }
 
-// The same for large products: a tile of 256 x 256 (three pieces: 256 x 128) by four wavefronts of a quarter each, one a SIMD, whose sums fill the accumulation registers; the others hold one set of
+// The same for large products: a tile of 256 x 256 (192 x 192 where that fills the chip better; three pieces: 256 x 128) by four wavefronts of a quarter each, one a SIMD, whose sums fill the accumulation registers; the others hold one set of
 // fragments a slab, and a set is read again when the products that want it are done. A copy of LDS is free when its last fragments are in registers: the step after next is requested right then, and
 // has a whole step's time to arrive. LDS is read 16 bytes for 8192 multiplications (by eight wavefronts of 128 x 64: 24 bytes, which takes LDS as long as the products).
-template <typename H, int P, bool AL, bool BL, typename E>
+template <typename H, int P, bool AL, bool BL, int BM, int BN, typename E>
 __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, const typename E::Args e) {
-    constexpr int BM = 256, BN = P < 3 ? 256 : 128, T = 256, I = 8, J = BN / 32, S = dense_slabs(P), N = I * J;
+    constexpr int T = 256, I = BM / 32, J = BN / 32, S = dense_slabs(P), N = I * J, EACH = N / (I + J);      // (a read for EACH products)
     typedef DenseTile<P, AL, BM, T> TA;
     typedef DenseTile<P, BL, BN, T> TB;
     constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
@@ -460,14 +460,14 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
             dense_meet<0>();
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                if (n % 4 == 0) { if (n / 4 < J) take_b(0, n / 4, now ^ 1); else take_a(0, n / 4 - J, now ^ 1); }
-                if (n % 4 == 2) request(n / 4, now);
+                if (n % EACH == 0) { if (n / EACH < J) take_b(0, n / EACH, now ^ 1); else take_a(0, n / EACH - J, now ^ 1); }
+                if (n % EACH == EACH / 2) request(n / EACH, now);
                 one(n, 1, 1, acc);
             }
         } else if constexpr (P == 2) {
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                if (n % 4 == 0) { if (n / 4 < I) take_a(0, n / 4, now); else take_b(1, n / 4 - I, now); }
+                if (n % EACH == 0) { if (n / EACH < I) take_a(0, n / EACH, now); else take_b(1, n / EACH - I, now); }
                 one(n, 1, 0, acc);
             }
 #pragma unroll
@@ -476,8 +476,8 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
             dense_meet<0>();
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                if (n % 4 == 0) { if (n / 4 < J) take_b(0, n / 4, now ^ 1); else take_a(1, n / 4 - J, now ^ 1); }
-                if (n % 4 == 2) request(n / 4, now);
+                if (n % EACH == 0) { if (n / EACH < J) take_b(0, n / EACH, now ^ 1); else take_a(1, n / EACH - J, now ^ 1); }
+                if (n % EACH == EACH / 2) request(n / EACH, now);
                 one(n, 0, 1, acc);
             }
         } else {
@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
             }
         }
     };
-    static_assert(P == 3 ? REQ / 2 <= N / 3 && REQ - REQ / 2 <= N / 3 : REQ == N / 4, "a place for every request");
+    static_assert(P == 3 ? REQ / 2 <= N / 3 && REQ - REQ / 2 <= N / 3 : REQ == I + J && N % (I + J) == 0, "a place for every request");
 #pragma unroll
     for (int j = 0; j < J; ++j) take_b(0, j, 0);
 #pragma unroll
@@ -548,12 +548,12 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
 // 51 / 36 / 46 / 52 / 58 / 75 / 211; 1024 x 1024 x 4096 78 / 54 / 33 / 37 / 18 / 19 / 41; 256 x 256 x 4096 77 / 38 / 32 / 24 / 17 / 15 / 10.
 struct DenseKind { int bm, bn, per_unit; double one, more, start; };
 struct DensePlan { int kind, splits; };
-enum { DENSE_LARGE, DENSE_128, DENSE_128_DEEP, DENSE_64, DENSE_64_DEEP, DENSE_64_GROUPS, DENSE_32, DENSE_KINDS };
+enum { DENSE_LARGE, DENSE_192, DENSE_128, DENSE_128_DEEP, DENSE_64, DENSE_64_DEEP, DENSE_64_GROUPS, DENSE_32, DENSE_KINDS };
 
 static const DenseKind DENSE_KIND[3][DENSE_KINDS] = {      // of one, two and three pieces
-    {{256, 256, 1, 1.35, 0, 8}, {128, 128, 2, 0.6, 0.35, 5}, {128, 128, 1, 0.5, 0, 5.5}, {64, 64, 5, 0.3, 0.12, 4}, {64, 64, 2, 0.21, 0.13, 3.7}, {64, 64, 1, 0.17, 0, 4.8}, {32, 32, 1, 0.08, 0, 4.8}},
-    {{256, 256, 1, 2.1, 0, 8}, {128, 128, 2, 0.95, 0.7, 5}, {128, 128, 1, 0.75, 0, 5}, {64, 64, 5, 0.42, 0.24, 4.5}, {64, 64, 2, 0.27, 0.17, 4}, {64, 64, 1, 0.24, 0, 5}, {32, 32, 1, 0.09, 0, 5.2}},
-    {{256, 128, 1, 1.9, 0, 8}, {128, 128, 1, 1.3, 0, 5}, {128, 128, 0, 0, 0, 0}, {64, 64, 3, 0.75, 0.25, 3}, {64, 64, 1, 0.42, 0, 3}, {64, 64, 0, 0, 0, 0}, {32, 32, 1, 0.25, 0, 3}}};
+    {{256, 256, 1, 1.35, 0, 8}, {192, 192, 1, 0.85, 0, 7}, {128, 128, 2, 0.6, 0.35, 5}, {128, 128, 1, 0.5, 0, 5.5}, {64, 64, 5, 0.3, 0.12, 4}, {64, 64, 2, 0.21, 0.13, 3.7}, {64, 64, 1, 0.17, 0, 4.8}, {32, 32, 1, 0.08, 0, 4.8}},
+    {{256, 256, 1, 2.1, 0, 8}, {192, 192, 1, 1.3, 0, 7}, {128, 128, 2, 0.95, 0.7, 5}, {128, 128, 1, 0.75, 0, 5}, {64, 64, 5, 0.42, 0.24, 4.5}, {64, 64, 2, 0.27, 0.17, 4}, {64, 64, 1, 0.24, 0, 5}, {32, 32, 1, 0.09, 0, 5.2}},
+    {{256, 128, 1, 1.9, 0, 8}, {192, 192, 0, 0, 0, 0}, {128, 128, 1, 1.3, 0, 5}, {128, 128, 0, 0, 0, 0}, {64, 64, 3, 0.75, 0.25, 3}, {64, 64, 1, 0.42, 0, 3}, {64, 64, 0, 0, 0, 0}, {32, 32, 1, 0.25, 0, 3}}};
 
 // The kind of tile and the number of parts of the reduction that promise the shortest time; the parts' sums take at most `parts_most` bytes and a launch that joins them.
 static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matrices, bool half, size_t parts_most) {
@@ -585,7 +585,10 @@ static void dense_launch(DenseArgs g, const typename E::Args& e, const DensePlan
 #define NO_DENSE(BM, BN, WM, WN, STAGES, GROUPS) hipLaunchKernelGGL((dense_kernel<H, P, AL, BL, BM, BN, WM, WN, STAGES, GROUPS, E>), grid, dim3(64 * WM * WN * GROUPS), 0, st, g, e)
     switch (p.kind) {
         case DENSE_LARGE:
-            hipLaunchKernelGGL((dense_large_kernel<H, P, AL, BL, E>), grid, dim3(256), 0, st, g, e);
+            hipLaunchKernelGGL((dense_large_kernel<H, P, AL, BL, 256, (P < 3 ? 256 : 128), E>), grid, dim3(256), 0, st, g, e);
+            break;
+        case DENSE_192:
+            if constexpr (P < 3) hipLaunchKernelGGL((dense_large_kernel<H, P, AL, BL, 192, 192, E>), grid, dim3(256), 0, st, g, e);
             break;
         case DENSE_128: NO_DENSE(128, 128, 2, 2, P < 3 ? 2 : 3, 1); break;
         case DENSE_128_DEEP:

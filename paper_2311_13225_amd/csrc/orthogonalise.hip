@@ -94,7 +94,7 @@ struct NsEnd {
 
 // ------------------------------------------------------------------------------------------------------- before the products
 
-constexpr int NS_SUMS = 256;        // blocks a matrix, at most, whose sums of squares make its norm
+constexpr int NS_SUMS = 1024;       // blocks a matrix, at most, whose sums of squares make its norm
 
 // U: the matrix itself, or the momentum after this step, m <- beta m + g, and U = g + beta m (nesterov) or m. First pass: the sums of squares in 64 bits (and the momentum stored);
 // second: 2^14 U / |U| in pieces. A matrix of zeros stays one.
@@ -151,7 +151,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) ns_pieces_kernel(NsSource<T> u, int32_t rows, int32_t cols, const double* __restrict__ sums, int32_t n_sums, NsMatrix to) {
     __shared__ double share[4];
     const int64_t z = blockIdx.y;
-    double sum = (int32_t)threadIdx.x < n_sums ? sums[z * NS_SUMS + threadIdx.x] : 0.0;
+    double sum = 0.0;
+    for (int32_t i = threadIdx.x; i < n_sums; i += 256) sum += sums[z * NS_SUMS + i];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
     if (lane_id() == 0) share[threadIdx.x >> 6] = sum;
