@@ -24,7 +24,7 @@ struct DenseArgs {
     DenseOperand a, b;
     int32_t M, N, K;
     const int32_t *d_M, *d_K;           // device scalars that limit M or K (NULL: none)
-    int32_t splits, tiles_m, tiles_n;
+    int32_t splits, tiles_m, tiles_n, matrices;
 };
 
 static inline size_t round_256(size_t b) { return (b + 255) / 256 * 256; }
@@ -112,31 +112,48 @@ __device__ __forceinline__ void dense_multiply(f32x4 (&acc)[I][J], const s16x8 (
         for (int j = 0; j < J; ++j) acc[i][j] = dense_mfma<H>(b[j], a[i], acc[i][j]);
 }
 
-// A block's place: tiles are dealt to the dies in runs, and walked in bands of `band` tile rows, so that a die's blocks share rows and columns in its L2.
+// A block's place: the tiles of all matrices are dealt to the dies in runs, and walked in bands of eight tile rows, so that a die's blocks share rows and columns in its L2 (four Gram matrices of 512 x 2048, each
+// matrix dealt to all dies: 22 us, to two of them 16).
 // HALF: the tiles on and above the diagonal of a square alone.
-static inline unsigned dense_grid(int64_t tiles_m, int64_t tiles_n, bool half) { return (unsigned)(ceil_div(half ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n, 8) * 8); }
+constexpr int DENSE_BAND = 8;
+static inline int64_t dense_tiles(int64_t tiles_m, int64_t tiles_n, bool half) { return half ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n; }
 template <bool HALF>
-__device__ __forceinline__ bool dense_place(const DenseArgs& g, int band, int& tm, int& tn) {
-    const int total = HALF ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n, padded = (int)gridDim.x;
-    const int id = ((int)blockIdx.x % 8) * (padded / 8) + (int)blockIdx.x / 8;
-    if (id >= total) return false;
-    if (HALF) {         // column tn begins behind tn (tn + 1) / 2 tiles (fewer than 2^24 of them, so the root is off by one at most)
-        tn = (int)((sqrtf(8.0f * (float)id + 1.0f) - 1.0f) * 0.5f);
-        tn += (tn + 1) * (tn + 2) / 2 <= id ? 1 : 0;
-        tn -= tn * (tn + 1) / 2 > id ? 1 : 0;
-        tn = __builtin_amdgcn_readfirstlane(tn);
-        tm = id - tn * (tn + 1) / 2;
+__device__ __forceinline__ bool dense_place(const DenseArgs& g, int& matrix, int& tm, int& tn) {
+    const int padded = (int)gridDim.x, tiles = HALF ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n;
+    int id = ((int)blockIdx.x % 8) * (padded / 8) + (int)blockIdx.x / 8;
+    if (id >= tiles * g.matrices) return false;
+    matrix = id / tiles;
+    id -= matrix * tiles;
+    if (HALF) {         // a band's corner on the diagonal, then its whole columns
+        int row = 0, rows, corner;
+        for (;; row += DENSE_BAND) {
+            rows = min(DENSE_BAND, g.tiles_m - row);
+            corner = rows * (rows + 1) / 2;
+            const int all = corner + (g.tiles_m - row - rows) * rows;
+            if (id < all) break;
+            id -= all;
+        }
+        if (id < corner) {
+            int j = 0;
+            while ((j + 1) * (j + 2) / 2 <= id) ++j;
+            tn = row + j;
+            tm = row + id - j * (j + 1) / 2;
+        } else {
+            id -= corner;
+            tn = row + rows + id / rows;
+            tm = row + id % rows;
+        }
         return true;
     }
-    const int per = band * g.tiles_n, b = id / per, rest = id - b * per, rows = min(band, g.tiles_m - b * band);
-    tm = b * band + rest % rows;
+    const int per = DENSE_BAND * g.tiles_n, b = id / per, rest = id - b * per, rows = min(DENSE_BAND, g.tiles_m - b * DENSE_BAND);
+    tm = b * DENSE_BAND + rest % rows;
     tn = rest / rows;
     return true;
 }
 
 // The sums of a block's tile to the epilogue: through LDS, 32 rows of a wavefront at a time, so that eight consecutive columns of a row meet in a lane and the lanes beside it go on along
 // the row. What the epilogue reads of those rows is asked for at once, before the first of them, and waits in LDS for its row (asked for row by row, 16384 x 8192 x 2048 bf16 with a residual lost 35 us of 250 a
-// tile): E::ahead(epilogue's arguments, m, n, columns there), then E::put(arguments, m, n, columns there, sums, what was read, M), which leaves in the sums what it stored; E::MIRROR: that
+// tile): E::ahead(epilogue's arguments, matrix, m, n, columns there), then E::put(arguments, matrix, m, n, columns there, sums, what was read, M), which leaves in the sums what it stored; E::MIRROR: that
 // is stored as C[n, m], too.
 template <int BM, int BN, int WM, int WN>
 struct DenseFinish {
@@ -145,7 +162,7 @@ struct DenseFinish {
     static_assert(ROWS % PASS == 0, "whole passes");
 };
 template <int BM, int BN, int WM, int WN, typename E, int I, int J>
-__device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename E::Args& e, int tm, int tn, int32_t M, f32x4 (&acc)[I][J], char* lds) {
+__device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename E::Args& e, int matrix, int tm, int tn, int32_t M, f32x4 (&acc)[I][J], char* lds) {
     typedef DenseFinish<BM, BN, WM, WN> F;
     constexpr int COLS = F::COLS, PITCH = F::PITCH, LANES = F::LANES, ROWS = F::ROWS, RI = ROWS / 16, PASS = F::PASS, TURNS = F::TURNS;
     constexpr bool HELD = TURNS > 2;
@@ -161,7 +178,7 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
         Ahead ahead[TURNS];
 #pragma unroll
         for (int t = 0; t < TURNS; ++t)
-            if (mine0 + t * PASS < M && here > 0) ahead[t] = E::ahead(e, mine0 + t * PASS, n, here);
+            if (mine0 + t * PASS < M && here > 0) ahead[t] = E::ahead(e, matrix, mine0 + t * PASS, n, here);
         Team<64, F::T>::sync();
 #pragma unroll
         for (int i = 0; i < RI; ++i)
@@ -182,7 +199,7 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
 #pragma unroll
                 for (int w = 0; w < 4; ++w) v[4 * q + w] = x[w];
             }
-            E::put(e, m, n, here, v, a, g.M);
+            E::put(e, matrix, m, n, here, v, a, g.M);
             if constexpr (E::MIRROR)
 #pragma unroll
                 for (int q = 0; q < 2; ++q) at[q] = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
@@ -204,7 +221,7 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
                 float v[8];
 #pragma unroll
                 for (int w = 0; w < 8; ++w) v[w] = m + w < M ? mine[(l % (ROWS / 8) * 8 + w) * PITCH + c] : 0.0f;
-                E::mirror(e, n2, m, v);
+                E::mirror(e, matrix, n2, m, v);
             }
         }
     }
@@ -253,8 +270,8 @@ __global__ void __launch_bounds__(64 * WM * WN * GROUPS) dense_kernel(const Dens
     typedef DenseTile<P, BL, BN, T> TB;
     constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
     __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, STAGES, GROUPS, DenseFinish<BM, BN, WM, WN>::BYTES)];
-    int tm, tn;
-    if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
+    int matrix, tm, tn;
+    if (!dense_place<E::MIRROR>(g, matrix, tm, tn)) return;
     const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * BM, n0 = tn * BN;
     if (m0 >= M) return;
     const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / T), wave = ((int)threadIdx.x & (T - 1)) >> 6, wm = wave / WN, wn = wave % WN;
@@ -263,8 +280,8 @@ __global__ void __launch_bounds__(64 * WM * WN * GROUPS) dense_kernel(const Dens
     TB tb;
     DenseOperand oa = g.a;
     if (AL) oa.extent = min(oa.extent, M);
-    ta.open(oa, blockIdx.z, m0);
-    tb.open(g.b, blockIdx.z, n0);
+    ta.open(oa, matrix, m0);
+    tb.open(g.b, matrix, n0);
     const int32_t steps = (K + TA::BK - 1) / TA::BK, first = (int32_t)((int64_t)steps * blockIdx.y / g.splits), last = (int32_t)((int64_t)steps * (blockIdx.y + 1) / g.splits);
     const int32_t end = min(K, last * TA::BK), whole = end / TA::BK;
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine + (uint32_t)wave * 1024u);
@@ -371,7 +388,7 @@ __global__ void __launch_bounds__(64 * WM * WN * GROUPS) dense_kernel(const Dens
         __syncthreads();
         if (group > 0) return;
     }
-    dense_finish<BM, BN, WM, WN, E>(g, e, tm, tn, M, acc, lds);
+    dense_finish<BM, BN, WM, WN, E>(g, e, matrix, tm, tn, M, acc, lds);
 }
 
 // The same for large products: a tile of 256 x 256 (192 x 192 where that fills the chip better; three pieces: 256 x 128) by four wavefronts of a quarter each, one a SIMD, whose sums fill the accumulation registers; the others hold one set of
@@ -384,8 +401,8 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
     typedef DenseTile<P, BL, BN, T> TB;
     constexpr int COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
     __shared__ __attribute__((aligned(1024))) char lds[dense_shared(P, BM, BN, 2, 1, DenseFinish<BM, BN, 2, 2>::BYTES)];
-    int tm, tn;
-    if (!dense_place<E::MIRROR>(g, 8, tm, tn)) return;
+    int matrix, tm, tn;
+    if (!dense_place<E::MIRROR>(g, matrix, tm, tn)) return;
     const int32_t M = rows_here(g.d_M, g.M), K = rows_here(g.d_K, g.K), m0 = tm * BM, n0 = tn * BN;
     if (m0 >= M) return;
     const int wave = (int)threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
@@ -393,8 +410,8 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
     TB tb;
     DenseOperand oa = g.a;
     if (AL) oa.extent = min(oa.extent, M);
-    ta.open(oa, blockIdx.z, m0);
-    tb.open(g.b, blockIdx.z, n0);
+    ta.open(oa, matrix, m0);
+    tb.open(g.b, matrix, n0);
     const int32_t steps = (K + TA::BK - 1) / TA::BK, first = (int32_t)((int64_t)steps * blockIdx.y / g.splits), last = (int32_t)((int64_t)steps * (blockIdx.y + 1) / g.splits);
     f32x4 acc[I][J];
     f32x4 big[P == 3 ? I : 1][P == 3 ? J : 1];
@@ -537,7 +554,7 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
             for (int j = 0; j < J; ++j) acc[i][j] += big[i][j];
     }
     dense_meet<0>();
-    dense_finish<BM, BN, 2, 2, E>(g, e, tm, tn, M, acc, lds);
+    dense_finish<BM, BN, 2, 2, E>(g, e, matrix, tm, tn, M, acc, lds);
 }
 
 // ------------------------------------------------------------------------------------------------------- plans
@@ -581,7 +598,8 @@ static void dense_launch(DenseArgs g, const typename E::Args& e, const DensePlan
     g.splits = p.splits;
     g.tiles_m = (int32_t)ceil_div(g.M, k.bm);
     g.tiles_n = (int32_t)ceil_div(g.N, k.bn);
-    const dim3 grid(dense_grid(g.tiles_m, g.tiles_n, E::MIRROR), (unsigned)p.splits, (unsigned)matrices);
+    g.matrices = (int32_t)matrices;
+    const dim3 grid((unsigned)(ceil_div(dense_tiles(g.tiles_m, g.tiles_n, E::MIRROR) * matrices, 8) * 8), (unsigned)p.splits);
 #define NO_DENSE(BM, BN, WM, WN, STAGES, GROUPS) hipLaunchKernelGGL((dense_kernel<H, P, AL, BL, BM, BN, WM, WN, STAGES, GROUPS, E>), grid, dim3(64 * WM * WN * GROUPS), 0, st, g, e)
     switch (p.kind) {
         case DENSE_LARGE:

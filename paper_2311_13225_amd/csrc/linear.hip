@@ -94,15 +94,15 @@ __device__ __forceinline__ void linear_end(const LinearEnd& e, int64_t m, int32_
 
 template <typename T>
 struct LinearOut {
-    struct Args { LinearEnd end; float* parts; int32_t N; };      // parts: sums of a split reduction [split][M][N] instead
+    struct Args { LinearEnd end; float* parts; int32_t pitch; };      // parts: sums of a split reduction instead, [split][M][pitch], pitch a multiple of 8: every run is whole
     static constexpr bool MIRROR = false;
     typedef Run<T, 8> Ahead;
-    __device__ static __forceinline__ Ahead ahead(const Args& e, int32_t m, int32_t n, int32_t here) { return linear_ahead<T, 8>(e.end, m, n, here); }
-    __device__ static __forceinline__ void put(const Args& e, int32_t m, int32_t n, int32_t here, float (&v)[8], const Ahead& residual, int32_t M) {
+    __device__ static __forceinline__ Ahead ahead(const Args& e, int32_t, int32_t m, int32_t n, int32_t here) { return linear_ahead<T, 8>(e.end, m, n, here); }
+    __device__ static __forceinline__ void put(const Args& e, int32_t, int32_t m, int32_t n, int32_t here, float (&v)[8], const Ahead& residual, int32_t M) {
         if (e.parts) {
             Run<float, 8> o;
             o.set(v);
-            o.store(e.parts + ((int64_t)blockIdx.y * M + m) * e.N + n, here);
+            o.store(e.parts + ((int64_t)blockIdx.y * M + m) * e.pitch + n);
         } else linear_end<T, 8>(e.end, m, n, here, v, residual);
     }
 };
@@ -142,14 +142,14 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const float* __restric
     const int32_t n = (int32_t)(i - m * per_row) * 4, here = min(4, N - n);
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (there) {
-        const float* from = parts + m * N + n;
-        const int64_t stride = (int64_t)M * N;
+        const int32_t pitch = (N + 7) / 8 * 8;
+        const float* from = parts + m * pitch + n;
+        const int64_t stride = (int64_t)M * pitch;
 #pragma unroll 4
         for (int32_t s = lane; s < splits; s += LANES) {
             Run<float, 4> r;
             float f[4];
-            if (here == 4) r.load(from + s * stride);
-            else r.load(from + s * stride, here, 0.0f);
+            r.load(from + s * stride);
             r.get(f);
 #pragma unroll
             for (int w = 0; w < 4; ++w) v[w] += f[w];
@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, con
     if (parts) {
         Run<float, 4> o;
         o.set(v);
-        o.store(parts + ((int64_t)blockIdx.y * cap + r) * N + col, here);
+        o.store(parts + ((int64_t)blockIdx.y * cap + r) * ((N + 7) / 8 * 8) + col);
     } else linear_end<T, 4>(e, r, col, here, v, linear_ahead<T, 4>(e, r, col, here));
 }
 
@@ -385,7 +385,7 @@ static int linear_few_splits(int64_t K, int64_t N, int64_t rows, int es) {
     while (splits < 32 && splits * 2 <= most && bytes > splits * (128 << 10)) splits *= 2;
     return splits == 2 && rows < 4 ? 1 : splits;
 }
-static size_t linear_parts_bytes(const LinearPlan& p, int64_t M, int64_t N) { return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0; }
+static size_t linear_parts_bytes(const LinearPlan& p, int64_t M, int64_t N) { return p.splits > 1 ? (size_t)p.splits * M * wide_of(N) * 4 : 0; }
 
 static inline int planes_of_type(no_dtype dt) { return dt == NO_F32 ? 3 : 1; }
 static inline size_t operand_bytes(no_dtype dt, int64_t rows, int64_t dim) { return round_256((size_t)rows * wide_of(dim) * 2 * planes_of_type(dt)); }
@@ -425,7 +425,7 @@ template <typename T, bool AL, bool BL>
 static bool linear_product(DenseArgs g, const LinearEnd& end, float* parts, const BiasJob& bias, hipStream_t st) {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;
     const LinearPlan p = linear_plan(g.M, g.N, g.K, P);
-    const typename LinearOut<T>::Args e{p.splits > 1 ? LinearEnd{} : end, p.splits > 1 ? parts : nullptr, g.N};
+    const typename LinearOut<T>::Args e{p.splits > 1 ? LinearEnd{} : end, p.splits > 1 ? parts : nullptr, (int32_t)wide_of(g.N)};
     dense_launch<__bf16, P, AL, BL, LinearOut<T>>(g, e, DensePlan{p.kind, p.splits}, 1, st);
     if (p.splits > 1) linear_join<T>(parts, p.splits, g.M, g.d_M, g.N, end, bias, st);
     return p.splits > 1;        // (the column sums went along)
@@ -535,7 +535,7 @@ extern "C" size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_
     if (px > parts) parts = px;
     if (pw > parts) parts = pw;
     if (n <= LINEAR_FEW) {
-        const size_t few = (size_t)linear_few_splits(d_in, d_out, n, dt == NO_F32 ? 4 : 2) * n * d_out * 4;
+        const size_t few = (size_t)linear_few_splits(d_in, d_out, n, dt == NO_F32 ? 4 : 2) * n * wide_of(d_out) * 4;
         if (few > parts) parts = few;
     }
     return 256 + operand_bytes(dt, n, d_in) + operand_bytes(dt, d_in, d_out) + operand_bytes(dt, n, d_out) + round_256((size_t)gz_blocks(n) * d_out * 4) + round_256(parts);

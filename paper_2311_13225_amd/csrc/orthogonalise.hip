@@ -49,29 +49,29 @@ struct NsEnd {
     };
     static constexpr bool MIRROR = SYMMETRIC;
     struct Ahead { f16x8 h, l; };
-    __device__ static __forceinline__ Ahead ahead(const Args& e, int32_t m, int32_t n, int32_t) {
+    __device__ static __forceinline__ Ahead ahead(const Args& e, int64_t z, int32_t m, int32_t n, int32_t) {
         Ahead a;
         if (e.from.p) {
-            const char* from = e.from.p + (int64_t)blockIdx.z * e.from.matrix + m * e.from.pitch + n * 2;
+            const char* from = e.from.p + z * e.from.matrix + m * e.from.pitch + n * 2;
             a.h = *reinterpret_cast<const f16x8*>(from);
             a.l = *reinterpret_cast<const f16x8*>(from + e.from.plane);
         }
         return a;
     }
-    __device__ static __forceinline__ void pieces(const Args& e, int32_t m, int32_t n, const float (&v)[8]) {
-        ns_store(v, e.to.p + (int64_t)blockIdx.z * e.to.matrix + m * e.to.pitch + n * 2, e.to.plane);
+    __device__ static __forceinline__ void pieces(const Args& e, int64_t z, int32_t m, int32_t n, const float (&v)[8]) {
+        ns_store(v, e.to.p + z * e.to.matrix + m * e.to.pitch + n * 2, e.to.plane);
     }
-    __device__ static __forceinline__ void put(const Args& e, int32_t m, int32_t n, int32_t here, float (&v)[8], const Ahead& a, int32_t) {
+    __device__ static __forceinline__ void put(const Args& e, int64_t z, int32_t m, int32_t n, int32_t here, float (&v)[8], const Ahead& a, int32_t) {
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
             v[w] *= e.by;
             if (e.from.p) v[w] += e.own * ((float)a.h[w] + (float)a.l[w]);
             if (w >= here) v[w] = 0.0f;
         }
-        if (SYMMETRIC || e.kind == NS_PIECES) return pieces(e, m, n, v);
+        if (SYMMETRIC || e.kind == NS_PIECES) return pieces(e, z, m, n, v);
 #pragma unroll
         for (int w = 0; w < 8; ++w) v[w] *= NS_VALUE;
-        const RowsOf out = e.out.of(blockIdx.z);
+        const RowsOf out = e.out.of(z);
         if (e.kind == NS_OUT_BF16) {
             Run<bf16_t, 8> o;
             o.set(v);
@@ -89,7 +89,7 @@ struct NsEnd {
         o.set(v);
         o.store(out.row<float>(m) + n, here);
     }
-    __device__ static __forceinline__ void mirror(const Args& e, int32_t m, int32_t n, const float (&v)[8]) { pieces(e, m, n, v); }
+    __device__ static __forceinline__ void mirror(const Args& e, int64_t z, int32_t m, int32_t n, const float (&v)[8]) { pieces(e, z, m, n, v); }
 };
 
 // ------------------------------------------------------------------------------------------------------- before the products
