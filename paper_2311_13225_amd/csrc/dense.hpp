@@ -221,7 +221,7 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
                 float v[8];
 #pragma unroll
                 for (int w = 0; w < 8; ++w) v[w] = m + w < M ? mine[(l % (ROWS / 8) * 8 + w) * PITCH + c] : 0.0f;
-                E::mirror(e, matrix, n2, m, v);
+                E::mirror(e, matrix, n2, m, v, g.M);
             }
         }
     }
@@ -582,10 +582,10 @@ static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matr
         if (k.per_unit == 0) continue;
         const int64_t a = ceil_div(M < 1 ? 1 : M, k.bm), b = ceil_div(N, k.bn), tiles = (half ? a * (a + 1) / 2 : a * b) * matrices;
         for (int splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 2) {
-            if (splits > 1 && (steps < splits * 4 || (size_t)splits * M * N * 4 > parts_most)) break;
+            if (splits > 1 && (steps < splits * 4 || (size_t)splits * M * wide_of(N) * matrices * 4 > parts_most)) break;
             const int64_t units = ceil_div(tiles * splits, 256), rounds = ceil_div(units, k.per_unit);
             double t = (double)rounds * ((double)ceil_div(steps, splits) * (k.one + k.more * (double)((rounds > 1 ? k.per_unit : units) - 1)) + k.start);
-            if (splits > 1) t += 4.0 + (double)splits * M * N * 8 / 4e6;
+            if (splits > 1) t += 5.0 + (double)splits * M * N * matrices * 8 / 3.5e6;
             if (t < least) { least = t; best = DensePlan{kind, splits}; }
         }
     }

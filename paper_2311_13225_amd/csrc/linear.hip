@@ -295,14 +295,16 @@ __global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z,
 // tiles of 32 x 32 8.6, eight rows 24 and 8.6; fp32, one row 13.9, eight of 2048 x 2048 13.2, where copy and tiles of nine rows of 8192 x 2048 take 48.)
 constexpr int LINEAR_FEW = 8, LINEAR_FEW_K = 1024;      // rows; reduction indices in LDS at a time
 
-template <typename T, int MR>
+template <typename T, int MR, bool SHORT>
 __global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int32_t K, int32_t N, int32_t splits, LinearEnd e, float* parts) {
-    constexpr int W = 16 / (int)sizeof(T), LANES = 8, LINES = 512 / LANES;
+    constexpr int W = 16 / (int)sizeof(T), LANES = 8, LINES = 512 / LANES, AHEAD = MR <= 2 ? 16 : 8;      // rows of the matrix requested at once
     __shared__ __attribute__((aligned(16))) float xs[LINEAR_FEW_K * MR];
     __shared__ float share[8][MR][LANES * W];
     const int32_t n = rows_here(d_n, cap);
     const int lane = (int)threadIdx.x & (LANES - 1), line = (int)threadIdx.x / LANES;
-    const int32_t c = ((int32_t)blockIdx.x * LANES + lane) * W;
+    const int32_t c0 = (int32_t)blockIdx.x * LANES * W, c = c0 + lane * W;
+    // (a run that would leave the row begins W before its end: requests are whole and nothing branches around them)
+    const Place<W, SHORT> place(c < N ? c : 0, N);
     const int32_t k0 = (int32_t)((int64_t)K * blockIdx.y / splits), k1 = (int32_t)((int64_t)K * (blockIdx.y + 1) / splits);
     float acc[MR][W] = {};
     for (int32_t kb = k0; kb < k1; kb += LINEAR_FEW_K) {
@@ -313,28 +315,21 @@ __global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, con
             xs[k * MR + r] = r < n ? to_f32(x.row<T>(r)[kb + k]) : 0.0f;
         }
         __syncthreads();
-        if (c < N) {
-            auto add = [&](const Run<T, W>& v, int32_t k) {
+        for (int32_t k = line; k < here; k += AHEAD * LINES) {
+            Run<T, W> v[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) place.load(v[a], w.row<T>(kb + min(k + a * LINES, here - 1)));
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
                 float f[W];
-                v.get(f);
+                v[a].get(f);
+                const int32_t at = k + a * LINES;
+                if (at < here) {
 #pragma unroll
-                for (int r = 0; r < MR; ++r)
+                    for (int r = 0; r < MR; ++r)
 #pragma unroll
-                    for (int j = 0; j < W; ++j) acc[r][j] += xs[k * MR + r] * f[j];
-            };
-            constexpr int AHEAD = 8;        // rows of the matrix requested at once
-            int32_t k = line;
-            for (; k + (AHEAD - 1) * LINES < here; k += AHEAD * LINES) {
-                Run<T, W> v[AHEAD];
-#pragma unroll
-                for (int a = 0; a < AHEAD; ++a) v[a].load_at(w.row<T>(kb + k + a * LINES), c, N, from_f32<T>(0.0f));
-#pragma unroll
-                for (int a = 0; a < AHEAD; ++a) add(v[a], k + a * LINES);
-            }
-            for (; k < here; k += LINES) {
-                Run<T, W> v;
-                v.load_at(w.row<T>(kb + k), c, N, from_f32<T>(0.0f));
-                add(v, k);
+                        for (int j = 0; j < W; ++j) acc[r][j] += xs[at * MR + r] * f[j];
+                }
             }
         }
     }
@@ -346,12 +341,13 @@ __global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, con
             float s = acc[r][j];
 #pragma unroll
             for (int o = LANES; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
-            if (lane_id() < LANES) share[threadIdx.x >> 6][r][lane * W + j] = s;
+            const int32_t col = place.at + j - c0;
+            if (lane_id() < LANES && c < N && col >= 0) share[threadIdx.x >> 6][r][col] = s;      // (two lanes at a row's end may hold a column, with the same sum)
         }
     __syncthreads();
     constexpr int UNITS = LANES * W / 4;
     const int r = (int)threadIdx.x / UNITS, u = (int)threadIdx.x % UNITS;
-    const int32_t col = (int32_t)blockIdx.x * LANES * W + u * 4;
+    const int32_t col = c0 + u * 4;
     if (r >= MR || r >= n || col >= N) return;
     float v[4] = {};
 #pragma unroll
@@ -438,12 +434,14 @@ static void linear_fwd(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int3
         const int splits = linear_few_splits(d_in, d_out, cap, sizeof(T));
         float* parts = splits > 1 ? (float*)ws : nullptr;
         const dim3 grid((unsigned)ceil_div(d_out, 128 / (int)sizeof(T)), (unsigned)splits);
-#define NO_FEW(MR) hipLaunchKernelGGL((linear_few_kernel<T, MR>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts)
+#define NO_FEW_AS(MR, SHORT) hipLaunchKernelGGL((linear_few_kernel<T, MR, SHORT>), grid, dim3(512), 0, st, x, w, d_n, cap, d_in, d_out, splits, end, parts)
+#define NO_FEW(MR) do { if (d_out < 16 / (int)sizeof(T)) NO_FEW_AS(MR, true); else NO_FEW_AS(MR, false); } while (0)
         if (cap <= 1) NO_FEW(1);
         else if (cap <= 2) NO_FEW(2);
         else if (cap <= 4) NO_FEW(4);
         else NO_FEW(8);
 #undef NO_FEW
+#undef NO_FEW_AS
         if (splits > 1) linear_join<T>(parts, splits, cap, d_n, d_out, end, BiasJob{}, st);
         return;
     }

@@ -46,6 +46,9 @@ struct NsEnd {
         int32_t kind;
         NsRows out;
         float keep, step;
+        float* parts;           // not NULL: sums of a part of the reduction, [split][matrix][rows][pitch] of fp32, instead
+        int32_t pitch;
+        int64_t part;           // values from split to split
     };
     static constexpr bool MIRROR = SYMMETRIC;
     struct Ahead { f16x8 h, l; };
@@ -58,10 +61,17 @@ struct NsEnd {
         }
         return a;
     }
+    // a part's place; M is the side of a square where there are parts
+    __device__ static __forceinline__ void keep_part(const Args& e, int64_t z, int32_t m, int32_t n, const float (&v)[8], int32_t M) {
+        Run<float, 8> o;
+        o.set(v);
+        o.store(e.parts + blockIdx.y * e.part + (z * M + m) * e.pitch + n);
+    }
     __device__ static __forceinline__ void pieces(const Args& e, int64_t z, int32_t m, int32_t n, const float (&v)[8]) {
         ns_store(v, e.to.p + z * e.to.matrix + m * e.to.pitch + n * 2, e.to.plane);
     }
-    __device__ static __forceinline__ void put(const Args& e, int64_t z, int32_t m, int32_t n, int32_t here, float (&v)[8], const Ahead& a, int32_t) {
+    __device__ static __forceinline__ void put(const Args& e, int64_t z, int32_t m, int32_t n, int32_t here, float (&v)[8], const Ahead& a, int32_t M) {
+        if (SYMMETRIC && e.parts) return keep_part(e, z, m, n, v, M);
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
             v[w] *= e.by;
@@ -89,8 +99,33 @@ struct NsEnd {
         o.set(v);
         o.store(out.row<float>(m) + n, here);
     }
-    __device__ static __forceinline__ void mirror(const Args& e, int64_t z, int32_t m, int32_t n, const float (&v)[8]) { pieces(e, z, m, n, v); }
+    __device__ static __forceinline__ void mirror(const Args& e, int64_t z, int32_t m, int32_t n, const float (&v)[8], int32_t M) {
+        if (e.parts) keep_part(e, z, m, n, v, M);
+        else pieces(e, z, m, n, v);
+    }
 };
+
+// The parts of Gram matrices added up in order, in pieces.
+__global__ void __launch_bounds__(256) ns_join_kernel(const float* __restrict__ parts, int32_t splits, int64_t part, int32_t side, int32_t pitch, int32_t matrices, float by, NsMatrix to) {
+    const int32_t units = pitch / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / units;
+    if (row >= (int64_t)matrices * side) return;
+    const int32_t c = (int32_t)(i - row * units) * 8;
+    float v[8] = {};
+#pragma unroll 4
+    for (int32_t s = 0; s < splits; ++s) {
+        Run<float, 8> r;
+        float f[8];
+        r.load(parts + s * part + row * pitch + c);
+        r.get(f);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v[w] += f[w];
+    }
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v[w] = c + w < side ? v[w] * by : 0.0f;
+    const int64_t z = row / side;
+    ns_store(v, to.p + z * to.matrix + (row - z * side) * to.pitch + c * 2, to.plane);
+}
 
 // ------------------------------------------------------------------------------------------------------- before the products
 
@@ -175,17 +210,21 @@ __global__ void __launch_bounds__(256) ns_pieces_kernel(NsSource<T> u, int32_t r
 
 template <bool AL, bool BL, bool HALF>
 static void ns_product(const NsMatrix& a, int32_t a_extent, const NsMatrix& b, int32_t b_extent, int32_t M, int32_t N, int32_t K, int32_t matrices, const typename NsEnd<HALF>::Args& e,
-                       hipStream_t st) {
+                       const DensePlan& plan, hipStream_t st) {
     DenseArgs g{};
     g.a = DenseOperand{a.p, a.pitch, a.matrix, a.plane, a_extent};
     g.b = DenseOperand{b.p, b.pitch, b.matrix, b.plane, b_extent};
     g.M = M; g.N = N; g.K = K;
-    dense_launch<_Float16, 2, AL, BL, NsEnd<HALF>>(g, e, dense_plan(M, N, K, 2, matrices, HALF, 0), matrices, st);
+    dense_launch<_Float16, 2, AL, BL, NsEnd<HALF>>(g, e, plan, matrices, st);
 }
+
+constexpr size_t NS_PARTS_MOST = (size_t)64 << 20;       // bytes of a Gram matrix's parts, at most
 
 struct NsRoom {
     NsMatrix x[2], gram, poly;
     double* sums;
+    float* parts;
+    DensePlan plan;         // of the Gram matrices
     size_t bytes;
 };
 
@@ -205,6 +244,9 @@ static NsRoom ns_room(char* ws, int64_t matrices, int64_t rows, int64_t cols) {
     r.x[1] = ns_matrix(p, matrices, rows, cols);
     r.gram = ns_matrix(p, matrices, side, side);
     r.poly = ns_matrix(p, matrices, side, side);
+    r.plan = dense_plan(side, side, rows < cols ? cols : rows, 2, matrices < 1 ? 1 : matrices, true, NS_PARTS_MOST);
+    r.parts = (float*)p;
+    if (r.plan.splits > 1) p += round_256((size_t)r.plan.splits * matrices * side * wide_of(side) * 4);
     r.bytes = (size_t)(p - ws);
     return r;
 }
@@ -223,15 +265,21 @@ static void newton_schulz(const NsSource<T>& u, int32_t matrices, int32_t rows, 
     const NsRows nowhere{{nullptr, 0}, 0};
     for (int32_t s = 0; s < steps; ++s) {
         const NsMatrix &x = room.x[s & 1], &next = room.x[(s & 1) ^ 1];
-        const NsEnd<true>::Args gram{none, room.gram, 0.0f, NS_VALUE, NS_PIECES, nowhere, 0.0f, 0.0f};
-        if (tall) ns_product<false, false, true>(x, wide_c, x, wide_c, side, side, rows, matrices, gram, st);
-        else ns_product<true, true, true>(x, rows, x, rows, side, side, cols, matrices, gram, st);
-        const NsEnd<true>::Args poly{room.gram, room.poly, NS_B, NS_C * NS_VALUE, NS_PIECES, nowhere, 0.0f, 0.0f};
-        ns_product<true, true, true>(room.gram, side, room.gram, side, side, side, side, matrices, poly, st);
+        const int32_t pitch = (int32_t)wide_of(side);
+        const int64_t part = (int64_t)matrices * side * pitch;
+        const bool split = room.plan.splits > 1;
+        const NsEnd<true>::Args gram{none, room.gram, 0.0f, NS_VALUE, NS_PIECES, nowhere, 0.0f, 0.0f, split ? room.parts : nullptr, pitch, part};
+        if (tall) ns_product<false, false, true>(x, wide_c, x, wide_c, side, side, rows, matrices, gram, room.plan, st);
+        else ns_product<true, true, true>(x, rows, x, rows, side, side, cols, matrices, gram, room.plan, st);
+        if (split)
+            hipLaunchKernelGGL(ns_join_kernel, dim3((unsigned)ceil_div(part / 8, 256)), dim3(256), 0, st, room.parts, room.plan.splits, part, side, pitch, matrices, NS_VALUE, room.gram);
+        const NsEnd<true>::Args poly{room.gram, room.poly, NS_B, NS_C * NS_VALUE, NS_PIECES, nowhere, 0.0f, 0.0f, nullptr, 0, 0};
+        ns_product<true, true, true>(room.gram, side, room.gram, side, side, side, side, matrices, poly, dense_plan(side, side, side, 2, matrices, true, 0), st);
         const bool last = s == steps - 1;
-        const NsEnd<false>::Args to{x, next, NS_A, NS_VALUE, last ? kind : (int32_t)NS_PIECES, out, keep, step};
-        if (tall) ns_product<true, true, false>(x, rows, room.poly, side, rows, cols, side, matrices, to, st);
-        else ns_product<true, false, false>(room.poly, side, x, wide_c, rows, cols, side, matrices, to, st);
+        const NsEnd<false>::Args to{x, next, NS_A, NS_VALUE, last ? kind : (int32_t)NS_PIECES, out, keep, step, nullptr, 0, 0};
+        const DensePlan plan = dense_plan(rows, cols, side, 2, matrices, false, 0);
+        if (tall) ns_product<true, true, false>(x, rows, room.poly, side, rows, cols, side, matrices, to, plan, st);
+        else ns_product<true, false, false>(room.poly, side, x, wide_c, rows, cols, side, matrices, to, plan, st);
     }
 }
 
