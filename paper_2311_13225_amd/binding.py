@@ -639,7 +639,7 @@ def no_logprobs_bwd(z: torch.Tensor, tokens: torch.Tensor, temperature: float, l
 
 # ------------------------------------------------------------------------------------------ dense block and its update
 
-NO_MAX_LINEAR_DIM, NO_MAX_UPDATE_DIM = 1 << 20, 32768
+NO_MAX_LINEAR_DIM, NO_MAX_LINEAR_ROWS, NO_MAX_UPDATE_DIM = 1 << 20, (1 << 31) - 1024, 32768
 
 
 def no_layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], eps: float, y: torch.Tensor,

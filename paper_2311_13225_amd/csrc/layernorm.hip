@@ -390,7 +390,7 @@ extern "C" int32_t no_layernorm_bwd(const void* d_s, no_dtype dt, int64_t s_stri
     bool direct = true;
 #define NO_NORM_AS(T, TEAM, THREADS, U)                                                                                                              \
     do {                                                                                                                                             \
-        room(layernorm_blocks(n_rows_cap, THREADS / TEAM, THREADS == 1024 ? 256 : LAYERNORM_PARTS), true);                                           \
+        room(layernorm_blocks(n_rows_cap, THREADS / TEAM, THREADS >= 512 ? 256 : LAYERNORM_PARTS), true);                                           \
         hipLaunchKernelGGL((layernorm_bwd_kernel<T, TEAM, THREADS, U>), dim3((unsigned)n_parts), dim3(THREADS), 0, st, s, d_weight, d_mean, d_rstd, gy, gs, d_n_rows, \
                            n_rows_cap, dim, gx, parts_w, parts_b);                                                                                   \
     } while (0)
@@ -407,8 +407,9 @@ extern "C" int32_t no_layernorm_bwd(const void* d_s, no_dtype dt, int64_t s_stri
         else if (units <= 256) NO_NORM_AS(T, (sizeof(T) == 2 ? 256 : 64), 256, (sizeof(T) == 2 ? 1 : 4));                                            \
         else if (units <= 512) NO_NORM_AS(T, 256, 256, 2);                                                                                           \
         else if (units <= 1024) NO_NORM_AS(T, 256, 256, 4);                                                                                          \
-        else if (units <= 2048) NO_NORM_AS(T, 1024, 1024, 2);                                                                                        \
-        else if (sizeof(T) == 4 && units <= 4096) NO_NORM_AS(T, 1024, 1024, sizeof(T) == 4 ? 4 : 2);                                                 \
+        /* (3000 x 16384 bf16 with grad_sum 165 us; 1024 lanes, whose registers do not hold it, 260) */                                             \
+        else if (units <= 2048) NO_NORM_AS(T, 512, 512, 4);                                                                                          \
+        else if (sizeof(T) == 4 && units <= 4096) NO_NORM_AS(float, 1024, 1024, 4);                                                                  \
         else {                                                                                                                                       \
             direct = false;                                                                                                                          \
             room(n_rows_cap < 64 ? n_rows_cap : 64, false);                                                                                          \

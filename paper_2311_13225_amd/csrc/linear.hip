@@ -516,7 +516,8 @@ static int32_t linear_sizes(const char* who, no_dtype dt, int32_t act, int32_t c
     NO_REQUIRE(dt == NO_F32 || dt == NO_BF16, NO_ERR_INVALID_ARG, "%s: values are NO_F32 or NO_BF16", who);
     NO_REQUIRE(act >= NO_ACT_NONE && act <= NO_ACT_SILU, NO_ERR_INVALID_ARG, "%s: unknown activation", who);
     NO_REQUIRE(cap >= 0 && d_in >= 1 && d_out >= 1, NO_ERR_INVALID_ARG, "%s: bad sizes", who);
-    NO_REQUIRE(d_in <= NO_MAX_LINEAR_DIM && d_out <= NO_MAX_LINEAR_DIM, NO_ERR_UNSUPPORTED, "%s: a side of more than %d", who, NO_MAX_LINEAR_DIM);
+    NO_REQUIRE(d_in <= NO_MAX_LINEAR_DIM && d_out <= NO_MAX_LINEAR_DIM && cap <= NO_MAX_LINEAR_ROWS, NO_ERR_UNSUPPORTED, "%s: a side of more than %d, or more than %d rows", who,
+               NO_MAX_LINEAR_DIM, NO_MAX_LINEAR_ROWS);
     return NO_OK;
 }
 
@@ -525,7 +526,7 @@ static int32_t linear_sizes(const char* who, no_dtype dt, int32_t act, int32_t c
 using namespace no;
 
 extern "C" size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_in, int32_t d_out) {
-    if ((dt != NO_F32 && dt != NO_BF16) || n_rows_cap < 0 || d_in < 1 || d_out < 1 || d_in > NO_MAX_LINEAR_DIM || d_out > NO_MAX_LINEAR_DIM) return 0;
+    if ((dt != NO_F32 && dt != NO_BF16) || n_rows_cap < 0 || d_in < 1 || d_out < 1 || d_in > NO_MAX_LINEAR_DIM || d_out > NO_MAX_LINEAR_DIM || n_rows_cap > NO_MAX_LINEAR_ROWS) return 0;
     const int pieces = planes_of_type(dt);
     const int64_t n = n_rows_cap;
     size_t parts = linear_parts_bytes(linear_plan(n, d_out, d_in, pieces), n, d_out);

@@ -37,13 +37,14 @@ def test_linear_refusals(lib):
     swept(lib.no_linear_fwd, good, [({0: None}, INVALID), ({3: None}, INVALID), ({15: None}, INVALID), ({17: None}, INVALID), ({17: ODD}, INVALID), ({18: 0}, CAPACITY), ({1: 2}, INVALID),
                                     ({1: -1}, INVALID), ({6: 4}, INVALID), ({6: -1}, INVALID), ({10: -1}, INVALID), ({11: 0}, INVALID), ({12: 0}, INVALID), ({2: 28}, INVALID), ({2: 34}, INVALID),
                                     ({4: 60}, INVALID), ({16: 60}, INVALID), ({7: P, 8: 60}, INVALID), ({13: P, 14: 60}, INVALID), ({0: ODD}, INVALID), ({3: ODD}, INVALID),
-                                    ({11: (1 << 20) + 1, 2: 1 << 23}, UNSUPPORTED), ({12: (1 << 20) + 1, 4: 1 << 23, 16: 1 << 23}, UNSUPPORTED)])
+                                    ({11: (1 << 20) + 1, 2: 1 << 23}, UNSUPPORTED), ({12: (1 << 20) + 1, 4: 1 << 23, 16: 1 << 23}, UNSUPPORTED),
+                                    ({10: (1 << 31) - 1023}, UNSUPPORTED)])
     #       x dt stride w stride act z stride gy stride n cap d_in d_out gx stride gw stride gb ws bytes stream
     good = [P, 0, 32, P, 64, 2, P, 64, P, 64, None, 4, 8, 16, P, 32, P, 64, P, P, 1 << 40, None]
     swept(lib.no_linear_bwd, good, [({0: None}, INVALID), ({3: None}, INVALID), ({6: None}, INVALID), ({8: None}, INVALID), ({19: None}, INVALID), ({19: ODD}, INVALID), ({20: 0}, CAPACITY),
                                     ({1: 2}, INVALID), ({5: 4}, INVALID), ({11: -1}, INVALID), ({12: 0}, INVALID), ({13: 0}, INVALID), ({2: 28}, INVALID), ({4: 60}, INVALID), ({7: 60}, INVALID),
                                     ({9: 60}, INVALID), ({15: 28}, INVALID), ({17: 60}, INVALID), ({14: ODD}, INVALID), ({12: (1 << 20) + 1, 2: 1 << 23, 15: 1 << 23}, UNSUPPORTED)])
-    for bad in ((2, 4, 8, 8), (0, -1, 8, 8), (0, 4, 0, 8), (0, 4, 8, 0), (0, 4, (1 << 20) + 1, 8), (1, 4, 8, (1 << 20) + 1)):
+    for bad in ((2, 4, 8, 8), (0, -1, 8, 8), (0, 4, 0, 8), (0, 4, 8, 0), (0, 4, (1 << 20) + 1, 8), (1, 4, 8, (1 << 20) + 1), (1, (1 << 31) - 1, 8, 8)):
         assert lib.no_linear_ws_bytes(*bad) == 0, bad
     assert lib.no_linear_ws_bytes(0, 0, 1, 1) > 0
     # (a size that does not fit 32 bits anywhere on its way)
