@@ -113,7 +113,7 @@ __device__ __forceinline__ void dense_multiply(f32x4 (&acc)[I][J], const s16x8 (
 }
 
 // A block's place: the tiles of all matrices are dealt to the dies in runs, and walked in bands of eight tile rows, so that a die's blocks share rows and columns in its L2 (four Gram matrices of 512 x 2048, each
-// matrix dealt to all dies: 22 us, to two of them 16).
+// matrix dealt to all dies: 22.2 us, to two of them 20.5).
 // HALF: the tiles on and above the diagonal of a square alone.
 constexpr int DENSE_BAND = 8;
 static inline int64_t dense_tiles(int64_t tiles_m, int64_t tiles_n, bool half) { return half ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n; }
@@ -557,6 +557,155 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
     dense_finish<BM, BN, 2, 2, E>(g, e, matrix, tm, tn, M, acc, lds);
 }
 
+// Values of fp32 rows cut on their way from LDS: A is the matrix itself, ALONG, at any alignment of a value, and only its last K % 32 columns are a copy (`tail`: 32 columns, zeros at the end), so that
+// nothing is read past a row; B is in three pieces, across. A tile of 256 x 128 by four wavefronts as above, but walked by fragments of 16 rows: a fragment's 24 products go on while the next
+// one is cut, one or two instructions beside each product, and the one after that is read. 24922 x 602 x 256: 64 us and 5 before it; behind a copy of A in
+// pieces, which takes 25, 62.
+struct DenseRawArgs {
+    DenseArgs g;            // g.a: the rows (pitch of 4-byte multiples); g.a.plane is not used
+    DenseOperand tail;
+};
+template <typename E>
+__global__ void __launch_bounds__(256, 1) dense_raw_kernel(const DenseRawArgs ga, const typename E::Args e) {
+    constexpr int BM = 256, BN = 128, T = 256, I = 8, J = 4, PRODUCTS = 6 * J;
+    typedef DenseTile<1, true, BM, T> TA;       // (32 values of 4 bytes take the place of 64 of 2)
+    typedef DenseTile<3, false, BN, T> TB;
+    constexpr int BK = 32, COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
+    static_assert(TB::BK == BK && REQ <= 2 * PRODUCTS, "steps of both operands, and a place for every request");
+    __shared__ __attribute__((aligned(1024))) char lds[dense_shared(3, BM, BN, 2, 1, DenseFinish<BM, BN, 2, 2>::BYTES)];
+    const DenseArgs& g = ga.g;
+    int matrix, tm, tn;
+    if (!dense_place<false>(g, matrix, tm, tn)) return;
+    const int32_t M = rows_here(g.d_M, g.M), K = g.K, m0 = tm * BM, n0 = tn * BN;
+    if (m0 >= M) return;
+    const int wave = (int)threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, l = (int)threadIdx.x & 63, gr = l >> 4, j16 = l & 15;
+    TA ta;
+    TB tb;
+    DenseOperand oa = g.a, ot = ga.tail;
+    oa.extent = ot.extent = min(oa.extent, M);
+    ta.open(oa, 0, m0);
+    tb.open(g.b, 0, n0);
+    const int32_t steps = (K + BK - 1) / BK, first = (int32_t)((int64_t)steps * blockIdx.y / g.splits), last = (int32_t)((int64_t)steps * (blockIdx.y + 1) / g.splits);
+    f32x4 acc[I][J], big[I][J];       // the largest product's sums apart from the other five's
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            acc[i][j] = big[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            asm volatile("" : "+a"(acc[i][j]));
+            asm volatile("" : "+a"(big[i][j]));
+        }
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + (uint32_t)wave * 1024u);
+    const int32_t whole = K / BK;
+    i32x4 ra, rb;
+    // what comes before the requests of step s (those past K are zeros, those past `last` are loaded and not used)
+    auto aim = [&](int32_t s) {
+        if (s >= whole) {
+            if (s == whole && K % BK != 0) {        // the copied columns, whose rows are whole
+                ta.open(ot, 0, m0);
+                ta.base -= (int64_t)whole * TA::BK * 2;
+            } else ta.cut(0);
+            tb.cut(K - s * BK);
+        }
+        ra = ta.source(s);
+        rb = tb.source(s);
+    };
+    auto request = [&](int n, int copy) {
+        if (n < TA::REQ) ta.request_one(n, ra, lds0 + copy * COPY);
+        else tb.request_one(n - TA::REQ, rb, lds0 + copy * COPY + TA::BYTES);
+    };
+    s16x8 fb[2][3][J];
+    i32x4 raw[2][2];                // two fragments' values on their way: eight a lane
+    i32x4 piece[2][3];              // this fragment's pieces and the next one's, pairs of values
+    uint32_t r0, r1;                // what is left of the pair that is cut
+    auto take_b = [&](int n, int half, int copy) { fb[half][n / J][n % J] = TB::fragment(lds + copy * COPY + TA::BYTES, wn * J + n % J, n / J); };
+    auto take_raw = [&](int i, int copy) {
+        const char* row = lds + copy * COPY + ((wm * I + i) * 16 + j16) * 128;
+        raw[i & 1][0] = *reinterpret_cast<const i32x4*>(row + ((2 * gr) ^ (j16 & 7)) * 16);
+        raw[i & 1][1] = *reinterpret_cast<const i32x4*>(row + ((2 * gr + 1) ^ (j16 & 7)) * 16);
+    };
+    // part n of 24 of cutting fragment i's values, x = h + m + l: six a pair
+    auto cut = [&](int n, int i) {
+        const int pair = n / 6, at = i & 1;
+        i32x4(&p)[3] = piece[at];
+        auto round = [&](int which) {
+            typedef float f2 __attribute__((ext_vector_type(2)));
+            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+            p[which][pair] = __builtin_bit_cast(int32_t, __builtin_convertvector((f2{__uint_as_float(r0), __uint_as_float(r1)}), b2));
+        };
+        auto left = [](uint32_t& r, uint32_t high) { r = __float_as_uint(__uint_as_float(r) - __uint_as_float(high)); };
+        if (n % 6 == 0) {
+            r0 = (uint32_t)raw[at][pair / 2][pair % 2 * 2];
+            r1 = (uint32_t)raw[at][pair / 2][pair % 2 * 2 + 1];
+            round(0);
+        }
+        if (n % 6 == 1) left(r0, (uint32_t)p[0][pair] << 16);
+        if (n % 6 == 2) { left(r1, (uint32_t)p[0][pair] & 0xffff0000u); round(1); }
+        if (n % 6 == 3) left(r0, (uint32_t)p[1][pair] << 16);
+        if (n % 6 == 4) left(r1, (uint32_t)p[1][pair] & 0xffff0000u);
+        if (n % 6 == 5) round(2);
+    };
+    constexpr int PA[6] = {0, 0, 0, 1, 1, 2}, PB[6] = {2, 0, 1, 1, 0, 0};      // (what was cut last is wanted last)
+    auto one = [&](int n, int i, int half) {
+        const int pair = n / J, j = n % J;
+        const s16x8 a = __builtin_bit_cast(s16x8, piece[i & 1][PA[pair]]);
+        if (pair == 1) dense_mfma_in_place<__bf16>(big[i][j], fb[half][PB[pair]][j], a);
+        else dense_mfma_in_place<__bf16>(acc[i][j], fb[half][PB[pair]][j], a);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    aim(first);
+#pragma unroll
+    for (int n = 0; n < REQ; ++n) request(n, 0);
+    aim(first + 1);
+#pragma unroll
+    for (int n = 0; n < REQ; ++n) request(n, 1);
+    dense_meet<REQ>();
+#pragma unroll
+    for (int n = 0; n < 3 * J; ++n) take_b(n, 0, 0);
+    take_raw(0, 0);
+    take_raw(1, 0);
+#pragma unroll
+    for (int n = 0; n < 24; ++n) cut(n, 0);
+    auto step = [&](auto copy_of, int32_t s) {
+        constexpr int now = decltype(copy_of)::value;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if (i == I - 2) {           // the last fragment of this copy is in registers
+                aim(s + 2);
+                dense_meet<0>();
+            }
+#pragma unroll
+            for (int n = 0; n < PRODUCTS; ++n) {
+                if (n == 0) {               // the fragment after the next one, into the place of the one that has been cut
+                    if (i < I - 2) take_raw(i + 2, now);
+                    else take_raw(i + 2 - I, now ^ 1);
+                }
+                cut(n, (i + 1) % I);
+                if (i >= I - 2) {
+                    const int k = (i - (I - 2)) * PRODUCTS + n;
+                    if (k % 4 == 0 && k / 4 < 3 * J) take_b(k / 4, now ^ 1, now ^ 1);
+                    if (k % 3 == 1 && k / 3 < REQ) request(k / 3, now);
+                }
+                one(n, i, now);
+            }
+        }
+    };
+    int32_t s = first;
+    for (; s + 1 < last; s += 2) {
+        step(std::integral_constant<int, 0>{}, s);
+        step(std::integral_constant<int, 1>{}, s + 1);
+    }
+    if (s < last) step(std::integral_constant<int, 0>{}, s);
+    dense_settle(acc);
+    dense_settle(big);
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[i][j] += big[i][j];
+    dense_meet<0>();
+    dense_finish<BM, BN, 2, 2, E>(g, e, 0, tm, tn, M, acc, lds);
+}
+
 // ------------------------------------------------------------------------------------------------------- plans
 
 // Kinds of tiles: sides, blocks of which a compute unit holds at most `per_unit` (by their LDS), and an estimate of their time in microseconds: `start` for each round of blocks, and for each step `one`
@@ -572,8 +721,9 @@ static const DenseKind DENSE_KIND[3][DENSE_KINDS] = {      // of one, two and th
     {{256, 256, 1, 2.1, 0, 8}, {192, 192, 1, 1.3, 0, 7}, {128, 128, 2, 0.95, 0.7, 5}, {128, 128, 1, 0.75, 0, 5}, {64, 64, 5, 0.42, 0.24, 4.5}, {64, 64, 2, 0.27, 0.17, 4}, {64, 64, 1, 0.24, 0, 5}, {32, 32, 1, 0.09, 0, 5.2}},
     {{256, 128, 1, 1.9, 0, 8}, {192, 192, 0, 0, 0, 0}, {128, 128, 1, 1.3, 0, 5}, {128, 128, 0, 0, 0, 0}, {64, 64, 3, 0.75, 0.25, 3}, {64, 64, 1, 0.42, 0, 3}, {64, 64, 0, 0, 0, 0}, {32, 32, 1, 0.25, 0, 3}}};
 
-// The kind of tile and the number of parts of the reduction that promise the shortest time; the parts' sums take at most `parts_most` bytes and a launch that joins them.
-static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matrices, bool half, size_t parts_most) {
+// The kind of tile and the number of parts of the reduction that promise the shortest time; the parts' sums take at most `parts_most` bytes and a launch that joins them; kinds other than the
+// large one need `elsewhere` us before them.
+static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matrices, bool half, size_t parts_most, double elsewhere = 0) {
     const int64_t steps = ceil_div(K < 1 ? 1 : K, dense_bk(P));
     DensePlan best{DENSE_64, 1};
     double least = 1e300;
@@ -586,10 +736,20 @@ static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matr
             const int64_t units = ceil_div(tiles * splits, 256), rounds = ceil_div(units, k.per_unit);
             double t = (double)rounds * ((double)ceil_div(steps, splits) * (k.one + k.more * (double)((rounds > 1 ? k.per_unit : units) - 1)) + k.start);
             if (splits > 1) t += 5.0 + (double)splits * M * N * matrices * 8 / 3.5e6;
+            if (kind != DENSE_LARGE) t += elsewhere;
             if (t < least) { least = t; best = DensePlan{kind, splits}; }
         }
     }
     return best;
+}
+
+template <typename E>
+static void dense_raw_launch(DenseRawArgs a, const typename E::Args& e, int splits, hipStream_t st) {
+    a.g.splits = splits;
+    a.g.matrices = 1;
+    a.g.tiles_m = (int32_t)ceil_div(a.g.M, 256);
+    a.g.tiles_n = (int32_t)ceil_div(a.g.N, 128);
+    hipLaunchKernelGGL((dense_raw_kernel<E>), dim3((unsigned)(ceil_div(dense_tiles(a.g.tiles_m, a.g.tiles_n, false), 8) * 8), (unsigned)splits), dim3(256), 0, st, a, e);
 }
 
 template <typename H, int P, bool AL, bool BL, typename E>

@@ -211,10 +211,22 @@ struct PackJob {
     int32_t cap, dim;
     char* out;              // NULL: nothing to do
     int64_t pitch;
-    int32_t plane, blocks;
+    int32_t plane, blocks;      // plane 0: up to 32 fp32 columns as they are, zeros behind them
 };
 template <typename T>
 __device__ __forceinline__ void pack_block(const PackJob& j, int32_t block) {
+    if (sizeof(T) == 4 && j.plane == 0) {
+        const int32_t n = rows_here(j.d_n, j.cap);
+        for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < (int64_t)n * 8; i += (int64_t)j.blocks * 256) {
+            const int32_t c = (int32_t)(i & 7) * 4;
+            const float* from = j.x.row<float>(i >> 3);
+            f32x4 v;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v[w] = c + w < j.dim ? from[c + w] : 0.0f;
+            *reinterpret_cast<f32x4*>(j.out + (i >> 3) * 128 + c * 4) = v;
+        }
+        return;
+    }
     const int32_t units = (j.dim + 7) / 8, n = rows_here(j.d_n, j.cap);
     for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < (int64_t)n * units; i += (int64_t)j.blocks * 256) {
         const int64_t r = i / units;
@@ -368,8 +380,8 @@ constexpr size_t LINEAR_PARTS_MOST = (size_t)128 << 20;      // bytes of parts, 
 
 struct LinearPlan { int kind, splits; };
 
-static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int P) {
-    const DensePlan p = dense_plan(M, N, K, P, 1, false, LINEAR_PARTS_MOST);
+static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int P, double elsewhere = 0) {
+    const DensePlan p = dense_plan(M, N, K, P, 1, false, LINEAR_PARTS_MOST, elsewhere);
     return LinearPlan{p.kind, p.splits};
 }
 // Parts of the reduction: blocks with 128 KB of the matrix each, but where two parts would do so for few rows, whose join costs what it saves. us by 1 / 2 / 4 / 8 / 16 parts: one bf16 row, 8192
@@ -380,6 +392,15 @@ static int linear_few_splits(int64_t K, int64_t N, int64_t rows, int es) {
     int splits = 1;
     while (splits < 32 && splits * 2 <= most && bytes > splits * (128 << 10)) splits *= 2;
     return splits == 2 && rows < 4 ? 1 : splits;
+}
+// The forward product: fp32 rows of 32 values or more, whose tile's offsets stay in 31 bits, are cut inside the large kind's product, those of other kinds by a pass before it that reads 4 and writes
+// 6 bytes a value, 8 TB/s between the caches and 5 us less than it says, which short sums do not get back (us with the pass and another kind / cut inside: 2000 x 4100 x 300 72 / 57;
+// 40001 x 64 x 250 34 / 38, 70000 x 127 x 130 54 / 70; with the pass and the same kind / cut inside: 24922 x 602 x 256 87 / 70).
+constexpr int32_t LINEAR_RAW_LEAST = 32;
+constexpr int64_t LINEAR_RAW_STRIDE = (int64_t)1 << 22;
+static LinearPlan linear_plan_fwd(int64_t M, int64_t N, int64_t K, int P) {
+    const double pass = P == 3 && K >= LINEAR_RAW_LEAST ? (double)M * K * 10 / 8e6 - 5.0 : 0.0;
+    return linear_plan(M, N, K, P, pass > 0 ? pass : 0.0);
 }
 static size_t linear_parts_bytes(const LinearPlan& p, int64_t M, int64_t N) { return p.splits > 1 ? (size_t)p.splits * M * wide_of(N) * 4 : 0; }
 
@@ -418,9 +439,8 @@ static void linear_pack(const PackJob& a, const PackJob& b, hipStream_t st) {
 }
 
 template <typename T, bool AL, bool BL>
-static bool linear_product(DenseArgs g, const LinearEnd& end, float* parts, const BiasJob& bias, hipStream_t st) {
+static bool linear_product(DenseArgs g, const LinearPlan& p, const LinearEnd& end, float* parts, const BiasJob& bias, hipStream_t st) {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;
-    const LinearPlan p = linear_plan(g.M, g.N, g.K, P);
     const typename LinearOut<T>::Args e{p.splits > 1 ? LinearEnd{} : end, p.splits > 1 ? parts : nullptr, (int32_t)wide_of(g.N)};
     dense_launch<__bf16, P, AL, BL, LinearOut<T>>(g, e, DensePlan{p.kind, p.splits}, 1, st);
     if (p.splits > 1) linear_join<T>(parts, p.splits, g.M, g.d_M, g.N, end, bias, st);
@@ -447,14 +467,31 @@ static void linear_fwd(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int3
     }
     DenseArgs g{};
     PackJob jx, jw;
+    g.M = cap; g.N = d_out; g.K = d_in;
+    g.d_M = d_n;
+    const LinearPlan plan = linear_plan_fwd(cap, d_out, d_in, planes_of_type(TypeOf<T>::code));
+    if constexpr (sizeof(T) == 4) {
+        if (plan.kind == DENSE_LARGE && d_in >= LINEAR_RAW_LEAST && x.stride <= LINEAR_RAW_STRIDE) {        // rows are read where they are, but for the columns that fill no step
+            const int32_t rest = d_in % 32;
+            const int64_t blocks = rest ? ceil_div((int64_t)cap * 8, 256) : 0;
+            char* tail = room.take((size_t)cap * 128);
+            jx = PackJob{RowsOf{x.p + (int64_t)(d_in - rest) * 4, x.stride}, d_n, cap, rest, tail, 128, 0, (int32_t)(blocks < 2048 ? blocks : 2048)};
+            g.a = DenseOperand{x.p, x.stride, 0, 0, cap};
+            g.b = linear_operand<T>(w, nullptr, d_in, d_out, room, jw);
+            g.b.extent = (int32_t)wide_of(d_out);
+            linear_pack<T>(jx, jw, st);
+            float* parts = plan.splits > 1 ? (float*)room.p : nullptr;
+            dense_raw_launch<LinearOut<T>>(DenseRawArgs{g, DenseOperand{tail, 128, 0, 0, cap}}, typename LinearOut<T>::Args{parts ? LinearEnd{} : end, parts, (int32_t)wide_of(d_out)}, plan.splits, st);
+            if (parts) linear_join<T>(parts, plan.splits, cap, d_n, d_out, end, BiasJob{}, st);
+            return;
+        }
+    }
     g.a = linear_operand<T>(x, d_n, cap, d_in, room, jx);
     g.b = linear_operand<T>(w, nullptr, d_in, d_out, room, jw);
     linear_pack<T>(jx, jw, st);
     g.a.extent = cap;
     g.b.extent = (int32_t)wide_of(d_out);
-    g.M = cap; g.N = d_out; g.K = d_in;
-    g.d_M = d_n;
-    linear_product<T, true, false>(g, end, (float*)room.p, BiasJob{}, st);
+    linear_product<T, true, false>(g, plan, end, (float*)room.p, BiasJob{}, st);
 }
 
 template <typename T>
@@ -498,7 +535,7 @@ static void linear_bwd(RowsOf x, RowsOf w, int32_t act, RowsOf z, RowsOf grad_y,
         g.b.extent = d_in;
         g.M = cap; g.N = d_in; g.K = d_out;
         g.d_M = d_n;
-        joined(linear_product<T, true, true>(g, LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_x, NO_ACT_NONE}, (float*)room.p, bias, st));
+        joined(linear_product<T, true, true>(g, linear_plan(g.M, g.N, g.K, planes_of_type(TypeOf<T>::code)), LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_x, NO_ACT_NONE}, (float*)room.p, bias, st));
     }
     if (grad_w.p) {
         DenseArgs g{};
@@ -507,7 +544,7 @@ static void linear_bwd(RowsOf x, RowsOf w, int32_t act, RowsOf z, RowsOf grad_y,
         g.b.extent = (int32_t)wide_of(d_out);
         g.M = d_in; g.N = d_out; g.K = cap;
         g.d_K = d_n;
-        joined(linear_product<T, false, false>(g, LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_w, NO_ACT_NONE}, (float*)room.p, bias, st));
+        joined(linear_product<T, false, false>(g, linear_plan(g.M, g.N, g.K, planes_of_type(TypeOf<T>::code)), LinearEnd{nullptr, {nullptr, 0}, {nullptr, 0}, grad_w, NO_ACT_NONE}, (float*)room.p, bias, st));
     }
     if (bias.grad_bias) hipLaunchKernelGGL(linear_bias_kernel, dim3((unsigned)ceil_div(d_out, 16)), dim3(256), 0, st, bias);
 }
@@ -529,7 +566,7 @@ extern "C" size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_
     if ((dt != NO_F32 && dt != NO_BF16) || n_rows_cap < 0 || d_in < 1 || d_out < 1 || d_in > NO_MAX_LINEAR_DIM || d_out > NO_MAX_LINEAR_DIM || n_rows_cap > NO_MAX_LINEAR_ROWS) return 0;
     const int pieces = planes_of_type(dt);
     const int64_t n = n_rows_cap;
-    size_t parts = linear_parts_bytes(linear_plan(n, d_out, d_in, pieces), n, d_out);
+    size_t parts = linear_parts_bytes(linear_plan_fwd(n, d_out, d_in, pieces), n, d_out);
     const size_t px = linear_parts_bytes(linear_plan(n, d_in, d_out, pieces), n, d_in), pw = linear_parts_bytes(linear_plan(d_in, d_out, n, pieces), d_in, d_out);
     if (px > parts) parts = px;
     if (pw > parts) parts = pw;

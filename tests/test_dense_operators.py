@@ -333,6 +333,48 @@ def test_linear_counts(n, d_in, d_out, dt):
     assert (gw == 0).all() and (gb == 0).all()
 
 
+@pytest.mark.parametrize("n,d_in,d_out,pad,off", [(40_000, 602, 256, 0, 0), (40_001, 64, 250, 0, 0), (38_000, 67, 258, 1, 1), (70_000, 127, 130, 3, 0), (12_345, 1030, 1000, 2, 3), (20_000, 96, 512, 4, 4), (2000, 4100, 300, 0, 1),
+                                                      (8192, 33, 1024, 0, 0), (9000, 32, 1024, 1, 0)])
+def test_linear_rows_cut_inside_the_product(n, d_in, d_out, pad, off):
+    """fp32 rows of a large product are read where they are, in whole steps of 32 and a rest: rows that are aligned to 4 bytes alone, a count, NaN behind it and in two rows."""
+    b, g = nb(), rng(n)
+    x = Rows(n, d_in, F32, pad, off, randn((n, d_in), g))
+    w, bias, r = randn((d_in, d_out), g, F32, d_in ** -0.5), randn((d_out,), g), randn((n, d_out), g)
+    ws = ws_of(b.no_linear_ws_bytes(F32, n, d_in, d_out))
+    y = Rows(n, d_out, F32, pad, off)
+    b.no_linear_fwd(x.t, w, bias, b.NO_ACT_NONE, y.t, ws, residual=r)
+    ref, tol = product(x.t, w)
+    ref = ref + bias.double() + r.double()
+    close(y.t, ref, tol + 3 * U * (ref.abs() + bias.double().abs() + r.double().abs()) + TINY, "y")
+    near(y.t, ref, d_in, F32, "y")
+    assert y.untouched()
+    whole, real = y.t.clone(), n - 777
+    x.t[real:], x.t[3, 0], x.t[700, d_in - 1], x.t[900, d_in // 2] = NAN, NAN, NAN, INF
+    ws.fill_(0xFF)                          # (NaN wherever a word of it is read unwritten)
+    out = Rows(n, d_out, F32, pad, off)
+    b.no_linear_fwd(x.t, w, bias, b.NO_ACT_NONE, out.t, ws, residual=r, n_rows=count(real))
+    assert out.untouched(rows=real)
+    assert out.t[3].isnan().all() and out.t[700].isnan().all() and not out.t[900].isfinite().any()
+    fine = torch.ones(real, dtype=torch.bool, device="cuda")
+    fine[[3, 700, 900]] = False
+    assert torch.equal(out.t[:real][fine], whole[:real][fine])
+
+
+@pytest.mark.parametrize("n,d_in,d_out", [(3000, 1000, 2900), (2900, 3000, 392), (1100, 700, 1100), (130, 300, 9000)])
+@BOTH
+def test_linear_of_middling_sizes(n, d_in, d_out, dt):
+    b, g = nb(), rng(n)
+    x, w, gy = randn((n, d_in), g, dt), randn((d_in, d_out), g, dt, d_in ** -0.5), randn((n, d_out), g, dt)
+    r, y = randn((n, d_out), g, dt), torch.empty((n, d_out), device="cuda", dtype=dt)
+    ws = ws_of(b.no_linear_ws_bytes(dt, n, d_in, d_out))
+    b.no_linear_fwd(x, w, None, b.NO_ACT_NONE, y, ws, residual=r)
+    near(y, x.double() @ w.double() + r.double(), d_in, dt, "y")
+    gx, gw = torch.empty_like(x), torch.empty_like(w)
+    b.no_linear_bwd(x, w, b.NO_ACT_NONE, None, gy, gx, gw, None, ws)
+    near(gx, gy.double() @ w.double().t().contiguous(), d_out, dt, "grad_x")
+    near(gw, x.double().t().contiguous() @ gy.double(), n, dt, "grad_w")
+
+
 def test_linear_pieces_keep_what_fp32_holds():
     """Values of very different size in one sum, which meet only their like: each column of x is 2^-k w's row. And small values, and rows of zeros."""
     b, g = nb(), rng(3)
@@ -448,6 +490,23 @@ def test_orthogonalise(n, rows, cols, dt):
     one = torch.empty((rows, cols), device="cuda")
     b.no_orthogonalise(x[n - 1], one, ws_of(b.no_orthogonalise_ws_bytes(1, rows, cols)))
     assert apart(one, wide[n - 1].double()) <= 2 * tol
+
+
+@pytest.mark.parametrize("n,rows,cols", [(1, 117, 3860), (1, 3860, 117), (4, 96, 2500), (2, 3001, 260)])
+@BOTH
+def test_orthogonalise_long_and_narrow(n, rows, cols, dt):
+    """Gram matrices whose long reduction is split."""
+    b, g = nb(), rng(rows + cols)
+    x = randn((n, rows, cols), g, dt, 0.01)
+    ws, out, again = ws_of(b.no_orthogonalise_ws_bytes(n, rows, cols)), torch.empty((n, rows, cols), device="cuda"), torch.empty((n, rows, cols), device="cuda")
+    for steps in (1, 5):
+        b.no_orthogonalise(x, out, ws, steps=steps)
+        ref = steps_ref(x.double(), steps)
+        tol = one_step_tol(max(rows, cols)) if steps == 1 else max(2 * apart(steps_ref(x.float(), steps), ref), 8 * 2.0 ** -22)
+        assert apart(out, ref) <= tol, (steps, apart(out, ref), tol)
+        ws.fill_(0xFF)
+        b.no_orthogonalise(x, again, ws, steps=steps)
+        assert torch.equal(out, again)
 
 
 @BOTH
