@@ -38,7 +38,8 @@ constexpr uint32_t DENSE_NOWHERE = 0x80000000u;      // past every buffer's rang
 // One operand's tile of R rows (or columns) and a step's slabs in LDS, loaded by T threads in requests of 16 bytes that go straight to LDS. A request's 64 lanes fill 1 KB in lane
 // order, so the order of the units in LDS is made by which unit a lane asks for: ALONG, unit u of row r stands at place u ^ (r & 7) of its 128 bytes (three pieces: at
 // u ^ (r >> 2 & 3) of its 192); across, the 32 bytes of 16 columns of line k stand at place c ^ f(k), f(k) = (k & 3) | (k >> 3 & 1) << 2 (192 columns, whose lines begin half of the banks apart: (k >> 1 & 1) |
-// (k >> 3 & 1) << 1). Then the 64 lanes of a fragment's read meet every bank equally often (SQ_LDS_BANK_CONFLICT 0).
+// (k >> 3 & 1) << 1). Then the 64 lanes of a fragment's read meet every bank equally often
+// (SQ_LDS_BANK_CONFLICT 0 with one piece; with more, where requests and reads meet, up to 6 % of the cycles in the large tiles, 17 % in two pieces of 128 x 128).
 template <int P, bool ALONG, int R, int T>
 struct DenseTile {
     static constexpr int SLABS = dense_slabs(P), BK = dense_bk(P), PER_ROW = ALONG ? SLABS * 4 : R / 8, BYTES = R * SLABS * 64, REQ = BYTES / (16 * T);
@@ -394,6 +395,8 @@ __global__ void __launch_bounds__(64 * WM * WN * GROUPS) dense_kernel(const Dens
 // The same for large products: a tile of 256 x 256 (192 x 192 where that fills the chip better; three pieces: 256 x 128) by four wavefronts of a quarter each, one a SIMD, whose sums fill the accumulation registers; the others hold one set of
 // fragments a slab, and a set is read again when the products that want it are done. A copy of LDS is free when its last fragments are in registers: the step after next is requested right then, and
 // has a whole step's time to arrive. LDS is read 16 bytes for 8192 multiplications (by eight wavefronts of 128 x 64: 24 bytes, which takes LDS as long as the products).
+// Bound by the matrix pipes at the clock that the power limit leaves: bf16 16384 x 8192 x 2048 439 us (1.25 PFLOP/s), both products of 8192 x 2048 x 8192's gradients 195 to 200 (1.4 when the card is cold);
+// two pieces, 4096^3 300 (1.37 PFLOP/s of pieces), its symmetric half 190 by 192 x 192.
 template <typename H, int P, bool AL, bool BL, int BM, int BN, typename E>
 __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, const typename E::Args e) {
     constexpr int T = 256, I = BM / 32, J = BN / 32, S = dense_slabs(P), N = I * J, EACH = N / (I + J);      // (a read for EACH products)

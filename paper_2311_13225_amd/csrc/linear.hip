@@ -247,6 +247,8 @@ __global__ void __launch_bounds__(256) linear_pack_kernel(PackJob a, PackJob b) 
 // The gradient of the pre-activation, gz = grad_y act'(z), laid out as an operand (gz NULL: grad_y is one as it stands), and its column sums over `per` rows a block: LANES threads along a
 // row, each with eight columns, and 256 / LANES rows at a time, whose sums are added in order; four of a thread's rows are requested at once.
 // The launch's other blocks lay out the rows of x and the matrix for the products behind it.
+// Of bf16 values gz is rounded to bf16 (a smooth slope's product by 2^-8 of it at most, relu's and none's not at all): the products then take 16-bit operands, at six times the rate of pieces, and the gradients' error over all
+// is 0.0023 where their own rounding leaves 0.0017. The column sums take it unrounded. Bound by memory: 8192 x 8192 bf16 gelu 75 us (403 MB, 5.4 TB/s).
 template <typename T, int ACT, int LANES>
 __global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z, const int32_t* d_n, int32_t cap, int32_t dim, int32_t per, int32_t wide, int32_t blocks, char* gz,
                                                         int64_t pitch, int32_t plane, float* parts, PackJob a, PackJob b) {
