@@ -158,7 +158,7 @@ __device__ __forceinline__ bool dense_place(const DenseArgs& g, int& matrix, int
 // is stored as C[n, m], too.
 template <int BM, int BN, int WM, int WN>
 struct DenseFinish {
-    static constexpr int T = 64 * WM * WN, COLS = BN / WN, PITCH = COLS + 4, LANES = COLS == 96 ? 16 : COLS / 8, ROWS = BM / WM < 32 ? BM / WM : 32, PASS = 64 / LANES, TURNS = ROWS / PASS, AHEAD = 32;
+    static constexpr int T = 64 * WM * WN, COLS = BN / WN, PITCH = COLS + 4, LANES = COLS == 96 ? 16 : COLS / 8, ROWS = BM / WM % 32 == 0 ? 32 : 16, PASS = 64 / LANES, TURNS = ROWS / PASS, AHEAD = 32;
     static constexpr int SUMS = WM * WN * ROWS * PITCH * 4, BYTES = SUMS + (TURNS > 2 ? T * TURNS * AHEAD : 0);
     static_assert(ROWS % PASS == 0, "whole passes");
 };
@@ -568,9 +568,9 @@ struct DenseRawArgs {
     DenseArgs g;            // g.a: the rows (pitch of 4-byte multiples); g.a.plane is not used
     DenseOperand tail;
 };
-template <typename E>
+template <int BM, typename E>
 __global__ void __launch_bounds__(256, 1) dense_raw_kernel(const DenseRawArgs ga, const typename E::Args e) {
-    constexpr int BM = 256, BN = 128, T = 256, I = 8, J = 4, PRODUCTS = 6 * J;
+    constexpr int BN = 128, T = 256, I = BM / 32, J = 4, PRODUCTS = 6 * J;
     typedef DenseTile<1, true, BM, T> TA;       // (32 values of 4 bytes take the place of 64 of 2)
     typedef DenseTile<3, false, BN, T> TB;
     constexpr int BK = 32, COPY = TA::BYTES + TB::BYTES, REQ = TA::REQ + TB::REQ;
@@ -622,14 +622,15 @@ __global__ void __launch_bounds__(256, 1) dense_raw_kernel(const DenseRawArgs ga
     i32x4 piece[2][3];              // this fragment's pieces and the next one's, pairs of values
     uint32_t r0, r1;                // what is left of the pair that is cut
     auto take_b = [&](int n, int half, int copy) { fb[half][n / J][n % J] = TB::fragment(lds + copy * COPY + TA::BYTES, wn * J + n % J, n / J); };
-    auto take_raw = [&](int i, int copy) {
+    // (fragments alternate from step to step, too: `turn` is a fragment's number in two steps)
+    auto take_raw = [&](int turn, int i, int copy) {
         const char* row = lds + copy * COPY + ((wm * I + i) * 16 + j16) * 128;
-        raw[i & 1][0] = *reinterpret_cast<const i32x4*>(row + ((2 * gr) ^ (j16 & 7)) * 16);
-        raw[i & 1][1] = *reinterpret_cast<const i32x4*>(row + ((2 * gr + 1) ^ (j16 & 7)) * 16);
+        raw[turn & 1][0] = *reinterpret_cast<const i32x4*>(row + ((2 * gr) ^ (j16 & 7)) * 16);
+        raw[turn & 1][1] = *reinterpret_cast<const i32x4*>(row + ((2 * gr + 1) ^ (j16 & 7)) * 16);
     };
-    // part n of 24 of cutting fragment i's values, x = h + m + l: six a pair
-    auto cut = [&](int n, int i) {
-        const int pair = n / 6, at = i & 1;
+    // part n of 24 of cutting a fragment's values, x = h + m + l: six a pair
+    auto cut = [&](int n, int turn) {
+        const int pair = n / 6, at = turn & 1;
         i32x4(&p)[3] = piece[at];
         auto round = [&](int which) {
             typedef float f2 __attribute__((ext_vector_type(2)));
@@ -649,9 +650,9 @@ __global__ void __launch_bounds__(256, 1) dense_raw_kernel(const DenseRawArgs ga
         if (n % 6 == 5) round(2);
     };
     constexpr int PA[6] = {0, 0, 0, 1, 1, 2}, PB[6] = {2, 0, 1, 1, 0, 0};      // (what was cut last is wanted last)
-    auto one = [&](int n, int i, int half) {
+    auto one = [&](int n, int turn, int i, int half) {
         const int pair = n / J, j = n % J;
-        const s16x8 a = __builtin_bit_cast(s16x8, piece[i & 1][PA[pair]]);
+        const s16x8 a = __builtin_bit_cast(s16x8, piece[turn & 1][PA[pair]]);
         if (pair == 1) dense_mfma_in_place<__bf16>(big[i][j], fb[half][PB[pair]][j], a);
         else dense_mfma_in_place<__bf16>(acc[i][j], fb[half][PB[pair]][j], a);
         __builtin_amdgcn_sched_barrier(0);
@@ -665,14 +666,15 @@ __global__ void __launch_bounds__(256, 1) dense_raw_kernel(const DenseRawArgs ga
     dense_meet<REQ>();
 #pragma unroll
     for (int n = 0; n < 3 * J; ++n) take_b(n, 0, 0);
-    take_raw(0, 0);
-    take_raw(1, 0);
+    take_raw(0, 0, 0);
+    take_raw(1, 1, 0);
 #pragma unroll
     for (int n = 0; n < 24; ++n) cut(n, 0);
     auto step = [&](auto copy_of, int32_t s) {
         constexpr int now = decltype(copy_of)::value;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
+            const int turn = now * I + i;
             if (i == I - 2) {           // the last fragment of this copy is in registers
                 aim(s + 2);
                 dense_meet<0>();
@@ -680,16 +682,16 @@ __global__ void __launch_bounds__(256, 1) dense_raw_kernel(const DenseRawArgs ga
 #pragma unroll
             for (int n = 0; n < PRODUCTS; ++n) {
                 if (n == 0) {               // the fragment after the next one, into the place of the one that has been cut
-                    if (i < I - 2) take_raw(i + 2, now);
-                    else take_raw(i + 2 - I, now ^ 1);
+                    if (i < I - 2) take_raw(turn + 2, i + 2, now);
+                    else take_raw(turn + 2, i + 2 - I, now ^ 1);
                 }
-                cut(n, (i + 1) % I);
+                cut(n, turn + 1);
                 if (i >= I - 2) {
                     const int k = (i - (I - 2)) * PRODUCTS + n;
                     if (k % 4 == 0 && k / 4 < 3 * J) take_b(k / 4, now ^ 1, now ^ 1);
                     if (k % 3 == 1 && k / 3 < REQ) request(k / 3, now);
                 }
-                one(n, i, now);
+                one(n, turn, i, now);
             }
         }
     };
@@ -724,6 +726,8 @@ static const DenseKind DENSE_KIND[3][DENSE_KINDS] = {      // of one, two and th
     {{256, 256, 1, 2.1, 0, 8}, {192, 192, 1, 1.3, 0, 7}, {128, 128, 2, 0.95, 0.7, 5}, {128, 128, 1, 0.75, 0, 5}, {64, 64, 5, 0.42, 0.24, 4.5}, {64, 64, 2, 0.27, 0.17, 4}, {64, 64, 1, 0.24, 0, 5}, {32, 32, 1, 0.09, 0, 5.2}},
     {{256, 128, 1, 1.9, 0, 8}, {192, 192, 0, 0, 0, 0}, {128, 128, 1, 1.3, 0, 5}, {128, 128, 0, 0, 0, 0}, {64, 64, 3, 0.75, 0.25, 3}, {64, 64, 1, 0.42, 0, 3}, {64, 64, 0, 0, 0, 0}, {32, 32, 1, 0.25, 0, 3}}};
 
+constexpr int64_t DENSE_TILES_MOST = (1 << 23) - 8;      // a launch's threads, 512 a tile at most, stay below 2^32; the large kind's stay so whatever memory holds
+
 // The kind of tile and the number of parts of the reduction that promise the shortest time; the parts' sums take at most `parts_most` bytes and a launch that joins them; kinds other than the
 // large one need `elsewhere` us before them.
 static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matrices, bool half, size_t parts_most, double elsewhere = 0) {
@@ -734,6 +738,7 @@ static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matr
         const DenseKind& k = DENSE_KIND[P - 1][kind];
         if (k.per_unit == 0) continue;
         const int64_t a = ceil_div(M < 1 ? 1 : M, k.bm), b = ceil_div(N, k.bn), tiles = (half ? a * (a + 1) / 2 : a * b) * matrices;
+        if (kind != DENSE_LARGE && tiles > DENSE_TILES_MOST) continue;
         for (int splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 2) {
             if (splits > 1 && (steps < splits * 4 || (size_t)splits * M * wide_of(N) * matrices * 4 > parts_most)) break;
             const int64_t units = ceil_div(tiles * splits, 256), rounds = ceil_div(units, k.per_unit);
@@ -746,13 +751,18 @@ static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matr
     return best;
 }
 
+// Tiles of 224 rows where they need fewer rows' time in all (24922 x 602 x 256: 224 blocks of 256 units instead of 196, XX us for 64).
 template <typename E>
 static void dense_raw_launch(DenseRawArgs a, const typename E::Args& e, int splits, hipStream_t st) {
     a.g.splits = splits;
     a.g.matrices = 1;
-    a.g.tiles_m = (int32_t)ceil_div(a.g.M, 256);
     a.g.tiles_n = (int32_t)ceil_div(a.g.N, 128);
-    hipLaunchKernelGGL((dense_raw_kernel<E>), dim3((unsigned)(ceil_div(dense_tiles(a.g.tiles_m, a.g.tiles_n, false), 8) * 8), (unsigned)splits), dim3(256), 0, st, a, e);
+    auto rounds = [&](int64_t rows) { return ceil_div(ceil_div(a.g.M, rows) * a.g.tiles_n * splits, 256); };
+    const bool low = rounds(224) * 224 < rounds(256) * 256;
+    a.g.tiles_m = (int32_t)ceil_div(a.g.M, low ? 224 : 256);
+    const dim3 grid((unsigned)(ceil_div(dense_tiles(a.g.tiles_m, a.g.tiles_n, false), 8) * 8), (unsigned)splits);
+    if (low) hipLaunchKernelGGL((dense_raw_kernel<224, E>), grid, dim3(256), 0, st, a, e);
+    else hipLaunchKernelGGL((dense_raw_kernel<256, E>), grid, dim3(256), 0, st, a, e);
 }
 
 template <typename H, int P, bool AL, bool BL, typename E>

@@ -375,6 +375,19 @@ def test_linear_of_middling_sizes(n, d_in, d_out, dt):
     near(gw, x.double().t().contiguous() @ gy.double(), n, dt, "grad_w")
 
 
+def test_linear_rows_whose_small_tiles_no_launch_holds():
+    """1.2 billion rows of one value: 18.75 million tiles of 64 rows, whose threads would pass 2^32."""
+    b, g, n, here = nb(), rng(1), 1_200_000_000, 1000
+    x, y = torch.empty((n, 1), device="cuda", dtype=BF16), torch.empty((n, 1), device="cuda", dtype=BF16)
+    x[:here], w = randn((here, 1), g, BF16), randn((1, 1), g, BF16)
+    y[:here + 1] = MARK
+    ws = torch.empty((b.no_linear_ws_bytes(BF16, n, 1, 1),), device="cuda", dtype=torch.uint8)
+    b.no_linear_fwd(x, w, None, b.NO_ACT_NONE, y, ws, n_rows=count(here))
+    ref = x[:here].double() * w.double()
+    close(y[:here], ref, half(BF16) * ref.abs() + TINY)
+    assert (y[here:here + 1] == MARK).all()
+
+
 def test_linear_pieces_keep_what_fp32_holds():
     """Values of very different size in one sum, which meet only their like: each column of x is 2^-k w's row. And small values, and rows of zeros."""
     b, g = nb(), rng(3)

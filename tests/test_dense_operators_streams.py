@@ -55,7 +55,8 @@ def muon(n, r, c, dt):
 ROUTES = [(layernorm, 700, 2049, BF16), (layernorm, 300, 100, F32), (layernorm, 70, 20_000, F32),
           (linear, 1, 512, 2048, BF16), (linear, 5, 300, 1001, F32), (linear, 33, 2048, 72, BF16), (linear, 1000, 256, 300, F32), (linear, 300, 1027, 129, BF16),
           (linear, 4100, 512, 2048, BF16), (linear, 9000, 100, 47, F32), (linear, 3000, 1000, 2000, F32),
-          (orthogonalise, 2, 300, 100, F32), (orthogonalise, 1, 1500, 1600, BF16), (muon, 2, 256, 602, BF16), (muon, 1, 2100, 2050, F32)]
+          (orthogonalise, 2, 300, 100, F32), (orthogonalise, 1, 1500, 1600, BF16), (muon, 2, 256, 602, BF16), (muon, 1, 2100, 2050, F32),
+          (layernorm, 200, 16_384, BF16), (linear, 25_000, 602, 256, F32), (linear, 2000, 4100, 300, F32), (orthogonalise, 1, 117, 3860, F32)]
 
 
 @pytest.mark.parametrize("route", ROUTES, ids=lambda r: "-".join(getattr(x, "__name__", str(x)) for x in r))
