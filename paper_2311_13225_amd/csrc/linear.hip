@@ -396,8 +396,8 @@ static int linear_few_splits(int64_t K, int64_t N, int64_t rows, int es) {
     return splits == 2 && rows < 4 ? 1 : splits;
 }
 // The forward product: fp32 rows of 32 values or more, whose tile's offsets stay in 31 bits, are cut inside the large kind's product, those of other kinds by a pass before it that reads 4 and writes
-// 6 bytes a value, 8 TB/s between the caches and 5 us less than it says, which short sums do not get back (us with the pass and another kind / cut inside: 2000 x 4100 x 300 72 / 57;
-// 40001 x 64 x 250 34 / 38, 70000 x 127 x 130 54 / 70; with the pass and the same kind / cut inside: 24922 x 602 x 256 87 / 70).
+// 6 bytes a value, 8 TB/s between the caches and 5 us less than it says, which short sums do not get back (us with the pass and another kind / cut inside: 2000 x 4100 x 300 72 / 56;
+// 40001 x 64 x 250 34 / 38, 70000 x 127 x 130 54 / 70; with the pass and the same kind / cut inside: 24922 x 602 x 256 87 / 63).
 constexpr int32_t LINEAR_RAW_LEAST = 32;
 constexpr int64_t LINEAR_RAW_STRIDE = (int64_t)1 << 22;
 static LinearPlan linear_plan_fwd(int64_t M, int64_t N, int64_t K, int P) {

@@ -375,6 +375,16 @@ def test_linear_of_middling_sizes(n, d_in, d_out, dt):
     near(gw, x.double().t().contiguous() @ gy.double(), n, dt, "grad_w")
 
 
+@pytest.mark.parametrize("n", [9, 500, 60_000])
+def test_linear_by_the_identity_gives_the_rows(n):
+    """The pieces' sum is the value, to the last bit, whichever kernel cuts them."""
+    b, g = nb(), rng(n)
+    x = randn((n, 250), g) * torch.pow(2.0, torch.randint(-60, 60, (n, 250), generator=g, device="cuda").float())
+    y = torch.empty_like(x)
+    b.no_linear_fwd(x, torch.eye(250, device="cuda"), None, b.NO_ACT_NONE, y, ws_of(b.no_linear_ws_bytes(F32, n, 250, 250)))
+    assert torch.equal(y, x)
+
+
 def test_linear_rows_whose_small_tiles_no_launch_holds():
     """1.2 billion rows of one value: 18.75 million tiles of 64 rows, whose threads would pass 2^32."""
     b, g, n, here = nb(), rng(1), 1_200_000_000, 1000
