@@ -650,7 +650,8 @@ __global__ void __launch_bounds__(256, 1) dense_raw_kernel(const DenseRawArgs ga
         if (n % 6 == 4) left(r1, (uint32_t)p[1][pair] & 0xffff0000u);
         if (n % 6 == 5) round(2);
     };
-    constexpr int PA[6] = {0, 0, 0, 1, 1, 2}, PB[6] = {2, 0, 1, 1, 0, 0};      // (what was cut last is wanted last)
+    // (what was cut last is wanted last: a piece is written five products or more before the first that reads it, which a product needs to be two instructions)
+    constexpr int PA[6] = {0, 0, 0, 1, 1, 2}, PB[6] = {2, 0, 1, 1, 0, 0};
     auto one = [&](int n, int turn, int i, int half) {
         const int pair = n / J, j = n % J;
         const s16x8 a = __builtin_bit_cast(s16x8, piece[turn & 1][PA[pair]]);
