@@ -66,14 +66,17 @@ struct DenseTile {
         step = ALONG ? BK * 2 : BK * o.pitch;
     }
     // Request i alone, by hand: the compiler takes a request for a write of LDS that every later read of LDS has to wait for, and cannot know that the two go to different copies. What it
-    // fills is waited for in dense_meet(). Nothing is masked here: cut() comes before the first step that is not whole.
+    // fills is waited for in dense_meet(). Nothing is masked here: cut() comes before the first step that is not whole. A load into LDS takes its place from m0, one wait state after a scalar instruction wrote that.
     __device__ __forceinline__ i32x4 source(int32_t s) const {
         const uint64_t at = (uint64_t)(base + (int64_t)s * step);
         return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), 0x7fffffff, 0x00020000};
     }
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"      /* (it warns of m0, which the compiler keeps no value in) */
     __device__ __forceinline__ void request_one(int i, i32x4 rsrc, uint32_t to) const {
-        asm volatile("s_add_u32 m0, %2, %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(off[i]), "s"(rsrc), "s"(to), "i"(i * T * 16) : "memory", "scc");
+        asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(off[i]), "s"(rsrc), "s"(to), "i"(i * T * 16) : "memory", "scc", "m0");
     }
+#pragma clang diagnostic pop
     // From here on only the first `left` reduction indices of a step are asked for.
     __device__ __forceinline__ void cut(int32_t left) {
 #pragma unroll
