@@ -415,7 +415,7 @@ typedef enum { NO_ACT_NONE = 0, NO_ACT_RELU = 1, NO_ACT_GELU = 2, NO_ACT_SILU = 
  * the call reads, but d_y may be d_residual itself (same address and stride). bf16 operands are multiplied as they are and summed in fp32. fp32 operands are multiplied in three bf16 pieces
  * each (the six largest of nine products, summed in fp32), no less exact than in fp32; there an operand that is infinite, NaN or above 3.38e38 makes the sums that it meets infinite or NaN, and one below 2^-110 is taken
  * with fewer digits. Up to 8 rows are multiplied in fp32.
- * One workspace size holds for the forward and the backward call. */
+ * One workspace size holds for the forward and the backward call, and for all calls whose sizes are no larger: no_linear_ws_bytes grows with each of them. */
 size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_in, int32_t d_out);
 int32_t no_linear_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_w, int64_t w_stride_bytes, const float* d_bias, no_act act,
                       const void* d_residual, int64_t residual_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t d_in, int32_t d_out,

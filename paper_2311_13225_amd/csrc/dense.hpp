@@ -733,10 +733,27 @@ static const DenseKind DENSE_KIND[3][DENSE_KINDS] = {      // of one, two and th
 
 constexpr int64_t DENSE_TILES_MOST = (1 << 23) - 8;      // a launch's threads, 512 a tile at most, stay below 2^32; the large kind's stay so whatever memory holds
 
+// Numbers of parts of a reduction: 1, 2, 3, 4, 8, ... 64, four steps or more in each.
+constexpr int DENSE_PARTS = 64;
+static inline int dense_more_parts(int splits) { return splits < 4 ? splits + 1 : splits * 2; }
+static inline int64_t dense_steps(int64_t K, int P) { return ceil_div(K < 1 ? 1 : K, dense_bk(P)); }
+static inline bool dense_parts_fit(int64_t steps, int splits) { return splits == 1 || steps >= splits * 4; }
+static inline size_t dense_parts_bytes(int64_t splits, int64_t M, int64_t N, int64_t matrices) { return splits > 1 ? (size_t)splits * M * wide_of(N) * matrices * 4 : 0; }
+
+// Room for the parts of any plan for a product of these or of smaller sizes. (A plan's own parts do not grow with the sizes: 2276 rows of 2048 x 8192 bf16 are split in three, 2504 are not. A program makes one
+// workspace for its largest batch.)
+static size_t dense_parts_room(int64_t M, int64_t N, int64_t K, int P, int64_t matrices, size_t parts_most) {
+    const int64_t steps = dense_steps(K, P);
+    int most = 1;
+    while (most < DENSE_PARTS && dense_parts_fit(steps, dense_more_parts(most))) most = dense_more_parts(most);
+    const size_t all = dense_parts_bytes(most, M, N, matrices);
+    return all < parts_most ? all : parts_most;
+}
+
 // The kind of tile and the number of parts of the reduction that promise the shortest time; the parts' sums take at most `parts_most` bytes and a launch that joins them; kinds other than the
 // large one need `elsewhere` us before them.
 static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matrices, bool half, size_t parts_most, double elsewhere = 0) {
-    const int64_t steps = ceil_div(K < 1 ? 1 : K, dense_bk(P));
+    const int64_t steps = dense_steps(K, P);
     DensePlan best{DENSE_64, 1};
     double least = 1e300;
     for (int kind = 0; kind < DENSE_KINDS; ++kind) {
@@ -744,8 +761,8 @@ static DensePlan dense_plan(int64_t M, int64_t N, int64_t K, int P, int64_t matr
         if (k.per_unit == 0) continue;
         const int64_t a = ceil_div(M < 1 ? 1 : M, k.bm), b = ceil_div(N, k.bn), tiles = (half ? a * (a + 1) / 2 : a * b) * matrices;
         if (kind != DENSE_LARGE && tiles > DENSE_TILES_MOST) continue;
-        for (int splits = 1; splits <= 64; splits = splits < 4 ? splits + 1 : splits * 2) {
-            if (splits > 1 && (steps < splits * 4 || (size_t)splits * M * wide_of(N) * matrices * 4 > parts_most)) break;
+        for (int splits = 1; splits <= DENSE_PARTS; splits = dense_more_parts(splits)) {
+            if (!dense_parts_fit(steps, splits) || dense_parts_bytes(splits, M, N, matrices) > parts_most) break;
             const int64_t units = ceil_div(tiles * splits, 256), rounds = ceil_div(units, k.per_unit);
             double t = (double)rounds * ((double)ceil_div(steps, splits) * (k.one + k.more * (double)((rounds > 1 ? k.per_unit : units) - 1)) + k.start);
             if (splits > 1) t += 5.0 + (double)splits * M * N * matrices * 8 / 3.5e6;

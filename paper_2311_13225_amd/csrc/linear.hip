@@ -404,7 +404,7 @@ static LinearPlan linear_plan_fwd(int64_t M, int64_t N, int64_t K, int P) {
     const double pass = P == 3 && K >= LINEAR_RAW_LEAST ? (double)M * K * 10 / 8e6 - 5.0 : 0.0;
     return linear_plan(M, N, K, P, pass > 0 ? pass : 0.0);
 }
-static size_t linear_parts_bytes(const LinearPlan& p, int64_t M, int64_t N) { return p.splits > 1 ? (size_t)p.splits * M * wide_of(N) * 4 : 0; }
+static size_t linear_parts_room(int64_t M, int64_t N, int64_t K, int P) { return dense_parts_room(M, N, K, P, 1, LINEAR_PARTS_MOST); }
 
 static inline int planes_of_type(no_dtype dt) { return dt == NO_F32 ? 3 : 1; }
 static inline size_t operand_bytes(no_dtype dt, int64_t rows, int64_t dim) { return round_256((size_t)rows * wide_of(dim) * 2 * planes_of_type(dt)); }
@@ -567,15 +567,10 @@ using namespace no;
 extern "C" size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_in, int32_t d_out) {
     if ((dt != NO_F32 && dt != NO_BF16) || n_rows_cap < 0 || d_in < 1 || d_out < 1 || d_in > NO_MAX_LINEAR_DIM || d_out > NO_MAX_LINEAR_DIM || n_rows_cap > NO_MAX_LINEAR_ROWS) return 0;
     const int pieces = planes_of_type(dt);
-    const int64_t n = n_rows_cap;
-    size_t parts = linear_parts_bytes(linear_plan_fwd(n, d_out, d_in, pieces), n, d_out);
-    const size_t px = linear_parts_bytes(linear_plan(n, d_in, d_out, pieces), n, d_in), pw = linear_parts_bytes(linear_plan(d_in, d_out, n, pieces), d_in, d_out);
-    if (px > parts) parts = px;
-    if (pw > parts) parts = pw;
-    if (n <= LINEAR_FEW) {
-        const size_t few = (size_t)linear_few_splits(d_in, d_out, n, dt == NO_F32 ? 4 : 2) * n * wide_of(d_out) * 4;
-        if (few > parts) parts = few;
-    }
+    const int64_t n = n_rows_cap, least = n < LINEAR_FEW ? n : LINEAR_FEW;
+    size_t parts = (size_t)linear_few_splits(d_in, d_out, least, dt == NO_F32 ? 4 : 2) * least * wide_of(d_out) * 4;        // (a call may have fewer rows than it is asked for)
+    for (const size_t room : {linear_parts_room(n, d_out, d_in, pieces), linear_parts_room(n, d_in, d_out, pieces), linear_parts_room(d_in, d_out, n, pieces)})
+        if (room > parts) parts = room;
     return 256 + operand_bytes(dt, n, d_in) + operand_bytes(dt, d_in, d_out) + operand_bytes(dt, n, d_out) + round_256((size_t)gz_blocks(n) * d_out * 4) + round_256(parts);
 }
 

@@ -1,0 +1,94 @@
+"""Which tiles and how many parts the library plans for its products, and the workspaces that those need, on the host.
+
+The products of the dense layer: forward [n, d_out] over d_in, input gradient [n, d_in] over d_out, weight gradient [d_in, d_out] over n; of an update: the smaller side's symmetric product over the longer side,
+its square, and the product with the matrix."""
+import ctypes as C
+import math
+import os
+import random
+import shutil
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+HIPCC = os.environ.get("HIPCC") or shutil.which("hipcc", path="/opt/rocm/bin") or shutil.which("hipcc")
+F32, BF16 = 0, 1
+LINEAR_PARTS, UPDATE_PARTS, FEW = 128 << 20, 64 << 20, 8
+
+
+@pytest.fixture(scope="session")
+def plan(tmp_path_factory):
+    """plan(M, N, K, pieces, matrices, half, parts_most, elsewhere) -> (kind, parts)"""
+    if not HIPCC:
+        pytest.skip("no hipcc here")
+    from paper_2311_13225_amd import build
+    path = str(tmp_path_factory.mktemp("plan") / "plan.so")
+    subprocess.run([HIPCC] + build.FLAGS + ["-w", "-shared", os.path.join(HERE, "products_plan.hip"), "-o", path], check=True)
+    f = C.CDLL(path).products_plan
+    f.argtypes = [C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int64, C.c_int32, C.c_uint64, C.c_double, C.POINTER(C.c_int32)]
+    out = (C.c_int32 * 2)()
+
+    def ask(m, n, k, pieces, matrices=1, half=False, parts_most=0, elsewhere=0.0):
+        f(m, n, k, pieces, matrices, half, parts_most, elsewhere, out)
+        return out[0], out[1]
+    return ask
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2311_13225_amd import binding as b
+    if not os.path.exists(b.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    return b.lib()
+
+
+def up(v, to):
+    return -(-v // to) * to
+
+
+def linear_plans(plan, dt, n, d_in, d_out):
+    """Per product of a dense layer: (name, kind, parts, bytes of parts)"""
+    pieces = 3 if dt == F32 else 1
+    layout = max(0.0, n * d_in * 10 / 8e6 - 5) if dt == F32 and d_in >= 32 else 0.0        # (other tiles than the large ones take fp32 rows behind a launch that lays them out)
+    for name, m, c, k, elsewhere in (("fwd", n, d_out, d_in, layout), ("grad_x", n, d_in, d_out, 0.0), ("grad_w", d_in, d_out, n, 0.0)):
+        kind, parts = plan(m, c, k, pieces, parts_most=LINEAR_PARTS, elsewhere=elsewhere)
+        yield name, kind, parts, parts * m * up(c, 8) * 4 if parts > 1 else 0
+
+
+def few_parts(dt, n, d_in, d_out):
+    size, splits = 4 if dt == F32 else 2, 1
+    while splits < 32 and splits * 2 <= max(1, d_in // 128) and d_in * min(d_out, 128 // size) * size > splits * (128 << 10):
+        splits *= 2
+    return (1 if splits == 2 and n < 4 else splits) * n * up(d_out, 8) * 4
+
+
+def linear_bytes(plan, dt, n, d_in, d_out):
+    """What the calls take of their workspace, at most."""
+    operand = lambda rows, dim: up(rows * up(dim, 8) * 2 * (3 if dt == F32 else 1), 256)  # noqa: E731
+    parts = max(p[3] for p in linear_plans(plan, dt, n, d_in, d_out))
+    if n <= FEW:
+        parts = max(parts, few_parts(dt, n, d_in, d_out))
+    return operand(n, d_in) + operand(d_in, d_out) + operand(n, d_out) + up(max(1, min(512, -(-n // 64))) * d_out * 4, 256) + parts
+
+
+def log_int(rng, lo, hi):
+    return max(lo, min(hi, round(math.exp(rng.uniform(math.log(max(lo, 1)), math.log(hi))))))
+
+
+def smaller(rng, sizes):
+    """The sizes with one or all of them made smaller."""
+    which = rng.randrange(len(sizes) + 1)
+    return tuple(max(1, int(v * rng.uniform(0.3, 1.0))) if which in (i, len(sizes)) else v for i, v in enumerate(sizes))
+
+
+@pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
+def test_linear_workspaces_grow_with_every_size(lib, plan, dt):
+    rng, size = random.Random(1), lambda s: lib.no_linear_ws_bytes(dt, *s)  # noqa: E731
+    for _ in range(6000):
+        sizes = tuple(log_int(rng, 1, hi) for hi in rng.choice(((64, 9000, 9000), (60_000, 9000, 9000), (60_000, 600, 600))))
+        less = smaller(rng, sizes)
+        assert size(less) <= size(sizes), (less, sizes)
+        assert size(less) >= linear_bytes(plan, dt, *less), less
+    assert size((8, 256, 256)) <= size((9, 256, 256)) and size((2276, 2048, 8192)) <= size((2504, 2048, 8192)) and size((0, 64, 64)) <= size((1, 64, 64))
