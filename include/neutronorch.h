@@ -433,7 +433,7 @@ int32_t no_linear_bwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, cons
  * matrix of zeros stays one), then `steps` times (1 to 100; 5 is usual) X <- a X + (b G + c G G) X with G = X X^T where rows <= cols, else X <- a X + X (b G + c G G) with G = X^T X, and
  * (a, b, c) = (3.4445, -4.7750, 2.0315): a singular value s goes to a s + b s^3 + c s^5 each time, and d_out takes the last X, of type dt_out. Products are of values held to 22 bits, summed in fp32.
  * dt, dt_out: NO_F32 or NO_BF16. Matrices lie x_matrix_bytes apart (not read for a single one), rows x_stride_bytes. d_out may be d_x itself (same type, address and strides). A matrix with an infinity or
- * NaN gives NaN throughout; others beside it are not touched by that. */
+ * NaN gives NaN throughout; others beside it are not touched by that. The workspace of one call holds for all whose sizes are no larger. */
 size_t no_orthogonalise_ws_bytes(int32_t n_matrices, int32_t rows, int32_t cols);
 int32_t no_orthogonalise(const void* d_x, no_dtype dt, int64_t x_stride_bytes, int64_t x_matrix_bytes, int32_t n_matrices, int32_t rows, int32_t cols, int32_t steps,
                          void* d_out, no_dtype dt_out, int64_t out_stride_bytes, int64_t out_matrix_bytes, void* d_ws, size_t ws_bytes, void* stream);

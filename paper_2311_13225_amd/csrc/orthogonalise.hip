@@ -248,7 +248,7 @@ static NsRoom ns_room(char* ws, int64_t matrices, int64_t rows, int64_t cols) {
     r.poly = ns_matrix(p, matrices, side, side);
     r.plan = dense_plan(side, side, rows < cols ? cols : rows, 2, matrices < 1 ? 1 : matrices, true, NS_PARTS_MOST);
     r.parts = (float*)p;
-    if (r.plan.splits > 1) p += round_256((size_t)r.plan.splits * matrices * side * wide_of(side) * 4);
+    p += round_256(dense_parts_room(side, side, rows < cols ? cols : rows, 2, matrices, NS_PARTS_MOST));       // (for matrices of smaller sides, too)
     r.bytes = (size_t)(p - ws);
     return r;
 }

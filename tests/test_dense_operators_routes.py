@@ -26,3 +26,17 @@ def test_linear_in_a_workspace_of_larger_sizes(most, fewer, dt):
         made.append((y.t, gx.t, gw.t, gb))
     for a, c in zip(*made):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("most,fewer", [((1, 256, 3900), (1, 256, 3300)), ((4, 100, 2600), (3, 96, 2500)), ((7, 3608, 63), (7, 3496, 63))])
+@BOTH
+def test_updates_in_a_workspace_of_larger_sizes(most, fewer, dt):
+    b, g = nb(), rng(fewer[1])
+    x, made = randn(fewer, g, dt, 0.01), []
+    for sizes in (most, fewer):
+        size = b.no_orthogonalise_ws_bytes(*sizes)
+        ws = ws_of(size + 4096)
+        ws[size:] = 0x5A
+        made.append(b.no_orthogonalise(x, torch.empty(fewer, device="cuda"), ws[:size]))
+        assert (ws[size:] == 0x5A).all()
+    assert torch.equal(*made)

@@ -92,3 +92,28 @@ def test_linear_workspaces_grow_with_every_size(lib, plan, dt):
         assert size(less) <= size(sizes), (less, sizes)
         assert size(less) >= linear_bytes(plan, dt, *less), less
     assert size((8, 256, 256)) <= size((9, 256, 256)) and size((2276, 2048, 8192)) <= size((2504, 2048, 8192)) and size((0, 64, 64)) <= size((1, 64, 64))
+
+
+def update_plans(plan, n, rows, cols):
+    """Per product of an update: (name, kind, parts, bytes of parts)"""
+    side, longer = min(rows, cols), max(rows, cols)
+    kind, parts = plan(side, side, longer, 2, n, True, UPDATE_PARTS)
+    yield "gram", kind, parts, parts * n * side * up(side, 8) * 4 if parts > 1 else 0
+    yield ("square",) + plan(side, side, side, 2, n, True) + (0,)
+    yield ("with_x",) + plan(rows, cols, side, 2, n) + (0,)
+
+
+def update_bytes(plan, n, rows, cols):
+    pieces = lambda r, c: up(n * r * up(c, 8) * 4, 256)  # noqa: E731
+    side = min(rows, cols)
+    return n * 1024 * 8 + 2 * pieces(rows, cols) + 2 * pieces(side, side) + max(p[3] for p in update_plans(plan, n, rows, cols))
+
+
+def test_update_workspaces_grow_with_every_size(lib, plan):
+    rng, size = random.Random(2), lambda s: lib.no_orthogonalise_ws_bytes(*s)  # noqa: E731
+    for _ in range(6000):
+        sizes = tuple(log_int(rng, 1, hi) for hi in rng.choice(((8, 5000, 5000), (300, 300, 300), (2, 300, 5000))))
+        less = smaller(rng, sizes)
+        assert size(less) <= size(sizes), (less, sizes)
+        assert size(less) >= update_bytes(plan, *less), less
+    assert size((7, 3496, 63)) <= size((7, 3608, 63)) and size((0, 9, 9)) <= size((1, 9, 9))
