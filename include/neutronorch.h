@@ -281,7 +281,7 @@ int32_t no_gcn_layer_bwd(const no_block_view* blk, no_arch form, int32_t d_in, c
  * n_rows_cap; rows from n on are neither read nor written, and with n_rows_cap == 0 the row arrays may be NULL. Sums, norms and softmax statistics are
  * fp32 or wider, results are rounded once, to nearest even. Reductions run in a fixed order. Offsets are 64 bits wide. A call that
  * takes a workspace may write all of it and leaves nothing there that has to survive; calls that overlap in time need one each. Workspaces are
- * 16-byte aligned. The ..._ws_bytes functions give 0 for sizes that the call refuses. Errors: NO_ERR_INVALID_ARG (NULL, sizes, strides,
+ * 16-byte aligned. The ..._ws_bytes functions give 0 for sizes that the call refuses, and grow with every size: a workspace holds for all calls whose sizes are no larger. Errors: NO_ERR_INVALID_ARG (NULL, sizes, strides,
  * alignment, types), NO_ERR_CAPACITY (workspace too small), NO_ERR_UNSUPPORTED (a width beyond the limits below), NO_ERR_HIP.
  * ---------------------------------------------------------------------------------------- */
 
@@ -415,7 +415,7 @@ typedef enum { NO_ACT_NONE = 0, NO_ACT_RELU = 1, NO_ACT_GELU = 2, NO_ACT_SILU = 
  * the call reads, but d_y may be d_residual itself (same address and stride). bf16 operands are multiplied as they are and summed in fp32. fp32 operands are multiplied in three bf16 pieces
  * each (the six largest of nine products, summed in fp32), no less exact than in fp32; there an operand that is infinite, NaN or above 3.38e38 makes the sums that it meets infinite or NaN, and one below 2^-110 is taken
  * with fewer digits. Up to 8 rows are multiplied in fp32.
- * One workspace size holds for the forward and the backward call, and for all calls whose sizes are no larger: no_linear_ws_bytes grows with each of them. */
+ * One workspace size holds for the forward and the backward call. */
 size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_in, int32_t d_out);
 int32_t no_linear_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_w, int64_t w_stride_bytes, const float* d_bias, no_act act,
                       const void* d_residual, int64_t residual_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t d_in, int32_t d_out,
@@ -433,7 +433,7 @@ int32_t no_linear_bwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, cons
  * matrix of zeros stays one), then `steps` times (1 to 100; 5 is usual) X <- a X + (b G + c G G) X with G = X X^T where rows <= cols, else X <- a X + X (b G + c G G) with G = X^T X, and
  * (a, b, c) = (3.4445, -4.7750, 2.0315): a singular value s goes to a s + b s^3 + c s^5 each time, and d_out takes the last X, of type dt_out. Products are of values held to 22 bits, summed in fp32.
  * dt, dt_out: NO_F32 or NO_BF16. Matrices lie x_matrix_bytes apart (not read for a single one), rows x_stride_bytes. d_out may be d_x itself (same type, address and strides). A matrix with an infinity or
- * NaN gives NaN throughout; others beside it are not touched by that. The workspace of one call holds for all whose sizes are no larger. */
+ * NaN gives NaN throughout; others beside it are not touched by that. */
 size_t no_orthogonalise_ws_bytes(int32_t n_matrices, int32_t rows, int32_t cols);
 int32_t no_orthogonalise(const void* d_x, no_dtype dt, int64_t x_stride_bytes, int64_t x_matrix_bytes, int32_t n_matrices, int32_t rows, int32_t cols, int32_t steps,
                          void* d_out, no_dtype dt_out, int64_t out_stride_bytes, int64_t out_matrix_bytes, void* d_ws, size_t ws_bytes, void* stream);

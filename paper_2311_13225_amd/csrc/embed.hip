@@ -70,6 +70,9 @@ constexpr int32_t EMBED_RANK_MOST = 4096;
 // More than these go through the radix sort (131072 of 64 columns: 66 us by tiles, 76 by radix; 200000: 129 and 95).
 constexpr int32_t EMBED_MERGE_MOST = 131072;
 
+// Chunks shorter than 64 are taken while 64 and so on down to twice their length leave fewer than 1024 wavefronts' work, n * (512 columns' worth of wavefronts) / (2 chunk) < 1025: their parts are these values at most, and a row.
+constexpr int64_t EMBED_SHORT_PARTS = 2050 * 512;
+
 struct EmbedPlan {      // the workspace, cut up
     int64_t n, tiles, chunks;
     int32_t chunk;
@@ -93,6 +96,14 @@ struct EmbedPlan {      // the workspace, cut up
         sort_ws = rank + (merged ? list : 0);
         parts = sort_ws + (radix ? (size_t)ceil_div((int64_t)radix_ws_bytes(n), 16) * 16 : 0);
         total = embed_few(n_, dim) ? 16 : parts + (size_t)chunks * 2 * (size_t)dim * 4 + 16;
+    }
+    // Room for any plan of these sizes or smaller ones (a plan's own needs do not grow with them): a program makes one workspace for its longest list.
+    size_t room(int32_t dim) const {
+        if (embed_few((int32_t)n, dim)) return 16;
+        const size_t list = (size_t)tiles * EMBED_TILE * 4, ranks = n <= EMBED_RANK_MOST ? 0 : n <= EMBED_MERGE_MOST ? list : (size_t)EMBED_MERGE_MOST * 4;
+        const size_t sort = radix ? (size_t)ceil_div((int64_t)RadixPlan(n).room_words() * 4, 16) * 16 : 0;
+        const int64_t least = ceil_div(n, 64) * dim, most = ceil_div(n, 8) * dim, brief = most < EMBED_SHORT_PARTS + dim ? most : EMBED_SHORT_PARTS + dim;
+        return list * (n <= EMBED_RANK_MOST ? 2 : 4) + (ranks > sort ? ranks : sort) + (size_t)(least > brief ? least : brief) * 8 + 16;
     }
 };
 
@@ -568,7 +579,7 @@ extern "C" int32_t no_embed_fwd(const void* d_table, no_dtype dt, int64_t n_rows
 
 extern "C" size_t no_embed_ws_bytes(int32_t n_ids_cap, int32_t dim) {
     if (n_ids_cap < 0 || dim < 1 || dim > NO_MAX_EMBED_DIM) return 0;
-    return EmbedPlan(n_ids_cap, dim).total;
+    return EmbedPlan(n_ids_cap, dim).room(dim);
 }
 
 extern "C" int32_t no_embed_bwd(const void* d_grad_out, no_dtype dt, int64_t grad_stride_bytes, const int32_t* d_ids, const int32_t* d_n_ids,

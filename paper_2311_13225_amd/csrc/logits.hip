@@ -764,6 +764,12 @@ static int32_t distill(const char* who, const void* z, no_dtype dt, int64_t stri
     return dt == NO_F32 ? distill<float>(who, a, ws, st) : distill<bf16_t>(who, a, ws, st);
 }
 
+// Pieces of these rows, or of any that are fewer or shorter (whose pieces may be more: they are made shorter until there are 1024 blocks for them, so that short ones are fewer than 2048).
+static int64_t pieces_room(int32_t n, int32_t classes) {
+    const int64_t longest = (int64_t)n * ceil_div(classes, 256 * 4 * 8), shortest = (int64_t)n * ceil_div(classes, 256 * 4), brief = shortest < 2048 ? shortest : 2048;
+    return longest > brief ? longest : brief;
+}
+static size_t parts_room(int32_t n, int32_t classes) { return ((size_t)pieces_room(n, classes) * sizeof(Sums) + 15) / 16 * 16; }
 static size_t parts_bytes(int32_t n, int32_t classes) { return ((size_t)n * (size_t)most_pieces(n, classes) * sizeof(Sums) + 15) / 16 * 16; }
 
 template <typename T>
@@ -833,7 +839,7 @@ using namespace no;
 
 extern "C" size_t no_distill_ws_bytes(int32_t n_rows_cap, int32_t n_classes) {
     if (n_rows_cap < 0 || n_classes < 1 || n_classes > NO_MAX_CLASSES) return 0;
-    return 16 + parts_bytes(n_rows_cap, n_classes);
+    return 16 + parts_room(n_rows_cap, n_classes);
 }
 
 extern "C" int32_t no_distill_fwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,
@@ -879,7 +885,7 @@ extern "C" int32_t no_distill_fwd_bwd(const void* d_z, no_dtype dt, int64_t z_st
 
 extern "C" size_t no_logprobs_ws_bytes(int32_t n_rows_cap, int32_t n_classes, int32_t k) {
     if (n_rows_cap < 0 || n_classes < 1 || n_classes > NO_MAX_CLASSES || k < 0 || k > NO_MAX_ALTERNATIVES) return 0;
-    return 16 + parts_bytes(n_rows_cap, n_classes) + (size_t)n_rows_cap * (size_t)most_pieces(n_rows_cap, n_classes) * (size_t)k * 8;
+    return 16 + parts_room(n_rows_cap, n_classes) + (size_t)pieces_room(n_rows_cap, n_classes) * (size_t)k * 8;
 }
 
 extern "C" int32_t no_logprobs_fwd(const void* d_z, no_dtype dt, int64_t z_stride_bytes, const int32_t* d_n_rows, int32_t n_rows_cap, int32_t n_classes,

@@ -36,6 +36,7 @@ struct RadixPlan {      // how n pairs are cut up; the scratch of one pass (any 
         n_chunks = ceil_div(n_tiles, tiles_per_chunk);
     }
     size_t ws_words() const { return (size_t)(n_tiles + n_chunks + 1) * RS_RADIX; }
+    size_t room_words() const { return (size_t)(n_tiles + (n_tiles < RS_MAX_CHUNKS ? n_tiles : RS_MAX_CHUNKS) + 1) * RS_RADIX; }      // for n pairs or fewer
     uint32_t* tile_excl(void* ws) const { return (uint32_t*)ws; }                                     // [n_tiles][RS_RADIX]
     uint32_t* chunk(void* ws) const { return (uint32_t*)ws + n_tiles * RS_RADIX; }                    // [n_chunks][RS_RADIX]
     uint32_t* totals(void* ws) const { return (uint32_t*)ws + (n_tiles + n_chunks) * RS_RADIX; }      // [RS_RADIX]
