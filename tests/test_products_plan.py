@@ -117,3 +117,82 @@ def test_update_workspaces_grow_with_every_size(lib, plan):
         assert size(less) <= size(sizes), (less, sizes)
         assert size(less) >= update_bytes(plan, *less), less
     assert size((7, 3496, 63)) <= size((7, 3608, 63)) and size((0, 9, 9)) <= size((1, 9, 9))
+
+
+# ------------------------------------------------------------------------------------------------------- what the tests on the GPU take
+
+KINDS = ((256, 256), (192, 192), (128, 128), (128, 128), (64, 64), (64, 64), (64, 64), (32, 32))        # tiles; the first is 256 x 128 of three pieces
+STEPS = 5           # of a reduction: enough for every copy in LDS to be filled again
+
+
+def tiles(kind, pieces):
+    return (256, 128) if kind == 0 and pieces == 3 else KINDS[kind]
+
+
+def linear_routes(plan, dt, n, d_in, d_out):
+    """(product, kind, split) -> whether its tiles are whole"""
+    pieces, step = (3, 32) if dt == F32 else (1, 64)
+    shapes = {"fwd": (n, d_out, d_in), "grad_x": (n, d_in, d_out), "grad_w": (d_in, d_out, n)}
+    for name, kind, parts, _ in linear_plans(plan, dt, n, d_in, d_out):
+        m, c, k = shapes[name]
+        if k > step * (STEPS - 1) and not (name == "fwd" and n <= FEW):
+            bm, bn = tiles(kind, pieces)
+            yield (dt, name, kind, parts > 1), m % bm == 0 and c % bn == 0
+
+
+def update_routes(plan, n, rows, cols):
+    side, longer, tall = min(rows, cols), max(rows, cols), rows > cols
+    shapes = {"gram": (side, side, longer), "square": (side, side, side), "with_x": (rows, cols, side)}
+    for name, kind, parts, _ in update_plans(plan, n, rows, cols):
+        m, c, k = shapes[name]
+        if k > 32 * (STEPS - 1):
+            bm, bn = tiles(kind, 2)
+            yield (name, tall and name != "square", kind, parts > 1), m % bm == 0 and c % bn == 0
+
+
+def on_the_gpu(plan):
+    from . import test_dense_operators_routes as r
+    seen = {}
+    for dt, sizes in ((F32, r.LINEAR_F32 + r.LARGE_F32), (BF16, r.LINEAR_BF16 + r.LARGE_BF16)):
+        for s in sizes:
+            for route, whole in linear_routes(plan, dt, *s):
+                seen.setdefault(route, set()).add(whole)
+    for s in r.UPDATES + r.LARGE_UPDATES:
+        for route, whole in update_routes(plan, *s):
+            seen.setdefault(route, set()).add(whole)
+    return seen
+
+
+def test_every_route_is_tested_on_the_gpu(plan):
+    """Sizes drawn over what the operators are measured at lead to no kind of tile, in no product, that the tests leave out, neither whole nor ragged."""
+    seen, rng, asked = on_the_gpu(plan), random.Random(4), set()
+
+    def side(lo, hi):
+        v, to = log_int(rng, lo, hi), rng.choice((1, 8, 64, 128, 192, 256))
+        return max(lo, v // to * to)
+    for _ in range(8000):
+        for dt in (F32, BF16):
+            n, d_in, d_out = side(1, 60_000), side(16, 9000), side(16, 9000)
+            if n * d_in * d_out <= 3e11:
+                asked.update(linear_routes(plan, dt, n, d_in, d_out))
+        n, rows, cols = log_int(rng, 1, 8), side(16, 4100), side(16, 4100)
+        if n * rows * cols * min(rows, cols) <= 1.4e11:
+            asked.update(update_routes(plan, n, rows, cols))
+    missing = sorted(str((route, "whole" if whole else "ragged")) for route, whole in asked if whole not in seen.get(route, ()))
+    assert len(asked) > 200 and not missing, (len(missing), missing)
+
+
+def test_the_cases_that_are_measured_take_tested_routes(plan):
+    from perf import more_operators
+    seen = on_the_gpu(plan)
+    for case in more_operators.listed():
+        kind = case["kind"]
+        if kind.startswith("linear"):
+            routes = linear_routes(plan, F32 if case["x"] == "f32" else BF16, case["n"], case["d_in"], case["d_out"])
+            routes = [r for r in routes if (r[0][1] == "fwd") == (kind == "linear_fwd")]
+        elif kind in ("muon", "orthogonalise"):
+            routes = update_routes(plan, case["matrices"], case["rows"], case["cols"])
+        else:
+            continue
+        for route, whole in routes:
+            assert whole in seen.get(route, ()), (case["name"], route, whole)
