@@ -190,3 +190,72 @@ def test_updates_in_a_workspace_of_larger_sizes(most, fewer, dt):
         made.append(b.no_orthogonalise(x, torch.empty(fewer, device="cuda"), ws[:size]))
         assert (ws[size:] == 0x5A).all()
     assert torch.equal(*made)
+
+
+# ------------------------------------------------------------------------------------------------------- far rows, long sides
+
+FAR = (1 << 22) + 64            # bytes between rows above what a tile's 31-bit offsets take
+
+
+@pytest.mark.parametrize("n,d_in,d_out", [(1, 100, 264), (5, 256, 64), (300, 256, 320), (300, 130, 70)])
+@BOTH
+def test_linear_with_rows_far_apart(n, d_in, d_out, dt):
+    """Rows (and rows of the matrix) more than 4 MB apart are laid out first."""
+    b, g = nb(), rng(n)
+    pitch = FAR // (2 if dt == BF16 else 4)
+
+    def far(rows, cols, like=None):
+        m = torch.empty((rows * pitch,), device="cuda", dtype=dt).view(rows, pitch)[:, :cols + 1]
+        m[:, cols] = 77.0                   # behind each row
+        if like is not None:
+            m[:, :cols] = like
+        return m[:, :cols], m[:, cols]
+    x, w, gy = randn((n, d_in), g, dt), randn((d_in, d_out), g, dt), randn((n, d_out), g, dt)
+    ws, bias = ws_of(b.no_linear_ws_bytes(dt, n, d_in, d_out)), torch.zeros((d_out,), device="cuda")
+    made = []
+    for place in (lambda r, c, like=None: (torch.empty((r, c), device="cuda", dtype=dt) if like is None else like, None), far):
+        (xx, _), (ww, _), (gg, _) = place(n, d_in, x), place(d_in, d_out, w), place(n, d_out, gy)
+        outs = place(n, d_out), place(n, d_out), place(n, d_in), place(d_in, d_out)
+        y, z, gx, gw = (o[0] for o in outs)
+        gb = torch.empty_like(bias)
+        b.no_linear_fwd(xx, ww, bias, b.NO_ACT_SILU, y, ws, residual=gg, z=z)
+        b.no_linear_bwd(xx, ww, b.NO_ACT_SILU, z, gg, gx, gw, gb, ws)
+        assert all(o[1] is None or (o[1] == 77.0).all() for o in outs)
+        made.append([o.clone() for o in (y, z, gx, gw, gb)])
+        ref, tol = product(x.double(), w.double())
+        close_rounded(z, ref, tol, dt, "z")
+        ref = act_ref(ref, "silu") + gy.double()
+        close_rounded(y, ref, 1.2 * tol + 8 * U * ref.abs() + 2 * U * gy.double().abs(), dt, "y")
+    for a, c in zip(*made):                 # (the same products on copies of the same values; few rows may be read as they are, in another order)
+        if n > 8:
+            assert torch.equal(a, c)
+
+
+def test_linear_rows_far_apart_in_large_tiles():
+    """fp32 rows whose tile's offsets would leave 31 bits are not cut inside the product."""
+    b, g, n, d_in, d_out = nb(), rng(3), 4096, 256, 4096
+    pitch = FAR // 4
+    assert n * pitch * 4 < 20 << 30
+    x = torch.empty((n * pitch,), device="cuda").view(n, pitch)[:, :d_in]
+    x.copy_(randn((n, d_in), g))
+    w, y, near = randn((d_in, d_out), g), torch.empty((n, d_out), device="cuda"), torch.empty((n, d_out), device="cuda")
+    ws = ws_of(b.no_linear_ws_bytes(F32, n, d_in, d_out))
+    b.no_linear_fwd(x, w, None, b.NO_ACT_NONE, y, ws)
+    b.no_linear_fwd(x.contiguous(), w, None, b.NO_ACT_NONE, near, ws)
+    ref, tol = product(x.double(), w.double())
+    close_rounded(y, ref, tol, F32, "far")
+    close_rounded(near, ref, tol, F32, "near")
+
+
+LONGEST = 1 << 20
+
+
+@pytest.mark.parametrize("n,d_in,d_out", [(1, LONGEST, 3), (3, LONGEST - 1, 40), (3, 40, LONGEST), (20, 9, LONGEST - 5), (300, LONGEST, 16), (300, 64, LONGEST)])
+@BOTH
+def test_linear_of_the_longest_sides(n, d_in, d_out, dt):
+    linear(n, d_in, d_out, dt, "none")
+
+
+@pytest.mark.parametrize("rows,cols", [(32_768, 9), (9, 32_768), (32_768, 130), (130, 32_767), (32_768, 1)])
+def test_updates_of_the_longest_sides(rows, cols):
+    test_updates_by_every_route(1, rows, cols)
