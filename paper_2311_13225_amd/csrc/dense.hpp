@@ -6,7 +6,6 @@
 namespace no {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -100,21 +99,6 @@ struct DenseTile {
         }
     }
 };
-
-template <typename H> __device__ __forceinline__ f32x4 dense_mfma(s16x8 a, s16x8 b, f32x4 c);
-template <> __device__ __forceinline__ f32x4 dense_mfma<__bf16>(s16x8 a, s16x8 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-template <> __device__ __forceinline__ f32x4 dense_mfma<_Float16>(s16x8 a, s16x8 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-template <typename H, int I, int J>
-__device__ __forceinline__ void dense_multiply(f32x4 (&acc)[I][J], const s16x8 (&a)[I], const s16x8 (&b)[J]) {
-#pragma unroll
-    for (int i = 0; i < I; ++i)
-#pragma unroll
-        for (int j = 0; j < J; ++j) acc[i][j] = dense_mfma<H>(b[j], a[i], acc[i][j]);
-}
 
 // A block's place: the tiles of all matrices are dealt to the dies in runs, and walked in bands of eight tile rows, so that a die's blocks share rows and columns in its L2 (four Gram matrices of 512 x 2048, each
 // matrix dealt to all dies: 22.2 us, to two of them 20.5).

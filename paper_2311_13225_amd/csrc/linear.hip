@@ -380,12 +380,7 @@ __global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, con
 
 constexpr size_t LINEAR_PARTS_MOST = (size_t)128 << 20;      // bytes of parts, at most
 
-struct LinearPlan { int kind, splits; };
-
-static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int P, double elsewhere = 0) {
-    const DensePlan p = dense_plan(M, N, K, P, 1, false, LINEAR_PARTS_MOST, elsewhere);
-    return LinearPlan{p.kind, p.splits};
-}
+static DensePlan linear_plan(int64_t M, int64_t N, int64_t K, int P, double elsewhere = 0) { return dense_plan(M, N, K, P, 1, false, LINEAR_PARTS_MOST, elsewhere); }
 // Parts of the reduction: blocks with 128 KB of the matrix each, but where two parts would do so for few rows, whose join costs what it saves. us by 1 / 2 / 4 / 8 / 16 parts: one bf16 row, 8192
 // columns, K = 2048 11.2 / 11.9 / 11.6 / 13.9; 2048 columns, K = 8192 31.6 / 20.7 / 13.6 / 11.7 / 11.5; 4096 x 4096 16.8 / 13.9 / 11.9 / 11.5 / 13.8; eight rows, 8192 columns, K = 2048 29.6 / 24.3 / 31.7;
 // 2048 columns, K = 8192 88 / 54 / 33 / 24 / 32. Half of the columns a block (64 bytes of a row, not 128): 15.1 for 11.2, 33 for 30.
@@ -400,7 +395,7 @@ static int linear_few_splits(int64_t K, int64_t N, int64_t rows, int es) {
 // 40001 x 64 x 250 34 / 38, 70000 x 127 x 130 54 / 70; with the pass and the same kind / cut inside: 24922 x 602 x 256 87 / 63).
 constexpr int32_t LINEAR_RAW_LEAST = 32;
 constexpr int64_t LINEAR_RAW_STRIDE = (int64_t)1 << 22;
-static LinearPlan linear_plan_fwd(int64_t M, int64_t N, int64_t K, int P) {
+static DensePlan linear_plan_fwd(int64_t M, int64_t N, int64_t K, int P) {
     const double pass = P == 3 && K >= LINEAR_RAW_LEAST ? (double)M * K * 10 / 8e6 - 5.0 : 0.0;
     return linear_plan(M, N, K, P, pass > 0 ? pass : 0.0);
 }
@@ -415,7 +410,7 @@ static inline int64_t gz_blocks(int64_t n) {
     return b < 1 ? 1 : b < 512 ? b : 512;
 }
 
-struct LinearRoom { char* p; size_t left; char* take(size_t b) { char* r = p; p += round_256(b); return r; } };
+struct LinearRoom { char* p; char* take(size_t b) { char* r = p; p += round_256(b); return r; } };
 
 // bf16 rows of whole, aligned 16 bytes (and not so far apart that a tile's offsets leave 31 bits).
 template <typename T>
@@ -441,17 +436,17 @@ static void linear_pack(const PackJob& a, const PackJob& b, hipStream_t st) {
 }
 
 template <typename T, bool AL, bool BL>
-static bool linear_product(DenseArgs g, const LinearPlan& p, const LinearEnd& end, float* parts, const BiasJob& bias, hipStream_t st) {
+static bool linear_product(DenseArgs g, const DensePlan& p, const LinearEnd& end, float* parts, const BiasJob& bias, hipStream_t st) {
     constexpr int P = sizeof(T) == 4 ? 3 : 1;
     const typename LinearOut<T>::Args e{p.splits > 1 ? LinearEnd{} : end, p.splits > 1 ? parts : nullptr, (int32_t)wide_of(g.N)};
-    dense_launch<__bf16, P, AL, BL, LinearOut<T>>(g, e, DensePlan{p.kind, p.splits}, 1, st);
+    dense_launch<__bf16, P, AL, BL, LinearOut<T>>(g, e, p, 1, st);
     if (p.splits > 1) linear_join<T>(parts, p.splits, g.M, g.d_M, g.N, end, bias, st);
     return p.splits > 1;        // (the column sums went along)
 }
 
 template <typename T>
 static void linear_fwd(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int32_t d_in, int32_t d_out, const LinearEnd& end, char* ws, hipStream_t st) {
-    LinearRoom room{ws, 0};
+    LinearRoom room{ws};
     if (cap <= LINEAR_FEW && !taken_as_it_is<T>(w, d_out)) {
         const int splits = linear_few_splits(d_in, d_out, cap, sizeof(T));
         float* parts = splits > 1 ? (float*)ws : nullptr;
@@ -471,7 +466,7 @@ static void linear_fwd(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int3
     PackJob jx, jw;
     g.M = cap; g.N = d_out; g.K = d_in;
     g.d_M = d_n;
-    const LinearPlan plan = linear_plan_fwd(cap, d_out, d_in, planes_of_type(TypeOf<T>::code));
+    const DensePlan plan = linear_plan_fwd(cap, d_out, d_in, planes_of_type(TypeOf<T>::code));
     if constexpr (sizeof(T) == 4) {
         if (plan.kind == DENSE_LARGE && d_in >= LINEAR_RAW_LEAST && x.stride <= LINEAR_RAW_STRIDE) {        // rows are read where they are, but for the columns that fill no step
             const int32_t rest = d_in % 32;
@@ -499,7 +494,7 @@ static void linear_fwd(RowsOf x, RowsOf w, const int32_t* d_n, int32_t cap, int3
 template <typename T>
 static void linear_bwd(RowsOf x, RowsOf w, int32_t act, RowsOf z, RowsOf grad_y, const int32_t* d_n, int32_t cap, int32_t d_in, int32_t d_out, RowsOf grad_x, RowsOf grad_w,
                        float* grad_bias, char* ws, hipStream_t st) {
-    LinearRoom room{ws, 0};
+    LinearRoom room{ws};
     const bool products = grad_x.p || grad_w.p;
     const bool as_is = act == NO_ACT_NONE && taken_as_it_is<T>(grad_y, d_out);
     DenseOperand gz{grad_y.p, grad_y.stride, 0, 0, 0};

@@ -140,7 +140,7 @@ struct NsSource {
     NsRows x, momentum;
     float beta;
     int32_t nesterov;
-    // eight values of row r from column c on; STORE: the momentum is this step's already
+    // eight values of row r from column c on; DONE: the momentum is this step's already
     template <bool DONE>
     __device__ __forceinline__ void get(int64_t z, int64_t r, int32_t c, int32_t cols, float (&f)[8]) const {
         Run<T, 8> v;
