@@ -413,8 +413,8 @@ typedef enum { NO_ACT_NONE = 0, NO_ACT_RELU = 1, NO_ACT_GELU = 2, NO_ACT_SILU = 
 /* Dense layer: z = d_x * d_w + d_bias, y = act(z) + d_residual, for rows d_x [n, d_in] and a matrix d_w [d_in, d_out]. dt: type of d_x, d_w, d_residual, d_z and d_y, NO_F32 or NO_BF16;
  * d_bias fp32 [d_out] (NULL: 0). d_z (NULL: not stored) takes z for the backward pass; the activation is taken of the sums before that rounding. d_y and d_z may not overlap what
  * the call reads, but d_y may be d_residual itself (same address and stride). bf16 operands are multiplied as they are and summed in fp32. fp32 operands are multiplied in three bf16 pieces
- * each (the six largest of nine products, summed in fp32), no less exact than in fp32; there an operand that is infinite, NaN or above 3.38e38 makes the sums that it meets infinite or NaN, and one below 2^-110 is taken
- * with fewer digits. Up to 8 rows are multiplied in fp32.
+ * each (the six largest of nine products, summed in fp32), no less exact than in fp32; sums that are not finite so are taken again in fp32, product by product, and a value below 2^-110 is taken with fewer digits. Up to
+ * 8 rows are multiplied in fp32.
  * One workspace size holds for the forward and the backward call. */
 size_t no_linear_ws_bytes(no_dtype dt, int32_t n_rows_cap, int32_t d_in, int32_t d_out);
 int32_t no_linear_fwd(const void* d_x, no_dtype dt, int64_t x_stride_bytes, const void* d_w, int64_t w_stride_bytes, const float* d_bias, no_act act,

@@ -139,6 +139,42 @@ __device__ __forceinline__ bool dense_place(const DenseArgs& g, int& matrix, int
     return true;
 }
 
+// A sum of products of three pieces that is not finite, once more in fp32, one product after the other, from the values that the pieces add up to (RAW: from fp32 rows as they lie): an infinity meets the other operand's
+// pieces, zeros and opposite signs among them, and a piece that is rounded up may leave fp32 where its value does not. The reduction's part is [k0, k1).
+template <bool AL, bool BL, bool RAW>
+struct DenseAgain {
+    static constexpr bool THERE = true;
+    const DenseArgs& g;
+    int32_t k0, k1;
+    template <bool ALONG>
+    __device__ __forceinline__ static float value(const DenseOperand& o, int32_t row, int32_t k) {
+        const char* p = o.p + (ALONG ? row * o.pitch + (int64_t)k * 2 : k * o.pitch + (int64_t)row * 2);
+        float f = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 3; ++q) f += to_f32(*reinterpret_cast<const bf16_t*>(p + (int64_t)q * o.plane));      // (exact, largest first)
+        return f;
+    }
+    __device__ __forceinline__ float operator()(int32_t m, int32_t n) const {
+        constexpr int U = 8;        // products whose factors are asked for at once
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int32_t k = k0; k < k1 && sum == sum; k += U) {       // (a NaN stays one)
+            float a[U], b[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t at = min(k + u, k1 - 1);
+                if constexpr (RAW) a[u] = *reinterpret_cast<const float*>(g.a.p + m * g.a.pitch + (int64_t)at * 4);
+                else a[u] = value<AL>(g.a, m, at);
+                b[u] = value<BL>(g.b, n, at);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) if (k + u < k1) sum = fmaf(a[u], b[u], sum);
+        }
+        return sum;
+    }
+};
+struct DenseOnce { static constexpr bool THERE = false; };      // sums of one piece, or of two
+
 // The sums of a block's tile to the epilogue: through LDS, 32 rows of a wavefront at a time, so that eight consecutive columns of a row meet in a lane and the lanes beside it go on along
 // the row. What the epilogue reads of those rows is asked for at once, before the first of them, and waits in LDS for its row (asked for row by row, 16384 x 8192 x 2048 bf16 with a residual lost 35 us of 250 a
 // tile): E::ahead(epilogue's arguments, matrix, m, n, columns there), then E::put(arguments, matrix, m, n, columns there, sums, what was read, M), which leaves in the sums what it stored; E::MIRROR: that
@@ -149,8 +185,8 @@ struct DenseFinish {
     static constexpr int SUMS = WM * WN * ROWS * PITCH * 4, BYTES = SUMS + (TURNS > 2 ? T * TURNS * AHEAD : 0);
     static_assert(ROWS % PASS == 0, "whole passes");
 };
-template <int BM, int BN, int WM, int WN, typename E, int I, int J>
-__device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename E::Args& e, int matrix, int tm, int tn, int32_t M, f32x4 (&acc)[I][J], char* lds) {
+template <int BM, int BN, int WM, int WN, typename E, int I, int J, typename Again>
+__device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename E::Args& e, int matrix, int tm, int tn, int32_t M, f32x4 (&acc)[I][J], char* lds, const Again& again) {
     typedef DenseFinish<BM, BN, WM, WN> F;
     constexpr int COLS = F::COLS, PITCH = F::PITCH, LANES = F::LANES, ROWS = F::ROWS, RI = ROWS / 16, PASS = F::PASS, TURNS = F::TURNS;
     constexpr bool HELD = TURNS > 2;
@@ -160,6 +196,15 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
     const int32_t nw = tn * BN + wn * COLS, n = nw + l % LANES * 8, here = l % LANES * 8 < COLS ? min(8, g.N - n) : 0;      // (of 16 lanes to 96 columns four have none)
     float* mine = reinterpret_cast<float*>(lds) + wave * ROWS * PITCH;
     Ahead* held = reinterpret_cast<Ahead*>(lds + F::SUMS) + (wave * 64 + l);
+    f32x4 odd = {0.0f, 0.0f, 0.0f, 0.0f};       // NaN from the first sum on that is not finite
+    if constexpr (Again::THERE)
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) odd[w] = fmaf(acc[i][j][w], 0.0f, odd[w]);
+    const bool any_odd = Again::THERE && __any((odd[0] + odd[1]) + (odd[2] + odd[3]) != 0.0f);
 #pragma unroll
     for (int i0 = 0; i0 < I; i0 += RI) {
         const int32_t mw = tm * BM + (wm * I + i0) * 16, mine0 = mw + l / LANES;
@@ -176,6 +221,15 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
 #pragma unroll
             for (int t = 0; t < TURNS; ++t) held[t * F::T] = ahead[t];
         Team<64, F::T>::sync();
+        if constexpr (Again::THERE) {
+            if (__builtin_expect(any_odd, 0))      // (its code out of the way: in line, 24922 x 256 x 256 takes 37.4 us for 35.1, by the fetch of what stands behind it)
+#pragma unroll 1
+                for (int k = 0; k < TURNS * 8; ++k) {
+                    const int t = k >> 3, w = k & 7;
+                    float* at = mine + (l / LANES + t * PASS) * PITCH + l % LANES * 8 + w;
+                    if (mine0 + t * PASS < M && w < here && !(fabsf(*at) < INFINITY)) *at = again(mine0 + t * PASS, n + w);
+                }
+        }
         auto turn = [&](int t, const Ahead& a) {
             const int32_t m = mine0 + t * PASS;
             if (m >= M || here <= 0) return;
@@ -376,7 +430,8 @@ __global__ void __launch_bounds__(64 * WM * WN * GROUPS) dense_kernel(const Dens
         __syncthreads();
         if (group > 0) return;
     }
-    dense_finish<BM, BN, WM, WN, E>(g, e, matrix, tm, tn, M, acc, lds);
+    if constexpr (P == 3) dense_finish<BM, BN, WM, WN, E>(g, e, matrix, tm, tn, M, acc, lds, DenseAgain<AL, BL, false>{g, first * TA::BK, end});
+    else dense_finish<BM, BN, WM, WN, E>(g, e, matrix, tm, tn, M, acc, lds, DenseOnce{});
 }
 
 // The same for large products: a tile of 256 x 256 (192 x 192 where that fills the chip better; three pieces: 256 x 128) by four wavefronts of a quarter each, one a SIMD, whose sums fill the accumulation registers; the others hold one set of
@@ -544,7 +599,8 @@ __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, 
             for (int j = 0; j < J; ++j) acc[i][j] += big[i][j];
     }
     dense_meet<0>();
-    dense_finish<BM, BN, 2, 2, E>(g, e, matrix, tm, tn, M, acc, lds);
+    if constexpr (P == 3) dense_finish<BM, BN, 2, 2, E>(g, e, matrix, tm, tn, M, acc, lds, DenseAgain<AL, BL, false>{g, first * TA::BK, end});
+    else dense_finish<BM, BN, 2, 2, E>(g, e, matrix, tm, tn, M, acc, lds, DenseOnce{});
 }
 
 // Values of fp32 rows cut on their way from LDS: A is the matrix itself, ALONG, at any alignment of a value, and only its last K % 32 columns are a copy (`tail`: 32 columns, zeros at the end), so that
@@ -697,7 +753,7 @@ __global__ void __launch_bounds__(256, 1) dense_raw_kernel(const DenseRawArgs ga
 #pragma unroll
         for (int j = 0; j < J; ++j) acc[i][j] += big[i][j];
     dense_meet<0>();
-    dense_finish<BM, BN, 2, 2, E>(g, e, 0, tm, tn, M, acc, lds);
+    dense_finish<BM, BN, 2, 2, E>(g, e, 0, tm, tn, M, acc, lds, DenseAgain<true, false, true>{g, first * BK, min(K, last * BK)});
 }
 
 // ------------------------------------------------------------------------------------------------------- plans

@@ -179,10 +179,11 @@ static void linear_join(const float* parts, int32_t splits, int32_t M, const int
 // ------------------------------------------------------------------------------------------------------- operands
 //
 // A product takes rows of whole 16 bytes. bf16 rows that are none are copied into rows of a multiple of 8 values, zeros at the end; fp32 rows are cut into three bf16 planes whose sum is
-// the value, x = h + m + l, rounded each time to the nearest (8 bits each, so nothing of the 24 is left over while the pieces are in range).
+// the value, x = h + m + l, rounded each time to the nearest (8 bits each, so nothing of the 24 is left over while the pieces are in range; the first one is held to the largest bf16).
 __device__ __forceinline__ void dense_cut(float x, float& h, float& m, float& l) {
-    h = to_f32(from_f32<bf16_t>(x));
-    const bool fine = fabsf(h) < INFINITY;      // (an infinity or NaN is all in the first piece)
+    constexpr float TOP = 0x1.fep127f;
+    const bool fine = fabsf(x) < INFINITY;      // (an infinity or NaN is all in the first piece)
+    h = to_f32(from_f32<bf16_t>(fine ? __builtin_amdgcn_fmed3f(x, -TOP, TOP) : x));
     m = fine ? to_f32(from_f32<bf16_t>(x - h)) : 0.0f;
     l = fine ? x - h - m : 0.0f;
 }

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from .test_dense_operators import ACTS, act_ref, apart, slope_ref, steps_ref
-from .test_operators import BF16, F32, TINY, U, Rows, close, half, nb, randn, rng, ws_of
+from .test_operators import BF16, F32, INF, NAN, TINY, U, Rows, close, half, nb, randn, rng, ws_of
 
 pytestmark = pytest.mark.gpu
 BOTH = pytest.mark.parametrize("dt", [F32, BF16], ids=["f32", "bf16"])
@@ -259,3 +259,50 @@ def test_linear_of_the_longest_sides(n, d_in, d_out, dt):
 @pytest.mark.parametrize("rows,cols", [(32_768, 9), (9, 32_768), (32_768, 130), (130, 32_767), (32_768, 1)])
 def test_updates_of_the_longest_sides(rows, cols):
     test_updates_by_every_route(1, rows, cols)
+
+
+# ------------------------------------------------------------------------------------------------------- values at the ends of the range
+
+def alike(got, ref, tol, what):
+    """NaN and infinities where the formula has them, the others close."""
+    got = got.double()
+    assert torch.equal(got.isnan(), ref.isnan()), what
+    wide = ref.isinf()
+    assert torch.equal(got[wide], ref[wide]), what
+    fine = ref.isfinite()
+    close(got[fine], ref[fine], tol[fine] + TINY, what)
+
+
+def scale_of(a, c):
+    """Magnitudes of a product of which some factors are no numbers: the others'."""
+    fine = lambda m: torch.where(m.isfinite(), m, 0.0).abs()  # noqa: E731
+    return (16 * U * math.sqrt(a.shape[1] + 64) + 2.0 ** -21) * (fine(a) @ fine(c))
+
+
+@pytest.mark.parametrize("n,d_in,d_out", [(8, 64, 72), (9, 64, 72), (300, 301, 263), (300, 8000, 40), (40, 24, 8000), (10_001, 256, 47), (24_922, 602, 256), (40_001, 64, 250), (2000, 4100, 300), (4096, 24, 4096),
+                                          (2048, 2048, 1100)])
+def test_linear_f32_at_the_ends_of_the_range(n, d_in, d_out):
+    """Infinite operands, and finite ones that round to none of bf16, give what products in fp32 give, whatever the number of rows."""
+    b, g = nb(), rng(n + d_out)
+    x, w, gy = randn((n, d_in), g), randn((d_in, d_out), g), randn((n, d_out), g)
+    x[1, 2], x[2, 5], x[n - 1, d_in - 1], x[4, 1], x[4, d_in // 2] = INF, -INF, INF, INF, INF
+    x[5, 3], x[6, 4] = 3.3999e38, -3.4e38           # above the largest bf16, 3.3895e38
+    w[3], w[4] = w[3] * 1e-3, w[4] * 1e-3
+    w[2, 0], w[5, d_out - 1] = 0.0, 2.0             # (a product of infinity and 0; a value of one piece)
+    gy[1, 2], gy[3, d_out - 1] = -INF, INF
+    gy[5, 6], gy[7, 7] = 3.3999e38, NAN
+    ws = ws_of(b.no_linear_ws_bytes(F32, n, d_in, d_out))
+    y, gx, gw, gb = torch.empty((n, d_out), device="cuda"), torch.empty_like(x), torch.empty_like(w), torch.empty((d_out,), device="cuda")
+    b.no_linear_fwd(x, w, None, b.NO_ACT_NONE, y, ws)
+    ref = x.double() @ w.double()
+    assert ref[5].isfinite().all() and ref[5].abs().max() > 1e34 and ref[2, :d_out - 1].isinf().all() and ref[1, 0].isnan()
+    alike(y, ref, scale_of(x.double(), w.double()), "y")
+    w[:, 6] *= 1e-3
+    x[5] = x[5] * 1e-3                              # (so that what meets the gradient's large value stays in range)
+    b.no_linear_bwd(x, w, b.NO_ACT_NONE, None, gy, gx, gw, gb, ws)
+    ref = gy.double() @ t(w.double())
+    assert ref[5].isfinite().all() and ref[5].abs().max() > 1e34
+    alike(gx, ref, scale_of(gy.double(), t(w.double())), "grad_x")
+    ref = t(x.double()) @ gy.double()
+    ref = torch.where(ref.abs() > 3.4028235e38, ref.sign() * INF, ref)
+    alike(gw, ref, scale_of(t(x.double()), gy.double()), "grad_w")
