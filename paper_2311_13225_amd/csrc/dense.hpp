@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(64 * WM * WN * GROUPS) dense_kernel(const Dens
 // The same for large products: a tile of 256 x 256 (192 x 192 where that fills the chip better; three pieces: 256 x 128) by four wavefronts of a quarter each, one a SIMD, whose sums fill the accumulation registers; the others hold one set of
 // fragments a slab, and a set is read again when the products that want it are done. A copy of LDS is free when its last fragments are in registers: the step after next is requested right then, and
 // has a whole step's time to arrive. LDS is read 16 bytes for 8192 multiplications (by eight wavefronts of 128 x 64: 24 bytes, which takes LDS as long as the products).
-// Bound by the matrix pipes at the clock that the power limit leaves: bf16 16384 x 8192 x 2048 439 us (1.25 PFLOP/s), both products of 8192 x 2048 x 8192's gradients 195 to 200 (1.4 when the card is cold);
+// Bound by the matrix pipes, at work in 56 to 75 % of the cycles, at the 1.9 to 2.15 GHz that the power limit leaves them (kernels below it run at 2.35): bf16 16384 x 8192 x 2048 439 us (1.25 PFLOP/s), both products of 8192 x 2048 x 8192's gradients 195 to 200 (1.4 when the card is cold);
 // two pieces, 4096^3 300 (1.37 PFLOP/s of pieces), its symmetric half 190 by 192 x 192.
 template <typename H, int P, bool AL, bool BL, int BM, int BN, typename E>
 __global__ void __launch_bounds__(256, 1) dense_large_kernel(const DenseArgs g, const typename E::Args e) {

@@ -4,8 +4,10 @@
 namespace no {
 
 // y = (s - mean) rstd weight + bias of s = x + residual, rstd = 1 / sqrt(mean of (s - mean)^2 + eps). A team of lanes holds a row in registers, U runs of 16 bytes a
-// lane, and goes over it three times (sum, squares of the differences, result), so that nothing cancels and memory sees the row once.
-// Bound by memory: 16384 x 4096 bf16 with residual and sum 94 us (537 MB, 5.7 TB/s), 50001 x 602 fp32 into bf16 38 (181 MB, 4.8 TB/s; arithmetic takes 73 % of its cycles), one row of 4096 3.1.
+// lane, and goes over it three times (sum, squares of the differences, result), so that nothing cancels and memory sees the row once, up to 16384 fp32 values and 32768 of bf16 (above 16384 of which 12 to 24 registers are
+// spilled); of wider rows 104 to 448 registers go to scratch.
+// Bound by memory: 16384 x 4096 bf16 with residual and sum 94 us (537 MB, 5.7 TB/s), 50001 x 602 fp32 into bf16 38 (181 MB, 4.8 TB/s; arithmetic takes 73 % of its cycles), 3000 x 16384 fp32 with residual 143 and 3000 x 32768
+// bf16 158 (786 MB, 5.5 and 5.0 TB/s), one row of 1024 3.0 in the kernel. By scratch: 1500 x 32768 fp32 202, 750 x 65536 fp32 428, 1500 x 65536 bf16 212 (786 MB each).
 template <typename T, typename Y, int TEAM, int THREADS, int U>
 __global__ void __launch_bounds__(THREADS) layernorm_fwd_kernel(RowsOf x, RowsOf residual, const float* __restrict__ weight, const float* __restrict__ bias, float eps,
                                                                 const int32_t* d_n, int32_t cap, int32_t dim, RowsOf sum, RowsOf y, float* mean_out, float* rstd_out) {
@@ -103,7 +105,8 @@ __global__ void __launch_bounds__(THREADS) layernorm_fwd_kernel(RowsOf x, RowsOf
 //
 // The gradients of weight and bias are sums over rows for every column: a team adds its rows' terms in registers while it makes their input gradients, a block joins
 // its teams' sums in LDS and stores one row of parts of each, and a second launch adds the blocks' parts in order.
-// Bound by memory: 16384 x 2048 bf16 with grad_sum 59 us (268 MB, 4.6 TB/s) and 3 to 5 for the parts; with the weights in LDS, or read again for every row, slower.
+// Bound by memory: 16384 x 2048 bf16 with grad_sum 59 us (268 MB, 4.6 TB/s) and 3 to 5 for the parts, of fp32 in all 94 (537 MB, 5.7 TB/s), 6000 x 8192 fp32 142 (5.5 TB/s); with the weights in LDS, or read again for every
+// row, slower. Rows of 8193 to 16384 values, whose weights, sums and next row do not fit the registers (89 of fp32 and 42 of bf16 are spilled): 3000 x 16384 fp32 313 (786 MB, 2.5 TB/s), bf16 163 (393 MB).
 
 constexpr int32_t LAYERNORM_PARTS = 512;     // rows of parts, at most
 
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(THREADS) layernorm_bwd_kernel(RowsOf s, const 
     put(db, parts_b);
 }
 
-// Rows too wide for registers: read twice.
+// Rows too wide for registers: an element a lane, read twice, and a third time for the parameters' gradients (1500 x 32768 fp32 323 us, 750 x 65536 377, 3000 x 32768 bf16 484, 1500 x 65536 510, 786 MB each at one reading).
 template <typename T>
 __global__ void __launch_bounds__(1024) layernorm_bwd_wide_kernel(RowsOf s, const float* __restrict__ weight, const float* __restrict__ mean_in, const float* __restrict__ rstd,
                                                                   RowsOf grad_y, RowsOf grad_sum, const int32_t* d_n, int32_t cap, int32_t dim, RowsOf grad_x) {
@@ -405,7 +408,7 @@ extern "C" int32_t no_layernorm_bwd(const void* d_s, no_dtype dt, int64_t s_stri
         else if (units <= 64) NO_NORM_AS(T, 64, 256, 1);                                                                                             \
         else if (units <= 128) NO_NORM_AS(T, 64, 256, 2);                                                                                            \
         else if (units <= 192) NO_NORM_AS(T, 64, 256, 3);                                                                                            \
-        /* (16384 x 2048 bf16 with grad_sum 63.0 us by a block a row, 66.2 by a wavefront, whose sums leave no registers for the next row; fp32 rows of as many bytes 93.7 and 92.6) */ \
+        /* (16384 x 2048 bf16 with grad_sum 63.0 us by a block a row, 66.2 by a wavefront, whose sums leave no registers for the next row; fp32 rows of as many bytes, 16384 x 1024, by a wavefront 48.4) */ \
         else if (units <= 256) NO_NORM_AS(T, (sizeof(T) == 2 ? 256 : 64), 256, (sizeof(T) == 2 ? 1 : 4));                                            \
         else if (units <= 512) NO_NORM_AS(T, 256, 256, 2);                                                                                           \
         else if (units <= 1024) NO_NORM_AS(T, 256, 256, 4);                                                                                          \

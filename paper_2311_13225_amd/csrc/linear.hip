@@ -4,7 +4,8 @@
 namespace no {
 
 // The share of the standard normal distribution below z, and e = exp(-z^2 / 2): with x = |z| / sqrt(2), erfc(x) = e t Q(t), t = 1 / (1 + 0.44 x), Q a polynomial of degree 7 fitted to exp(x^2) erfc(x)
-// (1 + 0.44 x) over [0, 10] with least relative error (1.8e-7; 5e-7 with the roundings of its evaluation). 17 instructions for share and slope together, where erff and expf are 60: the GELU gradient of 8192 x 8192
+// (1 + 0.44 x) over [0, 10] with least relative error (1.8e-7; with the roundings of its evaluation 7e-7 up to |z| = 3, then by the exponent's, 1.4e-6 at 5, 2.2e-6 at 6, 8e-6 at 13, of a share that 1 + erf has lost by then).
+// 17 instructions for share and slope together, where erff and expf are 60: the GELU gradient of 8192 x 8192
 // bf16 was bound by them.
 __device__ __forceinline__ float normal_share(float z, float& e) {
     const float t = __builtin_amdgcn_rcpf(1.0f + 0.44f * 0.70710678f * fabsf(z));
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(256) linear_pack_kernel(PackJob a, PackJob b) 
 // row, each with eight columns, and 256 / LANES rows at a time, whose sums are added in order; four of a thread's rows are requested at once.
 // The launch's other blocks lay out the rows of x and the matrix for the products behind it.
 // Of bf16 values gz is rounded to bf16 (a smooth slope's product by 2^-8 of it at most, relu's and none's not at all): the products then take 16-bit operands, at six times the rate of pieces, and the gradients' error over all
-// is 0.0023 where their own rounding leaves 0.0017. The column sums take it unrounded. Bound by memory: 8192 x 8192 bf16 gelu 75 us (403 MB, 5.4 TB/s).
+// is 0.0023 where their own rounding leaves 0.0017 (two pieces of gz would take both products, 400 us of 8192 x 2048 x 8192's 460, twice). The column sums take it unrounded. Bound by memory: 8192 x 8192 bf16 gelu 75 us (403 MB, 5.4 TB/s).
 template <typename T, int ACT, int LANES>
 __global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z, const int32_t* d_n, int32_t cap, int32_t dim, int32_t per, int32_t wide, int32_t blocks, char* gz,
                                                         int64_t pitch, int32_t plane, float* parts, PackJob a, PackJob b) {
@@ -306,8 +307,8 @@ __global__ void __launch_bounds__(256) linear_gz_kernel(RowsOf grad_y, RowsOf z,
 // ------------------------------------------------------------------------------------------------------- few rows
 //
 // Up to LINEAR_FEW rows of fp32, or with a bf16 matrix that a product cannot take as it is: the matrix would be copied for a single use, so it is read once, in its own order, and multiplied in
-// fp32. A thread has 16 bytes of columns and every 64th row of the block's share of the reduction, for all of the rows at once; rows of x stand in LDS as fp32. (One row, 2048 x 8192 bf16 11.2 us, one launch of
-// tiles of 32 x 32 8.6, eight rows 24 and 8.6; fp32, one row 13.9, eight of 2048 x 2048 13.2, where copy and tiles of nine rows of 8192 x 2048 take 48.)
+// fp32. A thread has 16 bytes of columns and every 64th row of the block's share of the reduction, for all of the rows at once; rows of x stand in LDS as fp32. (One row by a matrix of 2048 x 8192 bf16 that
+// begins 2 bytes off 16: 22.9 us, by tiles of 32 x 32 where it does not 10.1, eight rows 31.6 and 10.2; fp32, one row 15.3, eight of 2048 x 2048 17.6, of 8192 x 2048 24.2, where copy and tiles of nine rows take 50.5.)
 constexpr int LINEAR_FEW = 8, LINEAR_FEW_K = 1024;      // rows; reduction indices in LDS at a time
 
 template <typename T, int MR, bool SHORT>
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(512) linear_few_kernel(RowsOf x, RowsOf w, con
 constexpr size_t LINEAR_PARTS_MOST = (size_t)128 << 20;      // bytes of parts, at most
 
 static DensePlan linear_plan(int64_t M, int64_t N, int64_t K, int P, double elsewhere = 0) { return dense_plan(M, N, K, P, 1, false, LINEAR_PARTS_MOST, elsewhere); }
-// Parts of the reduction: blocks with 128 KB of the matrix each, but where two parts would do so for few rows, whose join costs what it saves. us by 1 / 2 / 4 / 8 / 16 parts: one bf16 row, 8192
+// Parts of the reduction: blocks with 128 KB of the matrix each, but where two parts would do so for few rows, whose join costs what it saves. us by 1 / 2 / 4 / 8 / 16 parts, of matrices that begin on 16 bytes: one bf16 row, 8192
 // columns, K = 2048 11.2 / 11.9 / 11.6 / 13.9; 2048 columns, K = 8192 31.6 / 20.7 / 13.6 / 11.7 / 11.5; 4096 x 4096 16.8 / 13.9 / 11.9 / 11.5 / 13.8; eight rows, 8192 columns, K = 2048 29.6 / 24.3 / 31.7;
 // 2048 columns, K = 8192 88 / 54 / 33 / 24 / 32. Half of the columns a block (64 bytes of a row, not 128): 15.1 for 11.2, 33 for 30.
 static int linear_few_splits(int64_t K, int64_t N, int64_t rows, int es) {
