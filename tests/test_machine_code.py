@@ -12,7 +12,8 @@ OBJDUMP = shutil.which("llvm-objdump", path="/opt/rocm/llvm/bin") or shutil.whic
 MAGIC = b"__CLANG_OFFLOAD_BUNDLE__"
 M0_WAIT = 1         # instructions, or states of an s_nop, between a scalar write of m0 and a load into LDS, whose place m0 gives
 SCALAR_WAIT = 5     # between a vector instruction that writes a scalar register and a memory request that reads it
-MFMA_WAIT = 2       # between a vector instruction's result and a matrix instruction that reads it as an operand
+MFMA_WAIT = 2       # between a vector instruction's result and a matrix instruction that reads it
+SUM_WAIT = 11       # between a matrix instruction of 16 x 16 x 32 and another that reads its sums, but for the next one that adds to them
 
 
 def code_objects(path):
@@ -63,6 +64,11 @@ def registers(operand, kind):
     """Numbers of the vector ('v') or scalar ('s') registers that an operand names."""
     m = re.match(r"%s\[(\d+):(\d+)\]" % kind, operand) or re.match(r"%s(\d+)\b" % kind, operand)
     return set(range(int(m.group(1)), int(m.group(m.lastindex)) + 1)) if m else set()
+
+
+def named(operands):
+    """Vector registers of either kind, by name."""
+    return {kind + str(r) for a in operands for kind in "va" for r in registers(a, kind)}
 
 
 def too_near(out, i, states, writes):
@@ -116,8 +122,25 @@ def test_a_matrix_instruction_waits_for_its_operands(listings):
             if not op.startswith("v_mfma"):
                 continue
             seen += 1
-            used = registers(args[1], "v") | registers(args[2], "v")
-            hit = too_near(out, i, MFMA_WAIT, lambda o, a: o.startswith("v_") and not o.startswith("v_mfma") and a and registers(a[0], "v") & used)
+            used = named(args[1:])
+            hit = too_near(out, i, MFMA_WAIT, lambda o, a: o.startswith("v_") and not o.startswith("v_mfma") and a and named(a[:1]) & used)
             if hit:
                 bad.append((kernel, hit, args))
+    assert seen > 1000 and not bad, (len(bad), bad[:1])
+
+
+def test_sums_are_read_when_they_are_there(listings):
+    seen, bad = 0, []
+    for out in listings:
+        for i, (kernel, op, args) in enumerate(out):
+            if not re.match(r"v_mfma\w*_16x16x32", op):
+                continue
+            seen += 1
+            made, passed = named(args[:1]), 0
+            for _, later, its in out[i + 1:i + 1 + SUM_WAIT]:
+                if passed >= SUM_WAIT or later == "":
+                    break
+                if not later.startswith(("v_mfma", "s_")) and named(its) & made:
+                    bad.append((kernel, args, later, its))
+                passed += int(its[0], 0) + 1 if later == "s_nop" else 1
     assert seen > 1000 and not bad, (len(bad), bad[:1])
