@@ -139,7 +139,7 @@ __device__ __forceinline__ bool dense_place(const DenseArgs& g, int& matrix, int
     return true;
 }
 
-// A sum of products of three pieces that is not finite, once more in fp32, one product after the other, from the values that the pieces add up to (RAW: from fp32 rows as they lie): an infinity meets the other operand's
+// Sums of products of three pieces that are not finite, once more in fp32, one product after the other, from the values that the pieces add up to (RAW: from fp32 rows as they lie): an infinity meets the other operand's
 // pieces, zeros and opposite signs among them, and a piece that is rounded up may leave fp32 where its value does not. The reduction's part is [k0, k1).
 template <bool AL, bool BL, bool RAW>
 struct DenseAgain {
@@ -154,23 +154,60 @@ struct DenseAgain {
         for (int q = 0; q < 3; ++q) f += to_f32(*reinterpret_cast<const bf16_t*>(p + (int64_t)q * o.plane));      // (exact, largest first)
         return f;
     }
-    __device__ __forceinline__ float operator()(int32_t m, int32_t n) const {
-        constexpr int U = 8;        // products whose factors are asked for at once
-        float sum = 0.0f;
+    // The factor of row m at index k of the reduction.
+    __device__ __forceinline__ float left(int32_t m, int32_t k) const {
+        if constexpr (RAW) return *reinterpret_cast<const float*>(g.a.p + m * g.a.pitch + (int64_t)k * 4);
+        else return value<AL>(g.a, m, k);
+    }
+    // Eight columns of row m from n on, `here` of them there: the sums at `at` that are not finite. A NaN stays one: then the rest of the reduction is left out. Columns that lie beside one another in memory are taken at once
+    // (8192 x 2048 x 8192 with NaN in the middle row of W, every sum anew: 47 ms, one by one 100), rows one by one, for their addresses would take the registers that let three blocks share a compute unit.
+    __device__ __forceinline__ void operator()(int32_t m, int32_t n, int32_t here, float* at) const {
+        if constexpr (BL) {
 #pragma unroll 1
-        for (int32_t k = k0; k < k1 && sum == sum; k += U) {       // (a NaN stays one)
-            float a[U], b[U];
+            for (int w = 0; w < here; ++w) {
+                if (fabsf(at[w]) < INFINITY) continue;
+                constexpr int U = 8;        // products whose factors are asked for at once
+                float sum = 0.0f;
+#pragma unroll 1
+                for (int32_t k = k0; k < k1 && sum == sum; k += U) {
+                    float a[U], b[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int32_t at = min(k + u, k1 - 1);
-                if constexpr (RAW) a[u] = *reinterpret_cast<const float*>(g.a.p + m * g.a.pitch + (int64_t)at * 4);
-                else a[u] = value<AL>(g.a, m, at);
-                b[u] = value<BL>(g.b, n, at);
+                    for (int u = 0; u < U; ++u) {
+                        a[u] = left(m, min(k + u, k1 - 1));
+                        b[u] = value<true>(g.b, n + w, min(k + u, k1 - 1));
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) if (k + u < k1) sum = fmaf(a[u], b[u], sum);
+                }
+                at[w] = sum;
+            }
+        } else {
+            bool odd = false;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) odd |= w < here && !(fabsf(at[w]) < INFINITY);
+            float sum[8] = {};
+#pragma unroll 1
+            for (int32_t k = k0; k < k1 && odd; ++k) {
+                const float a = left(m, k);
+                float b[8], f[8];
+                odd = false;
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    Run<bf16_t, 8> r;       // (rows of whole eights)
+                    r.load(reinterpret_cast<const bf16_t*>(g.b.p + k * g.b.pitch + (int64_t)q * g.b.plane) + n);
+                    r.get(f);
+#pragma unroll
+                    for (int w = 0; w < 8; ++w) b[w] = q ? b[w] + f[w] : f[w];
+                }
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    sum[w] = fmaf(a, b[w], sum[w]);
+                    odd |= sum[w] == sum[w];
+                }
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) if (k + u < k1) sum = fmaf(a[u], b[u], sum);
+            for (int w = 0; w < 8; ++w) if (!(fabsf(at[w]) < INFINITY)) at[w] = sum[w];
         }
-        return sum;
     }
 };
 struct DenseOnce { static constexpr bool THERE = false; };      // sums of one piece, or of two
@@ -224,11 +261,8 @@ __device__ __forceinline__ void dense_finish(const DenseArgs& g, const typename 
         if constexpr (Again::THERE) {
             if (__builtin_expect(any_odd, 0))      // (its code out of the way: in line, 24922 x 256 x 256 takes 37.4 us for 35.1, by the fetch of what stands behind it)
 #pragma unroll 1
-                for (int k = 0; k < TURNS * 8; ++k) {
-                    const int t = k >> 3, w = k & 7;
-                    float* at = mine + (l / LANES + t * PASS) * PITCH + l % LANES * 8 + w;
-                    if (mine0 + t * PASS < M && w < here && !(fabsf(*at) < INFINITY)) *at = again(mine0 + t * PASS, n + w);
-                }
+                for (int t = 0; t < TURNS; ++t)
+                    if (mine0 + t * PASS < M && here > 0) again(mine0 + t * PASS, n, here, mine + (l / LANES + t * PASS) * PITCH + l % LANES * 8);
         }
         auto turn = [&](int t, const Ahead& a) {
             const int32_t m = mine0 + t * PASS;
