@@ -25,13 +25,13 @@ LINEAR_BF16 = [(285, 280, 303), (384, 448, 384), (266, 7053, 264), (2040, 261, 1
                (4864, 64, 4224), (128, 2616, 5952), (768, 8064, 576), (16744, 5840, 72), (1351, 8832, 768), (56704, 1280, 128), (4618, 7296, 512),
                (8420, 256, 8352), (9216, 256, 8576), (38976, 192, 4224), (23040, 192, 8048), (34944, 32, 32), (2067, 6971, 8), (8, 2070, 7184),
                (1216, 32, 6688), (64, 8384, 512), (264, 4864, 2304), (256, 4224, 5344), (4224, 6080, 256), (5760, 192, 7968), (192, 7744, 6464),
-               (768, 6024, 2880), (256, 8296, 8832), (16616, 228, 6912), (16640, 256, 7592), (1812, 8225, 2397), (53896, 256, 3072)]
+               (768, 6024, 2880), (256, 8296, 8832), (16616, 228, 6912), (16640, 256, 7592), (1812, 8225, 2397), (53896, 256, 3328)]
 # matrices, rows, columns
 UPDATES = [(1, 130, 136), (1, 192, 192), (1, 196, 196), (1, 240, 224), (1, 1152, 1064), (1, 1408, 1152), (8, 816, 669), (7, 768, 917), (6, 1109, 1096),
            (6, 1152, 1184), (7, 1552, 1584), (8, 1536, 1664), (1, 224, 256), (5, 2267, 129), (8, 1792, 256), (8, 256, 2240), (8, 232, 3328),
            (6, 2560, 320), (8, 256, 3200), (8, 3328, 264), (7, 384, 2304), (7, 328, 3840), (5, 2496, 592), (5, 1536, 768), (8, 3840, 512),
            (4, 2048, 1024), (4, 768, 3840), (1, 2020, 16), (1, 3295, 16), (1, 16, 3356), (1, 3136, 32), (1, 32, 3264), (1, 320, 256), (5, 297, 1064),
-           (7, 710, 835), (5, 3072, 584), (5, 588, 3136), (7, 1028, 1144), (6, 1192, 1152), (8, 1447, 968), (8, 656, 3408), (3, 3198, 1120),
+           (7, 710, 835), (5, 3080, 584), (5, 588, 3136), (7, 1028, 1144), (6, 1192, 1152), (8, 1447, 968), (8, 656, 3408), (3, 3198, 1120),
            (3, 3328, 1152), (7, 768, 3692), (7, 1649, 1548), (6, 1920, 1792)]
 # sizes of real use: a block's two layers, forward and back, a hop's vertices, a narrow layer, updates of large matrices
 LARGE_F32 = [(24_922, 602, 256), (10_001, 256, 47)]
